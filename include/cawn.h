@@ -375,6 +375,113 @@ int cawn_phase_accumulate_fwd_static(const cawn_desc *d, const float *mag, const
 int cawn_stream_copy(const float *in0, const float *in1, float *out0, float *out1, size_t n,
                      void *stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * A second recurrent mixer and what stands around it in a layer: the gated delta rule, the group norm
+ * with an activation behind it, and dropout joined with the residual addition.  The rules at the head of this file hold: device pointers
+ * of the caller, no allocation, no synchronisation, everything enqueued on `stream`.  The workspaces of these calls need no
+ * initialisation and may be shared by calls ordered on one stream.
+ * ------------------------------------------------------------------------------------------------ */
+
+/*
+ * Gated delta rule.  Per batch row b and value head h, with the K x V state S, a = exp(decay[t]), beta[t], and the key and query
+ * of key head h / (H / Hk):
+ *     r    = a S[t-1]
+ *     u    = beta (v - r^T k)            what the state should hold for this key, less what it holds
+ *     S[t] = r + k u^T                   ( = a (I - beta k k^T) S[t-1] + beta k v^T )
+ *     o    = scale S[t]^T q
+ * with k and q replaced by k / sqrt(|k|^2 + norm_eps), q / sqrt(|q|^2 + norm_eps) when qk_norm = 1.
+ */
+typedef struct cawn_delta_desc {
+    int32_t B, L;         /* batch rows; tokens in THIS call (0 allowed: the state is passed through)               */
+    int32_t H, Hk;        /* value heads (v, o, decay, beta, state) and key heads (q, k); Hk divides H; 0 = H        */
+    int32_t K, V;         /* width of a key, 1..128 (beyond: CAWN_EUNSUPPORTED), and of a value                     */
+    int32_t bf16;         /* 0: q, k, v, o and their gradients are fp32; 1: bfloat16.  decay, beta, the state, the
+                             checkpoint and their gradients are fp32 either way, as is all arithmetic                */
+    int32_t qk_norm;      /* 1: q and k are normalised (above)                                                      */
+    float scale;          /* of the output                                                                          */
+    float norm_eps;
+    int64_t qk_stride_b, qk_stride_t;   /* element strides of q, k, dq, dk [B][L][Hk][K]; 0 = dense (t stride Hk*K,  */
+    int64_t v_stride_b, v_stride_t;     /*   b stride L * t stride); of v, dv [B][L][H][V]; of o, do [B][L][H][V].   */
+    int64_t o_stride_b, o_stride_t;     /*   Heads of one token lie side by side                                     */
+} cawn_delta_desc;
+
+/* The state [B][H][K][V] fp32 (its gradient alike).  0 for an invalid descriptor, as the two below. */
+size_t cawn_delta_state_bytes(const cawn_delta_desc *d);
+/* What the forward leaves for the backward: for every run of 64 tokens the state before it, and u of every token. */
+size_t cawn_delta_ckpt_bytes(const cawn_delta_desc *d);
+/* Scratch of either direction, 256-byte aligned. */
+size_t cawn_delta_workspace_bytes(const cawn_delta_desc *d);
+
+/*
+ * Forward: prefill, training, and single tokens (L = 1: one pass over the state).
+ *   q, k [B][L][Hk][K], v [B][L][H][V]; decay, beta [B][L][H] fp32, dense.  decay is the logarithm of the retention; every value
+ *       below -104, minus infinity among them, forgets the state completely (exp underflows there); beta is used as it is
+ *   lengths    device int32 [B] or NULL: row b has lengths[b] tokens (clamped to 0..L).  Of the rest nothing is read; o is 0 there
+ *       and the state is that behind the last token.  0: an unused slot, whose state is passed through
+ *   state_in   or NULL (zeros); state_out or NULL; they may be the same
+ *   ckpt       cawn_delta_ckpt_bytes() or NULL when no backward will follow
+ *   workspace  >= cawn_delta_workspace_bytes(d); calls of up to 16 tokens without ckpt use none
+ * Inputs must not alias outputs (but for the state).
+ */
+int cawn_delta_rule_fwd(const cawn_delta_desc *d, const void *q, const void *k, const void *v, const float *decay, const float *beta,
+                        const int32_t *lengths, const void *state_in, void *o, void *state_out, void *ckpt, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
+/*
+ * Backward.  q .. lengths as the forward had them, ckpt as it wrote it; dO (the gradient of o), dstate_out or NULL (zeros).
+ * dq, dk are summed over the value heads of a key head; ddecay is the gradient of the logarithm.  Gradients of tokens beyond
+ * lengths[b] are 0.  Any of dq, dk, dv, ddecay, dbeta, dstate_in may be NULL.  The same inputs give the same bits.
+ */
+int cawn_delta_rule_bwd(const cawn_delta_desc *d, const void *q, const void *k, const void *v, const float *decay, const float *beta,
+                        const int32_t *lengths, const void *ckpt, const void *dO, const void *dstate_out, void *dq, void *dk,
+                        void *dv, float *ddecay, float *dbeta, void *dstate_in, void *workspace, size_t workspace_bytes,
+                        void *stream);
+
+/*
+ * Group norm with an activation, channels last: x [B][T][C], the C channels in `groups` runs of C / groups.  Per (row, group)
+ *     mean, var over the T x C/groups values;   y = act(weight[c] (x - mean) / sqrt(var + eps) + bias[c])
+ * T = 1 normalises every token's heads by themselves (behind a recurrent mixer); T > 1 whole clips.
+ */
+typedef struct cawn_norm_desc {
+    int32_t B, T, C, groups;            /* groups divides C; B or T may be 0 (nothing is read or written but the gradients of the
+                                           parameters, which are 0 then)                                                          */
+    int32_t bf16;                       /* 1: x, y, dy, dx are bfloat16, else fp32; parameters, statistics and sums are fp32     */
+    int32_t act;                        /* 0 none, 1 SiLU z / (1 + e^-z), 2 GELU z (1 + erf(z / sqrt 2)) / 2                     */
+    float eps;
+    int32_t accumulate_param_grads;     /* backward: 0 overwrite, 1 add into dweight, dbias                                      */
+    int64_t x_stride_b, x_stride_t;     /* element strides of x and dx; 0 = dense; channels lie side by side                     */
+    int64_t y_stride_b, y_stride_t;     /* of y and dy                                                                           */
+} cawn_norm_desc;
+
+size_t cawn_group_norm_workspace_bytes(const cawn_norm_desc *d);
+/* weight, bias [C] fp32 or NULL (1, 0); stats [B][groups][2] (mean, 1 / sqrt(var + eps)) for the backward, or NULL. */
+int cawn_group_norm_fwd(const cawn_norm_desc *d, const void *x, const float *weight, const float *bias, void *y, float *stats,
+                        void *workspace, size_t workspace_bytes, void *stream);
+/* dx, dweight, dbias: any may be NULL.  The sums of dweight and dbias run in a fixed order. */
+int cawn_group_norm_bwd(const cawn_norm_desc *d, const void *x, const float *weight, const float *bias, const float *stats,
+                        const void *dy, void *dx, float *dweight, float *dbias, void *workspace, size_t workspace_bytes,
+                        void *stream);
+
+/*
+ * Dropout joined with the residual addition:  y = residual + keep x / (1 - p), the mask drawn from a counter and never stored.
+ * Element (r, c) of the rows x cols matrix has the number e = r cols + c; it is kept when word e % 4 of Philox-4x32-10 (Salmon et
+ * al., SC 2011) with the 128-bit counter (offset + e / 4, 0), low word first, under the key `seed` is at least floor(p 2^32).
+ * rng: DEVICE, uint64 {seed, offset}: read by the kernel, so that a captured graph may find other values at each replay.  The
+ * backward with the same rng and sizes uses the same mask; a call uses up ceil(rows cols / 4) of the offset.
+ */
+typedef struct cawn_dropout_desc {
+    int64_t rows, cols;
+    int64_t x_stride, residual_stride, y_stride;   /* element strides of rows; 0 = cols.  dx has x's, dy has y's     */
+    double p;                                      /* 0 <= p <= 1; 1 drops everything                              */
+    int32_t bf16;                                  /* x, residual, y, dy, dx: bfloat16 or fp32                     */
+    int32_t reserved;
+} cawn_dropout_desc;
+
+/* residual may be NULL (0).  x, residual may be y (in place, with the same strides).  A dropped element of x is not used, whatever it holds. */
+int cawn_dropout_add_fwd(const cawn_dropout_desc *d, const void *x, const void *residual, const uint64_t *rng, void *y, void *stream);
+/* dx = keep dy / (1 - p); the gradient of the residual is dy itself. */
+int cawn_dropout_add_bwd(const cawn_dropout_desc *d, const void *dy, const uint64_t *rng, void *dx, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -151,6 +151,83 @@ static PyObject *call(PyObject *self, PyObject *const *args, Py_ssize_t n)
     return PyLong_FromLong(r);
 }
 
+/*
+ * call_op(address, form, desc, tensor, ..., stream) for the operators with a descriptor of their own: form = 2 * (the descriptor's
+ * place in what setup_ops was given) + (1 when the last tensor is a workspace, whose size follows it).
+ */
+#define OP(n, PP, VV) case n: r = ws ? ((int (*)(const void *, VV, size_t, void *))fn)(view.buf, PP, bytes, st) \
+                                     : ((int (*)(const void *, VV, void *))fn)(view.buf, PP, st); break;
+#define P3 p[0], p[1], p[2]
+#define V3 void *, void *, void *
+#define P4 P3, p[3]
+#define V4 V3, void *
+#define P6 P4, p[4], p[5]
+#define V6 V4, void *, void *
+#define P9 P6, p[6], p[7], p[8]
+#define V9 V6, void *, void *, void *
+#define P11 P9, p[9], p[10]
+#define V11 V9, void *, void *
+
+static PyObject *op_types;                     /* the operators' descriptor types */
+static const Py_ssize_t op_sizes[] = {sizeof(cawn_delta_desc), sizeof(cawn_norm_desc), sizeof(cawn_dropout_desc)};
+
+static PyObject *call_op(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    (void)self;
+    const Py_ssize_t first = 3, np = n - first - 1;
+    if (np < 1 || np > MAX_P) return PyErr_Format(PyExc_TypeError, "call_op: wrong number of tensors");
+    void *fn = PyLong_AsVoidPtr(args[0]);
+    if (!fn) return PyErr_Occurred() ? NULL : PyErr_Format(PyExc_ValueError, "call_op: no function");
+    const long form = PyLong_AsLong(args[1]);
+    if (form == -1 && PyErr_Occurred()) return NULL;
+    if (!op_types || form < 0 || form / 2 >= (long)(sizeof op_sizes / sizeof op_sizes[0])) return PyErr_Format(PyExc_ValueError, "call_op: no such form");
+    const int ws = form % 2;
+    void *p[MAX_P], *st;
+    for (Py_ssize_t i = 0; i < np; ++i)
+        if (pointer(args[first + i], &p[i]) < 0) return NULL;
+    size_t bytes = 0;
+    if (ws && args[first + np - 1] != Py_None) {
+        PyObject *b = PyObject_GetAttr(args[first + np - 1], s_nbytes);
+        if (!b) return NULL;
+        bytes = PyLong_AsSize_t(b);
+        Py_DECREF(b);
+        if (bytes == (size_t)-1 && PyErr_Occurred()) return NULL;
+    }
+    if (stream_of(args[n - 1], &st) < 0) return NULL;
+    PyObject *type = PyTuple_GET_ITEM(op_types, form / 2);
+    const int is_desc = PyObject_IsInstance(args[2], type);
+    if (is_desc < 0) return NULL;
+    if (!is_desc) return PyErr_Format(PyExc_TypeError, "call_op: not a %s", ((PyTypeObject *)type)->tp_name);
+    Py_buffer view;
+    if (PyObject_GetBuffer(args[2], &view, PyBUF_SIMPLE) < 0) return NULL;
+    if (view.len < op_sizes[form / 2]) {
+        PyBuffer_Release(&view);
+        return PyErr_Format(PyExc_TypeError, "call_op: %s has another layout than include/cawn.h", ((PyTypeObject *)type)->tp_name);
+    }
+    int r = 0, known = 1;
+    Py_BEGIN_ALLOW_THREADS
+    switch (np) {
+        OP(3, P3, V3) OP(4, P4, V4) OP(6, P6, V6) OP(9, P9, V9) OP(11, P11, V11) OP(16, P16, V16)
+    default: known = 0;
+    }
+    Py_END_ALLOW_THREADS
+    PyBuffer_Release(&view);
+    if (!known) return PyErr_Format(PyExc_TypeError, "call_op: no entry point takes %zd tensors", np);
+    return PyLong_FromLong(r);
+}
+
+static PyObject *setup_ops(PyObject *self, PyObject *types)
+{
+    (void)self;
+    if (!PyTuple_Check(types) || PyTuple_GET_SIZE(types) != (Py_ssize_t)(sizeof op_sizes / sizeof op_sizes[0]))
+        return PyErr_Format(PyExc_TypeError, "setup_ops: a tuple of descriptor types");
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(types); ++i)
+        if (!PyType_Check(PyTuple_GET_ITEM(types, i))) return PyErr_Format(PyExc_TypeError, "setup_ops: a tuple of descriptor types");
+    Py_INCREF(types);
+    Py_XSETREF(op_types, types);
+    Py_RETURN_NONE;
+}
+
 static PyObject *setup(PyObject *self, PyObject *args)
 {
     (void)self;
@@ -166,6 +243,8 @@ static PyObject *setup(PyObject *self, PyObject *args)
 }
 
 static PyMethodDef methods[] = {{"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, "call an entry point of libcawn"},
+                                {"call_op", (PyCFunction)(void (*)(void))call_op, METH_FASTCALL, "call an operator with a descriptor of its own"},
+                                {"setup_ops", setup_ops, METH_O, "the operators' descriptor types"},
                                 {"setup", setup, METH_VARARGS, "descriptor type, current device, current raw stream of a device"},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_cawn_call", NULL, -1, methods, NULL, NULL, NULL, NULL};

@@ -1,0 +1,496 @@
+// Group norm with an activation, channels last, forward and backward.
+//
+// Forward: mean and variance over a group's values, y = act(w xh + b), xh = (x - mean) rstd.
+// Backward: dz = dy act'(z), t = w dz, dx = rstd (t - avg(t) - xh avg(t xh)), dw = sum dz xh, db = sum dz.
+//
+// Two forms, by T:
+//   T = 1 (a token's heads, each by itself): a run of 4 to 64 lanes holds a group in registers from the one read to the write; the
+//     variance is that of the centred values.  Bytes: x in, y out (backward: x, dy in, dx out).
+//   T > 1, or a group too wide for 64 lanes' registers: a workgroup sums a run of tokens over its channels, a second kernel joins
+//     the sums and applies them: x is read twice.  Sums are taken of x less the group's first value: as exact as two passes
+//     unless that value is many deviations off the mean.
+// Parameter gradients: every workgroup keeps its channels' sums over the rows it takes and leaves them in the workspace; a last
+// kernel adds these in a fixed order.
+#include "cawn_ops.hpp"
+
+using namespace cawn::ops;
+
+namespace {
+
+struct NormArgs {
+    const void *x, *dy;
+    const float *w, *b;
+    float *stats;
+    void *y, *dx;
+    float *part;            // T > 1: sums of a group's part
+    float *colpart;         // [rows][2][C]: a workgroup's share of dweight, dbias
+    int B, T, C, G, cg, act;
+    float eps;
+    long long xsb, xst, ysb, yst;
+    // geometry
+    int lpg, gb, rb, gblocks, rblocks;               // T = 1: lanes of a group; groups and rows of a workgroup; their numbers of workgroups
+    int cb, slots, ncb, splits, bblocks, t_run;      // T > 1: channels and groups of a workgroup, its column blocks, runs of tokens, rows at a time
+};
+
+__device__ inline float sigmoid_f(float z) { return 1.f / (1.f + __expf(-z)); }
+
+__device__ inline float act_f(float z, int act)
+{
+    if (act == 1) return z * sigmoid_f(z);
+    if (act == 2) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    return z;
+}
+
+__device__ inline float act_slope(float z, int act)
+{
+    if (act == 1) {
+        const float s = sigmoid_f(z);
+        return s * (1.f + z * (1.f - s));
+    }
+    if (act == 2) return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * 0.3989422804014327f * __expf(-0.5f * z * z);
+    return 1.f;
+}
+
+// sum over the run of `lanes` (a power of two) adjacent lanes, in every one of them
+__device__ inline float run_sum(float v, int lanes)
+{
+    for (int m = lanes >> 1; m > 0; m >>= 1) v += __shfl_xor(v, m);
+    return v;
+}
+
+template <int VEC> __device__ inline void params(const float *p, int c, float missing, float (&v)[VEC])
+{
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = p ? p[c + i] : missing;
+}
+
+// ---------------------------------------------------------------------------------------------- T = 1
+template <typename T, int VEC, int NIT, bool BWD> __global__ __launch_bounds__(256) void group_norm_rows(const NormArgs a)
+{
+    const int sub = threadIdx.x / a.lpg, lane = threadIdx.x % a.lpg, gi = sub % a.gb, ri = sub / a.gb;
+    const int g = (blockIdx.x % a.gblocks) * a.gb + gi, first = (blockIdx.x / a.gblocks) * a.rb + ri;
+    const bool mine = ri < a.rb && g < a.G;
+    const int c0 = (mine ? g : 0) * a.cg;
+    float w[NIT][VEC], bias[NIT][VEC], sw[BWD ? NIT : 1][VEC], sb[BWD ? NIT : 1][VEC];
+    bool in[NIT];
+#pragma unroll
+    for (int n = 0; n < NIT; ++n) {
+        const int c = (n * a.lpg + lane) * VEC;
+        in[n] = mine && c < a.cg;
+        params<VEC>(in[n] ? a.w : nullptr, c0 + c, 1.f, w[n]);
+        params<VEC>(in[n] ? a.b : nullptr, c0 + c, 0.f, bias[n]);
+        if (BWD) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) sw[n][i] = sb[n][i] = 0.f;
+        }
+    }
+    const float inv = 1.f / (float)a.cg;
+    for (long long r = first; r < a.B; r += (long long)a.rblocks * a.rb) {
+        const bool live = mine;
+        float x[NIT][VEC], d[BWD ? NIT : 1][VEC];
+        float s = 0.f;
+#pragma unroll
+        for (int n = 0; n < NIT; ++n) {
+            const int c = c0 + (n * a.lpg + lane) * VEC;
+            if (in[n]) load_n<T, VEC>((const T *)a.x + r * a.xsb + c, x[n]);
+            if (BWD && in[n]) load_n<T, VEC>((const T *)a.dy + r * a.ysb + c, d[n]);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                if (!in[n]) x[n][i] = 0.f;
+                if (BWD && !in[n]) d[n][i] = 0.f;
+                s += x[n][i];
+            }
+        }
+        float mean, rstd;
+        if (BWD) {
+            mean = live ? a.stats[(r * a.G + g) * 2] : 0.f;
+            rstd = live ? a.stats[(r * a.G + g) * 2 + 1] : 0.f;
+        } else {
+            mean = run_sum(s, a.lpg) * inv;
+            float q = 0.f;
+#pragma unroll
+            for (int n = 0; n < NIT; ++n)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) q += in[n] ? (x[n][i] - mean) * (x[n][i] - mean) : 0.f;
+            rstd = 1.f / sqrtf(run_sum(q, a.lpg) * inv + a.eps);
+            if (a.stats && live && lane == 0) a.stats[(r * a.G + g) * 2] = mean, a.stats[(r * a.G + g) * 2 + 1] = rstd;
+        }
+        if (!BWD) {
+#pragma unroll
+            for (int n = 0; n < NIT; ++n) {
+                if (!in[n]) continue;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) x[n][i] = act_f((x[n][i] - mean) * rstd * w[n][i] + bias[n][i], a.act);
+                store_n<T, VEC>((T *)a.y + r * a.ysb + c0 + (n * a.lpg + lane) * VEC, x[n]);
+            }
+        } else {
+            float m1 = 0.f, m2 = 0.f;
+#pragma unroll
+            for (int n = 0; n < NIT; ++n)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const float xh = (x[n][i] - mean) * rstd;
+                    const float dz = d[n][i] * act_slope(xh * w[n][i] + bias[n][i], a.act);
+                    if (in[n]) {
+                        sw[n][i] += dz * xh;
+                        sb[n][i] += dz;
+                    }
+                    x[n][i] = xh;
+                    d[n][i] = in[n] ? dz * w[n][i] : 0.f;
+                    m1 += d[n][i];
+                    m2 += in[n] ? d[n][i] * xh : 0.f;
+                }
+            m1 = run_sum(m1, a.lpg) * inv;
+            m2 = run_sum(m2, a.lpg) * inv;
+            if (a.dx) {
+#pragma unroll
+                for (int n = 0; n < NIT; ++n) {
+                    if (!in[n]) continue;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) x[n][i] = rstd * (d[n][i] - m1 - x[n][i] * m2);
+                    store_n<T, VEC>((T *)a.dx + r * a.xsb + c0 + (n * a.lpg + lane) * VEC, x[n]);
+                }
+            }
+        }
+    }
+    if (BWD && a.colpart) {
+        // the workgroup's rows of one channel, in the order of its runs of lanes
+        __shared__ float sh[256 * VEC * NIT];
+        float *out = a.colpart + (long long)(blockIdx.x / a.gblocks) * 2 * a.C;
+        for (int which = 0; which < 2; ++which) {
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < NIT; ++n)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) sh[(sub * NIT + n) * a.lpg * VEC + lane * VEC + i] = which ? sb[n][i] : sw[n][i];
+            __syncthreads();
+            if (mine && ri == 0) {
+#pragma unroll
+                for (int n = 0; n < NIT; ++n) {
+                    if (!in[n]) continue;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        float v = 0.f;
+                        for (int q = 0; q < a.rb; ++q) v += sh[((q * a.gb + gi) * NIT + n) * a.lpg * VEC + lane * VEC + i];
+                        out[which * a.C + c0 + (n * a.lpg + lane) * VEC + i] = v;
+                    }
+                }
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- T > 1
+// A workgroup: a.cb adjacent channels (whole groups, or a piece of one), a run of tokens, rows bblk, bblk + bblocks, ...
+// WHAT 0: sums of x and x^2 -> part;  1: y;  2: sums of t and t xh -> part, column sums -> colpart;  3: dx
+template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void group_norm_runs(const NormArgs a)
+{
+    __shared__ float sh[2][256 * (WHAT == 2 ? VEC : 1)];
+    __shared__ float stat[256][4];
+    const int units = a.cb / VEC, per = 256 / units, rp = threadIdx.x / units, unit = threadIdx.x % units;
+    const int blk = blockIdx.x, cblk = blk % a.ncb, split = blk / a.ncb % a.splits, bblk = blk / a.ncb / a.splits;
+    const bool mine = rp < per;
+    const int c = cblk * a.cb + unit * VEC;                             // the thread's channels
+    const int per_group = a.cg > a.cb ? a.cg / a.cb : 1;                // workgroups side by side that share a group
+    const int slot = a.cg > a.cb ? 0 : unit * VEC / a.cg, g = c / a.cg;
+    const int su = a.cg > a.cb ? units : a.cg / VEC;                    // units of a slot
+    const int t0 = split * a.t_run, t1 = min(a.T, t0 + a.t_run);
+    float w[VEC], bias[VEC], sw[VEC], sb[VEC];
+    params<VEC>(mine ? a.w : nullptr, c, 1.f, w);
+    params<VEC>(mine ? a.b : nullptr, c, 0.f, bias);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) sw[i] = sb[i] = 0.f;
+    const double n = (double)a.T * a.cg;
+    for (int b = bblk; b < a.B; b += a.bblocks) {
+        const T *xb = (const T *)a.x + b * a.xsb + c;
+        const float shift = WHAT == 0 && mine ? (float)*((const T *)a.x + b * a.xsb + (long long)g * a.cg) : 0.f;
+        float p0 = 0.f, p1 = 0.f;       // WHAT 1..3: mean, rstd
+        float m1 = 0.f, m2 = 0.f;
+        if (WHAT == 1 || WHAT == 3) {
+            // join the parts of this workgroup's groups: 16 lanes for each slot
+            __syncthreads();
+            for (int s = threadIdx.x / 16; s < a.slots; s += 16) {
+                const int gs = a.cg > a.cb ? g : cblk * a.slots + s;
+                double s1 = 0.0, s2 = 0.0;
+                for (int j = threadIdx.x % 16; j < a.splits * per_group; j += 16) {
+                    const int sp = j / per_group, cbk = a.cg > a.cb ? gs * per_group + j % per_group : cblk;
+                    const float *p = a.part + ((((long long)b * a.splits + sp) * a.ncb + cbk) * a.slots + s) * 2;
+                    s1 += p[0];
+                    s2 += p[1];
+                }
+                for (int m = 8; m > 0; m >>= 1) s1 += __shfl_xor(s1, m), s2 += __shfl_xor(s2, m);
+                s1 /= n, s2 /= n;
+                if (threadIdx.x % 16 == 0) {
+                    if (WHAT == 1) {
+                        const float first = (float)*((const T *)a.x + b * a.xsb + (long long)gs * a.cg);
+                        const double var = s2 - s1 * s1;
+                        stat[s][0] = (float)(first + s1);
+                        stat[s][1] = (float)(1.0 / sqrt((var > 0.0 || var != var ? var : 0.0) + (double)a.eps));
+                        const bool one = a.cg > a.cb ? cblk % per_group == 0 : true;
+                        if (a.stats && split == 0 && one) {
+                            a.stats[((long long)b * a.G + gs) * 2] = stat[s][0];
+                            a.stats[((long long)b * a.G + gs) * 2 + 1] = stat[s][1];
+                        }
+                    } else {
+                        stat[s][2] = (float)s1;
+                        stat[s][3] = (float)s2;
+                    }
+                }
+            }
+            __syncthreads();
+            if (WHAT == 1) p0 = stat[slot][0], p1 = stat[slot][1];
+            else m1 = stat[slot][2], m2 = stat[slot][3];
+        }
+        if (WHAT >= 2 && mine) {
+            p0 = a.stats[((long long)b * a.G + g) * 2];
+            p1 = a.stats[((long long)b * a.G + g) * 2 + 1];
+        }
+        float s1 = 0.f, s2 = 0.f;
+        if (mine) {
+            for (int t = t0 + rp; t < t1; t += per) {
+                float x[VEC], d[VEC];
+                load_n<T, VEC>(xb + t * a.xst, x);
+                if (WHAT >= 2) load_n<T, VEC>((const T *)a.dy + b * a.ysb + t * a.yst + c, d);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    if (WHAT == 0) {
+                        const float v = x[i] - shift;
+                        s1 += v;
+                        s2 += v * v;
+                    } else {
+                        const float xh = (x[i] - p0) * p1;
+                        const float z = xh * w[i] + bias[i];
+                        if (WHAT == 1) x[i] = act_f(z, a.act);
+                        else {
+                            const float dz = d[i] * act_slope(z, a.act), u = dz * w[i];
+                            if (WHAT == 2) {
+                                sw[i] += dz * xh;
+                                sb[i] += dz;
+                                s1 += u;
+                                s2 += u * xh;
+                            } else x[i] = p1 * (u - m1 - xh * m2);
+                        }
+                    }
+                }
+                if (WHAT == 1) store_n<T, VEC>((T *)a.y + b * a.ysb + t * a.yst + c, x);
+                if (WHAT == 3) store_n<T, VEC>((T *)a.dx + b * a.xsb + t * a.xst + c, x);
+            }
+        }
+        if (WHAT == 0 || WHAT == 2) {
+            // over the token phases of a unit, then over a slot's units
+            __syncthreads();
+            sh[0][threadIdx.x] = s1, sh[1][threadIdx.x] = s2;
+            __syncthreads();
+            if (rp == 0) {
+                for (int q = 1; q < per; ++q) s1 += sh[0][q * units + unit], s2 += sh[1][q * units + unit];
+                sh[0][unit] = s1, sh[1][unit] = s2;
+            }
+            __syncthreads();
+            if ((int)threadIdx.x < a.slots) {
+                float v1 = 0.f, v2 = 0.f;
+                for (int q = 0; q < su; ++q) v1 += sh[0][threadIdx.x * su + q], v2 += sh[1][threadIdx.x * su + q];
+                float *p = a.part + ((((long long)b * a.splits + split) * a.ncb + cblk) * a.slots + threadIdx.x) * 2;
+                p[0] = v1, p[1] = v2;
+            }
+        }
+    }
+    if (WHAT == 2 && a.colpart) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            sh[0][threadIdx.x * VEC + i] = sw[i];
+            sh[1][threadIdx.x * VEC + i] = sb[i];
+        }
+        __syncthreads();
+        if (rp == 0) {
+            float *out = a.colpart + ((long long)bblk * a.splits + split) * 2 * a.C;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                float v1 = 0.f, v2 = 0.f;
+                for (int q = 0; q < per; ++q) v1 += sh[0][(q * units + unit) * VEC + i], v2 += sh[1][(q * units + unit) * VEC + i];
+                out[c + i] = v1;
+                out[a.C + c + i] = v2;
+            }
+        }
+    }
+}
+
+// dweight, dbias: the sums of `rows` rows of [2][C], in a fixed order: 16 columns by 16 runs of rows a workgroup
+__global__ __launch_bounds__(256) void group_norm_columns(const float *part, int rows, int C, float *dw, float *db, int accumulate)
+{
+    __shared__ float sh[16][17];
+    const int col = threadIdx.x % 16, run = threadIdx.x / 16;
+    const long long c = (long long)blockIdx.x * 16 + col;
+    float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+    if (c < 2LL * C) {
+        int r = run;
+        for (; r + 48 < rows; r += 64) {
+            s0 += part[(long long)r * 2 * C + c];
+            s1 += part[(long long)(r + 16) * 2 * C + c];
+            s2 += part[(long long)(r + 32) * 2 * C + c];
+            s3 += part[(long long)(r + 48) * 2 * C + c];
+        }
+        for (; r < rows; r += 16) s0 += part[(long long)r * 2 * C + c];
+    }
+    sh[run][col] = (s0 + s1) + (s2 + s3);
+    __syncthreads();
+    if (run == 0 && c < 2LL * C) {
+        float v = 0.f;
+        for (int q = 0; q < 16; ++q) v += sh[q][col];
+        float *out = c < C ? dw : db;
+        const long long at = c < C ? c : c - C;
+        if (out) out[at] = accumulate ? out[at] + v : v;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- host
+struct Plan {
+    NormArgs a;
+    bool rows;              // the T = 1 form
+    int vec, nit;
+    long long blocks, colrows;
+    size_t part_bytes, bytes;
+};
+
+// The geometry must not depend on pointers: the workspace is sized without them.  Unaligned calls take vec = 1.
+bool plan_of(const cawn_norm_desc *d, bool wide, Plan *p)
+{
+    if (!d || d->B < 0 || d->T < 0 || d->C <= 0 || d->groups <= 0 || d->C % d->groups || d->act < 0 || d->act > 2 || (d->bf16 & ~1)) return false;
+    NormArgs &a = p->a;
+    a = NormArgs{};
+    a.B = d->B, a.T = d->T, a.C = d->C, a.G = d->groups, a.cg = d->C / d->groups, a.act = d->act, a.eps = d->eps;
+    a.xst = d->x_stride_t ? d->x_stride_t : d->C, a.yst = d->y_stride_t ? d->y_stride_t : d->C;
+    a.xsb = d->x_stride_b ? d->x_stride_b : a.xst * d->T, a.ysb = d->y_stride_b ? d->y_stride_b : a.yst * d->T;
+    if (a.xst < a.C || a.yst < a.C) return false;
+    const int most = d->bf16 ? 8 : 4;
+    const bool fits = a.cg % most == 0 && a.xst % most == 0 && a.xsb % most == 0 && a.yst % most == 0 && a.ysb % most == 0;
+    p->vec = wide && fits ? most : 1;
+    const long long lanes = ceil_div(a.cg, p->vec);
+    p->rows = a.T == 1 && lanes <= 64 * 4;
+    const long long cap = 33554432LL / (8LL * a.C) > 64 ? 33554432LL / (8LL * a.C) : 64;      // rows of parameter sums: 32 MiB of them
+    if (p->rows) {
+        a.lpg = 1;
+        while (a.lpg < 64 && a.lpg < lanes) a.lpg *= 2;
+        const long long nit = ceil_div(lanes, a.lpg);
+        p->nit = nit <= 1 ? 1 : nit <= 2 ? 2 : 4;
+        const int subs = 256 / a.lpg;
+        a.gb = a.G < subs ? a.G : subs;
+        a.rb = subs / a.gb;
+        a.gblocks = (int)ceil_div(a.G, a.gb);
+        long long rblocks = ceil_div(a.B, a.rb);
+        long long want = 2048 / a.gblocks > 1 ? 2048 / a.gblocks : 1;
+        if (want > cap) want = cap;
+        a.rblocks = (int)(rblocks < want ? rblocks : want);
+        p->blocks = (long long)a.rblocks * a.gblocks;
+        p->colrows = a.rblocks;
+        p->part_bytes = 0;
+    } else {
+        const int top = 256 * p->vec;
+        if (a.cg <= top) {
+            a.slots = top / a.cg < a.G ? top / a.cg : a.G;
+            while (a.G % a.slots) --a.slots;
+            a.cb = a.slots * a.cg;
+        } else {                            // the widest piece of a group that divides it
+            int units = 256;
+            while (a.cg / p->vec % units) --units;
+            a.slots = 1;
+            a.cb = units * p->vec;
+        }
+        a.ncb = a.C / a.cb;
+        const int per = 256 / (a.cb / p->vec);
+        long long bb = 2048 / a.ncb > 1 ? 2048 / a.ncb : 1;
+        if (bb > cap) bb = cap;
+        a.bblocks = (int)(a.B < bb ? a.B : bb);
+        long long splits = a.bblocks > 0 ? bb / a.bblocks : 1;
+        const long long useful = ceil_div(a.T, 4LL * per);          // a thread takes four tokens at least
+        if (splits > useful) splits = useful;
+        if (splits < 1) splits = 1;
+        a.t_run = (int)ceil_div(a.T, splits);
+        if (a.t_run < 1) a.t_run = 1;
+        a.splits = (int)(a.T > 0 ? ceil_div(a.T, a.t_run) : 1);
+        p->blocks = (long long)a.bblocks * a.splits * a.ncb;
+        p->colrows = (long long)a.bblocks * a.splits;
+        p->part_bytes = ((size_t)a.B * a.splits * a.ncb * a.slots * 8 + 255) / 256 * 256;
+    }
+    p->bytes = p->part_bytes + (size_t)p->colrows * 8 * a.C;
+    return true;
+}
+
+template <typename T, int VEC, bool BWD> void launch_rows(const Plan &p, hipStream_t s)
+{
+    const dim3 grid((unsigned)p.blocks);
+    switch (p.nit) {
+    case 1: hipLaunchKernelGGL((group_norm_rows<T, VEC, 1, BWD>), grid, dim3(256), 0, s, p.a); break;
+    case 2: hipLaunchKernelGGL((group_norm_rows<T, VEC, 2, BWD>), grid, dim3(256), 0, s, p.a); break;
+    default: hipLaunchKernelGGL((group_norm_rows<T, VEC, 4, BWD>), grid, dim3(256), 0, s, p.a); break;
+    }
+}
+
+template <typename T, int VEC> int launch(const Plan &p, bool bwd, float *dw, float *db, int accumulate, hipStream_t s)
+{
+    const dim3 grid((unsigned)p.blocks), nt(256);
+    if (p.rows) {
+        if (bwd) launch_rows<T, VEC, true>(p, s);
+        else launch_rows<T, VEC, false>(p, s);
+    } else if (!bwd) {
+        hipLaunchKernelGGL((group_norm_runs<T, VEC, 0>), grid, nt, 0, s, p.a);
+        hipLaunchKernelGGL((group_norm_runs<T, VEC, 1>), grid, nt, 0, s, p.a);
+    } else {
+        hipLaunchKernelGGL((group_norm_runs<T, VEC, 2>), grid, nt, 0, s, p.a);
+        if (p.a.dx) hipLaunchKernelGGL((group_norm_runs<T, VEC, 3>), grid, nt, 0, s, p.a);
+    }
+    if (p.a.colpart) hipLaunchKernelGGL(group_norm_columns, dim3((unsigned)ceil_div(2LL * p.a.C, 16)), nt, 0, s, p.a.colpart, (int)p.colrows, p.a.C, dw, db, accumulate);
+    return launched();
+}
+
+int run(const cawn_norm_desc *d, bool bwd, const void *x, const float *w, const float *b, void *y, float *stats, const void *dy, void *dx, float *dw, float *db,
+        void *ws, size_t bytes, void *stream)
+{
+    Plan p;
+    if (!plan_of(d, true, &p)) return CAWN_EINVAL;
+    hipStream_t s = (hipStream_t)stream;
+    const bool grads = bwd && (dw || db);
+    if (d->B == 0 || d->T == 0) {
+        if (grads && !d->accumulate_param_grads)        // the sums over nothing
+            hipLaunchKernelGGL(group_norm_columns, dim3((unsigned)ceil_div(2LL * p.a.C, 16)), dim3(256), 0, s, nullptr, 0, p.a.C, dw, db, 0);
+        return launched();
+    }
+    if (!x || (bwd ? !dy || !stats : !y)) return CAWN_EINVAL;
+    const size_t e = d->bf16 ? 2 : 4;
+    if (!aligned_to(x, e) || !aligned_to(y, e) || !aligned_to(dy, e) || !aligned_to(dx, e) || !aligned_to(w, 4) || !aligned_to(b, 4)) return CAWN_EINVAL;
+    if (!aligned_to(x, 16) || !aligned_to(y, 16) || !aligned_to(dy, 16) || !aligned_to(dx, 16)) plan_of(d, false, &p);
+    const size_t need = p.part_bytes + (grads ? (size_t)p.colrows * 8 * p.a.C : 0);
+    if (need > 0 && (!ws || bytes < need || !aligned_to(ws, 256))) return CAWN_EWORKSPACE;
+    if (p.blocks > 0x7fffffffLL) return CAWN_EUNSUPPORTED;
+    p.a.x = x, p.a.w = w, p.a.b = b, p.a.y = y, p.a.stats = stats, p.a.dy = dy, p.a.dx = dx;
+    p.a.part = (float *)ws;
+    p.a.colpart = grads ? (float *)((char *)ws + p.part_bytes) : nullptr;
+    if (bwd && !dx && !grads) return CAWN_OK;
+    const int acc = d->accumulate_param_grads;
+    if (d->bf16) return p.vec == 8 ? launch<bf16, 8>(p, bwd, dw, db, acc, s) : launch<bf16, 1>(p, bwd, dw, db, acc, s);
+    return p.vec == 4 ? launch<float, 4>(p, bwd, dw, db, acc, s) : launch<float, 1>(p, bwd, dw, db, acc, s);
+}
+
+} // namespace
+
+extern "C" {
+
+size_t cawn_group_norm_workspace_bytes(const cawn_norm_desc *d)
+{
+    Plan wide, narrow;
+    if (!plan_of(d, true, &wide) || !plan_of(d, false, &narrow)) return 0;
+    return wide.bytes > narrow.bytes ? wide.bytes : narrow.bytes;
+}
+
+int cawn_group_norm_fwd(const cawn_norm_desc *d, const void *x, const float *weight, const float *bias, void *y, float *stats, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return run(d, false, x, weight, bias, y, stats, nullptr, nullptr, nullptr, nullptr, workspace, workspace_bytes, stream);
+}
+
+int cawn_group_norm_bwd(const cawn_norm_desc *d, const void *x, const float *weight, const float *bias, const float *stats, const void *dy, void *dx, float *dweight,
+                        float *dbias, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return run(d, true, x, weight, bias, nullptr, const_cast<float *>(stats), dy, dx, dweight, dbias, workspace, workspace_bytes, stream);
+}
+
+} // extern "C"

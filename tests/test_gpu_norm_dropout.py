@@ -1,0 +1,190 @@
+"""Group norm with an activation, and dropout with the residual addition, against 64 bits through the C ABI."""
+import numpy as np
+import pytest
+import torch
+
+import ops_ref as R
+from gpu_util import DEV, rel_err
+from paper_2604_04250_amd import binding as K
+
+pytestmark = pytest.mark.gpu
+
+# fp32: a value is some ten roundings of 2^-24 away from its inputs, and the mean's own error moves it by as much of |mean| / deviation
+# (a few here); exp is good to 2e-6 of a slope.  bf16 adds one rounding to 8 significant bits, 2^-8 of the value at most.
+TOL = 4e-6
+TOL16 = 2.0 ** -8 + TOL
+# column sums: a term is of the size of the root of the sum's, so rounding adds up to 2^-24 times a few roots of the rows
+TOLSUM = 2e-5
+
+
+def _ws(d):
+    return torch.full((max(256, K.cawn_group_norm_workspace_bytes(d)),), 0xff, dtype=torch.uint8, device=DEV)
+
+
+def _strided(a, dtype, extra):
+    """A device tensor of a's values whose last axis lies in rows `extra` longer."""
+    t = torch.full(a.shape[:-1] + (a.shape[-1] + extra,), float("nan"), device=DEV, dtype=dtype)[..., : a.shape[-1]]
+    t.copy_(torch.from_numpy(a))
+    return t
+
+
+def _norm_case(B, T, C, G, kind, bf16, extra=0, seed=1, affine=True, shift=0.3):
+    r = np.random.Generator(np.random.PCG64(seed))
+    dt = torch.bfloat16 if bf16 else torch.float32
+    f32 = lambda a: a.astype(np.float32)  # noqa: E731
+    x, dy = _strided(f32(1.7 * r.standard_normal((B, T, C)) + shift), dt, extra), _strided(f32(r.standard_normal((B, T, C))), dt, extra)
+    w, b = (f32(1 + 0.2 * r.standard_normal(C)), f32(0.1 * r.standard_normal(C))) if affine else (None, None)
+    return x, dy, w, b, dt
+
+
+def _run_norm(x, dy, w, b, G, kind, dt, extra=0, accumulate=0, want=("dx", "dweight", "dbias")):
+    B, T, C = x.shape
+    d = K.make_norm_desc(B, T, C, G, act=kind, bf16=int(dt == torch.bfloat16), accumulate_param_grads=accumulate, x_stride_t=C + extra,
+                         y_stride_t=C + extra)
+    dev = lambda a: None if a is None else torch.from_numpy(a).to(DEV)  # noqa: E731
+    wd, bd, ws = dev(w), dev(b), _ws(d)
+    new = lambda: torch.full((B, T, C + extra), float("nan"), device=DEV, dtype=dt)  # noqa: E731
+    y, dx = new(), new()
+    stats = torch.full((B, G, 2), float("nan"), device=DEV)
+    dw, db = torch.full((C,), 1.0, device=DEV), torch.full((C,), 2.0, device=DEV)
+    K.check(K.cawn_group_norm_fwd(d, x, wd, bd, y, stats, ws))
+    K.check(K.cawn_group_norm_bwd(d, x, wd, bd, stats, dy, dx if "dx" in want else None, dw if "dweight" in want else None,
+                                  db if "dbias" in want else None, ws))
+    torch.cuda.synchronize()
+    for t in (y, dx if "dx" in want else y):
+        assert bool(torch.isnan(t[..., C:]).all())          # nothing is written between rows
+    return {k: t.float().cpu().numpy() for k, t in dict(y=y[..., :C], dx=dx[..., :C], dweight=dw, dbias=db, stats=stats).items()}
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("B,T,C,G,kind,extra", [
+    (1, 1, 768, 12, 1, 0), (5, 1, 768, 12, 1, 8), (1001, 1, 768, 12, 1, 0), (3, 1, 30, 1, 2, 0), (17, 1, 360, 12, 0, 3), (4, 1, 1, 1, 0, 0),
+    (9, 1, 64, 64, 1, 0), (33, 1, 2048, 1, 1, 0), (3, 1, 5000, 2, 2, 0), (2, 1, 4099, 1, 1, 0), (7, 1, 48, 2, 1, 1),
+    (2, 3, 768, 12, 1, 0), (3, 129, 96, 4, 2, 0), (1, 1023, 30, 2, 1, 0), (2, 77, 4096, 1, 0, 0), (2, 65, 4100, 4, 1, 4), (300, 2, 16, 4, 1, 0),
+    (1, 5000, 8, 8, 1, 0), (2, 7, 6144, 2, 1, 0)])
+def test_group_norm_forward_and_backward(B, T, C, G, kind, extra, bf16):
+    x, dy, w, b, dt = _norm_case(B, T, C, G, kind, bf16, extra, seed=B + T + C)
+    got = _run_norm(x, dy, w, b, G, kind, dt, extra)
+    x64, dy64 = (t.float().cpu().numpy() for t in (x, dy))
+    y, _, rstd, mean = R.norm_fwd(x64, w, b, G, kind)
+    ref = R.norm_bwd(x64, w, b, dy64, G, kind)
+    tol = TOL16 if bf16 else TOL
+    if C // G == 1 and T == 1:                                  # a group of one value: xh is 0, dx too
+        assert np.all(got["dx"] == 0)
+    else:
+        assert rel_err(got["dx"], ref["dx"]) <= tol
+    assert rel_err(got["y"], y) <= tol
+    assert rel_err(got["stats"][..., 0], mean[:, 0, :, 0]) <= TOL and rel_err(got["stats"][..., 1], rstd[:, 0, :, 0]) <= TOL
+    assert rel_err(got["dbias"], ref["dbias"]) <= TOLSUM
+    if not (C // G == 1 and T == 1):
+        assert rel_err(got["dweight"], ref["dweight"]) <= TOLSUM
+
+
+def test_group_norm_without_parameters_and_with_accumulation():
+    x, dy, w, b, dt = _norm_case(37, 1, 96, 4, 1, False)
+    ref = R.norm_bwd(x.cpu().numpy(), None, None, dy.cpu().numpy(), 4, 1)
+    got = _run_norm(x, dy, None, None, 4, 1, dt, accumulate=1)
+    assert rel_err(got["dx"], ref["dx"]) <= TOL
+    assert rel_err(got["dweight"] - 1, ref["dweight"]) <= TOLSUM and rel_err(got["dbias"] - 2, ref["dbias"]) <= TOLSUM
+    got = _run_norm(x, dy, w, b, 4, 1, dt, want=("dbias",))
+    assert rel_err(got["dbias"], R.norm_bwd(x.cpu().numpy(), w, b, dy.cpu().numpy(), 4, 1)["dbias"]) <= TOLSUM
+    assert np.all(got["dweight"] == 1)
+    got = _run_norm(x, dy, w, b, 4, 1, dt, want=("dx",))
+    assert np.all(got["dweight"] == 1) and np.all(got["dbias"] == 2)
+
+
+@pytest.mark.parametrize("T", [1, 200])
+def test_group_norm_far_from_zero_keeps_its_variance(T):
+    """A mean a thousand deviations away: the variance is that of centred values (x itself is held to 2^-24 of 1000 deviations,
+    which is what the tolerance grants)."""
+    x, dy, w, b, dt = _norm_case(6, T, 128, 2, 1, False, shift=1700.0)
+    got = _run_norm(x, dy, w, b, 2, 1, dt)
+    y, _, rstd, _ = R.norm_fwd(x.cpu().numpy(), w, b, 2, 1)
+    assert rel_err(got["stats"][..., 1], rstd[:, 0, :, 0]) <= 1e-5
+    assert rel_err(got["y"], y) <= 1000 * 2.0 ** -22
+
+
+def test_group_norm_of_nothing():
+    d = K.make_norm_desc(0, 3, 8, 2)
+    dw, db = torch.ones(8, device=DEV), torch.ones(8, device=DEV)
+    K.check(K.cawn_group_norm_fwd(d, None, None, None, None, None, None))
+    K.check(K.cawn_group_norm_bwd(d, None, None, None, None, None, None, dw, db, None))
+    torch.cuda.synchronize()
+    assert not dw.any() and not db.any()
+
+
+def test_group_norm_a_bad_row_stays_by_itself_and_repeats_bitwise():
+    for T in (1, 40):
+        x, dy, w, b, dt = _norm_case(9, T, 96, 4, 1, False)
+        clean = _run_norm(x, dy, w, b, 4, 1, dt)
+        again = _run_norm(x, dy, w, b, 4, 1, dt)
+        assert all(np.array_equal(clean[n], again[n]) for n in clean)
+        x[3, T // 2, 30] = float("inf")                         # group 1 of row 3
+        got = _run_norm(x, dy, w, b, 4, 1, dt)
+        bad = np.zeros((9, T, 96), bool)
+        bad[3, :, 24:48] = True
+        assert np.array_equal(got["y"][~bad], clean["y"][~bad]) and np.array_equal(got["dx"][~bad], clean["dx"][~bad])
+        assert not np.isfinite(got["stats"][3, 1]).all()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("rows,cols,stride,p", [(1, 1, 0, 0.5), (3, 5, 0, 0.1), (7, 64, 0, 0.3), (7, 64, 72, 0.3), (5, 24, 25, 0.5), (1, 1027, 0, 0.1),
+                                                (40, 31, 0, 0.0), (4, 16, 0, 1.0), (2, 9, 12, 1.0), (1, 7, 30, 0.25)])
+def test_dropout_is_its_mask(rows, cols, stride, p, bf16):
+    r = np.random.Generator(np.random.PCG64(rows * 1000 + cols))
+    dt = torch.bfloat16 if bf16 else torch.float32
+    seed, offset = 0x123456789abcdef, (1 << 32) - 3              # blocks on both sides of the counter's low word
+    extra = stride - cols if stride else 0
+    x, res, dy = (_strided(r.standard_normal((rows, cols)).astype(np.float32), dt, extra) for _ in range(3))
+    d = K.make_dropout_desc(rows, cols, p=p, bf16=int(bf16), x_stride=stride, residual_stride=stride, y_stride=stride)
+    rng = torch.tensor([seed, offset], dtype=torch.int64, device=DEV)
+    keep = R.keep_mask(rows, cols, seed, offset, p)
+    scale = np.float32(1 / (1 - p)) if p < 1 else np.float32(0)
+    new = lambda: torch.full((rows, cols + extra), float("nan"), device=DEV, dtype=dt)  # noqa: E731
+    num = lambda t: t.float().cpu().numpy()  # noqa: E731
+    rounded = lambda a: num(torch.from_numpy(a.astype(np.float32)).to(dt))  # noqa: E731
+    y, dx, y0 = new(), new(), new()
+    K.check(K.cawn_dropout_add_fwd(d, x, res, rng, y))
+    K.check(K.cawn_dropout_add_bwd(d, dy, rng, dx))
+    K.check(K.cawn_dropout_add_fwd(d, x, None, rng, y0))
+    torch.cuda.synchronize()
+    drop = lambda a: np.where(keep, num(a) * scale, np.float32(0))  # noqa: E731
+    assert np.array_equal(num(y[:, :cols]), rounded(num(res) + drop(x)))         # two fp32 roundings, as there
+    assert np.array_equal(num(dx[:, :cols]), rounded(drop(dy))) and np.array_equal(num(y0[:, :cols]), rounded(drop(x)))
+    for t in (y, dx, y0):
+        assert bool(torch.isnan(t[:, cols:]).all())
+    # dropped places may hold anything
+    x[torch.from_numpy(~keep).to(DEV)] = float("nan")
+    K.check(K.cawn_dropout_add_fwd(d, x, res, rng, y0))
+    if p > 0 and not stride:
+        K.check(K.cawn_dropout_add_fwd(d, x, res, rng, res))                     # in place
+        assert torch.equal(res, y)
+    torch.cuda.synchronize()
+    assert torch.equal(y0[:, :cols], y[:, :cols])
+
+
+def test_dropout_keeps_its_share_and_forgets_nothing_at_replays():
+    """A captured call finds the seed and offset that the device holds at each replay."""
+    n = 1 << 20
+    x, y = torch.ones(1, n, device=DEV), torch.empty(1, n, device=DEV)
+    d = K.make_dropout_desc(1, n, p=0.25)
+    rng = torch.tensor([7, 0], dtype=torch.int64, device=DEV)
+    K.check(K.cawn_dropout_add_fwd(d, x, None, rng, y))
+    torch.cuda.synchronize()
+    share = (y != 0).float().mean().item()
+    assert abs(share - 0.75) <= 5 * (0.25 * 0.75 / n) ** 0.5
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        K.check(K.cawn_dropout_add_fwd(d, x, None, rng, y))
+        rng[1] += n // 4
+    seen = []
+    for i in range(4):
+        at = rng.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = torch.empty_like(y)
+        K.check(K.cawn_dropout_add_fwd(d, x, None, at, eager))
+        torch.cuda.synchronize()
+        assert torch.equal(eager, y) and int(at[1]) == i * (n // 4)
+        assert all(not torch.equal(y, s) for s in seen)
+        seen.append(y.clone())
