@@ -27,12 +27,36 @@ struct Args {
     const float *dstate_out;
     void *dq, *dk, *dv;
     float *ddecay, *dbeta, *dstate_in;
-    // checkpoint and workspace
-    float *ck_state;                // [B][H][chunks][K][V]: the state before each chunk
-    float *ck_u;                    // [B][H][chunks][CHUNK][V]
-    char *ws;
     int chunks, slabs;
     int vec4;                       // state rows may be read 16 bytes at a time
+    int vecq, vecv, veco;           // rows of q, k (dq, dk), of v (dv), of o (dO) may be: 16 bytes at a time
+    // Chunked form.  The launches of a call treat the chunks c0 .. c1-1 of every row; the workspace holds `span` of them.
+    int c0, c1, span, VT;           // VT: tiles of 16 value columns
+    char *ws;
+    // tiles of the state before each chunk, and of u: in the checkpoint or in the workspace.  Chunk n of head bh begins
+    // bh * row + (n - first) * chunk bytes behind
+    char *s_tiles, *u_tiles;
+    size_t s_row, s_chunk, u_row, u_chunk;
+    int s_first, u_first;
+};
+
+// Sizes in the chunked form; everything is made of 1 KiB pieces: a matrix operand's plane (64 lanes x 8 bf16) or an fp32 tile
+// (16 x 16, a lane's four rows together).
+struct Sizes {
+    int KP, VT, wf, kf, ut, st;     // padded K; tiles of V; pieces of W, of K^T, of a chunk's u, of a state
+    size_t slot;                    // workspace of one chunk of one head, forward
+    size_t bslot;                   // backward
+    __host__ __device__ Sizes(int K, int V, int planes)
+    {
+        KP = K <= 32 ? 32 : K <= 64 ? 64 : 128;
+        VT = (V + 15) / 16;
+        wf = 4 * (KP / 32) * 3;
+        kf = (KP / 16) * 2 * planes;
+        ut = 4 * VT;
+        st = (KP / 16) * VT;
+        slot = (size_t)(wf + kf + ut + 2) * 1024;               // W, K^T, u, gates
+        bslot = (size_t)(wf + kf + ut + 2 + 2 * st) * 1024;     // ... dR for u, Y and dS
+    }
 };
 
 __device__ inline int row_length(const Args &a, int b)
@@ -42,6 +66,28 @@ __device__ inline int row_length(const Args &a, int b)
 }
 
 int launch_token(const Args &a, bool bf16, hipStream_t s);
+int launch_prepare(const Args &a, bool bf16, hipStream_t s);            // forward: W, K^T, T beta V, gates
+int launch_output(const Args &a, bool bf16, hipStream_t s);             // forward: o
+
+// The recurrence over chunks, either direction: X += W S, S = e S + K^T (c X) (+ Y), with S stored ahead of every chunk.
+struct StateArgs {
+    int B, L, H, K, V, VT, chunks, c0, c1, span;
+    const int32_t *lengths;
+    char *ws;                       // a chunk's slot: W, K^T, X0, gates, (Y)
+    size_t slot;
+    size_t x_at, gates_at, y_at;    // in the slot
+    char *s_tiles;                  // states ahead of the chunks
+    size_t s_row, s_chunk;          // bytes from one head's to the next, from one chunk's to the next
+    int s_first;                    // chunk of the first
+    char *x_tiles;                  // X of the chunks, likewise
+    size_t x_row, x_chunk;
+    int x_first;
+    char *carry;                    // [B H][st] tiles: from one launch to the next
+    const float *begin;             // row-major state at the beginning (or null: zero), read when `first`
+    float *end;                     // row-major state at the end, written when `last`
+    int first, last, keep_end;      // keep_end: the state behind the last chunk goes to s_tiles too
+};
+int launch_states(const StateArgs &a, bool bf16, bool reverse, hipStream_t s);
 
 } // namespace delta
 } // namespace cawn

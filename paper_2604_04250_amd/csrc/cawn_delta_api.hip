@@ -5,7 +5,12 @@ using namespace cawn;
 using namespace cawn::ops;
 using cawn::delta::Args;
 
+using cawn::delta::Sizes;
+using cawn::delta::StateArgs;
+
 namespace {
+
+constexpr size_t SPAN_BYTES = 128u << 20;
 
 int check(const cawn_delta_desc *d, Args *a)
 {
@@ -22,8 +27,34 @@ int check(const cawn_delta_desc *d, Args *a)
     a->qsb = d->qk_stride_b ? d->qk_stride_b : a->qst * d->L, a->vsb = d->v_stride_b ? d->v_stride_b : a->vst * d->L;
     a->osb = d->o_stride_b ? d->o_stride_b : a->ost * d->L;
     a->chunks = (int)ceil_div(d->L, delta::CHUNK);
+    a->VT = (int)ceil_div(d->V, 16);
+    if ((long long)d->B * d->H * ceil_div(d->V, 16) > 0x7fffffffLL) return CAWN_EUNSUPPORTED;
     return CAWN_OK;
 }
+
+// Chunks that the launches of a call treat at once: what they hand on to each other through the workspace is then still in the
+// 256 MiB memory-side cache, and the workspace does not grow with the sequence.
+int span_of(const Args &a, size_t per_chunk)
+{
+    const long long room = (long long)(SPAN_BYTES / ((size_t)a.B * a.H * per_chunk));
+    return (int)(room < 1 ? 1 : room < a.chunks ? room : a.chunks > 1 ? a.chunks : 1);
+}
+
+struct Layout { size_t slots, states, carry, bytes; int span; };
+Layout forward_layout(const Args &a, const Sizes &z)
+{
+    Layout l;
+    const size_t rows = (size_t)a.B * a.H;
+    l.span = span_of(a, z.slot + (size_t)z.st * 1024);
+    l.slots = rows * l.span * z.slot;
+    l.states = rows * l.span * z.st * 1024;
+    l.carry = rows * z.st * 1024;
+    l.bytes = l.slots + l.states + l.carry;
+    return l;
+}
+
+// states [B H][chunks + 1], then u [B H][chunks], in tiles
+size_t ckpt_bytes(const Args &a, const Sizes &z) { return (size_t)a.B * a.H * ((size_t)(a.chunks + 1) * z.st + (size_t)a.chunks * z.ut) * 1024; }
 
 bool misaligned(const cawn_delta_desc *d, const void *p) { return !aligned_to(p, d->bf16 ? 2 : 4); }
 
@@ -40,13 +71,15 @@ size_t cawn_delta_state_bytes(const cawn_delta_desc *d)
 size_t cawn_delta_ckpt_bytes(const cawn_delta_desc *d)
 {
     Args a;
-    return check(d, &a) != CAWN_OK ? 0 : (size_t)a.B * a.H * a.chunks * (a.K + delta::CHUNK) * a.V * 4;
+    return check(d, &a) != CAWN_OK ? 0 : ckpt_bytes(a, Sizes(a.K, a.V, 1));
 }
 
 size_t cawn_delta_workspace_bytes(const cawn_delta_desc *d)
 {
     Args a;
-    return check(d, &a) != CAWN_OK ? 0 : 256;
+    if (check(d, &a) != CAWN_OK) return 0;
+    const size_t bytes = forward_layout(a, Sizes(a.K, a.V, d->bf16 ? 1 : 3)).bytes;
+    return bytes > 256 ? bytes : 256;
 }
 
 int cawn_delta_rule_fwd(const cawn_delta_desc *d, const void *q, const void *k, const void *v, const float *decay, const float *beta, const int32_t *lengths,
@@ -60,8 +93,45 @@ int cawn_delta_rule_fwd(const cawn_delta_desc *d, const void *q, const void *k, 
         !aligned_to(state_in, 4) || !aligned_to(state_out, 4) || !aligned_to(ckpt, 16)) return CAWN_EINVAL;
     a.q = q, a.k = k, a.v = v, a.decay = decay, a.beta = beta, a.lengths = lengths, a.state_in = (const float *)state_in, a.o = o, a.state_out = (float *)state_out;
     a.vec4 = a.V % 4 == 0 && aligned_to(state_in, 16) && aligned_to(state_out, 16);
-    (void)workspace, (void)workspace_bytes;
-    return delta::launch_token(a, d->bf16, (hipStream_t)stream);
+    hipStream_t s = (hipStream_t)stream;
+    // token by token up to TOKEN_MAX
+    if (a.L <= delta::TOKEN_MAX && !ckpt) return delta::launch_token(a, d->bf16, s);
+    const int e = d->bf16 ? 2 : 4, w = 16 / e;
+    const Sizes z(a.K, a.V, d->bf16 ? 1 : 3);
+    const Layout l = forward_layout(a, z);
+    if (!workspace || workspace_bytes < l.bytes || !aligned_to(workspace, 256)) return CAWN_EWORKSPACE;
+    if ((long long)a.B * a.H * l.span > 0x7fffffffLL) return CAWN_EUNSUPPORTED;
+    a.vecq = a.K % w == 0 && a.qst % w == 0 && a.qsb % w == 0 && aligned_to(q, 16) && aligned_to(k, 16);
+    a.vecv = a.V % w == 0 && a.vst % w == 0 && a.vsb % w == 0 && aligned_to(v, 16);
+    a.veco = a.V % 4 == 0 && a.ost % 4 == 0 && a.osb % 4 == 0 && aligned_to(o, 4 * e);
+    a.ws = (char *)workspace;
+    a.span = l.span;
+    StateArgs t{};
+    t.B = a.B, t.L = a.L, t.H = a.H, t.K = a.K, t.V = a.V, t.VT = a.VT, t.chunks = a.chunks, t.span = l.span, t.lengths = a.lengths;
+    t.ws = a.ws, t.slot = z.slot, t.x_at = (size_t)(z.wf + z.kf) * 1024, t.gates_at = (size_t)(z.wf + z.kf + z.ut) * 1024;
+    t.carry = a.ws + l.slots + l.states;
+    t.begin = a.state_in, t.end = a.state_out;
+    if (ckpt) {
+        a.s_tiles = (char *)ckpt, a.s_chunk = (size_t)z.st * 1024, a.s_row = (size_t)(a.chunks + 1) * a.s_chunk;
+        a.u_tiles = a.s_tiles + (size_t)a.B * a.H * a.s_row, a.u_chunk = (size_t)z.ut * 1024, a.u_row = (size_t)a.chunks * a.u_chunk;
+        t.keep_end = 1;
+    } else {            // u takes the place of T beta V
+        a.s_tiles = a.ws + l.slots, a.s_chunk = (size_t)z.st * 1024, a.s_row = (size_t)l.span * a.s_chunk;
+        a.u_tiles = a.ws + t.x_at, a.u_chunk = z.slot, a.u_row = (size_t)l.span * z.slot;
+    }
+    t.s_tiles = a.s_tiles, t.s_row = a.s_row, t.s_chunk = a.s_chunk, t.x_tiles = a.u_tiles, t.x_row = a.u_row, t.x_chunk = a.u_chunk;
+    for (a.c0 = 0; a.c0 == 0 || a.c0 < a.chunks; a.c0 += l.span) {
+        a.c1 = a.c0 + l.span < a.chunks ? a.c0 + l.span : a.chunks;
+        a.s_first = a.u_first = ckpt ? 0 : a.c0;
+        t.c0 = a.c0, t.c1 = a.c1, t.s_first = t.x_first = a.s_first;
+        t.first = a.c0 == 0, t.last = a.c1 == a.chunks;
+        if (a.c1 > a.c0)
+            if (int r = delta::launch_prepare(a, d->bf16, s)) return r;
+        if (int r = delta::launch_states(t, d->bf16, false, s)) return r;
+        if (a.c1 > a.c0)
+            if (int r = delta::launch_output(a, d->bf16, s)) return r;
+    }
+    return CAWN_OK;
 }
 
 int cawn_delta_rule_bwd(const cawn_delta_desc *d, const void *q, const void *k, const void *v, const float *decay, const float *beta, const int32_t *lengths,

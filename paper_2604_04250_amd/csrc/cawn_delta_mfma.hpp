@@ -1,0 +1,286 @@
+// Gated delta rule by chunks: what the kernels share.
+//
+// A chunk of C = 64 tokens is treated at once.  With G the running sum of the decays, D_ij = exp(G_i - G_j) for i >= j,
+// N = strictly lower part of D o K K^T, P = lower part of D o Q K^T, T = (I + diag(beta) N)^-1:
+//     U   = T diag(beta) (V - diag(e^G) K S0)             the u of every token, S0 the state before the chunk
+//     O   = scale (diag(e^G) Q S0 + P U)
+//     S_C = e^{G_C} S0 + sum_j e^{G_C - G_j} k_j u_j^T
+// (the norms' factors of q and k multiply rows and columns of these and are applied there, never rounded into q and k).
+//
+// Matrix products run on the bf16 matrix instruction (16 x 16 x 32).  A bf16 operand is exact; an fp32 one is cut into three bf16
+// planes x = x0 + x1 + x2 of 8 bits each, 24 in all, and a product takes the pairs whose planes' numbers add up to less than 3: three
+// instructions for exact x fp32, six for fp32 x fp32, with the error of an fp32 product.  (The fp32 matrix instruction has a 16th of the
+// bf16 one's rate.)  Where only a bf16 output hangs on it, two planes and three pairs (16 bits) are enough.
+//
+// Layout of the instruction, g = lane / 16, c = lane % 16: operands hold row (column) c and eight steps of the contraction, 8g .. 8g+7;
+// the result holds column c and rows 4g .. 4g+3.  Which eight steps a lane holds is free as long as both operands agree, so two result
+// tiles (rows 4g .. 4g+3 of each) are one operand of the next product, without leaving their registers.  That order -- 4g .. 4g+3 of
+// the first 16 steps, then of the second -- is called the tile order below; "straight" is 8g .. 8g+7.
+#pragma once
+#include "cawn_delta.hpp"
+
+namespace cawn {
+namespace delta {
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4v lds_short4v;
+
+__device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+template <int N> struct Frag { bf16x8 p[N]; };      // an operand's planes, the leading one first
+
+// acc += a b, over the pairs of planes whose numbers add up to less than S
+template <int S, int NA, int NB> __device__ inline f32x4 mma(const Frag<NA> &a, const Frag<NB> &b, f32x4 acc)
+{
+#pragma unroll
+    for (int s = S - 1; s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int j = s - i;
+            if (j >= 0 && j < NB) acc = mfma(a.p[i], b.p[j], acc);
+        }
+    return acc;
+}
+
+template <int N> __device__ inline void split8(const float (&x)[8], Frag<N> &f)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float r = x[e];
+#pragma unroll
+        for (int p = 0; p < N; ++p) {
+            const bf16 h = (bf16)r;
+            f.p[p][e] = h;
+            if (p + 1 < N) r -= (float)h;
+        }
+    }
+}
+
+// two result tiles as one operand in tile order
+template <int N> __device__ inline void split_tiles(f32x4 lo, f32x4 hi, Frag<N> &f)
+{
+    const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    split8<N>(x, f);
+}
+
+// A matrix in LDS: N planes of ROWS x (COLS + 8) bf16.  (Eight more than COLS: rows begin on 16 bytes and not all in one bank.)
+template <int N, int ROWS, int COLS> struct Tile {
+    static constexpr int LD = COLS + 8, PLANE = ROWS * LD, BYTES = N * PLANE * 2, PLANES = N;
+    bf16 *p;
+    // row r0 + c, steps k0 + 8g ..: the contraction runs along the row
+    __device__ Frag<N> straight(int r0, int k0, int lane) const
+    {
+        Frag<N> f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) f.p[n] = *reinterpret_cast<const bf16x8 *>(p + n * PLANE + (r0 + lane % 16) * LD + k0 + 8 * (lane / 16));
+        return f;
+    }
+    // the same in tile order
+    __device__ Frag<N> tiled(int r0, int k0, int lane) const
+    {
+        Frag<N> f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const bf16 *q = p + n * PLANE + (r0 + lane % 16) * LD + k0 + 4 * (lane / 16);
+            const bf16x4 a = *reinterpret_cast<const bf16x4 *>(q), b = *reinterpret_cast<const bf16x4 *>(q + 16);
+            f.p[n] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        return f;
+    }
+    // column m0 + c, the contraction runs down the rows: 16 lanes fetch 4 rows of 16 and receive them transposed
+    __device__ static bf16x4 down(const bf16 *q)
+    {
+        return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)q));
+    }
+    __device__ Frag<N> straight_down(int k0, int m0, int lane) const
+    {
+        Frag<N> f;
+        const int i = lane % 16;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const bf16 *q = p + n * PLANE + (k0 + 8 * (lane / 16) + i / 4) * LD + m0 + 4 * (i % 4);
+            f.p[n] = __builtin_shufflevector(down(q), down(q + 4 * LD), 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        return f;
+    }
+    __device__ Frag<N> tiled_down(int k0, int m0, int lane) const
+    {
+        Frag<N> f;
+        const int i = lane % 16;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const bf16 *q = p + n * PLANE + (k0 + 4 * (lane / 16) + i / 4) * LD + m0 + 4 * (i % 4);
+            f.p[n] = __builtin_shufflevector(down(q), down(q + 16 * LD), 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        return f;
+    }
+};
+
+// `rows` (of 64) rows of `cols` elements into planes, zeros beyond; norm: 1 / sqrt(sum of squares + eps) of every row (1 beyond).
+// 256 threads; vec: rows may be read 16 bytes at a time.
+template <typename T, int N, int COLS>
+__device__ inline void stage_rows(const Tile<N, CHUNK, COLS> &t, const T *base, long long stride, int rows, int cols, bool vec, float *norm, bool normed, float eps)
+{
+    constexpr int U = COLS / 8;         // units of 8 columns: a row's lie in adjacent lanes
+    for (int u = threadIdx.x; u < CHUNK * U; u += 256) {
+        const int r = u / U, c = u % U * 8;
+        float x[8];
+        const T *src = base + (long long)r * stride + c;
+        if (r < rows && c + 8 <= cols && vec) {
+            if constexpr (sizeof(T) == 2) load_n<T, 8>(src, x);
+            else {
+                float a[4], b[4];
+                load_n<T, 4>(src, a);
+                load_n<T, 4>(src + 4, b);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = r < rows && c + i < cols ? (float)src[i] : 0.f;
+        }
+        if (norm) {
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
+#pragma unroll
+            for (int m = U / 2; m > 0; m >>= 1) s += __shfl_xor(s, m);
+            if (u % U == 0) norm[r] = normed && r < rows ? 1.f / sqrtf(s + eps) : 1.f;
+        }
+        Frag<N> f;
+        split8<N>(x, f);
+#pragma unroll
+        for (int n = 0; n < N; ++n) *reinterpret_cast<bf16x8 *>(t.p + n * Tile<N, CHUNK, COLS>::PLANE + r * Tile<N, CHUNK, COLS>::LD + c) = f.p[n];
+    }
+}
+
+// Per token of a chunk; also what later kernels find in the workspace, in this order
+struct Gates {
+    float gh[CHUNK], gl[CHUNK];     // G in two parts: exact differences, whatever the sum
+    float eg[CHUNK], ed[CHUNK];     // e^G, e^{G_C - G}
+    float beta[CHUNK];
+    float rk[CHUNK], rq[CHUNK];
+    float c[CHUNK];                 // factor of a token's row in the update of the state
+};
+
+constexpr float BETA_MIN = 8.673617379884035e-19f;      // 2^-60: betas nearer to 0 count as this, so that u / beta exists
+
+// Wave 0 fills gh, gl, eg, ed, beta of the chunk that begins at token t0 of row b, head h; `n` of its tokens exist.
+__device__ inline void load_gates(const Args &a, Gates &G, int b, int h, int t0, int n)
+{
+    if (threadIdx.x >= CHUNK) return;
+    const int i = threadIdx.x;
+    const long long at = ((long long)b * a.L + t0 + i) * a.H + h;
+    float g = i < n ? a.decay[at] : 0.f, beta = i < n ? a.beta[at] : 1.f;
+    if (g < DECAY_MIN) g = DECAY_MIN;
+    if (fabsf(beta) < BETA_MIN) beta = copysignf(BETA_MIN, beta);
+    double s = g;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const double o = __shfl_up(s, m);
+        if (i >= m) s += o;
+    }
+    const double total = __shfl(s, 63);
+    G.gh[i] = (float)s;
+    G.gl[i] = (float)(s - (double)(float)s);
+    G.eg[i] = expf((float)s);
+    G.ed[i] = expf((float)(total - s));
+    G.beta[i] = beta;
+}
+
+__device__ inline float decay_between(const Gates &G, int i, int j)
+{
+    return __expf((G.gh[i] - G.gh[j]) + (G.gl[i] - G.gl[j]));
+}
+
+// (I + L)^-1 in place: L strictly lower, 64 x 64 fp32 in LDS, zeros above.  Blocks of 16 by substitution, a column a lane; then
+// [[A,0],[C,B]]^-1 = [[A^-1,0],[-B^-1 C A^-1, B^-1]] twice, on the fp32 matrix instruction (16 x 16 x 4: lane c + 16 g holds step g; the
+// four steps of a call are taken as 4g + s, s = 0..3, so that a result is an operand of the next).  256 threads.
+constexpr int TLD = CHUNK + 4;
+__device__ inline f32x4 mul16(const float *A, f32x4 B, f32x4 acc, int lane)     // A 16 x 16 in LDS, B in result layout
+{
+    const f32x4 a = *reinterpret_cast<const f32x4 *>(A + (lane % 16) * TLD + 4 * (lane / 16));
+#pragma unroll
+    for (int s = 0; s < 4; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s], B[s], acc, 0, 0, 0);
+    return acc;
+}
+__device__ inline f32x4 tile16(const float *A, int lane)        // in result layout
+{
+    f32x4 x;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[r] = A[(4 * (lane / 16) + r) * TLD + lane % 16];
+    return x;
+}
+__device__ inline void put16(float *A, f32x4 x, int lane, float sign)
+{
+#pragma unroll
+    for (int r = 0; r < 4; ++r) A[(4 * (lane / 16) + r) * TLD + lane % 16] = sign * x[r];
+}
+__device__ inline void invert(float *T)
+{
+    const int w = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 16;
+    float *D = T + (16 * w) * TLD + 16 * w;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = i == c ? 1.f : 0.f;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) {
+        float row[16];
+#pragma unroll
+        for (int q = 0; q < (i + 3) / 4; ++q) {
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(D + i * TLD + 4 * q);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) row[4 * q + e] = v[e];
+        }
+#pragma unroll
+        for (int j = 0; j < i; ++j) x[i] = fmaf(-row[j], x[j], x[i]);
+    }
+    __syncthreads();
+    if (lane < 16) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) D[i * TLD + c] = x[i];
+    }
+    __syncthreads();
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    if (w < 2) {
+        float *A = T + 32 * w * TLD + 32 * w;
+        const f32x4 m = mul16(A + 16 * TLD, tile16(A, lane), zero, lane);
+        put16(A + 16 * TLD, mul16(A + 16 * TLD + 16, m, zero, lane), lane, -1.f);
+    }
+    __syncthreads();
+    const int ct = w & 1, rt = w >> 1;
+    f32x4 X[2] = {zero, zero}, out = zero;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+            if (m >= ct) X[kt] = mul16(T + (32 + 16 * kt) * TLD + 16 * m, tile16(T + 16 * m * TLD + 16 * ct, lane), X[kt], lane);
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+        if (kt <= rt) out = mul16(T + (32 + 16 * rt) * TLD + 32 + 16 * kt, X[kt], out, lane);
+    __syncthreads();
+    put16(T + (32 + 16 * rt) * TLD + 16 * ct, out, lane, -1.f);
+    __syncthreads();
+}
+
+// beta_i N_ij of the chunk into T (fp32, zeros on and above the diagonal): wave w makes row tile w
+template <int N, int KP> __device__ inline void system_of(const Tile<N, CHUNK, KP> &k, const Gates &G, float *T)
+{
+    const int w = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 16, g = lane / 16;
+    for (int ct = 0; ct < 4; ++ct) {
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        if (ct <= w) {
+#pragma unroll
+            for (int ks = 0; ks < KP / 32; ++ks) acc = mma<3>(k.straight(16 * w, 32 * ks, lane), k.straight(16 * ct, 32 * ks, lane), acc);
+        }
+        const int j = 16 * ct + c;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 16 * w + 4 * g + r;
+            T[i * TLD + j] = i > j ? acc[r] * (G.beta[i] * G.rk[i] * G.rk[j] * decay_between(G, i, j)) : 0.f;
+        }
+    }
+}
+
+} // namespace delta
+} // namespace cawn
