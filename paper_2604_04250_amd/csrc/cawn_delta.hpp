@@ -69,6 +69,9 @@ int launch_token(const Args &a, bool bf16, hipStream_t s);
 int launch_prepare(const Args &a, bool bf16, hipStream_t s);            // forward: W, K^T, T beta V, gates
 int launch_output(const Args &a, bool bf16, hipStream_t s);             // forward: o
 
+int launch_adjoint(const Args &a, bool bf16, hipStream_t s);            // backward: Wd, K^T, dR0, Y, gates
+int launch_gradients(const Args &a, bool bf16, hipStream_t s);          // backward: every gradient but the state's
+
 // The recurrence over chunks, either direction: X += W S, S = e S + K^T (c X) (+ Y), with S stored ahead of every chunk.
 struct StateArgs {
     int B, L, H, K, V, VT, chunks, c0, c1, span;

@@ -53,6 +53,18 @@ Layout forward_layout(const Args &a, const Sizes &z)
     return l;
 }
 
+Layout backward_layout(const Args &a, const Sizes &z)
+{
+    Layout l;
+    const size_t rows = (size_t)a.B * a.H;
+    l.span = span_of(a, z.bslot);
+    l.slots = rows * l.span * z.bslot;
+    l.states = 0;
+    l.carry = rows * z.st * 1024;
+    l.bytes = l.slots + l.carry;
+    return l;
+}
+
 // states [B H][chunks + 1], then u [B H][chunks], in tiles
 size_t ckpt_bytes(const Args &a, const Sizes &z) { return (size_t)a.B * a.H * ((size_t)(a.chunks + 1) * z.st + (size_t)a.chunks * z.ut) * 1024; }
 
@@ -78,7 +90,8 @@ size_t cawn_delta_workspace_bytes(const cawn_delta_desc *d)
 {
     Args a;
     if (check(d, &a) != CAWN_OK) return 0;
-    const size_t bytes = forward_layout(a, Sizes(a.K, a.V, d->bf16 ? 1 : 3)).bytes;
+    const Sizes z(a.K, a.V, d->bf16 ? 1 : 3);
+    const size_t f = forward_layout(a, z).bytes, r = backward_layout(a, z).bytes, bytes = f > r ? f : r;
     return bytes > 256 ? bytes : 256;
 }
 
@@ -138,7 +151,45 @@ int cawn_delta_rule_bwd(const cawn_delta_desc *d, const void *q, const void *k, 
                         const void *ckpt, const void *dO, const void *dstate_out, void *dq, void *dk, void *dv, float *ddecay, float *dbeta, void *dstate_in,
                         void *workspace, size_t workspace_bytes, void *stream)
 {
-    return CAWN_EUNSUPPORTED;
+    Args a;
+    if (int r = check(d, &a)) return r;
+    if (a.B == 0) return CAWN_OK;
+    if (a.L > 0 && (!q || !k || !v || !decay || !beta || !ckpt || !dO)) return CAWN_EINVAL;
+    if (misaligned(d, q) || misaligned(d, k) || misaligned(d, v) || misaligned(d, dO) || misaligned(d, dq) || misaligned(d, dk) || misaligned(d, dv) ||
+        !aligned_to(decay, 4) || !aligned_to(beta, 4) || !aligned_to(lengths, 4) || !aligned_to(ckpt, 16) || !aligned_to(dstate_out, 4) ||
+        !aligned_to(ddecay, 4) || !aligned_to(dbeta, 4) || !aligned_to(dstate_in, 4)) return CAWN_EINVAL;
+    const int e = d->bf16 ? 2 : 4, w = 16 / e;
+    const Sizes z(a.K, a.V, d->bf16 ? 1 : 3);
+    const Layout l = backward_layout(a, z);
+    if (!workspace || workspace_bytes < l.bytes || !aligned_to(workspace, 256)) return CAWN_EWORKSPACE;
+    if ((long long)a.B * a.H * l.span > 0x7fffffffLL) return CAWN_EUNSUPPORTED;
+    a.q = q, a.k = k, a.v = v, a.decay = decay, a.beta = beta, a.lengths = lengths, a.dO = dO;
+    a.dq = dq, a.dk = dk, a.dv = dv, a.ddecay = ddecay, a.dbeta = dbeta;
+    a.vecq = a.K % w == 0 && a.qst % w == 0 && a.qsb % w == 0 && aligned_to(q, 16) && aligned_to(k, 16);
+    a.veco = a.V % w == 0 && a.ost % w == 0 && a.osb % w == 0 && aligned_to(dO, 16);
+    a.ws = (char *)workspace;
+    a.span = l.span;
+    a.s_tiles = (char *)const_cast<void *>(ckpt), a.s_chunk = (size_t)z.st * 1024, a.s_row = (size_t)(a.chunks + 1) * a.s_chunk;
+    a.u_tiles = a.s_tiles + (size_t)a.B * a.H * a.s_row, a.u_chunk = (size_t)z.ut * 1024, a.u_row = (size_t)a.chunks * a.u_chunk;
+    StateArgs t{};
+    t.B = a.B, t.L = a.L, t.H = a.H, t.K = a.K, t.V = a.V, t.VT = a.VT, t.chunks = a.chunks, t.span = l.span, t.lengths = a.lengths;
+    t.ws = a.ws, t.slot = z.bslot, t.x_at = (size_t)(z.wf + z.kf) * 1024, t.gates_at = t.x_at + (size_t)z.ut * 1024, t.y_at = t.gates_at + 2048;
+    t.s_tiles = a.ws + t.y_at + (size_t)z.st * 1024, t.s_row = (size_t)l.span * z.bslot, t.s_chunk = z.bslot;
+    t.x_tiles = a.ws + t.x_at, t.x_row = t.s_row, t.x_chunk = z.bslot;
+    t.carry = a.ws + l.slots;
+    t.begin = (const float *)dstate_out, t.end = (float *)dstate_in;
+    hipStream_t s = (hipStream_t)stream;
+    for (a.c1 = a.chunks;; a.c1 = a.c0) {       // from the last chunks to the first
+        a.c0 = a.c1 > l.span ? a.c1 - l.span : 0;
+        t.c0 = a.c0, t.c1 = a.c1, t.s_first = t.x_first = a.c0;
+        t.first = a.c1 == a.chunks, t.last = a.c0 == 0;
+        if (a.c1 > a.c0)
+            if (int r = delta::launch_adjoint(a, d->bf16, s)) return r;
+        if (int r = delta::launch_states(t, d->bf16, true, s)) return r;
+        if (a.c1 > a.c0)
+            if (int r = delta::launch_gradients(a, d->bf16, s)) return r;
+        if (a.c0 == 0) return CAWN_OK;
+    }
 }
 
 } // extern "C"

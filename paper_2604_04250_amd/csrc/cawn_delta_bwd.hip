@@ -1,0 +1,533 @@
+// Gated delta rule by chunks, backward.
+//
+// With dS the gradient of the state behind a chunk, dO that of its output, and the forward's S0 and U from the checkpoint:
+//     dR  = T^T (scale P^T dO + KD dS),  KD = diag(e^{G_C - G}) K      gradient of U through everything but T's inverse; dV = beta dR
+//     dS0 = e^{G_C} dS + scale (e^G Q)^T dO - (beta e^G K)^T dR
+//     Z   = scale (dO U^T) o D (lower),  M = -(beta dR U^T) o D (strictly lower)
+//     dQ  = scale e^G dO S0^T + Z K
+//     dK  = -beta e^G dR S0^T + M K + Z^T Q + M^T K + e^{G_C - G} U dS^T
+//     dbeta_i = dR_i . U_i / beta_i
+//     ddecay_t = sum_{i >= t, in the chunk} (q_i . dq_i - v_i . dv_i) + <dS, S_C>
+// The last line: a decay scales all that a later query reads and all that came before it; summed over the places where e^{G_i} stands
+// (queries, keys that read, keys that write) the keys' two shares meet in dR.U and cancel, and what is left is the above.
+//
+// Three kernels, like the forward: what a chunk contributes by itself (delta_adjoint), the recurrence from the last chunk to the first
+// (delta_states, reversed), and the gradients of a chunk (delta_gradients).
+#include <stddef.h>
+
+#include "cawn_delta_mfma.hpp"
+
+namespace cawn {
+namespace delta {
+
+// LDS of delta_adjoint, offsets in bytes: k, q, dO, the triangular system, and the operands of P^T and T^T (4 x 2 x 3 pieces each).
+// Three planes of 128 columns leave no room for all at once: dO and T^T then take the place of k behind its last use.
+template <int NP, int KP> struct AdjointLds {
+    static constexpr bool TIGHT = NP == 3 && KP == 128;
+    static constexpr int KB = Tile<NP, CHUNK, KP>::BYTES, OPS = 4 * 2 * 3 * 1024;
+    static constexpr int Q = KB, M = 2 * KB, P = M + CHUNK * TLD * 4, T = TIGHT ? 0 : P + OPS, D = T + OPS;
+    static constexpr int BYTES = TIGHT ? P + OPS : D + Tile<NP, CHUNK, 64>::BYTES;
+    static_assert(!TIGHT || D + Tile<NP, CHUNK, 64>::BYTES <= KB, "behind k's last use");
+};
+
+// Operands and tiles of the reversed delta_states: Wd = T^T KD, K^T, dR0 = T^T scale P^T dO, Y = scale (e^G Q)^T dO, gates.
+template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void delta_adjoint(const Args a)
+{
+    constexpr int KS = KP / 32, KT = KP / 16;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ Gates G;
+    const int blk = blockIdx.x, n = a.c0 + blk % (a.c1 - a.c0), bh = blk / (a.c1 - a.c0), h = bh % a.H, b = bh / a.H;
+    const int len = row_length(a, b), t0 = n * CHUNK, rows = min(CHUNK, len - t0);
+    if (rows <= 0) return;
+    const Sizes z(a.K, a.V, NP);
+    char *slot = a.ws + ((size_t)bh * a.span + (n - a.c0)) * z.bslot;
+    using A = AdjointLds<NP, KP>;
+    const Tile<NP, CHUNK, KP> k{(bf16 *)lds}, q{(bf16 *)(lds + A::Q)};
+    const Tile<NP, CHUNK, 64> d{(bf16 *)(lds + A::D)};
+    float *M = (float *)(lds + A::M);
+    bf16x8 *pf = reinterpret_cast<bf16x8 *>(lds + A::P), *tf = reinterpret_cast<bf16x8 *>(lds + A::T);
+    const int w = threadIdx.x / 64, lane = threadIdx.x % 64, g = lane / 16, c = lane % 16;
+    const long long qat = b * a.qsb + t0 * a.qst + (long long)(h / (a.H / a.Hk)) * a.K;
+    const T *dop = (const T *)a.dO + b * a.osb + t0 * a.ost + (long long)h * a.V;
+    stage_rows<T, NP, KP>(k, (const T *)a.k + qat, a.qst, rows, a.K, a.vecq, G.rk, a.norm, a.eps);
+    stage_rows<T, NP, KP>(q, (const T *)a.q + qat, a.qst, rows, a.K, a.vecq, G.rq, a.norm, a.eps);
+    if (!A::TIGHT) stage_rows<T, NP, 64>(d, dop, a.ost, rows, min(64, a.V), a.veco, nullptr, false, 0.f);
+    load_gates(a, G, b, h, t0, rows);
+    __syncthreads();
+    if (threadIdx.x < CHUNK) G.c[threadIdx.x] = -(G.beta[threadIdx.x] * G.eg[threadIdx.x] * G.rk[threadIdx.x]);
+    system_of<NP, KP>(k, G, M);
+    // column tile w of scale P: result layout has the rows i that the product P^T dO runs over
+    {
+        f32x4 p[4];
+        const int j = 16 * w + c;
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            p[it] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (it < w) continue;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) p[it] = mma<3>(q.straight(16 * it, 32 * ks, lane), k.straight(16 * w, 32 * ks, lane), p[it]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * it + 4 * g + r;
+                p[it][r] = i >= j ? p[it][r] * (a.scale * G.rq[i] * G.rk[j] * decay_between(G, i, j)) : 0.f;
+            }
+        }
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            Frag<3> f;
+            split_tiles<3>(p[2 * ks], p[2 * ks + 1], f);
+#pragma unroll
+            for (int e = 0; e < 3; ++e) pf[((w * 2 + ks) * 3 + e) * 64 + lane] = f.p[e];
+        }
+    }
+    __syncthreads();
+    {
+        float *out = (float *)(slot + (size_t)(z.wf + z.kf + z.ut) * 1024);
+        for (int i = threadIdx.x; i < (int)(sizeof(Gates) / 4); i += 256) out[i] = ((const float *)&G)[i];
+        bf16x8 *kt = reinterpret_cast<bf16x8 *>(slot + (size_t)z.wf * 1024) + lane;
+        for (int u = w; u < KT * 2; u += 4) {
+            const Frag<NP> f = k.tiled_down(32 * (u % 2), 16 * (u / 2), lane);
+#pragma unroll
+            for (int p = 0; p < NP; ++p) kt[(u * NP + p) * 64] = f.p[p];
+        }
+    }
+    invert(M);
+    {
+        // row tile w of T^T: plain for dR0 (shared), rows of KD scaled for Wd (own)
+        Frag<3> tw[2], tt[2];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            float x[8], xw[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = 32 * ks + 16 * (e / 4) + 4 * g + e % 4;
+                x[e] = M[i * TLD + 16 * w + c];
+                xw[e] = x[e] * (G.ed[i] * G.rk[i]);
+            }
+            split8<3>(x, tt[ks]);
+            split8<3>(xw, tw[ks]);
+        }
+        bf16x8 *wf = reinterpret_cast<bf16x8 *>(slot) + lane;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            f32x4 acc[2];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                acc[half] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (w < 2) acc[half] = mma<3>(k.tiled_down(0, 32 * ks + 16 * half, lane), tw[0], acc[half]);
+                acc[half] = mma<3>(k.tiled_down(32, 32 * ks + 16 * half, lane), tw[1], acc[half]);
+            }
+            Frag<3> f;
+            split_tiles<3>(acc[0], acc[1], f);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) wf[((w * KS + ks) * 3 + p) * 64] = f.p[p];
+        }
+        if (A::TIGHT) __syncthreads();
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int e = 0; e < 3; ++e) tf[((w * 2 + ks) * 3 + e) * 64 + lane] = tt[ks].p[e];
+        if (A::TIGHT) stage_rows<T, NP, 64>(d, dop, a.ost, rows, min(64, a.V), a.veco, nullptr, false, 0.f);
+    }
+    __syncthreads();
+    char *x0 = slot + (size_t)(z.wf + z.kf) * 1024 + lane * 16, *y0 = slot + (size_t)(z.wf + z.kf + z.ut + 2) * 1024 + lane * 16;
+    for (int v0 = 0; v0 < a.V; v0 += 64) {
+        if (v0 > 0) {
+            __syncthreads();
+            stage_rows<T, NP, 64>(d, dop + v0, a.ost, rows, min(64, a.V - v0), a.veco, nullptr, false, 0.f);
+            __syncthreads();
+        }
+        const int vt = v0 / 16 + w;             // a wave's own column tile, all rows of it
+        if (vt >= a.VT) continue;
+        Frag<NP> df[2];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) df[ks] = d.tiled_down(32 * ks, 16 * w, lane);
+        auto op = [&](const bf16x8 *base, int t, int ks) {
+            Frag<3> f;
+#pragma unroll
+            for (int e = 0; e < 3; ++e) f.p[e] = base[((t * 2 + ks) * 3 + e) * 64 + lane];
+            return f;
+        };
+        f32x4 Y[4];
+#pragma unroll
+        for (int jt = 0; jt < 4; ++jt) {
+            Y[jt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (jt < 2) Y[jt] = mma<3>(op(pf, jt, 0), df[0], Y[jt]);
+            Y[jt] = mma<3>(op(pf, jt, 1), df[1], Y[jt]);
+        }
+        Frag<3> yf[2];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) split_tiles<3>(Y[2 * ks], Y[2 * ks + 1], yf[ks]);
+#pragma unroll
+        for (int jt = 0; jt < 4; ++jt) {
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+            if (jt < 2) acc = mma<3>(op(tf, jt, 0), yf[0], acc);
+            acc = mma<3>(op(tf, jt, 1), yf[1], acc);
+            *reinterpret_cast<f32x4 *>(x0 + ((size_t)jt * a.VT + vt) * 1024) = acc;
+        }
+        // Y: rows of dO scaled in fp32
+        Frag<3> sf[2];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = 32 * ks + 16 * (e / 4) + 4 * g + e % 4;
+                float s = 0.f;
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p) s += (float)df[ks].p[p][e];
+                x[e] = s * (a.scale * G.rq[i] * G.eg[i]);
+            }
+            split8<3>(x, sf[ks]);
+        }
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) acc = mma<3>(q.tiled_down(32 * ks, 16 * t, lane), sf[ks], acc);
+            *reinterpret_cast<f32x4 *>(y0 + ((size_t)t * a.VT + vt) * 1024) = acc;
+        }
+    }
+}
+
+// Gradients of a chunk.  A workgroup takes all value heads of a key head, one after the other, and keeps dq and dk in registers: wave w
+// rows 16 w .. of them.  First everything that runs over the value columns, 32 at a time, with U, dR, S0 and dS in LDS as they come
+// from their tiles (a tile's lane holds four rows of a column: a matrix is kept as its transpose, and read down); then, in the same
+// LDS, Z and M with q and k.
+// dq carries ddecay and takes full precision; dk of a bf16 call takes two planes (16 bits) of its operands.
+template <typename T, int NP, int KP> struct GradLds {
+    static constexpr int PK = NP == 1 ? 2 : 3;          // planes of what only dk needs
+    using MatU = Tile<3, 32, 64>;
+    using MatR = Tile<3, 32, 64>;
+    using MatS = Tile<3, 32, KP>;
+    using MatD = Tile<PK, 32, KP>;
+    using MatO = Tile<NP, CHUNK, 32>;
+    using MatQ = Tile<NP, CHUNK, KP>;
+    using MatZ = Tile<3, CHUNK, CHUNK>;
+    using MatM = Tile<PK, CHUNK, CHUNK>;
+    static constexpr int FIRST = MatU::BYTES + MatR::BYTES + MatS::BYTES + MatD::BYTES + MatO::BYTES;
+    static constexpr int SECOND = 2 * MatQ::BYTES + MatZ::BYTES + MatM::BYTES;
+    static constexpr int BYTES = FIRST > SECOND ? FIRST : SECOND;
+};
+
+// four rows of a column, N planes, into a transposed matrix
+template <int N, int ROWS, int COLS> __device__ inline void put_column(const Tile<N, ROWS, COLS> &t, int col, int row0, f32x4 x)
+{
+    float r[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+        bf16x4 h;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            h[i] = (bf16)r[i];
+            r[i] -= (float)h[i];
+        }
+        *reinterpret_cast<bf16x4 *>(t.p + p * Tile<N, ROWS, COLS>::PLANE + col * Tile<N, ROWS, COLS>::LD + row0) = h;
+    }
+}
+
+// sum over the 16 lanes of a result tile's row
+__device__ inline float row_sum(float x)
+{
+#pragma unroll
+    for (int m = 8; m > 0; m >>= 1) x += __shfl_xor(x, m);
+    return x;
+}
+
+template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void delta_gradients(const Args a)
+{
+    using L = GradLds<T, NP, KP>;
+    constexpr int KT = KP / 16, PK = L::PK;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ Gates G;
+    __shared__ float qdq[CHUNK], vdv[CHUNK], udr[CHUNK], part[4];
+    const int blk = blockIdx.x, n = a.c0 + blk % (a.c1 - a.c0), bk = blk / (a.c1 - a.c0), hk = bk % a.Hk, b = bk / a.Hk, rep = a.H / a.Hk;
+    const int len = row_length(a, b), t0 = n * CHUNK, rows = min(CHUNK, len - t0), all = min(CHUNK, a.L - t0);
+    const long long qat = b * a.qsb + t0 * a.qst + (long long)hk * a.K;
+    const int w = threadIdx.x / 64, lane = threadIdx.x % 64, g = lane / 16, c = lane % 16;
+    if (rows <= 0) {                            // tokens that the row does not have
+        for (int i = threadIdx.x; i < all * a.K; i += 256) {
+            const long long at = qat + (long long)(i / a.K) * a.qst + i % a.K;
+            if (a.dq) ((T *)a.dq)[at] = (T)0.f;
+            if (a.dk) ((T *)a.dk)[at] = (T)0.f;
+        }
+        for (int hh = 0; hh < rep; ++hh) {
+            const int h = hk * rep + hh;
+            if (a.dv)
+                for (int i = threadIdx.x; i < all * a.V; i += 256) ((T *)a.dv)[b * a.vsb + (t0 + i / a.V) * a.vst + (long long)h * a.V + i % a.V] = (T)0.f;
+            if ((int)threadIdx.x < all) {
+                const long long at = ((long long)b * a.L + t0 + threadIdx.x) * a.H + h;
+                if (a.ddecay) a.ddecay[at] = 0.f;
+                if (a.dbeta) a.dbeta[at] = 0.f;
+            }
+        }
+        return;
+    }
+    const Sizes z(a.K, a.V, NP);
+    const typename L::MatU ut{(bf16 *)lds};
+    const typename L::MatR rt{(bf16 *)(lds + L::MatU::BYTES)};
+    const typename L::MatS st{(bf16 *)(lds + L::MatU::BYTES + L::MatR::BYTES)};
+    const typename L::MatD dt{(bf16 *)(lds + L::MatU::BYTES + L::MatR::BYTES + L::MatS::BYTES)};
+    const typename L::MatO ot{(bf16 *)(lds + L::MatU::BYTES + L::MatR::BYTES + L::MatS::BYTES + L::MatD::BYTES)};
+    const typename L::MatQ qm{(bf16 *)lds}, km{(bf16 *)(lds + L::MatQ::BYTES)};
+    const typename L::MatZ zm{(bf16 *)(lds + 2 * L::MatQ::BYTES)};
+    const typename L::MatM mm{(bf16 *)(lds + 2 * L::MatQ::BYTES + L::MatZ::BYTES)};
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    f32x4 dq[KT], dk[KT];
+#pragma unroll
+    for (int t = 0; t < KT; ++t) dq[t] = dk[t] = zero;
+    for (int hh = 0; hh < rep; ++hh) {
+        const int h = hk * rep + hh, bh = b * a.H + h;
+        const char *slot = a.ws + ((size_t)bh * a.span + (n - a.c0)) * z.bslot;
+        const char *sp = a.s_tiles + bh * a.s_row + (n - a.s_first) * a.s_chunk, *up = a.u_tiles + bh * a.u_row + (n - a.u_first) * a.u_chunk;
+        const char *rp = slot + (size_t)(z.wf + z.kf) * 1024, *dp = slot + (size_t)(z.wf + z.kf + z.ut + 2 + z.st) * 1024;
+        __syncthreads();                        // the previous head's LDS
+        {
+            const float *in = (const float *)(slot + (size_t)(z.wf + z.kf + z.ut) * 1024);
+            for (int i = threadIdx.x; i < (int)(sizeof(Gates) / 4); i += 256) ((float *)&G)[i] = in[i];
+        }
+        if (threadIdx.x < CHUNK) vdv[threadIdx.x] = udr[threadIdx.x] = 0.f;
+        f32x4 A1[KT], A2[KT], A3[KT], zt[4], mt[4];
+#pragma unroll
+        for (int t = 0; t < KT; ++t) A1[t] = A2[t] = A3[t] = zero;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) zt[t] = mt[t] = zero;
+        float inner = 0.f;                      // <dS, S_C>
+        float sv[4] = {0.f, 0.f, 0.f, 0.f}, su[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int v0 = 0; v0 < a.V; v0 += 32) {
+            __syncthreads();
+            // wave w: row tile w of U and dR; row tiles w, w + 4 of S0 and dS
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int vt = v0 / 16 + half, v = 16 * vt + c;
+                const bool there = vt < a.VT;
+                f32x4 u = zero, r = zero;
+                if (there) {
+                    u = *reinterpret_cast<const f32x4 *>(up + ((size_t)w * a.VT + vt) * 1024 + lane * 16);
+                    r = *reinterpret_cast<const f32x4 *>(rp + ((size_t)w * a.VT + vt) * 1024 + lane * 16);
+                }
+                put_column(ut, 16 * half + c, 16 * w + 4 * g, u);
+                put_column(rt, 16 * half + c, 16 * w + 4 * g, r);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = 16 * w + 4 * g + e;
+                    su[e] += u[e] * r[e];
+                    const float dv = G.beta[i] * r[e];
+                    if (v < a.V && i < all) {
+                        const long long at = b * a.vsb + (t0 + i) * a.vst + (long long)h * a.V + v;
+                        if (i < rows) sv[e] += (float)((const T *)a.v)[at] * dv;
+                        if (a.dv) ((T *)a.dv)[at] = (T)(i < rows ? dv : 0.f);
+                    }
+                }
+#pragma unroll
+                for (int t = w; t < KT; t += 4) {
+                    f32x4 s = zero, d = zero, e = zero;
+                    if (there) {
+                        s = *reinterpret_cast<const f32x4 *>(sp + ((size_t)t * a.VT + vt) * 1024 + lane * 16);
+                        e = *reinterpret_cast<const f32x4 *>(sp + a.s_chunk + ((size_t)t * a.VT + vt) * 1024 + lane * 16);
+                        d = *reinterpret_cast<const f32x4 *>(dp + ((size_t)t * a.VT + vt) * 1024 + lane * 16);
+                    }
+                    put_column(st, 16 * half + c, 16 * t + 4 * g, s);
+                    put_column(dt, 16 * half + c, 16 * t + 4 * g, d);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) inner += d[x] * e[x];
+                }
+            }
+            stage_rows<T, NP, 32>(ot, (const T *)a.dO + b * a.osb + t0 * a.ost + (long long)h * a.V + v0, a.ost, rows, min(32, a.V - v0), a.veco, nullptr, false, 0.f);
+            __syncthreads();
+            const Frag<NP> o = ot.straight(16 * w, 0, lane);
+            const Frag<3> r = rt.straight_down(0, 16 * w, lane);
+            Frag<PK> u;
+            {
+                const Frag<3> u3 = ut.straight_down(0, 16 * w, lane);
+#pragma unroll
+                for (int p = 0; p < PK; ++p) u.p[p] = u3.p[p];
+            }
+            // Z^T and M^T (before their factors): rows j, column i = c of row tile w
+#pragma unroll
+            for (int jt = 0; jt < 4; ++jt) {
+                if (jt > w) break;
+                const Frag<3> uj = ut.straight_down(0, 16 * jt, lane);
+                zt[jt] = mma<3>(uj, o, zt[jt]);
+                mt[jt] = mma<PK>(uj, r, mt[jt]);
+            }
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                const Frag<3> s = st.straight_down(0, 16 * t, lane);
+                A1[t] = mma<3>(o, s, A1[t]);
+                A2[t] = mma<PK>(r, s, A2[t]);
+                A3[t] = mma<PK>(u, dt.straight_down(0, 16 * t, lane), A3[t]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float s = row_sum(sv[e]), t = row_sum(su[e]);
+            if (c == 0) vdv[16 * w + 4 * g + e] = s, udr[16 * w + 4 * g + e] = t;
+        }
+#pragma unroll
+        for (int m = 32; m > 0; m >>= 1) inner += __shfl_xor(inner, m);
+        if (lane == 0) part[w] = inner;
+        __syncthreads();                        // the LDS of the first half is free
+        stage_rows<T, NP, KP>(qm, (const T *)a.q + qat, a.qst, rows, a.K, a.vecq, nullptr, false, 0.f);
+        stage_rows<T, NP, KP>(km, (const T *)a.k + qat, a.qst, rows, a.K, a.vecq, nullptr, false, 0.f);
+        {
+            const int i = 16 * w + c;
+#pragma unroll
+            for (int jt = 0; jt < 4; ++jt) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int j = 16 * jt + 4 * g + r;
+                    const float D = i >= j ? decay_between(G, i, j) : 0.f;
+                    zt[jt][r] = i >= j ? zt[jt][r] * (a.scale * D) : 0.f;
+                    mt[jt][r] = i > j ? -mt[jt][r] * (G.beta[i] * D) : 0.f;
+                }
+                put_column(zm, i, 16 * jt + 4 * g, zt[jt]);     // (here the column of the transpose is the row)
+                put_column(mm, i, 16 * jt + 4 * g, mt[jt]);
+            }
+        }
+        __syncthreads();
+        // dq^ = scale e^G A1 + Z (rk k);  dk^ = -beta e^G A2 + e^{G_C - G} A3 + M (rk k) + Z^T (rq q) + M^T (rk k): the norms' factors of the
+        // summed tokens scale Z's and M's columns (rows), so they are applied to the operand
+        auto scaled = [&](auto f, const float *by, int k0) {     // f's eight steps times by[step]
+            constexpr int N = sizeof(f) / 16;
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float s = 0.f;
+#pragma unroll
+                for (int p = N - 1; p >= 0; --p) s += (float)f.p[p][e];
+                x[e] = s * by[k0 + 8 * g + e];
+            }
+            decltype(f) y;
+            split8<N>(x, y);
+            return y;
+        };
+        f32x4 q1[KT];
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * w + 4 * g + r;
+                q1[t][r] = a.scale * G.eg[i] * A1[t][r];
+                A2[t][r] = G.ed[i] * A3[t][r] - G.beta[i] * G.eg[i] * A2[t][r];
+            }
+        }
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            if (2 * ks <= w) {
+                const Frag<3> zf = scaled(zm.straight(16 * w, 32 * ks, lane), G.rk, 32 * ks);
+                const Frag<PK> mf = scaled(mm.straight(16 * w, 32 * ks, lane), G.rk, 32 * ks);
+#pragma unroll
+                for (int t = 0; t < KT; ++t) {
+                    const Frag<NP> kf = km.straight_down(32 * ks, 16 * t, lane);
+                    q1[t] = mma<3>(zf, kf, q1[t]);
+                    A2[t] = mma<PK>(mf, kf, A2[t]);
+                }
+            }
+            if (2 * ks + 1 >= w) {
+                const Frag<3> zf = scaled(zm.straight_down(32 * ks, 16 * w, lane), G.rq, 32 * ks);
+                const Frag<PK> mf = scaled(mm.straight_down(32 * ks, 16 * w, lane), G.rk, 32 * ks);
+#pragma unroll
+                for (int t = 0; t < KT; ++t) {
+                    A2[t] = mma<PK>(zf, qm.straight_down(32 * ks, 16 * t, lane), A2[t]);
+                    A2[t] = mma<PK>(mf, km.straight_down(32 * ks, 16 * t, lane), A2[t]);
+                }
+            }
+        }
+        // q . dq of this head, from the planes of q
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 16 * w + 4 * g + r;
+            float s = 0.f;
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                float x = 0.f;
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p) x += (float)qm.p[p * L::MatQ::PLANE + i * L::MatQ::LD + 16 * t + c];
+                s += x * q1[t][r];
+                dq[t][r] += q1[t][r];
+                dk[t][r] += A2[t][r];
+            }
+            s = row_sum(s) * G.rq[i];
+            if (c == 0) qdq[i] = s;
+        }
+        __syncthreads();
+        if (threadIdx.x < CHUNK) {
+            const int i = threadIdx.x;
+            float s = i < rows ? qdq[i] - vdv[i] : 0.f;
+#pragma unroll
+            for (int m = 1; m < 64; m <<= 1) {          // sum over the tokens behind
+                const float o = __shfl_down(s, m);
+                if (i + m < 64) s += o;
+            }
+            s += (part[0] + part[1]) + (part[2] + part[3]);
+            if (i < all) {
+                const long long at = ((long long)b * a.L + t0 + i) * a.H + h;
+                // (a complete forgetting hangs on nothing; the sum would leave its rounding)
+                if (a.ddecay) a.ddecay[at] = i < rows && !(a.decay[at] < DECAY_MIN) ? s : 0.f;
+                if (a.dbeta) a.dbeta[at] = i < rows ? udr[i] / G.beta[i] : 0.f;
+            }
+        }
+    }
+    // through the norm, and out: dx = r (dx^ - x^ (x^ . dx^))
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        T *out = (T *)(which ? a.dk : a.dq);
+        if (!out) continue;
+        const typename L::MatQ &xm = which ? km : qm;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 16 * w + 4 * g + r;
+            const float f = which ? G.rk[i] : G.rq[i];
+            float x[KT], s = 0.f;
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                x[t] = 0.f;
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p) x[t] += (float)xm.p[p * L::MatQ::PLANE + i * L::MatQ::LD + 16 * t + c];
+                s += x[t] * (which ? dk[t][r] : dq[t][r]);
+            }
+            s = a.norm ? row_sum(s) * f * f : 0.f;
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                const int col = 16 * t + c;
+                if (i < all && col < a.K) out[qat + (long long)i * a.qst + col] = (T)(i < rows ? f * ((which ? dk[t][r] : dq[t][r]) - x[t] * s) : 0.f);
+            }
+        }
+    }
+}
+
+template <typename T, int NP, int KP> static int adjoint_kp(const Args &a, hipStream_t s)
+{
+    constexpr int bytes = AdjointLds<NP, KP>::BYTES;
+    static_assert(bytes + sizeof(Gates) <= 163840, "LDS");
+    if (hipFuncSetAttribute((const void *)delta_adjoint<T, NP, KP>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CAWN_ELAUNCH;
+    hipLaunchKernelGGL((delta_adjoint<T, NP, KP>), dim3((unsigned)((long long)a.B * a.H * (a.c1 - a.c0))), dim3(256), bytes, s, a);
+    return launched();
+}
+
+template <typename T, int NP, int KP> static int gradients_kp(const Args &a, hipStream_t s)
+{
+    constexpr int bytes = GradLds<T, NP, KP>::BYTES;
+    static_assert(bytes + sizeof(Gates) + 1024 <= 163840, "LDS");
+    if (hipFuncSetAttribute((const void *)delta_gradients<T, NP, KP>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CAWN_ELAUNCH;
+    hipLaunchKernelGGL((delta_gradients<T, NP, KP>), dim3((unsigned)((long long)a.B * a.Hk * (a.c1 - a.c0))), dim3(256), bytes, s, a);
+    return launched();
+}
+
+int launch_adjoint(const Args &a, bool bf16_, hipStream_t s)
+{
+    if (a.K <= 32) return bf16_ ? adjoint_kp<bf16, 1, 32>(a, s) : adjoint_kp<float, 3, 32>(a, s);
+    if (a.K <= 64) return bf16_ ? adjoint_kp<bf16, 1, 64>(a, s) : adjoint_kp<float, 3, 64>(a, s);
+    return bf16_ ? adjoint_kp<bf16, 1, 128>(a, s) : adjoint_kp<float, 3, 128>(a, s);
+}
+
+int launch_gradients(const Args &a, bool bf16_, hipStream_t s)
+{
+    if (a.K <= 32) return bf16_ ? gradients_kp<bf16, 1, 32>(a, s) : gradients_kp<float, 3, 32>(a, s);
+    if (a.K <= 64) return bf16_ ? gradients_kp<bf16, 1, 64>(a, s) : gradients_kp<float, 3, 64>(a, s);
+    return bf16_ ? gradients_kp<bf16, 1, 128>(a, s) : gradients_kp<float, 3, 128>(a, s);
+}
+
+} // namespace delta
+} // namespace cawn
