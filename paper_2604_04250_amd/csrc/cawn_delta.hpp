@@ -9,6 +9,7 @@ using namespace cawn::ops;
 
 constexpr int CHUNK = 64;           // tokens treated at once by the chunked kernels
 constexpr int TOKEN_MAX = 16;       // longest call that goes token by token
+constexpr int GATE_FLOATS = 5 * CHUNK;
 constexpr float DECAY_MIN = -104.f; // exp underflows to 0 below: a decay of minus infinity counts as this, so that sums of decays stay finite
 
 struct Args {
@@ -38,6 +39,11 @@ struct Args {
     char *s_tiles, *u_tiles;
     size_t s_row, s_chunk, u_row, u_chunk;
     int s_first, u_first;
+    // Segments of seg_chunks chunks; per head and chunk GATE_FLOATS gates; per head and segment the matrix A (KP x KP, row-major),
+    // the offset b and the state at its begin, in tiles
+    int segments, seg_chunks;
+    float *gates;
+    char *seg_a, *seg_b, *seg_s;
 };
 
 // Sizes in the chunked form; everything is made of 1 KiB pieces: a matrix operand's plane (64 lanes x 8 bf16) or an fp32 tile
@@ -66,8 +72,9 @@ __device__ inline int row_length(const Args &a, int b)
 }
 
 int launch_token(const Args &a, bool bf16, hipStream_t s);
-int launch_prepare(const Args &a, bool bf16, hipStream_t s);            // forward: W, K^T, T beta V, gates
-int launch_output(const Args &a, bool bf16, hipStream_t s);             // forward: o
+int launch_gates(const Args &a, hipStream_t s);
+int launch_scan(const Args &a, bool bf16, hipStream_t s);               // forward, behind the gates
+int launch_join(const Args &a, bool reverse, hipStream_t s);
 
 int launch_adjoint(const Args &a, bool bf16, hipStream_t s);            // backward: Wd, K^T, dR0, Y, gates
 int launch_gradients(const Args &a, bool bf16, hipStream_t s);          // backward: every gradient but the state's

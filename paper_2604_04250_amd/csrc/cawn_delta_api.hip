@@ -12,6 +12,21 @@ namespace {
 
 constexpr size_t SPAN_BYTES = 128u << 20;
 
+// How a row's chunks are cut into segments.  A segment costs each of its chunks twice (what it makes of a state, then its outputs) and
+// one link of the join, so two segments gain nothing; many shorten the two passes until the chip is full or the links cost as much.
+void cut(Args *a)
+{
+    const long long groups = (long long)a->B * a->H * ceil_div(a->VT, 4);
+    const long long want = groups > 0 ? 768 / groups : 1;
+    a->segments = 1, a->seg_chunks = a->chunks;
+    if (want < 3 || a->chunks < 6) return;
+    long long m = ceil_div(a->chunks, want);
+    while (m * m * 13 < a->chunks) ++m;
+    const long long segments = ceil_div(a->chunks, m);
+    if (segments < 3) return;
+    a->segments = (int)segments, a->seg_chunks = (int)m;
+}
+
 int check(const cawn_delta_desc *d, Args *a)
 {
     if (!d || d->B < 0 || d->L < 0 || d->H <= 0 || d->Hk < 0 || d->K <= 0 || d->V <= 0 || (d->bf16 & ~1) || (d->qk_norm & ~1)) return CAWN_EINVAL;
@@ -29,6 +44,7 @@ int check(const cawn_delta_desc *d, Args *a)
     a->chunks = (int)ceil_div(d->L, delta::CHUNK);
     a->VT = (int)ceil_div(d->V, 16);
     if ((long long)d->B * d->H * ceil_div(d->V, 16) > 0x7fffffffLL) return CAWN_EUNSUPPORTED;
+    cut(a);
     return CAWN_OK;
 }
 
@@ -40,26 +56,25 @@ int span_of(const Args &a, size_t per_chunk)
     return (int)(room < 1 ? 1 : room < a.chunks ? room : a.chunks > 1 ? a.chunks : 1);
 }
 
-struct Layout { size_t slots, states, carry, bytes; int span; };
+struct Layout { size_t gates, a, b, s, slots, carry, bytes; int span; };
 Layout forward_layout(const Args &a, const Sizes &z)
 {
-    Layout l;
+    Layout l{};
     const size_t rows = (size_t)a.B * a.H;
-    l.span = span_of(a, z.slot + (size_t)z.st * 1024);
-    l.slots = rows * l.span * z.slot;
-    l.states = rows * l.span * z.st * 1024;
-    l.carry = rows * z.st * 1024;
-    l.bytes = l.slots + l.states + l.carry;
+    l.gates = 0;
+    l.a = (rows * a.chunks * delta::GATE_FLOATS * 4 + 1023) / 1024 * 1024;
+    l.b = l.a + (a.segments > 1 ? rows * a.segments * z.KP * z.KP * 4 : 0);
+    l.s = l.b + (a.segments > 1 ? rows * a.segments * z.st * 1024 : 0);
+    l.bytes = l.s + (a.segments > 1 ? rows * a.segments * z.st * 1024 : 0);
     return l;
 }
 
 Layout backward_layout(const Args &a, const Sizes &z)
 {
-    Layout l;
+    Layout l{};
     const size_t rows = (size_t)a.B * a.H;
     l.span = span_of(a, z.bslot);
     l.slots = rows * l.span * z.bslot;
-    l.states = 0;
     l.carry = rows * z.st * 1024;
     l.bytes = l.slots + l.carry;
     return l;
@@ -113,38 +128,17 @@ int cawn_delta_rule_fwd(const cawn_delta_desc *d, const void *q, const void *k, 
     const Sizes z(a.K, a.V, d->bf16 ? 1 : 3);
     const Layout l = forward_layout(a, z);
     if (!workspace || workspace_bytes < l.bytes || !aligned_to(workspace, 256)) return CAWN_EWORKSPACE;
-    if ((long long)a.B * a.H * l.span > 0x7fffffffLL) return CAWN_EUNSUPPORTED;
+    if ((long long)a.B * a.H * (a.segments > a.chunks ? a.segments : a.chunks) * ceil_div(a.VT + z.KP / 16, 4) > 0x7fffffffLL) return CAWN_EUNSUPPORTED;
     a.vecq = a.K % w == 0 && a.qst % w == 0 && a.qsb % w == 0 && aligned_to(q, 16) && aligned_to(k, 16);
-    a.vecv = a.V % w == 0 && a.vst % w == 0 && a.vsb % w == 0 && aligned_to(v, 16);
     a.veco = a.V % 4 == 0 && a.ost % 4 == 0 && a.osb % 4 == 0 && aligned_to(o, 4 * e);
-    a.ws = (char *)workspace;
-    a.span = l.span;
-    StateArgs t{};
-    t.B = a.B, t.L = a.L, t.H = a.H, t.K = a.K, t.V = a.V, t.VT = a.VT, t.chunks = a.chunks, t.span = l.span, t.lengths = a.lengths;
-    t.ws = a.ws, t.slot = z.slot, t.x_at = (size_t)(z.wf + z.kf) * 1024, t.gates_at = (size_t)(z.wf + z.kf + z.ut) * 1024;
-    t.carry = a.ws + l.slots + l.states;
-    t.begin = a.state_in, t.end = a.state_out;
+    char *ws = (char *)workspace;
+    a.gates = (float *)ws, a.seg_a = ws + l.a, a.seg_b = ws + l.b, a.seg_s = ws + l.s;
     if (ckpt) {
         a.s_tiles = (char *)ckpt, a.s_chunk = (size_t)z.st * 1024, a.s_row = (size_t)(a.chunks + 1) * a.s_chunk;
         a.u_tiles = a.s_tiles + (size_t)a.B * a.H * a.s_row, a.u_chunk = (size_t)z.ut * 1024, a.u_row = (size_t)a.chunks * a.u_chunk;
-        t.keep_end = 1;
-    } else {            // u takes the place of T beta V
-        a.s_tiles = a.ws + l.slots, a.s_chunk = (size_t)z.st * 1024, a.s_row = (size_t)l.span * a.s_chunk;
-        a.u_tiles = a.ws + t.x_at, a.u_chunk = z.slot, a.u_row = (size_t)l.span * z.slot;
     }
-    t.s_tiles = a.s_tiles, t.s_row = a.s_row, t.s_chunk = a.s_chunk, t.x_tiles = a.u_tiles, t.x_row = a.u_row, t.x_chunk = a.u_chunk;
-    for (a.c0 = 0; a.c0 == 0 || a.c0 < a.chunks; a.c0 += l.span) {
-        a.c1 = a.c0 + l.span < a.chunks ? a.c0 + l.span : a.chunks;
-        a.s_first = a.u_first = ckpt ? 0 : a.c0;
-        t.c0 = a.c0, t.c1 = a.c1, t.s_first = t.x_first = a.s_first;
-        t.first = a.c0 == 0, t.last = a.c1 == a.chunks;
-        if (a.c1 > a.c0)
-            if (int r = delta::launch_prepare(a, d->bf16, s)) return r;
-        if (int r = delta::launch_states(t, d->bf16, false, s)) return r;
-        if (a.c1 > a.c0)
-            if (int r = delta::launch_output(a, d->bf16, s)) return r;
-    }
-    return CAWN_OK;
+    if (int r = delta::launch_gates(a, s)) return r;
+    return delta::launch_scan(a, d->bf16, s);
 }
 
 int cawn_delta_rule_bwd(const cawn_delta_desc *d, const void *q, const void *k, const void *v, const float *decay, const float *beta, const int32_t *lengths,

@@ -91,7 +91,7 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
             for (int p = 0; p < NP; ++p) kt[(u * NP + p) * 64] = f.p[p];
         }
     }
-    invert(M);
+    invert(M, w, lane);
     {
         // row tile w of T^T: plain for dR0 (shared), rows of KD scaled for Wd (own)
         Frag<3> tw[2], tt[2];
@@ -237,7 +237,7 @@ __device__ inline float row_sum(float x)
 template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void delta_gradients(const Args a)
 {
     using L = GradLds<T, NP, KP>;
-    constexpr int KT = KP / 16, PK = L::PK;
+    constexpr int KT = KP / 16, PK = L::PK, OWN = (KT + 3) / 4;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ Gates G;
     __shared__ float qdq[CHUNK], vdv[CHUNK], udr[CHUNK], part[4];
@@ -294,47 +294,63 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
         for (int t = 0; t < 4; ++t) zt[t] = mt[t] = zero;
         float inner = 0.f;                      // <dS, S_C>
         float sv[4] = {0.f, 0.f, 0.f, 0.f}, su[4] = {0.f, 0.f, 0.f, 0.f};
+        // A step's loads are all under way before the first is wanted: tiles, and (from where something is, and dropped below) v and dO.
+        // Wave w: row tile w of U and dR; row tiles w, w + 4 of the states
+        f32x4 tu[2], tr[2], ts[OWN][2], te[OWN][2], td[OWN][2];
+        T tv[2][4];
+        RowsAhead<T, NP, 32, 256> to;
+        auto ahead = [&](int v0) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int vt = min(v0 / 16 + half, a.VT - 1), v = min(16 * vt + c, a.V - 1);
+                tu[half] = *reinterpret_cast<const f32x4 *>(up + ((size_t)w * a.VT + vt) * 1024 + lane * 16);
+                tr[half] = *reinterpret_cast<const f32x4 *>(rp + ((size_t)w * a.VT + vt) * 1024 + lane * 16);
+#pragma unroll
+                for (int o = 0; o < OWN; ++o) {
+                    const size_t at = ((size_t)min(w + 4 * o, KT - 1) * a.VT + vt) * 1024 + lane * 16;
+                    ts[o][half] = *reinterpret_cast<const f32x4 *>(sp + at);
+                    te[o][half] = *reinterpret_cast<const f32x4 *>(sp + a.s_chunk + at);
+                    td[o][half] = *reinterpret_cast<const f32x4 *>(dp + at);
+                }
+                const T *vp = (const T *)a.v + b * a.vsb + (long long)t0 * a.vst + (long long)h * a.V + v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) tv[half][e] = vp[min(16 * w + 4 * g + e, rows - 1) * a.vst];
+            }
+            to.load(threadIdx.x, (const T *)a.dO + b * a.osb + (long long)t0 * a.ost + (long long)h * a.V + v0, a.ost, rows, min(32, a.V - v0), a.veco);
+        };
+        ahead(0);
         for (int v0 = 0; v0 < a.V; v0 += 32) {
             __syncthreads();
-            // wave w: row tile w of U and dR; row tiles w, w + 4 of S0 and dS
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int vt = v0 / 16 + half, v = 16 * vt + c;
                 const bool there = vt < a.VT;
-                f32x4 u = zero, r = zero;
-                if (there) {
-                    u = *reinterpret_cast<const f32x4 *>(up + ((size_t)w * a.VT + vt) * 1024 + lane * 16);
-                    r = *reinterpret_cast<const f32x4 *>(rp + ((size_t)w * a.VT + vt) * 1024 + lane * 16);
-                }
+                const f32x4 u = there ? tu[half] : zero, r = there ? tr[half] : zero;
                 put_column(ut, 16 * half + c, 16 * w + 4 * g, u);
                 put_column(rt, 16 * half + c, 16 * w + 4 * g, r);
+                T *dvp = (T *)a.dv + b * a.vsb + (long long)t0 * a.vst + (long long)h * a.V + v;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int i = 16 * w + 4 * g + e;
                     su[e] += u[e] * r[e];
                     const float dv = G.beta[i] * r[e];
-                    if (v < a.V && i < all) {
-                        const long long at = b * a.vsb + (t0 + i) * a.vst + (long long)h * a.V + v;
-                        if (i < rows) sv[e] += (float)((const T *)a.v)[at] * dv;
-                        if (a.dv) ((T *)a.dv)[at] = (T)(i < rows ? dv : 0.f);
-                    }
+                    sv[e] += v < a.V && i < rows ? (float)tv[half][e] * dv : 0.f;
+                    if (a.dv && v < a.V && i < all) dvp[i * a.vst] = (T)(i < rows ? dv : 0.f);
                 }
 #pragma unroll
-                for (int t = w; t < KT; t += 4) {
-                    f32x4 s = zero, d = zero, e = zero;
-                    if (there) {
-                        s = *reinterpret_cast<const f32x4 *>(sp + ((size_t)t * a.VT + vt) * 1024 + lane * 16);
-                        e = *reinterpret_cast<const f32x4 *>(sp + a.s_chunk + ((size_t)t * a.VT + vt) * 1024 + lane * 16);
-                        d = *reinterpret_cast<const f32x4 *>(dp + ((size_t)t * a.VT + vt) * 1024 + lane * 16);
-                    }
+                for (int o = 0; o < OWN; ++o) {
+                    const int t = w + 4 * o;
+                    if (t >= KT) break;
+                    const f32x4 s = there ? ts[o][half] : zero, d = there ? td[o][half] : zero;
                     put_column(st, 16 * half + c, 16 * t + 4 * g, s);
                     put_column(dt, 16 * half + c, 16 * t + 4 * g, d);
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) inner += d[x] * e[x];
+                    for (int x = 0; x < 4; ++x) inner += d[x] * te[o][half][x];
                 }
             }
-            stage_rows<T, NP, 32>(ot, (const T *)a.dO + b * a.osb + t0 * a.ost + (long long)h * a.V + v0, a.ost, rows, min(32, a.V - v0), a.veco, nullptr, false, 0.f);
+            to.put_plain(threadIdx.x, ot, rows, min(32, a.V - v0));
             __syncthreads();
+            if (v0 + 32 < a.V) ahead(v0 + 32);
             const Frag<NP> o = ot.straight(16 * w, 0, lane);
             const Frag<3> r = rt.straight_down(0, 16 * w, lane);
             Frag<PK> u;

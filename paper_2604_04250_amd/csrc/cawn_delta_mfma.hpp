@@ -154,13 +154,82 @@ __device__ inline void stage_rows(const Tile<N, CHUNK, COLS> &t, const T *base, 
     }
 }
 
+// The same in two steps, so that a chunk's rows travel while the one before is treated: into registers, and from there into planes.
+template <typename T, int N, int COLS, int NT> struct RowsAhead {
+    static constexpr int U = COLS / 8, UNITS = CHUNK * U / NT;
+    Pack<T, 8> x[UNITS];
+    // What is not there is loaded from where something is, and dropped in put(): a load behind a lane's branch would be waited for.
+    // rows, cols >= 1; vec: cols a multiple of 16 bytes' elements, and every row aligned to 16 bytes
+    __device__ void load(int tid, const T *base, long long stride, int rows, int cols, bool vec)
+    {
+        constexpr int W = 16 / sizeof(T);
+#pragma unroll
+        for (int e = 0; e < UNITS; ++e) {
+            const int u = tid + e * NT, r = min(u / U, rows - 1), c = u % U * 8;
+            const T *src = base + r * stride;
+            if (vec) {
+#pragma unroll
+                for (int p = 0; p < 8 / W; ++p) *reinterpret_cast<f32x4 *>(&x[e].v[p * W]) = *reinterpret_cast<const f32x4 *>(src + min(c + p * W, cols - W));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[e].v[i] = src[min(c + i, cols - 1)];
+            }
+        }
+    }
+    __device__ void put_plain(int tid, const Tile<N, CHUNK, COLS> &t, int rows, int cols)
+    {
+        if (rows < CHUNK || cols < COLS) {              // (the same for all lanes)
+#pragma unroll
+            for (int e = 0; e < UNITS; ++e) {
+                const int u = tid + e * NT, r = u / U, c = u % U * 8;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (r >= rows || c + i >= cols) x[e].v[i] = (T)0.f;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < UNITS; ++e) {
+            const int u = tid + e * NT, r = u / U, c = u % U * 8;
+            bf16 *dst = t.p + r * Tile<N, CHUNK, COLS>::LD + c;
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<Pack<T, 8> *>(dst) = x[e];
+            else {
+                float y[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = x[e].v[i];
+                Frag<N> f;
+                split8<N>(y, f);
+#pragma unroll
+                for (int n = 0; n < N; ++n) *reinterpret_cast<bf16x8 *>(dst + n * Tile<N, CHUNK, COLS>::PLANE) = f.p[n];
+            }
+        }
+    }
+    // ... and the rows' norm factors
+    __device__ void put(int tid, const Tile<N, CHUNK, COLS> &t, float *norm, int rows, int cols, bool normed, float eps)
+    {
+        put_plain(tid, t, rows, cols);
+#pragma unroll
+        for (int e = 0; e < UNITS; ++e) {
+            const int u = tid + e * NT, r = u / U;
+            if (normed) {
+                float s = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s = fmaf((float)x[e].v[i], (float)x[e].v[i], s);
+#pragma unroll
+                for (int m = U / 2; m > 0; m >>= 1) s += __shfl_xor(s, m);
+                if (u % U == 0) norm[r] = r < rows ? 1.f / sqrtf(s + eps) : 1.f;
+            } else if (u % U == 0) norm[r] = 1.f;
+        }
+    }
+};
+
 // Per token of a chunk; also what later kernels find in the workspace, in this order
 struct Gates {
-    float gh[CHUNK], gl[CHUNK];     // G in two parts: exact differences, whatever the sum
+    float gh[CHUNK], gl[CHUNK];     // G / ln 2 in two parts: exact differences, whatever the sum
     float eg[CHUNK], ed[CHUNK];     // e^G, e^{G_C - G}
     float beta[CHUNK];
-    float rk[CHUNK], rq[CHUNK];
+    float rk[CHUNK], rq[CHUNK];     // factors of the norms
     float c[CHUNK];                 // factor of a token's row in the update of the state
+    float x[CHUNK];                 // (scan: beta e^G / |k|)
 };
 
 constexpr float BETA_MIN = 8.673617379884035e-19f;      // 2^-60: betas nearer to 0 count as this, so that u / beta exists
@@ -181,8 +250,9 @@ __device__ inline void load_gates(const Args &a, Gates &G, int b, int h, int t0,
         if (i >= m) s += o;
     }
     const double total = __shfl(s, 63);
-    G.gh[i] = (float)s;
-    G.gl[i] = (float)(s - (double)(float)s);
+    const double two = s * 1.4426950408889634;
+    G.gh[i] = (float)two;
+    G.gl[i] = (float)(two - (double)(float)two);
     G.eg[i] = expf((float)s);
     G.ed[i] = expf((float)(total - s));
     G.beta[i] = beta;
@@ -190,7 +260,7 @@ __device__ inline void load_gates(const Args &a, Gates &G, int b, int h, int t0,
 
 __device__ inline float decay_between(const Gates &G, int i, int j)
 {
-    return __expf((G.gh[i] - G.gh[j]) + (G.gl[i] - G.gl[j]));
+    return __builtin_amdgcn_exp2f((G.gh[i] - G.gh[j]) + (G.gl[i] - G.gl[j]));
 }
 
 // (I + L)^-1 in place: L strictly lower, 64 x 64 fp32 in LDS, zeros above.  Blocks of 16 by substitution, a column a lane; then
@@ -216,27 +286,35 @@ __device__ inline void put16(float *A, f32x4 x, int lane, float sign)
 #pragma unroll
     for (int r = 0; r < 4; ++r) A[(4 * (lane / 16) + r) * TLD + lane % 16] = sign * x[r];
 }
-__device__ inline void invert(float *T)
+__device__ inline void invert(float *T, int w, int lane)         // (waves beyond the fourth only wait with the others)
 {
-    const int w = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 16;
+    const int c = lane % 16;
     float *D = T + (16 * w) * TLD + 16 * w;
     float x[16];
+    if (w < 4) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = i == c ? 1.f : 0.f;
+        for (int i = 0; i < 16; ++i) x[i] = i == c ? 1.f : 0.f;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) {
-        float row[16];
+        for (int q = 0; q < 4; ++q) {
+            // four rows at a time (all of them at once would take 136 registers)
+            f32x4 L[4][4];
 #pragma unroll
-        for (int q = 0; q < (i + 3) / 4; ++q) {
-            const f32x4 v = *reinterpret_cast<const f32x4 *>(D + i * TLD + 4 * q);
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) row[4 * q + e] = v[e];
+                for (int e = 0; e <= q; ++e) L[i][e] = *reinterpret_cast<const f32x4 *>(D + (4 * q + i) * TLD + 4 * e);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < 4 * q; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[4 * q + i] = fmaf(-L[i][j / 4][j % 4], x[j], x[4 * q + i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = j + 1; i < 4; ++i) x[4 * q + i] = fmaf(-L[i][q][j], x[4 * q + j], x[4 * q + i]);
         }
-#pragma unroll
-        for (int j = 0; j < i; ++j) x[i] = fmaf(-row[j], x[j], x[i]);
     }
     __syncthreads();
-    if (lane < 16) {
+    if (w < 4 && lane < 16) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) D[i * TLD + c] = x[i];
     }
@@ -254,12 +332,12 @@ __device__ inline void invert(float *T)
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int m = 0; m < 2; ++m)
-            if (m >= ct) X[kt] = mul16(T + (32 + 16 * kt) * TLD + 16 * m, tile16(T + 16 * m * TLD + 16 * ct, lane), X[kt], lane);
+            if (m >= ct && w < 4) X[kt] = mul16(T + (32 + 16 * kt) * TLD + 16 * m, tile16(T + 16 * m * TLD + 16 * ct, lane), X[kt], lane);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
-        if (kt <= rt) out = mul16(T + (32 + 16 * rt) * TLD + 32 + 16 * kt, X[kt], out, lane);
+        if (kt <= rt && w < 4) out = mul16(T + (32 + 16 * rt) * TLD + 32 + 16 * kt, X[kt], out, lane);
     __syncthreads();
-    put16(T + (32 + 16 * rt) * TLD + 16 * ct, out, lane, -1.f);
+    if (w < 4) put16(T + (32 + 16 * rt) * TLD + 16 * ct, out, lane, -1.f);
     __syncthreads();
 }
 

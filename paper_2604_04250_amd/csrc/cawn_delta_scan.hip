@@ -1,0 +1,428 @@
+// Gated delta rule by chunks, forward.
+//
+// The chunks of a row are a chain, and a chain is as slow as its links; so the row is cut into segments, each of them some chunks that
+// a workgroup takes one after the other with the state in its registers:
+//   delta_gates   running sums of the decays, for every chunk at once
+//   delta_scan    MODE 1, all segments but the last at once: what a segment makes of a state, S_end = A S_begin + b; A comes from running
+//                 the recurrence on the columns of the identity with v = 0
+//   delta_join    the states at the segments' begins, one product a segment
+//   delta_scan    MODE 0, all segments at once: the outputs
+// Nothing of a chunk goes through memory but its inputs and outputs (and, for a backward, the state before it and its u).  With enough
+// rows and heads to fill the chip there is one segment, and MODE 0 is all.
+//
+// A wave owns 16 columns of the state, all rows of them, in result layout, which is the operand layout of the next product.  Per chunk:
+//     X = beta (V - e^G K S),  U = T X,  O^T = scale (e^G S^T Q^T + U^T P^T),  S = e^{G_C} S + K^T (e^{G_C - G} U)
+// and before that, by all waves together, T (a row tile of the system a wave, inverted in place) and P.
+#include <stddef.h>
+
+#include "cawn_delta_mfma.hpp"
+
+namespace cawn {
+namespace delta {
+
+// a wave per chunk
+__global__ __launch_bounds__(256) void delta_gates(const Args a)
+{
+    const long long at = (long long)blockIdx.x * 4 + threadIdx.x / 64;
+    if (at >= (long long)a.B * a.H * a.chunks) return;
+    const int n = (int)(at % a.chunks), bh = (int)(at / a.chunks), b = bh / a.H, h = bh % a.H;
+    const int rows = min(CHUNK, row_length(a, b) - n * CHUNK), i = threadIdx.x % 64;
+    if (rows <= 0) return;
+    const long long from = ((long long)b * a.L + n * CHUNK + i) * a.H + h;
+    float g = i < rows ? a.decay[from] : 0.f, beta = i < rows ? a.beta[from] : 1.f;
+    if (g < DECAY_MIN) g = DECAY_MIN;
+    if (fabsf(beta) < BETA_MIN) beta = copysignf(BETA_MIN, beta);
+    double s = g;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const double o = __shfl_up(s, m);
+        if (i >= m) s += o;
+    }
+    const double total = __shfl(s, 63);
+    float *G = a.gates + at * GATE_FLOATS + i;
+    const double two = s * 1.4426950408889634;
+    G[0] = (float)two;
+    G[64] = (float)(two - (double)(float)two);
+    G[128] = expf((float)s);
+    G[192] = expf((float)(total - s));
+    G[256] = beta;
+}
+
+#ifndef FENCE
+#define FENCE __builtin_amdgcn_sched_barrier(0);
+#endif
+#ifndef WMAX0
+#define WMAX0 3
+#endif
+#ifndef WMAX1
+#define WMAX1 2
+#endif
+template <int NP, int KP, int MODE> struct ScanLds {
+    static constexpr int PO = NP == 1 ? 2 : 3;
+    static constexpr int KB = Tile<NP, CHUNK, KP>::BYTES, M = MODE == 0 ? 2 * KB : KB;
+    static constexpr int MB = 6 * 3 * 1024 > CHUNK * TLD * 4 ? 6 * 3 * 1024 : CHUNK * TLD * 4;      // the system, then T's operands
+    static constexpr int P = M + MB, BYTES = P + (MODE == 0 ? 6 * PO * 1024 : 0);
+    // waves a SIMD that the registers are budgeted for: as many workgroups as the LDS holds
+    static constexpr int HELD = 163840 / (BYTES + (int)sizeof(Gates)), WAVES = MODE == 0 ? (HELD > WMAX0 ? WMAX0 : HELD) : (HELD > WMAX1 ? WMAX1 : HELD) * 2;
+};
+
+// T and P are lower triangular: of the operands (row tile, 32 columns) those of tiles 0 and 1 have one, those of 2 and 3 two
+__device__ inline constexpr int lower(int t, int ks) { return t < 2 ? t : 2 + (t - 2) * 2 + ks; }
+
+template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MODE == 0 ? 256 : 512), (ScanLds<NP, KP, MODE>::WAVES)) void delta_scan(const Args a)
+{
+    using L = ScanLds<NP, KP, MODE>;
+    constexpr int KS = KP / 32, KT = KP / 16, PO = L::PO, NT = MODE == 0 ? 256 : 512, NW = NT / 64;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ Gates G;
+    const Tile<NP, CHUNK, KP> k{(bf16 *)lds}, q{(bf16 *)(lds + L::KB)};
+    float *M = (float *)(lds + L::M);
+    bf16x8 *tf = reinterpret_cast<bf16x8 *>(lds + L::M), *pf = reinterpret_cast<bf16x8 *>(lds + L::P);
+    const int rows_all = a.B * a.H, blk = blockIdx.x, bh = blk % rows_all, nseg = MODE == 0 ? a.segments : a.segments - 1;
+    const int seg = blk / rows_all % nseg, group = blk / rows_all / nseg, b = bh / a.H, h = bh % a.H;
+    const int len = row_length(a, b), nb = (len + CHUNK - 1) / CHUNK;
+    const int n0 = min(seg * a.seg_chunks, nb), n1 = min(n0 + a.seg_chunks, nb);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    int tid = threadIdx.x, lane = tid % 64, g = lane / 16, c = lane % 16;
+    // column tile: of v, and (MODE 1) beyond it of the identity
+    const int ct = group * NW + w, at = ct - a.VT;
+    const bool of_v = ct < a.VT, mine = of_v || (MODE == 1 && at < KT);
+    int v = 16 * ct + c;
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+
+    f32x4 S[KT];
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+        S[t] = zero;
+        if (MODE == 1) {
+            if (!of_v && at == t) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[t][r] = 4 * g + r == c ? 1.f : 0.f;
+            }
+        } else if (of_v && seg > 0) S[t] = *reinterpret_cast<const f32x4 *>(a.seg_s + (((size_t)bh * a.segments + seg) * KT * a.VT + (size_t)t * a.VT + ct) * 1024 + lane * 16);
+        else if (of_v && a.state_in && v < a.V) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (16 * t + 4 * g + r < a.K) S[t][r] = a.state_in[((long long)bh * a.K + 16 * t + 4 * g + r) * a.V + v];
+        }
+    }
+
+    // Lane numbers anew, in every chunk and between its steps: left to itself the compiler forms all that follows from them (row
+    // numbers, comparisons, addresses: hundreds of values) ahead of the loop, and keeps them.
+    auto anew = [&]() {
+        tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        lane = tid % 64, g = lane / 16, c = lane % 16, v = 16 * ct + c;
+    };
+    RowsAhead<T, NP, KP, NT> ka, qa;
+    float ga[2];
+    auto ahead = [&](int n) {
+        const int rows = min(CHUNK, len - n * CHUNK);
+        const long long t0 = (long long)n * CHUNK, qat = b * a.qsb + t0 * a.qst + (long long)(h / (a.H / a.Hk)) * a.K;
+        ka.load(tid, (const T *)a.k + qat, a.qst, rows, a.K, a.vecq);
+        if (MODE == 0) qa.load(tid, (const T *)a.q + qat, a.qst, rows, a.K, a.vecq);
+        const float *gp = a.gates + ((long long)bh * a.chunks + n) * GATE_FLOATS;
+        ga[0] = tid < GATE_FLOATS ? gp[tid] : 0.f;
+        ga[1] = tid + NT < GATE_FLOATS ? gp[tid + NT] : 0.f;
+    };
+    if (n0 < n1) ahead(n0);
+    for (int n = n0; n < n1; ++n) {
+        const int rows = min(CHUNK, len - n * CHUNK);
+        anew();
+        if (n > n0) __syncthreads();
+        ka.put(tid, k, G.rk, rows, a.K, a.norm, a.eps);
+        if (MODE == 0) qa.put(tid, q, G.rq, rows, a.K, a.norm, a.eps);
+        if (tid < GATE_FLOATS) (&G.gh[0])[tid] = ga[0];
+        if (tid + NT < GATE_FLOATS) (&G.gh[0])[tid + NT] = ga[1];
+        __syncthreads();
+        // v is wanted last.  (What is not there is loaded from where something is, and dropped where it is used: a load behind a lane's
+        // branch, or one whose value is converted at once, would be waited for here)
+        T va[4][4];
+        // a lane's place among rows of v (4g .. and column c), in elements
+        const long long vlane = 4 * g * a.vst + c;
+        if (of_v) {
+            const T *vp = (const T *)a.v + b * a.vsb + (long long)n * CHUNK * a.vst + (long long)h * a.V;
+            if (rows == CHUNK && 16 * ct + 16 <= a.V) {
+                vp += 16 * ct;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) va[t][r] = (vp + (16 * t + r) * a.vst)[vlane];
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) va[t][r] = vp[min(16 * t + 4 * g + r, rows - 1) * a.vst + min(v, a.V - 1)];
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (16 * t + 4 * g + r >= rows || v >= a.V) va[t][r] = (T)0.f;
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) va[t][r] = (T)0.f;
+        }
+        if (tid < CHUNK) {
+            G.c[tid] = G.ed[tid] * G.rk[tid];
+            G.x[tid] = G.beta[tid] * G.eg[tid] * G.rk[tid];
+        }
+        if (n + 1 < n1) ahead(n + 1);
+        anew();
+        // the system's row tile w (transposed, so that its decays serve P^T too) and P's
+        if (w < 4) {
+            f32x4 nt[4], pt[4];
+            const int i = 16 * w + c;
+#pragma unroll
+            for (int jt = 0; jt < 4; ++jt) {
+                nt[jt] = pt[jt] = zero;
+                if (jt <= w) {
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) {
+                        const Frag<NP> f = k.straight(16 * jt, 32 * ks, lane);
+                        nt[jt] = mma<3>(f, k.straight(16 * w, 32 * ks, lane), nt[jt]);
+                        if (MODE == 0) pt[jt] = mma<3>(f, q.straight(16 * w, 32 * ks, lane), pt[jt]);
+                    }
+                    const float m = G.beta[i] * G.rk[i];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int j = 16 * jt + 4 * g + r;
+                        const float d = G.rk[j] * decay_between(G, i, j);
+                        nt[jt][r] = i > j ? nt[jt][r] * (m * d) : 0.f;
+                        if (MODE == 0) pt[jt][r] = i >= j ? pt[jt][r] * d : 0.f;
+                    }
+                }
+                *reinterpret_cast<f32x4 *>(M + i * TLD + 16 * jt + 4 * g) = nt[jt];
+                FENCE
+            }
+            if (MODE == 0) {
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    if (2 * ks > w) break;
+                    Frag<PO> f;
+                    split_tiles<PO>(pt[2 * ks], pt[2 * ks + 1], f);
+#pragma unroll
+                    for (int e = 0; e < PO; ++e) pf[(lower(w, ks) * PO + e) * 64 + lane] = f.p[e];
+                }
+            }
+        }
+        __syncthreads();
+        anew();
+        invert(M, w, lane);
+        anew();
+        Frag<3> tw[2];
+        if (w < 4) {
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                float y[8];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const f32x4 e = *reinterpret_cast<const f32x4 *>(M + (16 * w + c) * TLD + 32 * ks + 16 * half + 4 * g);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) y[4 * half + r] = e[r];
+                }
+                split8<3>(y, tw[ks]);
+            }
+        }
+        __syncthreads();
+        if (w < 4) {
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                if (2 * ks > w) break;
+#pragma unroll
+                for (int e = 0; e < 3; ++e) tf[(lower(w, ks) * 3 + e) * 64 + lane] = tw[ks].p[e];
+            }
+        }
+        // what hangs on the state before the chunk
+        if (MODE == 0 && a.s_tiles && mine) {
+            char *st = a.s_tiles + bh * a.s_row + n * a.s_chunk + (size_t)ct * 1024 + lane * 16;
+#pragma unroll
+            for (int t = 0; t < KT; ++t) *reinterpret_cast<f32x4 *>(st + (size_t)t * a.VT * 1024) = S[t];
+        }
+        anew();
+        f32x4 U[4];
+        f32x4 O[MODE == 0 ? 4 : 1];
+        {
+            Frag<3> sf[KS];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) split_tiles<3>(S[2 * ks], S[2 * ks + 1], sf[ks]);
+            f32x4 X[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                X[t] = zero;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) X[t] = mma<3>(k.tiled(16 * t, 32 * ks, lane), sf[ks], X[t]);
+                FENCE
+            }
+            if (MODE == 0) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    O[t] = zero;
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) {
+                        Frag<PO> f;
+#pragma unroll
+                        for (int e = 0; e < PO; ++e) f.p[e] = sf[ks].p[e];
+                        O[t] = mma<PO>(f, q.tiled(16 * t, 32 * ks, lane), O[t]);
+                    }
+                    O[t] *= G.eg[16 * t + c];
+                    FENCE
+                }
+            }
+            Frag<3> xf[2];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const f32x4 xs = *reinterpret_cast<const f32x4 *>(G.x + 16 * t + 4 * g), be = *reinterpret_cast<const f32x4 *>(G.beta + 16 * t + 4 * g);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) X[t][r] = fmaf(-xs[r], X[t][r], be[r] * (float)va[t][r]);
+            }
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) split_tiles<3>(X[2 * ks], X[2 * ks + 1], xf[ks]);
+            __syncthreads();                    // T's operands
+            anew();
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                U[t] = zero;
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    if (2 * ks > t) break;
+                    Frag<3> f;
+#pragma unroll
+                    for (int e = 0; e < 3; ++e) f.p[e] = tf[(lower(t, ks) * 3 + e) * 64 + lane];
+                    U[t] = mma<3>(f, xf[ks], U[t]);
+                }
+                FENCE
+            }
+        }
+        anew();
+        if (MODE == 0) {
+            if (a.u_tiles && mine) {
+                char *ut = a.u_tiles + bh * a.u_row + n * a.u_chunk + (size_t)ct * 1024 + lane * 16;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4 *>(ut + (size_t)t * a.VT * 1024) = U[t];
+            }
+            Frag<PO> uf[2];
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) split_tiles<PO>(U[2 * ks], U[2 * ks + 1], uf[ks]);
+            const int all = min(CHUNK, a.L - n * CHUNK);
+            const long long olane = c * a.ost + 4 * g;      // a lane's place among rows of o
+            T *op = (T *)a.o + b * a.osb + (long long)n * CHUNK * a.ost + (long long)h * a.V + 16 * ct;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    if (2 * ks > t) break;
+                    Frag<PO> f;
+#pragma unroll
+                    for (int e = 0; e < PO; ++e) f.p[e] = pf[(lower(t, ks) * PO + e) * 64 + lane];
+                    O[t] = mma<PO>(uf[ks], f, O[t]);
+                }
+                FENCE
+                const int i = 16 * t + c;
+                const float m = i < rows ? a.scale * G.rq[i] : 0.f;
+                float y[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) y[r] = O[t][r] * m;
+                if (rows < CHUNK && i >= rows) y[0] = y[1] = y[2] = y[3] = 0.f;         // (whatever the state holds)
+                if (!mine) continue;
+                T *dst = op + (long long)(16 * t) * a.ost;
+                if (rows == CHUNK && a.veco && 16 * ct + 16 <= a.V) store_n<T, 4>(dst + olane, y);
+                else if (i < all) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (16 * ct + 4 * g + r < a.V) dst[olane + r] = (T)y[r];
+                }
+            }
+        }
+        anew();
+        {
+            Frag<3> uf[2];
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                f32x4 y[2];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int t = 2 * ks + half;
+                    y[half] = U[t] * *reinterpret_cast<const f32x4 *>(G.c + 16 * t + 4 * g);
+                }
+                split_tiles<3>(y[0], y[1], uf[ks]);
+            }
+            const float e = G.eg[CHUNK - 1];
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                S[t] *= e;
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) S[t] = mma<3>(k.tiled_down(32 * ks, 16 * t, lane), uf[ks], S[t]);
+                FENCE
+            }
+        }
+    }
+    if (MODE == 0) {
+        // chunks of this segment that the row does not have
+        const int last = min(seg == a.segments - 1 ? a.chunks : (seg + 1) * a.seg_chunks, a.chunks);
+        for (int t = max(n1, seg * a.seg_chunks) * CHUNK + (int)threadIdx.x / 64; t < min(last * CHUNK, a.L); t += NW) {
+            const int vv = group * NW * 16 + lane;
+            if (vv < a.V) ((T *)a.o)[b * a.osb + (long long)t * a.ost + (long long)h * a.V + vv] = (T)0.f;
+        }
+    }
+    if (!mine) return;
+    if (MODE == 1) {
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+            if (of_v) *reinterpret_cast<f32x4 *>(a.seg_b + (((size_t)bh * a.segments + seg) * KT * a.VT + (size_t)t * a.VT + ct) * 1024 + lane * 16) = S[t];
+            else {
+                float *A = (float *)a.seg_a + ((size_t)bh * a.segments + seg) * KP * KP + (size_t)(16 * t + 4 * g) * KP + 16 * at + c;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) A[r * KP] = S[t][r];
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+        if (a.s_tiles && n1 == nb && (n1 > n0 || nb == 0) && (nb > 0 || seg == 0))
+            *reinterpret_cast<f32x4 *>(a.s_tiles + bh * a.s_row + nb * a.s_chunk + ((size_t)t * a.VT + ct) * 1024 + lane * 16) = S[t];
+        if (seg == a.segments - 1 && a.state_out && v < a.V) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (16 * t + 4 * g + r < a.K) a.state_out[((long long)bh * a.K + 16 * t + 4 * g + r) * a.V + v] = S[t][r];
+        }
+    }
+}
+
+template <typename T, int NP, int KP> static int scan_kp(const Args &a, hipStream_t s)
+{
+    const long long rows = (long long)a.B * a.H;
+    if (a.segments > 1) {
+        constexpr int bytes = ScanLds<NP, KP, 1>::BYTES;
+        if (bytes > 60000 && hipFuncSetAttribute((const void *)delta_scan<T, NP, KP, 1>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CAWN_ELAUNCH;
+        hipLaunchKernelGGL((delta_scan<T, NP, KP, 1>), dim3((unsigned)(rows * (a.segments - 1) * ceil_div(a.VT + KP / 16, 8))), dim3(512), bytes, s, a);
+        if (int r = launched()) return r;
+        if (int r = launch_join(a, false, s)) return r;
+    }
+    constexpr int bytes = ScanLds<NP, KP, 0>::BYTES;
+    static_assert(bytes + sizeof(Gates) <= 163840, "LDS");
+    if (bytes > 60000 && hipFuncSetAttribute((const void *)delta_scan<T, NP, KP, 0>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CAWN_ELAUNCH;
+    hipLaunchKernelGGL((delta_scan<T, NP, KP, 0>), dim3((unsigned)(rows * a.segments * ceil_div(a.VT, 4))), dim3(256), bytes, s, a);
+    return launched();
+}
+
+int launch_gates(const Args &a, hipStream_t s)
+{
+    const long long n = (long long)a.B * a.H * a.chunks;
+    if (n == 0) return CAWN_OK;
+    hipLaunchKernelGGL(delta_gates, dim3((unsigned)ceil_div(n, 4)), dim3(256), 0, s, a);
+    return launched();
+}
+
+int launch_scan(const Args &a, bool bf16_, hipStream_t s)
+{
+    if (a.K <= 32) return bf16_ ? scan_kp<bf16, 1, 32>(a, s) : scan_kp<float, 3, 32>(a, s);
+    if (a.K <= 64) return bf16_ ? scan_kp<bf16, 1, 64>(a, s) : scan_kp<float, 3, 64>(a, s);
+    return bf16_ ? scan_kp<bf16, 1, 128>(a, s) : scan_kp<float, 3, 128>(a, s);
+}
+
+} // namespace delta
+} // namespace cawn
