@@ -9,7 +9,7 @@ using namespace cawn::ops;
 
 constexpr int CHUNK = 64;           // tokens treated at once by the chunked kernels
 constexpr int TOKEN_MAX = 16;       // longest call that goes token by token
-constexpr int GATE_FLOATS = 5 * CHUNK;
+constexpr int GATE_FLOATS = 9 * CHUNK;
 constexpr float DECAY_MIN = -104.f; // exp underflows to 0 below: a decay of minus infinity counts as this, so that sums of decays stay finite
 
 struct Args {
@@ -43,6 +43,7 @@ struct Args {
     // the offset b and the state at its begin, in tiles
     int segments, seg_chunks;
     float *gates;
+    char *t_ops, *tt_ops;           // per head and chunk T's operands, and its transpose's (null: not wanted)
     char *seg_a, *seg_b, *seg_s;
 };
 
@@ -61,7 +62,7 @@ struct Sizes {
         ut = 4 * VT;
         st = (KP / 16) * VT;
         slot = (size_t)(wf + kf + ut + 2) * 1024;               // W, K^T, u, gates
-        bslot = (size_t)(wf + kf + ut + 2 + 2 * st) * 1024;     // ... dR for u, Y and dS
+        bslot = (size_t)(wf + kf + ut + 3 + 2 * st) * 1024;     // ... dR for u, Y and dS
     }
 };
 
@@ -72,7 +73,7 @@ __device__ inline int row_length(const Args &a, int b)
 }
 
 int launch_token(const Args &a, bool bf16, hipStream_t s);
-int launch_gates(const Args &a, hipStream_t s);
+int launch_system(const Args &a, bool bf16, hipStream_t s);
 int launch_scan(const Args &a, bool bf16, hipStream_t s);               // forward, behind the gates
 int launch_join(const Args &a, bool reverse, hipStream_t s);
 

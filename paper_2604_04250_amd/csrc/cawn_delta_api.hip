@@ -56,13 +56,13 @@ int span_of(const Args &a, size_t per_chunk)
     return (int)(room < 1 ? 1 : room < a.chunks ? room : a.chunks > 1 ? a.chunks : 1);
 }
 
-struct Layout { size_t gates, a, b, s, slots, carry, bytes; int span; };
+struct Layout { size_t t, a, b, s, slots, carry, bytes; int span; };
 Layout forward_layout(const Args &a, const Sizes &z)
 {
     Layout l{};
     const size_t rows = (size_t)a.B * a.H;
-    l.gates = 0;
-    l.a = (rows * a.chunks * delta::GATE_FLOATS * 4 + 1023) / 1024 * 1024;
+    l.t = (rows * a.chunks * delta::GATE_FLOATS * 4 + 1023) / 1024 * 1024;
+    l.a = l.t + rows * a.chunks * 18 * 1024;
     l.b = l.a + (a.segments > 1 ? rows * a.segments * z.KP * z.KP * 4 : 0);
     l.s = l.b + (a.segments > 1 ? rows * a.segments * z.st * 1024 : 0);
     l.bytes = l.s + (a.segments > 1 ? rows * a.segments * z.st * 1024 : 0);
@@ -132,12 +132,12 @@ int cawn_delta_rule_fwd(const cawn_delta_desc *d, const void *q, const void *k, 
     a.vecq = a.K % w == 0 && a.qst % w == 0 && a.qsb % w == 0 && aligned_to(q, 16) && aligned_to(k, 16);
     a.veco = a.V % 4 == 0 && a.ost % 4 == 0 && a.osb % 4 == 0 && aligned_to(o, 4 * e);
     char *ws = (char *)workspace;
-    a.gates = (float *)ws, a.seg_a = ws + l.a, a.seg_b = ws + l.b, a.seg_s = ws + l.s;
+    a.gates = (float *)ws, a.t_ops = ws + l.t, a.seg_a = ws + l.a, a.seg_b = ws + l.b, a.seg_s = ws + l.s;
     if (ckpt) {
         a.s_tiles = (char *)ckpt, a.s_chunk = (size_t)z.st * 1024, a.s_row = (size_t)(a.chunks + 1) * a.s_chunk;
         a.u_tiles = a.s_tiles + (size_t)a.B * a.H * a.s_row, a.u_chunk = (size_t)z.ut * 1024, a.u_row = (size_t)a.chunks * a.u_chunk;
     }
-    if (int r = delta::launch_gates(a, s)) return r;
+    if (int r = delta::launch_system(a, d->bf16, s)) return r;
     return delta::launch_scan(a, d->bf16, s);
 }
 
@@ -167,7 +167,7 @@ int cawn_delta_rule_bwd(const cawn_delta_desc *d, const void *q, const void *k, 
     a.u_tiles = a.s_tiles + (size_t)a.B * a.H * a.s_row, a.u_chunk = (size_t)z.ut * 1024, a.u_row = (size_t)a.chunks * a.u_chunk;
     StateArgs t{};
     t.B = a.B, t.L = a.L, t.H = a.H, t.K = a.K, t.V = a.V, t.VT = a.VT, t.chunks = a.chunks, t.span = l.span, t.lengths = a.lengths;
-    t.ws = a.ws, t.slot = z.bslot, t.x_at = (size_t)(z.wf + z.kf) * 1024, t.gates_at = t.x_at + (size_t)z.ut * 1024, t.y_at = t.gates_at + 2048;
+    t.ws = a.ws, t.slot = z.bslot, t.x_at = (size_t)(z.wf + z.kf) * 1024, t.gates_at = t.x_at + (size_t)z.ut * 1024, t.y_at = t.gates_at + 3 * 1024;
     t.s_tiles = a.ws + t.y_at + (size_t)z.st * 1024, t.s_row = (size_t)l.span * z.bslot, t.s_chunk = z.bslot;
     t.x_tiles = a.ws + t.x_at, t.x_row = t.s_row, t.x_chunk = z.bslot;
     t.carry = a.ws + l.slots;

@@ -130,7 +130,7 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
         if (A::TIGHT) stage_rows<T, NP, 64>(d, dop, a.ost, rows, min(64, a.V), a.veco, nullptr, false, 0.f);
     }
     __syncthreads();
-    char *x0 = slot + (size_t)(z.wf + z.kf) * 1024 + lane * 16, *y0 = slot + (size_t)(z.wf + z.kf + z.ut + 2) * 1024 + lane * 16;
+    char *x0 = slot + (size_t)(z.wf + z.kf) * 1024 + lane * 16, *y0 = slot + (size_t)(z.wf + z.kf + z.ut + 3) * 1024 + lane * 16;
     for (int v0 = 0; v0 < a.V; v0 += 64) {
         if (v0 > 0) {
             __syncthreads();
@@ -280,7 +280,7 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
         const int h = hk * rep + hh, bh = b * a.H + h;
         const char *slot = a.ws + ((size_t)bh * a.span + (n - a.c0)) * z.bslot;
         const char *sp = a.s_tiles + bh * a.s_row + (n - a.s_first) * a.s_chunk, *up = a.u_tiles + bh * a.u_row + (n - a.u_first) * a.u_chunk;
-        const char *rp = slot + (size_t)(z.wf + z.kf) * 1024, *dp = slot + (size_t)(z.wf + z.kf + z.ut + 2 + z.st) * 1024;
+        const char *rp = slot + (size_t)(z.wf + z.kf) * 1024, *dp = slot + (size_t)(z.wf + z.kf + z.ut + 3 + z.st) * 1024;
         __syncthreads();                        // the previous head's LDS
         {
             const float *in = (const float *)(slot + (size_t)(z.wf + z.kf + z.ut) * 1024);

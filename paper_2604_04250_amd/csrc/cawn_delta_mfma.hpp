@@ -63,6 +63,22 @@ template <int N> __device__ inline void split_tiles(f32x4 lo, f32x4 hi, Frag<N> 
     split8<N>(x, f);
 }
 
+// T and P are lower triangular: of their operands (row tile, 32 columns) row tiles 0 and 1 have one that is not zero, 2 and 3 two; of
+// the transpose's tiles 0 and 1 two, 2 and 3 one
+__device__ inline constexpr int lower(int t, int ks) { return t < 2 ? t : 2 + (t - 2) * 2 + ks; }
+__device__ inline constexpr int upper(int t, int ks) { return t < 2 ? t * 2 + ks : 2 + t; }
+constexpr int T_BYTES = 6 * 3 * 1024;
+
+// 1 KiB from memory straight into LDS, 16 bytes a lane; src the lane's, dst the wave's (the same in all lanes).  Waited for with vmcnt
+__device__ inline void load_piece(const char *src, char *dst)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src, (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
+#else
+    (void)src, (void)dst;
+#endif
+}
+
 // A matrix in LDS: N planes of ROWS x (COLS + 8) bf16.  (Eight more than COLS: rows begin on 16 bytes and not all in one bank.)
 template <int N, int ROWS, int COLS> struct Tile {
     static constexpr int LD = COLS + 8, PLANE = ROWS * LD, BYTES = N * PLANE * 2, PLANES = N;
@@ -207,13 +223,18 @@ template <typename T, int N, int COLS, int NT> struct RowsAhead {
     __device__ void put(int tid, const Tile<N, CHUNK, COLS> &t, float *norm, int rows, int cols, bool normed, float eps)
     {
         put_plain(tid, t, rows, cols);
+        factors(tid, norm, rows, COLS, normed, eps);
+    }
+    // (cols: of which what lies beyond has not been zeroed yet)
+    __device__ void factors(int tid, float *norm, int rows, int cols, bool normed, float eps)
+    {
 #pragma unroll
         for (int e = 0; e < UNITS; ++e) {
             const int u = tid + e * NT, r = u / U;
             if (normed) {
                 float s = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s = fmaf((float)x[e].v[i], (float)x[e].v[i], s);
+                for (int i = 0; i < 8; ++i) s = u % U * 8 + i < cols ? fmaf((float)x[e].v[i], (float)x[e].v[i], s) : s;
 #pragma unroll
                 for (int m = U / 2; m > 0; m >>= 1) s += __shfl_xor(s, m);
                 if (u % U == 0) norm[r] = r < rows ? 1.f / sqrtf(s + eps) : 1.f;
@@ -229,8 +250,10 @@ struct Gates {
     float beta[CHUNK];
     float rk[CHUNK], rq[CHUNK];     // factors of the norms
     float c[CHUNK];                 // factor of a token's row in the update of the state
-    float x[CHUNK];                 // (scan: beta e^G / |k|)
+    float x[CHUNK];                 // factor of k S in X: beta e^G / |k|, 0 for tokens that are not there
 };
+
+static_assert(sizeof(Gates) == GATE_FLOATS * 4, "as the workspace keeps them");
 
 constexpr float BETA_MIN = 8.673617379884035e-19f;      // 2^-60: betas nearer to 0 count as this, so that u / beta exists
 

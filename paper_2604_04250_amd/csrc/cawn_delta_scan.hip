@@ -2,7 +2,7 @@
 //
 // The chunks of a row are a chain, and a chain is as slow as its links; so the row is cut into segments, each of them some chunks that
 // a workgroup takes one after the other with the state in its registers:
-//   delta_gates   running sums of the decays, for every chunk at once
+//   delta_system  what a chunk is by itself: running sums of the decays, norms, T; all chunks at once
 //   delta_scan    MODE 1, all segments but the last at once: what a segment makes of a state, S_end = A S_begin + b; A comes from running
 //                 the recurrence on the columns of the identity with v = 0
 //   delta_join    the states at the segments' begins, one product a segment
@@ -12,7 +12,7 @@
 //
 // A wave owns 16 columns of the state, all rows of them, in result layout, which is the operand layout of the next product.  Per chunk:
 //     X = beta (V - e^G K S),  U = T X,  O^T = scale (e^G S^T Q^T + U^T P^T),  S = e^{G_C} S + K^T (e^{G_C - G} U)
-// and before that, by all waves together, T (a row tile of the system a wave, inverted in place) and P.
+// with P made by all waves together and T fetched as operands.
 #include <stddef.h>
 
 #include "cawn_delta_mfma.hpp"
@@ -20,32 +20,82 @@
 namespace cawn {
 namespace delta {
 
-// a wave per chunk
-__global__ __launch_bounds__(256) void delta_gates(const Args a)
+// What a chunk is by itself, every chunk a workgroup: gates, the norms' factors, and T = (I + diag(beta) N)^-1 as operands: row tile t,
+// 32 columns ks at lower(t, ks), three planes each; for a backward its transpose too.
+template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void delta_system(const Args a)
 {
-    const long long at = (long long)blockIdx.x * 4 + threadIdx.x / 64;
-    if (at >= (long long)a.B * a.H * a.chunks) return;
-    const int n = (int)(at % a.chunks), bh = (int)(at / a.chunks), b = bh / a.H, h = bh % a.H;
-    const int rows = min(CHUNK, row_length(a, b) - n * CHUNK), i = threadIdx.x % 64;
+    constexpr int KS = KP / 32;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ Gates G;
+    const int n = blockIdx.x % a.chunks, bh = blockIdx.x / a.chunks, b = bh / a.H, h = bh % a.H;
+    const int rows = min(CHUNK, row_length(a, b) - n * CHUNK);
     if (rows <= 0) return;
-    const long long from = ((long long)b * a.L + n * CHUNK + i) * a.H + h;
-    float g = i < rows ? a.decay[from] : 0.f, beta = i < rows ? a.beta[from] : 1.f;
-    if (g < DECAY_MIN) g = DECAY_MIN;
-    if (fabsf(beta) < BETA_MIN) beta = copysignf(BETA_MIN, beta);
-    double s = g;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const double o = __shfl_up(s, m);
-        if (i >= m) s += o;
+    const Tile<NP, CHUNK, KP> k{(bf16 *)lds};
+    float *M = (float *)(lds + Tile<NP, CHUNK, KP>::BYTES);
+    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, g = lane / 16, c = lane % 16;
+    const long long qat = b * a.qsb + (long long)n * CHUNK * a.qst + (long long)(h / (a.H / a.Hk)) * a.K;
+    RowsAhead<T, NP, KP, 256> ka, qa;
+    ka.load(tid, (const T *)a.k + qat, a.qst, rows, a.K, a.vecq);
+    if (a.norm) qa.load(tid, (const T *)a.q + qat, a.qst, rows, a.K, a.vecq);
+    load_gates(a, G, b, h, n * CHUNK, rows);
+    ka.put(tid, k, G.rk, rows, a.K, a.norm, a.eps);
+    qa.factors(tid, G.rq, rows, a.K, a.norm, a.eps);
+    __syncthreads();
+    if (tid < CHUNK) {
+        G.c[tid] = G.ed[tid] * G.rk[tid];
+        G.x[tid] = tid < rows ? G.beta[tid] * G.eg[tid] * G.rk[tid] : 0.f;
     }
-    const double total = __shfl(s, 63);
-    float *G = a.gates + at * GATE_FLOATS + i;
-    const double two = s * 1.4426950408889634;
-    G[0] = (float)two;
-    G[64] = (float)(two - (double)(float)two);
-    G[128] = expf((float)s);
-    G[192] = expf((float)(total - s));
-    G[256] = beta;
+    {
+        const int i = 16 * w + c;
+        const float m = G.beta[i] * G.rk[i];
+#pragma unroll
+        for (int jt = 0; jt < 4; ++jt) {
+            f32x4 x = {0.f, 0.f, 0.f, 0.f};
+            if (jt <= w) {
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) x = mma<3>(k.straight(16 * jt, 32 * ks, lane), k.straight(16 * w, 32 * ks, lane), x);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int j = 16 * jt + 4 * g + r;
+                    x[r] = i > j ? x[r] * (m * G.rk[j] * decay_between(G, i, j)) : 0.f;
+                }
+            }
+            *reinterpret_cast<f32x4 *>(M + i * TLD + 16 * jt + 4 * g) = x;
+        }
+    }
+    __syncthreads();
+    const long long at = (long long)bh * a.chunks + n;
+    for (int i = tid; i < (int)(sizeof(Gates) / 4); i += 256) a.gates[at * GATE_FLOATS + i] = ((const float *)&G)[i];
+    invert(M, w, lane);
+    bf16x8 *out = reinterpret_cast<bf16x8 *>(a.t_ops + (size_t)at * T_BYTES) + lane;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+        if (2 * ks > w) break;
+        float y[8];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const f32x4 e = *reinterpret_cast<const f32x4 *>(M + (16 * w + c) * TLD + 32 * ks + 16 * half + 4 * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[4 * half + r] = e[r];
+        }
+        Frag<3> f;
+        split8<3>(y, f);
+#pragma unroll
+        for (int e = 0; e < 3; ++e) out[(lower(w, ks) * 3 + e) * 64] = f.p[e];
+    }
+    if (!a.tt_ops) return;
+    out = reinterpret_cast<bf16x8 *>(a.tt_ops + (size_t)at * T_BYTES) + lane;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+        if (2 * ks + 1 < w) continue;
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = M[(32 * ks + 16 * (e / 4) + 4 * g + e % 4) * TLD + 16 * w + c];
+        Frag<3> f;
+        split8<3>(y, f);
+#pragma unroll
+        for (int e = 0; e < 3; ++e) out[(upper(w, ks) * 3 + e) * 64] = f.p[e];
+    }
 }
 
 #ifndef FENCE
@@ -59,15 +109,11 @@ __global__ __launch_bounds__(256) void delta_gates(const Args a)
 #endif
 template <int NP, int KP, int MODE> struct ScanLds {
     static constexpr int PO = NP == 1 ? 2 : 3;
-    static constexpr int KB = Tile<NP, CHUNK, KP>::BYTES, M = MODE == 0 ? 2 * KB : KB;
-    static constexpr int MB = 6 * 3 * 1024 > CHUNK * TLD * 4 ? 6 * 3 * 1024 : CHUNK * TLD * 4;      // the system, then T's operands
-    static constexpr int P = M + MB, BYTES = P + (MODE == 0 ? 6 * PO * 1024 : 0);
+    static constexpr int KB = Tile<NP, CHUNK, KP>::BYTES, TO = MODE == 0 ? 2 * KB : KB;     // k, q; T's operands; P's
+    static constexpr int P = TO + T_BYTES, BYTES = P + (MODE == 0 ? 6 * PO * 1024 : 0);
     // waves a SIMD that the registers are budgeted for: as many workgroups as the LDS holds
     static constexpr int HELD = 163840 / (BYTES + (int)sizeof(Gates)), WAVES = MODE == 0 ? (HELD > WMAX0 ? WMAX0 : HELD) : (HELD > WMAX1 ? WMAX1 : HELD) * 2;
 };
-
-// T and P are lower triangular: of the operands (row tile, 32 columns) those of tiles 0 and 1 have one, those of 2 and 3 two
-__device__ inline constexpr int lower(int t, int ks) { return t < 2 ? t : 2 + (t - 2) * 2 + ks; }
 
 template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MODE == 0 ? 256 : 512), (ScanLds<NP, KP, MODE>::WAVES)) void delta_scan(const Args a)
 {
@@ -76,8 +122,7 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ Gates G;
     const Tile<NP, CHUNK, KP> k{(bf16 *)lds}, q{(bf16 *)(lds + L::KB)};
-    float *M = (float *)(lds + L::M);
-    bf16x8 *tf = reinterpret_cast<bf16x8 *>(lds + L::M), *pf = reinterpret_cast<bf16x8 *>(lds + L::P);
+    bf16x8 *tf = reinterpret_cast<bf16x8 *>(lds + L::TO), *pf = reinterpret_cast<bf16x8 *>(lds + L::P);
     const int rows_all = a.B * a.H, blk = blockIdx.x, bh = blk % rows_all, nseg = MODE == 0 ? a.segments : a.segments - 1;
     const int seg = blk / rows_all % nseg, group = blk / rows_all / nseg, b = bh / a.H, h = bh % a.H;
     const int len = row_length(a, b), nb = (len + CHUNK - 1) / CHUNK;
@@ -115,25 +160,37 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
         lane = tid % 64, g = lane / 16, c = lane % 16, v = 16 * ct + c;
     };
     RowsAhead<T, NP, KP, NT> ka, qa;
-    float ga[2];
+    constexpr int GN = (GATE_FLOATS + NT - 1) / NT;
+    float ga[GN];
     auto ahead = [&](int n) {
         const int rows = min(CHUNK, len - n * CHUNK);
-        const long long t0 = (long long)n * CHUNK, qat = b * a.qsb + t0 * a.qst + (long long)(h / (a.H / a.Hk)) * a.K;
+        const long long qat = b * a.qsb + (long long)n * CHUNK * a.qst + (long long)(h / (a.H / a.Hk)) * a.K;
         ka.load(tid, (const T *)a.k + qat, a.qst, rows, a.K, a.vecq);
         if (MODE == 0) qa.load(tid, (const T *)a.q + qat, a.qst, rows, a.K, a.vecq);
         const float *gp = a.gates + ((long long)bh * a.chunks + n) * GATE_FLOATS;
-        ga[0] = tid < GATE_FLOATS ? gp[tid] : 0.f;
-        ga[1] = tid + NT < GATE_FLOATS ? gp[tid + NT] : 0.f;
+#pragma unroll
+        for (int e = 0; e < GN; ++e) ga[e] = gp[min(tid + e * NT, GATE_FLOATS - 1)];
     };
     if (n0 < n1) ahead(n0);
     for (int n = n0; n < n1; ++n) {
         const int rows = min(CHUNK, len - n * CHUNK);
         anew();
         if (n > n0) __syncthreads();
-        ka.put(tid, k, G.rk, rows, a.K, a.norm, a.eps);
-        if (MODE == 0) qa.put(tid, q, G.rq, rows, a.K, a.norm, a.eps);
-        if (tid < GATE_FLOATS) (&G.gh[0])[tid] = ga[0];
-        if (tid + NT < GATE_FLOATS) (&G.gh[0])[tid + NT] = ga[1];
+        ka.put_plain(tid, k, rows, a.K);
+        if (MODE == 0) qa.put_plain(tid, q, rows, a.K);
+#pragma unroll
+        for (int e = 0; e < GN; ++e)
+            if (tid + e * NT < GATE_FLOATS) ((float *)&G)[tid + e * NT] = ga[e];
+        {
+            // T's operands come straight into LDS
+            const char *src = a.t_ops + ((size_t)bh * a.chunks + n) * T_BYTES + lane * 16;
+            char *dst = lds + L::TO;
+#pragma unroll
+            for (int u = 0; u < (T_BYTES / 1024 + NW - 1) / NW; ++u) {
+                const int i = u * NW + w;
+                if (i < T_BYTES / 1024) load_piece(src + (size_t)i * 1024, dst + i * 1024);
+            }
+        }
         __syncthreads();
         // v is wanted last.  (What is not there is loaded from where something is, and dropped where it is used: a load behind a lane's
         // branch, or one whose value is converted at once, would be waited for here)
@@ -165,74 +222,33 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
 #pragma unroll
                 for (int r = 0; r < 4; ++r) va[t][r] = (T)0.f;
         }
-        if (tid < CHUNK) {
-            G.c[tid] = G.ed[tid] * G.rk[tid];
-            G.x[tid] = G.beta[tid] * G.eg[tid] * G.rk[tid];
-        }
         if (n + 1 < n1) ahead(n + 1);
         anew();
-        // the system's row tile w (transposed, so that its decays serve P^T too) and P's
-        if (w < 4) {
-            f32x4 nt[4], pt[4];
+        // P's row tile w, transposed: its result layout is the operand's
+        if (MODE == 0) {
+            f32x4 pt[4];
             const int i = 16 * w + c;
 #pragma unroll
             for (int jt = 0; jt < 4; ++jt) {
-                nt[jt] = pt[jt] = zero;
+                pt[jt] = zero;
                 if (jt <= w) {
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) {
-                        const Frag<NP> f = k.straight(16 * jt, 32 * ks, lane);
-                        nt[jt] = mma<3>(f, k.straight(16 * w, 32 * ks, lane), nt[jt]);
-                        if (MODE == 0) pt[jt] = mma<3>(f, q.straight(16 * w, 32 * ks, lane), pt[jt]);
-                    }
-                    const float m = G.beta[i] * G.rk[i];
+                    for (int ks = 0; ks < KS; ++ks) pt[jt] = mma<3>(k.straight(16 * jt, 32 * ks, lane), q.straight(16 * w, 32 * ks, lane), pt[jt]);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int j = 16 * jt + 4 * g + r;
-                        const float d = G.rk[j] * decay_between(G, i, j);
-                        nt[jt][r] = i > j ? nt[jt][r] * (m * d) : 0.f;
-                        if (MODE == 0) pt[jt][r] = i >= j ? pt[jt][r] * d : 0.f;
+                        pt[jt][r] = i >= j ? pt[jt][r] * (G.rk[j] * decay_between(G, i, j)) : 0.f;
                     }
                 }
-                *reinterpret_cast<f32x4 *>(M + i * TLD + 16 * jt + 4 * g) = nt[jt];
                 FENCE
             }
-            if (MODE == 0) {
-#pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-                    if (2 * ks > w) break;
-                    Frag<PO> f;
-                    split_tiles<PO>(pt[2 * ks], pt[2 * ks + 1], f);
-#pragma unroll
-                    for (int e = 0; e < PO; ++e) pf[(lower(w, ks) * PO + e) * 64 + lane] = f.p[e];
-                }
-            }
-        }
-        __syncthreads();
-        anew();
-        invert(M, w, lane);
-        anew();
-        Frag<3> tw[2];
-        if (w < 4) {
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                float y[8];
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const f32x4 e = *reinterpret_cast<const f32x4 *>(M + (16 * w + c) * TLD + 32 * ks + 16 * half + 4 * g);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) y[4 * half + r] = e[r];
-                }
-                split8<3>(y, tw[ks]);
-            }
-        }
-        __syncthreads();
-        if (w < 4) {
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
                 if (2 * ks > w) break;
+                Frag<PO> f;
+                split_tiles<PO>(pt[2 * ks], pt[2 * ks + 1], f);
 #pragma unroll
-                for (int e = 0; e < 3; ++e) tf[(lower(w, ks) * 3 + e) * 64 + lane] = tw[ks].p[e];
+                for (int e = 0; e < PO; ++e) pf[(lower(w, ks) * PO + e) * 64 + lane] = f.p[e];
             }
         }
         // what hangs on the state before the chunk
@@ -280,7 +296,8 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
             }
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) split_tiles<3>(X[2 * ks], X[2 * ks + 1], xf[ks]);
-            __syncthreads();                    // T's operands
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();                    // T's and P's operands
             anew();
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
@@ -409,12 +426,21 @@ template <typename T, int NP, int KP> static int scan_kp(const Args &a, hipStrea
     return launched();
 }
 
-int launch_gates(const Args &a, hipStream_t s)
+template <typename T, int NP, int KP> static int system_kp(const Args &a, hipStream_t s)
 {
+    constexpr int bytes = Tile<NP, CHUNK, KP>::BYTES + CHUNK * TLD * 4;
+    if (bytes > 60000 && hipFuncSetAttribute((const void *)delta_system<T, NP, KP>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CAWN_ELAUNCH;
     const long long n = (long long)a.B * a.H * a.chunks;
     if (n == 0) return CAWN_OK;
-    hipLaunchKernelGGL(delta_gates, dim3((unsigned)ceil_div(n, 4)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((delta_system<T, NP, KP>), dim3((unsigned)n), dim3(256), bytes, s, a);
     return launched();
+}
+
+int launch_system(const Args &a, bool bf16_, hipStream_t s)
+{
+    if (a.K <= 32) return bf16_ ? system_kp<bf16, 1, 32>(a, s) : system_kp<float, 3, 32>(a, s);
+    if (a.K <= 64) return bf16_ ? system_kp<bf16, 1, 64>(a, s) : system_kp<float, 3, 64>(a, s);
+    return bf16_ ? system_kp<bf16, 1, 128>(a, s) : system_kp<float, 3, 128>(a, s);
 }
 
 int launch_scan(const Args &a, bool bf16_, hipStream_t s)
