@@ -18,7 +18,7 @@ SOURCES = ["cawn_fwd_hconv_valve_ret.hip", "cawn_fwd_hconv_ret.hip", "cawn_fwd_h
            "cawn_fwd_short_plain.hip", "cawn_fwd_short_valve.hip", "cawn_fwd_short_ret.hip", "cawn_fwd_short_valve_ret.hip",
            "cawn_api.hip", "cawn_fwd.hip", "cawn_bwd.hip", "cawn_bwd_plain.hip", "cawn_bwd_valve.hip",
            "cawn_bwd_ret.hip", "cawn_bwd_hconv.hip", "cawn_bwd_hconv_valve.hip", "cawn_bwd_hconv_ret.hip",
-           "cawn_delta_api.hip", "cawn_delta_token.hip", "cawn_delta_scan.hip", "cawn_delta_join.hip", "cawn_delta_bwd.hip", "cawn_delta_states.hip",
+           "cawn_delta_api.hip", "cawn_delta_token.hip", "cawn_delta_scan.hip", "cawn_delta_join.hip", "cawn_delta_back.hip", "cawn_delta_bwd.hip",
            "cawn_norm.hip", "cawn_dropout.hip"]
 # The backward kernel is a persistent loop whose body fills its register budget (4 waves per SIMD).
 # Hoisting loop-invariant copies of uniform values and addresses out of that loop costs ~10 VGPRs

@@ -6,11 +6,8 @@ using namespace cawn::ops;
 using cawn::delta::Args;
 
 using cawn::delta::Sizes;
-using cawn::delta::StateArgs;
 
 namespace {
-
-constexpr size_t SPAN_BYTES = 128u << 20;
 
 // How a row's chunks are cut into segments.  A segment costs each of its chunks twice (what it makes of a state, then its outputs) and
 // one link of the join, so two segments gain nothing; many shorten the two passes until the chip is full or the links cost as much.
@@ -48,40 +45,50 @@ int check(const cawn_delta_desc *d, Args *a)
     return CAWN_OK;
 }
 
-// Chunks that the launches of a call treat at once: what they hand on to each other through the workspace is then still in the
-// 256 MiB memory-side cache, and the workspace does not grow with the sequence.
-int span_of(const Args &a, size_t per_chunk)
+// Byte offsets.  Kept for the backward: states [B H][chunks + 1] and u [B H][chunks] in tiles, gates, the operands of T^T, A of the segments.
+// Scratch of the forward: gates and A (unless kept), T's operands, b and the begins of the segments; of the backward: dR and dS of every
+// chunk, b and the ends of the segments.
+struct Layout { size_t u, gates, tt, a, ckpt; size_t fwd_gates, fwd_a, t, b, s, fwd; size_t ds, rb, rs, bwd; };
+Layout layout_of(const Args &a)
 {
-    const long long room = (long long)(SPAN_BYTES / ((size_t)a.B * a.H * per_chunk));
-    return (int)(room < 1 ? 1 : room < a.chunks ? room : a.chunks > 1 ? a.chunks : 1);
-}
-
-struct Layout { size_t t, a, b, s, slots, carry, bytes; int span; };
-Layout forward_layout(const Args &a, const Sizes &z)
-{
-    Layout l{};
-    const size_t rows = (size_t)a.B * a.H;
-    l.t = (rows * a.chunks * delta::GATE_FLOATS * 4 + 1023) / 1024 * 1024;
-    l.a = l.t + rows * a.chunks * 18 * 1024;
-    l.b = l.a + (a.segments > 1 ? rows * a.segments * z.KP * z.KP * 4 : 0);
-    l.s = l.b + (a.segments > 1 ? rows * a.segments * z.st * 1024 : 0);
-    l.bytes = l.s + (a.segments > 1 ? rows * a.segments * z.st * 1024 : 0);
+    Layout l;
+    const Sizes z(a.K, a.V);
+    const size_t heads = (size_t)a.B * a.H, all = heads * a.chunks, segs = a.segments > 1 ? heads * a.segments : 0;
+    const size_t gates = (all * delta::GATE_FLOATS * 4 + 1023) / 1024 * 1024, am = segs * z.KP * z.KP * 4, states = segs * z.st * 1024;
+    l.u = heads * (a.chunks + 1) * z.st * 1024;
+    l.gates = l.u + all * z.ut * 1024;
+    l.tt = l.gates + gates;
+    l.a = l.tt + all * delta::OPERAND_BYTES;
+    l.ckpt = l.a + am;
+    l.fwd_gates = 0;
+    l.fwd_a = gates;
+    l.t = l.fwd_a + am;
+    l.b = l.t + all * delta::OPERAND_BYTES;
+    l.s = l.b + states;
+    l.fwd = l.s + states;
+    l.ds = all * z.ut * 1024;
+    l.rb = l.ds + all * z.st * 1024;
+    l.rs = l.rb + states;
+    l.bwd = l.rs + states;
     return l;
 }
 
-Layout backward_layout(const Args &a, const Sizes &z)
+// the checkpoint's parts
+void keep(Args *a, const Layout &l, void *ckpt)
 {
-    Layout l{};
-    const size_t rows = (size_t)a.B * a.H;
-    l.span = span_of(a, z.bslot);
-    l.slots = rows * l.span * z.bslot;
-    l.carry = rows * z.st * 1024;
-    l.bytes = l.slots + l.carry;
-    return l;
+    const Sizes z(a->K, a->V);
+    char *p = (char *)ckpt;
+    a->s_tiles = p, a->s_chunk = (size_t)z.st * 1024, a->s_row = (size_t)(a->chunks + 1) * a->s_chunk;
+    a->u_tiles = p + l.u, a->u_chunk = (size_t)z.ut * 1024, a->u_row = (size_t)a->chunks * a->u_chunk;
+    a->gates = (float *)(p + l.gates), a->tt_ops = p + l.tt, a->seg_a = p + l.a;
 }
 
-// states [B H][chunks + 1], then u [B H][chunks], in tiles
-size_t ckpt_bytes(const Args &a, const Sizes &z) { return (size_t)a.B * a.H * ((size_t)(a.chunks + 1) * z.st + (size_t)a.chunks * z.ut) * 1024; }
+// more workgroups than a grid has
+bool too_many(const Args &a)
+{
+    const long long most = a.segments > a.chunks ? a.segments : a.chunks;
+    return (long long)a.B * a.H * ceil_div(a.VT + 8, 4) > 0x7fffffffLL / (most > 0 ? most : 1);
+}
 
 bool misaligned(const cawn_delta_desc *d, const void *p) { return !aligned_to(p, d->bf16 ? 2 : 4); }
 
@@ -98,15 +105,15 @@ size_t cawn_delta_state_bytes(const cawn_delta_desc *d)
 size_t cawn_delta_ckpt_bytes(const cawn_delta_desc *d)
 {
     Args a;
-    return check(d, &a) != CAWN_OK ? 0 : ckpt_bytes(a, Sizes(a.K, a.V, 1));
+    return check(d, &a) != CAWN_OK ? 0 : layout_of(a).ckpt;
 }
 
 size_t cawn_delta_workspace_bytes(const cawn_delta_desc *d)
 {
     Args a;
     if (check(d, &a) != CAWN_OK) return 0;
-    const Sizes z(a.K, a.V, d->bf16 ? 1 : 3);
-    const size_t f = forward_layout(a, z).bytes, r = backward_layout(a, z).bytes, bytes = f > r ? f : r;
+    const Layout l = layout_of(a);
+    const size_t bytes = l.fwd > l.bwd ? l.fwd : l.bwd;
     return bytes > 256 ? bytes : 256;
 }
 
@@ -125,18 +132,14 @@ int cawn_delta_rule_fwd(const cawn_delta_desc *d, const void *q, const void *k, 
     // token by token up to TOKEN_MAX
     if (a.L <= delta::TOKEN_MAX && !ckpt) return delta::launch_token(a, d->bf16, s);
     const int e = d->bf16 ? 2 : 4, w = 16 / e;
-    const Sizes z(a.K, a.V, d->bf16 ? 1 : 3);
-    const Layout l = forward_layout(a, z);
-    if (!workspace || workspace_bytes < l.bytes || !aligned_to(workspace, 256)) return CAWN_EWORKSPACE;
-    if ((long long)a.B * a.H * (a.segments > a.chunks ? a.segments : a.chunks) * ceil_div(a.VT + z.KP / 16, 4) > 0x7fffffffLL) return CAWN_EUNSUPPORTED;
+    const Layout l = layout_of(a);
+    if (!workspace || workspace_bytes < l.fwd || !aligned_to(workspace, 256)) return CAWN_EWORKSPACE;
+    if (too_many(a)) return CAWN_EUNSUPPORTED;
     a.vecq = a.K % w == 0 && a.qst % w == 0 && a.qsb % w == 0 && aligned_to(q, 16) && aligned_to(k, 16);
     a.veco = a.V % 4 == 0 && a.ost % 4 == 0 && a.osb % 4 == 0 && aligned_to(o, 4 * e);
     char *ws = (char *)workspace;
-    a.gates = (float *)ws, a.t_ops = ws + l.t, a.seg_a = ws + l.a, a.seg_b = ws + l.b, a.seg_s = ws + l.s;
-    if (ckpt) {
-        a.s_tiles = (char *)ckpt, a.s_chunk = (size_t)z.st * 1024, a.s_row = (size_t)(a.chunks + 1) * a.s_chunk;
-        a.u_tiles = a.s_tiles + (size_t)a.B * a.H * a.s_row, a.u_chunk = (size_t)z.ut * 1024, a.u_row = (size_t)a.chunks * a.u_chunk;
-    }
+    a.gates = (float *)(ws + l.fwd_gates), a.seg_a = ws + l.fwd_a, a.t_ops = ws + l.t, a.seg_b = ws + l.b, a.seg_s = ws + l.s;
+    if (ckpt) keep(&a, l, ckpt);
     if (int r = delta::launch_system(a, d->bf16, s)) return r;
     return delta::launch_scan(a, d->bf16, s);
 }
@@ -153,37 +156,19 @@ int cawn_delta_rule_bwd(const cawn_delta_desc *d, const void *q, const void *k, 
         !aligned_to(decay, 4) || !aligned_to(beta, 4) || !aligned_to(lengths, 4) || !aligned_to(ckpt, 16) || !aligned_to(dstate_out, 4) ||
         !aligned_to(ddecay, 4) || !aligned_to(dbeta, 4) || !aligned_to(dstate_in, 4)) return CAWN_EINVAL;
     const int e = d->bf16 ? 2 : 4, w = 16 / e;
-    const Sizes z(a.K, a.V, d->bf16 ? 1 : 3);
-    const Layout l = backward_layout(a, z);
-    if (!workspace || workspace_bytes < l.bytes || !aligned_to(workspace, 256)) return CAWN_EWORKSPACE;
-    if ((long long)a.B * a.H * l.span > 0x7fffffffLL) return CAWN_EUNSUPPORTED;
-    a.q = q, a.k = k, a.v = v, a.decay = decay, a.beta = beta, a.lengths = lengths, a.dO = dO;
-    a.dq = dq, a.dk = dk, a.dv = dv, a.ddecay = ddecay, a.dbeta = dbeta;
+    const Layout l = layout_of(a);
+    if (!workspace || workspace_bytes < l.bwd || !aligned_to(workspace, 256)) return CAWN_EWORKSPACE;
+    if (too_many(a)) return CAWN_EUNSUPPORTED;
+    a.q = q, a.k = k, a.v = v, a.decay = decay, a.beta = beta, a.lengths = lengths, a.dO = dO, a.dstate_out = (const float *)dstate_out;
+    a.dq = dq, a.dk = dk, a.dv = dv, a.ddecay = ddecay, a.dbeta = dbeta, a.dstate_in = (float *)dstate_in;
     a.vecq = a.K % w == 0 && a.qst % w == 0 && a.qsb % w == 0 && aligned_to(q, 16) && aligned_to(k, 16);
     a.veco = a.V % w == 0 && a.ost % w == 0 && a.osb % w == 0 && aligned_to(dO, 16);
-    a.ws = (char *)workspace;
-    a.span = l.span;
-    a.s_tiles = (char *)const_cast<void *>(ckpt), a.s_chunk = (size_t)z.st * 1024, a.s_row = (size_t)(a.chunks + 1) * a.s_chunk;
-    a.u_tiles = a.s_tiles + (size_t)a.B * a.H * a.s_row, a.u_chunk = (size_t)z.ut * 1024, a.u_row = (size_t)a.chunks * a.u_chunk;
-    StateArgs t{};
-    t.B = a.B, t.L = a.L, t.H = a.H, t.K = a.K, t.V = a.V, t.VT = a.VT, t.chunks = a.chunks, t.span = l.span, t.lengths = a.lengths;
-    t.ws = a.ws, t.slot = z.bslot, t.x_at = (size_t)(z.wf + z.kf) * 1024, t.gates_at = t.x_at + (size_t)z.ut * 1024, t.y_at = t.gates_at + 3 * 1024;
-    t.s_tiles = a.ws + t.y_at + (size_t)z.st * 1024, t.s_row = (size_t)l.span * z.bslot, t.s_chunk = z.bslot;
-    t.x_tiles = a.ws + t.x_at, t.x_row = t.s_row, t.x_chunk = z.bslot;
-    t.carry = a.ws + l.slots;
-    t.begin = (const float *)dstate_out, t.end = (float *)dstate_in;
+    keep(&a, l, const_cast<void *>(ckpt));
+    char *ws = (char *)workspace;
+    a.dr_tiles = ws, a.ds_tiles = ws + l.ds, a.seg_b = ws + l.rb, a.seg_s = ws + l.rs;
     hipStream_t s = (hipStream_t)stream;
-    for (a.c1 = a.chunks;; a.c1 = a.c0) {       // from the last chunks to the first
-        a.c0 = a.c1 > l.span ? a.c1 - l.span : 0;
-        t.c0 = a.c0, t.c1 = a.c1, t.s_first = t.x_first = a.c0;
-        t.first = a.c1 == a.chunks, t.last = a.c0 == 0;
-        if (a.c1 > a.c0)
-            if (int r = delta::launch_adjoint(a, d->bf16, s)) return r;
-        if (int r = delta::launch_states(t, d->bf16, true, s)) return r;
-        if (a.c1 > a.c0)
-            if (int r = delta::launch_gradients(a, d->bf16, s)) return r;
-        if (a.c0 == 0) return CAWN_OK;
-    }
+    if (int r = delta::launch_back(a, d->bf16, s)) return r;
+    return dq || dk || dv || ddecay || dbeta ? delta::launch_gradients(a, d->bf16, s) : CAWN_OK;
 }
 
 } // extern "C"

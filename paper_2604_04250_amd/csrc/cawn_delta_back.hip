@@ -1,0 +1,272 @@
+// Gated delta rule by chunks, backward: the recurrence from the last chunk to the first, in segments like the forward.
+//
+// With dS the gradient of the state behind a chunk, dO that of its output, KD = diag(e^{G_C - G}) K:
+//     dR  = T^T (scale P^T dO + KD dS)            the gradient of U through everything but T; dV = beta dR
+//     dS0 = e^{G_C} dS + scale (e^G Q)^T dO - (beta e^G K)^T dR
+// dS0 is A^T dS plus what the segment's own dO add, A the forward's: MODE 1 finds the latter from dS = 0 (all segments but the first at
+// once), delta_join the gradients behind the segments' ends, MODE 0 runs through all segments and leaves dR and dS of every chunk to
+// delta_gradients.  Waves, columns and operands as in the forward; P^T takes three planes, because dR carries fp32 gradients.
+#include "cawn_delta_mfma.hpp"
+
+namespace cawn {
+namespace delta {
+
+template <int NP, int KP> struct BackLds {
+    static constexpr int KB = Tile<NP, CHUNK, KP>::BYTES, TO = 2 * KB, P = TO + T_BYTES, BYTES = P + T_BYTES;
+    static constexpr int HELD = 163840 / (BYTES + (int)sizeof(Gates)), WAVES = HELD > 3 ? 3 : HELD;
+};
+
+template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__(256, (BackLds<NP, KP>::WAVES)) void delta_back(const Args a)
+{
+    using L = BackLds<NP, KP>;
+    constexpr int KS = KP / 32, KT = KP / 16, NT = 256, NW = 4;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ Gates G;
+    const Tile<NP, CHUNK, KP> k{(bf16 *)lds}, q{(bf16 *)(lds + L::KB)};
+    bf16x8 *tf = reinterpret_cast<bf16x8 *>(lds + L::TO), *pf = reinterpret_cast<bf16x8 *>(lds + L::P);
+    const int rows_all = a.B * a.H, blk = blockIdx.x, bh = blk % rows_all, nseg = MODE == 0 ? a.segments : a.segments - 1;
+    const int seg = blk / rows_all % nseg + (MODE == 0 ? 0 : 1), group = blk / rows_all / nseg, b = bh / a.H, h = bh % a.H;
+    const int len = row_length(a, b), nb = (len + CHUNK - 1) / CHUNK;
+    const int n0 = min(seg * a.seg_chunks, nb), n1 = min(n0 + a.seg_chunks, nb);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    int tid = threadIdx.x, lane = tid % 64, g = lane / 16, c = lane % 16;
+    const int ct = group * NW + w;
+    const bool mine = ct < a.VT;
+    int v = 16 * ct + c;
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+
+    f32x4 S[KT];                                // dS
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+        S[t] = zero;
+        if (MODE == 1 || !mine) continue;
+        if (seg < a.segments - 1) S[t] = *reinterpret_cast<const f32x4 *>(a.seg_s + (((size_t)bh * a.segments + seg) * KT * a.VT + (size_t)t * a.VT + ct) * 1024 + lane * 16);
+        else if (a.dstate_out && v < a.V) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (16 * t + 4 * g + r < a.K) S[t][r] = a.dstate_out[((long long)bh * a.K + 16 * t + 4 * g + r) * a.V + v];
+        }
+    }
+    auto anew = [&]() {                         // (as in delta_scan)
+        tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        lane = tid % 64, g = lane / 16, c = lane % 16, v = 16 * ct + c;
+    };
+    RowsAhead<T, NP, KP, NT> ka, qa;
+    constexpr int GN = (GATE_FLOATS + NT - 1) / NT;
+    float ga[GN];
+    auto ahead = [&](int n) {
+        const int rows = min(CHUNK, len - n * CHUNK);
+        const long long qat = b * a.qsb + (long long)n * CHUNK * a.qst + (long long)(h / (a.H / a.Hk)) * a.K;
+        ka.load(tid, (const T *)a.k + qat, a.qst, rows, a.K, a.vecq);
+        qa.load(tid, (const T *)a.q + qat, a.qst, rows, a.K, a.vecq);
+        const float *gp = a.gates + ((long long)bh * a.chunks + n) * GATE_FLOATS;
+#pragma unroll
+        for (int e = 0; e < GN; ++e) ga[e] = gp[min(tid + e * NT, GATE_FLOATS - 1)];
+    };
+    if (n0 < n1) ahead(n1 - 1);
+    for (int n = n1 - 1; n >= n0; --n) {
+        const int rows = min(CHUNK, len - n * CHUNK);
+        anew();
+        if (n < n1 - 1) __syncthreads();
+        ka.put_plain(tid, k, rows, a.K);
+        qa.put_plain(tid, q, rows, a.K);
+#pragma unroll
+        for (int e = 0; e < GN; ++e)
+            if (tid + e * NT < GATE_FLOATS) ((float *)&G)[tid + e * NT] = ga[e];
+        {
+            const char *src = a.tt_ops + ((size_t)bh * a.chunks + n) * T_BYTES + lane * 16;
+#pragma unroll
+            for (int u = 0; u < (T_BYTES / 1024 + NW - 1) / NW; ++u) {
+                const int i = u * NW + w;
+                if (i < T_BYTES / 1024) load_piece(src + (size_t)i * 1024, lds + L::TO + i * 1024);
+            }
+        }
+        __syncthreads();
+        T da[4][4];
+        if (mine) {
+            const T *dp = (const T *)a.dO + b * a.osb + (long long)n * CHUNK * a.ost + (long long)h * a.V;
+            if (rows == CHUNK && 16 * ct + 16 <= a.V) {
+                dp += 16 * ct;
+                const long long dlane = 4 * g * a.ost + c;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) da[t][r] = (dp + (16 * t + r) * a.ost)[dlane];
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) da[t][r] = dp[min(16 * t + 4 * g + r, rows - 1) * a.ost + min(v, a.V - 1)];
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (16 * t + 4 * g + r >= rows || v >= a.V) da[t][r] = (T)0.f;
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) da[t][r] = (T)0.f;
+        }
+        if (n > n0) ahead(n - 1);
+        anew();
+        // column tile w of scale P: its result layout is the operand of P^T
+        {
+            f32x4 p[4];
+            const int j = 16 * w + c;
+            const float m = a.scale * G.rk[j];
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                p[it] = zero;
+                if (it < w) continue;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) p[it] = mma<3>(q.straight(16 * it, 32 * ks, lane), k.straight(16 * w, 32 * ks, lane), p[it]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 16 * it + 4 * g + r;
+                    p[it][r] = i >= j ? p[it][r] * (m * G.rq[i] * decay_between(G, i, j)) : 0.f;
+                }
+            }
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                if (2 * ks + 1 < w) continue;
+                Frag<3> f;
+                split_tiles<3>(p[2 * ks], p[2 * ks + 1], f);
+#pragma unroll
+                for (int e = 0; e < 3; ++e) pf[(upper(w, ks) * 3 + e) * 64 + lane] = f.p[e];
+            }
+        }
+        if (MODE == 0 && mine) {
+            char *st = a.ds_tiles + ((size_t)bh * a.chunks + n) * KT * a.VT * 1024 + (size_t)ct * 1024 + lane * 16;
+#pragma unroll
+            for (int t = 0; t < KT; ++t) *reinterpret_cast<f32x4 *>(st + (size_t)t * a.VT * 1024) = S[t];
+        }
+        anew();
+        f32x4 Z[4] = {zero, zero, zero, zero}, R[4] = {zero, zero, zero, zero};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            Frag<3> sf;
+            Frag<NP> f[4];
+            split_tiles<3>(S[2 * ks], S[2 * ks + 1], sf);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) f[t] = k.tiled(16 * t, 32 * ks, lane);
+            mma_each<3>(f, sf, Z);
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) Z[t] *= *reinterpret_cast<const f32x4 *>(G.c + 16 * t + 4 * g);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();                        // the operands of T^T and P^T
+        anew();
+        // upper triangular: row tiles 0 and 1 take both halves of the tokens, 2 and 3 the second
+        auto times = [&](const bf16x8 *ops, const auto &lo, const auto &hi, f32x4 *acc) {
+            Frag<3> f[4], f2[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 3; ++e) f2[t].p[e] = ops[(upper(t, 0) * 3 + e) * 64 + lane];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 3; ++e) f[t].p[e] = ops[(upper(t, 1) * 3 + e) * 64 + lane];
+            mma_each<3>(f2, lo, acc);
+            mma_each<3>(f, hi, acc);
+        };
+        {
+            Frag<NP> df[2];
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) df[ks].p[0][e] = da[2 * ks + e / 4][e % 4];
+                } else {
+                    float y[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = (float)da[2 * ks + e / 4][e % 4];
+                    split8<NP>(y, df[ks]);
+                }
+            }
+            times(pf, df[0], df[1], Z);
+        }
+        {
+            Frag<3> zf[2];
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) split_tiles<3>(Z[2 * ks], Z[2 * ks + 1], zf[ks]);
+            times(tf, zf[0], zf[1], R);
+        }
+        if (MODE == 0 && mine) {
+            char *rt = a.dr_tiles + ((size_t)bh * a.chunks + n) * 4 * a.VT * 1024 + (size_t)ct * 1024 + lane * 16;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4 *>(rt + (size_t)t * a.VT * 1024) = R[t];
+        }
+        anew();
+        {
+            const float e = G.eg[CHUNK - 1];
+#pragma unroll
+            for (int t = 0; t < KT; ++t) S[t] *= e;
+            constexpr int AT = KT < 4 ? KT : 4;
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                Frag<3> of, rf;
+                f32x4 o[2], r[2];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int t = 2 * ks + half;
+                    const f32x4 eg = *reinterpret_cast<const f32x4 *>(G.eg + 16 * t + 4 * g), rq = *reinterpret_cast<const f32x4 *>(G.rq + 16 * t + 4 * g);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) o[half][x] = (float)da[t][x] * (a.scale * eg[x] * rq[x]);
+                    r[half] = -R[t] * *reinterpret_cast<const f32x4 *>(G.x + 16 * t + 4 * g);
+                }
+                split_tiles<3>(o[0], o[1], of);
+                split_tiles<3>(r[0], r[1], rf);
+#pragma unroll
+                for (int t0 = 0; t0 < KT; t0 += AT) {
+                    Frag<NP> f[AT];
+#pragma unroll
+                    for (int t = 0; t < AT; ++t) f[t] = q.tiled_down(32 * ks, 16 * (t0 + t), lane);
+                    mma_each<3>(f, of, S + t0);
+#pragma unroll
+                    for (int t = 0; t < AT; ++t) f[t] = k.tiled_down(32 * ks, 16 * (t0 + t), lane);
+                    mma_each<3>(f, rf, S + t0);
+                }
+            }
+        }
+    }
+    if (!mine) return;
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+        if (MODE == 1) *reinterpret_cast<f32x4 *>(a.seg_b + (((size_t)bh * a.segments + seg) * KT * a.VT + (size_t)t * a.VT + ct) * 1024 + lane * 16) = S[t];
+        else if (seg == 0 && a.dstate_in && v < a.V) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (16 * t + 4 * g + r < a.K) a.dstate_in[((long long)bh * a.K + 16 * t + 4 * g + r) * a.V + v] = S[t][r];
+        }
+    }
+}
+
+template <typename T, int NP, int KP> static int back_kp(const Args &a, hipStream_t s)
+{
+    constexpr int bytes = BackLds<NP, KP>::BYTES;
+    static_assert(bytes + sizeof(Gates) <= 163840, "LDS");
+    const long long wgs = (long long)a.B * a.H * ceil_div(a.VT, 4);
+    if (bytes > 60000 && (hipFuncSetAttribute((const void *)delta_back<T, NP, KP, 0>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess ||
+                          hipFuncSetAttribute((const void *)delta_back<T, NP, KP, 1>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess)) return CAWN_ELAUNCH;
+    if (a.segments > 1) {
+        hipLaunchKernelGGL((delta_back<T, NP, KP, 1>), dim3((unsigned)(wgs * (a.segments - 1))), dim3(256), bytes, s, a);
+        if (int r = launched()) return r;
+        if (int r = launch_join(a, true, s)) return r;
+    }
+    hipLaunchKernelGGL((delta_back<T, NP, KP, 0>), dim3((unsigned)(wgs * a.segments)), dim3(256), bytes, s, a);
+    return launched();
+}
+
+int launch_back(const Args &a, bool bf16_, hipStream_t s)
+{
+    if (a.K <= 32) return bf16_ ? back_kp<bf16, 1, 32>(a, s) : back_kp<float, 3, 32>(a, s);
+    if (a.K <= 64) return bf16_ ? back_kp<bf16, 1, 64>(a, s) : back_kp<float, 3, 64>(a, s);
+    return bf16_ ? back_kp<bf16, 1, 128>(a, s) : back_kp<float, 3, 128>(a, s);
+}
+
+} // namespace delta
+} // namespace cawn

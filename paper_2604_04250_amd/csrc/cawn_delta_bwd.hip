@@ -11,184 +11,13 @@
 // The last line: a decay scales all that a later query reads and all that came before it; summed over the places where e^{G_i} stands
 // (queries, keys that read, keys that write) the keys' two shares meet in dR.U and cancel, and what is left is the above.
 //
-// Three kernels, like the forward: what a chunk contributes by itself (delta_adjoint), the recurrence from the last chunk to the first
-// (delta_states, reversed), and the gradients of a chunk (delta_gradients).
+// dR and dS come from the recurrence (delta_back); here every chunk is a workgroup.
 #include <stddef.h>
 
 #include "cawn_delta_mfma.hpp"
 
 namespace cawn {
 namespace delta {
-
-// LDS of delta_adjoint, offsets in bytes: k, q, dO, the triangular system, and the operands of P^T and T^T (4 x 2 x 3 pieces each).
-// Three planes of 128 columns leave no room for all at once: dO and T^T then take the place of k behind its last use.
-template <int NP, int KP> struct AdjointLds {
-    static constexpr bool TIGHT = NP == 3 && KP == 128;
-    static constexpr int KB = Tile<NP, CHUNK, KP>::BYTES, OPS = 4 * 2 * 3 * 1024;
-    static constexpr int Q = KB, M = 2 * KB, P = M + CHUNK * TLD * 4, T = TIGHT ? 0 : P + OPS, D = T + OPS;
-    static constexpr int BYTES = TIGHT ? P + OPS : D + Tile<NP, CHUNK, 64>::BYTES;
-    static_assert(!TIGHT || D + Tile<NP, CHUNK, 64>::BYTES <= KB, "behind k's last use");
-};
-
-// Operands and tiles of the reversed delta_states: Wd = T^T KD, K^T, dR0 = T^T scale P^T dO, Y = scale (e^G Q)^T dO, gates.
-template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void delta_adjoint(const Args a)
-{
-    constexpr int KS = KP / 32, KT = KP / 16;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ Gates G;
-    const int blk = blockIdx.x, n = a.c0 + blk % (a.c1 - a.c0), bh = blk / (a.c1 - a.c0), h = bh % a.H, b = bh / a.H;
-    const int len = row_length(a, b), t0 = n * CHUNK, rows = min(CHUNK, len - t0);
-    if (rows <= 0) return;
-    const Sizes z(a.K, a.V, NP);
-    char *slot = a.ws + ((size_t)bh * a.span + (n - a.c0)) * z.bslot;
-    using A = AdjointLds<NP, KP>;
-    const Tile<NP, CHUNK, KP> k{(bf16 *)lds}, q{(bf16 *)(lds + A::Q)};
-    const Tile<NP, CHUNK, 64> d{(bf16 *)(lds + A::D)};
-    float *M = (float *)(lds + A::M);
-    bf16x8 *pf = reinterpret_cast<bf16x8 *>(lds + A::P), *tf = reinterpret_cast<bf16x8 *>(lds + A::T);
-    const int w = threadIdx.x / 64, lane = threadIdx.x % 64, g = lane / 16, c = lane % 16;
-    const long long qat = b * a.qsb + t0 * a.qst + (long long)(h / (a.H / a.Hk)) * a.K;
-    const T *dop = (const T *)a.dO + b * a.osb + t0 * a.ost + (long long)h * a.V;
-    stage_rows<T, NP, KP>(k, (const T *)a.k + qat, a.qst, rows, a.K, a.vecq, G.rk, a.norm, a.eps);
-    stage_rows<T, NP, KP>(q, (const T *)a.q + qat, a.qst, rows, a.K, a.vecq, G.rq, a.norm, a.eps);
-    if (!A::TIGHT) stage_rows<T, NP, 64>(d, dop, a.ost, rows, min(64, a.V), a.veco, nullptr, false, 0.f);
-    load_gates(a, G, b, h, t0, rows);
-    __syncthreads();
-    if (threadIdx.x < CHUNK) G.c[threadIdx.x] = -(G.beta[threadIdx.x] * G.eg[threadIdx.x] * G.rk[threadIdx.x]);
-    system_of<NP, KP>(k, G, M);
-    // column tile w of scale P: result layout has the rows i that the product P^T dO runs over
-    {
-        f32x4 p[4];
-        const int j = 16 * w + c;
-#pragma unroll
-        for (int it = 0; it < 4; ++it) {
-            p[it] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (it < w) continue;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) p[it] = mma<3>(q.straight(16 * it, 32 * ks, lane), k.straight(16 * w, 32 * ks, lane), p[it]);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * it + 4 * g + r;
-                p[it][r] = i >= j ? p[it][r] * (a.scale * G.rq[i] * G.rk[j] * decay_between(G, i, j)) : 0.f;
-            }
-        }
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            Frag<3> f;
-            split_tiles<3>(p[2 * ks], p[2 * ks + 1], f);
-#pragma unroll
-            for (int e = 0; e < 3; ++e) pf[((w * 2 + ks) * 3 + e) * 64 + lane] = f.p[e];
-        }
-    }
-    __syncthreads();
-    {
-        float *out = (float *)(slot + (size_t)(z.wf + z.kf + z.ut) * 1024);
-        for (int i = threadIdx.x; i < (int)(sizeof(Gates) / 4); i += 256) out[i] = ((const float *)&G)[i];
-        bf16x8 *kt = reinterpret_cast<bf16x8 *>(slot + (size_t)z.wf * 1024) + lane;
-        for (int u = w; u < KT * 2; u += 4) {
-            const Frag<NP> f = k.tiled_down(32 * (u % 2), 16 * (u / 2), lane);
-#pragma unroll
-            for (int p = 0; p < NP; ++p) kt[(u * NP + p) * 64] = f.p[p];
-        }
-    }
-    invert(M, w, lane);
-    {
-        // row tile w of T^T: plain for dR0 (shared), rows of KD scaled for Wd (own)
-        Frag<3> tw[2], tt[2];
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            float x[8], xw[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int i = 32 * ks + 16 * (e / 4) + 4 * g + e % 4;
-                x[e] = M[i * TLD + 16 * w + c];
-                xw[e] = x[e] * (G.ed[i] * G.rk[i]);
-            }
-            split8<3>(x, tt[ks]);
-            split8<3>(xw, tw[ks]);
-        }
-        bf16x8 *wf = reinterpret_cast<bf16x8 *>(slot) + lane;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            f32x4 acc[2];
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                acc[half] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (w < 2) acc[half] = mma<3>(k.tiled_down(0, 32 * ks + 16 * half, lane), tw[0], acc[half]);
-                acc[half] = mma<3>(k.tiled_down(32, 32 * ks + 16 * half, lane), tw[1], acc[half]);
-            }
-            Frag<3> f;
-            split_tiles<3>(acc[0], acc[1], f);
-#pragma unroll
-            for (int p = 0; p < 3; ++p) wf[((w * KS + ks) * 3 + p) * 64] = f.p[p];
-        }
-        if (A::TIGHT) __syncthreads();
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-            for (int e = 0; e < 3; ++e) tf[((w * 2 + ks) * 3 + e) * 64 + lane] = tt[ks].p[e];
-        if (A::TIGHT) stage_rows<T, NP, 64>(d, dop, a.ost, rows, min(64, a.V), a.veco, nullptr, false, 0.f);
-    }
-    __syncthreads();
-    char *x0 = slot + (size_t)(z.wf + z.kf) * 1024 + lane * 16, *y0 = slot + (size_t)(z.wf + z.kf + z.ut + 3) * 1024 + lane * 16;
-    for (int v0 = 0; v0 < a.V; v0 += 64) {
-        if (v0 > 0) {
-            __syncthreads();
-            stage_rows<T, NP, 64>(d, dop + v0, a.ost, rows, min(64, a.V - v0), a.veco, nullptr, false, 0.f);
-            __syncthreads();
-        }
-        const int vt = v0 / 16 + w;             // a wave's own column tile, all rows of it
-        if (vt >= a.VT) continue;
-        Frag<NP> df[2];
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) df[ks] = d.tiled_down(32 * ks, 16 * w, lane);
-        auto op = [&](const bf16x8 *base, int t, int ks) {
-            Frag<3> f;
-#pragma unroll
-            for (int e = 0; e < 3; ++e) f.p[e] = base[((t * 2 + ks) * 3 + e) * 64 + lane];
-            return f;
-        };
-        f32x4 Y[4];
-#pragma unroll
-        for (int jt = 0; jt < 4; ++jt) {
-            Y[jt] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (jt < 2) Y[jt] = mma<3>(op(pf, jt, 0), df[0], Y[jt]);
-            Y[jt] = mma<3>(op(pf, jt, 1), df[1], Y[jt]);
-        }
-        Frag<3> yf[2];
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) split_tiles<3>(Y[2 * ks], Y[2 * ks + 1], yf[ks]);
-#pragma unroll
-        for (int jt = 0; jt < 4; ++jt) {
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-            if (jt < 2) acc = mma<3>(op(tf, jt, 0), yf[0], acc);
-            acc = mma<3>(op(tf, jt, 1), yf[1], acc);
-            *reinterpret_cast<f32x4 *>(x0 + ((size_t)jt * a.VT + vt) * 1024) = acc;
-        }
-        // Y: rows of dO scaled in fp32
-        Frag<3> sf[2];
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int i = 32 * ks + 16 * (e / 4) + 4 * g + e % 4;
-                float s = 0.f;
-#pragma unroll
-                for (int p = NP - 1; p >= 0; --p) s += (float)df[ks].p[p][e];
-                x[e] = s * (a.scale * G.rq[i] * G.eg[i]);
-            }
-            split8<3>(x, sf[ks]);
-        }
-#pragma unroll
-        for (int t = 0; t < KT; ++t) {
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) acc = mma<3>(q.tiled_down(32 * ks, 16 * t, lane), sf[ks], acc);
-            *reinterpret_cast<f32x4 *>(y0 + ((size_t)t * a.VT + vt) * 1024) = acc;
-        }
-    }
-}
 
 // Gradients of a chunk.  A workgroup takes all value heads of a key head, one after the other, and keeps dq and dk in registers: wave w
 // rows 16 w .. of them.  First everything that runs over the value columns, 32 at a time, with U, dR, S0 and dS in LDS as they come
@@ -241,7 +70,7 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ Gates G;
     __shared__ float qdq[CHUNK], vdv[CHUNK], udr[CHUNK], part[4];
-    const int blk = blockIdx.x, n = a.c0 + blk % (a.c1 - a.c0), bk = blk / (a.c1 - a.c0), hk = bk % a.Hk, b = bk / a.Hk, rep = a.H / a.Hk;
+    const int blk = blockIdx.x, n = blk % a.chunks, bk = blk / a.chunks, hk = bk % a.Hk, b = bk / a.Hk, rep = a.H / a.Hk;
     const int len = row_length(a, b), t0 = n * CHUNK, rows = min(CHUNK, len - t0), all = min(CHUNK, a.L - t0);
     const long long qat = b * a.qsb + t0 * a.qst + (long long)hk * a.K;
     const int w = threadIdx.x / 64, lane = threadIdx.x % 64, g = lane / 16, c = lane % 16;
@@ -263,7 +92,7 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
         }
         return;
     }
-    const Sizes z(a.K, a.V, NP);
+    const Sizes z(a.K, a.V);
     const typename L::MatU ut{(bf16 *)lds};
     const typename L::MatR rt{(bf16 *)(lds + L::MatU::BYTES)};
     const typename L::MatS st{(bf16 *)(lds + L::MatU::BYTES + L::MatR::BYTES)};
@@ -278,13 +107,13 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
     for (int t = 0; t < KT; ++t) dq[t] = dk[t] = zero;
     for (int hh = 0; hh < rep; ++hh) {
         const int h = hk * rep + hh, bh = b * a.H + h;
-        const char *slot = a.ws + ((size_t)bh * a.span + (n - a.c0)) * z.bslot;
-        const char *sp = a.s_tiles + bh * a.s_row + (n - a.s_first) * a.s_chunk, *up = a.u_tiles + bh * a.u_row + (n - a.u_first) * a.u_chunk;
-        const char *rp = slot + (size_t)(z.wf + z.kf) * 1024, *dp = slot + (size_t)(z.wf + z.kf + z.ut + 3 + z.st) * 1024;
+        const size_t at = (size_t)bh * a.chunks + n;
+        const char *sp = a.s_tiles + bh * a.s_row + n * a.s_chunk, *up = a.u_tiles + bh * a.u_row + n * a.u_chunk;
+        const char *rp = a.dr_tiles + at * z.ut * 1024, *dp = a.ds_tiles + at * z.st * 1024;
         __syncthreads();                        // the previous head's LDS
         {
-            const float *in = (const float *)(slot + (size_t)(z.wf + z.kf + z.ut) * 1024);
-            for (int i = threadIdx.x; i < (int)(sizeof(Gates) / 4); i += 256) ((float *)&G)[i] = in[i];
+            const float *in = a.gates + at * GATE_FLOATS;
+            for (int i = threadIdx.x; i < GATE_FLOATS; i += 256) ((float *)&G)[i] = in[i];
         }
         if (threadIdx.x < CHUNK) vdv[threadIdx.x] = udr[threadIdx.x] = 0.f;
         f32x4 A1[KT], A2[KT], A3[KT], zt[4], mt[4];
@@ -513,29 +342,14 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
     }
 }
 
-template <typename T, int NP, int KP> static int adjoint_kp(const Args &a, hipStream_t s)
-{
-    constexpr int bytes = AdjointLds<NP, KP>::BYTES;
-    static_assert(bytes + sizeof(Gates) <= 163840, "LDS");
-    if (hipFuncSetAttribute((const void *)delta_adjoint<T, NP, KP>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CAWN_ELAUNCH;
-    hipLaunchKernelGGL((delta_adjoint<T, NP, KP>), dim3((unsigned)((long long)a.B * a.H * (a.c1 - a.c0))), dim3(256), bytes, s, a);
-    return launched();
-}
-
 template <typename T, int NP, int KP> static int gradients_kp(const Args &a, hipStream_t s)
 {
     constexpr int bytes = GradLds<T, NP, KP>::BYTES;
+    if (a.chunks == 0) return CAWN_OK;
     static_assert(bytes + sizeof(Gates) + 1024 <= 163840, "LDS");
     if (hipFuncSetAttribute((const void *)delta_gradients<T, NP, KP>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CAWN_ELAUNCH;
-    hipLaunchKernelGGL((delta_gradients<T, NP, KP>), dim3((unsigned)((long long)a.B * a.Hk * (a.c1 - a.c0))), dim3(256), bytes, s, a);
+    hipLaunchKernelGGL((delta_gradients<T, NP, KP>), dim3((unsigned)((long long)a.B * a.Hk * a.chunks)), dim3(256), bytes, s, a);
     return launched();
-}
-
-int launch_adjoint(const Args &a, bool bf16_, hipStream_t s)
-{
-    if (a.K <= 32) return bf16_ ? adjoint_kp<bf16, 1, 32>(a, s) : adjoint_kp<float, 3, 32>(a, s);
-    if (a.K <= 64) return bf16_ ? adjoint_kp<bf16, 1, 64>(a, s) : adjoint_kp<float, 3, 64>(a, s);
-    return bf16_ ? adjoint_kp<bf16, 1, 128>(a, s) : adjoint_kp<float, 3, 128>(a, s);
 }
 
 int launch_gradients(const Args &a, bool bf16_, hipStream_t s)

@@ -42,6 +42,33 @@ template <int S, int NA, int NB> __device__ inline f32x4 mma(const Frag<NA> &a, 
     return acc;
 }
 
+// N products with a factor in common, side by side: one instruction's result is the next one's operand, so a product by itself is a
+// chain of waits
+template <int S, int N, int NA, int NB> __device__ inline void mma_each(const Frag<NA> (&a)[N], const Frag<NB> &b, f32x4 *acc)
+{
+#pragma unroll
+    for (int s = S - 1; s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int j = s - i;
+            if (j < 0 || j >= NB) continue;
+#pragma unroll
+            for (int n = 0; n < N; ++n) acc[n] = mfma(a[n].p[i], b.p[j], acc[n]);
+        }
+}
+template <int S, int N, int NA, int NB> __device__ inline void mma_each(const Frag<NA> &a, const Frag<NB> (&b)[N], f32x4 *acc)
+{
+#pragma unroll
+    for (int s = S - 1; s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int j = s - i;
+            if (j < 0 || j >= NB) continue;
+#pragma unroll
+            for (int n = 0; n < N; ++n) acc[n] = mfma(a.p[i], b[n].p[j], acc[n]);
+        }
+}
+
 template <int N> __device__ inline void split8(const float (&x)[8], Frag<N> &f)
 {
 #pragma unroll
@@ -68,6 +95,7 @@ template <int N> __device__ inline void split_tiles(f32x4 lo, f32x4 hi, Frag<N> 
 __device__ inline constexpr int lower(int t, int ks) { return t < 2 ? t : 2 + (t - 2) * 2 + ks; }
 __device__ inline constexpr int upper(int t, int ks) { return t < 2 ? t * 2 + ks : 2 + t; }
 constexpr int T_BYTES = 6 * 3 * 1024;
+static_assert(T_BYTES == OPERAND_BYTES, "");
 
 // 1 KiB from memory straight into LDS, 16 bytes a lane; src the lane's, dst the wave's (the same in all lanes).  Waited for with vmcnt
 __device__ inline void load_piece(const char *src, char *dst)
@@ -362,25 +390,6 @@ __device__ inline void invert(float *T, int w, int lane)         // (waves beyon
     __syncthreads();
     if (w < 4) put16(T + (32 + 16 * rt) * TLD + 16 * ct, out, lane, -1.f);
     __syncthreads();
-}
-
-// beta_i N_ij of the chunk into T (fp32, zeros on and above the diagonal): wave w makes row tile w
-template <int N, int KP> __device__ inline void system_of(const Tile<N, CHUNK, KP> &k, const Gates &G, float *T)
-{
-    const int w = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 16, g = lane / 16;
-    for (int ct = 0; ct < 4; ++ct) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        if (ct <= w) {
-#pragma unroll
-            for (int ks = 0; ks < KP / 32; ++ks) acc = mma<3>(k.straight(16 * w, 32 * ks, lane), k.straight(16 * ct, 32 * ks, lane), acc);
-        }
-        const int j = 16 * ct + c;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = 16 * w + 4 * g + r;
-            T[i * TLD + j] = i > j ? acc[r] * (G.beta[i] * G.rk[i] * G.rk[j] * decay_between(G, i, j)) : 0.f;
-        }
-    }
 }
 
 } // namespace delta

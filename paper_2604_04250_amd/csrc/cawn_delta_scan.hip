@@ -3,7 +3,7 @@
 // The chunks of a row are a chain, and a chain is as slow as its links; so the row is cut into segments, each of them some chunks that
 // a workgroup takes one after the other with the state in its registers:
 //   delta_system  what a chunk is by itself: running sums of the decays, norms, T; all chunks at once
-//   delta_scan    MODE 1, all segments but the last at once: what a segment makes of a state, S_end = A S_begin + b; A comes from running
+//   delta_scan    MODE 1, all segments at once (the last only for a backward, which takes A from here): what a segment makes of a state, S_end = A S_begin + b; A comes from running
 //                 the recurrence on the columns of the identity with v = 0
 //   delta_join    the states at the segments' begins, one product a segment
 //   delta_scan    MODE 0, all segments at once: the outputs
@@ -98,21 +98,12 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
     }
 }
 
-#ifndef FENCE
-#define FENCE __builtin_amdgcn_sched_barrier(0);
-#endif
-#ifndef WMAX0
-#define WMAX0 3
-#endif
-#ifndef WMAX1
-#define WMAX1 2
-#endif
 template <int NP, int KP, int MODE> struct ScanLds {
     static constexpr int PO = NP == 1 ? 2 : 3;
     static constexpr int KB = Tile<NP, CHUNK, KP>::BYTES, TO = MODE == 0 ? 2 * KB : KB;     // k, q; T's operands; P's
     static constexpr int P = TO + T_BYTES, BYTES = P + (MODE == 0 ? 6 * PO * 1024 : 0);
-    // waves a SIMD that the registers are budgeted for: as many workgroups as the LDS holds
-    static constexpr int HELD = 163840 / (BYTES + (int)sizeof(Gates)), WAVES = MODE == 0 ? (HELD > WMAX0 ? WMAX0 : HELD) : (HELD > WMAX1 ? WMAX1 : HELD) * 2;
+    // waves a SIMD that the registers are budgeted for: as many workgroups as the LDS holds, three (MODE 1, of eight waves: two) at most
+    static constexpr int HELD = 163840 / (BYTES + (int)sizeof(Gates)), WAVES = MODE == 0 ? (HELD > 3 ? 3 : HELD) : (HELD > 2 ? 2 : HELD) * 2;
 };
 
 template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MODE == 0 ? 256 : 512), (ScanLds<NP, KP, MODE>::WAVES)) void delta_scan(const Args a)
@@ -123,7 +114,7 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
     __shared__ Gates G;
     const Tile<NP, CHUNK, KP> k{(bf16 *)lds}, q{(bf16 *)(lds + L::KB)};
     bf16x8 *tf = reinterpret_cast<bf16x8 *>(lds + L::TO), *pf = reinterpret_cast<bf16x8 *>(lds + L::P);
-    const int rows_all = a.B * a.H, blk = blockIdx.x, bh = blk % rows_all, nseg = MODE == 0 ? a.segments : a.segments - 1;
+    const int rows_all = a.B * a.H, blk = blockIdx.x, bh = blk % rows_all, nseg = MODE == 0 || a.tt_ops ? a.segments : a.segments - 1;
     const int seg = blk / rows_all % nseg, group = blk / rows_all / nseg, b = bh / a.H, h = bh % a.H;
     const int len = row_length(a, b), nb = (len + CHUNK - 1) / CHUNK;
     const int n0 = min(seg * a.seg_chunks, nb), n1 = min(n0 + a.seg_chunks, nb);
@@ -240,7 +231,6 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
                         pt[jt][r] = i >= j ? pt[jt][r] * (G.rk[j] * decay_between(G, i, j)) : 0.f;
                     }
                 }
-                FENCE
             }
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
@@ -264,28 +254,29 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
             Frag<3> sf[KS];
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) split_tiles<3>(S[2 * ks], S[2 * ks + 1], sf[ks]);
-            f32x4 X[4];
+            f32x4 X[4] = {zero, zero, zero, zero};
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                X[t] = zero;
+            for (int ks = 0; ks < KS; ++ks) {
+                Frag<NP> f[4];
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) X[t] = mma<3>(k.tiled(16 * t, 32 * ks, lane), sf[ks], X[t]);
-                FENCE
+                for (int t = 0; t < 4; ++t) f[t] = k.tiled(16 * t, 32 * ks, lane);
+                mma_each<3>(f, sf[ks], X);
             }
             if (MODE == 0) {
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    O[t] = zero;
+                for (int t = 0; t < 4; ++t) O[t] = zero;
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) {
-                        Frag<PO> f;
+                for (int ks = 0; ks < KS; ++ks) {
+                    Frag<PO> s;
+                    Frag<NP> f[4];
 #pragma unroll
-                        for (int e = 0; e < PO; ++e) f.p[e] = sf[ks].p[e];
-                        O[t] = mma<PO>(f, q.tiled(16 * t, 32 * ks, lane), O[t]);
-                    }
-                    O[t] *= G.eg[16 * t + c];
-                    FENCE
+                    for (int e = 0; e < PO; ++e) s.p[e] = sf[ks].p[e];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) f[t] = q.tiled(16 * t, 32 * ks, lane);
+                    mma_each<PO>(s, f, O);
                 }
+#pragma unroll
+                for (int t = 0; t < 4; ++t) O[t] *= G.eg[16 * t + c];
             }
             Frag<3> xf[2];
 #pragma unroll
@@ -299,19 +290,20 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();                    // T's and P's operands
             anew();
+            Frag<3> f[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 U[t] = zero;
 #pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-                    if (2 * ks > t) break;
-                    Frag<3> f;
-#pragma unroll
-                    for (int e = 0; e < 3; ++e) f.p[e] = tf[(lower(t, ks) * 3 + e) * 64 + lane];
-                    U[t] = mma<3>(f, xf[ks], U[t]);
-                }
-                FENCE
+                for (int e = 0; e < 3; ++e) f[t].p[e] = tf[(lower(t, 0) * 3 + e) * 64 + lane];
             }
+            mma_each<3>(f, xf[0], U);
+            Frag<3> f2[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 3; ++e) f2[t].p[e] = tf[(lower(2 + t, 1) * 3 + e) * 64 + lane];
+            mma_each<3>(f2, xf[1], U + 2);
         }
         anew();
         if (MODE == 0) {
@@ -326,17 +318,21 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
             const int all = min(CHUNK, a.L - n * CHUNK);
             const long long olane = c * a.ost + 4 * g;      // a lane's place among rows of o
             T *op = (T *)a.o + b * a.osb + (long long)n * CHUNK * a.ost + (long long)h * a.V + 16 * ct;
+            {
+                Frag<PO> f[4], f2[2];
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int e = 0; e < PO; ++e) f[t].p[e] = pf[(lower(t, 0) * PO + e) * 64 + lane];
+                mma_each<PO>(uf[0], f, O);
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < PO; ++e) f2[t].p[e] = pf[(lower(2 + t, 1) * PO + e) * 64 + lane];
+                mma_each<PO>(uf[1], f2, O + 2);
+            }
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-#pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-                    if (2 * ks > t) break;
-                    Frag<PO> f;
-#pragma unroll
-                    for (int e = 0; e < PO; ++e) f.p[e] = pf[(lower(t, ks) * PO + e) * 64 + lane];
-                    O[t] = mma<PO>(uf[ks], f, O[t]);
-                }
-                FENCE
                 const int i = 16 * t + c;
                 const float m = i < rows ? a.scale * G.rq[i] : 0.f;
                 float y[4];
@@ -368,12 +364,17 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
             }
             const float e = G.eg[CHUNK - 1];
 #pragma unroll
-            for (int t = 0; t < KT; ++t) {
-                S[t] *= e;
+            for (int t = 0; t < KT; ++t) S[t] *= e;
+            constexpr int AT = KT < 4 ? KT : 4;
 #pragma unroll
-                for (int ks = 0; ks < 2; ++ks) S[t] = mma<3>(k.tiled_down(32 * ks, 16 * t, lane), uf[ks], S[t]);
-                FENCE
-            }
+            for (int t0 = 0; t0 < KT; t0 += AT)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    Frag<NP> f[AT];
+#pragma unroll
+                    for (int t = 0; t < AT; ++t) f[t] = k.tiled_down(32 * ks, 16 * (t0 + t), lane);
+                    mma_each<3>(f, uf[ks], S + t0);
+                }
         }
     }
     if (MODE == 0) {
@@ -415,7 +416,7 @@ template <typename T, int NP, int KP> static int scan_kp(const Args &a, hipStrea
     if (a.segments > 1) {
         constexpr int bytes = ScanLds<NP, KP, 1>::BYTES;
         if (bytes > 60000 && hipFuncSetAttribute((const void *)delta_scan<T, NP, KP, 1>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CAWN_ELAUNCH;
-        hipLaunchKernelGGL((delta_scan<T, NP, KP, 1>), dim3((unsigned)(rows * (a.segments - 1) * ceil_div(a.VT + KP / 16, 8))), dim3(512), bytes, s, a);
+        hipLaunchKernelGGL((delta_scan<T, NP, KP, 1>), dim3((unsigned)(rows * (a.tt_ops ? a.segments : a.segments - 1) * ceil_div(a.VT + KP / 16, 8))), dim3(512), bytes, s, a);
         if (int r = launched()) return r;
         if (int r = launch_join(a, false, s)) return r;
     }
