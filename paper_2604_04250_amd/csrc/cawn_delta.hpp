@@ -31,7 +31,8 @@ struct Args {
     float *ddecay, *dbeta, *dstate_in;
     int chunks, slabs;              // chunks of a full row; (token form) slabs of a head's columns
     int vec4;                       // state rows may be read 16 bytes at a time
-    int vecq, vecv, veco;           // rows of q, k (dq, dk), of v (dv), of o (dO) may be: 16 bytes at a time
+    int vecq, veco;                 // rows of q and k, of o (four values) and dO (16 bytes) may be taken several values at a time
+    int vecd;                       // rows of dq, dk: four values
     // Chunked form.  Tiles of the state before each chunk (and behind the last) and of u, kept for a backward (null: not wanted): those of
     // chunk n of head bh begin bh * row + n * chunk bytes behind
     int VT;                         // tiles of 16 value columns

@@ -163,6 +163,7 @@ int cawn_delta_rule_bwd(const cawn_delta_desc *d, const void *q, const void *k, 
     a.dq = dq, a.dk = dk, a.dv = dv, a.ddecay = ddecay, a.dbeta = dbeta, a.dstate_in = (float *)dstate_in;
     a.vecq = a.K % w == 0 && a.qst % w == 0 && a.qsb % w == 0 && aligned_to(q, 16) && aligned_to(k, 16);
     a.veco = a.V % w == 0 && a.ost % w == 0 && a.osb % w == 0 && aligned_to(dO, 16);
+    a.vecd = a.K % 4 == 0 && a.qst % 4 == 0 && a.qsb % 4 == 0 && aligned_to(dq, 4 * e) && aligned_to(dk, 4 * e);
     keep(&a, l, const_cast<void *>(ckpt));
     char *ws = (char *)workspace;
     a.dr_tiles = ws, a.ds_tiles = ws + l.ds, a.seg_b = ws + l.rb, a.seg_s = ws + l.rs;

@@ -37,6 +37,7 @@ template <typename T, int NP, int KP> struct GradLds {
     static constexpr int FIRST = MatU::BYTES + MatR::BYTES + MatS::BYTES + MatD::BYTES + MatO::BYTES;
     static constexpr int SECOND = 2 * MatQ::BYTES + MatZ::BYTES + MatM::BYTES;
     static constexpr int BYTES = FIRST > SECOND ? FIRST : SECOND;
+    static constexpr int HELD = 163840 / (BYTES + 4096), WAVES = HELD > 2 ? 2 : HELD;     // waves a SIMD: as many workgroups as the LDS holds, two at most
 };
 
 // four rows of a column, N planes, into a transposed matrix
@@ -55,6 +56,20 @@ template <int N, int ROWS, int COLS> __device__ inline void put_column(const Til
     }
 }
 
+// four values of a row, from their planes
+template <int N, int ROWS, int COLS> __device__ inline void row_of(const Tile<N, ROWS, COLS> &t, int row, int col, float (&x)[4])
+{
+    bf16x4 h[N];
+#pragma unroll
+    for (int p = 0; p < N; ++p) h[p] = *reinterpret_cast<const bf16x4 *>(t.p + p * Tile<N, ROWS, COLS>::PLANE + row * Tile<N, ROWS, COLS>::LD + col);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        x[r] = 0.f;
+#pragma unroll
+        for (int p = N - 1; p >= 0; --p) x[r] += (float)h[p][r];
+    }
+}
+
 // sum over the 16 lanes of a result tile's row
 __device__ inline float row_sum(float x)
 {
@@ -63,7 +78,8 @@ __device__ inline float row_sum(float x)
     return x;
 }
 
-template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void delta_gradients(const Args a)
+// SHARED: several value heads to a key head
+template <typename T, int NP, int KP, bool SHARED> __global__ __launch_bounds__(256, (GradLds<T, NP, KP>::WAVES)) void delta_gradients(const Args a)
 {
     using L = GradLds<T, NP, KP>;
     constexpr int KT = KP / 16, PK = L::PK, OWN = (KT + 3) / 4;
@@ -73,7 +89,13 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
     const int blk = blockIdx.x, n = blk % a.chunks, bk = blk / a.chunks, hk = bk % a.Hk, b = bk / a.Hk, rep = a.H / a.Hk;
     const int len = row_length(a, b), t0 = n * CHUNK, rows = min(CHUNK, len - t0), all = min(CHUNK, a.L - t0);
     const long long qat = b * a.qsb + t0 * a.qst + (long long)hk * a.K;
-    const int w = threadIdx.x / 64, lane = threadIdx.x % 64, g = lane / 16, c = lane % 16;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    int tid = threadIdx.x, lane = tid % 64, g = lane / 16, c = lane % 16;
+    auto anew = [&]() {                         // (as in delta_scan)
+        tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        lane = tid % 64, g = lane / 16, c = lane % 16;
+    };
     if (rows <= 0) {                            // tokens that the row does not have
         for (int i = threadIdx.x; i < all * a.K; i += 256) {
             const long long at = qat + (long long)(i / a.K) * a.qst + i % a.K;
@@ -103,19 +125,17 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
     const typename L::MatM mm{(bf16 *)(lds + 2 * L::MatQ::BYTES + L::MatZ::BYTES)};
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     f32x4 dq[KT], dk[KT];
+    if (SHARED) {
 #pragma unroll
-    for (int t = 0; t < KT; ++t) dq[t] = dk[t] = zero;
-    for (int hh = 0; hh < rep; ++hh) {
+        for (int t = 0; t < KT; ++t) dq[t] = dk[t] = zero;
+    }
+    for (int hh = 0; hh < (SHARED ? rep : 1); ++hh) {
         const int h = hk * rep + hh, bh = b * a.H + h;
         const size_t at = (size_t)bh * a.chunks + n;
         const char *sp = a.s_tiles + bh * a.s_row + n * a.s_chunk, *up = a.u_tiles + bh * a.u_row + n * a.u_chunk;
         const char *rp = a.dr_tiles + at * z.ut * 1024, *dp = a.ds_tiles + at * z.st * 1024;
         __syncthreads();                        // the previous head's LDS
-        {
-            const float *in = a.gates + at * GATE_FLOATS;
-            for (int i = threadIdx.x; i < GATE_FLOATS; i += 256) ((float *)&G)[i] = in[i];
-        }
-        if (threadIdx.x < CHUNK) vdv[threadIdx.x] = udr[threadIdx.x] = 0.f;
+        anew();
         f32x4 A1[KT], A2[KT], A3[KT], zt[4], mt[4];
 #pragma unroll
         for (int t = 0; t < KT; ++t) A1[t] = A2[t] = A3[t] = zero;
@@ -128,6 +148,7 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
         f32x4 tu[2], tr[2], ts[OWN][2], te[OWN][2], td[OWN][2];
         T tv[2][4];
         RowsAhead<T, NP, 32, 256> to;
+        RowsAhead<T, NP, KP, 256> qa, ka;
         auto ahead = [&](int v0) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -145,11 +166,13 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
 #pragma unroll
                 for (int e = 0; e < 4; ++e) tv[half][e] = vp[min(16 * w + 4 * g + e, rows - 1) * a.vst];
             }
-            to.load(threadIdx.x, (const T *)a.dO + b * a.osb + (long long)t0 * a.ost + (long long)h * a.V + v0, a.ost, rows, min(32, a.V - v0), a.veco);
+            to.load(tid, (const T *)a.dO + b * a.osb + (long long)t0 * a.ost + (long long)h * a.V + v0, a.ost, rows, min(32, a.V - v0), a.veco);
         };
         ahead(0);
+        for (int i = tid; i < GATE_FLOATS; i += 256) ((float *)&G)[i] = a.gates[at * GATE_FLOATS + i];
         for (int v0 = 0; v0 < a.V; v0 += 32) {
             __syncthreads();
+            anew();
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int vt = v0 / 16 + half, v = 16 * vt + c;
@@ -177,9 +200,14 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
                     for (int x = 0; x < 4; ++x) inner += d[x] * te[o][half][x];
                 }
             }
-            to.put_plain(threadIdx.x, ot, rows, min(32, a.V - v0));
+            to.put_plain(tid, ot, rows, min(32, a.V - v0));
             __syncthreads();
             if (v0 + 32 < a.V) ahead(v0 + 32);
+            else {                              // the second half's
+                qa.load(tid, (const T *)a.q + qat, a.qst, rows, a.K, a.vecq);
+                ka.load(tid, (const T *)a.k + qat, a.qst, rows, a.K, a.vecq);
+            }
+            anew();
             const Frag<NP> o = ot.straight(16 * w, 0, lane);
             const Frag<3> r = rt.straight_down(0, 16 * w, lane);
             Frag<PK> u;
@@ -188,20 +216,27 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
 #pragma unroll
                 for (int p = 0; p < PK; ++p) u.p[p] = u3.p[p];
             }
-            // Z^T and M^T (before their factors): rows j, column i = c of row tile w
+            // before their factors: Z^T and M^T, rows j and column i = c of row tile w; dO S0^T and the like, rows f and column i = c
 #pragma unroll
-            for (int jt = 0; jt < 4; ++jt) {
-                if (jt > w) break;
-                const Frag<3> uj = ut.straight_down(0, 16 * jt, lane);
-                zt[jt] = mma<3>(uj, o, zt[jt]);
-                mt[jt] = mma<PK>(uj, r, mt[jt]);
+            for (int j0 = 0; j0 < 4; j0 += 2) {         // (two at a time: registers)
+                if (j0 > w) break;
+                Frag<3> uj[2];
+#pragma unroll
+                for (int jt = 0; jt < 2; ++jt) uj[jt] = ut.straight_down(0, 16 * (j0 + jt), lane);
+                mma_each<3>(uj, o, zt + j0);            // (one beyond row tile w: it is masked below)
+                mma_each<PK>(uj, r, mt + j0);
+                __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
-            for (int t = 0; t < KT; ++t) {
-                const Frag<3> s = st.straight_down(0, 16 * t, lane);
-                A1[t] = mma<3>(o, s, A1[t]);
-                A2[t] = mma<PK>(r, s, A2[t]);
-                A3[t] = mma<PK>(u, dt.straight_down(0, 16 * t, lane), A3[t]);
+            for (int t0 = 0; t0 < KT; t0 += 2) {
+                Frag<3> f[2];
+                Frag<PK> d[2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) f[t] = st.straight_down(0, 16 * (t0 + t), lane), d[t] = dt.straight_down(0, 16 * (t0 + t), lane);
+                mma_each<3>(f, o, A1 + t0);
+                mma_each<PK>(f, r, A2 + t0);
+                mma_each<PK>(d, u, A3 + t0);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
 #pragma unroll
@@ -213,92 +248,77 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
         for (int m = 32; m > 0; m >>= 1) inner += __shfl_xor(inner, m);
         if (lane == 0) part[w] = inner;
         __syncthreads();                        // the LDS of the first half is free
-        stage_rows<T, NP, KP>(qm, (const T *)a.q + qat, a.qst, rows, a.K, a.vecq, nullptr, false, 0.f);
-        stage_rows<T, NP, KP>(km, (const T *)a.k + qat, a.qst, rows, a.K, a.vecq, nullptr, false, 0.f);
-        {
-            const int i = 16 * w + c;
+        anew();
+        qa.put_plain(tid, qm, rows, a.K);
+        ka.put_plain(tid, km, rows, a.K);
+        const int i = 16 * w + c;               // the lane's token from here on
+        const float eg = G.eg[i], beta = G.beta[i], rk = G.rk[i], rq = G.rq[i], sq = a.scale * rq, bk = -beta * rk;
 #pragma unroll
-            for (int jt = 0; jt < 4; ++jt) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int j = 16 * jt + 4 * g + r;
-                    const float D = i >= j ? decay_between(G, i, j) : 0.f;
-                    zt[jt][r] = i >= j ? zt[jt][r] * (a.scale * D) : 0.f;
-                    mt[jt][r] = i > j ? -mt[jt][r] * (G.beta[i] * D) : 0.f;
-                }
-                put_column(zm, i, 16 * jt + 4 * g, zt[jt]);     // (here the column of the transpose is the row)
-                put_column(mm, i, 16 * jt + 4 * g, mt[jt]);
-            }
-        }
-        __syncthreads();
-        // dq^ = scale e^G A1 + Z (rk k);  dk^ = -beta e^G A2 + e^{G_C - G} A3 + M (rk k) + Z^T (rq q) + M^T (rk k): the norms' factors of the
-        // summed tokens scale Z's and M's columns (rows), so they are applied to the operand
-        auto scaled = [&](auto f, const float *by, int k0) {     // f's eight steps times by[step]
-            constexpr int N = sizeof(f) / 16;
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float s = 0.f;
-#pragma unroll
-                for (int p = N - 1; p >= 0; --p) s += (float)f.p[p][e];
-                x[e] = s * by[k0 + 8 * g + e];
-            }
-            decltype(f) y;
-            split8<N>(x, y);
-            return y;
-        };
-        f32x4 q1[KT];
-#pragma unroll
-        for (int t = 0; t < KT; ++t) {
+        for (int jt = 0; jt < 4; ++jt) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int i = 16 * w + 4 * g + r;
-                q1[t][r] = a.scale * G.eg[i] * A1[t][r];
-                A2[t][r] = G.ed[i] * A3[t][r] - G.beta[i] * G.eg[i] * A2[t][r];
+                const int j = 16 * jt + 4 * g + r;
+                const float D = i >= j ? G.rk[j] * decay_between(G, i, j) : 0.f;
+                zt[jt][r] = i >= j ? zt[jt][r] * (sq * D) : 0.f;
+                mt[jt][r] = i > j ? mt[jt][r] * (bk * D) : 0.f;
             }
+            put_column(zm, i, 16 * jt + 4 * g, zt[jt]);         // (here the column of the transpose is the row)
+            put_column(mm, i, 16 * jt + 4 * g, mt[jt]);
         }
+        // y = r dx^ of the norm's x^ = r x:  yq = scale rq e^G A1 + Z k,  yk = rk (e^{G_C - G} A3 - beta e^G A2) + M k + Z^T q + M^T k
+        const float f1 = sq * eg, f2 = bk * eg, f3 = rk * G.ed[i];
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+            A1[t] *= f1;
+            A2[t] = f3 * A3[t] + f2 * A2[t];
+        }
+        __syncthreads();
+        anew();
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-            if (2 * ks <= w) {
-                const Frag<3> zf = scaled(zm.straight(16 * w, 32 * ks, lane), G.rk, 32 * ks);
-                const Frag<PK> mf = scaled(mm.straight(16 * w, 32 * ks, lane), G.rk, 32 * ks);
+            constexpr int AT = KT < 4 ? KT : 4;
+            const bool left = 2 * ks <= w, right = 2 * ks + 1 >= w;
+            Frag<3> zf, zd;
+            Frag<PK> mf, md;
+            if (left) zf = zm.straight(16 * w, 32 * ks, lane), mf = mm.straight(16 * w, 32 * ks, lane);
+            if (right) zd = zm.straight_down(32 * ks, 16 * w, lane), md = mm.straight_down(32 * ks, 16 * w, lane);
 #pragma unroll
-                for (int t = 0; t < KT; ++t) {
-                    const Frag<NP> kf = km.straight_down(32 * ks, 16 * t, lane);
-                    q1[t] = mma<3>(zf, kf, q1[t]);
-                    A2[t] = mma<PK>(mf, kf, A2[t]);
+            for (int t0 = 0; t0 < KT; t0 += AT) {
+                Frag<NP> kf[AT], qf[AT];
+#pragma unroll
+                for (int t = 0; t < AT; ++t) kf[t] = km.straight_down(32 * ks, 16 * (t0 + t), lane);
+                if (left) {
+                    mma_each<3>(kf, zf, A1 + t0);
+                    mma_each<PK>(kf, mf, A2 + t0);
                 }
-            }
-            if (2 * ks + 1 >= w) {
-                const Frag<3> zf = scaled(zm.straight_down(32 * ks, 16 * w, lane), G.rq, 32 * ks);
-                const Frag<PK> mf = scaled(mm.straight_down(32 * ks, 16 * w, lane), G.rk, 32 * ks);
+                if (right) {
 #pragma unroll
-                for (int t = 0; t < KT; ++t) {
-                    A2[t] = mma<PK>(zf, qm.straight_down(32 * ks, 16 * t, lane), A2[t]);
-                    A2[t] = mma<PK>(mf, km.straight_down(32 * ks, 16 * t, lane), A2[t]);
+                    for (int t = 0; t < AT; ++t) qf[t] = qm.straight_down(32 * ks, 16 * (t0 + t), lane);
+                    mma_each<PK>(qf, zd, A2 + t0);
+                    mma_each<PK>(kf, md, A2 + t0);
                 }
             }
         }
-        // q . dq of this head, from the planes of q
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = 16 * w + 4 * g + r;
+        anew();
+        // q^ . dq^ of this head = q . yq
+        {
             float s = 0.f;
 #pragma unroll
             for (int t = 0; t < KT; ++t) {
-                float x = 0.f;
+                float x[4];
+                row_of(qm, 16 * w + c, 16 * t + 4 * g, x);
 #pragma unroll
-                for (int p = NP - 1; p >= 0; --p) x += (float)qm.p[p * L::MatQ::PLANE + i * L::MatQ::LD + 16 * t + c];
-                s += x * q1[t][r];
-                dq[t][r] += q1[t][r];
-                dk[t][r] += A2[t][r];
+                for (int r = 0; r < 4; ++r) s = fmaf(x[r], A1[t][r], s);
+                dq[t] = SHARED ? dq[t] + A1[t] : A1[t];
+                dk[t] = SHARED ? dk[t] + A2[t] : A2[t];
             }
-            s = row_sum(s) * G.rq[i];
-            if (c == 0) qdq[i] = s;
+            s += __shfl_xor(s, 16);
+            s += __shfl_xor(s, 32);
+            if (g == 0) qdq[16 * w + c] = s;
         }
         __syncthreads();
-        if (threadIdx.x < CHUNK) {
-            const int i = threadIdx.x;
+        if (tid < CHUNK) {
+            const int i = tid;
             float s = i < rows ? qdq[i] - vdv[i] : 0.f;
 #pragma unroll
             for (int m = 1; m < 64; m <<= 1) {          // sum over the tokens behind
@@ -314,42 +334,52 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
             }
         }
     }
-    // through the norm, and out: dx = r (dx^ - x^ (x^ . dx^))
+    // through the norm, and out: dx = r (dx^ - x^ (x^ . dx^)) = y - r^2 x (x . y)
+    const int i = 16 * w + c;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        T *out = (T *)(which ? a.dk : a.dq);
-        if (!out) continue;
+        if (!(which ? a.dk : a.dq)) continue;
         const typename L::MatQ &xm = which ? km : qm;
+        T *out = (T *)(which ? a.dk : a.dq) + qat + (long long)i * a.qst + 4 * g;
+        float x[KT][4], s = 0.f;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = 16 * w + 4 * g + r;
-            const float f = which ? G.rk[i] : G.rq[i];
-            float x[KT], s = 0.f;
+        for (int t = 0; t < KT; ++t) {
+            row_of(xm, i, 16 * t + 4 * g, x[t]);
 #pragma unroll
-            for (int t = 0; t < KT; ++t) {
-                x[t] = 0.f;
+            for (int r = 0; r < 4; ++r) s = fmaf(x[t][r], which ? dk[t][r] : dq[t][r], s);
+        }
+        s += __shfl_xor(s, 16);
+        s += __shfl_xor(s, 32);
+        const float f = which ? G.rk[i] : G.rq[i];
+        s = a.norm ? -s * f * f : 0.f;
+        if (i >= all) continue;
 #pragma unroll
-                for (int p = NP - 1; p >= 0; --p) x[t] += (float)xm.p[p * L::MatQ::PLANE + i * L::MatQ::LD + 16 * t + c];
-                s += x[t] * (which ? dk[t][r] : dq[t][r]);
-            }
-            s = a.norm ? row_sum(s) * f * f : 0.f;
+        for (int t = 0; t < KT; ++t) {
+            float y[4];
 #pragma unroll
-            for (int t = 0; t < KT; ++t) {
-                const int col = 16 * t + c;
-                if (i < all && col < a.K) out[qat + (long long)i * a.qst + col] = (T)(i < rows ? f * ((which ? dk[t][r] : dq[t][r]) - x[t] * s) : 0.f);
+            for (int r = 0; r < 4; ++r) y[r] = i < rows ? fmaf(x[t][r], s, which ? dk[t][r] : dq[t][r]) : 0.f;
+            if (a.vecd && 16 * t + 4 * g + 4 <= a.K) store_n<T, 4>(out + 16 * t, y);
+            else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (16 * t + 4 * g + r < a.K) out[16 * t + r] = (T)y[r];
             }
         }
     }
 }
 
-template <typename T, int NP, int KP> static int gradients_kp(const Args &a, hipStream_t s)
+template <typename T, int NP, int KP, bool SHARED> static int gradients_of(const Args &a, hipStream_t s)
 {
     constexpr int bytes = GradLds<T, NP, KP>::BYTES;
-    if (a.chunks == 0) return CAWN_OK;
     static_assert(bytes + sizeof(Gates) + 1024 <= 163840, "LDS");
-    if (hipFuncSetAttribute((const void *)delta_gradients<T, NP, KP>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CAWN_ELAUNCH;
-    hipLaunchKernelGGL((delta_gradients<T, NP, KP>), dim3((unsigned)((long long)a.B * a.Hk * a.chunks)), dim3(256), bytes, s, a);
+    if (a.chunks == 0) return CAWN_OK;
+    if (hipFuncSetAttribute((const void *)delta_gradients<T, NP, KP, SHARED>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CAWN_ELAUNCH;
+    hipLaunchKernelGGL((delta_gradients<T, NP, KP, SHARED>), dim3((unsigned)((long long)a.B * a.Hk * a.chunks)), dim3(256), bytes, s, a);
     return launched();
+}
+template <typename T, int NP, int KP> static int gradients_kp(const Args &a, hipStream_t s)
+{
+    return a.H > a.Hk ? gradients_of<T, NP, KP, true>(a, s) : gradients_of<T, NP, KP, false>(a, s);
 }
 
 int launch_gradients(const Args &a, bool bf16_, hipStream_t s)

@@ -217,6 +217,7 @@ template <typename T, int N, int COLS, int NT> struct RowsAhead {
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[e].v[i] = src[min(c + i, cols - 1)];
+                __builtin_amdgcn_sched_barrier(0);      // (one unit's single values at a time: they take a register each)
             }
         }
     }
