@@ -1,8 +1,9 @@
 // Gated delta rule by chunks: the states at the segments' begins (forward, S' = A S + b) or, for the gradient, behind their ends
 // (S' = A^T S + b, from the last segment to the first).
 //
-// A workgroup takes 64 columns of a head's state.  Wave w owns the rows of row tiles w, w + 4 of them; it splits its own rows of A and
-// its own tiles of the new state, and the waves pass each other the state's planes in LDS: one barrier a segment.
+// A workgroup takes 16 columns of a head's state: the segments are a chain, and what counts is the time of one link.  Wave w owns row
+// tiles w and w + 4; it splits its own rows of A (fetched a link ahead) and its own tiles of the new state, and the waves pass each other
+// the state's planes in LDS: one barrier a link.
 #include "cawn_delta_mfma.hpp"
 
 namespace cawn {
@@ -11,106 +12,113 @@ namespace delta {
 template <int KP, bool REV> __global__ __launch_bounds__(256) void delta_join(const Args a)
 {
     constexpr int KS = KP / 32, KT = KP / 16, OWN = (KT + 3) / 4;
-    extern __shared__ __attribute__((aligned(16))) char lds[];      // [2][4 column tiles][KS][3] pieces
-    const int groups = (a.VT + 3) / 4, bh = blockIdx.x / groups, vg = blockIdx.x % groups;
+    __shared__ __attribute__((aligned(16))) char lds[2 * KS * 3 * 1024];
+    const int bh = blockIdx.x / a.VT, vt = blockIdx.x % a.VT;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, g = lane / 16, c = lane % 16;
     const size_t st = (size_t)KT * a.VT * 1024;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     const float *begin = REV ? a.dstate_out : a.state_in;
-    f32x4 S[OWN][4];
+    const int links = a.segments - 1;
+    f32x4 S[OWN], bn[OWN];
+    float an[OWN][KS][8];
     auto put = [&](int buf) {
 #pragma unroll
         for (int o = 0; o < OWN; ++o) {
             const int t = w + 4 * o;
             if (t >= KT) break;
+            float r[4] = {S[o][0], S[o][1], S[o][2], S[o][3]};
 #pragma unroll
-            for (int ct = 0; ct < 4; ++ct) {
-                float r[4] = {S[o][ct][0], S[o][ct][1], S[o][ct][2], S[o][ct][3]};
+            for (int p = 0; p < 3; ++p) {
+                bf16x4 h;
 #pragma unroll
-                for (int p = 0; p < 3; ++p) {
-                    bf16x4 h;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        h[e] = (bf16)r[e];
-                        r[e] -= (float)h[e];
-                    }
-                    *reinterpret_cast<bf16x4 *>(lds + ((((buf * 4 + ct) * KS + t / 2) * 3 + p) * 64 + lane) * 16 + (t % 2) * 8) = h;
+                for (int e = 0; e < 4; ++e) {
+                    h[e] = (bf16)r[e];
+                    r[e] -= (float)h[e];
                 }
+                *reinterpret_cast<bf16x4 *>(lds + (((buf * KS + t / 2) * 3 + p) * 64 + lane) * 16 + (t % 2) * 8) = h;
             }
         }
     };
-    const int links = a.segments - 1;
-    auto seg_of = [&](int i) { return REV ? a.segments - 1 - i : i; };      // the i-th link runs over this segment
-#pragma unroll
-    for (int o = 0; o < OWN; ++o)
-#pragma unroll
-        for (int ct = 0; ct < 4; ++ct) {
-            S[o][ct] = zero;
-            const int t = w + 4 * o, v = 16 * (4 * vg + ct) + c;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int f = 16 * t + 4 * g + r;
-                if (begin && f < a.K && v < a.V) S[o][ct][r] = begin[((long long)bh * a.K + f) * a.V + v];
-            }
-        }
-    put(0);
-    for (int i = 0; i < links; ++i) {
-        const int s = seg_of(i);
+    auto fetch = [&](int i) {                   // of the i-th link
+        const int s = REV ? a.segments - 1 - i : i;
         const float *A = (const float *)a.seg_a + ((size_t)bh * a.segments + s) * KP * KP;
-        const char *bt = a.seg_b + ((size_t)bh * a.segments + s) * st + lane * 16;
-        char *to = a.seg_s + ((size_t)bh * a.segments + (REV ? s - 1 : s + 1)) * st + lane * 16;
-        Frag<3> af[OWN][KS];
 #pragma unroll
         for (int o = 0; o < OWN; ++o) {
-            const int t = w + 4 * o;
-            if (t >= KT) break;
+            const int t = min(w + 4 * o, KT - 1), row = 16 * t + c;
+            bn[o] = *reinterpret_cast<const f32x4 *>(a.seg_b + ((size_t)bh * a.segments + s) * st + ((size_t)t * a.VT + vt) * 1024 + lane * 16);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                float x[8];
+            for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int step = 32 * ks + 16 * (e / 4) + 4 * g + e % 4, row = 16 * t + c;
-                    x[e] = REV ? A[step * KP + row] : A[row * KP + step];
+                for (int half = 0; half < 2; ++half) {
+                    const int step = 32 * ks + 16 * half + 4 * g;
+                    if (REV) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) an[o][ks][4 * half + e] = A[(step + e) * KP + row];
+                    } else {
+                        const f32x4 x = *reinterpret_cast<const f32x4 *>(A + row * KP + step);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) an[o][ks][4 * half + e] = x[e];
+                    }
                 }
-                split8<3>(x, af[o][ks]);
-            }
-#pragma unroll
-            for (int ct = 0; ct < 4; ++ct) {
-                const int vt = 4 * vg + ct;
-                S[o][ct] = vt < a.VT ? *reinterpret_cast<const f32x4 *>(bt + ((size_t)t * a.VT + vt) * 1024) : zero;
-            }
         }
-        __syncthreads();
+    };
+    fetch(0);
 #pragma unroll
-        for (int ct = 0; ct < 4; ++ct)
+    for (int o = 0; o < OWN; ++o) {
+        S[o] = zero;
+        const int t = w + 4 * o, v = 16 * vt + c;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                Frag<3> f;
-#pragma unroll
-                for (int p = 0; p < 3; ++p) f.p[p] = *reinterpret_cast<const bf16x8 *>(lds + (((((i & 1) * 4 + ct) * KS + ks) * 3 + p) * 64 + lane) * 16);
-#pragma unroll
-                for (int o = 0; o < OWN; ++o)
-                    if (w + 4 * o < KT) S[o][ct] = mma<3>(af[o][ks], f, S[o][ct]);
-            }
+        for (int r = 0; r < 4; ++r) {
+            const int f = 16 * t + 4 * g + r;
+            if (begin && f < a.K && v < a.V) S[o][r] = begin[((long long)bh * a.K + f) * a.V + v];
+        }
+    }
+    put(0);
+    for (int i = 0; i < links; ++i) {
+        const int s = REV ? a.segments - 1 - i : i;
+        char *to = a.seg_s + ((size_t)bh * a.segments + (REV ? s - 1 : s + 1)) * st + lane * 16;
+        Frag<3> af[OWN][KS];
+        f32x4 acc[OWN][KS];
 #pragma unroll
         for (int o = 0; o < OWN; ++o)
 #pragma unroll
-            for (int ct = 0; ct < 4; ++ct) {
-                const int t = w + 4 * o, vt = 4 * vg + ct;
-                if (t < KT && vt < a.VT) *reinterpret_cast<f32x4 *>(to + ((size_t)t * a.VT + vt) * 1024) = S[o][ct];
+            for (int ks = 0; ks < KS; ++ks) {
+                split8<3>(an[o][ks], af[o][ks]);
+                acc[o][ks] = ks == 0 ? bn[o] : zero;
             }
+        if (i + 1 < links) fetch(i + 1);
+        __syncthreads();
+        Frag<3> f[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int p = 0; p < 3; ++p) f[ks].p[p] = *reinterpret_cast<const bf16x8 *>(lds + ((((i & 1) * KS + ks) * 3 + p) * 64 + lane) * 16);
+        // a chain of instructions for every 32 rows of the state, side by side
+#pragma unroll
+        for (int q = 2; q >= 0; --q)
+#pragma unroll
+            for (int p = 0; p <= q; ++p)
+#pragma unroll
+                for (int o = 0; o < OWN; ++o)
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) acc[o][ks] = mfma(af[o][ks].p[p], f[ks].p[q - p], acc[o][ks]);
+#pragma unroll
+        for (int o = 0; o < OWN; ++o) {
+            S[o] = acc[o][0];
+#pragma unroll
+            for (int ks = 1; ks < KS; ++ks) S[o] += acc[o][ks];
+            const int t = w + 4 * o;
+            if (t < KT) *reinterpret_cast<f32x4 *>(to + ((size_t)t * a.VT + vt) * 1024) = S[o];
+        }
         if (i + 1 < links) put((i + 1) & 1);
     }
 }
 
 template <int KP> static int join_kp(const Args &a, bool reverse, hipStream_t s)
 {
-    constexpr int bytes = 2 * 4 * (KP / 32) * 3 * 1024;
-    const void *fn = reverse ? (const void *)delta_join<KP, true> : (const void *)delta_join<KP, false>;
-    if (bytes > 60000 && hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CAWN_ELAUNCH;
-    const dim3 grid((unsigned)((long long)a.B * a.H * ceil_div(a.VT, 4)));
-    if (reverse) hipLaunchKernelGGL((delta_join<KP, true>), grid, dim3(256), bytes, s, a);
-    else hipLaunchKernelGGL((delta_join<KP, false>), grid, dim3(256), bytes, s, a);
+    const dim3 grid((unsigned)((long long)a.B * a.H * a.VT));
+    if (reverse) hipLaunchKernelGGL((delta_join<KP, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((delta_join<KP, false>), grid, dim3(256), 0, s, a);
     return launched();
 }
 
