@@ -32,12 +32,29 @@ struct NormArgs {
     int cb, slots, ncb, splits, bblocks, t_run;      // T > 1: channels and groups of a workgroup, its column blocks, runs of tokens, rows at a time
 };
 
-__device__ inline float sigmoid_f(float z) { return 1.f / (1.f + __expf(-z)); }
+// (v_rcp_f32 is good to one unit in the last place; a division takes ten instructions, and these kernels have about as many to spare
+// per value as memory leaves them)
+__device__ inline float sigmoid_f(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+
+// The normal distribution function (1 + erf(z / sqrt 2)) / 2 and its density's exponential, by Abramowitz and Stegun 7.1.26: with x = |z| / sqrt 2 and
+// t = 1 / (1 + 0.3275911 x), erfc(x) = (a1 t + .. + a5 t^5) e^{-x^2} within 1.5e-7.  The exponential serves the slope too.
+__device__ inline float normal_f(float z, float &e)
+{
+    e = __expf(-0.5f * z * z);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.f));
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f);
+    const float half = 0.5f * p * t * e;        // the smaller tail
+    return z < 0.f ? half : 1.f - half;
+}
 
 __device__ inline float act_f(float z, int act)
 {
+    float e;
     if (act == 1) return z * sigmoid_f(z);
-    if (act == 2) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    if (act == 2) return z * normal_f(z, e);
     return z;
 }
 
@@ -45,9 +62,13 @@ __device__ inline float act_slope(float z, int act)
 {
     if (act == 1) {
         const float s = sigmoid_f(z);
-        return s * (1.f + z * (1.f - s));
+        return s * fmaf(z, 1.f - s, 1.f);
     }
-    if (act == 2) return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * 0.3989422804014327f * __expf(-0.5f * z * z);
+    if (act == 2) {
+        float e;
+        const float n = normal_f(z, e);
+        return fmaf(z * 0.3989422804014327f, e, n);
+    }
     return 1.f;
 }
 
@@ -85,33 +106,46 @@ template <typename T, int VEC, int NIT, bool BWD> __global__ __launch_bounds__(2
         }
     }
     const float inv = 1.f / (float)a.cg;
-    for (long long r = first; r < a.B; r += (long long)a.rblocks * a.rb) {
+    // a row's values travel while the one before is worked on
+    Pack<T, VEC> xn[NIT], dn[BWD ? NIT : 1];
+    float mn = 0.f, sn = 0.f;
+    auto fetch = [&](long long r) {
+#pragma unroll
+        for (int n = 0; n < NIT; ++n) {
+            const int c = c0 + (in[n] ? (n * a.lpg + lane) * VEC : 0);
+            xn[n] = *reinterpret_cast<const Pack<T, VEC> *>((const T *)a.x + r * a.xsb + c);
+            if (BWD) dn[n] = *reinterpret_cast<const Pack<T, VEC> *>((const T *)a.dy + r * a.ysb + c);
+        }
+        if (BWD) mn = a.stats[(r * a.G + (mine ? g : 0)) * 2], sn = a.stats[(r * a.G + (mine ? g : 0)) * 2 + 1];
+    };
+    const long long stride = (long long)a.rblocks * a.rb;
+    if (first < a.B) fetch(first);
+    for (long long r = first; r < a.B; r += stride) {
         const bool live = mine;
         float x[NIT][VEC], d[BWD ? NIT : 1][VEC];
         float s = 0.f;
+        const float m0 = mn, s0 = sn;
 #pragma unroll
         for (int n = 0; n < NIT; ++n) {
-            const int c = c0 + (n * a.lpg + lane) * VEC;
-            if (in[n]) load_n<T, VEC>((const T *)a.x + r * a.xsb + c, x[n]);
-            if (BWD && in[n]) load_n<T, VEC>((const T *)a.dy + r * a.ysb + c, d[n]);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                if (!in[n]) x[n][i] = 0.f;
-                if (BWD && !in[n]) d[n][i] = 0.f;
+                x[n][i] = in[n] ? (float)xn[n].v[i] : 0.f;
+                if (BWD) d[n][i] = in[n] ? (float)dn[n].v[i] : 0.f;
                 s += x[n][i];
             }
         }
+        fetch(r + stride < a.B ? r + stride : r);
         float mean, rstd;
         if (BWD) {
-            mean = live ? a.stats[(r * a.G + g) * 2] : 0.f;
-            rstd = live ? a.stats[(r * a.G + g) * 2 + 1] : 0.f;
+            mean = live ? m0 : 0.f;
+            rstd = live ? s0 : 0.f;
         } else {
             mean = run_sum(s, a.lpg) * inv;
             float q = 0.f;
 #pragma unroll
             for (int n = 0; n < NIT; ++n)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) q += in[n] ? (x[n][i] - mean) * (x[n][i] - mean) : 0.f;
+                for (int i = 0; i < VEC; ++i) q = in[n] ? fmaf(x[n][i] - mean, x[n][i] - mean, q) : q;
             rstd = 1.f / sqrtf(run_sum(q, a.lpg) * inv + a.eps);
             if (a.stats && live && lane == 0) a.stats[(r * a.G + g) * 2] = mean, a.stats[(r * a.G + g) * 2 + 1] = rstd;
         }
@@ -120,7 +154,7 @@ template <typename T, int VEC, int NIT, bool BWD> __global__ __launch_bounds__(2
             for (int n = 0; n < NIT; ++n) {
                 if (!in[n]) continue;
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) x[n][i] = act_f((x[n][i] - mean) * rstd * w[n][i] + bias[n][i], a.act);
+                for (int i = 0; i < VEC; ++i) x[n][i] = act_f(fmaf((x[n][i] - mean) * rstd, w[n][i], bias[n][i]), a.act);
                 store_n<T, VEC>((T *)a.y + r * a.ysb + c0 + (n * a.lpg + lane) * VEC, x[n]);
             }
         } else {
@@ -130,15 +164,14 @@ template <typename T, int VEC, int NIT, bool BWD> __global__ __launch_bounds__(2
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
                     const float xh = (x[n][i] - mean) * rstd;
-                    const float dz = d[n][i] * act_slope(xh * w[n][i] + bias[n][i], a.act);
-                    if (in[n]) {
-                        sw[n][i] += dz * xh;
-                        sb[n][i] += dz;
-                    }
+                    // (lanes without values hold zeros: dy and so dz are 0 there)
+                    const float dz = d[n][i] * act_slope(fmaf(xh, w[n][i], bias[n][i]), a.act);
+                    sw[n][i] = fmaf(dz, xh, sw[n][i]);
+                    sb[n][i] += dz;
                     x[n][i] = xh;
-                    d[n][i] = in[n] ? dz * w[n][i] : 0.f;
+                    d[n][i] = dz * w[n][i];
                     m1 += d[n][i];
-                    m2 += in[n] ? d[n][i] * xh : 0.f;
+                    m2 = fmaf(d[n][i], xh, m2);
                 }
             m1 = run_sum(m1, a.lpg) * inv;
             m2 = run_sum(m2, a.lpg) * inv;
@@ -187,8 +220,9 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
 {
     __shared__ float sh[2][256 * (WHAT == 2 ? VEC : 1)];
     __shared__ float stat[256][4];
-    const int units = a.cb / VEC, per = 256 / units, rp = threadIdx.x / units, unit = threadIdx.x % units;
-    const int blk = blockIdx.x, cblk = blk % a.ncb, split = blk / a.ncb % a.splits, bblk = blk / a.ncb / a.splits;
+    const int units = a.cb / VEC, per = (int)blockDim.x / units, rp = threadIdx.x / units, unit = threadIdx.x % units;
+    // (the second pass goes backwards: what the first read last is still in the memory-side cache)
+    const int blk = WHAT == 1 || WHAT == 3 ? gridDim.x - 1 - blockIdx.x : blockIdx.x, cblk = blk % a.ncb, split = blk / a.ncb % a.splits, bblk = blk / a.ncb / a.splits;
     const bool mine = rp < per;
     const int c = cblk * a.cb + unit * VEC;                             // the thread's channels
     const int per_group = a.cg > a.cb ? a.cg / a.cb : 1;                // workgroups side by side that share a group
@@ -209,7 +243,7 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
         if (WHAT == 1 || WHAT == 3) {
             // join the parts of this workgroup's groups: 16 lanes for each slot
             __syncthreads();
-            for (int s = threadIdx.x / 16; s < a.slots; s += 16) {
+            for (int s = threadIdx.x / 16; s < a.slots; s += (int)blockDim.x / 16) {
                 const int gs = a.cg > a.cb ? g : cblk * a.slots + s;
                 double s1 = 0.0, s2 = 0.0;
                 for (int j = threadIdx.x % 16; j < a.splits * per_group; j += 16) {
@@ -247,27 +281,43 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
         }
         float s1 = 0.f, s2 = 0.f;
         if (mine) {
+            // two tokens ahead (behind the last, the last again)
+            Pack<T, VEC> xa[2], da[2];
+            const T *db = WHAT >= 2 ? (const T *)a.dy + b * a.ysb + c : nullptr;
+            auto fetch = [&](int e, int t) {
+                t = min(t, t1 - 1);
+                xa[e] = *reinterpret_cast<const Pack<T, VEC> *>(xb + t * a.xst);
+                if (WHAT >= 2) da[e] = *reinterpret_cast<const Pack<T, VEC> *>(db + t * a.yst);
+            };
+            fetch(0, t0 + rp);
+            fetch(1, t0 + rp + per);
             for (int t = t0 + rp; t < t1; t += per) {
                 float x[VEC], d[VEC];
-                load_n<T, VEC>(xb + t * a.xst, x);
-                if (WHAT >= 2) load_n<T, VEC>((const T *)a.dy + b * a.ysb + t * a.yst + c, d);
+                const Pack<T, VEC> x0 = xa[0], d0 = da[0];
+                xa[0] = xa[1], da[0] = da[1];
+                fetch(1, t + 2 * per);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    x[i] = (float)x0.v[i];
+                    if (WHAT >= 2) d[i] = (float)d0.v[i];
+                }
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
                     if (WHAT == 0) {
                         const float v = x[i] - shift;
                         s1 += v;
-                        s2 += v * v;
+                        s2 = fmaf(v, v, s2);
                     } else {
                         const float xh = (x[i] - p0) * p1;
-                        const float z = xh * w[i] + bias[i];
+                        const float z = fmaf(xh, w[i], bias[i]);
                         if (WHAT == 1) x[i] = act_f(z, a.act);
                         else {
                             const float dz = d[i] * act_slope(z, a.act), u = dz * w[i];
                             if (WHAT == 2) {
-                                sw[i] += dz * xh;
+                                sw[i] = fmaf(dz, xh, sw[i]);
                                 sb[i] += dz;
                                 s1 += u;
-                                s2 += u * xh;
+                                s2 = fmaf(u, xh, s2);
                             } else x[i] = p1 * (u - m1 - xh * m2);
                         }
                     }
@@ -315,28 +365,24 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
     }
 }
 
-// dweight, dbias: the sums of `rows` rows of [2][C], in a fixed order: 16 columns by 16 runs of rows a workgroup
-__global__ __launch_bounds__(256) void group_norm_columns(const float *part, int rows, int C, float *dw, float *db, int accumulate)
+// dweight, dbias: the sums of `rows` rows of [2][C], in a fixed order: 16 columns by 64 runs of rows a workgroup
+__global__ __launch_bounds__(1024) void group_norm_columns(const float *part, int rows, int C, float *dw, float *db, int accumulate)
 {
-    __shared__ float sh[16][17];
+    __shared__ float sh[64][17];
     const int col = threadIdx.x % 16, run = threadIdx.x / 16;
     const long long c = (long long)blockIdx.x * 16 + col;
-    float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
     if (c < 2LL * C) {
-        int r = run;
-        for (; r + 48 < rows; r += 64) {
-            s0 += part[(long long)r * 2 * C + c];
-            s1 += part[(long long)(r + 16) * 2 * C + c];
-            s2 += part[(long long)(r + 32) * 2 * C + c];
-            s3 += part[(long long)(r + 48) * 2 * C + c];
+        for (int r = run; r < rows; r += 256) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += r + 64 * e < rows ? part[(long long)(r + 64 * e) * 2 * C + c] : 0.f;
         }
-        for (; r < rows; r += 16) s0 += part[(long long)r * 2 * C + c];
     }
-    sh[run][col] = (s0 + s1) + (s2 + s3);
+    sh[run][col] = (s[0] + s[1]) + (s[2] + s[3]);
     __syncthreads();
     if (run == 0 && c < 2LL * C) {
         float v = 0.f;
-        for (int q = 0; q < 16; ++q) v += sh[q][col];
+        for (int q = 0; q < 64; ++q) v += sh[q][col];
         float *out = c < C ? dw : db;
         const long long at = c < C ? c : c - C;
         if (out) out[at] = accumulate ? out[at] + v : v;
@@ -349,6 +395,7 @@ struct Plan {
     bool rows;              // the T = 1 form
     int vec, nit;
     long long blocks, colrows;
+    int threads;            // whole waves of those that have work
     size_t part_bytes, bytes;
 };
 
@@ -377,6 +424,7 @@ bool plan_of(const cawn_norm_desc *d, bool wide, Plan *p)
         a.gb = a.G < subs ? a.G : subs;
         a.rb = subs / a.gb;
         a.gblocks = (int)ceil_div(a.G, a.gb);
+        p->threads = (a.lpg * a.gb * a.rb + 63) / 64 * 64;
         long long rblocks = ceil_div(a.B, a.rb);
         long long want = 2048 / a.gblocks > 1 ? 2048 / a.gblocks : 1;
         if (want > cap) want = cap;
@@ -398,6 +446,7 @@ bool plan_of(const cawn_norm_desc *d, bool wide, Plan *p)
         }
         a.ncb = a.C / a.cb;
         const int per = 256 / (a.cb / p->vec);
+        p->threads = (a.cb / p->vec * per + 63) / 64 * 64;
         long long bb = 2048 / a.ncb > 1 ? 2048 / a.ncb : 1;
         if (bb > cap) bb = cap;
         a.bblocks = (int)(a.B < bb ? a.B : bb);
@@ -420,15 +469,15 @@ template <typename T, int VEC, bool BWD> void launch_rows(const Plan &p, hipStre
 {
     const dim3 grid((unsigned)p.blocks);
     switch (p.nit) {
-    case 1: hipLaunchKernelGGL((group_norm_rows<T, VEC, 1, BWD>), grid, dim3(256), 0, s, p.a); break;
-    case 2: hipLaunchKernelGGL((group_norm_rows<T, VEC, 2, BWD>), grid, dim3(256), 0, s, p.a); break;
-    default: hipLaunchKernelGGL((group_norm_rows<T, VEC, 4, BWD>), grid, dim3(256), 0, s, p.a); break;
+    case 1: hipLaunchKernelGGL((group_norm_rows<T, VEC, 1, BWD>), grid, dim3(p.threads), 0, s, p.a); break;
+    case 2: hipLaunchKernelGGL((group_norm_rows<T, VEC, 2, BWD>), grid, dim3(p.threads), 0, s, p.a); break;
+    default: hipLaunchKernelGGL((group_norm_rows<T, VEC, 4, BWD>), grid, dim3(p.threads), 0, s, p.a); break;
     }
 }
 
 template <typename T, int VEC> int launch(const Plan &p, bool bwd, float *dw, float *db, int accumulate, hipStream_t s)
 {
-    const dim3 grid((unsigned)p.blocks), nt(256);
+    const dim3 grid((unsigned)p.blocks), nt(p.threads);
     if (p.rows) {
         if (bwd) launch_rows<T, VEC, true>(p, s);
         else launch_rows<T, VEC, false>(p, s);
@@ -439,7 +488,7 @@ template <typename T, int VEC> int launch(const Plan &p, bool bwd, float *dw, fl
         hipLaunchKernelGGL((group_norm_runs<T, VEC, 2>), grid, nt, 0, s, p.a);
         if (p.a.dx) hipLaunchKernelGGL((group_norm_runs<T, VEC, 3>), grid, nt, 0, s, p.a);
     }
-    if (p.a.colpart) hipLaunchKernelGGL(group_norm_columns, dim3((unsigned)ceil_div(2LL * p.a.C, 16)), nt, 0, s, p.a.colpart, (int)p.colrows, p.a.C, dw, db, accumulate);
+    if (p.a.colpart) hipLaunchKernelGGL(group_norm_columns, dim3((unsigned)ceil_div(2LL * p.a.C, 16)), dim3(1024), 0, s, p.a.colpart, (int)p.colrows, p.a.C, dw, db, accumulate);
     return launched();
 }
 
@@ -452,7 +501,7 @@ int run(const cawn_norm_desc *d, bool bwd, const void *x, const float *w, const 
     const bool grads = bwd && (dw || db);
     if (d->B == 0 || d->T == 0) {
         if (grads && !d->accumulate_param_grads)        // the sums over nothing
-            hipLaunchKernelGGL(group_norm_columns, dim3((unsigned)ceil_div(2LL * p.a.C, 16)), dim3(256), 0, s, nullptr, 0, p.a.C, dw, db, 0);
+            hipLaunchKernelGGL(group_norm_columns, dim3((unsigned)ceil_div(2LL * p.a.C, 16)), dim3(1024), 0, s, nullptr, 0, p.a.C, dw, db, 0);
         return launched();
     }
     if (!x || (bwd ? !dy || !stats : !y)) return CAWN_EINVAL;
