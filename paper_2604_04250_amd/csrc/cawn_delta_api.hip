@@ -129,13 +129,13 @@ int cawn_delta_rule_fwd(const cawn_delta_desc *d, const void *q, const void *k, 
     a.q = q, a.k = k, a.v = v, a.decay = decay, a.beta = beta, a.lengths = lengths, a.state_in = (const float *)state_in, a.o = o, a.state_out = (float *)state_out;
     a.vec4 = a.V % 4 == 0 && aligned_to(state_in, 16) && aligned_to(state_out, 16);
     hipStream_t s = (hipStream_t)stream;
+    const int e = d->bf16 ? 2 : 4, w = 16 / e;
+    a.vecq = a.K % 8 == 0 && a.qst % w == 0 && a.qsb % w == 0 && aligned_to(q, 16) && aligned_to(k, 16);
     // token by token up to TOKEN_MAX
     if (a.L <= delta::TOKEN_MAX && !ckpt) return delta::launch_token(a, d->bf16, s);
-    const int e = d->bf16 ? 2 : 4, w = 16 / e;
     const Layout l = layout_of(a);
     if (!workspace || workspace_bytes < l.fwd || !aligned_to(workspace, 256)) return CAWN_EWORKSPACE;
     if (too_many(a)) return CAWN_EUNSUPPORTED;
-    a.vecq = a.K % w == 0 && a.qst % w == 0 && a.qsb % w == 0 && aligned_to(q, 16) && aligned_to(k, 16);
     a.veco = a.V % 4 == 0 && a.ost % 4 == 0 && a.osb % 4 == 0 && aligned_to(o, 4 * e);
     char *ws = (char *)workspace;
     a.gates = (float *)(ws + l.fwd_gates), a.seg_a = ws + l.fwd_a, a.t_ops = ws + l.t, a.seg_b = ws + l.b, a.seg_s = ws + l.s;
