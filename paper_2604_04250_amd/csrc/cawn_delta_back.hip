@@ -47,19 +47,21 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__(256
                 if (16 * t + 4 * g + r < a.K) S[t][r] = a.dstate_out[((long long)bh * a.K + 16 * t + 4 * g + r) * a.V + v];
         }
     }
+    long long qst = a.qst, ost = a.ost;
+    uint32_t l16 = 16 * lane;
     auto anew = [&]() {                         // (as in delta_scan)
         tid = threadIdx.x;
         asm volatile("" : "+v"(tid));
-        lane = tid % 64, g = lane / 16, c = lane % 16, v = 16 * ct + c;
+        lane = tid % 64, g = lane / 16, c = lane % 16, v = 16 * ct + c, l16 = 16 * lane;
     };
     RowsAhead<T, NP, KP, NT> ka, qa;
     constexpr int GN = (GATE_FLOATS + NT - 1) / NT;
     float ga[GN];
     auto ahead = [&](int n) {
         const int rows = min(CHUNK, len - n * CHUNK);
-        const long long qat = b * a.qsb + (long long)n * CHUNK * a.qst + (long long)(h / (a.H / a.Hk)) * a.K;
-        ka.load(tid, (const T *)a.k + qat, a.qst, rows, a.K, a.vecq);
-        qa.load(tid, (const T *)a.q + qat, a.qst, rows, a.K, a.vecq);
+        const long long qat = b * a.qsb + (long long)n * CHUNK * qst + (long long)(h / (a.H / a.Hk)) * a.K;
+        ka.load(tid, (const T *)a.k + qat, qst, rows, a.K, a.vecq);
+        qa.load(tid, (const T *)a.q + qat, qst, rows, a.K, a.vecq);
         const float *gp = a.gates + ((long long)bh * a.chunks + n) * GATE_FLOATS;
 #pragma unroll
         for (int e = 0; e < GN; ++e) ga[e] = gp[min(tid + e * NT, GATE_FLOATS - 1)];
@@ -68,6 +70,7 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__(256
     for (int n = n1 - 1; n >= n0; --n) {
         const int rows = min(CHUNK, len - n * CHUNK);
         anew();
+        asm volatile("" : "+s"(qst), "+s"(ost));
         if (n < n1 - 1) __syncthreads();
         ka.put_plain(tid, k, rows, a.K);
         qa.put_plain(tid, q, rows, a.K);
@@ -75,29 +78,29 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__(256
         for (int e = 0; e < GN; ++e)
             if (tid + e * NT < GATE_FLOATS) ((float *)&G)[tid + e * NT] = ga[e];
         {
-            const char *src = a.tt_ops + ((size_t)bh * a.chunks + n) * T_BYTES + lane * 16;
+            const char *src = a.tt_ops + ((size_t)bh * a.chunks + n) * T_BYTES;
 #pragma unroll
             for (int u = 0; u < (T_BYTES / 1024 + NW - 1) / NW; ++u) {
                 const int i = u * NW + w;
-                if (i < T_BYTES / 1024) load_piece(src + (size_t)i * 1024, lds + L::TO + i * 1024);
+                if (i < T_BYTES / 1024) load_piece(src + (size_t)i * 1024 + l16, lds + L::TO + i * 1024);
             }
         }
         __syncthreads();
         T da[4][4];
         if (mine) {
-            const T *dp = (const T *)a.dO + b * a.osb + (long long)n * CHUNK * a.ost + (long long)h * a.V;
-            if (rows == CHUNK && 16 * ct + 16 <= a.V) {
+            const T *dp = (const T *)a.dO + b * a.osb + (long long)n * CHUNK * ost + (long long)h * a.V;
+            if (rows == CHUNK && 16 * ct + 16 <= a.V && ost < (1 << 22)) {
                 dp += 16 * ct;
-                const long long dlane = 4 * g * a.ost + c;
+                const uint32_t dlane = (4 * (uint32_t)g * (uint32_t)ost + c) * sizeof(T);
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) da[t][r] = (dp + (16 * t + r) * a.ost)[dlane];
+                    for (int r = 0; r < 4; ++r) da[t][r] = *reinterpret_cast<const T *>((const char *)(dp + (16 * t + r) * ost) + dlane);
             } else {
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) da[t][r] = dp[min(16 * t + 4 * g + r, rows - 1) * a.ost + min(v, a.V - 1)];
+                    for (int r = 0; r < 4; ++r) da[t][r] = dp[min(16 * t + 4 * g + r, rows - 1) * ost + min(v, a.V - 1)];
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -139,9 +142,9 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__(256
             }
         }
         if (MODE == 0 && mine) {
-            char *st = a.ds_tiles + ((size_t)bh * a.chunks + n) * KT * a.VT * 1024 + (size_t)ct * 1024 + lane * 16;
+            char *st = a.ds_tiles + ((size_t)bh * a.chunks + n) * KT * a.VT * 1024 + (size_t)ct * 1024;
 #pragma unroll
-            for (int t = 0; t < KT; ++t) *reinterpret_cast<f32x4 *>(st + (size_t)t * a.VT * 1024) = S[t];
+            for (int t = 0; t < KT; ++t) *reinterpret_cast<f32x4 *>(st + (size_t)t * a.VT * 1024 + l16) = S[t];
         }
         anew();
         f32x4 Z[4] = {zero, zero, zero, zero}, R[4] = {zero, zero, zero, zero};
@@ -196,9 +199,9 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__(256
             times(tf, zf[0], zf[1], R);
         }
         if (MODE == 0 && mine) {
-            char *rt = a.dr_tiles + ((size_t)bh * a.chunks + n) * 4 * a.VT * 1024 + (size_t)ct * 1024 + lane * 16;
+            char *rt = a.dr_tiles + ((size_t)bh * a.chunks + n) * 4 * a.VT * 1024 + (size_t)ct * 1024;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4 *>(rt + (size_t)t * a.VT * 1024) = R[t];
+            for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4 *>(rt + (size_t)t * a.VT * 1024 + l16) = R[t];
         }
         anew();
         {

@@ -206,7 +206,19 @@ template <typename T, int N, int COLS, int NT> struct RowsAhead {
     // rows, cols >= 1; vec: cols a multiple of 16 bytes' elements, and every row aligned to 16 bytes
     __device__ void load(int tid, const T *base, long long stride, int rows, int cols, bool vec)
     {
-        constexpr int W = 16 / sizeof(T);
+        constexpr int W = 16 / sizeof(T), STEP = NT / U;        // rows from one unit of a lane to its next
+        const long long row = stride * (long long)sizeof(T);
+        if (vec && rows == CHUNK && cols == COLS && row < (1 << 24)) {
+            // all there: one offset a lane, the rest the same for all
+            const uint32_t at = (uint32_t)(tid / U) * (uint32_t)row + (uint32_t)(tid % U) * (8 * sizeof(T));
+#pragma unroll
+            for (int e = 0; e < UNITS; ++e) {
+                const char *src = (const char *)base + e * STEP * row;
+#pragma unroll
+                for (int p = 0; p < 8 / W; ++p) *reinterpret_cast<f32x4 *>(&x[e].v[p * W]) = *reinterpret_cast<const f32x4 *>(src + at + p * 16);
+            }
+            return;
+        }
 #pragma unroll
         for (int e = 0; e < UNITS; ++e) {
             const int u = tid + e * NT, r = min(u / U, rows - 1), c = u % U * 8;
@@ -217,8 +229,8 @@ template <typename T, int N, int COLS, int NT> struct RowsAhead {
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[e].v[i] = src[min(c + i, cols - 1)];
-                __builtin_amdgcn_sched_barrier(0);      // (one unit's single values at a time: they take a register each)
             }
+            __builtin_amdgcn_sched_barrier(0);          // (one unit at a time: single values take a register each)
         }
     }
     __device__ void put_plain(int tid, const Tile<N, CHUNK, COLS> &t, int rows, int cols)

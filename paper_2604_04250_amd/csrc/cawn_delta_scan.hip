@@ -145,19 +145,22 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
 
     // Lane numbers anew, in every chunk and between its steps: left to itself the compiler forms all that follows from them (row
     // numbers, comparisons, addresses: hundreds of values) ahead of the loop, and keeps them.
+    // The strides likewise: their multiples would fill the scalar registers.
+    long long qst = a.qst, vst = a.vst, ost = a.ost;
+    uint32_t l16 = 16 * lane;
     auto anew = [&]() {
         tid = threadIdx.x;
         asm volatile("" : "+v"(tid));
-        lane = tid % 64, g = lane / 16, c = lane % 16, v = 16 * ct + c;
+        lane = tid % 64, g = lane / 16, c = lane % 16, v = 16 * ct + c, l16 = 16 * lane;
     };
     RowsAhead<T, NP, KP, NT> ka, qa;
     constexpr int GN = (GATE_FLOATS + NT - 1) / NT;
     float ga[GN];
     auto ahead = [&](int n) {
         const int rows = min(CHUNK, len - n * CHUNK);
-        const long long qat = b * a.qsb + (long long)n * CHUNK * a.qst + (long long)(h / (a.H / a.Hk)) * a.K;
-        ka.load(tid, (const T *)a.k + qat, a.qst, rows, a.K, a.vecq);
-        if (MODE == 0) qa.load(tid, (const T *)a.q + qat, a.qst, rows, a.K, a.vecq);
+        const long long qat = b * a.qsb + (long long)n * CHUNK * qst + (long long)(h / (a.H / a.Hk)) * a.K;
+        ka.load(tid, (const T *)a.k + qat, qst, rows, a.K, a.vecq);
+        if (MODE == 0) qa.load(tid, (const T *)a.q + qat, qst, rows, a.K, a.vecq);
         const float *gp = a.gates + ((long long)bh * a.chunks + n) * GATE_FLOATS;
 #pragma unroll
         for (int e = 0; e < GN; ++e) ga[e] = gp[min(tid + e * NT, GATE_FLOATS - 1)];
@@ -166,6 +169,7 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
     for (int n = n0; n < n1; ++n) {
         const int rows = min(CHUNK, len - n * CHUNK);
         anew();
+        asm volatile("" : "+s"(qst), "+s"(vst), "+s"(ost));
         if (n > n0) __syncthreads();
         ka.put_plain(tid, k, rows, a.K);
         if (MODE == 0) qa.put_plain(tid, q, rows, a.K);
@@ -174,33 +178,32 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
             if (tid + e * NT < GATE_FLOATS) ((float *)&G)[tid + e * NT] = ga[e];
         {
             // T's operands come straight into LDS
-            const char *src = a.t_ops + ((size_t)bh * a.chunks + n) * T_BYTES + lane * 16;
+            const char *src = a.t_ops + ((size_t)bh * a.chunks + n) * T_BYTES;
             char *dst = lds + L::TO;
 #pragma unroll
             for (int u = 0; u < (T_BYTES / 1024 + NW - 1) / NW; ++u) {
                 const int i = u * NW + w;
-                if (i < T_BYTES / 1024) load_piece(src + (size_t)i * 1024, dst + i * 1024);
+                if (i < T_BYTES / 1024) load_piece(src + (size_t)i * 1024 + l16, dst + i * 1024);
             }
         }
         __syncthreads();
         // v is wanted last.  (What is not there is loaded from where something is, and dropped where it is used: a load behind a lane's
         // branch, or one whose value is converted at once, would be waited for here)
         T va[4][4];
-        // a lane's place among rows of v (4g .. and column c), in elements
-        const long long vlane = 4 * g * a.vst + c;
         if (of_v) {
-            const T *vp = (const T *)a.v + b * a.vsb + (long long)n * CHUNK * a.vst + (long long)h * a.V;
-            if (rows == CHUNK && 16 * ct + 16 <= a.V) {
+            const T *vp = (const T *)a.v + b * a.vsb + (long long)n * CHUNK * vst + (long long)h * a.V;
+            if (rows == CHUNK && 16 * ct + 16 <= a.V && vst < (1 << 22)) {
                 vp += 16 * ct;
+                const uint32_t vlane = (4 * (uint32_t)g * (uint32_t)vst + c) * sizeof(T);         // a lane's place among the rows
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) va[t][r] = (vp + (16 * t + r) * a.vst)[vlane];
+                    for (int r = 0; r < 4; ++r) va[t][r] = *reinterpret_cast<const T *>((const char *)(vp + (16 * t + r) * vst) + vlane);
             } else {
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) va[t][r] = vp[min(16 * t + 4 * g + r, rows - 1) * a.vst + min(v, a.V - 1)];
+                    for (int r = 0; r < 4; ++r) va[t][r] = vp[min(16 * t + 4 * g + r, rows - 1) * vst + min(v, a.V - 1)];
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -243,9 +246,9 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
         }
         // what hangs on the state before the chunk
         if (MODE == 0 && a.s_tiles && mine) {
-            char *st = a.s_tiles + bh * a.s_row + n * a.s_chunk + (size_t)ct * 1024 + lane * 16;
+            char *st = a.s_tiles + bh * a.s_row + n * a.s_chunk + (size_t)ct * 1024;
 #pragma unroll
-            for (int t = 0; t < KT; ++t) *reinterpret_cast<f32x4 *>(st + (size_t)t * a.VT * 1024) = S[t];
+            for (int t = 0; t < KT; ++t) *reinterpret_cast<f32x4 *>(st + (size_t)t * a.VT * 1024 + l16) = S[t];
         }
         anew();
         f32x4 U[4];
@@ -308,16 +311,18 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
         anew();
         if (MODE == 0) {
             if (a.u_tiles && mine) {
-                char *ut = a.u_tiles + bh * a.u_row + n * a.u_chunk + (size_t)ct * 1024 + lane * 16;
+                char *ut = a.u_tiles + bh * a.u_row + n * a.u_chunk + (size_t)ct * 1024;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4 *>(ut + (size_t)t * a.VT * 1024) = U[t];
+                for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4 *>(ut + (size_t)t * a.VT * 1024 + l16) = U[t];
             }
             Frag<PO> uf[2];
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) split_tiles<PO>(U[2 * ks], U[2 * ks + 1], uf[ks]);
             const int all = min(CHUNK, a.L - n * CHUNK);
-            const long long olane = c * a.ost + 4 * g;      // a lane's place among rows of o
-            T *op = (T *)a.o + b * a.osb + (long long)n * CHUNK * a.ost + (long long)h * a.V + 16 * ct;
+            // a lane's place among rows of o, in bytes
+            const bool whole = rows == CHUNK && a.veco && 16 * ct + 16 <= a.V && ost < (1 << 22);
+            const uint32_t olane = ((uint32_t)c * (uint32_t)ost + 4 * g) * sizeof(T);
+            T *op = (T *)a.o + b * a.osb + (long long)n * CHUNK * ost + (long long)h * a.V + 16 * ct;
             {
                 Frag<PO> f[4], f2[2];
 #pragma unroll
@@ -340,12 +345,12 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
                 for (int r = 0; r < 4; ++r) y[r] = O[t][r] * m;
                 if (rows < CHUNK && i >= rows) y[0] = y[1] = y[2] = y[3] = 0.f;         // (whatever the state holds)
                 if (!mine) continue;
-                T *dst = op + (long long)(16 * t) * a.ost;
-                if (rows == CHUNK && a.veco && 16 * ct + 16 <= a.V) store_n<T, 4>(dst + olane, y);
+                T *dst = op + (long long)(16 * t) * ost;
+                if (whole) store_n<T, 4>(reinterpret_cast<T *>((char *)dst + olane), y);
                 else if (i < all) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (16 * ct + 4 * g + r < a.V) dst[olane + r] = (T)y[r];
+                        if (16 * ct + 4 * g + r < a.V) dst[c * ost + 4 * g + r] = (T)y[r];
                 }
             }
         }
