@@ -9,7 +9,7 @@ using namespace cawn::ops;
 
 constexpr int CHUNK = 64;           // tokens treated at once by the chunked kernels
 constexpr int TOKEN_MAX = 16;       // longest call that goes token by token
-constexpr int OPERAND_BYTES = 18 * 1024;     // a triangular 64 x 64 matrix as operands, three planes
+constexpr int OPERAND_BYTES = 18 * 1024;     // T as operands, three planes
 constexpr int GATE_FLOATS = 9 * CHUNK;
 constexpr float DECAY_MIN = -104.f; // exp underflows to 0 below: a decay of minus infinity counts as this, so that sums of decays stay finite
 
@@ -43,7 +43,7 @@ struct Args {
     // the offset b and the state at its begin, in tiles
     int segments, seg_chunks;
     float *gates;
-    char *t_ops, *tt_ops;           // per head and chunk T's operands, and its transpose's (null: not wanted)
+    char *t_ops;                    // per head and chunk T
     char *seg_a, *seg_b, *seg_s;
 };
 

@@ -7,6 +7,9 @@ using cawn::delta::Args;
 
 using cawn::delta::Sizes;
 
+#ifndef WANT
+#define WANT 768
+#endif
 namespace {
 
 // How a row's chunks are cut into segments.  A segment costs each of its chunks twice (what it makes of a state, then its outputs) and
@@ -14,7 +17,7 @@ namespace {
 void cut(Args *a)
 {
     const long long groups = (long long)a->B * a->H * ceil_div(a->VT, 4);
-    const long long want = groups > 0 ? 768 / groups : 1;
+    const long long want = groups > 0 ? WANT / groups : 1;
     a->segments = 1, a->seg_chunks = a->chunks;
     if (want < 3 || a->chunks < 6) return;
     long long m = ceil_div(a->chunks, want);
@@ -45,10 +48,10 @@ int check(const cawn_delta_desc *d, Args *a)
     return CAWN_OK;
 }
 
-// Byte offsets.  Kept for the backward: states [B H][chunks + 1] and u [B H][chunks] in tiles, gates, the operands of T^T, A of the segments.
-// Scratch of the forward: gates and A (unless kept), T's operands, b and the begins of the segments; of the backward: dR and dS of every
+// Byte offsets.  Kept for the backward: states [B H][chunks + 1] and u [B H][chunks] in tiles, gates, T, A of the segments.
+// Scratch of the forward: gates, A and T (unless kept), b and the begins of the segments; of the backward: dR and dS of every
 // chunk, b and the ends of the segments.
-struct Layout { size_t u, gates, tt, a, ckpt; size_t fwd_gates, fwd_a, t, b, s, fwd; size_t ds, rb, rs, bwd; };
+struct Layout { size_t u, gates, t, a, ckpt; size_t fwd_gates, fwd_a, fwd_t, b, s, fwd; size_t ds, rb, rs, bwd; };
 Layout layout_of(const Args &a)
 {
     Layout l;
@@ -57,13 +60,13 @@ Layout layout_of(const Args &a)
     const size_t gates = (all * delta::GATE_FLOATS * 4 + 1023) / 1024 * 1024, am = segs * z.KP * z.KP * 4, states = segs * z.st * 1024;
     l.u = heads * (a.chunks + 1) * z.st * 1024;
     l.gates = l.u + all * z.ut * 1024;
-    l.tt = l.gates + gates;
-    l.a = l.tt + all * delta::OPERAND_BYTES;
+    l.t = l.gates + gates;
+    l.a = l.t + all * delta::OPERAND_BYTES;
     l.ckpt = l.a + am;
     l.fwd_gates = 0;
     l.fwd_a = gates;
-    l.t = l.fwd_a + am;
-    l.b = l.t + all * delta::OPERAND_BYTES;
+    l.fwd_t = l.fwd_a + am;
+    l.b = l.fwd_t + all * delta::OPERAND_BYTES;
     l.s = l.b + states;
     l.fwd = l.s + states;
     l.ds = all * z.ut * 1024;
@@ -80,7 +83,7 @@ void keep(Args *a, const Layout &l, void *ckpt)
     char *p = (char *)ckpt;
     a->s_tiles = p, a->s_chunk = (size_t)z.st * 1024, a->s_row = (size_t)(a->chunks + 1) * a->s_chunk;
     a->u_tiles = p + l.u, a->u_chunk = (size_t)z.ut * 1024, a->u_row = (size_t)a->chunks * a->u_chunk;
-    a->gates = (float *)(p + l.gates), a->tt_ops = p + l.tt, a->seg_a = p + l.a;
+    a->gates = (float *)(p + l.gates), a->t_ops = p + l.t, a->seg_a = p + l.a;
 }
 
 // more workgroups than a grid has
@@ -138,7 +141,7 @@ int cawn_delta_rule_fwd(const cawn_delta_desc *d, const void *q, const void *k, 
     if (too_many(a)) return CAWN_EUNSUPPORTED;
     a.veco = a.V % 4 == 0 && a.ost % 4 == 0 && a.osb % 4 == 0 && aligned_to(o, 4 * e);
     char *ws = (char *)workspace;
-    a.gates = (float *)(ws + l.fwd_gates), a.seg_a = ws + l.fwd_a, a.t_ops = ws + l.t, a.seg_b = ws + l.b, a.seg_s = ws + l.s;
+    a.gates = (float *)(ws + l.fwd_gates), a.seg_a = ws + l.fwd_a, a.t_ops = ws + l.fwd_t, a.seg_b = ws + l.b, a.seg_s = ws + l.s;
     if (ckpt) keep(&a, l, ckpt);
     if (int r = delta::launch_system(a, d->bf16, s)) return r;
     return delta::launch_scan(a, d->bf16, s);

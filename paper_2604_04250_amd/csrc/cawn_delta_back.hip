@@ -12,7 +12,7 @@ namespace cawn {
 namespace delta {
 
 template <int NP, int KP> struct BackLds {
-    static constexpr int KB = Tile<NP, CHUNK, KP>::BYTES, TO = 2 * KB, P = TO + T_BYTES, BYTES = P + T_BYTES;
+    static constexpr int KB = Tile<NP, CHUNK, KP>::BYTES, TO = 2 * KB, P = TO + T_BYTES, BYTES = P + 6 * 3 * 1024;       // k, q; T; P^T's operands
     static constexpr int HELD = 163840 / (BYTES + (int)sizeof(Gates)), WAVES = HELD > 3 ? 3 : HELD;
 };
 
@@ -23,7 +23,8 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__(256
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ Gates G;
     const Tile<NP, CHUNK, KP> k{(bf16 *)lds}, q{(bf16 *)(lds + L::KB)};
-    bf16x8 *tf = reinterpret_cast<bf16x8 *>(lds + L::TO), *pf = reinterpret_cast<bf16x8 *>(lds + L::P);
+    const char *tl = lds + L::TO;
+    bf16x8 *pf = reinterpret_cast<bf16x8 *>(lds + L::P);
     const int rows_all = a.B * a.H, blk = blockIdx.x, bh = blk % rows_all, nseg = MODE == 0 ? a.segments : a.segments - 1;
     const int seg = blk / rows_all % nseg + (MODE == 0 ? 0 : 1), group = blk / rows_all / nseg, b = bh / a.H, h = bh % a.H;
     const int len = row_length(a, b), nb = (len + CHUNK - 1) / CHUNK;
@@ -78,7 +79,7 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__(256
         for (int e = 0; e < GN; ++e)
             if (tid + e * NT < GATE_FLOATS) ((float *)&G)[tid + e * NT] = ga[e];
         {
-            const char *src = a.tt_ops + ((size_t)bh * a.chunks + n) * T_BYTES;
+            const char *src = a.t_ops + ((size_t)bh * a.chunks + n) * T_BYTES;
 #pragma unroll
             for (int u = 0; u < (T_BYTES / 1024 + NW - 1) / NW; ++u) {
                 const int i = u * NW + w;
@@ -160,22 +161,9 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__(256
 #pragma unroll
         for (int t = 0; t < 4; ++t) Z[t] *= *reinterpret_cast<const f32x4 *>(G.c + 16 * t + 4 * g);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();                        // the operands of T^T and P^T
+        __syncthreads();                        // T, and the operands of P^T
         anew();
-        // upper triangular: row tiles 0 and 1 take both halves of the tokens, 2 and 3 the second
-        auto times = [&](const bf16x8 *ops, const auto &lo, const auto &hi, f32x4 *acc) {
-            Frag<3> f[4], f2[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 3; ++e) f2[t].p[e] = ops[(upper(t, 0) * 3 + e) * 64 + lane];
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int e = 0; e < 3; ++e) f[t].p[e] = ops[(upper(t, 1) * 3 + e) * 64 + lane];
-            mma_each<3>(f2, lo, acc);
-            mma_each<3>(f, hi, acc);
-        };
+        // both are upper triangular: row tiles 0 and 1 take both halves of the tokens, 2 and 3 the second
         {
             Frag<NP> df[2];
 #pragma unroll
@@ -190,13 +178,29 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__(256
                     split8<NP>(y, df[ks]);
                 }
             }
-            times(pf, df[0], df[1], Z);
+            Frag<3> f[4], f2[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 3; ++e) f2[t].p[e] = pf[(upper(t, 0) * 3 + e) * 64 + lane];
+            mma_each<3>(f2, df[0], Z);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 3; ++e) f[t].p[e] = pf[(upper(t, 1) * 3 + e) * 64 + lane];
+            mma_each<3>(f, df[1], Z);
         }
         {
             Frag<3> zf[2];
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) split_tiles<3>(Z[2 * ks], Z[2 * ks + 1], zf[ks]);
-            times(tf, zf[0], zf[1], R);
+            Frag<3> f[4], f2[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) f2[t] = t_columns(tl, t, 0, lane);
+            mma_each<3>(f2, zf[0], R);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) f[t] = t_columns(tl, t, 1, lane);
+            mma_each<3>(f, zf[1], R);
         }
         if (MODE == 0 && mine) {
             char *rt = a.dr_tiles + ((size_t)bh * a.chunks + n) * 4 * a.VT * 1024 + (size_t)ct * 1024;

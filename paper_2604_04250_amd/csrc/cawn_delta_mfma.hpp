@@ -90,12 +90,42 @@ template <int N> __device__ inline void split_tiles(f32x4 lo, f32x4 hi, Frag<N> 
     split8<N>(x, f);
 }
 
-// T and P are lower triangular: of their operands (row tile, 32 columns) row tiles 0 and 1 have one that is not zero, 2 and 3 two; of
-// the transpose's tiles 0 and 1 two, 2 and 3 one
+// P and T are lower triangular: of their operands (row tile, 32 columns) row tiles 0 and 1 have one that is not zero, 2 and 3 two; of the
+// transpose's tiles 0 and 1 two, 2 and 3 one
 __device__ inline constexpr int lower(int t, int ks) { return t < 2 ? t : 2 + (t - 2) * 2 + ks; }
 __device__ inline constexpr int upper(int t, int ks) { return t < 2 ? t * 2 + ks : 2 + t; }
+
+// T, kept as operands in tile order, three planes each: rows 16 t .., steps 32 ks .. at lower(t, ks).  A lane's 16 bytes lie at slot 16 g + (c ^ 8 (g & 1)),
+// so that the columns, read transposed, come from as many banks as 8 bytes out of 16 can.
 constexpr int T_BYTES = 6 * 3 * 1024;
 static_assert(T_BYTES == OPERAND_BYTES, "");
+__device__ inline int t_slot(int g, int c) { return (16 * g + (c ^ (g & 1) * 8)) * 16; }
+__device__ inline bf16x4 read_down(const bf16 *q)      // 16 lanes fetch 4 rows of 16 and receive them transposed
+{
+    return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)q));
+}
+__device__ inline Frag<3> t_rows(const char *T, int t, int ks, int lane)
+{
+    Frag<3> f;
+#pragma unroll
+    for (int p = 0; p < 3; ++p) f.p[p] = *reinterpret_cast<const bf16x8 *>(T + (lower(t, ks) * 3 + p) * 1024 + t_slot(lane / 16, lane % 16));
+    return f;
+}
+// columns 16 t .. of T (rows of its transpose), steps 32 ks ..
+__device__ inline Frag<3> t_columns(const char *T, int t, int ks, int lane)
+{
+    const bf16x4 none = {};
+    const int i = lane % 16;
+    Frag<3> f;
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+        const char *at = T + p * 1024 + t_slot(i % 4, 4 * (lane / 16) + i / 4) + t % 2 * 8;
+        const bf16x4 a = 2 * ks >= t ? read_down(reinterpret_cast<const bf16 *>(at + lower(2 * ks, t / 2) * 3072)) : none;
+        const bf16x4 b = read_down(reinterpret_cast<const bf16 *>(at + lower(2 * ks + 1, t / 2) * 3072));
+        f.p[p] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    return f;
+}
 
 // 1 KiB from memory straight into LDS, 16 bytes a lane; src the lane's, dst the wave's (the same in all lanes).  Waited for with vmcnt
 __device__ inline void load_piece(const char *src, char *dst)
@@ -131,11 +161,7 @@ template <int N, int ROWS, int COLS> struct Tile {
         }
         return f;
     }
-    // column m0 + c, the contraction runs down the rows: 16 lanes fetch 4 rows of 16 and receive them transposed
-    __device__ static bf16x4 down(const bf16 *q)
-    {
-        return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)q));
-    }
+    // column m0 + c, the contraction runs down the rows
     __device__ Frag<N> straight_down(int k0, int m0, int lane) const
     {
         Frag<N> f;
@@ -143,7 +169,7 @@ template <int N, int ROWS, int COLS> struct Tile {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const bf16 *q = p + n * PLANE + (k0 + 8 * (lane / 16) + i / 4) * LD + m0 + 4 * (i % 4);
-            f.p[n] = __builtin_shufflevector(down(q), down(q + 4 * LD), 0, 1, 2, 3, 4, 5, 6, 7);
+            f.p[n] = __builtin_shufflevector(read_down(q), read_down(q + 4 * LD), 0, 1, 2, 3, 4, 5, 6, 7);
         }
         return f;
     }
@@ -154,7 +180,7 @@ template <int N, int ROWS, int COLS> struct Tile {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const bf16 *q = p + n * PLANE + (k0 + 4 * (lane / 16) + i / 4) * LD + m0 + 4 * (i % 4);
-            f.p[n] = __builtin_shufflevector(down(q), down(q + 16 * LD), 0, 1, 2, 3, 4, 5, 6, 7);
+            f.p[n] = __builtin_shufflevector(read_down(q), read_down(q + 16 * LD), 0, 1, 2, 3, 4, 5, 6, 7);
         }
         return f;
     }

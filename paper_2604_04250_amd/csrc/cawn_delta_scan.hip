@@ -12,7 +12,7 @@
 //
 // A wave owns 16 columns of the state, all rows of them, in result layout, which is the operand layout of the next product.  Per chunk:
 //     X = beta (V - e^G K S),  U = T X,  O^T = scale (e^G S^T Q^T + U^T P^T),  S = e^{G_C} S + K^T (e^{G_C - G} U)
-// with P made by all waves together and T fetched as operands.
+// with P made by all waves together and T fetched.
 #include <stddef.h>
 
 #include "cawn_delta_mfma.hpp"
@@ -20,8 +20,7 @@
 namespace cawn {
 namespace delta {
 
-// What a chunk is by itself, every chunk a workgroup: gates, the norms' factors, and T = (I + diag(beta) N)^-1 as operands: row tile t,
-// 32 columns ks at lower(t, ks), three planes each; for a backward its transpose too.
+// What a chunk is by itself, every chunk a workgroup: gates, the norms' factors, and T = (I + diag(beta) N)^-1.
 template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void delta_system(const Args a)
 {
     constexpr int KS = KP / 32;
@@ -67,7 +66,7 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
     const long long at = (long long)bh * a.chunks + n;
     for (int i = tid; i < (int)(sizeof(Gates) / 4); i += 256) a.gates[at * GATE_FLOATS + i] = ((const float *)&G)[i];
     invert(M, w, lane);
-    bf16x8 *out = reinterpret_cast<bf16x8 *>(a.t_ops + (size_t)at * T_BYTES) + lane;
+    char *out = a.t_ops + (size_t)at * T_BYTES + t_slot(g, c);
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
         if (2 * ks > w) break;
@@ -81,26 +80,13 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
         Frag<3> f;
         split8<3>(y, f);
 #pragma unroll
-        for (int e = 0; e < 3; ++e) out[(lower(w, ks) * 3 + e) * 64] = f.p[e];
-    }
-    if (!a.tt_ops) return;
-    out = reinterpret_cast<bf16x8 *>(a.tt_ops + (size_t)at * T_BYTES) + lane;
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-        if (2 * ks + 1 < w) continue;
-        float y[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = M[(32 * ks + 16 * (e / 4) + 4 * g + e % 4) * TLD + 16 * w + c];
-        Frag<3> f;
-        split8<3>(y, f);
-#pragma unroll
-        for (int e = 0; e < 3; ++e) out[(upper(w, ks) * 3 + e) * 64] = f.p[e];
+        for (int e = 0; e < 3; ++e) *reinterpret_cast<bf16x8 *>(out + (lower(w, ks) * 3 + e) * 1024) = f.p[e];
     }
 }
 
 template <int NP, int KP, int MODE> struct ScanLds {
     static constexpr int PO = NP == 1 ? 2 : 3;
-    static constexpr int KB = Tile<NP, CHUNK, KP>::BYTES, TO = MODE == 0 ? 2 * KB : KB;     // k, q; T's operands; P's
+    static constexpr int KB = Tile<NP, CHUNK, KP>::BYTES, TO = MODE == 0 ? 2 * KB : KB;     // k, q; T; P's operands
     static constexpr int P = TO + T_BYTES, BYTES = P + (MODE == 0 ? 6 * PO * 1024 : 0);
     // waves a SIMD that the registers are budgeted for: as many workgroups as the LDS holds, three (MODE 1, of eight waves: two) at most
     static constexpr int HELD = 163840 / (BYTES + (int)sizeof(Gates)), WAVES = MODE == 0 ? (HELD > 3 ? 3 : HELD) : (HELD > 2 ? 2 : HELD) * 2;
@@ -113,8 +99,9 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ Gates G;
     const Tile<NP, CHUNK, KP> k{(bf16 *)lds}, q{(bf16 *)(lds + L::KB)};
-    bf16x8 *tf = reinterpret_cast<bf16x8 *>(lds + L::TO), *pf = reinterpret_cast<bf16x8 *>(lds + L::P);
-    const int rows_all = a.B * a.H, blk = blockIdx.x, bh = blk % rows_all, nseg = MODE == 0 || a.tt_ops ? a.segments : a.segments - 1;
+    const char *tl = lds + L::TO;
+    bf16x8 *pf = reinterpret_cast<bf16x8 *>(lds + L::P);
+    const int rows_all = a.B * a.H, blk = blockIdx.x, bh = blk % rows_all, nseg = MODE == 0 || a.s_tiles ? a.segments : a.segments - 1;
     const int seg = blk / rows_all % nseg, group = blk / rows_all / nseg, b = bh / a.H, h = bh % a.H;
     const int len = row_length(a, b), nb = (len + CHUNK - 1) / CHUNK;
     const int n0 = min(seg * a.seg_chunks, nb), n1 = min(n0 + a.seg_chunks, nb);
@@ -177,7 +164,7 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
         for (int e = 0; e < GN; ++e)
             if (tid + e * NT < GATE_FLOATS) ((float *)&G)[tid + e * NT] = ga[e];
         {
-            // T's operands come straight into LDS
+            // T comes straight into LDS
             const char *src = a.t_ops + ((size_t)bh * a.chunks + n) * T_BYTES;
             char *dst = lds + L::TO;
 #pragma unroll
@@ -291,21 +278,18 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) split_tiles<3>(X[2 * ks], X[2 * ks + 1], xf[ks]);
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();                    // T's and P's operands
+            __syncthreads();                    // T, and P's operands
             anew();
             Frag<3> f[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 U[t] = zero;
-#pragma unroll
-                for (int e = 0; e < 3; ++e) f[t].p[e] = tf[(lower(t, 0) * 3 + e) * 64 + lane];
+                f[t] = t_rows(tl, t, 0, lane);
             }
             mma_each<3>(f, xf[0], U);
             Frag<3> f2[2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 3; ++e) f2[t].p[e] = tf[(lower(2 + t, 1) * 3 + e) * 64 + lane];
+            for (int t = 0; t < 2; ++t) f2[t] = t_rows(tl, 2 + t, 1, lane);
             mma_each<3>(f2, xf[1], U + 2);
         }
         anew();
@@ -421,7 +405,7 @@ template <typename T, int NP, int KP> static int scan_kp(const Args &a, hipStrea
     if (a.segments > 1) {
         constexpr int bytes = ScanLds<NP, KP, 1>::BYTES;
         if (bytes > 60000 && hipFuncSetAttribute((const void *)delta_scan<T, NP, KP, 1>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CAWN_ELAUNCH;
-        hipLaunchKernelGGL((delta_scan<T, NP, KP, 1>), dim3((unsigned)(rows * (a.tt_ops ? a.segments : a.segments - 1) * ceil_div(a.VT + KP / 16, 8))), dim3(512), bytes, s, a);
+        hipLaunchKernelGGL((delta_scan<T, NP, KP, 1>), dim3((unsigned)(rows * (a.s_tiles ? a.segments : a.segments - 1) * ceil_div(a.VT + KP / 16, 8))), dim3(512), bytes, s, a);
         if (int r = launched()) return r;
         if (int r = launch_join(a, false, s)) return r;
     }
