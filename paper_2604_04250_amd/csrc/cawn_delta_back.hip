@@ -78,6 +78,7 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__(256
 #pragma unroll
         for (int e = 0; e < GN; ++e)
             if (tid + e * NT < GATE_FLOATS) ((float *)&G)[tid + e * NT] = ga[e];
+        __syncthreads();
         {
             const char *src = a.t_ops + ((size_t)bh * a.chunks + n) * T_BYTES;
 #pragma unroll
@@ -86,7 +87,6 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__(256
                 if (i < T_BYTES / 1024) load_piece(src + (size_t)i * 1024 + l16, lds + L::TO + i * 1024);
             }
         }
-        __syncthreads();
         T da[4][4];
         if (mine) {
             const T *dp = (const T *)a.dO + b * a.osb + (long long)n * CHUNK * ost + (long long)h * a.V;

@@ -163,8 +163,9 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
 #pragma unroll
         for (int e = 0; e < GN; ++e)
             if (tid + e * NT < GATE_FLOATS) ((float *)&G)[tid + e * NT] = ga[e];
+        __syncthreads();
         {
-            // T comes straight into LDS
+            // T comes straight into LDS (behind the barrier, which would wait for it)
             const char *src = a.t_ops + ((size_t)bh * a.chunks + n) * T_BYTES;
             char *dst = lds + L::TO;
 #pragma unroll
@@ -173,7 +174,6 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
                 if (i < T_BYTES / 1024) load_piece(src + (size_t)i * 1024 + l16, dst + i * 1024);
             }
         }
-        __syncthreads();
         // v is wanted last.  (What is not there is loaded from where something is, and dropped where it is used: a load behind a lane's
         // branch, or one whose value is converted at once, would be waited for here)
         T va[4][4];
