@@ -142,11 +142,6 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__(256
                 for (int e = 0; e < 3; ++e) pf[(upper(w, ks) * 3 + e) * 64 + lane] = f.p[e];
             }
         }
-        if (MODE == 0 && mine) {
-            char *st = a.ds_tiles + ((size_t)bh * a.chunks + n) * KT * a.VT * 1024 + (size_t)ct * 1024;
-#pragma unroll
-            for (int t = 0; t < KT; ++t) *reinterpret_cast<f32x4 *>(st + (size_t)t * a.VT * 1024 + l16) = S[t];
-        }
         anew();
         f32x4 Z[4] = {zero, zero, zero, zero}, R[4] = {zero, zero, zero, zero};
 #pragma unroll
@@ -201,6 +196,12 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__(256
 #pragma unroll
             for (int t = 0; t < 4; ++t) f[t] = t_columns(tl, t, 1, lane);
             mma_each<3>(f, zf[1], R);
+        }
+        // (stores behind the wait for T, which would wait for them too)
+        if (MODE == 0 && mine) {
+            char *st = a.ds_tiles + ((size_t)bh * a.chunks + n) * KT * a.VT * 1024 + (size_t)ct * 1024;
+#pragma unroll
+            for (int t = 0; t < KT; ++t) *reinterpret_cast<f32x4 *>(st + (size_t)t * a.VT * 1024 + l16) = S[t];
         }
         if (MODE == 0 && mine) {
             char *rt = a.dr_tiles + ((size_t)bh * a.chunks + n) * 4 * a.VT * 1024 + (size_t)ct * 1024;

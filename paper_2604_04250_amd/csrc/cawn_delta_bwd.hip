@@ -43,17 +43,10 @@ template <typename T, int NP, int KP> struct GradLds {
 // four rows of a column, N planes, into a transposed matrix
 template <int N, int ROWS, int COLS> __device__ inline void put_column(const Tile<N, ROWS, COLS> &t, int col, int row0, f32x4 x)
 {
-    float r[4] = {x[0], x[1], x[2], x[3]};
+    bf16x4 h[N];
+    split4<N>(x, h);
 #pragma unroll
-    for (int p = 0; p < N; ++p) {
-        bf16x4 h;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            h[i] = (bf16)r[i];
-            r[i] -= (float)h[i];
-        }
-        *reinterpret_cast<bf16x4 *>(t.p + p * Tile<N, ROWS, COLS>::PLANE + col * Tile<N, ROWS, COLS>::LD + row0) = h;
-    }
+    for (int p = 0; p < N; ++p) *reinterpret_cast<bf16x4 *>(t.p + p * Tile<N, ROWS, COLS>::PLANE + col * Tile<N, ROWS, COLS>::LD + row0) = h[p];
 }
 
 // four values of a row, from their planes

@@ -26,17 +26,10 @@ template <int KP, bool REV> __global__ __launch_bounds__(256) void delta_join(co
         for (int o = 0; o < OWN; ++o) {
             const int t = w + 4 * o;
             if (t >= KT) break;
-            float r[4] = {S[o][0], S[o][1], S[o][2], S[o][3]};
+            bf16x4 h[3];
+            split4<3>(S[o], h);
 #pragma unroll
-            for (int p = 0; p < 3; ++p) {
-                bf16x4 h;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    h[e] = (bf16)r[e];
-                    r[e] -= (float)h[e];
-                }
-                *reinterpret_cast<bf16x4 *>(lds + (((buf * KS + t / 2) * 3 + p) * 64 + lane) * 16 + (t % 2) * 8) = h;
-            }
+            for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x4 *>(lds + (((buf * KS + t / 2) * 3 + p) * 64 + lane) * 16 + (t % 2) * 8) = h[p];
         }
     };
     auto fetch = [&](int i) {                   // of the i-th link

@@ -69,18 +69,47 @@ template <int S, int N, int NA, int NB> __device__ inline void mma_each(const Fr
         }
 }
 
-template <int N> __device__ inline void split8(const float (&x)[8], Frag<N> &f)
+// Pairs at a time: one conversion makes two values of a plane
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+template <int N, int W> __device__ inline void split_pairs(const float *x, bf16 (*f)[W])
 {
+    static_assert(W % 2 == 0, "");
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        float r = x[e];
+    for (int e = 0; e < W; e += 2) {
+        float lo = x[e], hi = x[e + 1];
 #pragma unroll
         for (int p = 0; p < N; ++p) {
-            const bf16 h = (bf16)r;
-            f.p[p][e] = h;
-            if (p + 1 < N) r -= (float)h;
+            const f32x2 r = {lo, hi};
+            const bf16x2 h = __builtin_convertvector(r, bf16x2);
+            if (p + 1 < N) {
+                const uint32_t u = __builtin_bit_cast(uint32_t, h);
+                lo -= __builtin_bit_cast(float, u << 16);
+                hi -= __builtin_bit_cast(float, u & 0xffff0000u);
+            }
+            f[p][e] = h[0], f[p][e + 1] = h[1];
         }
     }
+}
+
+template <int N> __device__ inline void split8(const float (&x)[8], Frag<N> &f)
+{
+    bf16 y[N][8];
+    split_pairs<N, 8>(x, y);
+#pragma unroll
+    for (int p = 0; p < N; ++p)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f.p[p][e] = y[p][e];
+}
+// four values, plane by plane
+template <int N> __device__ inline void split4(f32x4 x, bf16x4 (&f)[N])
+{
+    const float r[4] = {x[0], x[1], x[2], x[3]};
+    bf16 y[N][4];
+    split_pairs<N, 4>(r, y);
+#pragma unroll
+    for (int p = 0; p < N; ++p)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[p][e] = y[p][e];
 }
 
 // two result tiles as one operand in tile order

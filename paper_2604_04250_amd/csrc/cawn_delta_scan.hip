@@ -232,11 +232,6 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
             }
         }
         // what hangs on the state before the chunk
-        if (MODE == 0 && a.s_tiles && mine) {
-            char *st = a.s_tiles + bh * a.s_row + n * a.s_chunk + (size_t)ct * 1024;
-#pragma unroll
-            for (int t = 0; t < KT; ++t) *reinterpret_cast<f32x4 *>(st + (size_t)t * a.VT * 1024 + l16) = S[t];
-        }
         anew();
         f32x4 U[4];
         f32x4 O[MODE == 0 ? 4 : 1];
@@ -294,6 +289,12 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
         }
         anew();
         if (MODE == 0) {
+            // (stores behind the wait for T, which would wait for them too)
+            if (a.s_tiles && mine) {
+                char *st = a.s_tiles + bh * a.s_row + n * a.s_chunk + (size_t)ct * 1024;
+#pragma unroll
+                for (int t = 0; t < KT; ++t) *reinterpret_cast<f32x4 *>(st + (size_t)t * a.VT * 1024 + l16) = S[t];
+            }
             if (a.u_tiles && mine) {
                 char *ut = a.u_tiles + bh * a.u_row + n * a.u_chunk + (size_t)ct * 1024;
 #pragma unroll
