@@ -84,18 +84,23 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
     }
 }
 
-template <int NP, int KP, int MODE> struct ScanLds {
+// The scan's LDS: k, q (MODE 0); T; P's operands.  With one plane to an operand P has a place of its own and is made ahead of the products
+// with the state; with three it would leave room for one workgroup a CU, so P is made where T was, for one more barrier (4,096 tokens of
+// 12 heads of 64 in fp32: 90 us, against 99 in a place of its own; bf16, 2 x 32,768 tokens of 32 heads of 128: 3,131 us in T's place, 3,049 in its own).
+template <int NP, int KP, int MODE, int NW> struct ScanLds {
     static constexpr int PO = NP == 1 ? 2 : 3;
-    static constexpr int KB = Tile<NP, CHUNK, KP>::BYTES, TO = MODE == 0 ? 2 * KB : KB;     // k, q; T; P's operands
-    static constexpr int P = TO + T_BYTES, BYTES = P + (MODE == 0 ? 6 * PO * 1024 : 0);
-    // waves a SIMD that the registers are budgeted for: as many workgroups as the LDS holds, three (MODE 1, of eight waves: two) at most
-    static constexpr int HELD = 163840 / (BYTES + (int)sizeof(Gates)), WAVES = MODE == 0 ? (HELD > 3 ? 3 : HELD) : (HELD > 2 ? 2 : HELD) * 2;
+    static constexpr int KB = Tile<NP, CHUNK, KP>::BYTES, TO = MODE == 0 ? 2 * KB : KB;
+    static constexpr bool P_EARLY = NP == 1;
+    static constexpr int P = P_EARLY ? TO + T_BYTES : TO, BYTES = TO + T_BYTES + (MODE == 0 && P_EARLY ? 6 * PO * 1024 : 0);
+    static_assert(6 * PO * 1024 <= T_BYTES, "P in T's place");
+    // waves a SIMD that the registers are budgeted for: as many workgroups as the LDS holds, but three waves (MODE 1: four) at most
+    static constexpr int HELD = 163840 / (BYTES + (int)sizeof(Gates)) * NW / 4, MOST = MODE == 1 ? 4 : 3, WAVES = HELD > MOST ? MOST : HELD;
 };
 
-template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MODE == 0 ? 256 : 512), (ScanLds<NP, KP, MODE>::WAVES)) void delta_scan(const Args a)
+template <typename T, int NP, int KP, int MODE, int NW> __global__ __launch_bounds__((64 * NW), (ScanLds<NP, KP, MODE, NW>::WAVES)) void delta_scan(const Args a)
 {
-    using L = ScanLds<NP, KP, MODE>;
-    constexpr int KS = KP / 32, KT = KP / 16, PO = L::PO, NT = MODE == 0 ? 256 : 512, NW = NT / 64;
+    using L = ScanLds<NP, KP, MODE, NW>;
+    constexpr int KS = KP / 32, KT = KP / 16, PO = L::PO, NT = 64 * NW;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ Gates G;
     const Tile<NP, CHUNK, KP> k{(bf16 *)lds}, q{(bf16 *)(lds + L::KB)};
@@ -152,6 +157,33 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
 #pragma unroll
         for (int e = 0; e < GN; ++e) ga[e] = gp[min(tid + e * NT, GATE_FLOATS - 1)];
     };
+    auto make_p = [&]() {
+        // P's operands, transposed (the result layout is the operand's), shared out: with four waves the first two, whose rows are short, take two
+        const int two = NW == 4 && w < 2, first = two ? 2 * w : NW == 4 ? w + 2 : w;
+        for (int id = first; id < min(first + 1 + two, 6); ++id) {
+            anew();
+            const int it = id < 2 ? id : id / 2 + 1, js = id == 3 || id == 5, i = 16 * it + c;
+            f32x4 pt[2];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int jt = 2 * js + half;
+                pt[half] = zero;
+                if (jt <= it) {
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) pt[half] = mma<3>(k.straight(16 * jt, 32 * ks, lane), q.straight(16 * it, 32 * ks, lane), pt[half]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int j = 16 * jt + 4 * g + r;
+                        pt[half][r] = i >= j ? pt[half][r] * (G.rk[j] * decay_between(G, i, j)) : 0.f;
+                    }
+                }
+            }
+            Frag<PO> f;
+            split_tiles<PO>(pt[0], pt[1], f);
+#pragma unroll
+            for (int e = 0; e < PO; ++e) pf[(id * PO + e) * 64 + lane] = f.p[e];
+        }
+    };
     if (n0 < n1) ahead(n0);
     for (int n = n0; n < n1; ++n) {
         const int rows = min(CHUNK, len - n * CHUNK);
@@ -205,32 +237,7 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
         }
         if (n + 1 < n1) ahead(n + 1);
         anew();
-        // P's row tile w, transposed: its result layout is the operand's
-        if (MODE == 0) {
-            f32x4 pt[4];
-            const int i = 16 * w + c;
-#pragma unroll
-            for (int jt = 0; jt < 4; ++jt) {
-                pt[jt] = zero;
-                if (jt <= w) {
-#pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) pt[jt] = mma<3>(k.straight(16 * jt, 32 * ks, lane), q.straight(16 * w, 32 * ks, lane), pt[jt]);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int j = 16 * jt + 4 * g + r;
-                        pt[jt][r] = i >= j ? pt[jt][r] * (G.rk[j] * decay_between(G, i, j)) : 0.f;
-                    }
-                }
-            }
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                if (2 * ks > w) break;
-                Frag<PO> f;
-                split_tiles<PO>(pt[2 * ks], pt[2 * ks + 1], f);
-#pragma unroll
-                for (int e = 0; e < PO; ++e) pf[(lower(w, ks) * PO + e) * 64 + lane] = f.p[e];
-            }
-        }
+        if (MODE == 0 && L::P_EARLY) make_p();
         // what hangs on the state before the chunk
         anew();
         f32x4 U[4];
@@ -273,7 +280,7 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) split_tiles<3>(X[2 * ks], X[2 * ks + 1], xf[ks]);
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();                    // T, and P's operands
+            __syncthreads();                    // T
             anew();
             Frag<3> f[4];
 #pragma unroll
@@ -300,6 +307,41 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
 #pragma unroll
                 for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4 *>(ut + (size_t)t * a.VT * 1024 + l16) = U[t];
             }
+        }
+        if (MODE == 0 && !L::P_EARLY) {
+            __syncthreads();                    // nobody reads T any more
+            make_p();
+        }
+        anew();
+        {
+            Frag<3> uf[2];
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                f32x4 y[2];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int t = 2 * ks + half;
+                    y[half] = U[t] * *reinterpret_cast<const f32x4 *>(G.c + 16 * t + 4 * g);
+                }
+                split_tiles<3>(y[0], y[1], uf[ks]);
+            }
+            const float e = G.eg[CHUNK - 1];
+#pragma unroll
+            for (int t = 0; t < KT; ++t) S[t] *= e;
+            constexpr int AT = KT < 4 ? KT : 4;
+#pragma unroll
+            for (int t0 = 0; t0 < KT; t0 += AT)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    Frag<NP> f[AT];
+#pragma unroll
+                    for (int t = 0; t < AT; ++t) f[t] = k.tiled_down(32 * ks, 16 * (t0 + t), lane);
+                    mma_each<3>(f, uf[ks], S + t0);
+                }
+        }
+        if (MODE == 0) {
+            if (!L::P_EARLY) __syncthreads();   // P's operands
+            anew();
             Frag<PO> uf[2];
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) split_tiles<PO>(U[2 * ks], U[2 * ks + 1], uf[ks]);
@@ -339,40 +381,12 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
                 }
             }
         }
-        anew();
-        {
-            Frag<3> uf[2];
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                f32x4 y[2];
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int t = 2 * ks + half;
-                    y[half] = U[t] * *reinterpret_cast<const f32x4 *>(G.c + 16 * t + 4 * g);
-                }
-                split_tiles<3>(y[0], y[1], uf[ks]);
-            }
-            const float e = G.eg[CHUNK - 1];
-#pragma unroll
-            for (int t = 0; t < KT; ++t) S[t] *= e;
-            constexpr int AT = KT < 4 ? KT : 4;
-#pragma unroll
-            for (int t0 = 0; t0 < KT; t0 += AT)
-#pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-                    Frag<NP> f[AT];
-#pragma unroll
-                    for (int t = 0; t < AT; ++t) f[t] = k.tiled_down(32 * ks, 16 * (t0 + t), lane);
-                    mma_each<3>(f, uf[ks], S + t0);
-                }
-        }
     }
     if (MODE == 0) {
         // chunks of this segment that the row does not have
         const int last = min(seg == a.segments - 1 ? a.chunks : (seg + 1) * a.seg_chunks, a.chunks);
         for (int t = max(n1, seg * a.seg_chunks) * CHUNK + (int)threadIdx.x / 64; t < min(last * CHUNK, a.L); t += NW) {
-            const int vv = group * NW * 16 + lane;
-            if (vv < a.V) ((T *)a.o)[b * a.osb + (long long)t * a.ost + (long long)h * a.V + vv] = (T)0.f;
+            for (int vv = group * NW * 16 + lane; vv < min(a.V, (group + 1) * NW * 16); vv += 64) ((T *)a.o)[b * a.osb + (long long)t * a.ost + (long long)h * a.V + vv] = (T)0.f;
         }
     }
     if (!mine) return;
@@ -400,21 +414,26 @@ template <typename T, int NP, int KP, int MODE> __global__ __launch_bounds__((MO
     }
 }
 
+template <typename T, int NP, int KP, int MODE, int NW> static int launch(const Args &a, long long segments, long long tiles, hipStream_t s)
+{
+    constexpr int bytes = ScanLds<NP, KP, MODE, NW>::BYTES;
+    static_assert(bytes + sizeof(Gates) <= 163840, "LDS");
+    if (bytes > 60000 && hipFuncSetAttribute((const void *)delta_scan<T, NP, KP, MODE, NW>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CAWN_ELAUNCH;
+    hipLaunchKernelGGL((delta_scan<T, NP, KP, MODE, NW>), dim3((unsigned)((long long)a.B * a.H * segments * ceil_div(tiles, NW))), dim3(64 * NW), bytes, s, a);
+    return launched();
+}
+
 template <typename T, int NP, int KP> static int scan_kp(const Args &a, hipStream_t s)
 {
-    const long long rows = (long long)a.B * a.H;
     if (a.segments > 1) {
-        constexpr int bytes = ScanLds<NP, KP, 1>::BYTES;
-        if (bytes > 60000 && hipFuncSetAttribute((const void *)delta_scan<T, NP, KP, 1>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CAWN_ELAUNCH;
-        hipLaunchKernelGGL((delta_scan<T, NP, KP, 1>), dim3((unsigned)(rows * (a.s_tiles ? a.segments : a.segments - 1) * ceil_div(a.VT + KP / 16, 8))), dim3(512), bytes, s, a);
-        if (int r = launched()) return r;
+        if (int r = launch<T, NP, KP, 1, 8>(a, a.s_tiles ? a.segments : a.segments - 1, a.VT + KP / 16, s)) return r;
         if (int r = launch_join(a, false, s)) return r;
     }
-    constexpr int bytes = ScanLds<NP, KP, 0>::BYTES;
-    static_assert(bytes + sizeof(Gates) <= 163840, "LDS");
-    if (bytes > 60000 && hipFuncSetAttribute((const void *)delta_scan<T, NP, KP, 0>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CAWN_ELAUNCH;
-    hipLaunchKernelGGL((delta_scan<T, NP, KP, 0>), dim3((unsigned)(rows * a.segments * ceil_div(a.VT, 4))), dim3(256), bytes, s, a);
-    return launched();
+    // Where the LDS holds one workgroup of four waves a CU, eight waves take twice the columns, if there are as many (4,096 tokens of 8 heads
+    // of 128 in fp32: 186 us, 213 with four waves).  Elsewhere eight waves wait for each other (bf16, 2 x 32,768 of 32 heads of 128: 3,390 us, 3,049 with four)
+    if constexpr (NP == 3 && KP == 128)
+        if (a.VT > 4) return launch<T, NP, KP, 0, 8>(a, a.segments, a.VT, s);
+    return launch<T, NP, KP, 0, 4>(a, a.segments, a.VT, s);
 }
 
 template <typename T, int NP, int KP> static int system_kp(const Args &a, hipStream_t s)
