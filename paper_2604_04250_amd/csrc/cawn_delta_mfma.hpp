@@ -215,53 +215,18 @@ template <int N, int ROWS, int COLS> struct Tile {
     }
 };
 
-// `rows` (of 64) rows of `cols` elements into planes, zeros beyond; norm: 1 / sqrt(sum of squares + eps) of every row (1 beyond).
-// 256 threads; vec: rows may be read 16 bytes at a time.
-template <typename T, int N, int COLS>
-__device__ inline void stage_rows(const Tile<N, CHUNK, COLS> &t, const T *base, long long stride, int rows, int cols, bool vec, float *norm, bool normed, float eps)
-{
-    constexpr int U = COLS / 8;         // units of 8 columns: a row's lie in adjacent lanes
-    for (int u = threadIdx.x; u < CHUNK * U; u += 256) {
-        const int r = u / U, c = u % U * 8;
-        float x[8];
-        const T *src = base + (long long)r * stride + c;
-        if (r < rows && c + 8 <= cols && vec) {
-            if constexpr (sizeof(T) == 2) load_n<T, 8>(src, x);
-            else {
-                float a[4], b[4];
-                load_n<T, 4>(src, a);
-                load_n<T, 4>(src + 4, b);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = r < rows && c + i < cols ? (float)src[i] : 0.f;
-        }
-        if (norm) {
-            float s = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
-#pragma unroll
-            for (int m = U / 2; m > 0; m >>= 1) s += __shfl_xor(s, m);
-            if (u % U == 0) norm[r] = normed && r < rows ? 1.f / sqrtf(s + eps) : 1.f;
-        }
-        Frag<N> f;
-        split8<N>(x, f);
-#pragma unroll
-        for (int n = 0; n < N; ++n) *reinterpret_cast<bf16x8 *>(t.p + n * Tile<N, CHUNK, COLS>::PLANE + r * Tile<N, CHUNK, COLS>::LD + c) = f.p[n];
-    }
-}
-
-// The same in two steps, so that a chunk's rows travel while the one before is treated: into registers, and from there into planes.
+// `rows` (of 64) rows of `cols` elements into planes, zeros beyond, in two steps, so that a chunk's rows travel while the one before is
+// treated: into registers, and from there into planes.  (Lanes beyond 64 rows' units do what others do too.)
 template <typename T, int N, int COLS, int NT> struct RowsAhead {
-    static constexpr int U = COLS / 8, UNITS = CHUNK * U / NT;
+    static constexpr int U = COLS / 8, ALL = CHUNK * U, UNITS = ALL < NT ? 1 : ALL / NT;
+    static_assert(ALL < NT ? NT % ALL == 0 : ALL % NT == 0, "");
     Pack<T, 8> x[UNITS];
     // What is not there is loaded from where something is, and dropped in put(): a load behind a lane's branch would be waited for.
     // rows, cols >= 1; vec: cols a multiple of 16 bytes' elements, and every row aligned to 16 bytes
     __device__ void load(int tid, const T *base, long long stride, int rows, int cols, bool vec)
     {
         constexpr int W = 16 / sizeof(T), STEP = NT / U;        // rows from one unit of a lane to its next
+        if (ALL < NT) tid %= ALL;
         const long long row = stride * (long long)sizeof(T);
         if (vec && rows == CHUNK && cols == COLS && row < (1 << 24)) {
             // all there: one offset a lane, the rest the same for all
@@ -290,6 +255,7 @@ template <typename T, int N, int COLS, int NT> struct RowsAhead {
     }
     __device__ void put_plain(int tid, const Tile<N, CHUNK, COLS> &t, int rows, int cols)
     {
+        if (ALL < NT) tid %= ALL;
         if (rows < CHUNK || cols < COLS) {              // (the same for all lanes)
 #pragma unroll
             for (int e = 0; e < UNITS; ++e) {
@@ -324,6 +290,7 @@ template <typename T, int N, int COLS, int NT> struct RowsAhead {
     // (cols: of which what lies beyond has not been zeroed yet)
     __device__ void factors(int tid, float *norm, int rows, int cols, bool normed, float eps)
     {
+        if (ALL < NT) tid %= ALL;
 #pragma unroll
         for (int e = 0; e < UNITS; ++e) {
             const int u = tid + e * NT, r = u / U;
