@@ -68,6 +68,7 @@ __device__ inline int row_length(const Args &a, int b)
 
 int launch_token(const Args &a, bool bf16, hipStream_t s);
 int launch_system(const Args &a, bool bf16, hipStream_t s);
+int scan_held(int K, int VT, bool bf16_, int *columns);      // workgroups of the scan that a CU holds, and the column tiles of each
 int launch_scan(const Args &a, bool bf16, hipStream_t s);               // forward, behind the gates
 int launch_join(const Args &a, bool reverse, hipStream_t s);
 

@@ -7,20 +7,25 @@ using cawn::delta::Args;
 
 using cawn::delta::Sizes;
 
-#ifndef WANT
-#define WANT 768
-#endif
 namespace {
 
 // How a row's chunks are cut into segments.  A segment costs each of its chunks twice (what it makes of a state, then its outputs) and
 // one link of the join, so two segments gain nothing; many shorten the two passes until the chip is full or the links cost as much.
-void cut(Args *a)
+// Full are 256 CUs with the scan's workgroups that one holds; beyond that a second round would begin.  (Two short rounds of one chunk
+// are no longer than one of two, if the second is a sixteenth at most: 5 x 777 tokens of 4 heads of 64 x 128, fp32, training: 145 us, 152.)
+// (Whole calls, for 512, 768 and 1,024 workgroups: 8 x 8,192 tokens of 12 heads of 64, bf16, training, three to a CU: 1,547, 1,469, 1,521 us;
+// 4 x 4,096 tokens of 8 heads of 128, the same, two to a CU: 718, 828, 803 us.)  A link of the join takes about a thirteenth of a
+// chunk's two passes, which is where the least length of a segment comes from.
+void cut(Args *a, bool bf16)
 {
-    const long long groups = (long long)a->B * a->H * ceil_div(a->VT, 4);
-    const long long want = groups > 0 ? WANT / groups : 1;
+    int columns;
+    const long long slots = 256LL * delta::scan_held(a->K, a->VT, bf16, &columns);
+    const long long groups = (long long)a->B * a->H * ceil_div(a->VT, columns);
+    const long long want = groups > 0 ? slots / groups : 1;
     a->segments = 1, a->seg_chunks = a->chunks;
     if (want < 3 || a->chunks < 6) return;
     long long m = ceil_div(a->chunks, want);
+    if (m == 2 && groups * a->chunks * 16 <= slots * 17) m = 1;
     while (m * m * 13 < a->chunks) ++m;
     const long long segments = ceil_div(a->chunks, m);
     if (segments < 3) return;
@@ -44,7 +49,7 @@ int check(const cawn_delta_desc *d, Args *a)
     a->chunks = (int)ceil_div(d->L, delta::CHUNK);
     a->VT = (int)ceil_div(d->V, 16);
     if ((long long)d->B * d->H * ceil_div(d->V, 16) > 0x7fffffffLL) return CAWN_EUNSUPPORTED;
-    cut(a);
+    cut(a, d->bf16 != 0);
     return CAWN_OK;
 }
 

@@ -453,6 +453,20 @@ int launch_system(const Args &a, bool bf16_, hipStream_t s)
     return bf16_ ? system_kp<bf16, 1, 128>(a, s) : system_kp<float, 3, 128>(a, s);
 }
 
+template <int NP, int KP> static int held(int VT, int *columns)
+{
+    const bool wide = NP == 3 && KP == 128 && VT > 4;           // as scan_kp has it
+    *columns = wide ? 8 : 4;
+    return wide ? ScanLds<NP, KP, 0, 8>::WAVES / 2 : ScanLds<NP, KP, 0, 4>::WAVES;
+}
+
+int scan_held(int K, int VT, bool bf16_, int *columns)
+{
+    if (K <= 32) return bf16_ ? held<1, 32>(VT, columns) : held<3, 32>(VT, columns);
+    if (K <= 64) return bf16_ ? held<1, 64>(VT, columns) : held<3, 64>(VT, columns);
+    return bf16_ ? held<1, 128>(VT, columns) : held<3, 128>(VT, columns);
+}
+
 int launch_scan(const Args &a, bool bf16_, hipStream_t s)
 {
     if (a.K <= 32) return bf16_ ? scan_kp<bf16, 1, 32>(a, s) : scan_kp<float, 3, 32>(a, s);
