@@ -7,8 +7,9 @@
 //   T = 1 (a token's heads, each by itself): a run of 4 to 64 lanes holds a group in registers from the one read to the write; the
 //     variance is that of the centred values.  Bytes: x in, y out (backward: x, dy in, dx out).
 //   T > 1, or a group too wide for 64 lanes' registers: a workgroup sums a run of tokens over its channels, a second kernel joins
-//     the sums and applies them: x is read twice.  Sums are taken of x less the group's first value: as exact as two passes
-//     unless that value is many deviations off the mean.
+//     the sums and applies them: x is read twice.  A thread's sums are of x less its own first value, and threads and workgroups are
+//     joined as (count, mean, sum of squares about it), means within a run as differences from its first value: neither a mean of many
+//     deviations nor a first value that is far off costs the variance its digits.
 // Parameter gradients: every workgroup keeps its channels' sums over the rows it takes and leaves them in the workspace; a last
 // kernel adds these in a fixed order.
 #include "cawn_ops.hpp"
@@ -215,7 +216,7 @@ template <typename T, int VEC, int NIT, bool BWD> __global__ __launch_bounds__(2
 
 // ---------------------------------------------------------------------------------------------- T > 1
 // A workgroup: a.cb adjacent channels (whole groups, or a piece of one), a run of tokens, rows bblk, bblk + bblocks, ...
-// WHAT 0: sums of x and x^2 -> part;  1: y;  2: sums of t and t xh -> part, column sums -> colpart;  3: dx
+// WHAT 0: mean and sum of squares about it -> part;  1: y;  2: sums of t and t xh -> part, column sums -> colpart;  3: dx
 template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void group_norm_runs(const NormArgs a)
 {
     __shared__ float sh[2][256 * (WHAT == 2 ? VEC : 1)];
@@ -237,7 +238,6 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
     const double n = (double)a.T * a.cg;
     for (int b = bblk; b < a.B; b += a.bblocks) {
         const T *xb = (const T *)a.x + b * a.xsb + c;
-        const float shift = WHAT == 0 && mine ? (float)*((const T *)a.x + b * a.xsb + (long long)g * a.cg) : 0.f;
         float p0 = 0.f, p1 = 0.f;       // WHAT 1..3: mean, rstd
         float m1 = 0.f, m2 = 0.f;
         if (WHAT == 1 || WHAT == 3) {
@@ -246,19 +246,23 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
             for (int s = threadIdx.x / 16; s < a.slots; s += (int)blockDim.x / 16) {
                 const int gs = a.cg > a.cb ? g : cblk * a.slots + s;
                 double s1 = 0.0, s2 = 0.0;
+                const double about = WHAT == 1 ? (double)a.part[(((long long)b * a.splits * a.ncb + (a.cg > a.cb ? gs * per_group : cblk)) * a.slots + s) * 2] : 0.0;
+                const double wide = a.cg > a.cb ? a.cb : a.cg;      // channels of a part
                 for (int j = threadIdx.x % 16; j < a.splits * per_group; j += 16) {
                     const int sp = j / per_group, cbk = a.cg > a.cb ? gs * per_group + j % per_group : cblk;
                     const float *p = a.part + ((((long long)b * a.splits + sp) * a.ncb + cbk) * a.slots + s) * 2;
-                    s1 += p[0];
-                    s2 += p[1];
+                    if (WHAT == 1) {        // its mean and squares, seen from the first part's mean
+                        const double values = (double)(min(a.T, (sp + 1) * a.t_run) - sp * a.t_run) * wide, off = (double)p[0] - about;
+                        s1 += values * off;
+                        s2 += (double)p[1] + values * off * off;
+                    } else s1 += p[0], s2 += p[1];
                 }
                 for (int m = 8; m > 0; m >>= 1) s1 += __shfl_xor(s1, m), s2 += __shfl_xor(s2, m);
                 s1 /= n, s2 /= n;
                 if (threadIdx.x % 16 == 0) {
                     if (WHAT == 1) {
-                        const float first = (float)*((const T *)a.x + b * a.xsb + (long long)gs * a.cg);
                         const double var = s2 - s1 * s1;
-                        stat[s][0] = (float)(first + s1);
+                        stat[s][0] = (float)(about + s1);
                         stat[s][1] = (float)(1.0 / sqrt((var > 0.0 || var != var ? var : 0.0) + (double)a.eps));
                         const bool one = a.cg > a.cb ? cblk % per_group == 0 : true;
                         if (a.stats && split == 0 && one) {
@@ -279,7 +283,7 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
             p0 = a.stats[((long long)b * a.G + g) * 2];
             p1 = a.stats[((long long)b * a.G + g) * 2 + 1];
         }
-        float s1 = 0.f, s2 = 0.f;
+        float s1 = 0.f, s2 = 0.f, shift = 0.f;
         if (mine) {
             // two tokens ahead (behind the last, the last again)
             Pack<T, VEC> xa[2], da[2];
@@ -291,6 +295,7 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
             };
             fetch(0, t0 + rp);
             fetch(1, t0 + rp + per);
+            if (WHAT == 0) shift = (float)xa[0].v[0];
             for (int t = t0 + rp; t < t1; t += per) {
                 float x[VEC], d[VEC];
                 const Pack<T, VEC> x0 = xa[0], d0 = da[0];
@@ -328,17 +333,47 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
         }
         if (WHAT == 0 || WHAT == 2) {
             // over the token phases of a unit, then over a slot's units
+            auto values = [&](int phase) { return t0 + phase < t1 ? (float)((t1 - t0 - phase + per - 1) / per * VEC) : 0.f; };
+            // (n1, a1, a2) and (n2, b1, b2), counts, means and squares about them, into the first
+            auto join = [](float n1, float &a1, float &a2, float n2, float b1, float b2) {
+                if (n2 == 0.f) return;
+                const float off = b1 - a1, part = n2 / (n1 + n2);
+                a1 = fmaf(off, part, a1);
+                a2 += b2 + off * off * (n1 * part);
+            };
+            // the run's first value of the group
+            const float ref = WHAT == 0 && mine ? (float)*((const T *)a.x + b * a.xsb + t0 * a.xst + (a.cg > a.cb ? cblk * a.cb : g * a.cg)) : 0.f;
+            if (WHAT == 0 && mine && values(rp) > 0.f) {
+                const float avg = s1 / values(rp);
+                s2 = fmaxf(fmaf(-s1, avg, s2), 0.f) + 0.f * s2;        // (an infinity or NaN stays one)
+                s1 = shift - ref + avg;
+            }
             __syncthreads();
             sh[0][threadIdx.x] = s1, sh[1][threadIdx.x] = s2;
             __syncthreads();
             if (rp == 0) {
-                for (int q = 1; q < per; ++q) s1 += sh[0][q * units + unit], s2 += sh[1][q * units + unit];
+                float have = values(0);
+                for (int q = 1; q < per; ++q) {
+                    if (WHAT == 0) {
+                        join(have, s1, s2, values(q), sh[0][q * units + unit], sh[1][q * units + unit]);
+                        have += values(q);
+                    } else s1 += sh[0][q * units + unit], s2 += sh[1][q * units + unit];
+                }
                 sh[0][unit] = s1, sh[1][unit] = s2;
+                if (WHAT == 0 && unit % su == 0) stat[slot][0] = ref;
             }
             __syncthreads();
             if ((int)threadIdx.x < a.slots) {
-                float v1 = 0.f, v2 = 0.f;
-                for (int q = 0; q < su; ++q) v1 += sh[0][threadIdx.x * su + q], v2 += sh[1][threadIdx.x * su + q];
+                float v1 = 0.f, v2 = 0.f, have = 0.f;
+                const float each = (float)(t1 - t0) * VEC;
+                for (int q = 0; q < su; ++q) {
+                    const float u1 = sh[0][threadIdx.x * su + q], u2 = sh[1][threadIdx.x * su + q];
+                    if (WHAT == 0) {
+                        join(have, v1, v2, each, u1, u2);
+                        have += each;
+                    } else v1 += u1, v2 += u2;
+                }
+                if (WHAT == 0) v1 += stat[threadIdx.x][0];
                 float *p = a.part + ((((long long)b * a.splits + split) * a.ncb + cblk) * a.slots + threadIdx.x) * 2;
                 p[0] = v1, p[1] = v2;
             }

@@ -104,6 +104,20 @@ def test_group_norm_far_from_zero_keeps_its_variance(T):
     assert rel_err(got["y"], y) <= 1000 * 2.0 ** -22
 
 
+@pytest.mark.parametrize("C,G,T,at", [(32, 2, 20000, 0), (32, 2, 20000, 7001), (4096, 1, 700, 0)])
+def test_group_norm_of_clips_that_hold_one_far_value(C, G, T, at):
+    """Values a thousand deviations off zero and one zero among them, a group's first or another: the variance is a few times one
+    deviation's square.  Granted as above: 2^-24 of 1000 deviations, over a deviation of one at least."""
+    x, dy, w, b, dt = _norm_case(2, T, C, G, 0, False, shift=0.0)
+    x += 1700.0
+    x[:, at, :: C // G] = 0.0
+    got = _run_norm(x, dy, w, b, G, 0, dt)
+    y, _, rstd, mean = R.norm_fwd(x.cpu().numpy(), w, b, G, 0)
+    assert rel_err(got["stats"][..., 0], mean[:, 0, :, 0]) <= 2.0 ** -22
+    assert rel_err(got["stats"][..., 1], rstd[:, 0, :, 0]) <= 1e-5
+    assert rel_err(got["y"], y) <= 1000 * 2.0 ** -22
+
+
 def test_group_norm_of_nothing():
     d = K.make_norm_desc(0, 3, 8, 2)
     dw, db = torch.ones(8, device=DEV), torch.ones(8, device=DEV)
