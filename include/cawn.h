@@ -407,7 +407,8 @@ typedef struct cawn_delta_desc {
 
 /* The state [B][H][K][V] fp32 (its gradient alike).  0 for an invalid descriptor, as the two below. */
 size_t cawn_delta_state_bytes(const cawn_delta_desc *d);
-/* What the forward leaves for the backward: for every run of 64 tokens the state before it, and u of every token. */
+/* What the forward leaves for the backward: for every run of 64 tokens the state before it, its u, gates and triangular inverse, and
+ * what the row's segments make of a state. */
 size_t cawn_delta_ckpt_bytes(const cawn_delta_desc *d);
 /* Scratch of either direction, 256-byte aligned. */
 size_t cawn_delta_workspace_bytes(const cawn_delta_desc *d);
@@ -421,7 +422,8 @@ size_t cawn_delta_workspace_bytes(const cawn_delta_desc *d);
  *   state_in   or NULL (zeros); state_out or NULL; they may be the same
  *   ckpt       cawn_delta_ckpt_bytes() or NULL when no backward will follow
  *   workspace  >= cawn_delta_workspace_bytes(d); calls of up to 16 tokens without ckpt use none
- * Inputs must not alias outputs (but for the state).
+ * Inputs must not alias outputs (but for the state).  A value that is not finite reaches the tokens behind it, as the formula has it, and may
+ * reach those before it in the same 64 tokens of the call.
  */
 int cawn_delta_rule_fwd(const cawn_delta_desc *d, const void *q, const void *k, const void *v, const float *decay, const float *beta,
                         const int32_t *lengths, const void *state_in, void *o, void *state_out, void *ckpt, void *workspace,

@@ -31,7 +31,7 @@ struct Args {
     float *ddecay, *dbeta, *dstate_in;
     int chunks, slabs;              // chunks of a full row; (token form) slabs of a head's columns
     int vec4;                       // state rows may be read 16 bytes at a time
-    int vecq, veco;                 // rows of q and k, of o (four values) and dO (16 bytes) may be taken several values at a time
+    int vecq, veco;                 // rows of q and k (16 bytes), of o (four values) and dO (16 bytes) may be taken several values at a time
     int vecd;                       // rows of dq, dk: four values
     // Chunked form.  Tiles of the state before each chunk (and behind the last) and of u, kept for a backward (null: not wanted): those of
     // chunk n of head bh begin bh * row + n * chunk bytes behind
@@ -68,10 +68,9 @@ __device__ inline int row_length(const Args &a, int b)
 
 int launch_token(const Args &a, bool bf16, hipStream_t s);
 int launch_system(const Args &a, bool bf16, hipStream_t s);
-int scan_held(int K, int VT, bool bf16_, int *columns);      // workgroups of the scan that a CU holds, and the column tiles of each
+int scan_held(int K, int VT, bool bf16, int *columns);                  // workgroups of the scan that a CU holds, and the column tiles of each
 int launch_scan(const Args &a, bool bf16, hipStream_t s);               // forward, behind the gates
 int launch_join(const Args &a, bool reverse, hipStream_t s);
-
 int launch_back(const Args &a, bool bf16, hipStream_t s);               // backward: the recurrence
 int launch_gradients(const Args &a, bool bf16, hipStream_t s);          // backward: every gradient but the state's
 

@@ -139,7 +139,8 @@ int cawn_delta_rule_fwd(const cawn_delta_desc *d, const void *q, const void *k, 
     hipStream_t s = (hipStream_t)stream;
     const int e = d->bf16 ? 2 : 4, w = 16 / e;
     a.vecq = a.K % 8 == 0 && a.qst % w == 0 && a.qsb % w == 0 && aligned_to(q, 16) && aligned_to(k, 16);
-    // token by token up to TOKEN_MAX
+    // token by token up to TOKEN_MAX.  (12 heads of 64, bf16: 16 tokens 19.3 us, 20.0 by chunks, 32 tokens 35.9 and 20.2; 32 rows of 32 heads of
+    // 128: 105 us and 137, 190 and 139.)
     if (a.L <= delta::TOKEN_MAX && !ckpt) return delta::launch_token(a, d->bf16, s);
     const Layout l = layout_of(a);
     if (!workspace || workspace_bytes < l.fwd || !aligned_to(workspace, 256)) return CAWN_EWORKSPACE;

@@ -12,8 +12,6 @@
 // (queries, keys that read, keys that write) the keys' two shares meet in dR.U and cancel, and what is left is the above.
 //
 // dR and dS come from the recurrence (delta_back); here every chunk is a workgroup.
-#include <stddef.h>
-
 #include "cawn_delta_mfma.hpp"
 
 namespace cawn {
@@ -24,6 +22,9 @@ namespace delta {
 // from their tiles (a tile's lane holds four rows of a column: a matrix is kept as its transpose, and read down); then, in the same
 // LDS, Z and M with q and k.
 // dq carries ddecay and takes full precision; dk of a bf16 call takes two planes (16 bits) of its operands.
+// Measured: 8 x 8,192 tokens of 12 heads of 64 in bf16: 620 us for 1.7 GB (of them U, dR, S0, S_C and dS 1.0), 2.7 TB/s.  Of a workgroup's time a third
+// is the way of its first loads and last stores, the rest splits, products and barriers in turn: neither bandwidth nor the units are full.
+// Eight waves of half the columns, not four of all: fp32, 5 x 777 tokens of 4 heads of 64 x 128 45 us, 53; this shape 620 us, 625.
 template <typename T, int NP, int KP> struct GradLds {
     static constexpr int PK = NP == 1 ? 2 : 3;          // planes of what only dk needs
     using MatU = Tile<3, 32, 64>;

@@ -168,7 +168,7 @@ __device__ inline void load_piece(const char *src, char *dst)
 
 // A matrix in LDS: N planes of ROWS x (COLS + 8) bf16.  (Eight more than COLS: rows begin on 16 bytes and not all in one bank.)
 template <int N, int ROWS, int COLS> struct Tile {
-    static constexpr int LD = COLS + 8, PLANE = ROWS * LD, BYTES = N * PLANE * 2, PLANES = N;
+    static constexpr int LD = COLS + 8, PLANE = ROWS * LD, BYTES = N * PLANE * 2;
     bf16 *p;
     // row r0 + c, steps k0 + 8g ..: the contraction runs along the row
     __device__ Frag<N> straight(int r0, int k0, int lane) const

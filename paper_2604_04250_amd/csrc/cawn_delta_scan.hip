@@ -12,15 +12,20 @@
 //
 // A wave owns 16 columns of the state, all rows of them, in result layout, which is the operand layout of the next product.  Per chunk:
 //     X = beta (V - e^G K S),  U = T X,  O^T = scale (e^G S^T Q^T + U^T P^T),  S = e^{G_C} S + K^T (e^{G_C - G} U)
-// with P made by all waves together and T fetched.
-#include <stddef.h>
-
+// with P made by all waves together and T fetched.  Four waves to 64 columns keep the state's columns in registers and share what the
+// chunk's rows give; k, q and gates of the next chunk travel meanwhile.
+//
+// Measured, bf16, whole kernels: 8 x 8,192 tokens of 12 heads of 64 (a training step's forward): delta_system 130 us, MODE 1 186, join 16, MODE 0
+// 267 (1.0 GB, of them 0.4 the checkpoint); 2 x 32,768 tokens of 32 heads of 128: 440, 1,253, 28 and 1,545 us.  What bounds MODE 0 and 1 is
+// instruction issue: the matrix units are busy a sixth to a third of the time, vector instructions (splits into planes, factors)
+// another third to half, and between the barriers of a chunk the two to four waves of a SIMD do not always have the other kind to offer.
 #include "cawn_delta_mfma.hpp"
 
 namespace cawn {
 namespace delta {
 
-// What a chunk is by itself, every chunk a workgroup: gates, the norms' factors, and T = (I + diag(beta) N)^-1.
+// What a chunk is by itself, every chunk a workgroup: gates, the norms' factors, and T = (I + diag(beta) N)^-1.  Bound by vector
+// instructions (58 % of the time at K = 64, 69 % at 128) and by the chain of the inverse, four workgroups a CU.
 template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void delta_system(const Args a)
 {
     constexpr int KS = KP / 32;
