@@ -90,3 +90,52 @@ def test_it_learns():
     model = E.Recall(8).to(DEV)
     losses = E.train(model, 120, 8, 6)
     assert np.isfinite(losses).all() and np.mean(losses[-10:]) < 0.5 * losses[0]
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_captured_and_replayed(bf16):
+    """The calls of a training step in a graph: every replay, with other work and new inputs between, gives what the calls give by themselves."""
+    K = E.K
+    dt = torch.bfloat16 if bf16 else torch.float32
+    B, L, H, Kw, V = 2, 300, 3, 64, 72
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    new = lambda *s, t=dt: torch.randn(s, generator=gen, device=DEV).to(t)  # noqa: E731
+    d = K.make_delta_desc(B, L, H, Kw, V, qk_norm=1, bf16=int(bf16))
+    n = K.make_norm_desc(B * L, 1, H * V, H, act=1, bf16=int(bf16))
+    p = K.make_dropout_desc(B * L, H * V, p=0.2, bf16=int(bf16))
+    q, k, v, do = new(B, L, H, Kw), new(B, L, H, Kw), new(B, L, H, V), new(B, L, H, V)
+    decay, beta, w, b = -new(B, L, H, t=torch.float32).abs(), new(B, L, H, t=torch.float32), new(H * V, t=torch.float32), new(H * V, t=torch.float32)
+    state, rng = new(B, H, Kw, V, t=torch.float32), torch.tensor([5, 6], device=DEV)
+    ck, ws = E._scratch(K.cawn_delta_ckpt_bytes(d), DEV), E._scratch(K.cawn_delta_workspace_bytes(d), DEV)
+    nws = E._scratch(K.cawn_group_norm_workspace_bytes(n), DEV)
+
+    def step(out):
+        K.check(K.cawn_delta_rule_fwd(d, q, k, v, decay, beta, None, state, out["o"], out["s"], ck, ws))
+        K.check(K.cawn_group_norm_fwd(n, out["o"], w, b, out["y"], out["stats"], nws))
+        K.check(K.cawn_dropout_add_fwd(p, out["y"], v, rng, out["z"]))
+        K.check(K.cawn_dropout_add_bwd(p, do, rng, out["dy"]))
+        K.check(K.cawn_group_norm_bwd(n, out["o"], w, b, out["stats"], out["dy"], out["do"], out["dw"], out["db"], nws))
+        K.check(K.cawn_delta_rule_bwd(d, q, k, v, decay, beta, None, ck, out["do"], None, out["dq"], out["dk"], out["dv"], out["da"], out["dbeta"],
+                                      out["ds"], ws))
+
+    def outputs():
+        e = torch.empty_like
+        return dict(o=e(v), s=e(state), y=e(v), z=e(v), dy=e(v), do=e(v), stats=torch.empty(B * L, H, 2, device=DEV), dw=e(w), db=e(b), dq=e(q), dk=e(k), dv=e(v),
+                    da=e(decay), dbeta=e(beta), ds=e(state))
+
+    kept = outputs()
+    step(kept)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(kept)
+    for i in range(4):
+        q.copy_(new(B, L, H, Kw)), state.mul_(0.5), rng.add_(torch.tensor([0, 1000], device=DEV))
+        want = outputs()
+        step(want)
+        for t in kept.values():
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(kept[x], want[x]) for x in want), (i, [x for x in want if not torch.equal(kept[x], want[x])])
