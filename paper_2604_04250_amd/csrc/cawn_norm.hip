@@ -10,8 +10,8 @@
 //     the sums and applies them: x is read twice.  A thread's sums are of x less its own first value, and threads and workgroups are
 //     joined as (count, mean, sum of squares about it), means within a run as differences from its first value: neither a mean of many
 //     deviations nor a first value that is far off costs the variance its digits.
-// Both are bound by memory.  Measured, forward and backward: 65,536 tokens of 12 heads of 64 in bf16 125 us for 0.50 GB (4.0 TB/s; a large copy
-// reaches 5.2); 8 x 8,191 tokens of 12 groups of 64 in fp32 364 us for 1.6 GB with the second reads (4.4 TB/s).
+// Both are bound by memory.  Measured, forward and backward: 65,536 tokens of 12 heads of 64 in bf16 115 us for 0.50 GB (4.4 TB/s; a large copy
+// reaches 5.2); 8 x 8,191 tokens of 12 groups of 64 in fp32 345 us for 1.6 GB with the second reads (4.7 TB/s).
 // Parameter gradients: every workgroup keeps its channels' sums over the rows it takes and leaves them in the workspace; a last
 // kernel adds these in a fixed order.
 #include "cawn_ops.hpp"
@@ -437,7 +437,7 @@ struct Plan {
 };
 
 // The geometry must not depend on pointers: the workspace is sized without them.  Unaligned calls take vec = 1.
-bool plan_of(const cawn_norm_desc *d, bool wide, Plan *p)
+bool plan_of(const cawn_norm_desc *d, bool wide, bool bwd, Plan *p)
 {
     if (!d || d->B < 0 || d->T < 0 || d->C <= 0 || d->groups <= 0 || d->C % d->groups || d->act < 0 || d->act > 2 || (d->bf16 & ~1)) return false;
     NormArgs &a = p->a;
@@ -466,7 +466,10 @@ bool plan_of(const cawn_norm_desc *d, bool wide, Plan *p)
         a.gblocks = (int)ceil_div(a.G, a.gb);
         p->threads = (a.lpg * a.gb * a.rb + 63) / 64 * 64;
         long long rblocks = ceil_div(a.B, a.rb);
-        long long want = 2048 / a.gblocks > 1 ? 2048 / a.gblocks : 1;
+        // as many as are there at once, eight or (backward) six to a CU: a second round would be half empty (65,536 tokens of 12 heads of 64 in
+        // bf16, forward and backward, both on 2,048, 1,536, 1,024: 123, 116, 133 us; forward alone 43, on 1,536 47 us)
+        const int groups = bwd ? 1536 : 2048;
+        long long want = groups / a.gblocks > 1 ? groups / a.gblocks : 1;
         if (want > cap) want = cap;
         a.rblocks = (int)(rblocks < want ? rblocks : want);
         p->blocks = (long long)a.rblocks * a.gblocks;
@@ -487,12 +490,17 @@ bool plan_of(const cawn_norm_desc *d, bool wide, Plan *p)
         a.ncb = a.C / a.cb;
         const int per = 256 / (a.cb / p->vec);
         p->threads = (a.cb / p->vec * per + 63) / 64 * 64;
-        long long bb = 2048 / a.ncb > 1 ? 2048 / a.ncb : 1;
+        // (8 x 8,191 tokens of 12 groups of 64 in fp32, both directions, backward on 2,048, 1,024: 364, 345 us: every
+        // workgroup leaves column sums)
+        const int groups = bwd ? 1024 : 2048;
+        long long bb = groups / a.ncb > 1 ? groups / a.ncb : 1;
         if (bb > cap) bb = cap;
         a.bblocks = (int)(a.B < bb ? a.B : bb);
         long long splits = a.bblocks > 0 ? bb / a.bblocks : 1;
         const long long useful = ceil_div(a.T, 4LL * per);          // a thread takes four tokens at least
         if (splits > useful) splits = useful;
+        if (splits > 512) splits = 512;                             // all parts are joined by everyone (one row of 16,384 x 768, fp32, both
+                                                                    // directions, parts up to 1,024, 512, 256: 168, 120, 151 us)
         if (splits < 1) splits = 1;
         a.t_run = (int)ceil_div(a.T, splits);
         if (a.t_run < 1) a.t_run = 1;
@@ -536,7 +544,7 @@ int run(const cawn_norm_desc *d, bool bwd, const void *x, const float *w, const 
         void *ws, size_t bytes, void *stream)
 {
     Plan p;
-    if (!plan_of(d, true, &p)) return CAWN_EINVAL;
+    if (!plan_of(d, true, bwd, &p)) return CAWN_EINVAL;
     hipStream_t s = (hipStream_t)stream;
     const bool grads = bwd && (dw || db);
     if (d->B == 0 || d->T == 0) {
@@ -547,7 +555,7 @@ int run(const cawn_norm_desc *d, bool bwd, const void *x, const float *w, const 
     if (!x || (bwd ? !dy || !stats : !y)) return CAWN_EINVAL;
     const size_t e = d->bf16 ? 2 : 4;
     if (!aligned_to(x, e) || !aligned_to(y, e) || !aligned_to(dy, e) || !aligned_to(dx, e) || !aligned_to(w, 4) || !aligned_to(b, 4)) return CAWN_EINVAL;
-    if (!aligned_to(x, 16) || !aligned_to(y, 16) || !aligned_to(dy, 16) || !aligned_to(dx, 16)) plan_of(d, false, &p);
+    if (!aligned_to(x, 16) || !aligned_to(y, 16) || !aligned_to(dy, 16) || !aligned_to(dx, 16)) plan_of(d, false, bwd, &p);
     const size_t need = p.part_bytes + (grads ? (size_t)p.colrows * 8 * p.a.C : 0);
     if (need > 0 && (!ws || bytes < need || !aligned_to(ws, 256))) return CAWN_EWORKSPACE;
     if (p.blocks > 0x7fffffffLL) return CAWN_EUNSUPPORTED;
@@ -566,9 +574,13 @@ extern "C" {
 
 size_t cawn_group_norm_workspace_bytes(const cawn_norm_desc *d)
 {
-    Plan wide, narrow;
-    if (!plan_of(d, true, &wide) || !plan_of(d, false, &narrow)) return 0;
-    return wide.bytes > narrow.bytes ? wide.bytes : narrow.bytes;
+    size_t most = 0;
+    for (int i = 0; i < 4; ++i) {
+        Plan p;
+        if (!plan_of(d, i & 1, i & 2, &p)) return 0;
+        most = most > p.bytes ? most : p.bytes;
+    }
+    return most;
 }
 
 int cawn_group_norm_fwd(const cawn_norm_desc *d, const void *x, const float *weight, const float *bias, void *y, float *stats, void *workspace, size_t workspace_bytes, void *stream)
