@@ -98,8 +98,8 @@ template <int NP, int KP, int MODE, int NW> struct ScanLds {
     static constexpr bool P_EARLY = NP == 1;
     static constexpr int P = P_EARLY ? TO + T_BYTES : TO, BYTES = TO + T_BYTES + (MODE == 0 && P_EARLY ? 6 * PO * 1024 : 0);
     static_assert(6 * PO * 1024 <= T_BYTES, "P in T's place");
-    // waves a SIMD that the registers are budgeted for: as many workgroups as the LDS holds, but three waves (MODE 1: four) at most
-    static constexpr int HELD = 163840 / (BYTES + (int)sizeof(Gates)) * NW / 4, MOST = MODE == 1 ? 4 : 3, WAVES = HELD > MOST ? MOST : HELD;
+    // waves a SIMD that the registers are budgeted for: as many workgroups as the LDS holds, but three waves (MODE 1 of K <= 64: four) at most
+    static constexpr int HELD = 163840 / (BYTES + (int)sizeof(Gates)) * NW / 4, MOST = MODE == 1 && KP < 128 ? 4 : 3, WAVES = HELD > MOST ? MOST : HELD;
 };
 
 template <typename T, int NP, int KP, int MODE, int NW> __global__ __launch_bounds__((64 * NW), (ScanLds<NP, KP, MODE, NW>::WAVES)) void delta_scan(const Args a)
@@ -431,7 +431,14 @@ template <typename T, int NP, int KP, int MODE, int NW> static int launch(const 
 template <typename T, int NP, int KP> static int scan_kp(const Args &a, hipStream_t s)
 {
     if (a.segments > 1) {
-        if (int r = launch<T, NP, KP, 1, 8>(a, a.s_tiles ? a.segments : a.segments - 1, a.VT + KP / 16, s)) return r;
+        // Eight waves where they divide the columns; four where half of eight would have none, and at K = 128, where they have more registers (us for
+        // eight and four: 8 x 8,192 tokens of 12 heads of 64 in bf16, training, 1,436 and 1,463; 8 x 4,096 of 8 heads of 64 x 128 275 and 240;
+        // 8 x 4,096 of 16 heads of 32, training, 687 and 649; 2 x 32,768 of 32 heads of 128 2,765 and 2,643)
+        const long long segments = a.s_tiles ? a.segments : a.segments - 1, tiles = a.VT + KP / 16;
+        int r;
+        if constexpr (KP == 128) r = launch<T, NP, KP, 1, 4>(a, segments, tiles, s);
+        else r = ceil_div(tiles, 4) % 2 ? launch<T, NP, KP, 1, 4>(a, segments, tiles, s) : launch<T, NP, KP, 1, 8>(a, segments, tiles, s);
+        if (r) return r;
         if (int r = launch_join(a, false, s)) return r;
     }
     // Where the LDS holds one workgroup of four waves a CU, eight waves take twice the columns, if there are as many (4,096 tokens of 8 heads
