@@ -16,9 +16,9 @@
 // chunk's rows give; k, q and gates of the next chunk travel meanwhile.
 //
 // Measured, bf16, whole kernels: 8 x 8,192 tokens of 12 heads of 64 (a training step's forward): delta_system 130 us, MODE 1 186, join 16, MODE 0
-// 267 (1.0 GB, of them 0.4 the checkpoint); 2 x 32,768 tokens of 32 heads of 128: 440, 1,253, 28 and 1,545 us.  What bounds MODE 0 and 1 is
-// instruction issue: the matrix units are busy a sixth to a third of the time, vector instructions (splits into planes, factors)
-// another third to half, and between the barriers of a chunk the two to four waves of a SIMD do not always have the other kind to offer.
+// 267 (1.0 GB, of them 0.4 the checkpoint); 2 x 32,768 tokens of 32 heads of 128: 420, 937, 27 and 1,421 us.  What bounds MODE 0 and 1 is
+// instruction issue: the matrix units are busy a sixth to two fifths of the time, vector instructions (splits into planes, factors)
+// another third to two thirds, and between the barriers of a chunk the two to four waves of a SIMD do not always have the other kind to offer.
 #include "cawn_delta_mfma.hpp"
 
 namespace cawn {
