@@ -149,8 +149,8 @@ __device__ inline Frag<3> t_columns(const char *T, int t, int ks, int lane)
 #pragma unroll
     for (int p = 0; p < 3; ++p) {
         const char *at = T + p * 1024 + t_slot(i % 4, 4 * (lane / 16) + i / 4) + t % 2 * 8;
-        const bf16x4 a = 2 * ks >= t ? read_down(reinterpret_cast<const bf16 *>(at + lower(2 * ks, t / 2) * 3072)) : none;
-        const bf16x4 b = read_down(reinterpret_cast<const bf16 *>(at + lower(2 * ks + 1, t / 2) * 3072));
+        const bf16x4 a = 2 * ks >= t ? read_down(reinterpret_cast<const bf16 *>(at + lower(2 * ks, t / 2) * 3 * 1024)) : none;
+        const bf16x4 b = read_down(reinterpret_cast<const bf16 *>(at + lower(2 * ks + 1, t / 2) * 3 * 1024));
         f.p[p] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     }
     return f;
