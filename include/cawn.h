@@ -432,7 +432,8 @@ int cawn_delta_rule_fwd(const cawn_delta_desc *d, const void *q, const void *k, 
 /*
  * Backward.  q .. lengths as the forward had them, ckpt as it wrote it; dO (the gradient of o), dstate_out or NULL (zeros).
  * dq, dk are summed over the value heads of a key head; ddecay is the gradient of the logarithm.  Gradients of tokens beyond
- * lengths[b] are 0.  Any of dq, dk, dv, ddecay, dbeta, dstate_in may be NULL.  The same inputs give the same bits.
+ * lengths[b] are 0.  Any of dq, dk, dv, ddecay, dbeta, dstate_in may be NULL; dstate_in may be dstate_out.  The same inputs give the same
+ * bits.
  */
 int cawn_delta_rule_bwd(const cawn_delta_desc *d, const void *q, const void *k, const void *v, const float *decay, const float *beta,
                         const int32_t *lengths, const void *ckpt, const void *dO, const void *dstate_out, void *dq, void *dk,

@@ -40,7 +40,7 @@ struct Args {
     size_t s_row, s_chunk, u_row, u_chunk;
     char *dr_tiles, *ds_tiles;      // backward: dR and dS of every chunk, in tiles
     // Segments of seg_chunks chunks; per head and chunk GATE_FLOATS gates; per head and segment the matrix A (KP x KP, row-major),
-    // the offset b and the state at its begin, in tiles
+    // the offset b and the state at its begin (backward: its gradient behind its end), in tiles
     int segments, seg_chunks;
     float *gates;
     char *t_ops;                    // per head and chunk T

@@ -45,7 +45,7 @@ template <typename T, int NP, int KP, int MODE, int NW> __global__ __launch_boun
     for (int t = 0; t < KT; ++t) {
         S[t] = zero;
         if (MODE == 1 || !mine) continue;
-        if (seg < a.segments - 1) S[t] = *reinterpret_cast<const f32x4 *>(a.seg_s + (((size_t)bh * a.segments + seg) * KT * a.VT + (size_t)t * a.VT + ct) * 1024 + lane * 16);
+        if (a.segments > 1) S[t] = *reinterpret_cast<const f32x4 *>(a.seg_s + (((size_t)bh * a.segments + seg) * KT * a.VT + (size_t)t * a.VT + ct) * 1024 + lane * 16);
         else if (a.dstate_out && v < a.V) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)

@@ -1,5 +1,7 @@
 // Gated delta rule by chunks: the states at the segments' begins (forward, S' = A S + b) or, for the gradient, behind their ends
-// (S' = A^T S + b, from the last segment to the first).
+// (S' = A^T S + b, from the last segment to the first).  The first of the chain, which is the caller's, is written down with the others: the pass
+// over the segments takes all of them from here, because the workgroup that stores the caller's other end does not wait for the one
+// that begins with this, and both may be one buffer.
 //
 // A workgroup takes 16 columns of a head's state: the segments are a chain, and what counts is the time of one link.  Wave w owns row
 // tiles w and w + 4; it splits its own rows of A (fetched a link ahead) and its own tiles of the new state, and the waves pass each other
@@ -66,6 +68,14 @@ template <int KP, bool REV> __global__ __launch_bounds__(256) void delta_join(co
         for (int r = 0; r < 4; ++r) {
             const int f = 16 * t + 4 * g + r;
             if (begin && f < a.K && v < a.V) S[o][r] = begin[((long long)bh * a.K + f) * a.V + v];
+        }
+    }
+    {
+        char *to = a.seg_s + ((size_t)bh * a.segments + (REV ? links : 0)) * st + lane * 16;
+#pragma unroll
+        for (int o = 0; o < OWN; ++o) {
+            const int t = w + 4 * o;
+            if (t < KT) *reinterpret_cast<f32x4 *>(to + ((size_t)t * a.VT + vt) * 1024) = S[o];
         }
     }
     put(0);

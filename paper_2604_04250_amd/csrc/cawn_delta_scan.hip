@@ -132,7 +132,7 @@ template <typename T, int NP, int KP, int MODE, int NW> __global__ __launch_boun
 #pragma unroll
                 for (int r = 0; r < 4; ++r) S[t][r] = 4 * g + r == c ? 1.f : 0.f;
             }
-        } else if (of_v && seg > 0) S[t] = *reinterpret_cast<const f32x4 *>(a.seg_s + (((size_t)bh * a.segments + seg) * KT * a.VT + (size_t)t * a.VT + ct) * 1024 + lane * 16);
+        } else if (of_v && a.segments > 1) S[t] = *reinterpret_cast<const f32x4 *>(a.seg_s + (((size_t)bh * a.segments + seg) * KT * a.VT + (size_t)t * a.VT + ct) * 1024 + lane * 16);
         else if (of_v && a.state_in && v < a.V) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
