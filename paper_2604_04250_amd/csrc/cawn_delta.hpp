@@ -33,7 +33,7 @@ struct Args {
     int vec4;                       // state rows may be read 16 bytes at a time
     int vecq, veco;                 // rows of q and k (16 bytes), of o (four values) and dO (16 bytes) may be taken several values at a time
     int vecd;                       // rows of dq, dk: four values
-    // Chunked form.  Tiles of the state before each chunk (and behind the last) and of u, kept for a backward (null: not wanted): those of
+    // Chunked form.  Tiles of the state before each chunk and of u, kept for a backward (null: not wanted): those of
     // chunk n of head bh begin bh * row + n * chunk bytes behind
     int VT;                         // tiles of 16 value columns
     char *s_tiles, *u_tiles;

@@ -53,7 +53,7 @@ int check(const cawn_delta_desc *d, Args *a)
     return CAWN_OK;
 }
 
-// Byte offsets.  Kept for the backward: states [B H][chunks + 1] and u [B H][chunks] in tiles, gates, T, A of the segments.
+// Byte offsets.  Kept for the backward: states and u [B H][chunks] in tiles, gates, T, A of the segments.
 // Scratch of the forward: gates, A and T (unless kept), b and the begins of the segments; of the backward: dR and dS of every
 // chunk, b and the ends of the segments.
 struct Layout { size_t u, gates, t, a, ckpt; size_t fwd_gates, fwd_a, fwd_t, b, s, fwd; size_t ds, rb, rs, bwd; };
@@ -63,7 +63,7 @@ Layout layout_of(const Args &a)
     const Sizes z(a.K, a.V);
     const size_t heads = (size_t)a.B * a.H, all = heads * a.chunks, segs = a.segments > 1 ? heads * a.segments : 0;
     const size_t gates = (all * delta::GATE_FLOATS * 4 + 1023) / 1024 * 1024, am = segs * z.KP * z.KP * 4, states = segs * z.st * 1024;
-    l.u = heads * (a.chunks + 1) * z.st * 1024;
+    l.u = all * z.st * 1024;
     l.gates = l.u + all * z.ut * 1024;
     l.t = l.gates + gates;
     l.a = l.t + all * delta::OPERAND_BYTES;
@@ -86,7 +86,7 @@ void keep(Args *a, const Layout &l, void *ckpt)
 {
     const Sizes z(a->K, a->V);
     char *p = (char *)ckpt;
-    a->s_tiles = p, a->s_chunk = (size_t)z.st * 1024, a->s_row = (size_t)(a->chunks + 1) * a->s_chunk;
+    a->s_tiles = p, a->s_chunk = (size_t)z.st * 1024, a->s_row = (size_t)a->chunks * a->s_chunk;
     a->u_tiles = p + l.u, a->u_chunk = (size_t)z.ut * 1024, a->u_row = (size_t)a->chunks * a->u_chunk;
     a->gates = (float *)(p + l.gates), a->t_ops = p + l.t, a->seg_a = p + l.a;
 }

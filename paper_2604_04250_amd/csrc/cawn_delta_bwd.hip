@@ -7,9 +7,12 @@
 //     dQ  = scale e^G dO S0^T + Z K
 //     dK  = -beta e^G dR S0^T + M K + Z^T Q + M^T K + e^{G_C - G} U dS^T
 //     dbeta_i = dR_i . U_i / beta_i
-//     ddecay_t = sum_{i >= t, in the chunk} (q_i . dq_i - v_i . dv_i) + <dS, S_C>
-// The last line: a decay scales all that a later query reads and all that came before it; summed over the places where e^{G_i} stands
-// (queries, keys that read, keys that write) the keys' two shares meet in dR.U and cancel, and what is left is the above.
+//     ddecay_t = sum_{i >= t} a_i + sum_{j < t} b_j + sum_{i >= t > j} (Z_ij q_i . k_j + M_ij k_i . k_j) + e^{G_C} <dS, S0>
+//     a_i = q_i . (scale e^G dO S0^T)_i - k_i . (beta e^G dR S0^T)_i,   b_j = k_j . (e^{G_C - G} U dS^T)_j
+// The last: a decay scales all that passes from before its token to it and behind it, from the chunk's begin or a token in it to its end or a
+// token in it.  Every term holds the factors of the decays between its ends, the token's own among them, and the sum has its digits however little is
+// left of what came before.  (The same sum is that of q.dq - v.dv over the tokens behind, and <dS, S_C>: there the terms do not shrink with the decay, cancel,
+// and leave their rounding, 1e-2 of the gradient at a decay of -8 and nothing but rounding from -15 on.)
 //
 // dR and dS come from the recurrence (delta_back); here every chunk is a workgroup.
 #include "cawn_delta_mfma.hpp"
@@ -21,10 +24,11 @@ namespace delta {
 // and wave 4 + w rows 16 w .. of them, half of the columns each.  First everything that runs over the value columns, 32 at a time, with U, dR, S0 and dS in LDS as they come
 // from their tiles (a tile's lane holds four rows of a column: a matrix is kept as its transpose, and read down); then, in the same
 // LDS, Z and M with q and k.
-// dq carries ddecay and takes full precision; dk of a bf16 call takes two planes (16 bits) of its operands.
+// dq takes full precision; dk of a bf16 call takes two planes (16 bits) of its operands.
 // Measured: 8 x 8,192 tokens of 12 heads of 64 in bf16: 620 us for 1.7 GB (of them U, dR, S0, S_C and dS 1.0), 2.7 TB/s.  Of a workgroup's time a third
 // is the way of its first loads and last stores, the rest splits, products and barriers in turn: neither bandwidth nor the units are full.
 // Eight waves of half the columns, not four of all: fp32, 5 x 777 tokens of 4 heads of 64 x 128 45 us, 53; this shape 620 us, 625.
+constexpr int WLD = CHUNK + 4;          // (four rows apart begin in other banks)
 template <typename T, int NP, int KP> struct GradLds {
     static constexpr int PK = NP == 1 ? 2 : 3;          // planes of what only dk needs
     using MatU = Tile<3, 32, 64>;
@@ -35,6 +39,7 @@ template <typename T, int NP, int KP> struct GradLds {
     using MatQ = Tile<NP, CHUNK, KP>;
     using MatZ = Tile<3, CHUNK, CHUNK>;
     using MatM = Tile<PK, CHUNK, CHUNK>;
+    static_assert(MatZ::BYTES >= (CHUNK * WLD + CHUNK / 4 * CHUNK + 4 * CHUNK) * 4, "wl, its sums and the norms' in Z's place");
     static constexpr int FIRST = MatU::BYTES + MatR::BYTES + MatS::BYTES + MatD::BYTES + MatO::BYTES;
     static constexpr int SECOND = 2 * MatQ::BYTES + MatZ::BYTES + MatM::BYTES;
     static constexpr int BYTES = FIRST > SECOND ? FIRST : SECOND;
@@ -81,7 +86,7 @@ template <typename T, int NP, int KP, bool SHARED> __global__ __launch_bounds__(
     constexpr int KT = KP / 16, KH = KT / 2, PK = L::PK, OWN = (KT + 3) / 4, NT = 512;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ Gates G;
-    __shared__ float qdq[2][CHUNK], vdv[2][CHUNK], udr[2][CHUNK], part[8];
+    __shared__ float reads[2][CHUNK], writes[2][CHUNK], udr[2][CHUNK], part[8];       // a, b, dR.U; shares of <dS, S0>
     const int blk = blockIdx.x, n = blk % a.chunks, bk = blk / a.chunks, hk = bk % a.Hk, b = bk / a.Hk, rep = a.H / a.Hk;
     const int len = row_length(a, b), t0 = n * CHUNK, rows = min(CHUNK, len - t0), all = min(CHUNK, a.L - t0);
     const long long qat = b * a.qsb + t0 * a.qst + (long long)hk * a.K;
@@ -139,27 +144,22 @@ template <typename T, int NP, int KP, bool SHARED> __global__ __launch_bounds__(
         for (int t = 0; t < KH; ++t) A1[t] = A2[t] = A3[t] = zero;
 #pragma unroll
         for (int t = 0; t < 2; ++t) zt[t] = mt[t] = zero;
-        float inner = 0.f;                      // <dS, S_C>
-        float sv[4] = {0.f, 0.f, 0.f, 0.f}, su[4] = {0.f, 0.f, 0.f, 0.f};
-        // A step's loads are all under way before the first is wanted: tiles, and (from where something is, and dropped below) v and dO.
+        float inner = 0.f;                      // <dS, S0>
+        float su[4] = {0.f, 0.f, 0.f, 0.f};
+        // A step's loads are all under way before the first is wanted: tiles, and (from where something is, and dropped below) dO.
         // Waves w and 4 + w: row tile w of U and dR; row tiles w, w + 4 of the states; a column tile each
-        f32x4 tu, tr, ts[OWN], te[OWN], td[OWN];
-        T tv[4];
+        f32x4 tu, tr, ts[OWN], td[OWN];
         RowsAhead<T, NP, 32, NT> to;
         auto ahead = [&](int v0) {
-            const int vt = min(v0 / 16 + half, a.VT - 1), v = min(16 * vt + c, a.V - 1);
+            const int vt = min(v0 / 16 + half, a.VT - 1);
             tu = *reinterpret_cast<const f32x4 *>(up + ((size_t)w * a.VT + vt) * 1024 + lane * 16);
             tr = *reinterpret_cast<const f32x4 *>(rp + ((size_t)w * a.VT + vt) * 1024 + lane * 16);
 #pragma unroll
             for (int o = 0; o < OWN; ++o) {
                 const size_t at = ((size_t)min(w + 4 * o, KT - 1) * a.VT + vt) * 1024 + lane * 16;
                 ts[o] = *reinterpret_cast<const f32x4 *>(sp + at);
-                te[o] = *reinterpret_cast<const f32x4 *>(sp + a.s_chunk + at);
                 td[o] = *reinterpret_cast<const f32x4 *>(dp + at);
             }
-            const T *vp = (const T *)a.v + b * a.vsb + (long long)t0 * a.vst + (long long)h * a.V + v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) tv[e] = vp[min(16 * w + 4 * g + e, rows - 1) * a.vst];
             to.load(tid, (const T *)a.dO + b * a.osb + (long long)t0 * a.ost + (long long)h * a.V + v0, a.ost, rows, min(32, a.V - v0), a.veco);
         };
         // (the gates first: what is loaded before them would have to come before they do)
@@ -186,7 +186,6 @@ template <typename T, int NP, int KP, bool SHARED> __global__ __launch_bounds__(
                     const int i = 16 * w + 4 * g + e;
                     su[e] += u[e] * r[e];
                     const float dv = G.beta[i] * r[e];
-                    sv[e] += v < a.V && i < rows ? (float)tv[e] * dv : 0.f;
                     if (a.dv && v < a.V && i < all) dvp[i * a.vst] = (T)(i < rows ? dv : 0.f);
                 }
 #pragma unroll
@@ -197,7 +196,7 @@ template <typename T, int NP, int KP, bool SHARED> __global__ __launch_bounds__(
                     put_column(st, 16 * half + c, 16 * t + 4 * g, s);
                     put_column(dt, 16 * half + c, 16 * t + 4 * g, d);
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) inner += d[x] * te[o][x];
+                    for (int x = 0; x < 4; ++x) inner += d[x] * s[x];
                 }
             }
             to.put_plain(tid, ot, rows, min(32, a.V - v0));
@@ -243,8 +242,8 @@ template <typename T, int NP, int KP, bool SHARED> __global__ __launch_bounds__(
         ka.load(tid, (const T *)a.k + qat, a.qst, rows, a.K, a.vecq);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float s = row_sum(sv[e]), t = row_sum(su[e]);
-            if (c == 0) vdv[half][16 * w + 4 * g + e] = s, udr[half][16 * w + 4 * g + e] = t;
+            const float t = row_sum(su[e]);
+            if (c == 0) udr[half][16 * w + 4 * g + e] = t;
         }
 #pragma unroll
         for (int m = 32; m > 0; m >>= 1) inner += __shfl_xor(inner, m);
@@ -270,12 +269,42 @@ template <typename T, int NP, int KP, bool SHARED> __global__ __launch_bounds__(
         }
         // y = r dx^ of the norm's x^ = r x:  yq = scale rq e^G A1 + Z k,  yk = rk (e^{G_C - G} A3 - beta e^G A2) + M k + Z^T q + M^T k
         const float f1 = sq * eg, f2 = bk * eg, f3 = rk * G.ed[i];
-#pragma unroll
-        for (int t = 0; t < KH; ++t) {
-            A1[t] *= f1;
-            A2[t] = f3 * A3[t] + f2 * A2[t];
-        }
         __syncthreads();
+        anew();
+        // Z o Q K^T + M o K K^T, of which ddecay takes what lies below; a and b
+        f32x4 wt[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            if (own(e) > w) continue;
+            f32x4 qk = zero, kk = zero;
+#pragma unroll
+            for (int ks = 0; ks < KP / 32; ++ks) {
+                const Frag<NP> kj = km.straight(16 * own(e), 32 * ks, lane);
+                qk = mma<3>(kj, qm.straight(16 * w, 32 * ks, lane), qk);
+                kk = mma<3>(kj, km.straight(16 * w, 32 * ks, lane), kk);
+            }
+            wt[e] = zt[e] * qk + mt[e] * kk;
+        }
+        {
+            float sa = 0.f, sb = 0.f;
+#pragma unroll
+            for (int t = 0; t < KH; ++t) {
+                float xq[4], xk[4];
+                row_of(qm, 16 * w + c, 16 * (half * KH + t) + 4 * g, xq);
+                row_of(km, 16 * w + c, 16 * (half * KH + t) + 4 * g, xk);
+                A1[t] *= f1, A2[t] *= f2, A3[t] *= f3;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    sa = fmaf(xq[r], A1[t][r], sa);
+                    sa = fmaf(xk[r], A2[t][r], sa);
+                    sb = fmaf(xk[r], A3[t][r], sb);
+                }
+                A2[t] += A3[t];
+            }
+            sa += __shfl_xor(sa, 16), sb += __shfl_xor(sb, 16);
+            sa += __shfl_xor(sa, 32), sb += __shfl_xor(sb, 32);
+            if (g == 0) reads[half][16 * w + c] = sa, writes[half][16 * w + c] = sb;
+        }
         anew();
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
@@ -302,44 +331,58 @@ template <typename T, int NP, int KP, bool SHARED> __global__ __launch_bounds__(
                 }
             }
         }
+#pragma unroll
+        for (int t = 0; t < KH; ++t) {
+            dq[t] = SHARED ? dq[t] + A1[t] : A1[t];
+            dk[t] = SHARED ? dk[t] + A2[t] : A2[t];
+        }
+        __syncthreads();                        // nobody wants Z any more
         anew();
-        // q^ . dq^ of this head = q . yq
-        {
-            float s = 0.f;
+        // wl[j][i], and the sums of four rows j of it (rows beyond i, which are not written, are dropped below)
+        float *wl = (float *)zm.p, *quads = wl + CHUNK * WLD;
 #pragma unroll
-            for (int t = 0; t < KH; ++t) {
-                float x[4];
-                row_of(qm, 16 * w + c, 16 * (half * KH + t) + 4 * g, x);
+        for (int e = 0; e < 2; ++e) {
+            if (own(e) > w) continue;
+            const int j0 = 16 * own(e) + 4 * g;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) s = fmaf(x[r], A1[t][r], s);
-                dq[t] = SHARED ? dq[t] + A1[t] : A1[t];
-                dk[t] = SHARED ? dk[t] + A2[t] : A2[t];
-            }
-            s += __shfl_xor(s, 16);
-            s += __shfl_xor(s, 32);
-            if (g == 0) qdq[half][16 * w + c] = s;
+            for (int r = 0; r < 4; ++r) wl[(j0 + r) * WLD + 16 * w + c] = wt[e][r];
+            quads[j0 / 4 * CHUNK + 16 * w + c] = (wt[e][0] + wt[e][1]) + (wt[e][2] + wt[e][3]);
         }
         __syncthreads();
-        if (tid < CHUNK) {
-            const int i = tid;
-            float s = i < rows ? (qdq[0][i] + qdq[1][i]) - (vdv[0][i] + vdv[1][i]) : 0.f;
+        {
+            // a wave takes eight tokens t, a lane one i: what passes from before t to i, or (i < t) from i to the chunk's end
+            const int i = lane, first = 8 * wave;
+            const float read = reads[0][i] + reads[1][i], write = writes[0][i] + writes[1][i];
+            float before = 0.f, x[8];
+            for (int j = 0; j < 2 * wave; ++j) before += quads[j * CHUNK + i];
 #pragma unroll
-            for (int m = 1; m < 64; m <<= 1) {          // sum over the tokens behind
-                const float o = __shfl_down(s, m);
-                if (i + m < 64) s += o;
+            for (int e = 0; e < 8; ++e) {
+                x[e] = i >= rows ? 0.f : i >= first + e ? before + read : write;
+                before += wl[(first + e) * WLD + i];
             }
-            s += ((part[0] + part[1]) + (part[2] + part[3])) + ((part[4] + part[5]) + (part[6] + part[7]));
-            if (i < all) {
-                const long long at = ((long long)b * a.L + t0 + i) * a.H + h;
-                // (a complete forgetting hangs on nothing; the sum would leave its rounding)
-                if (a.ddecay) a.ddecay[at] = i < rows && !(a.decay[at] < DECAY_MIN) ? s : 0.f;
-                if (a.dbeta) a.dbeta[at] = i < rows ? (udr[0][i] + udr[1][i]) / G.beta[i] : 0.f;
+            // eight sums over the lanes: halves of them change hands, so that a lane is left with one
+#pragma unroll
+            for (int m = 32, n = 4; n > 0; m >>= 1, n >>= 1) {
+#pragma unroll
+                for (int e = 0; e < n; ++e) {
+                    const float give = i & m ? x[e] : x[e + n];
+                    x[e] = (i & m ? x[e + n] : x[e]) + __shfl_xor(give, m);
+                }
             }
+            x[0] += __shfl_xor(x[0], 4);
+            x[0] += __shfl_xor(x[0], 2);
+            x[0] += __shfl_xor(x[0], 1);
+            const int t = first + (lane >> 3);          // bits 5, 4, 3 of the lane: which half was kept
+            const float whole = ((part[0] + part[1]) + (part[2] + part[3])) + ((part[4] + part[5]) + (part[6] + part[7]));
+            const long long at = ((long long)b * a.L + t0 + t) * a.H + h;
+            // (a complete forgetting hangs on nothing)
+            if (a.ddecay && lane % 8 == 0 && t < all) a.ddecay[at] = t < rows && !(a.decay[at] < DECAY_MIN) ? fmaf(G.eg[CHUNK - 1], whole, x[0]) : 0.f;
         }
+        if (a.dbeta && tid < all) a.dbeta[((long long)b * a.L + t0 + tid) * a.H + h] = tid < rows ? (udr[0][tid] + udr[1][tid]) / G.beta[tid] : 0.f;
     }
     // through the norm, and out: dx = r (dx^ - x^ (x^ . dx^)) = y - r^2 x (x . y)
     const int i = 16 * w + c, f0 = 16 * KH * half + 4 * g;
-    float (*xdx)[2][CHUNK] = reinterpret_cast<float (*)[2][CHUNK]>(zm.p);       // (nobody wants Z any more)
+    float (*xdx)[2][CHUNK] = reinterpret_cast<float (*)[2][CHUNK]>((float *)zm.p + CHUNK * WLD + CHUNK / 4 * CHUNK);      // (behind wl and its sums)
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         float s = 0.f;

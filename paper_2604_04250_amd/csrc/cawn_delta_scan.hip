@@ -409,8 +409,6 @@ template <typename T, int NP, int KP, int MODE, int NW> __global__ __launch_boun
     }
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
-        if (a.s_tiles && n1 == nb && (n1 > n0 || nb == 0) && (nb > 0 || seg == 0))
-            *reinterpret_cast<f32x4 *>(a.s_tiles + bh * a.s_row + nb * a.s_chunk + ((size_t)t * a.VT + ct) * 1024 + lane * 16) = S[t];
         if (seg == a.segments - 1 && a.state_out && v < a.V) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
