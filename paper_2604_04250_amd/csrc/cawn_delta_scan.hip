@@ -89,23 +89,24 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
     }
 }
 
-// The scan's LDS: k, q (MODE 0); T; P's operands.  With one plane to an operand P has a place of its own and is made ahead of the products
-// with the state; with three it would leave room for one workgroup a CU, so P is made where T was, for one more barrier (4,096 tokens of
-// 12 heads of 64 in fp32: 90 us, against 99 in a place of its own; bf16, 2 x 32,768 tokens of 32 heads of 128: 3,131 us in T's place, 3,049 in its own).
+// The scan's LDS: k, q (MODE 0); T; P's operands.  P has a place of its own and is made ahead of the products with the state where that costs no
+// workgroup of a CU; elsewhere it is made where T was, for one more barrier.  (In T's place and in its own, us: one workgroup a CU either way, 4,096 tokens
+// of 8 heads of 128 in fp32 172 and 167; two, 2 x 32,768 of 32 heads of 128 in bf16 2,743 and 2,683; three and two, 8 x 8,192 of 12 heads of 64 in
+// bf16, training, 1,441 and 1,542, but 4 x 16,384 of 8 heads, forward, 355 and 340; two and one, 4,096 of 12 heads of 64 in fp32 90 and 95.)
 template <int NP, int KP, int MODE, int NW> struct ScanLds {
-    static constexpr int PO = NP == 1 ? 2 : 3;
     static constexpr int KB = Tile<NP, CHUNK, KP>::BYTES, TO = MODE == 0 ? 2 * KB : KB;
-    static constexpr bool P_EARLY = NP == 1;
-    static constexpr int P = P_EARLY ? TO + T_BYTES : TO, BYTES = TO + T_BYTES + (MODE == 0 && P_EARLY ? 6 * PO * 1024 : 0);
-    static_assert(6 * PO * 1024 <= T_BYTES, "P in T's place");
     // waves a SIMD that the registers are budgeted for: as many workgroups as the LDS holds, but three waves (MODE 1 of K <= 64: four) at most
-    static constexpr int HELD = 163840 / (BYTES + (int)sizeof(Gates)) * NW / 4, MOST = MODE == 1 && KP < 128 ? 4 : 3, WAVES = HELD > MOST ? MOST : HELD;
+    static constexpr int MOST = MODE == 1 && KP < 128 ? 4 : 3;
+    static constexpr int waves(int bytes) { return 163840 / (bytes + (int)sizeof(Gates)) * NW / 4 > MOST ? MOST : 163840 / (bytes + (int)sizeof(Gates)) * NW / 4; }
+    static constexpr bool P_EARLY = MODE == 0 && waves(TO + 2 * T_BYTES) == waves(TO + T_BYTES);
+    static constexpr int P = P_EARLY ? TO + T_BYTES : TO, BYTES = P + T_BYTES;
+    static constexpr int WAVES = waves(BYTES);
 };
 
 template <typename T, int NP, int KP, int MODE, int NW> __global__ __launch_bounds__((64 * NW), (ScanLds<NP, KP, MODE, NW>::WAVES)) void delta_scan(const Args a)
 {
     using L = ScanLds<NP, KP, MODE, NW>;
-    constexpr int KS = KP / 32, KT = KP / 16, PO = L::PO, NT = 64 * NW;
+    constexpr int KS = KP / 32, KT = KP / 16, NT = 64 * NW;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ Gates G;
     const Tile<NP, CHUNK, KP> k{(bf16 *)lds}, q{(bf16 *)(lds + L::KB)};
@@ -183,10 +184,10 @@ template <typename T, int NP, int KP, int MODE, int NW> __global__ __launch_boun
                     }
                 }
             }
-            Frag<PO> f;
-            split_tiles<PO>(pt[0], pt[1], f);
+            Frag<3> f;
+            split_tiles<3>(pt[0], pt[1], f);
 #pragma unroll
-            for (int e = 0; e < PO; ++e) pf[(id * PO + e) * 64 + lane] = f.p[e];
+            for (int e = 0; e < 3; ++e) pf[(id * 3 + e) * 64 + lane] = f.p[e];
         }
     };
     if (n0 < n1) ahead(n0);
@@ -264,13 +265,10 @@ template <typename T, int NP, int KP, int MODE, int NW> __global__ __launch_boun
                 for (int t = 0; t < 4; ++t) O[t] = zero;
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    Frag<PO> s;
                     Frag<NP> f[4];
 #pragma unroll
-                    for (int e = 0; e < PO; ++e) s.p[e] = sf[ks].p[e];
-#pragma unroll
                     for (int t = 0; t < 4; ++t) f[t] = q.tiled(16 * t, 32 * ks, lane);
-                    mma_each<PO>(s, f, O);
+                    mma_each<3>(sf[ks], f, O);
                 }
 #pragma unroll
                 for (int t = 0; t < 4; ++t) O[t] *= G.eg[16 * t + c];
@@ -347,26 +345,26 @@ template <typename T, int NP, int KP, int MODE, int NW> __global__ __launch_boun
         if (MODE == 0) {
             if (!L::P_EARLY) __syncthreads();   // P's operands
             anew();
-            Frag<PO> uf[2];
+            Frag<3> uf[2];
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks) split_tiles<PO>(U[2 * ks], U[2 * ks + 1], uf[ks]);
+            for (int ks = 0; ks < 2; ++ks) split_tiles<3>(U[2 * ks], U[2 * ks + 1], uf[ks]);
             const int all = min(CHUNK, a.L - n * CHUNK);
             // a lane's place among rows of o, in bytes
             const bool whole = rows == CHUNK && a.veco && 16 * ct + 16 <= a.V && ost < (1 << 22);
             const uint32_t olane = ((uint32_t)c * (uint32_t)ost + 4 * g) * sizeof(T);
             T *op = (T *)a.o + b * a.osb + (long long)n * CHUNK * ost + (long long)h * a.V + 16 * ct;
             {
-                Frag<PO> f[4], f2[2];
+                Frag<3> f[4], f2[2];
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
-                    for (int e = 0; e < PO; ++e) f[t].p[e] = pf[(lower(t, 0) * PO + e) * 64 + lane];
-                mma_each<PO>(uf[0], f, O);
+                    for (int e = 0; e < 3; ++e) f[t].p[e] = pf[(lower(t, 0) * 3 + e) * 64 + lane];
+                mma_each<3>(uf[0], f, O);
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int e = 0; e < PO; ++e) f2[t].p[e] = pf[(lower(2 + t, 1) * PO + e) * 64 + lane];
-                mma_each<PO>(uf[1], f2, O + 2);
+                    for (int e = 0; e < 3; ++e) f2[t].p[e] = pf[(lower(2 + t, 1) * 3 + e) * 64 + lane];
+                mma_each<3>(uf[1], f2, O + 2);
             }
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
