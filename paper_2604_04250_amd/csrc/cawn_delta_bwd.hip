@@ -24,21 +24,19 @@ namespace delta {
 // and wave 4 + w rows 16 w .. of them, half of the columns each.  First everything that runs over the value columns, 32 at a time, with U, dR, S0 and dS in LDS as they come
 // from their tiles (a tile's lane holds four rows of a column: a matrix is kept as its transpose, and read down); then, in the same
 // LDS, Z and M with q and k.
-// dq takes full precision; dk of a bf16 call takes two planes (16 bits) of its operands.
 // Measured: 8 x 8,192 tokens of 12 heads of 64 in bf16: 620 us for 1.7 GB (of them U, dR, S0, S_C and dS 1.0), 2.7 TB/s.  Of a workgroup's time a third
 // is the way of its first loads and last stores, the rest splits, products and barriers in turn: neither bandwidth nor the units are full.
 // Eight waves of half the columns, not four of all: fp32, 5 x 777 tokens of 4 heads of 64 x 128 45 us, 53; this shape 620 us, 625.
 constexpr int WLD = CHUNK + 4;          // (four rows apart begin in other banks)
 template <typename T, int NP, int KP> struct GradLds {
-    static constexpr int PK = NP == 1 ? 2 : 3;          // planes of what only dk needs
     using MatU = Tile<3, 32, 64>;
-    using MatR = Tile<PK, 32, 64>;
+    using MatR = Tile<3, 32, 64>;
     using MatS = Tile<3, 32, KP>;
-    using MatD = Tile<PK, 32, KP>;
+    using MatD = Tile<3, 32, KP>;
     using MatO = Tile<NP, CHUNK, 32>;
     using MatQ = Tile<NP, CHUNK, KP>;
     using MatZ = Tile<3, CHUNK, CHUNK>;
-    using MatM = Tile<PK, CHUNK, CHUNK>;
+    using MatM = Tile<3, CHUNK, CHUNK>;
     static_assert(MatZ::BYTES >= (CHUNK * WLD + CHUNK / 4 * CHUNK + 4 * CHUNK) * 4, "wl, its sums and the norms' in Z's place");
     static constexpr int FIRST = MatU::BYTES + MatR::BYTES + MatS::BYTES + MatD::BYTES + MatO::BYTES;
     static constexpr int SECOND = 2 * MatQ::BYTES + MatZ::BYTES + MatM::BYTES;
@@ -83,7 +81,7 @@ __device__ inline float row_sum(float x)
 template <typename T, int NP, int KP, bool SHARED> __global__ __launch_bounds__(512, (SHARED ? 2 : GradLds<T, NP, KP>::WAVES)) void delta_gradients(const Args a)
 {
     using L = GradLds<T, NP, KP>;
-    constexpr int KT = KP / 16, KH = KT / 2, PK = L::PK, OWN = (KT + 3) / 4, NT = 512;
+    constexpr int KT = KP / 16, KH = KT / 2, OWN = (KT + 3) / 4, NT = 512;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ Gates G;
     __shared__ float reads[2][CHUNK], writes[2][CHUNK], udr[2][CHUNK], part[8];       // a, b, dR.U; shares of <dS, S0>
@@ -203,7 +201,7 @@ template <typename T, int NP, int KP, bool SHARED> __global__ __launch_bounds__(
             __syncthreads();
             anew();
             const Frag<NP> o = ot.straight(16 * w, 0, lane);
-            const Frag<PK> r = rt.straight_down(0, 16 * w, lane);
+            const Frag<3> r = rt.straight_down(0, 16 * w, lane);
             // before their factors: Z^T and M^T, rows j and column i = c of row tile w; dO S0^T and the like, rows f and column i = c
             // (a tile at a time: there are four waves a SIMD to fill the pauses, but no registers)
 #pragma unroll
@@ -211,7 +209,7 @@ template <typename T, int NP, int KP, bool SHARED> __global__ __launch_bounds__(
                 if (own(e) > w) continue;
                 const Frag<3> uj[1] = {ut.straight_down(0, 16 * own(e), lane)};
                 mma_each<3>(uj, o, zt + e);
-                mma_each<PK>(uj, r, mt + e);
+                mma_each<3>(uj, r, mt + e);
                 __builtin_amdgcn_sched_barrier(0);
             }
             anew();
@@ -219,19 +217,14 @@ template <typename T, int NP, int KP, bool SHARED> __global__ __launch_bounds__(
             for (int t = 0; t < KH; ++t) {
                 const Frag<3> f[1] = {st.straight_down(0, 16 * (half * KH + t), lane)};
                 mma_each<3>(f, o, A1 + t);
-                mma_each<PK>(f, r, A2 + t);
+                mma_each<3>(f, r, A2 + t);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            Frag<PK> u;
-            {
-                const Frag<3> u3 = ut.straight_down(0, 16 * w, lane);
-#pragma unroll
-                for (int p = 0; p < PK; ++p) u.p[p] = u3.p[p];
-            }
+            const Frag<3> u = ut.straight_down(0, 16 * w, lane);
 #pragma unroll
             for (int t = 0; t < KH; ++t) {
-                const Frag<PK> d[1] = {dt.straight_down(0, 16 * (half * KH + t), lane)};
-                mma_each<PK>(d, u, A3 + t);
+                const Frag<3> d[1] = {dt.straight_down(0, 16 * (half * KH + t), lane)};
+                mma_each<3>(d, u, A3 + t);
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (v0 + 32 < a.V) ahead(v0 + 32);
@@ -310,8 +303,7 @@ template <typename T, int NP, int KP, bool SHARED> __global__ __launch_bounds__(
         for (int ks = 0; ks < 2; ++ks) {
             constexpr int AT = KH < 4 ? KH : 4;
             const bool left = 2 * ks <= w, right = 2 * ks + 1 >= w;
-            Frag<3> zf, zd;
-            Frag<PK> mf, md;
+            Frag<3> zf, zd, mf, md;
             if (left) zf = zm.straight(16 * w, 32 * ks, lane), mf = mm.straight(16 * w, 32 * ks, lane);
             if (right) zd = zm.straight_down(32 * ks, 16 * w, lane), md = mm.straight_down(32 * ks, 16 * w, lane);
 #pragma unroll
@@ -321,13 +313,13 @@ template <typename T, int NP, int KP, bool SHARED> __global__ __launch_bounds__(
                 for (int t = 0; t < AT; ++t) kf[t] = km.straight_down(32 * ks, 16 * (half * KH + t0 + t), lane);
                 if (left) {
                     mma_each<3>(kf, zf, A1 + t0);
-                    mma_each<PK>(kf, mf, A2 + t0);
+                    mma_each<3>(kf, mf, A2 + t0);
                 }
                 if (right) {
 #pragma unroll
                     for (int t = 0; t < AT; ++t) qf[t] = qm.straight_down(32 * ks, 16 * (half * KH + t0 + t), lane);
-                    mma_each<PK>(qf, zd, A2 + t0);
-                    mma_each<PK>(kf, md, A2 + t0);
+                    mma_each<3>(qf, zd, A2 + t0);
+                    mma_each<3>(kf, md, A2 + t0);
                 }
             }
         }

@@ -10,7 +10,7 @@
 // Matrix products run on the bf16 matrix instruction (16 x 16 x 32).  A bf16 operand is exact; an fp32 one is cut into three bf16
 // planes x = x0 + x1 + x2 of 8 bits each, 24 in all, and a product takes the pairs whose planes' numbers add up to less than 3: three
 // instructions for exact x fp32, six for fp32 x fp32, with the error of an fp32 product.  (The fp32 matrix instruction has a 16th of the
-// bf16 one's rate.)  The gradient of the keys of a bf16 call takes two planes and three pairs (16 bits).
+// bf16 one's rate.)
 //
 // Layout of the instruction, g = lane / 16, c = lane % 16: operands hold row (column) c and eight steps of the contraction, 8g .. 8g+7;
 // the result holds column c and rows 4g .. 4g+3.  Which eight steps a lane holds is free as long as both operands agree, so two result
