@@ -1,7 +1,7 @@
 // Gated delta rule by chunks: the states at the segments' begins (forward, S' = A S + b) or, for the gradient, behind their ends
 // (S' = A^T S + b, from the last segment to the first).  The first of the chain, which is the caller's, is written down with the others: the pass
 // over the segments takes all of them from here, because the workgroup that stores the caller's other end does not wait for the one
-// that begins with this, and both may be one buffer.
+// that begins with this, and both may be one buffer.  A segment that the row does not reach is no link: the state passes it unchanged.
 //
 // A workgroup takes 16 columns of a head's state: the segments are a chain, and what counts is the time of one link.  Wave w owns row
 // tiles w and w + 4; it splits its own rows of A (fetched a link ahead) and its own tiles of the new state, and the waves pass each other
@@ -22,7 +22,9 @@ template <int KP, bool REV> __global__ __launch_bounds__(256) void delta_join(co
     const size_t st = (size_t)KT * a.VT * 1024;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     const float *begin = REV ? a.dstate_out : a.state_in;
-    const int links = a.segments - 1;
+    // links first .. last - 1 belong to segments that hold chunks of the row
+    const int links = a.segments - 1, live = ((row_length(a, bh / a.H) + CHUNK - 1) / CHUNK + a.seg_chunks - 1) / a.seg_chunks;
+    const int first = REV ? min(a.segments - live, links) : 0, last = REV ? links : min(live, links);
     f32x4 S[OWN], bn[OWN];
     float an[OWN][KS][8];
     auto put = [&](int buf) {
@@ -59,7 +61,13 @@ template <int KP, bool REV> __global__ __launch_bounds__(256) void delta_join(co
                 }
         }
     };
-    fetch(0);
+    auto leave = [&](int s) {                   // the state as segment s finds it
+        char *to = a.seg_s + ((size_t)bh * a.segments + s) * st + ((size_t)w * a.VT + vt) * 1024 + lane * 16;
+#pragma unroll
+        for (int o = 0; o < OWN; ++o)
+            if (w + 4 * o < KT) *reinterpret_cast<f32x4 *>(to + (size_t)(4 * o) * a.VT * 1024) = S[o];
+    };
+    if (first < last) fetch(first);
 #pragma unroll
     for (int o = 0; o < OWN; ++o) {
         S[o] = zero;
@@ -70,18 +78,10 @@ template <int KP, bool REV> __global__ __launch_bounds__(256) void delta_join(co
             if (begin && f < a.K && v < a.V) S[o][r] = begin[((long long)bh * a.K + f) * a.V + v];
         }
     }
-    {
-        char *to = a.seg_s + ((size_t)bh * a.segments + (REV ? links : 0)) * st + lane * 16;
-#pragma unroll
-        for (int o = 0; o < OWN; ++o) {
-            const int t = w + 4 * o;
-            if (t < KT) *reinterpret_cast<f32x4 *>(to + ((size_t)t * a.VT + vt) * 1024) = S[o];
-        }
-    }
-    put(0);
-    for (int i = 0; i < links; ++i) {
-        const int s = REV ? a.segments - 1 - i : i;
-        char *to = a.seg_s + ((size_t)bh * a.segments + (REV ? s - 1 : s + 1)) * st + lane * 16;
+    leave(REV ? links : 0);
+    for (int i = 0; i < first; ++i) leave(links - 1 - i);
+    put(first & 1);
+    for (int i = first; i < last; ++i) {
         Frag<3> af[OWN][KS];
         f32x4 acc[OWN][KS];
 #pragma unroll
@@ -91,7 +91,7 @@ template <int KP, bool REV> __global__ __launch_bounds__(256) void delta_join(co
                 split8<3>(an[o][ks], af[o][ks]);
                 acc[o][ks] = ks == 0 ? bn[o] : zero;
             }
-        if (i + 1 < links) fetch(i + 1);
+        if (i + 1 < last) fetch(i + 1);
         __syncthreads();
         Frag<3> f[KS];
 #pragma unroll
@@ -112,11 +112,11 @@ template <int KP, bool REV> __global__ __launch_bounds__(256) void delta_join(co
             S[o] = acc[o][0];
 #pragma unroll
             for (int ks = 1; ks < KS; ++ks) S[o] += acc[o][ks];
-            const int t = w + 4 * o;
-            if (t < KT) *reinterpret_cast<f32x4 *>(to + ((size_t)t * a.VT + vt) * 1024) = S[o];
         }
-        if (i + 1 < links) put((i + 1) & 1);
+        leave(REV ? links - 1 - i : i + 1);
+        if (i + 1 < last) put((i + 1) & 1);
     }
+    for (int i = last; i < links; ++i) leave(i + 1);
 }
 
 template <int KP> static int join_kp(const Args &a, bool reverse, hipStream_t s)

@@ -116,6 +116,7 @@ template <typename T, int NP, int KP, int MODE, int NW> __global__ __launch_boun
     const int seg = blk / rows_all % nseg, group = blk / rows_all / nseg, b = bh / a.H, h = bh % a.H;
     const int len = row_length(a, b), nb = (len + CHUNK - 1) / CHUNK;
     const int n0 = min(seg * a.seg_chunks, nb), n1 = min(n0 + a.seg_chunks, nb);
+    if (MODE == 1 && n0 == n1) return;          // (the join asks nothing of a segment that the row does not reach)
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     int tid = threadIdx.x, lane = tid % 64, g = lane / 16, c = lane % 16;
     // column tile: of v, and (MODE 1) beyond it of the identity

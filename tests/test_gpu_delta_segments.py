@@ -53,3 +53,24 @@ def test_gradients_behind_a_state_in_place_and_in_place_themselves(B, L, H, Hk, 
     torch.cuda.synchronize()
     for n in NAMES:
         assert torch.equal(got[n], apart[n]), n
+
+
+@pytest.mark.parametrize("Kd,V", [(64, 64), (128, 40), (20, 24)])
+def test_the_state_of_an_unused_slot_is_passed_through_bit_by_bit(Kd, V):
+    """Whatever it holds, and the rows beside it are what they are without it."""
+    x = make(3, 450, 2, 1, Kd, V, False, 1, 51, [450, 0, 65])
+    d = desc(x, 1)
+    clean_o, clean_s, _ = fwd(x, d)
+    clean = run_bwd(x, d)
+    for t in (x["state_in"], x["dstate_out"]):
+        flat = t[1].view(-1)
+        flat[::7], flat[1::7], flat[2::7], flat[3::7] = float("nan"), float("inf"), -3.3e38, 1.2345678e-36
+        flat[4::7], flat[5::7] = 1e-45, -0.0
+    for o, so in (fwd(x, d)[:2], _in_place(x, d, True)[:2]):
+        assert torch.equal(so[1].view(torch.int32), x["state_in"][1].view(torch.int32))
+        assert not o[1].any() and all(torch.equal(o[b], clean_o[b]) and torch.equal(so[b], clean_s[b]) for b in (0, 2))
+    got = run_bwd(x, d)
+    assert torch.equal(got["dstate_in"][1].view(torch.int32), x["dstate_out"][1].view(torch.int32))
+    for n in NAMES:
+        assert all(torch.equal(got[n][b], clean[n][b]) for b in (0, 2)), n
+        assert n == "dstate_in" or not got[n][1].any(), n
