@@ -5,7 +5,7 @@ import torch
 
 from gpu_util import rel_err
 from paper_2604_04250_amd import binding as K
-from test_gpu_delta import TOL, buffers, desc, fwd, host, make, num, ref_fwd
+from test_gpu_delta import TOL, TOL16, buffers, desc, fwd, host, make, num, ref_fwd
 from test_gpu_delta_bwd import NAMES, ref
 from test_gpu_delta_bwd import check as check_gradients
 from test_gpu_delta_bwd import run as run_bwd
@@ -74,3 +74,75 @@ def test_the_state_of_an_unused_slot_is_passed_through_bit_by_bit(Kd, V):
     for n in NAMES:
         assert all(torch.equal(got[n][b], clean[n][b]) for b in (0, 2)), n
         assert n == "dstate_in" or not got[n][1].any(), n
+
+
+# six chunks and more: MODE 1 of both passes and the join at every padded width of a key (32, 64, 128), on value tiles that fill eight waves, leave half
+# of them empty or end inside one; heads that share keys; rows without tokens, of one, ending in the first segment, inside a chunk and on its edge
+SEGMENTED = [(1, 400, 2, 2, 16, 40, 0, None), (2, 390, 4, 2, 33, 256, 1, [390, 0]), (3, 450, 2, 1, 128, 40, 1, [449, 0, 65]), (2, 520, 3, 3, 128, 256, 0, [1, 512]),
+             (1, 1100, 2, 1, 127, 72, 1, None), (4, 385, 2, 2, 5, 7, 1, [385, 384, 64, -2]), (2, 700, 6, 2, 64, 128, 1, [700, 130]), (1, 2500, 1, 1, 32, 200, 1, None),
+             (2, 640, 2, 1, 96, 16, 0, [640, 321]), (1, 390, 12, 4, 64, 33, 1, [999]), (1, 5000, 1, 1, 24, 64, 1, [4801])]
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("B,L,H,Hk,Kd,V,norm,lengths", SEGMENTED)
+def test_forward_in_segments(B, L, H, Hk, Kd, V, norm, lengths, bf16):
+    x = make(B, L, H, Hk, Kd, V, bf16, norm, 3 * L + V, lengths)
+    ref_o, ref_s = ref_fwd(host(x), norm)
+    for ckpt in (False, True):
+        o, so, _ = fwd(x, desc(x, norm), ckpt)
+        assert rel_err(num(o), ref_o) <= (TOL16 if bf16 else TOL)
+        assert rel_err(num(so), ref_s) <= TOL
+        for b, n in enumerate(lengths or ()):
+            assert not o[b, max(n, 0):].any()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("B,L,H,Hk,Kd,V,norm,lengths", SEGMENTED)
+def test_gradients_in_segments(B, L, H, Hk, Kd, V, norm, lengths, bf16):
+    x = make(B, L, H, Hk, Kd, V, bf16, norm, 5 * L + V, lengths)
+    got = run_bwd(x, desc(x, norm))
+    check_gradients(got, ref(host(x), norm), bf16)
+    for b, n in enumerate(lengths or ()):
+        for m in NAMES[:5]:
+            assert not got[m][b, max(n, 0):].any(), m
+
+
+@pytest.mark.parametrize("Kd,V", [(64, 72), (128, 40)])
+def test_what_lies_beyond_a_row_is_not_read_in_segments(Kd, V):
+    x = make(3, 450, 2, 1, Kd, V, False, 1, 61, [449, 0, 70])
+    clean_o, clean_s, _ = fwd(x, desc(x, 1))
+    clean = run_bwd(x, desc(x, 1))
+    for n in ("q", "k", "v", "decay", "beta", "do"):
+        x[n][0, 449:], x[n][1], x[n][2, 70:] = float("nan"), float("nan"), float("inf")
+    o, so, _ = fwd(x, desc(x, 1))
+    assert torch.equal(o, clean_o) and torch.equal(so, clean_s)
+    got = run_bwd(x, desc(x, 1))
+    assert all(torch.equal(got[n], clean[n]) for n in NAMES)
+
+
+@pytest.mark.parametrize("cut", [300, 384, 449])
+def test_forgetting_completely_in_segments(cut):
+    """Across a segment's edge, and on it."""
+    x = make(1, 500, 2, 2, 64, 64, False, 1, 62)
+    x["decay"][0, cut] = float("-inf")
+    o, so, _ = fwd(x, desc(x, 1))
+    ref_o, ref_s = ref_fwd(host(x), 1)
+    assert rel_err(num(o), ref_o) <= TOL and rel_err(num(so), ref_s) <= TOL
+    check_gradients(run_bwd(x, desc(x, 1)), ref(host(x), 1), False)
+
+
+def test_a_long_sequence_passed_in_long_pieces_in_place():
+    """Pieces that are cut into segments, the state carried in one buffer from each to the next, single tokens between them."""
+    x = make(2, 1800, 3, 3, 64, 64, False, 1, 63)
+    ref_o, ref_s = ref_fwd(host(x), 1)
+    state, at, parts = x["state_in"].clone(), 0, []
+    for n in (449, 1, 640, 16, 694):
+        piece = [x[m][:, at:at + n].contiguous() for m in ("q", "k", "v", "decay", "beta")]
+        d = K.make_delta_desc(2, n, 3, 64, 64, scale=0.6, qk_norm=1)
+        o = torch.empty(2, n, 3, 64, device=x["v"].device)
+        K.check(K.cawn_delta_rule_fwd(d, *piece, None, state, o, state, None, buffers(d)[1]))
+        parts.append(o)
+        at += n
+    torch.cuda.synchronize()
+    assert at == 1800
+    assert rel_err(num(torch.cat(parts, 1)), ref_o) <= TOL and rel_err(num(state), ref_s) <= TOL
