@@ -11,11 +11,13 @@ namespace {
 
 // How a row's chunks are cut into segments.  A segment costs each of its chunks twice (what it makes of a state, then its outputs) and
 // one link of the join, so two segments gain nothing; many shorten the two passes until the chip is full or the links cost as much.
-// Full are 256 CUs with the scan's workgroups that one holds; beyond that a second round would begin.  (Two short rounds of one chunk
-// are no longer than one of two, if the second is a sixteenth at most: 5 x 777 tokens of 4 heads of 64 x 128, fp32, training: 145 us, 152.)
+// Full are 256 CUs with the scan's workgroups that one holds; beyond that a second round would begin.
 // (Whole calls, for 512, 768 and 1,024 workgroups: 8 x 8,192 tokens of 12 heads of 64, bf16, training, three to a CU: 1,547, 1,469, 1,521 us;
-// 4 x 4,096 tokens of 8 heads of 128, the same, two to a CU: 718, 828, 803 us.)  A link of the join takes about a thirteenth of a
-// chunk's two passes, which is where the least length of a segment comes from.
+// 4 x 4,096 tokens of 8 heads of 128, the same, two to a CU: 718, 828, 803 us.)
+// With workgroups to spare, chunks / m links of m chunks each take least where m^2 is the chunks times the ratio of a link's time to that of a chunk's
+// two passes.  The ratio is not one number (a 19th to a 24th by the kernels' times, and the passes' begins and ends beside), so the rule's is the one
+// that served best (us for 6, 9, 13, 19 and 26: fp32, 1,024 tokens of 8 heads of 64 53, 53, 53, 47, 47, 4,096 of 12 heads 97, 91, 91, 99, 99, 8,192 of 8
+// heads 128, 123, 123, 133, 133, 16,384 of them 218, 207, 197, 195, 195; bf16 training, 8,192 of them 254, 245, 245, 256, 256).
 void cut(Args *a, bool bf16)
 {
     int columns;
@@ -25,7 +27,6 @@ void cut(Args *a, bool bf16)
     a->segments = 1, a->seg_chunks = a->chunks;
     if (want < 3 || a->chunks < 6) return;
     long long m = ceil_div(a->chunks, want);
-    if (m == 2 && groups * a->chunks * 16 <= slots * 17) m = 1;
     while (m * m * 13 < a->chunks) ++m;
     const long long segments = ceil_div(a->chunks, m);
     if (segments < 3) return;
