@@ -34,7 +34,7 @@ template <typename T, int KP, int VS, int NW, bool VEC4> __global__ __launch_bou
     const int w = threadIdx.x / 64, lane = threadIdx.x % 64, v0 = slab * VS + (lane % CL) * 4, r0 = (w * RG + lane / CL) * NR;
     const int n = row_length(a, b), hk = h / (a.H / a.Hk);
     const long long sbase = ((long long)b * a.H + h) * a.K * a.V;
-    if (n == 0 && a.state_out == a.state_in && a.L == 0) return;
+    const bool idle = n == 0 && (!a.state_out || a.state_out == a.state_in);    // nothing is asked of the state
     // A token's inputs.  What is not there is loaded from where something is and dropped where it is used: a load behind a lane's branch, or
     // one converted at once, would be waited for by itself
     T kn[NR], qn[NR], vn[4];
@@ -59,7 +59,7 @@ template <typename T, int KP, int VS, int NW, bool VEC4> __global__ __launch_bou
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         const long long at = sbase + (long long)min(r0 + i, a.K - 1) * a.V;
-        if (!a.state_in) {
+        if (!a.state_in || idle) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) S[i][j] = 0.f;
         } else if (VEC4) load_n<float, 4>(a.state_in + at + min(v0, a.V - 4), S[i]);
@@ -131,7 +131,7 @@ template <typename T, int KP, int VS, int NW, bool VEC4> __global__ __launch_bou
                 if (v0 + j < a.V) op[v0 + j] = (T)0.f;
         }
     }
-    if (!a.state_out || (n == 0 && a.state_out == a.state_in)) return;
+    if (!a.state_out || idle) return;
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         const long long at = sbase + (long long)(r0 + i) * a.V + v0;
