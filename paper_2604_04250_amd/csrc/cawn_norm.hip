@@ -7,9 +7,9 @@
 //   T = 1 (a token's heads, each by itself): a run of 4 to 64 lanes holds a group in registers from the one read to the write; the
 //     variance is that of the centred values.  Bytes: x in, y out (backward: x, dy in, dx out).
 //   T > 1, or a group too wide for 64 lanes' registers: a workgroup sums a run of tokens over its channels, a second kernel joins
-//     the sums and applies them: x is read twice.  A thread's sums are of x less its own first value, and threads and workgroups are
-//     joined as (count, mean, sum of squares about it), means within a run as differences from its first value: neither a mean of many
-//     deviations nor a first value that is far off costs the variance its digits.
+//     the sums and applies them: x is read twice.  A thread's sums are of x less its own first value over 64 tokens at most; these, threads and
+//     workgroups are joined as (count, mean, sum of squares about it), means within a run as differences from its first value: neither a
+//     mean of many deviations, a first value that is far off nor a long clip costs the variance its digits.
 // Both are bound by memory.  Measured, forward and backward: 65,536 tokens of 12 heads of 64 in bf16 115 us for 0.50 GB (4.4 TB/s; a large copy
 // reaches 5.2); 8 x 8,191 tokens of 12 groups of 64 in fp32 345 us for 1.6 GB with the second reads (4.7 TB/s).
 // Parameter gradients: every workgroup keeps its channels' sums over the rows it takes and leaves them in the workspace; a last
@@ -223,6 +223,7 @@ template <typename T, int VEC, int NIT, bool BWD> __global__ __launch_bounds__(2
 // ---------------------------------------------------------------------------------------------- T > 1
 // A workgroup: a.cb adjacent channels (whole groups, or a piece of one), a run of tokens, rows bblk, bblk + bblocks, ...
 // WHAT 0: mean and sum of squares about it -> part;  1: y;  2: sums of t and t xh -> part, column sums -> colpart;  3: dx
+constexpr int FOLD = 64;        // tokens of a thread's plain sums; a sum of 8,192 squares of bf16 values is off by 1e-5, and always upwards
 template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void group_norm_runs(const NormArgs a)
 {
     __shared__ float sh[2][256 * (WHAT == 2 ? VEC : 1)];
@@ -242,6 +243,13 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
 #pragma unroll
     for (int i = 0; i < VEC; ++i) sw[i] = sb[i] = 0.f;
     const double n = (double)a.T * a.cg;
+    // (n1, a1, a2) and (n2, b1, b2), counts, means and squares about them, into the first
+    auto join = [](float n1, float &a1, float &a2, float n2, float b1, float b2) {
+        if (n2 == 0.f) return;
+        const float off = b1 - a1, part = n2 / (n1 + n2);
+        a1 = fmaf(off, part, a1);
+        a2 += b2 + off * off * (n1 * part);
+    };
     for (int b = bblk; b < a.B; b += a.bblocks) {
         const T *xb = (const T *)a.x + b * a.xsb + c;
         float p0 = 0.f, p1 = 0.f;       // WHAT 1..3: mean, rstd
@@ -290,6 +298,7 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
             p1 = a.stats[((long long)b * a.G + g) * 2 + 1];
         }
         float s1 = 0.f, s2 = 0.f, shift = 0.f;
+        float counted = 0.f, mean = 0.f, about = 0.f;           // WHAT 0: values folded so far, their mean less the shift, squares about it
         if (mine) {
             // two tokens ahead (behind the last, the last again)
             Pack<T, VEC> xa[2], da[2];
@@ -302,7 +311,7 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
             fetch(0, t0 + rp);
             fetch(1, t0 + rp + per);
             if (WHAT == 0) shift = (float)xa[0].v[0];
-            for (int t = t0 + rp; t < t1; t += per) {
+            for (int t = t0 + rp, fold = FOLD; t < t1; t += per) {
                 float x[VEC], d[VEC];
                 const Pack<T, VEC> x0 = xa[0], d0 = da[0];
                 xa[0] = xa[1], da[0] = da[1];
@@ -335,25 +344,20 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
                 }
                 if (WHAT == 1) store_n<T, VEC>((T *)a.y + b * a.ysb + t * a.yst + c, x);
                 if (WHAT == 3) store_n<T, VEC>((T *)a.dx + b * a.xsb + t * a.xst + c, x);
+                if (WHAT == 0 && (--fold == 0 || t + per >= t1)) {
+                    const float values = (float)((FOLD - fold) * VEC), avg = s1 / values;
+                    join(counted, mean, about, values, avg, fmaxf(fmaf(-s1, avg, s2), 0.f) + 0.f * s2);        // (an infinity or NaN stays one)
+                    counted += values;
+                    s1 = s2 = 0.f, fold = FOLD;
+                }
             }
         }
         if (WHAT == 0 || WHAT == 2) {
             // over the token phases of a unit, then over a slot's units
             auto values = [&](int phase) { return t0 + phase < t1 ? (float)((t1 - t0 - phase + per - 1) / per * VEC) : 0.f; };
-            // (n1, a1, a2) and (n2, b1, b2), counts, means and squares about them, into the first
-            auto join = [](float n1, float &a1, float &a2, float n2, float b1, float b2) {
-                if (n2 == 0.f) return;
-                const float off = b1 - a1, part = n2 / (n1 + n2);
-                a1 = fmaf(off, part, a1);
-                a2 += b2 + off * off * (n1 * part);
-            };
             // the run's first value of the group
             const float ref = WHAT == 0 && mine ? (float)*((const T *)a.x + b * a.xsb + t0 * a.xst + (a.cg > a.cb ? cblk * a.cb : g * a.cg)) : 0.f;
-            if (WHAT == 0 && mine && values(rp) > 0.f) {
-                const float avg = s1 / values(rp);
-                s2 = fmaxf(fmaf(-s1, avg, s2), 0.f) + 0.f * s2;        // (an infinity or NaN stays one)
-                s1 = shift - ref + avg;
-            }
+            if (WHAT == 0 && mine && counted > 0.f) s1 = shift - ref + mean, s2 = about;
             __syncthreads();
             sh[0][threadIdx.x] = s1, sh[1][threadIdx.x] = s2;
             __syncthreads();
