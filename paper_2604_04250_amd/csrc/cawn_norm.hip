@@ -197,7 +197,7 @@ template <typename T, int VEC, int NIT, bool BWD> __global__ __launch_bounds__(2
         // the workgroup's rows of one channel, in the order of its runs of lanes
         __shared__ float sh[256 * VEC * NIT];
         float *out = a.colpart + (long long)(blockIdx.x / a.gblocks) * 2 * a.C;
-        for (int which = 0; which < 2; ++which) {
+        for (int which = 0; which < 2; ++which, out += a.C) {
             __syncthreads();
 #pragma unroll
             for (int n = 0; n < NIT; ++n)
@@ -212,7 +212,7 @@ template <typename T, int VEC, int NIT, bool BWD> __global__ __launch_bounds__(2
                     for (int i = 0; i < VEC; ++i) {
                         float v = 0.f;
                         for (int q = 0; q < a.rb; ++q) v += sh[((q * a.gb + gi) * NIT + n) * a.lpg * VEC + lane * VEC + i];
-                        out[which * a.C + c0 + (n * a.lpg + lane) * VEC + i] = v;
+                        out[c0 + (n * a.lpg + lane) * VEC + i] = v;
                     }
                 }
             }
@@ -236,7 +236,8 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
     const int per_group = a.cg > a.cb ? a.cg / a.cb : 1;                // workgroups side by side that share a group
     const int slot = a.cg > a.cb ? 0 : unit * VEC / a.cg, g = c / a.cg;
     const int su = a.cg > a.cb ? units : a.cg / VEC;                    // units of a slot
-    const int t0 = split * a.t_run, t1 = min(a.T, t0 + a.t_run);
+    // (rows and tokens without a sign: T and B go up to 2^31 - 1, and a step or two beyond the last of them has to stay above it)
+    const uint32_t t0 = (uint32_t)split * a.t_run, t1 = min((uint32_t)a.T, t0 + a.t_run);
     float w[VEC], bias[VEC], sw[VEC], sb[VEC];
     params<VEC>(mine ? a.w : nullptr, c, 1.f, w);
     params<VEC>(mine ? a.b : nullptr, c, 0.f, bias);
@@ -250,7 +251,7 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
         a1 = fmaf(off, part, a1);
         a2 += b2 + off * off * (n1 * part);
     };
-    for (int b = bblk; b < a.B; b += a.bblocks) {
+    for (uint32_t b = bblk; b < (uint32_t)a.B; b += a.bblocks) {
         const T *xb = (const T *)a.x + b * a.xsb + c;
         float p0 = 0.f, p1 = 0.f;       // WHAT 1..3: mean, rstd
         float m1 = 0.f, m2 = 0.f;
@@ -266,7 +267,7 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
                     const int sp = j / per_group, cbk = a.cg > a.cb ? gs * per_group + j % per_group : cblk;
                     const float *p = a.part + ((((long long)b * a.splits + sp) * a.ncb + cbk) * a.slots + s) * 2;
                     if (WHAT == 1) {        // its mean and squares, seen from the first part's mean
-                        const double values = (double)(min(a.T, (sp + 1) * a.t_run) - sp * a.t_run) * wide, off = (double)p[0] - about;
+                        const double values = (double)(min((uint32_t)a.T, (uint32_t)(sp + 1) * a.t_run) - (uint32_t)sp * a.t_run) * wide, off = (double)p[0] - about;
                         s1 += values * off;
                         s2 += (double)p[1] + values * off * off;
                     } else s1 += p[0], s2 += p[1];
@@ -303,7 +304,7 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
             // two tokens ahead (behind the last, the last again)
             Pack<T, VEC> xa[2], da[2];
             const T *db = WHAT >= 2 ? (const T *)a.dy + b * a.ysb + c : nullptr;
-            auto fetch = [&](int e, int t) {
+            auto fetch = [&](int e, uint32_t t) {
                 t = min(t, t1 - 1);
                 xa[e] = *reinterpret_cast<const Pack<T, VEC> *>(xb + t * a.xst);
                 if (WHAT >= 2) da[e] = *reinterpret_cast<const Pack<T, VEC> *>(db + t * a.yst);
@@ -311,7 +312,8 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
             fetch(0, t0 + rp);
             fetch(1, t0 + rp + per);
             if (WHAT == 0) shift = (float)xa[0].v[0];
-            for (int t = t0 + rp, fold = FOLD; t < t1; t += per) {
+            int fold = FOLD;
+            for (uint32_t t = t0 + rp; t < t1; t += per) {
                 float x[VEC], d[VEC];
                 const Pack<T, VEC> x0 = xa[0], d0 = da[0];
                 xa[0] = xa[1], da[0] = da[1];
@@ -354,7 +356,7 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
         }
         if (WHAT == 0 || WHAT == 2) {
             // over the token phases of a unit, then over a slot's units
-            auto values = [&](int phase) { return t0 + phase < t1 ? (float)((t1 - t0 - phase + per - 1) / per * VEC) : 0.f; };
+            auto values = [&](uint32_t phase) { return t0 + phase < t1 ? (float)((t1 - t0 - phase + per - 1) / per * VEC) : 0.f; };
             // the run's first value of the group
             const float ref = WHAT == 0 && mine ? (float)*((const T *)a.x + b * a.xsb + t0 * a.xst + (a.cg > a.cb ? cblk * a.cb : g * a.cg)) : 0.f;
             if (WHAT == 0 && mine && counted > 0.f) s1 = shift - ref + mean, s2 = about;
@@ -404,7 +406,7 @@ template <typename T, int VEC, int WHAT> __global__ __launch_bounds__(256) void 
                 float v1 = 0.f, v2 = 0.f;
                 for (int q = 0; q < per; ++q) v1 += sh[0][(q * units + unit) * VEC + i], v2 += sh[1][(q * units + unit) * VEC + i];
                 out[c + i] = v1;
-                out[a.C + c + i] = v2;
+                out[(long long)a.C + c + i] = v2;
             }
         }
     }

@@ -40,3 +40,29 @@ def test_the_variance_of_a_billion_values():
     mean, rstd = _moments(x)
     assert abs(float(stats[0, 0, 0]) - mean) <= 4e-6
     assert abs(float(stats[0, 0, 1]) / rstd - 1) <= 4e-6
+
+
+def test_a_clip_of_the_longest_length():
+    """One channel, 2^31 - 1 tokens in bf16.  A value is some ten roundings of 2^-24 from its inputs, then one of 2^-8; a column sum of 2^31 terms that 2^17 threads
+    add up, 2^14 each, holds 2^-24 of a thread's own sum in each addition: 2^7 roundings of random sign, 1e-5 of the sum's usual size."""
+    T = 2 ** 31 - 1
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    x, dy = _filled(T, gen), _filled(T, gen)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    w, b = torch.full((1,), 1.25, device=DEV), torch.full((1,), -0.5, device=DEV)
+    stats, dw, db = torch.empty(1, 1, 2, device=DEV), torch.empty(1, device=DEV), torch.empty(1, device=DEV)
+    d = K.make_norm_desc(1, T, 1, 1, bf16=1)
+    ws = torch.empty(max(256, K.cawn_group_norm_workspace_bytes(d)), dtype=torch.uint8, device=DEV)
+    K.check(K.cawn_group_norm_fwd(d, x, w, b, y, stats, ws))
+    K.check(K.cawn_group_norm_bwd(d, x, w, b, stats, dy, dx, dw, db, ws))
+    torch.cuda.synchronize()
+    mean, rstd = _moments(x)
+    assert abs(float(stats[0, 0, 0]) - mean) <= 4e-6 and abs(float(stats[0, 0, 1]) / rstd - 1) <= 4e-6
+    total = lambda f: sum(float(f(s)) for s in _parts(T))  # noqa: E731
+    xh = lambda s: (x[0, s].double() - mean) * rstd  # noqa: E731
+    sum_b, sum_w = total(lambda s: dy[0, s].double().sum()), total(lambda s: (dy[0, s].double() * xh(s)).sum())
+    assert abs(float(db) - sum_b) <= 2e-5 * max(abs(sum_b), T ** 0.5) and abs(float(dw) - sum_w) <= 2e-5 * max(abs(sum_w), T ** 0.5)
+    for s in _parts(T):
+        for got, want in ((y, 1.25 * xh(s) - 0.5), (dx, 1.25 * rstd * (dy[0, s].double() - sum_b / T - xh(s) * (sum_w / T)))):
+            err = (got[0, s].double() - want).abs()
+            assert bool((err <= (2.0 ** -8 + 4e-6) * want.abs().clamp_min(1.0)).all())
