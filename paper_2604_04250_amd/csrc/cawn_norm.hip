@@ -554,7 +554,7 @@ int run(const cawn_norm_desc *d, bool bwd, const void *x, const float *w, const 
         void *ws, size_t bytes, void *stream)
 {
     Plan p;
-    if (!plan_of(d, true, bwd, &p)) return CAWN_EINVAL;
+    if (!plan_of(d, true, bwd, &p) || !aligned_to(stats, 4) || !aligned_to(dw, 4) || !aligned_to(db, 4)) return CAWN_EINVAL;
     hipStream_t s = (hipStream_t)stream;
     const bool grads = bwd && (dw || db);
     if (d->B == 0 || d->T == 0) {
