@@ -32,7 +32,8 @@ class DeltaRule(torch.autograd.Function):
         B, L, H, V = v.shape
         Hk, Kw = k.shape[2:]
         d = K.make_delta_desc(B, L, H, Kw, V, Hk=Hk, scale=Kw ** -0.5, qk_norm=1, bf16=int(v.dtype == torch.bfloat16))
-        q, k, v, decay, beta = (t.contiguous() for t in (q, k, v, decay, beta))
+        q, k, v, decay, beta, state = (t.contiguous() for t in (q, k, v, decay, beta, state))
+        lengths = None if lengths is None else lengths.contiguous()
         train = any(ctx.needs_input_grad)
         ckpt = _scratch(K.cawn_delta_ckpt_bytes(d), v.device) if train else None
         workspace = _scratch(K.cawn_delta_workspace_bytes(d), v.device)
@@ -45,10 +46,11 @@ class DeltaRule(torch.autograd.Function):
     @staticmethod
     def backward(ctx, do, dstate_out):
         q, k, v, decay, beta = ctx.saved_tensors
+        do, dstate_out = do.contiguous(), dstate_out.contiguous()
         dq, dk, dv, ddecay, dbeta = (torch.empty_like(t) for t in (q, k, v, decay, beta))
         dstate = torch.empty_like(dstate_out) if ctx.needs_input_grad[5] else None
-        K.check(K.cawn_delta_rule_bwd(ctx.d, q, k, v, decay, beta, ctx.lengths, ctx.ckpt, do.contiguous(), dstate_out.contiguous(), dq, dk, dv,
-                                      ddecay, dbeta, dstate, ctx.workspace))
+        K.check(K.cawn_delta_rule_bwd(ctx.d, q, k, v, decay, beta, ctx.lengths, ctx.ckpt, do, dstate_out, dq, dk, dv, ddecay,
+                                      dbeta, dstate, ctx.workspace))
         return dq, dk, dv, ddecay, dbeta, dstate, None
 
 
@@ -57,6 +59,7 @@ class HeadNorm(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, weight, bias, groups):
+        x, weight, bias = x.contiguous(), weight.contiguous(), bias.contiguous()
         d = K.make_norm_desc(x.shape[0], 1, x.shape[1], groups, act=1, bf16=int(x.dtype == torch.bfloat16))
         y, stats = torch.empty_like(x), torch.empty((x.shape[0], groups, 2), device=x.device)
         workspace = _scratch(K.cawn_group_norm_workspace_bytes(d), x.device)
