@@ -24,6 +24,13 @@ def _scratch(nbytes, device):
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
+def _types(wanted, **tensors):
+    """The entry points take pointers: what a tensor holds has to be checked before."""
+    for name, t in tensors.items():
+        if t is not None and t.dtype != wanted:
+            raise TypeError(f"{name} is {t.dtype}, not {wanted}")
+
+
 class DeltaRule(torch.autograd.Function):
     """q, k [B,L,Hk,K], v [B,L,H,V], decay, beta [B,L,H] fp32, state [B,H,K,V] fp32 -> o [B,L,H,V], state behind the last token."""
 
@@ -31,6 +38,9 @@ class DeltaRule(torch.autograd.Function):
     def forward(ctx, q, k, v, decay, beta, state, lengths):
         B, L, H, V = v.shape
         Hk, Kw = k.shape[2:]
+        _types(torch.bfloat16 if v.dtype == torch.bfloat16 else torch.float32, q=q, k=k, v=v)
+        _types(torch.float32, decay=decay, beta=beta, state=state)
+        _types(torch.int32, lengths=lengths)
         d = K.make_delta_desc(B, L, H, Kw, V, Hk=Hk, scale=Kw ** -0.5, qk_norm=1, bf16=int(v.dtype == torch.bfloat16))
         q, k, v, decay, beta, state = (t.contiguous() for t in (q, k, v, decay, beta, state))
         lengths = None if lengths is None else lengths.contiguous()
@@ -55,11 +65,13 @@ class DeltaRule(torch.autograd.Function):
 
 
 class HeadNorm(torch.autograd.Function):
-    """SiLU(norm(x) weight + bias) of [tokens, C], every token's `groups` heads by themselves."""
+    """SiLU(norm(x) weight + bias) of [tokens, C], every token's `groups` heads by themselves; weight and bias of any type, taken in fp32."""
 
     @staticmethod
     def forward(ctx, x, weight, bias, groups):
-        x, weight, bias = x.contiguous(), weight.contiguous(), bias.contiguous()
+        _types(torch.bfloat16 if x.dtype == torch.bfloat16 else torch.float32, x=x)
+        ctx.types = weight.dtype, bias.dtype
+        x, weight, bias = x.contiguous(), weight.float().contiguous(), bias.float().contiguous()
         d = K.make_norm_desc(x.shape[0], 1, x.shape[1], groups, act=1, bf16=int(x.dtype == torch.bfloat16))
         y, stats = torch.empty_like(x), torch.empty((x.shape[0], groups, 2), device=x.device)
         workspace = _scratch(K.cawn_group_norm_workspace_bytes(d), x.device)
@@ -73,7 +85,7 @@ class HeadNorm(torch.autograd.Function):
         x, weight, bias, stats = ctx.saved_tensors
         dx, dw, db = torch.empty_like(x), torch.empty_like(weight), torch.empty_like(bias)
         K.check(K.cawn_group_norm_bwd(ctx.d, x, weight, bias, stats, dy.contiguous(), dx, dw, db, ctx.workspace))
-        return dx, dw, db, None
+        return dx, dw.to(ctx.types[0]), db.to(ctx.types[1]), None
 
 
 class DropoutAdd(torch.autograd.Function):
@@ -81,6 +93,8 @@ class DropoutAdd(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, residual, rng, p):
+        _types(torch.bfloat16 if x.dtype == torch.bfloat16 else torch.float32, x=x, residual=residual)
+        _types(torch.int64, rng=rng)
         d = K.make_dropout_desc(*x.shape, p=p, bf16=int(x.dtype == torch.bfloat16))
         x, residual = x.contiguous(), residual.contiguous()
         y = torch.empty_like(x)
