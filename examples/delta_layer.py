@@ -15,6 +15,7 @@ import sys
 
 import torch
 import torch.nn.functional as F
+from torch.autograd.function import once_differentiable
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2604_04250_amd import binding as K  # noqa: E402
@@ -54,6 +55,7 @@ class DeltaRule(torch.autograd.Function):
         return o, state_out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do, dstate_out):
         q, k, v, decay, beta = ctx.saved_tensors
         do, dstate_out = do.contiguous(), dstate_out.contiguous()
@@ -81,6 +83,7 @@ class HeadNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight, bias, stats = ctx.saved_tensors
         dx, dw, db = torch.empty_like(x), torch.empty_like(weight), torch.empty_like(bias)
@@ -104,6 +107,7 @@ class DropoutAdd(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         rng, = ctx.saved_tensors
         dy = dy.contiguous()

@@ -1,4 +1,4 @@
-"""The example's functions on tensors as programs have them: strided, of other types."""
+"""The example's functions on tensors as programs have them: strided, of other types, differentiated twice."""
 import pytest
 import torch
 
@@ -76,3 +76,12 @@ def test_types_that_would_be_misread_are_refused():
         E.DropoutAdd.apply(t, t.bfloat16(), torch.tensor([1, 0], device=DEV), 0.1)
     with pytest.raises(TypeError, match="rng"):
         E.DropoutAdd.apply(t, t, torch.tensor([1, 0], device=DEV, dtype=torch.int32), 0.1)
+
+
+def test_a_second_derivative_is_an_error():
+    x = [t.requires_grad_() for t in _inputs()]
+    t, w = torch.randn(8, 32, device=DEV, requires_grad=True), torch.randn(32, device=DEV, requires_grad=True)
+    for out, at in ((E.DeltaRule.apply(*x, None)[0], x[0]), (E.HeadNorm.apply(t, w, w, 2), t), (E.DropoutAdd.apply(t, t, torch.tensor([1, 0], device=DEV), 0.1), t)):
+        g, = torch.autograd.grad(out.square().sum(), at, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            g.square().sum().backward()
