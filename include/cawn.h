@@ -416,7 +416,8 @@ size_t cawn_delta_workspace_bytes(const cawn_delta_desc *d);
 /*
  * Forward: prefill, training, and single tokens (L = 1: one pass over the state).
  *   q, k [B][L][Hk][K], v [B][L][H][V]; decay, beta [B][L][H] fp32, dense.  decay is the logarithm of the retention; every value
- *       below -104, minus infinity among them, forgets the state completely (exp underflows there); beta is used as it is
+ *       below -104, minus infinity among them, forgets the state completely (exp underflows there); beta is used as it is, but
+ *       that calls of more than 16 tokens or with a checkpoint take one nearer to 0 than 2^-60 as 2^-60 (beta = 0 adds 1e-18 of its value)
  *   lengths    device int32 [B] or NULL: row b has lengths[b] tokens (clamped to 0..L).  Of the rest nothing is read; o is 0 there
  *       and the state is that behind the last token.  0: an unused slot, whose state is passed through
  *   state_in   or NULL (zeros); state_out or NULL; they may be the same

@@ -12,8 +12,8 @@ namespace {
 // How a row's chunks are cut into segments.  A segment costs each of its chunks twice (what it makes of a state, then its outputs) and
 // one link of the join, so two segments gain nothing; many shorten the two passes until the chip is full or the links cost as much.
 // Full are 256 CUs with the scan's workgroups that one holds; beyond that a second round would begin.
-// (Whole calls, for 512, 768 and 1,024 workgroups: 8 x 8,192 tokens of 12 heads of 64, bf16, training, three to a CU: 1,547, 1,469, 1,521 us;
-// 4 x 4,096 tokens of 8 heads of 128, the same, two to a CU: 718, 828, 803 us.)
+// (Whole calls, for 512, 768 and 1,024 workgroups: 8 x 8,192 tokens of 12 heads of 64, bf16, training, three to a CU: 1,594, 1,477, 1,554 us;
+// 4 x 4,096 tokens of 8 heads of 128, the same, two to a CU: 722, 832, 809 us.)
 // With workgroups to spare, chunks / m links of m chunks each take least where m^2 is the chunks times the ratio of a link's time to that of a chunk's
 // two passes.  The ratio is not one number (a 19th to a 24th by the kernels' times, and the passes' begins and ends beside), so the rule's is the one
 // that served best (us for 6, 9, 13, 19 and 26: fp32, 1,024 tokens of 8 heads of 64 53, 53, 53, 47, 47, 4,096 of 12 heads 97, 91, 91, 99, 99, 8,192 of 8
@@ -140,8 +140,9 @@ int cawn_delta_rule_fwd(const cawn_delta_desc *d, const void *q, const void *k, 
     hipStream_t s = (hipStream_t)stream;
     const int e = d->bf16 ? 2 : 4, w = 16 / e;
     a.vecq = a.K % 8 == 0 && a.qst % w == 0 && a.qsb % w == 0 && aligned_to(q, 16) && aligned_to(k, 16);
-    // token by token up to TOKEN_MAX.  (12 heads of 64, bf16: 16 tokens 19.3 us, 20.0 by chunks, 32 tokens 35.9 and 20.2; 32 rows of 32 heads of
-    // 128: 105 us and 137, 190 and 139.)
+    // Token by token up to TOKEN_MAX.  (us token by token and by chunks, bf16: 12 heads of 64, 8 tokens 10.9 and 19.3, 16 tokens 19.3 and 19.2, 32 tokens
+    // 35.8 and 19.6; 32 rows of 32 heads of 128, 16 tokens 105 and 86, 32 tokens 190 and 91.  Calls of up to 16 tokens need no workspace, so
+    // the line is there for many rows as well.)
     if (a.L <= delta::TOKEN_MAX && !ckpt) return delta::launch_token(a, d->bf16, s);
     const Layout l = layout_of(a);
     if (!workspace || workspace_bytes < l.fwd || !aligned_to(workspace, 256)) return CAWN_EWORKSPACE;

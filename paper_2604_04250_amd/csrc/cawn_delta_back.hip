@@ -7,7 +7,7 @@
 // once), delta_join the gradients behind the segments' ends, MODE 0 runs through all segments and leaves dR and dS of every chunk to
 // delta_gradients.  Waves, columns and operands as in the forward; P^T takes three planes, because dR carries fp32 gradients.
 //
-// Measured: 8 x 8,192 tokens of 12 heads of 64 in bf16: MODE 1 190 us, MODE 0 221 (0.9 GB), bound by instruction issue like the forward.
+// Measured: 8 x 8,192 tokens of 12 heads of 64 in bf16: MODE 1 181 us, MODE 0 213 (1.0 GB), bound by instruction issue like the forward.
 #include "cawn_delta_mfma.hpp"
 
 namespace cawn {

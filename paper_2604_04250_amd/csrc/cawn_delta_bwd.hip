@@ -24,9 +24,9 @@ namespace delta {
 // and wave 4 + w rows 16 w .. of them, half of the columns each.  First everything that runs over the value columns, 32 at a time, with U, dR, S0 and dS in LDS as they come
 // from their tiles (a tile's lane holds four rows of a column: a matrix is kept as its transpose, and read down); then, in the same
 // LDS, Z and M with q and k.
-// Measured: 8 x 8,192 tokens of 12 heads of 64 in bf16: 620 us for 1.7 GB (of them U, dR, S0, S_C and dS 1.0), 2.7 TB/s.  Of a workgroup's time a third
+// Measured: 8 x 8,192 tokens of 12 heads of 64 in bf16: 622 us for 1.5 GB (of them U, dR, S0 and dS 0.8), 2.4 TB/s.  Of a workgroup's time a third
 // is the way of its first loads and last stores, the rest splits, products and barriers in turn: neither bandwidth nor the units are full.
-// Eight waves of half the columns, not four of all: fp32, 5 x 777 tokens of 4 heads of 64 x 128 45 us, 53; this shape 620 us, 625.
+// Eight waves of half the columns, not four of all: fp32, 5 x 777 tokens of 4 heads of 64 x 128 45 us, 53; this shape within 1 %.
 constexpr int WLD = CHUNK + 4;          // (four rows apart begin in other banks)
 template <typename T, int NP, int KP> struct GradLds {
     using MatU = Tile<3, 32, 64>;
@@ -42,7 +42,7 @@ template <typename T, int NP, int KP> struct GradLds {
     static constexpr int SECOND = 2 * MatQ::BYTES + MatZ::BYTES + MatM::BYTES;
     static constexpr int BYTES = FIRST > SECOND ? FIRST : SECOND;
     // waves a SIMD: as many workgroups as the LDS holds, two at most.  (With SHARED one, which has registers for the sums over the heads:
-    // 4 x 4,096 tokens of 12 heads of 64 on 4 of keys in bf16, whole backward and forward: 471 us, 489 with two.)
+    // 4 x 4,096 tokens of 12 heads of 64 on 4 of keys in bf16, whole backward and forward: 452 us, 479 with two.)
     static constexpr int HELD = 163840 / (BYTES + 4096), WAVES = HELD > 2 ? 4 : 2 * HELD;
 };
 

@@ -5,8 +5,8 @@
 //
 // A workgroup takes 16 columns of a head's state: the segments are a chain, and what counts is the time of one link.  Wave w owns row
 // tiles w and w + 4; it splits its own rows of A (fetched a link ahead) and its own tiles of the new state, and the waves pass each other
-// the state's planes in LDS: one barrier a link.  A link takes some 0.8 us (4,096 tokens of 12 heads of 64 in fp32, 21 links: 22 us; 2 x 32,768 tokens
-// of 32 heads of 128, 3 links of 13 MB each: 27 us): the chain split, LDS, six products, sum.  Rows of A fetched two or four links ahead made the
+// the state's planes in LDS: one barrier a link.  A link takes 1.0 to 1.2 us (4,096 tokens of 12 heads of 64 in fp32, 21 links: 22 us; 4 x 2,048 in bf16, 15
+// links: 18 us), eight where it moves 13 MB (2 x 32,768 tokens of 32 heads of 128, 3 links: 25 us): the chain split, LDS, six products, sum.  Rows of A fetched two or four links ahead made the
 // first call 2 us slower.
 #include "cawn_delta_mfma.hpp"
 

@@ -15,9 +15,9 @@
 // with P made by all waves together and T fetched.  Four waves to 64 columns keep the state's columns in registers and share what the
 // chunk's rows give; k, q and gates of the next chunk travel meanwhile.
 //
-// Measured, bf16, whole kernels: 8 x 8,192 tokens of 12 heads of 64 (a training step's forward): delta_system 130 us, MODE 1 186, join 16, MODE 0
-// 267 (1.0 GB, of them 0.4 the checkpoint); 2 x 32,768 tokens of 32 heads of 128: 420, 937, 27 and 1,421 us.  What bounds MODE 0 and 1 is
-// instruction issue: the matrix units are busy a sixth to two fifths of the time, vector instructions (splits into planes, factors)
+// Measured, bf16, whole kernels: 8 x 8,192 tokens of 12 heads of 64 (a training step's forward): delta_system 124 us, MODE 1 183, join 16, MODE 0
+// 287 (1.1 GB, of them 0.4 the checkpoint); 2 x 32,768 tokens of 32 heads of 128: 420, 949, 25 and 1,541 us.  What bounds MODE 0 and 1 is
+// instruction issue: the matrix units are busy a fifth to two fifths of the time, vector instructions (splits into planes, factors)
 // another third to two thirds, and between the barriers of a chunk the two to four waves of a SIMD do not always have the other kind to offer.
 #include "cawn_delta_mfma.hpp"
 
@@ -25,7 +25,7 @@ namespace cawn {
 namespace delta {
 
 // What a chunk is by itself, every chunk a workgroup: gates, the norms' factors, and T = (I + diag(beta) N)^-1.  Bound by vector
-// instructions (58 % of the time at K = 64, 69 % at 128) and by the chain of the inverse, four workgroups a CU.
+// instructions (59 % of the time at K = 64, 70 % at 128) and by the chain of the inverse, four workgroups a CU.
 template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void delta_system(const Args a)
 {
     constexpr int KS = KP / 32;
@@ -91,8 +91,8 @@ template <typename T, int NP, int KP> __global__ __launch_bounds__(256) void del
 
 // The scan's LDS: k, q (MODE 0); T; P's operands.  P has a place of its own and is made ahead of the products with the state where that costs no
 // workgroup of a CU; elsewhere it is made where T was, for one more barrier.  (In T's place and in its own, us: one workgroup a CU either way, 4,096 tokens
-// of 8 heads of 128 in fp32 172 and 167; two, 2 x 32,768 of 32 heads of 128 in bf16 2,743 and 2,683; three and two, 8 x 8,192 of 12 heads of 64 in
-// bf16, training, 1,441 and 1,542, but 4 x 16,384 of 8 heads, forward, 355 and 340; two and one, 4,096 of 12 heads of 64 in fp32 90 and 95.)
+// of 8 heads of 128 in fp32 174 and 169; two, 2 x 32,768 of 32 heads of 128 in bf16 2,855 and 2,803; three and two, 8 x 8,192 of 12 heads of 64 in
+// bf16, training, 1,477 and 1,572, but 4 x 16,384 of 8 heads, forward, 364 and 348; two and one, 4,096 of 12 heads of 64 in fp32 91 and 95.)
 template <int NP, int KP, int MODE, int NW> struct ScanLds {
     static constexpr int KB = Tile<NP, CHUNK, KP>::BYTES, TO = MODE == 0 ? 2 * KB : KB;
     // waves a SIMD that the registers are budgeted for: as many workgroups as the LDS holds, but three waves (MODE 1 of K <= 64: four) at most
@@ -429,8 +429,8 @@ template <typename T, int NP, int KP> static int scan_kp(const Args &a, hipStrea
 {
     if (a.segments > 1) {
         // Eight waves where they divide the columns; four where half of eight would have none, and at K = 128, where they have more registers (us for
-        // eight and four: 8 x 8,192 tokens of 12 heads of 64 in bf16, training, 1,436 and 1,463; 8 x 4,096 of 8 heads of 64 x 128 275 and 240;
-        // 8 x 4,096 of 16 heads of 32, training, 687 and 649; 2 x 32,768 of 32 heads of 128 2,765 and 2,643)
+        // eight and four: 8 x 8,192 tokens of 12 heads of 64 in bf16, training, 1,476 and 1,510; 8 x 4,096 of 8 heads of 64 x 128 283 and 257;
+        // 8 x 4,096 of 16 heads of 32, training, 700 and 663; 2 x 32,768 of 32 heads of 128 3,094 and 2,790)
         const long long segments = a.s_tiles ? a.segments : a.segments - 1, tiles = a.VT + KP / 16;
         int r;
         if constexpr (KP == 128) r = launch<T, NP, KP, 1, 4>(a, segments, tiles, s);
@@ -438,8 +438,9 @@ template <typename T, int NP, int KP> static int scan_kp(const Args &a, hipStrea
         if (r) return r;
         if (int r = launch_join(a, false, s)) return r;
     }
-    // Where the LDS holds one workgroup of four waves a CU, eight waves take twice the columns, if there are as many (4,096 tokens of 8 heads
-    // of 128 in fp32: 186 us, 213 with four waves).  Elsewhere eight waves wait for each other (bf16, 2 x 32,768 of 32 heads of 128: 3,390 us, 3,049 with four)
+    // Where the LDS holds one workgroup of four waves a CU, eight waves take twice the columns, if there are as many (us for eight and four, 4,096
+    // tokens of 8 heads in fp32: of 128 x 192 184 and 197, of 128 x 128 169 and 160).  Elsewhere four, where eight gain on long rows and lose on others
+    // (bf16, heads of 128: 2 x 32,768 of 32 2,622 and 2,790, 4 x 16,384 of 8 747 and 775; 16 x 512 of 8 105 and 91, 16 x 4,096 of them, training, 2,332 and 2,253)
     if constexpr (NP == 3 && KP == 128)
         if (a.VT > 4) return launch<T, NP, KP, 0, 8>(a, a.segments, a.VT, s);
     return launch<T, NP, KP, 0, 4>(a, a.segments, a.VT, s);

@@ -10,8 +10,8 @@
 //     the sums and applies them: x is read twice.  A thread's sums are of x less its own first value over 64 tokens at most; these, threads and
 //     workgroups are joined as (count, mean, sum of squares about it), means within a run as differences from its first value: neither a
 //     mean of many deviations, a first value that is far off nor a long clip costs the variance its digits.
-// Both are bound by memory.  Measured, forward and backward: 65,536 tokens of 12 heads of 64 in bf16 115 us for 0.50 GB (4.4 TB/s; a large copy
-// reaches 5.2); 8 x 8,191 tokens of 12 groups of 64 in fp32 345 us for 1.6 GB with the second reads (4.7 TB/s).
+// Both are bound by memory.  Measured, forward and backward: 65,536 tokens of 12 heads of 64 in bf16 116 us for 0.50 GB (4.3 TB/s; a large copy
+// reaches 5.2); 8 x 8,191 tokens of 12 groups of 64 in fp32 346 us for 1.6 GB with the second reads (4.7 TB/s).
 // Parameter gradients: every workgroup keeps its channels' sums over the rows it takes and leaves them in the workspace; a last
 // kernel adds these in a fixed order.
 #include "cawn_ops.hpp"
@@ -459,10 +459,10 @@ bool plan_of(const cawn_norm_desc *d, bool wide, bool bwd, Plan *p)
     const int most = d->bf16 ? 8 : 4;
     const bool fits = a.cg % most == 0 && a.xst % most == 0 && a.xsb % most == 0 && a.yst % most == 0 && a.ysb % most == 0;
     // 16 bytes an access, or single values where rows or groups do not begin on them (65,536 tokens of 12 heads of 64 in bf16, both directions:
-    // 124 us, 352; 8 x 8,191 of 12 groups of 64 in fp32: 364 us, 433)
+    // 117 us, 376; 8 x 8,191 of 12 groups of 64 in fp32: 345 us, 497)
     p->vec = wide && fits ? most : 1;
     const long long lanes = ceil_div(a.cg, p->vec);
-    // groups in registers where a run of lanes holds one (the first shape above: 124 us, 444 with sums joined by a second kernel)
+    // groups in registers where a run of lanes holds one (the first shape above: 117 us, 534 with sums joined by a second kernel)
     p->rows = a.T == 1 && lanes <= 64 * 4;
     const long long cap = 33554432LL / (8LL * a.C) > 64 ? 33554432LL / (8LL * a.C) : 64;      // rows of parameter sums: 32 MiB of them
     if (p->rows) {
@@ -477,7 +477,7 @@ bool plan_of(const cawn_norm_desc *d, bool wide, bool bwd, Plan *p)
         p->threads = (a.lpg * a.gb * a.rb + 63) / 64 * 64;
         long long rblocks = ceil_div(a.B, a.rb);
         // as many as are there at once, eight or (backward) six to a CU: a second round would be half empty (65,536 tokens of 12 heads of 64 in
-        // bf16, forward and backward, both on 2,048, 1,536, 1,024: 123, 116, 133 us; forward alone 43, on 1,536 47 us)
+        // bf16, forward and backward, the latter on 2,048, 1,536, 1,024: 125, 117, 134 us; forward alone 44, on 1,024 57 us)
         const int groups = bwd ? 1536 : 2048;
         long long want = groups / a.gblocks > 1 ? groups / a.gblocks : 1;
         if (want > cap) want = cap;
@@ -500,7 +500,7 @@ bool plan_of(const cawn_norm_desc *d, bool wide, bool bwd, Plan *p)
         a.ncb = a.C / a.cb;
         const int per = 256 / (a.cb / p->vec);
         p->threads = (a.cb / p->vec * per + 63) / 64 * 64;
-        // (8 x 8,191 tokens of 12 groups of 64 in fp32, both directions, backward on 2,048, 1,024: 364, 345 us: every
+        // (8 x 8,191 tokens of 12 groups of 64 in fp32, both directions, backward on 2,048, 1,024: 366, 345 us: every
         // workgroup leaves column sums)
         const int groups = bwd ? 1024 : 2048;
         long long bb = groups / a.ncb > 1 ? groups / a.ncb : 1;
@@ -510,7 +510,7 @@ bool plan_of(const cawn_norm_desc *d, bool wide, bool bwd, Plan *p)
         const long long useful = ceil_div(a.T, 4LL * per);          // a thread takes four tokens at least
         if (splits > useful) splits = useful;
         if (splits > 512) splits = 512;                             // all parts are joined by everyone (one row of 16,384 x 768, fp32, both
-                                                                    // directions, parts up to 1,024, 512, 256: 168, 120, 151 us)
+                                                                    // directions, parts up to 1,024, 512, 256: 131, 120, 153 us)
         if (splits < 1) splits = 1;
         a.t_run = (int)ceil_div(a.T, splits);
         if (a.t_run < 1) a.t_run = 1;
