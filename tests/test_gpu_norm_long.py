@@ -66,3 +66,27 @@ def test_a_clip_of_the_longest_length():
         for got, want in ((y, 1.25 * xh(s) - 0.5), (dx, 1.25 * rstd * (dy[0, s].double() - sum_b / T - xh(s) * (sum_w / T)))):
             err = (got[0, s].double() - want).abs()
             assert bool((err <= (2.0 ** -8 + 4e-6) * want.abs().clamp_min(1.0)).all())
+
+
+def test_many_rows_of_more_tokens_than_a_plain_sum_takes():
+    """More rows than workgroups, so that one takes rows one after the other, each of 150 tokens a thread: sums are folded within a row and begin anew with the next."""
+    B, T, C = 2049, 150, 2048
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.empty(B, T, C, device=DEV, dtype=torch.bfloat16)
+    for b in range(0, B, 512):
+        x[b:b + 512] = torch.randn(x[b:b + 512].shape, generator=gen, device=DEV).bfloat16() * 1.5 + 0.25
+    x[2048] = x[2048] * 3 - 7
+    x[0] += 5
+    y, stats = torch.empty_like(x), torch.empty(B, 2, 2, device=DEV)
+    d = K.make_norm_desc(B, T, C, 2, act=1, bf16=1)
+    ws = torch.empty(max(256, K.cawn_group_norm_workspace_bytes(d)), dtype=torch.uint8, device=DEV)
+    K.check(K.cawn_group_norm_fwd(d, x, None, None, y, stats, ws))
+    torch.cuda.synchronize()
+    for b in (0, 1, 1024, 2047, 2048):
+        v = x[b].double().view(T, 2, C // 2)
+        mean, var = v.mean((0, 2)), v.var((0, 2), correction=0)
+        rstd = (var + 1e-5) ** -0.5
+        assert bool(((stats[b, :, 0].double() - mean).abs() <= 4e-6 * mean.abs().clamp_min(1.0)).all()) and bool(((stats[b, :, 1].double() / rstd - 1).abs() <= 4e-6).all())
+        z = (v - mean[None, :, None]) * rstd[None, :, None]
+        want = (z * torch.sigmoid(z)).view(T, C)
+        assert bool(((y[b].double() - want).abs() <= (2.0 ** -8 + 1e-5) * want.abs().clamp_min(1.0)).all())
