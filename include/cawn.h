@@ -486,6 +486,135 @@ int cawn_dropout_add_fwd(const cawn_dropout_desc *d, const void *x, const void *
 /* dx = keep dy / (1 - p); the gradient of the residual is dy itself. */
 int cawn_dropout_add_bwd(const cawn_dropout_desc *d, const void *dy, const uint64_t *rng, void *dx, void *stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * A third recurrent mixer, the selective state space scan, with the short causal convolution in front of it, and the root-mean-square
+ * norm joined with the residual addition that a layer begins with.  The rules at the head of this file hold; the workspaces of these
+ * calls need no initialisation and may be shared by calls ordered on one stream (two captured graphs that run at once are not).
+ * ------------------------------------------------------------------------------------------------ */
+
+/*
+ * Selective state space scan.  Per batch row b, channel c with its N states S, and group g = c / (D / G) of the channels that share B and C:
+ *     delta = softplus(dt[t][c] + dt_bias[c])       dt_softplus = 0: without softplus
+ *     S[t]  = exp(delta A[c]) S[t-1] + delta x[t][c] Bm[t][g]
+ *     y[t]  = (Cm[t][g] . S[t] + Dskip[c] x[t][c]) z[t][c] / (1 + e^-z[t][c])
+ */
+typedef struct cawn_scan_desc {
+    int32_t B, L;         /* batch rows; tokens in THIS call (0 allowed: the state is passed through)               */
+    int32_t D, N;         /* channels, and states of each, 1..128 (beyond: CAWN_EUNSUPPORTED)                       */
+    int32_t G;            /* groups of channels that share Bm and Cm; divides D; 0 = 1                              */
+    int32_t bf16;         /* 0: x, dt, Bm, Cm, z, y and their gradients are fp32; 1: bfloat16.  A, Dskip, dt_bias, the state, the
+                             checkpoint and their gradients are fp32 either way, as is all arithmetic                */
+    int32_t dt_softplus;  /* 1: softplus (above); 0: delta = dt + dt_bias                                           */
+    int32_t accumulate_param_grads;     /* backward: 0 overwrite, 1 add into dA, dDskip, ddt_bias                    */
+    int64_t x_stride_b, x_stride_t;     /* element strides of x, dx [B][L][D]; 0 = dense (t stride D, b stride       */
+    int64_t dt_stride_b, dt_stride_t;   /*   L * t stride); of dt, ddt [B][L][D];                                    */
+    int64_t bc_stride_b, bc_stride_t;   /*   of Bm, Cm, dBm, dCm [B][L][G][N];                                       */
+    int64_t z_stride_b, z_stride_t;     /*   of z, dz [B][L][D];                                                     */
+    int64_t y_stride_b, y_stride_t;     /*   of y, dy [B][L][D].  Values of one token lie side by side               */
+} cawn_scan_desc;
+
+/* The state [B][D][N] fp32 (its gradient alike).  0 for an invalid descriptor, as the two below. */
+size_t cawn_selective_scan_state_bytes(const cawn_scan_desc *d);
+/* What the forward leaves for the backward: the states before every run of 16 tokens, Bm and Cm in fp32. */
+size_t cawn_selective_scan_ckpt_bytes(const cawn_scan_desc *d);
+/* Scratch of either direction, 256-byte aligned. */
+size_t cawn_selective_scan_workspace_bytes(const cawn_scan_desc *d);
+
+/*
+ * Forward: prefill, training, and single tokens (L = 1: one pass over the state).
+ *   A [D][N], Dskip [D] or NULL (0), dt_bias [D] or NULL (0): fp32, dense.  A is the rate itself, below 0 in use
+ *   z          or NULL: y without its last factor
+ *   lengths    device int32 [B] or NULL: row b has lengths[b] tokens (clamped to 0..L).  Of the rest nothing is read; y is 0 there
+ *       and the state is that behind the last token.  0: an unused slot, whose state is passed through
+ *   state_in   or NULL (zeros); state_out or NULL; they may be the same
+ *   ckpt       cawn_selective_scan_ckpt_bytes(), 16-byte aligned, or NULL when no backward will follow
+ *   workspace  >= cawn_selective_scan_workspace_bytes(d); calls of up to 16 tokens without ckpt use none
+ * Inputs must not alias outputs (but for the state).  A value that is not finite reaches the tokens behind it, as the formula has it; one that
+ * the formula makes infinite may be NaN.
+ */
+int cawn_selective_scan_fwd(const cawn_scan_desc *d, const void *x, const void *dt, const float *A, const void *Bm, const void *Cm,
+                            const float *Dskip, const void *z, const float *dt_bias, const int32_t *lengths, const void *state_in,
+                            void *y, void *state_out, void *ckpt, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Backward.  x .. lengths as the forward had them, ckpt as it wrote it; dy, dstate_out or NULL (zeros).  dBm, dCm are summed over the
+ * channels of a group, dA, dDskip, ddt_bias over rows and tokens.  Gradients of tokens beyond lengths[b] are 0.  Any of the gradients may be
+ * NULL; dz without z, dDskip without Dskip, ddt_bias without dt_bias are not asked for with a pointer: CAWN_EINVAL.  dstate_in may be
+ * dstate_out.  The same inputs give the same bits.
+ */
+int cawn_selective_scan_bwd(const cawn_scan_desc *d, const void *x, const void *dt, const float *A, const void *Bm, const void *Cm,
+                            const float *Dskip, const void *z, const float *dt_bias, const int32_t *lengths, const void *ckpt,
+                            const void *dy, const void *dstate_out, void *dx, void *ddt, float *dA, void *dBm, void *dCm, float *dDskip,
+                            void *dz, float *ddt_bias, void *dstate_in, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Short causal convolution along the tokens, each channel by itself, with an activation:
+ *     y[b][t][c] = act(bias[c] + sum_{i<k} w[c][i] x[b][t-(k-1)+i][c])
+ * (cawn_syntax_conv is the layer's own, with its clamp and forward alone.)
+ */
+typedef struct cawn_conv_desc {
+    int32_t B, L, C, k;                 /* rows, tokens of THIS call (0 allowed: the state is passed through), channels, taps 1..4 (beyond:
+                                           CAWN_EUNSUPPORTED)                                                                          */
+    int32_t act;                        /* 0 none, 1 SiLU                                                                              */
+    int32_t bf16;                       /* 1: x, y, dy, dx are bfloat16, else fp32; taps, bias, state and their gradients are fp32     */
+    int32_t accumulate_param_grads;     /* backward: 0 overwrite, 1 add into dw, dbias                                                 */
+    int32_t reserved;                   /* 0                                                                                           */
+    int64_t x_stride_b, x_stride_t;     /* element strides of x and dx; 0 = dense; channels lie side by side                           */
+    int64_t y_stride_b, y_stride_t;     /* of y and dy                                                                                 */
+} cawn_conv_desc;
+
+/* The state [B][k-1][C] fp32: the k-1 inputs before the next token, the oldest first. */
+size_t cawn_causal_conv_state_bytes(const cawn_conv_desc *d);
+size_t cawn_causal_conv_workspace_bytes(const cawn_conv_desc *d);       /* of the backward; the forward uses none */
+/*
+ *   w [C][k] fp32, bias [C] fp32 or NULL (0)
+ *   lengths    as in cawn_selective_scan_fwd
+ *   state_in   or NULL (zeros); state_out or NULL; they may be the same
+ * x must not alias y.
+ */
+int cawn_causal_conv_fwd(const cawn_conv_desc *d, const void *x, const float *w, const float *bias, const int32_t *lengths,
+                         const void *state_in, void *y, void *state_out, void *stream);
+/* dx, dw, dbias, dstate_in: any may be NULL; dstate_out or NULL (zeros); dstate_in may be dstate_out.  The sums of dw and dbias run in a fixed
+ * order. */
+int cawn_causal_conv_bwd(const cawn_conv_desc *d, const void *x, const float *w, const float *bias, const int32_t *lengths,
+                         const void *state_in, const void *dy, const void *dstate_out, void *dx, float *dw, float *dbias, void *dstate_in,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Root-mean-square norm joined with the residual addition in front of it, rows x C:
+ *     h = x + residual     (rounded to h's type: the residual stream goes on from it)
+ *     y = weight h / sqrt(mean(h^2) + eps)
+ * and, on request, y in 8 bits for a product in 8 bits:
+ *     scales[r][j] = max |y| / 448 over the j-th `block` channels of the row;  q = y / scale rounded to OCP e4m3 (y is not rounded before)
+ * A block of zeros (or of values below 448 x 2^-126) has the scale 0 and zeros; one that holds a NaN has a NaN for its scale.
+ */
+typedef struct cawn_rms_desc {
+    int64_t rows;                       /* 0 allowed (nothing is read or written but dweight, which is 0 then)                          */
+    int32_t C;                          /* 1..32768 (beyond: CAWN_EUNSUPPORTED)                                                        */
+    int32_t bf16;                       /* 1: x, y, dy, dx are bfloat16, else fp32                                                     */
+    int32_t residual_bf16;              /* 1: residual, h, dh, dresidual are bfloat16, else fp32.  weight, rstd, scales, dweight are fp32 */
+    int32_t block;                      /* channels that share a scale, a multiple of 16; 0: the whole row                             */
+    float eps;
+    int32_t accumulate_param_grads;     /* backward: 0 overwrite, 1 add into dweight                                                   */
+    int64_t x_stride, residual_stride, y_stride;    /* element strides of rows; 0 = C.  dx has x's; h, dh and dresidual have residual's; dy, q y's */
+} cawn_rms_desc;
+
+size_t cawn_rms_norm_add_workspace_bytes(const cawn_rms_desc *d);       /* of the backward; the forward uses none */
+/*
+ * weight [C] or NULL (1); residual or NULL (h = x); h or NULL (it is not kept); y, q either or both, the other NULL; scales [rows][ceil(C / block)]
+ * (one a row with block 0), asked for with q and only with it; rstd [rows] = 1 / sqrt(mean + eps) for the backward, or NULL.
+ * x or residual may be h, x may be y (in place, with the same type and stride).
+ */
+int cawn_rms_norm_add_fwd(const cawn_rms_desc *d, const void *x, const void *residual, const float *weight, void *h, void *y, void *q,
+                          float *scales, float *rstd, void *stream);
+/*
+ * h and rstd as the forward wrote them (without a residual and with equal types h is x); dy; dh, the gradient that reaches h from later, or NULL (0).
+ * dx and dresidual hold the same gradient in their types; dx, dresidual, dweight: any may be NULL.  dy may be dx, dh may be dresidual.  The sums of
+ * dweight run in a fixed order.
+ */
+int cawn_rms_norm_add_bwd(const cawn_rms_desc *d, const void *h, const float *weight, const float *rstd, const void *dy, const void *dh,
+                          void *dx, void *dresidual, float *dweight, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

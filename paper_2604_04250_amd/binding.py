@@ -26,7 +26,11 @@ EXPORTS = ["cawn_state_bytes", "cawn_workspace_bytes", "cawn_ckpt_bytes", "cawn_
            "cawn_phase_accumulate_valve_bwd", "cawn_stream_copy", "cawn_phase_accumulate_fwd_static",
            "cawn_delta_state_bytes", "cawn_delta_ckpt_bytes", "cawn_delta_workspace_bytes", "cawn_delta_rule_fwd",
            "cawn_delta_rule_bwd", "cawn_group_norm_workspace_bytes", "cawn_group_norm_fwd", "cawn_group_norm_bwd",
-           "cawn_dropout_add_fwd", "cawn_dropout_add_bwd"]
+           "cawn_dropout_add_fwd", "cawn_dropout_add_bwd",
+           "cawn_selective_scan_state_bytes", "cawn_selective_scan_ckpt_bytes", "cawn_selective_scan_workspace_bytes",
+           "cawn_selective_scan_fwd", "cawn_selective_scan_bwd", "cawn_causal_conv_state_bytes", "cawn_causal_conv_workspace_bytes",
+           "cawn_causal_conv_fwd", "cawn_causal_conv_bwd", "cawn_rms_norm_add_workspace_bytes", "cawn_rms_norm_add_fwd",
+           "cawn_rms_norm_add_bwd"]
 
 
 class cawn_desc(C.Structure):
@@ -71,6 +75,26 @@ class cawn_dropout_desc(C.Structure):
                 ("y_stride", C.c_int64), ("p", C.c_double), ("bf16", C.c_int32), ("reserved", C.c_int32)]
 
 
+class cawn_scan_desc(C.Structure):
+    _fields_ = [("B", C.c_int32), ("L", C.c_int32), ("D", C.c_int32), ("N", C.c_int32), ("G", C.c_int32), ("bf16", C.c_int32),
+                ("dt_softplus", C.c_int32), ("accumulate_param_grads", C.c_int32),
+                ("x_stride_b", C.c_int64), ("x_stride_t", C.c_int64), ("dt_stride_b", C.c_int64), ("dt_stride_t", C.c_int64),
+                ("bc_stride_b", C.c_int64), ("bc_stride_t", C.c_int64), ("z_stride_b", C.c_int64), ("z_stride_t", C.c_int64),
+                ("y_stride_b", C.c_int64), ("y_stride_t", C.c_int64)]
+
+
+class cawn_conv_desc(C.Structure):
+    _fields_ = [("B", C.c_int32), ("L", C.c_int32), ("C", C.c_int32), ("k", C.c_int32), ("act", C.c_int32), ("bf16", C.c_int32),
+                ("accumulate_param_grads", C.c_int32), ("reserved", C.c_int32),
+                ("x_stride_b", C.c_int64), ("x_stride_t", C.c_int64), ("y_stride_b", C.c_int64), ("y_stride_t", C.c_int64)]
+
+
+class cawn_rms_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("C", C.c_int32), ("bf16", C.c_int32), ("residual_bf16", C.c_int32), ("block", C.c_int32),
+                ("eps", C.c_float), ("accumulate_param_grads", C.c_int32),
+                ("x_stride", C.c_int64), ("residual_stride", C.c_int64), ("y_stride", C.c_int64)]
+
+
 def make_delta_desc(B, L, H, K, V, Hk=0, scale=1.0, qk_norm=0, norm_eps=1e-6, bf16=0, qk_stride_b=0, qk_stride_t=0,
                     v_stride_b=0, v_stride_t=0, o_stride_b=0, o_stride_t=0) -> cawn_delta_desc:
     return cawn_delta_desc(B, L, H, Hk, K, V, bf16, qk_norm, scale, norm_eps, qk_stride_b, qk_stride_t, v_stride_b, v_stride_t,
@@ -84,6 +108,22 @@ def make_norm_desc(B, T, C, groups, act=0, eps=1e-5, bf16=0, accumulate_param_gr
 
 def make_dropout_desc(rows, cols, p=0.1, bf16=0, x_stride=0, residual_stride=0, y_stride=0) -> cawn_dropout_desc:
     return cawn_dropout_desc(rows, cols, x_stride, residual_stride, y_stride, p, bf16, 0)
+
+
+def make_scan_desc(B, L, D, N, G=1, dt_softplus=1, bf16=0, accumulate_param_grads=0, x_stride_b=0, x_stride_t=0, dt_stride_b=0,
+                   dt_stride_t=0, bc_stride_b=0, bc_stride_t=0, z_stride_b=0, z_stride_t=0, y_stride_b=0, y_stride_t=0) -> cawn_scan_desc:
+    return cawn_scan_desc(B, L, D, N, G, bf16, dt_softplus, accumulate_param_grads, x_stride_b, x_stride_t, dt_stride_b, dt_stride_t,
+                          bc_stride_b, bc_stride_t, z_stride_b, z_stride_t, y_stride_b, y_stride_t)
+
+
+def make_conv_desc(B, L, C, k, act=0, bf16=0, accumulate_param_grads=0, x_stride_b=0, x_stride_t=0, y_stride_b=0,
+                   y_stride_t=0) -> cawn_conv_desc:
+    return cawn_conv_desc(B, L, C, k, act, bf16, accumulate_param_grads, 0, x_stride_b, x_stride_t, y_stride_b, y_stride_t)
+
+
+def make_rms_desc(rows, C, eps=1e-5, bf16=0, residual_bf16=0, block=0, accumulate_param_grads=0, x_stride=0, residual_stride=0,
+                  y_stride=0) -> cawn_rms_desc:
+    return cawn_rms_desc(rows, C, bf16, residual_bf16, block, eps, accumulate_param_grads, x_stride, residual_stride, y_stride)
 
 
 _lib = None
@@ -135,12 +175,18 @@ def lib() -> C.CDLL:
                                                       [C.c_size_t, C.c_int32, C.c_void_p])
         L.cawn_stream_copy.argtypes = [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
         for n, ty in (("cawn_delta_state_bytes", cawn_delta_desc), ("cawn_delta_ckpt_bytes", cawn_delta_desc),
-                      ("cawn_delta_workspace_bytes", cawn_delta_desc), ("cawn_group_norm_workspace_bytes", cawn_norm_desc)):
+                      ("cawn_delta_workspace_bytes", cawn_delta_desc), ("cawn_group_norm_workspace_bytes", cawn_norm_desc),
+                      ("cawn_selective_scan_state_bytes", cawn_scan_desc), ("cawn_selective_scan_ckpt_bytes", cawn_scan_desc),
+                      ("cawn_selective_scan_workspace_bytes", cawn_scan_desc), ("cawn_causal_conv_state_bytes", cawn_conv_desc),
+                      ("cawn_causal_conv_workspace_bytes", cawn_conv_desc), ("cawn_rms_norm_add_workspace_bytes", cawn_rms_desc)):
             getattr(L, n).restype = C.c_size_t
             getattr(L, n).argtypes = [C.POINTER(ty)]
         for n, ty, pointers, sized in (("cawn_delta_rule_fwd", cawn_delta_desc, 11, True), ("cawn_delta_rule_bwd", cawn_delta_desc, 16, True),
                                        ("cawn_group_norm_fwd", cawn_norm_desc, 6, True), ("cawn_group_norm_bwd", cawn_norm_desc, 9, True),
-                                       ("cawn_dropout_add_fwd", cawn_dropout_desc, 4, False), ("cawn_dropout_add_bwd", cawn_dropout_desc, 3, False)):
+                                       ("cawn_dropout_add_fwd", cawn_dropout_desc, 4, False), ("cawn_dropout_add_bwd", cawn_dropout_desc, 3, False),
+                                       ("cawn_selective_scan_fwd", cawn_scan_desc, 14, True), ("cawn_selective_scan_bwd", cawn_scan_desc, 22, True),
+                                       ("cawn_causal_conv_fwd", cawn_conv_desc, 7, False), ("cawn_causal_conv_bwd", cawn_conv_desc, 12, True),
+                                       ("cawn_rms_norm_add_fwd", cawn_rms_desc, 8, False), ("cawn_rms_norm_add_bwd", cawn_rms_desc, 9, True)):
             getattr(L, n).argtypes = [C.POINTER(ty)] + [C.c_void_p] * pointers + [C.c_size_t] * sized + [C.c_void_p]
         L.cawn_phase_accumulate_fwd_static.argtypes = [C.POINTER(cawn_desc)] + [C.c_void_p] * 13
         try:
@@ -149,7 +195,7 @@ def lib() -> C.CDLL:
             raise RuntimeError("the marshalling module _cawn_call is missing: build it with __graft_entry__.build(); "
                                "there is no fallback path") from e
         _cawn_call.setup(cawn_desc, getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device), _raw_stream())
-        _cawn_call.setup_ops((cawn_delta_desc, cawn_norm_desc, cawn_dropout_desc))
+        _cawn_call.setup_ops((cawn_delta_desc, cawn_norm_desc, cawn_dropout_desc, cawn_scan_desc, cawn_conv_desc, cawn_rms_desc))
         for n in EXPORTS:
             if n.startswith("cawn_phase_accumulate") or n in _OPS:
                 _entry[n] = C.cast(getattr(L, n), C.c_void_p).value
@@ -173,7 +219,8 @@ def _enter(name, form, *args) -> int:
 
 # operators with a descriptor of their own: 2 * the descriptor's place in setup_ops, + 1 where a workspace comes last
 _OPS = {"cawn_delta_rule_fwd": 1, "cawn_delta_rule_bwd": 1, "cawn_group_norm_fwd": 3, "cawn_group_norm_bwd": 3,
-        "cawn_dropout_add_fwd": 4, "cawn_dropout_add_bwd": 4}
+        "cawn_dropout_add_fwd": 4, "cawn_dropout_add_bwd": 4, "cawn_selective_scan_fwd": 7, "cawn_selective_scan_bwd": 7,
+        "cawn_causal_conv_fwd": 8, "cawn_causal_conv_bwd": 9, "cawn_rms_norm_add_fwd": 10, "cawn_rms_norm_add_bwd": 11}
 
 
 def _enter_op(name, *args) -> int:
@@ -385,6 +432,61 @@ def cawn_dropout_add_fwd(d, x, residual, rng, y, stream=None) -> int:
 
 def cawn_dropout_add_bwd(d, dy, rng, dx, stream=None) -> int:
     return _enter_op("cawn_dropout_add_bwd", d, dy, rng, dx, stream)
+
+
+def cawn_selective_scan_state_bytes(d: cawn_scan_desc) -> int:
+    return int(lib().cawn_selective_scan_state_bytes(C.byref(d)))
+
+
+def cawn_selective_scan_ckpt_bytes(d: cawn_scan_desc) -> int:
+    return int(lib().cawn_selective_scan_ckpt_bytes(C.byref(d)))
+
+
+def cawn_selective_scan_workspace_bytes(d: cawn_scan_desc) -> int:
+    return int(lib().cawn_selective_scan_workspace_bytes(C.byref(d)))
+
+
+def cawn_selective_scan_fwd(d, x, dt, A, Bm, Cm, Dskip, z, dt_bias, lengths, state_in, y, state_out, ckpt, workspace, stream=None) -> int:
+    """x, dt, Bm, Cm, z, y: fp32 tensors, or torch.bfloat16 with d.bf16 = 1; A, Dskip, dt_bias, states fp32; lengths torch.int32."""
+    return _enter_op("cawn_selective_scan_fwd", d, x, dt, A, Bm, Cm, Dskip, z, dt_bias, lengths, state_in, y, state_out, ckpt, workspace,
+                     stream)
+
+
+def cawn_selective_scan_bwd(d, x, dt, A, Bm, Cm, Dskip, z, dt_bias, lengths, ckpt, dy, dstate_out, dx, ddt, dA, dBm, dCm, dDskip, dz,
+                            ddt_bias, dstate_in, workspace, stream=None) -> int:
+    """dy and dx, ddt, dBm, dCm, dz: the type of x; the other gradients fp32."""
+    return _enter_op("cawn_selective_scan_bwd", d, x, dt, A, Bm, Cm, Dskip, z, dt_bias, lengths, ckpt, dy, dstate_out, dx, ddt, dA, dBm, dCm,
+                     dDskip, dz, ddt_bias, dstate_in, workspace, stream)
+
+
+def cawn_causal_conv_state_bytes(d: cawn_conv_desc) -> int:
+    return int(lib().cawn_causal_conv_state_bytes(C.byref(d)))
+
+
+def cawn_causal_conv_workspace_bytes(d: cawn_conv_desc) -> int:
+    return int(lib().cawn_causal_conv_workspace_bytes(C.byref(d)))
+
+
+def cawn_causal_conv_fwd(d, x, w, bias, lengths, state_in, y, state_out, stream=None) -> int:
+    """x, y: fp32 tensors, or torch.bfloat16 with d.bf16 = 1; w, bias, states fp32; lengths torch.int32."""
+    return _enter_op("cawn_causal_conv_fwd", d, x, w, bias, lengths, state_in, y, state_out, stream)
+
+
+def cawn_causal_conv_bwd(d, x, w, bias, lengths, state_in, dy, dstate_out, dx, dw, dbias, dstate_in, workspace, stream=None) -> int:
+    return _enter_op("cawn_causal_conv_bwd", d, x, w, bias, lengths, state_in, dy, dstate_out, dx, dw, dbias, dstate_in, workspace, stream)
+
+
+def cawn_rms_norm_add_workspace_bytes(d: cawn_rms_desc) -> int:
+    return int(lib().cawn_rms_norm_add_workspace_bytes(C.byref(d)))
+
+
+def cawn_rms_norm_add_fwd(d, x, residual, weight, h, y, q, scales, rstd, stream=None) -> int:
+    """x, y: fp32 tensors, or torch.bfloat16 with d.bf16 = 1; residual, h: the same by d.residual_bf16; q torch.float8_e4m3fn; the rest fp32."""
+    return _enter_op("cawn_rms_norm_add_fwd", d, x, residual, weight, h, y, q, scales, rstd, stream)
+
+
+def cawn_rms_norm_add_bwd(d, h, weight, rstd, dy, dh, dx, dresidual, dweight, workspace, stream=None) -> int:
+    return _enter_op("cawn_rms_norm_add_bwd", d, h, weight, rstd, dy, dh, dx, dresidual, dweight, workspace, stream)
 
 
 def alloc_workspace(d: cawn_desc, device="cuda:0") -> torch.Tensor:

@@ -163,13 +163,20 @@ static PyObject *call(PyObject *self, PyObject *const *args, Py_ssize_t n)
 #define V4 V3, void *
 #define P6 P4, p[4], p[5]
 #define V6 V4, void *, void *
-#define P9 P6, p[6], p[7], p[8]
-#define V9 V6, void *, void *, void *
+#define P7 P6, p[6]
+#define V7 V6, void *
+#define P8 P7, p[7]
+#define V8 V7, void *
+#define P9 P8, p[8]
+#define V9 V8, void *
 #define P11 P9, p[9], p[10]
 #define V11 V9, void *, void *
+#define P12 P11, p[11]
+#define V12 V11, void *
 
 static PyObject *op_types;                     /* the operators' descriptor types */
-static const Py_ssize_t op_sizes[] = {sizeof(cawn_delta_desc), sizeof(cawn_norm_desc), sizeof(cawn_dropout_desc)};
+static const Py_ssize_t op_sizes[] = {sizeof(cawn_delta_desc), sizeof(cawn_norm_desc), sizeof(cawn_dropout_desc),
+                                      sizeof(cawn_scan_desc), sizeof(cawn_conv_desc), sizeof(cawn_rms_desc)};
 
 static PyObject *call_op(PyObject *self, PyObject *const *args, Py_ssize_t n)
 {
@@ -207,7 +214,8 @@ static PyObject *call_op(PyObject *self, PyObject *const *args, Py_ssize_t n)
     int r = 0, known = 1;
     Py_BEGIN_ALLOW_THREADS
     switch (np) {
-        OP(3, P3, V3) OP(4, P4, V4) OP(6, P6, V6) OP(9, P9, V9) OP(11, P11, V11) OP(16, P16, V16)
+        OP(3, P3, V3) OP(4, P4, V4) OP(6, P6, V6) OP(7, P7, V7) OP(8, P8, V8) OP(9, P9, V9) OP(11, P11, V11) OP(12, P12, V12) OP(14, P14, V14)
+        OP(16, P16, V16) OP(22, P22, V22)
     default: known = 0;
     }
     Py_END_ALLOW_THREADS

@@ -1,0 +1,411 @@
+// Short causal convolution along the tokens with an activation, channels last, forward and backward.
+//
+// Forward: z[t] = bias + sum_i w[i] x[t-(k-1)+i], y = act(z).
+// Backward: dz = dy act'(z) with z made again, dx[t] = sum_i w[k-1-i] dz[t+i], dw[i] = sum_t dz[t] x[t-(k-1)+i], db = sum_t dz[t].
+//
+// A thread takes VEC adjacent channels (16 bytes) along a run of tokens; the k - 1 inputs before the run's first token are read again, and backward
+// the k - 1 tokens behind its last.  Bound by memory.
+// The row's state (the k - 1 inputs before its first token, in fp32) is read and replaced by the thread of the row's first run alone.
+#include "cawn_sums.hpp"
+
+using namespace cawn::ops;
+
+namespace {
+
+constexpr int K_MAX = 4;
+
+struct ConvArgs {
+    const void *x, *dy;
+    const float *w, *bias, *state_in, *dstate_out;
+    const int32_t *lengths;
+    void *y, *dx;
+    float *state_out, *dstate_in, *part;
+    int B, L, C, act;
+    long long xsb, xst, ysb, yst;
+    int units;              // of VEC channels in a row
+    int run;                // tokens of a run
+    long long runs;         // of a row
+    int ub, rb, ublocks;    // backward: units and runs of a workgroup, workgroups side by side
+    long long rblocks;
+};
+
+__device__ inline int row_length(const ConvArgs &a, int b)
+{
+    const int n = a.lengths ? a.lengths[b] : a.L;
+    return n < 0 ? 0 : n < a.L ? n : a.L;
+}
+
+__device__ inline float sigmoid_f(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+
+template <int K, int VEC> struct Taps {
+    float w[K][VEC], b[VEC];
+    __device__ Taps(const ConvArgs &a, int c)
+    {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+#pragma unroll
+            for (int i = 0; i < K; ++i) w[i][j] = a.w[(long long)(c + j) * K + i];
+            b[j] = a.bias ? a.bias[c + j] : 0.f;
+        }
+    }
+};
+
+// Input `back` (1 .. K - 1) places before the row's first token
+template <int K, int VEC> __device__ inline void before_row(const ConvArgs &a, int b, int back, int c, float (&x)[VEC])
+{
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) x[j] = a.state_in ? a.state_in[((long long)b * (K - 1) + (K - 1 - back)) * a.C + c + j] : 0.f;
+}
+
+template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void conv_forward(const ConvArgs a)
+{
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x, rest = id / a.units;
+    const int c = (int)(id - rest * a.units) * VEC;
+    const long long bl = rest / a.runs;
+    if (bl >= a.B) return;
+    const int b = (int)bl, n = row_length(a, b);
+    const long long t0 = (rest - bl * a.runs) * a.run, t1 = min((long long)n, t0 + a.run), end = min((long long)a.L, t0 + a.run);
+    const T *x = (const T *)a.x + b * a.xsb + c;
+    T *y = (T *)a.y + b * a.ysb + c;
+    const Taps<K, VEC> p(a, c);
+    float win[K][VEC];          // the K inputs that a token sees, the newest last
+#pragma unroll
+    for (int i = 1; i < K; ++i) {
+        const long long t = t0 - (K - i);
+        if (t >= 0 && t < n) load_n<T, VEC>(x + t * a.xst, win[i]);
+        else if (t < 0) before_row<K, VEC>(a, b, (int)-t, c, win[i]);
+        else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) win[i][j] = 0.f;
+        }
+    }
+    if (t0 == 0 && K > 1 && a.state_out) {
+        // the last K - 1 of what came before and the row's own; all is read before any is written
+        float s[K > 1 ? K - 1 : 1][VEC];
+#pragma unroll
+        for (int i = 0; i < K - 1; ++i) {
+            const long long t = (long long)n - (K - 1) + i;
+            if (t >= 0) load_n<T, VEC>(x + t * a.xst, s[i]);
+            else before_row<K, VEC>(a, b, (int)-t, c, s[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < K - 1; ++i)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) a.state_out[((long long)b * (K - 1) + i) * a.C + c + j] = s[i][j];
+    }
+    for (long long t = t0; t < t1; ++t) {
+#pragma unroll
+        for (int i = 0; i + 1 < K; ++i)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) win[i][j] = win[i + 1][j];
+        load_n<T, VEC>(x + t * a.xst, win[K - 1]);
+        float z[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            z[j] = p.b[j];
+#pragma unroll
+            for (int i = 0; i < K; ++i) z[j] = fmaf(p.w[i][j], win[i][j], z[j]);
+            if (a.act) z[j] *= sigmoid_f(z[j]);
+        }
+        store_n<T, VEC>(y + t * a.yst, z);
+    }
+    for (long long t = max(t0, (long long)n); t < end; ++t) {
+        const float z[VEC] = {};
+        store_n<T, VEC>(y + t * a.yst, z);
+    }
+}
+
+// dz of token t of the row, from the inputs that it sees
+template <typename T, int K, int VEC> __device__ inline void slope(const ConvArgs &a, const Taps<K, VEC> &p, const float (&win)[K][VEC], const float (&dy)[VEC], float (&dz)[VEC])
+{
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        dz[j] = dy[j];
+        if (a.act) {
+            float z = p.b[j];
+#pragma unroll
+            for (int i = 0; i < K; ++i) z = fmaf(p.w[i][j], win[i][j], z);
+            const float f = sigmoid_f(z);
+            dz[j] *= f * fmaf(z, 1.f - f, 1.f);
+        }
+    }
+}
+
+template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void conv_backward(const ConvArgs a)
+{
+    __shared__ float sh[256 * VEC];
+    const int unit = threadIdx.x % a.ub, row = threadIdx.x / a.ub;
+    const long long rblk = blockIdx.x / a.ublocks;
+    const int u = (int)(blockIdx.x - rblk * a.ublocks) * a.ub + unit;
+    const int c = (u < a.units ? u : 0) * VEC;
+    const Taps<K, VEC> p(a, c);
+    float dw[K][VEC], db[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        db[j] = 0.f;
+#pragma unroll
+        for (int i = 0; i < K; ++i) dw[i][j] = 0.f;
+    }
+    const long long all = a.runs * a.B;
+    for (long long rr = rblk * a.rb + row; u < a.units && row < a.rb && rr < all; rr += a.rblocks * a.rb) {
+        const int b = (int)(rr / a.runs), n = row_length(a, b);
+        const long long t0 = (rr - b * a.runs) * a.run, t1 = min((long long)n, t0 + a.run), end = min((long long)a.L, t0 + a.run);
+        const T *x = (const T *)a.x + b * a.xsb + c, *dyp = (const T *)a.dy + b * a.ysb + c;
+        T *dx = a.dx ? (T *)a.dx + b * a.xsb + c : nullptr;
+        float win[K][VEC], dzs[K][VEC];     // the inputs that a token sees; dz of it and the K - 1 before it, the newest last
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) dzs[i][j] = 0.f;
+#pragma unroll
+        for (int i = 1; i < K; ++i) {
+            const long long t = t0 - (K - i);
+            if (t0 >= t1) continue;
+            if (t >= 0) load_n<T, VEC>(x + t * a.xst, win[i]);
+            else before_row<K, VEC>(a, b, (int)-t, c, win[i]);
+        }
+        // up to K - 1 tokens behind the run: dx of its last tokens needs their dz
+        for (long long t = t0; t < t1 + K - 1 && t0 < t1; ++t) {
+#pragma unroll
+            for (int i = 0; i + 1 < K; ++i)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) win[i][j] = win[i + 1][j], dzs[i][j] = dzs[i + 1][j];
+            if (t < n) {
+                float dy[VEC];
+                load_n<T, VEC>(x + t * a.xst, win[K - 1]);
+                load_n<T, VEC>(dyp + t * a.yst, dy);
+                slope<T, K, VEC>(a, p, win, dy, dzs[K - 1]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) dzs[K - 1][j] = 0.f;
+            }
+            if (t < t1) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    db[j] += dzs[K - 1][j];
+#pragma unroll
+                    for (int i = 0; i < K; ++i) dw[i][j] = fmaf(dzs[K - 1][j], win[i][j], dw[i][j]);
+                }
+            }
+            const long long at = t - (K - 1);       // its dz have all come
+            if (dx && at >= t0) {
+                float d[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    d[j] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < K; ++i) d[j] = fmaf(p.w[K - 1 - i][j], dzs[i][j], d[j]);
+                }
+                const long long left = at - (n - (K - 1));
+                if (K > 1 && a.dstate_out && left >= 0) {       // the token is part of the state behind the row
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) d[j] += a.dstate_out[((long long)b * (K - 1) + left) * a.C + c + j];
+                }
+                store_n<T, VEC>(dx + at * a.xst, d);
+            }
+        }
+        if (dx) {
+            for (long long t = max(t0, (long long)n); t < end; ++t) {
+                const float z[VEC] = {};
+                store_n<T, VEC>(dx + t * a.xst, z);
+            }
+        }
+    }
+    if (!a.part) return;
+    // the workgroup's runs, in their order: [K + 1][C] a workgroup
+#pragma unroll
+    for (int i = 0; i <= K; ++i) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) sh[threadIdx.x * VEC + j] = i < K ? dw[i < K ? i : 0][j] : db[j];
+        __syncthreads();
+        if (row == 0 && u < a.units) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                float v = 0.f;
+                for (int q = 0; q < a.rb; ++q) v += sh[(q * a.ub + unit) * VEC + j];
+                a.part[(rblk * (K + 1) + i) * a.C + c + j] = v;
+            }
+        }
+    }
+}
+
+// The gradient of the state before the row: what its first K - 1 tokens make of it, and what of it is still there behind the last.
+template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void conv_state_backward(const ConvArgs a)
+{
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x, b = id / a.units;
+    if (b >= a.B) return;
+    const int c = (int)(id - b * a.units) * VEC, n = row_length(a, (int)b);
+    const Taps<K, VEC> p(a, c);
+    float d[K][VEC], win[K][VEC];
+#pragma unroll
+    for (int i = 0; i < K - 1; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) d[i][j] = a.dstate_out && i >= n ? a.dstate_out[(b * (K - 1) + (i - n)) * a.C + c + j] : 0.f;
+#pragma unroll
+    for (int i = 1; i < K; ++i) before_row<K, VEC>(a, (int)b, K - i, c, win[i]);
+#pragma unroll
+    for (int t = 0; t < K - 1; ++t) {
+        if (t >= n) break;
+        float dy[VEC], dz[VEC];
+#pragma unroll
+        for (int i = 0; i + 1 < K; ++i)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) win[i][j] = win[i + 1][j];
+        load_n<T, VEC>((const T *)a.x + b * a.xsb + t * a.xst + c, win[K - 1]);
+        load_n<T, VEC>((const T *)a.dy + b * a.ysb + t * a.yst + c, dy);
+        slope<T, K, VEC>(a, p, win, dy, dz);
+#pragma unroll
+        for (int i = t; i < K - 1; ++i)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) d[i][j] = fmaf(p.w[i - t][j], dz[j], d[i][j]);
+    }
+#pragma unroll
+    for (int i = 0; i < K - 1; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) a.dstate_in[(b * (K - 1) + i) * a.C + c + j] = d[i][j];
+}
+
+struct TapSums {        // column (i, c) of a part's [K + 1][C]
+    float *dw, *db;
+    int C, K;
+    __device__ float *operator()(long long at) const
+    {
+        const int i = (int)(at / C), c = (int)(at - (long long)i * C);
+        return i < K ? (dw ? dw + (long long)c * K + i : nullptr) : (db ? db + c : nullptr);
+    }
+};
+
+// ---------------------------------------------------------------------------------------------- host
+struct Plan {
+    ConvArgs a;
+    int vec, k;
+    long long blocks;
+};
+
+// The geometry must not depend on pointers: the workspace is sized without them.  Rows that do not begin on 16 bytes are taken value by value.
+int plan_of(const cawn_conv_desc *d, bool aligned, bool bwd, Plan *p)
+{
+    if (!d || d->B < 0 || d->L < 0 || d->C <= 0 || d->k <= 0 || d->act < 0 || d->act > 1 || (d->bf16 & ~1) || d->reserved) return CAWN_EINVAL;
+    if (d->k > K_MAX) return CAWN_EUNSUPPORTED;
+    ConvArgs &a = p->a;
+    a = ConvArgs{};
+    a.B = d->B, a.L = d->L, a.C = d->C, a.act = d->act, p->k = d->k;
+    a.xst = d->x_stride_t ? d->x_stride_t : d->C, a.yst = d->y_stride_t ? d->y_stride_t : d->C;
+    if (a.xst < a.C || a.yst < a.C) return CAWN_EINVAL;
+    a.xsb = d->x_stride_b ? d->x_stride_b : a.xst * d->L, a.ysb = d->y_stride_b ? d->y_stride_b : a.yst * d->L;
+    const int most = d->bf16 ? 8 : 4;
+    p->vec = aligned && a.C % most == 0 && a.xst % most == 0 && a.xsb % most == 0 && a.yst % most == 0 && a.ysb % most == 0 ? most : 1;
+    a.units = a.C / p->vec;
+    a.run = bwd ? 32 : 16;
+    a.runs = a.L > 0 ? ceil_div(a.L, a.run) : 1;
+    const long long all = a.runs * a.B;
+    if (all > (1LL << 40) / a.units) return CAWN_EUNSUPPORTED;
+    if (!bwd) p->blocks = ceil_div(all * a.units, 256);
+    else {
+        a.ub = a.units < 32 ? a.units : 32;
+        a.rb = 256 / a.ub;
+        a.ublocks = (int)ceil_div(a.units, a.ub);
+        const long long want = 1024 / a.ublocks > 1 ? 1024 / a.ublocks : 1, there = ceil_div(all, a.rb);
+        a.rblocks = there < want ? there : want;
+        if (a.rblocks < 1) a.rblocks = 1;
+        p->blocks = a.rblocks * a.ublocks;
+    }
+    return p->blocks > 0x7fffffffLL ? CAWN_EUNSUPPORTED : CAWN_OK;
+}
+
+size_t part_bytes(const Plan &p) { return (size_t)p.a.rblocks * (p.k + 1) * p.a.C * 4; }
+
+template <typename T, int K, int VEC> int launch(const Plan &p, bool bwd, hipStream_t s)
+{
+    if (!bwd) hipLaunchKernelGGL((conv_forward<T, K, VEC>), dim3((unsigned)p.blocks), dim3(256), 0, s, p.a);
+    else {
+        if (p.a.dx || p.a.part) hipLaunchKernelGGL((conv_backward<T, K, VEC>), dim3((unsigned)p.blocks), dim3(256), 0, s, p.a);
+        // (behind the other, which reads the gradient of the state that this may replace)
+        if (K > 1 && p.a.dstate_in) hipLaunchKernelGGL((conv_state_backward<T, K, VEC>), dim3((unsigned)ceil_div((long long)p.a.B * p.a.units, 256)), dim3(256), 0, s, p.a);
+    }
+    return launched();
+}
+
+template <typename T, int VEC> int launch_k(const Plan &p, bool bwd, hipStream_t s)
+{
+    switch (p.k) {
+    case 1: return launch<T, 1, VEC>(p, bwd, s);
+    case 2: return launch<T, 2, VEC>(p, bwd, s);
+    case 3: return launch<T, 3, VEC>(p, bwd, s);
+    default: return launch<T, 4, VEC>(p, bwd, s);
+    }
+}
+
+int run(const cawn_conv_desc *d, const Plan &p, bool bwd, hipStream_t s)
+{
+    if (d->bf16) return p.vec > 1 ? launch_k<bf16, 8>(p, bwd, s) : launch_k<bf16, 1>(p, bwd, s);
+    return p.vec > 1 ? launch_k<float, 4>(p, bwd, s) : launch_k<float, 1>(p, bwd, s);
+}
+
+} // namespace
+
+extern "C" {
+
+size_t cawn_causal_conv_state_bytes(const cawn_conv_desc *d)
+{
+    Plan p;
+    return plan_of(d, true, false, &p) != CAWN_OK ? 0 : (size_t)d->B * (d->k - 1) * d->C * 4;
+}
+
+size_t cawn_causal_conv_workspace_bytes(const cawn_conv_desc *d)
+{
+    size_t most = 256;
+    for (int i = 0; i < 2; ++i) {
+        Plan p;
+        if (plan_of(d, i != 0, true, &p) != CAWN_OK) return 0;
+        most = most > part_bytes(p) ? most : part_bytes(p);
+    }
+    return most;
+}
+
+int cawn_causal_conv_fwd(const cawn_conv_desc *d, const void *x, const float *w, const float *bias, const int32_t *lengths, const void *state_in, void *y, void *state_out,
+                         void *stream)
+{
+    Plan p;
+    if (int r = plan_of(d, true, false, &p)) return r;
+    const size_t e = d->bf16 ? 2 : 4;
+    if (!aligned_to(x, e) || !aligned_to(y, e) || !aligned_to(w, 4) || !aligned_to(bias, 4) || !aligned_to(lengths, 4) || !aligned_to(state_in, 4) || !aligned_to(state_out, 4))
+        return CAWN_EINVAL;
+    if (d->B == 0) return CAWN_OK;
+    if (!w || (d->L > 0 && (!x || !y))) return CAWN_EINVAL;
+    if (!aligned_to(x, 16) || !aligned_to(y, 16)) {
+        if (int r = plan_of(d, false, false, &p)) return r;
+    }
+    p.a.x = x, p.a.w = w, p.a.bias = bias, p.a.lengths = lengths, p.a.state_in = (const float *)state_in, p.a.y = y, p.a.state_out = (float *)state_out;
+    return run(d, p, false, (hipStream_t)stream);
+}
+
+int cawn_causal_conv_bwd(const cawn_conv_desc *d, const void *x, const float *w, const float *bias, const int32_t *lengths, const void *state_in, const void *dy,
+                         const void *dstate_out, void *dx, float *dw, float *dbias, void *dstate_in, void *workspace, size_t workspace_bytes, void *stream)
+{
+    Plan p;
+    if (int r = plan_of(d, true, true, &p)) return r;
+    const size_t e = d->bf16 ? 2 : 4;
+    if (!aligned_to(x, e) || !aligned_to(dy, e) || !aligned_to(dx, e) || !aligned_to(w, 4) || !aligned_to(bias, 4) || !aligned_to(lengths, 4) || !aligned_to(state_in, 4) ||
+        !aligned_to(dstate_out, 4) || !aligned_to(dstate_in, 4) || !aligned_to(dw, 4) || !aligned_to(dbias, 4)) return CAWN_EINVAL;
+    hipStream_t s = (hipStream_t)stream;
+    const bool grads = dw || dbias;
+    const TapSums out{dw, dbias, d->C, d->k};
+    if (d->B == 0) {
+        if (grads && !d->accumulate_param_grads) launch_sums(nullptr, 0, (long long)d->C * (d->k + 1), out, 0, s);      // the sums over nothing
+        return launched();
+    }
+    if (!w || (d->L > 0 && (!x || !dy))) return CAWN_EINVAL;
+    if (!aligned_to(x, 16) || !aligned_to(dy, 16) || !aligned_to(dx, 16)) {
+        if (int r = plan_of(d, false, true, &p)) return r;
+    }
+    if (grads && (!workspace || workspace_bytes < part_bytes(p) || !aligned_to(workspace, 256))) return CAWN_EWORKSPACE;
+    p.a.x = x, p.a.w = w, p.a.bias = bias, p.a.lengths = lengths, p.a.state_in = (const float *)state_in, p.a.dy = dy, p.a.dstate_out = (const float *)dstate_out;
+    p.a.dx = dx, p.a.dstate_in = (float *)dstate_in, p.a.part = grads ? (float *)workspace : nullptr;
+    if (int r = run(d, p, true, s)) return r;
+    if (grads) launch_sums(p.a.part, p.a.rblocks, (long long)d->C * (d->k + 1), out, d->accumulate_param_grads, s);
+    return launched();
+}
+
+} // extern "C"

@@ -1,0 +1,521 @@
+// Root-mean-square norm joined with the residual addition in front of it, forward and backward, its output in 8 bits among them.
+//
+// Forward: h = x + residual, rounded to h's type; y = w h rstd, rstd = 1 / sqrt(mean h^2 + eps); q = e4m3(y / scale), scale = max |y| / 448 over a block.
+// Backward: hh = h rstd, t = w dy, dr = dh + rstd (t - hh avg(t hh)), dw = sum dy hh.
+//
+// A row is in registers from its one read to its write: a run of 4 to 64 lanes holds it, or a workgroup of 256 to 1,024; the longest are read again.
+// Bound by memory.
+// The sum of squares is plain: all of its terms have one sign.
+#include "cawn_sums.hpp"
+
+using namespace cawn::ops;
+
+namespace {
+
+struct RmsArgs {
+    const void *x, *res, *dy, *dh;
+    const float *w, *rstd_in;
+    void *h, *y, *dx, *dres;
+    uint8_t *q;
+    float *scales, *rstd, *part;
+    long long rows, xs, rs, ys;
+    int C, block, blocks;       // channels of a scale, scales of a row
+    int lpr, rpw;               // lanes of a row, rows that a workgroup has at once
+    int lpb;                    // lanes that share a scale (a power of two up to 64, within a row's), 0: by way of LDS
+    float eps;
+};
+
+constexpr float E4M3_MAX = 448.f;
+
+// N adjacent elements, 16 bytes an access at most
+template <typename T, int N> __device__ inline void read_n(const T *p, float (&x)[N])
+{
+    constexpr int W = N * sizeof(T) <= 16 ? N : 16 / sizeof(T);
+#pragma unroll
+    for (int i = 0; i < N; i += W) {
+        const Pack<T, W> a = *reinterpret_cast<const Pack<T, W> *>(p + i);
+#pragma unroll
+        for (int j = 0; j < W; ++j) x[i + j] = (float)a.v[j];
+    }
+}
+template <typename T, int N> __device__ inline void write_n(T *p, const float (&x)[N])
+{
+    constexpr int W = N * sizeof(T) <= 16 ? N : 16 / sizeof(T);
+#pragma unroll
+    for (int i = 0; i < N; i += W) {
+        Pack<T, W> a;
+#pragma unroll
+        for (int j = 0; j < W; ++j) a.v[j] = (T)x[i + j];
+        *reinterpret_cast<Pack<T, W> *>(p + i) = a;
+    }
+}
+
+__device__ inline float nan_max(float a, float b) { return a >= b || a != a ? a : b; }      // a NaN stays
+template <bool MAX> __device__ inline float two(float a, float b) { return MAX ? nan_max(a, b) : a + b; }
+
+// sum or maximum over the run of `lanes` (a power of two) adjacent lanes, in every one of them
+template <bool MAX> __device__ inline float over_run(float v, int lanes)
+{
+    for (int m = lanes >> 1; m > 0; m >>= 1) v = two<MAX>(v, __shfl_xor(v, m));
+    return v;
+}
+
+// ... over a row: its run of lanes, or the workgroup
+template <bool WIDE, bool MAX> __device__ inline float over_row(float v, int lpr, float *sh)
+{
+    v = over_run<MAX>(v, WIDE ? 64 : lpr);
+    if (!WIDE) return v;
+    __syncthreads();                // (what the last call left has been read)
+    if (threadIdx.x % 64 == 0) sh[threadIdx.x / 64] = v;
+    __syncthreads();
+    v = sh[0];
+    for (int i = 1; i < (int)blockDim.x / 64; ++i) v = two<MAX>(v, sh[i]);
+    return v;
+}
+
+// four values as e4m3, rounded to nearest even
+__device__ inline uint32_t e4m3_4(float a, float b, float c, float d)
+{
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+}
+
+// Scale of a block whose largest magnitude is m; 0 for one of zeros, or of values so small that the scale would lose its digits.
+__device__ inline float scale_of(float m) { return m < E4M3_MAX * 1.17549435e-38f ? 0.f : m / E4M3_MAX; }
+
+// VEC values y of the type's 8 bits
+template <int VEC> __device__ inline void write_q(uint8_t *q, const float (&y)[VEC], float scale)
+{
+    float v[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = scale == 0.f ? 0.f : y[i] / scale;
+    if constexpr (VEC == 1) *q = (uint8_t)(e4m3_4(v[0], 0.f, 0.f, 0.f) & 0xff);
+    else if constexpr (VEC == 4) *reinterpret_cast<uint32_t *>(q) = e4m3_4(v[0], v[1], v[2], v[3]);
+    else *reinterpret_cast<uint2 *>(q) = make_uint2(e4m3_4(v[0], v[1], v[2], v[3]), e4m3_4(v[4], v[5], v[6], v[7]));
+}
+
+// VEC values of h, as they are kept
+template <typename X, typename R, int VEC> __device__ inline void read_h(const RmsArgs &a, long long r, int c, float (&h)[VEC])
+{
+    read_n<X, VEC>((const X *)a.x + r * a.xs + c, h);
+    if (a.res) {
+        float v[VEC];
+        read_n<R, VEC>((const R *)a.res + r * a.rs + c, v);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) h[i] += v[i];
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) h[i] = (float)(R)h[i];
+}
+
+template <int VEC> __device__ inline float largest(const float (&y)[VEC])
+{
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) m = nan_max(fabsf(y[i]), m);
+    return m;
+}
+
+// X, R: types of x, y and of the residual stream.  WIDE: a row is the workgroup's.
+template <typename X, typename R, int VEC, int NIT, bool WIDE, int THREADS> __global__ __launch_bounds__(THREADS) void rms_forward(const RmsArgs a)
+{
+    __shared__ float sh[WIDE ? THREADS / 64 : 1];
+    __shared__ uint32_t most[THREADS * NIT * VEC / 16 + 256];     // maxima of the blocks, as the bits of values without a sign
+    const int run = WIDE ? 0 : threadIdx.x / a.lpr, lane = WIDE ? threadIdx.x : threadIdx.x % a.lpr;
+    const int step = WIDE ? THREADS : a.lpr;
+    float w[NIT][VEC];
+    bool in[NIT];
+#pragma unroll
+    for (int n = 0; n < NIT; ++n) {
+        const int c = (n * step + lane) * VEC;
+        in[n] = c < a.C;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) w[n][i] = in[n] && a.w ? a.w[c + i] : 1.f;
+    }
+    const long long stride = (long long)gridDim.x * a.rpw;
+    const float inv = 1.f / (float)a.C;
+    // (all runs of a workgroup go round equally often: there are barriers inside)
+    for (long long r0 = (long long)blockIdx.x * a.rpw; r0 < a.rows; r0 += stride) {
+        const bool live = r0 + run < a.rows;
+        const long long r = live ? r0 + run : r0;
+        float h[NIT][VEC], s = 0.f;
+#pragma unroll
+        for (int n = 0; n < NIT; ++n) {
+            read_h<X, R, VEC>(a, r, in[n] ? (n * step + lane) * VEC : 0, h[n]);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                h[n][i] = in[n] ? h[n][i] : 0.f;
+                s = fmaf(h[n][i], h[n][i], s);
+            }
+        }
+        const float rstd = 1.f / sqrtf(over_row<WIDE, false>(s, a.lpr, sh) * inv + a.eps);
+        if (live && lane == 0 && a.rstd) a.rstd[r] = rstd;
+#pragma unroll
+        for (int n = 0; n < NIT; ++n) {
+            const int c = (n * step + lane) * VEC;
+            if (live && in[n] && a.h) write_n<R, VEC>((R *)a.h + r * a.rs + c, h[n]);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) h[n][i] = h[n][i] * rstd * w[n][i];
+            if (live && in[n] && a.y) write_n<X, VEC>((X *)a.y + r * a.ys + c, h[n]);
+        }
+        if (!a.q) continue;
+        float m[NIT];
+#pragma unroll
+        for (int n = 0; n < NIT; ++n) m[n] = in[n] ? largest<VEC>(h[n]) : 0.f;
+        if (a.block == 0) {
+            float t = m[0];
+#pragma unroll
+            for (int n = 1; n < NIT; ++n) t = nan_max(m[n], t);
+            t = over_row<WIDE, true>(t, a.lpr, sh);
+#pragma unroll
+            for (int n = 0; n < NIT; ++n) m[n] = t;
+        } else if (a.lpb > 0) {
+#pragma unroll
+            for (int n = 0; n < NIT; ++n) m[n] = over_run<true>(m[n], a.lpb);
+        } else {
+            __syncthreads();
+            for (int i = threadIdx.x; i < a.blocks * a.rpw; i += THREADS) most[i] = 0;
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < NIT; ++n) {
+                const int c = (n * step + lane) * VEC;      // (a block is a multiple of 16 channels: of VEC)
+                if (in[n] && live) atomicMax(&most[run * a.blocks + c / a.block], __float_as_uint(m[n]) & 0x7fffffffu);
+            }
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < NIT; ++n) {
+                const int c = (n * step + lane) * VEC;
+                if (in[n] && live) m[n] = __uint_as_float(most[run * a.blocks + c / a.block]);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NIT; ++n) {
+            const int c = (n * step + lane) * VEC;
+            if (!live || !in[n]) continue;
+            const float scale = scale_of(m[n]);
+            const int j = a.block ? c / a.block : 0;
+            if (c == j * a.block) a.scales[r * a.blocks + j] = scale;
+            write_q<VEC>(a.q + r * a.ys + c, h[n], scale);
+        }
+    }
+}
+
+// Rows that no workgroup's registers hold: read twice, three times where 8 bits are asked for.
+template <typename X, typename R, int VEC> __global__ __launch_bounds__(1024) void rms_forward_long(const RmsArgs a)
+{
+    __shared__ float sh[16];
+    __shared__ uint32_t most[2048];
+    for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        float s = 0.f;
+        for (int c = threadIdx.x * VEC; c < a.C; c += 1024 * VEC) {
+            float h[VEC];
+            read_h<X, R, VEC>(a, r, c, h);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) s = fmaf(h[i], h[i], s);
+        }
+        const float rstd = 1.f / sqrtf(over_row<true, false>(s, 0, sh) / (float)a.C + a.eps);
+        if (threadIdx.x == 0 && a.rstd) a.rstd[r] = rstd;
+        const int per = a.block ? a.block : a.C;
+        float whole = 0.f;
+        // (h or y may lie where x or the residual did: nothing is written before the last reading, and there by the thread that has read it)
+        auto norm = [&](int c, float(&h)[VEC]) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) h[i] = h[i] * rstd * (a.w ? a.w[c + i] : 1.f);
+        };
+        if (a.q) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < a.blocks; i += 1024) most[i] = 0;
+            __syncthreads();
+            for (int c = threadIdx.x * VEC; c < a.C; c += 1024 * VEC) {
+                float h[VEC];
+                read_h<X, R, VEC>(a, r, c, h);
+                norm(c, h);
+                const float m = largest<VEC>(h);
+                if (a.block) atomicMax(&most[c / per], __float_as_uint(m) & 0x7fffffffu);
+                else whole = nan_max(m, whole);
+            }
+            __syncthreads();
+            if (!a.block) whole = over_row<true, true>(whole, 0, sh);
+        }
+        for (int c = threadIdx.x * VEC; c < a.C; c += 1024 * VEC) {
+            float h[VEC];
+            read_h<X, R, VEC>(a, r, c, h);
+            if (a.h) write_n<R, VEC>((R *)a.h + r * a.rs + c, h);
+            norm(c, h);
+            if (a.y) write_n<X, VEC>((X *)a.y + r * a.ys + c, h);
+            if (a.q) {
+                const float scale = scale_of(a.block ? __uint_as_float(most[c / per]) : whole);
+                if (c % per == 0) a.scales[r * a.blocks + c / per] = scale;
+                write_q<VEC>(a.q + r * a.ys + c, h, scale);
+            }
+        }
+    }
+}
+
+// VEC values of hh and of t = w dy
+template <typename X, typename R, int VEC> __device__ inline void read_back(const RmsArgs &a, long long r, int c, float rstd, float (&h)[VEC], float (&t)[VEC])
+{
+    read_n<R, VEC>((const R *)a.x + r * a.rs + c, h);
+    read_n<X, VEC>((const X *)a.dy + r * a.ys + c, t);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) h[i] *= rstd;
+}
+
+// dr of VEC values, into dx and dresidual
+template <typename X, typename R, int VEC> __device__ inline void write_back(const RmsArgs &a, long long r, int c, float rstd, float s, const float (&h)[VEC], const float (&t)[VEC])
+{
+    float d[VEC];
+    if (a.dh) read_n<R, VEC>((const R *)a.dh + r * a.rs + c, d);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) d[i] = fmaf(rstd, fmaf(-h[i], s, t[i]), a.dh ? d[i] : 0.f);
+    if (a.dx) write_n<X, VEC>((X *)a.dx + r * a.xs + c, d);
+    if (a.dres) write_n<R, VEC>((R *)a.dres + r * a.rs + c, d);
+}
+
+template <typename X, typename R, int VEC, int NIT, bool WIDE, int THREADS> __global__ __launch_bounds__(THREADS) void rms_backward(const RmsArgs a)
+{
+    __shared__ float sh[WIDE ? THREADS / 64 : THREADS * NIT * VEC];
+    const int run = WIDE ? 0 : threadIdx.x / a.lpr, lane = WIDE ? threadIdx.x : threadIdx.x % a.lpr;
+    const int step = WIDE ? THREADS : a.lpr;
+    float w[NIT][VEC], sw[NIT][VEC];
+    bool in[NIT];
+#pragma unroll
+    for (int n = 0; n < NIT; ++n) {
+        const int c = (n * step + lane) * VEC;
+        in[n] = c < a.C;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) w[n][i] = in[n] && a.w ? a.w[c + i] : 1.f, sw[n][i] = 0.f;
+    }
+    const long long stride = (long long)gridDim.x * a.rpw;
+    const float inv = 1.f / (float)a.C;
+    for (long long r0 = (long long)blockIdx.x * a.rpw; r0 < a.rows; r0 += stride) {
+        const bool live = r0 + run < a.rows;
+        const long long r = live ? r0 + run : r0;
+        const float rstd = a.rstd_in[r];
+        float h[NIT][VEC], t[NIT][VEC], s = 0.f;
+#pragma unroll
+        for (int n = 0; n < NIT; ++n) {
+            read_back<X, R, VEC>(a, r, in[n] ? (n * step + lane) * VEC : 0, rstd, h[n], t[n]);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                h[n][i] = in[n] && live ? h[n][i] : 0.f;
+                t[n][i] = in[n] && live ? t[n][i] : 0.f;
+                sw[n][i] = fmaf(t[n][i], h[n][i], sw[n][i]);
+                t[n][i] *= w[n][i];
+                s = fmaf(t[n][i], h[n][i], s);
+            }
+        }
+        s = over_row<WIDE, false>(s, a.lpr, sh) * inv;
+        if (!live || (!a.dx && !a.dres)) continue;      // (the row's lanes all, and no barrier is left out: a workgroup's row is live)
+#pragma unroll
+        for (int n = 0; n < NIT; ++n)
+            if (in[n]) write_back<X, R, VEC>(a, r, (n * step + lane) * VEC, rstd, s, h[n], t[n]);
+    }
+    if (!a.part) return;
+    float *out = a.part + (long long)blockIdx.x * a.C;
+    if (!WIDE) {        // the runs of a workgroup, in their order
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < NIT; ++n)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) sh[((run * NIT + n) * a.lpr + lane) * VEC + i] = sw[n][i];
+        __syncthreads();
+        if (run) return;
+#pragma unroll
+        for (int n = 0; n < NIT; ++n)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                for (int q = 1; q < a.rpw; ++q) sw[n][i] += sh[((q * NIT + n) * a.lpr + lane) * VEC + i];
+    }
+#pragma unroll
+    for (int n = 0; n < NIT; ++n) {
+        const int c = (n * step + lane) * VEC;
+        if (!in[n]) continue;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) out[c + i] = sw[n][i];
+    }
+}
+
+// Rows that no workgroup's registers hold: read twice, the sums of dweight in the workspace.
+template <typename X, typename R, int VEC> __global__ __launch_bounds__(1024) void rms_backward_long(const RmsArgs a)
+{
+    __shared__ float sh[16];
+    float *part = a.part ? a.part + (long long)blockIdx.x * a.C : nullptr;
+    bool first = true;
+    for (long long r = blockIdx.x; r < a.rows; r += gridDim.x, first = false) {
+        const float rstd = a.rstd_in[r];
+        float s = 0.f;
+        for (int c = threadIdx.x * VEC; c < a.C; c += 1024 * VEC) {
+            float h[VEC], t[VEC];
+            read_back<X, R, VEC>(a, r, c, rstd, h, t);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float g = t[i] * h[i];
+                if (part) part[c + i] = first ? g : part[c + i] + g;        // (the thread's own columns)
+                s = fmaf(g, a.w ? a.w[c + i] : 1.f, s);
+            }
+        }
+        s = over_row<true, false>(s, 0, sh) / (float)a.C;
+        if (!a.dx && !a.dres) continue;
+        for (int c = threadIdx.x * VEC; c < a.C; c += 1024 * VEC) {
+            float h[VEC], t[VEC];
+            read_back<X, R, VEC>(a, r, c, rstd, h, t);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) t[i] *= a.w ? a.w[c + i] : 1.f;
+            write_back<X, R, VEC>(a, r, c, rstd, s, h, t);
+        }
+    }
+}
+
+struct Plain {
+    float *out;
+    __device__ float *operator()(long long c) const { return out + c; }
+};
+
+// ---------------------------------------------------------------------------------------------- host
+struct Plan {
+    RmsArgs a;
+    int vec, nit, threads;
+    bool wide, held;            // a row is a workgroup's; it is in registers
+    long long blocks;
+};
+
+// The geometry must not depend on pointers: the workspace is sized without them.  Rows that do not begin on 16 bytes are taken value by value.
+int plan_of(const cawn_rms_desc *d, bool aligned, bool bwd, Plan *p)
+{
+    if (!d || d->rows < 0 || d->C <= 0 || (d->bf16 & ~1) || (d->residual_bf16 & ~1) || d->block < 0 || d->block % 16) return CAWN_EINVAL;
+    if (d->C > 32768) return CAWN_EUNSUPPORTED;
+    RmsArgs &a = p->a;
+    a = RmsArgs{};
+    a.rows = d->rows, a.C = d->C, a.eps = d->eps;
+    a.xs = d->x_stride ? d->x_stride : a.C, a.rs = d->residual_stride ? d->residual_stride : a.C, a.ys = d->y_stride ? d->y_stride : a.C;
+    if (a.xs < a.C || a.rs < a.C || a.ys < a.C) return CAWN_EINVAL;
+    a.block = d->block >= d->C ? 0 : d->block;
+    a.blocks = a.block ? (int)ceil_div(a.C, a.block) : 1;
+    const int most = d->bf16 ? 8 : 4, each = d->bf16 || d->residual_bf16 ? 8 : 4;       // (strides of the narrower type)
+    p->vec = aligned && a.C % most == 0 && a.xs % each == 0 && a.rs % each == 0 && a.ys % each == 0 ? most : 1;
+    const int units = (int)ceil_div(a.C, p->vec);
+    p->wide = units > 192;
+    p->held = true;
+    if (!p->wide) {
+        // the run of lanes that has fewest to spare
+        int best = 1 << 30;
+        for (int nit = 1; nit <= 3; ++nit)
+            for (int lanes = 4; lanes <= 64; lanes *= 2)
+                if (lanes * nit >= units && lanes * nit < best) best = lanes * nit, a.lpr = lanes, p->nit = nit;
+        p->threads = 256;
+        a.rpw = 256 / a.lpr;
+    } else {        // 16 values a thread at most, 8 where they come one by one
+        const int top = p->vec == 8 ? 2 : p->vec == 4 ? 4 : 8;
+        p->threads = units <= 256 * top ? 256 : units <= 512 * top ? 512 : 1024;
+        p->held = units <= 1024 * top;
+        a.lpr = p->threads, a.rpw = 1;
+        const int nit = (int)ceil_div(units, p->threads);
+        p->nit = nit <= 1 ? 1 : nit <= 2 ? 2 : nit <= 4 ? 4 : 8;
+    }
+    a.lpb = 0;
+    if (a.block) {
+        const int lanes = a.block / p->vec;
+        if ((lanes & (lanes - 1)) == 0 && lanes <= 64 && lanes <= a.lpr) a.lpb = lanes;
+    }
+    const long long all = ceil_div(a.rows, a.rpw), there = bwd ? 1024 : 4096;
+    p->blocks = all < there ? all : there;
+    return CAWN_OK;
+}
+
+template <typename X, typename R, int VEC, int NIT, bool WIDE, int THREADS> void go(const Plan &p, bool bwd, hipStream_t s)
+{
+    if (bwd) hipLaunchKernelGGL((rms_backward<X, R, VEC, NIT, WIDE, THREADS>), dim3((unsigned)p.blocks), dim3(THREADS), 0, s, p.a);
+    else hipLaunchKernelGGL((rms_forward<X, R, VEC, NIT, WIDE, THREADS>), dim3((unsigned)p.blocks), dim3(THREADS), 0, s, p.a);
+}
+
+template <typename X, typename R, int VEC, int THREADS> void go_wide(const Plan &p, bool bwd, hipStream_t s)
+{
+    constexpr int TOP = VEC == 8 ? 2 : VEC == 4 ? 4 : 8;
+    if (p.nit == 1) go<X, R, VEC, 1, true, THREADS>(p, bwd, s);
+    else if (p.nit == 2) go<X, R, VEC, 2, true, THREADS>(p, bwd, s);
+    else if (p.nit == 4) go<X, R, VEC, TOP < 4 ? TOP : 4, true, THREADS>(p, bwd, s);
+    else go<X, R, VEC, TOP, true, THREADS>(p, bwd, s);
+}
+
+template <typename X, typename R, int VEC> int launch(const Plan &p, bool bwd, hipStream_t s)
+{
+    if (!p.wide) {
+        if (p.nit == 1) go<X, R, VEC, 1, false, 256>(p, bwd, s);
+        else if (p.nit == 2) go<X, R, VEC, 2, false, 256>(p, bwd, s);
+        else go<X, R, VEC, 3, false, 256>(p, bwd, s);
+    } else if (!p.held) {
+        if (bwd) hipLaunchKernelGGL((rms_backward_long<X, R, VEC>), dim3((unsigned)p.blocks), dim3(1024), 0, s, p.a);
+        else hipLaunchKernelGGL((rms_forward_long<X, R, VEC>), dim3((unsigned)p.blocks), dim3(1024), 0, s, p.a);
+    } else if (p.threads == 256) go_wide<X, R, VEC, 256>(p, bwd, s);
+    else if (p.threads == 512) go_wide<X, R, VEC, 512>(p, bwd, s);
+    else go_wide<X, R, VEC, 1024>(p, bwd, s);
+    return launched();
+}
+
+int run(const cawn_rms_desc *d, const Plan &p, bool bwd, hipStream_t s)
+{
+    if (d->bf16) {
+        if (d->residual_bf16) return p.vec > 1 ? launch<bf16, bf16, 8>(p, bwd, s) : launch<bf16, bf16, 1>(p, bwd, s);
+        return p.vec > 1 ? launch<bf16, float, 8>(p, bwd, s) : launch<bf16, float, 1>(p, bwd, s);
+    }
+    if (d->residual_bf16) return p.vec > 1 ? launch<float, bf16, 4>(p, bwd, s) : launch<float, bf16, 1>(p, bwd, s);
+    return p.vec > 1 ? launch<float, float, 4>(p, bwd, s) : launch<float, float, 1>(p, bwd, s);
+}
+
+} // namespace
+
+extern "C" {
+
+size_t cawn_rms_norm_add_workspace_bytes(const cawn_rms_desc *d)
+{
+    size_t most = 0;
+    for (int i = 0; i < 2; ++i) {
+        Plan p;
+        if (plan_of(d, i != 0, true, &p) != CAWN_OK) return 0;
+        const size_t bytes = (size_t)p.blocks * p.a.C * 4;
+        most = most > bytes ? most : bytes;
+    }
+    return most > 256 ? most : 256;
+}
+
+int cawn_rms_norm_add_fwd(const cawn_rms_desc *d, const void *x, const void *residual, const float *weight, void *h, void *y, void *q, float *scales, float *rstd,
+                          void *stream)
+{
+    Plan p;
+    if (int r = plan_of(d, true, false, &p)) return r;
+    const size_t e = d->bf16 ? 2 : 4, f = d->residual_bf16 ? 2 : 4;
+    if (!aligned_to(x, e) || !aligned_to(y, e) || !aligned_to(residual, f) || !aligned_to(h, f) || !aligned_to(weight, 4) || !aligned_to(scales, 4) || !aligned_to(rstd, 4))
+        return CAWN_EINVAL;
+    if ((y == nullptr && q == nullptr) || (q == nullptr) != (scales == nullptr)) return CAWN_EINVAL;
+    if (d->rows == 0) return CAWN_OK;
+    if (!x) return CAWN_EINVAL;
+    if (!aligned_to(x, 16) || !aligned_to(y, 16) || !aligned_to(residual, 16) || !aligned_to(h, 16) || !aligned_to(q, 8)) plan_of(d, false, false, &p);
+    p.a.x = x, p.a.res = residual, p.a.w = weight, p.a.h = h, p.a.y = y, p.a.q = (uint8_t *)q, p.a.scales = scales, p.a.rstd = rstd;
+    return run(d, p, false, (hipStream_t)stream);
+}
+
+int cawn_rms_norm_add_bwd(const cawn_rms_desc *d, const void *h, const float *weight, const float *rstd, const void *dy, const void *dh, void *dx, void *dresidual,
+                          float *dweight, void *workspace, size_t workspace_bytes, void *stream)
+{
+    Plan p;
+    if (int r = plan_of(d, true, true, &p)) return r;
+    const size_t e = d->bf16 ? 2 : 4, f = d->residual_bf16 ? 2 : 4;
+    if (!aligned_to(h, f) || !aligned_to(dh, f) || !aligned_to(dresidual, f) || !aligned_to(dy, e) || !aligned_to(dx, e) || !aligned_to(weight, 4) || !aligned_to(rstd, 4) ||
+        !aligned_to(dweight, 4)) return CAWN_EINVAL;
+    hipStream_t s = (hipStream_t)stream;
+    if (d->rows == 0) {
+        if (dweight && !d->accumulate_param_grads) launch_sums(nullptr, 0, d->C, Plain{dweight}, 0, s);     // the sum over nothing
+        return launched();
+    }
+    if (!h || !rstd || !dy) return CAWN_EINVAL;
+    if (!dx && !dresidual && !dweight) return CAWN_OK;
+    if (!aligned_to(h, 16) || !aligned_to(dh, 16) || !aligned_to(dresidual, 16) || !aligned_to(dy, 16) || !aligned_to(dx, 16)) plan_of(d, false, true, &p);
+    if (dweight && (!workspace || workspace_bytes < (size_t)p.blocks * p.a.C * 4 || !aligned_to(workspace, 256))) return CAWN_EWORKSPACE;
+    p.a.x = h, p.a.w = weight, p.a.rstd_in = rstd, p.a.dy = dy, p.a.dh = dh, p.a.dx = dx, p.a.dres = dresidual, p.a.part = dweight ? (float *)workspace : nullptr;
+    if (int r = run(d, p, true, s)) return r;
+    if (dweight) launch_sums(p.a.part, p.blocks, p.a.C, Plain{dweight}, d->accumulate_param_grads, s);
+    return launched();
+}
+
+} // extern "C"

@@ -1,0 +1,207 @@
+// Selective state space scan: argument checks, sizes and the choice of a form.
+#include "cawn_select.hpp"
+
+using namespace cawn;
+using namespace cawn::ops;
+using cawn::select::Args;
+using cawn::select::TILE;
+
+namespace {
+
+// How a row's tiles are cut into segments: until the chip has `waves` of them.
+void cut(Args *a, long long waves)
+{
+    const long long columns = (long long)a->B * a->G * a->cbg * (a->NB > 1 ? a->NB : a->wide);
+    const long long want = columns > 0 ? waves / columns : 1;
+    a->segments = 1, a->seg_tiles = a->tiles > 0 ? a->tiles : 1;
+    if (want < 2 || a->tiles < 2) return;
+    a->seg_tiles = (int)ceil_div(a->tiles, want);
+    a->segments = (int)ceil_div(a->tiles, a->seg_tiles);
+}
+
+// More workgroups than a grid has, in any of the launches, or more bytes than are counted.
+bool too_many(const Args &a)
+{
+    const long long most = 1LL << 38;       // threads
+    const double npt = a.NP * a.NB, rows = (double)a.B * a.G;
+    if ((double)a.B * a.tiles * a.Dp * npt > 1e17) return true;
+    return rows * a.tiles * npt * 2 * TILE > most || (double)a.B * a.Dp * npt > most || rows * a.segments * a.cbg > (double)0x7fffffff;
+}
+
+int check(const cawn_scan_desc *d, bool bwd, Args *a)
+{
+    if (!d || d->B < 0 || d->L < 0 || d->D <= 0 || d->N <= 0 || d->G < 0 || (d->bf16 & ~1) || (d->dt_softplus & ~1)) return CAWN_EINVAL;
+    const int G = d->G ? d->G : 1;
+    if (d->D % G) return CAWN_EINVAL;
+    if (d->N > select::N_MAX) return CAWN_EUNSUPPORTED;
+    *a = Args{};
+    a->B = d->B, a->L = d->L, a->D = d->D, a->N = d->N, a->G = G, a->cg = d->D / G, a->softplus = d->dt_softplus;
+    const long long gn = (long long)G * d->N;
+    a->xst = d->x_stride_t ? d->x_stride_t : d->D, a->dst = d->dt_stride_t ? d->dt_stride_t : d->D, a->bst = d->bc_stride_t ? d->bc_stride_t : gn;
+    a->zst = d->z_stride_t ? d->z_stride_t : d->D, a->yst = d->y_stride_t ? d->y_stride_t : d->D;
+    if (a->xst < d->D || a->dst < d->D || a->bst < gn || a->zst < d->D || a->yst < d->D) return CAWN_EINVAL;
+    a->xsb = d->x_stride_b ? d->x_stride_b : a->xst * d->L, a->dsb = d->dt_stride_b ? d->dt_stride_b : a->dst * d->L;
+    a->bsb = d->bc_stride_b ? d->bc_stride_b : a->bst * d->L, a->zsb = d->z_stride_b ? d->z_stride_b : a->zst * d->L;
+    a->ysb = d->y_stride_b ? d->y_stride_b : a->yst * d->L;
+    a->NP = d->N <= 4 ? 4 : d->N <= 8 ? 8 : 16;
+    a->NB = d->N <= 16 ? 1 : d->N <= 32 ? 2 : d->N <= 64 ? 4 : 8;
+    a->cpg = (int)ceil_div(a->cg, 64);
+    a->wide = a->NB > 1 ? 1 : a->cpg < 4 ? a->cpg : 4;
+    a->cbg = (int)ceil_div(a->cpg, a->wide);
+    a->parts = a->cbg;
+    if ((long long)a->cpg * G > 0x7fffffffLL / 64) return CAWN_EUNSUPPORTED;
+    a->Dp = a->cpg * G * 64;
+    a->tiles = (int)ceil_div(d->L, TILE);
+    cut(a, bwd ? 2048 : 4096);
+    return too_many(*a) ? CAWN_EUNSUPPORTED : CAWN_OK;
+}
+
+// Byte offsets.  Kept for the backward: B and C, states before each tile.  Scratch: forward B and C (unless kept), of segments their b, sum of delta and
+// begin; backward the same of its own segments, and the partial sums.
+struct Layout { size_t ck, ckpt; size_t b, g, s, fwd; size_t pbc, pa, pd, bwd; };
+Layout layout_of(const Args &f, const Args &r)
+{
+    const size_t npt = f.NP * f.NB, state = (size_t)f.Dp * npt * 4;
+    auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+    Layout l;
+    const size_t bc = up((size_t)f.B * f.tiles * f.G * npt * 2 * TILE * 4);
+    l.ck = bc;
+    l.ckpt = bc + (size_t)f.B * f.tiles * state;
+    const size_t fs = f.segments > 1 ? (size_t)f.B * f.segments : 0, rs = r.segments > 1 ? (size_t)r.B * r.segments : 0;
+    auto parts = [&](size_t n, size_t *b, size_t *g, size_t *s) {
+        *s = *b + n * state;
+        *g = *s + n * state;
+        return up(*g + n * f.Dp * 4);
+    };
+    l.b = bc;
+    l.fwd = parts(fs, &l.b, &l.g, &l.s);
+    size_t b = 0, g, s;
+    l.pbc = parts(rs, &b, &g, &s);
+    l.pa = l.pbc + up((size_t)r.B * r.tiles * TILE * r.G * r.parts * 2 * npt * 4);
+    l.pd = l.pa + up((size_t)r.B * r.segments * state);
+    l.bwd = l.pd + (size_t)r.B * r.segments * r.NB * 2 * r.Dp * 4;
+    return l;
+}
+
+void segments_of(Args *a, char *ws, size_t begin)
+{
+    const size_t n = (size_t)a->B * a->segments, state = (size_t)a->Dp * a->NP * a->NB * 4;
+    a->seg_b = (float *)(ws + begin), a->seg_s = (float *)(ws + begin + n * state), a->seg_g = (float *)(ws + begin + 2 * n * state);
+}
+
+struct RateSums {       // column (channel in its padded place, state) -> A's
+    float *out;
+    int N, NPT, cpg, cg;
+    __device__ float *operator()(long long c) const
+    {
+        const long long pad = c / NPT, g = pad / 64 / cpg, in = pad - g * cpg * 64;
+        const int n = (int)(c - pad * NPT);
+        return n < N && in < cg ? out + (g * cg + in) * N + n : nullptr;
+    }
+};
+
+struct ChannelSums {    // column (0: D, 1: bias; channel in its padded place)
+    float *dD, *db;
+    int Dp, cpg, cg;
+    __device__ float *operator()(long long c) const
+    {
+        float *out = c < Dp ? dD : db;
+        const long long pad = c < Dp ? c : c - Dp, g = pad / 64 / cpg, in = pad - g * cpg * 64;
+        return out && in < cg ? out + g * cg + in : nullptr;
+    }
+};
+
+bool misaligned(const cawn_scan_desc *d, const void *p) { return !aligned_to(p, d->bf16 ? 2 : 4); }
+
+} // namespace
+
+extern "C" {
+
+size_t cawn_selective_scan_state_bytes(const cawn_scan_desc *d)
+{
+    Args a;
+    return check(d, false, &a) != CAWN_OK ? 0 : (size_t)a.B * a.D * a.N * 4;
+}
+
+size_t cawn_selective_scan_ckpt_bytes(const cawn_scan_desc *d)
+{
+    Args a;
+    return check(d, false, &a) != CAWN_OK ? 0 : layout_of(a, a).ckpt;
+}
+
+size_t cawn_selective_scan_workspace_bytes(const cawn_scan_desc *d)
+{
+    Args a, r;
+    if (check(d, false, &a) != CAWN_OK || check(d, true, &r) != CAWN_OK) return 0;
+    const Layout l = layout_of(a, r);
+    const size_t bytes = l.fwd > l.bwd ? l.fwd : l.bwd;
+    return bytes > 256 ? bytes : 256;
+}
+
+int cawn_selective_scan_fwd(const cawn_scan_desc *d, const void *x, const void *dt, const float *A, const void *Bm, const void *Cm, const float *Dskip, const void *z,
+                            const float *dt_bias, const int32_t *lengths, const void *state_in, void *y, void *state_out, void *ckpt, void *workspace,
+                            size_t workspace_bytes, void *stream)
+{
+    Args a;
+    if (int r = check(d, false, &a)) return r;
+    if (a.B == 0) return CAWN_OK;
+    if (!A || (a.L > 0 && (!x || !dt || !Bm || !Cm || !y))) return CAWN_EINVAL;
+    if (misaligned(d, x) || misaligned(d, dt) || misaligned(d, Bm) || misaligned(d, Cm) || misaligned(d, z) || misaligned(d, y) || !aligned_to(A, 4) || !aligned_to(Dskip, 4) ||
+        !aligned_to(dt_bias, 4) || !aligned_to(lengths, 4) || !aligned_to(state_in, 4) || !aligned_to(state_out, 4) || !aligned_to(ckpt, 16)) return CAWN_EINVAL;
+    a.x = x, a.dt = dt, a.A = A, a.Bm = Bm, a.Cm = Cm, a.Dk = Dskip, a.z = z, a.bias = dt_bias, a.lengths = lengths, a.state_in = (const float *)state_in;
+    a.y = y, a.state_out = (float *)state_out;
+    hipStream_t s = (hipStream_t)stream;
+    if (a.L <= select::TOKEN_MAX && !ckpt) return select::launch_token(a, d->bf16, s);
+    const Layout l = layout_of(a, a);
+    if (!workspace || workspace_bytes < l.fwd || !aligned_to(workspace, 256)) return CAWN_EWORKSPACE;
+    a.bc = (float *)(ckpt ? ckpt : workspace);
+    if (ckpt) a.ck = (float *)((char *)ckpt + l.ck);
+    segments_of(&a, (char *)workspace, l.b);
+    return select::launch_forward(a, d->bf16, s);
+}
+
+int cawn_selective_scan_bwd(const cawn_scan_desc *d, const void *x, const void *dt, const float *A, const void *Bm, const void *Cm, const float *Dskip, const void *z,
+                            const float *dt_bias, const int32_t *lengths, const void *ckpt, const void *dy, const void *dstate_out, void *dx, void *ddt, float *dA,
+                            void *dBm, void *dCm, float *dDskip, void *dz, float *ddt_bias, void *dstate_in, void *workspace, size_t workspace_bytes, void *stream)
+{
+    Args a;
+    if (int r = check(d, true, &a)) return r;
+    if ((dz && !z) || (dDskip && !Dskip) || (ddt_bias && !dt_bias)) return CAWN_EINVAL;
+    if (misaligned(d, x) || misaligned(d, dt) || misaligned(d, Bm) || misaligned(d, Cm) || misaligned(d, z) || misaligned(d, dy) || misaligned(d, dx) || misaligned(d, ddt) ||
+        misaligned(d, dBm) || misaligned(d, dCm) || misaligned(d, dz) || !aligned_to(A, 4) || !aligned_to(Dskip, 4) || !aligned_to(dt_bias, 4) || !aligned_to(lengths, 4) ||
+        !aligned_to(ckpt, 16) || !aligned_to(dstate_out, 4) || !aligned_to(dA, 4) || !aligned_to(dDskip, 4) || !aligned_to(ddt_bias, 4) || !aligned_to(dstate_in, 4))
+        return CAWN_EINVAL;
+    hipStream_t s = (hipStream_t)stream;
+    const select::Args &c = a;
+    const int NPT = c.NP * c.NB, add = d->accumulate_param_grads;
+    const RateSums rates{dA, c.N, NPT, c.cpg, c.cg};
+    const ChannelSums channels{dDskip, ddt_bias, c.Dp, c.cpg, c.cg};
+    if (a.B == 0) {         // the sums over nothing
+        if (dA && !add) launch_sums(nullptr, 0, (long long)c.Dp * NPT, rates, 0, s);
+        if ((dDskip || ddt_bias) && !add) launch_sums(nullptr, 0, 2LL * c.Dp, channels, 0, s);
+        return launched();
+    }
+    if (!A || (a.L > 0 && (!x || !dt || !Bm || !Cm || !ckpt || !dy))) return CAWN_EINVAL;
+    Args f;
+    check(d, false, &f);
+    const Layout l = layout_of(f, a);
+    if (!workspace || workspace_bytes < l.bwd || !aligned_to(workspace, 256)) return CAWN_EWORKSPACE;
+    a.x = x, a.dt = dt, a.A = A, a.Bm = Bm, a.Cm = Cm, a.Dk = Dskip, a.z = z, a.bias = dt_bias, a.lengths = lengths, a.dy = dy, a.dstate_out = (const float *)dstate_out;
+    a.dx = dx, a.ddt = ddt, a.dB = dBm, a.dC = dCm, a.dz = dz, a.dstate_in = (float *)dstate_in;
+    a.bc = (float *)const_cast<void *>(ckpt), a.ck = (float *)((char *)const_cast<void *>(ckpt) + l.ck);
+    char *ws = (char *)workspace;
+    segments_of(&a, ws, 0);
+    a.part_bc = dBm || dCm ? (float *)(ws + l.pbc) : nullptr;
+    a.part_a = dA ? (float *)(ws + l.pa) : nullptr;
+    a.part_d = dDskip || ddt_bias ? (float *)(ws + l.pd) : nullptr;
+    if (int r = select::launch_backward(a, d->bf16, s)) return r;
+    if (a.part_bc) {
+        if (int r = select::launch_bc_sums(a, d->bf16, s)) return r;
+    }
+    const long long rows = (long long)a.B * a.segments;
+    if (dA) launch_sums(a.part_a, rows, (long long)a.Dp * NPT, rates, add, s);
+    if (a.part_d) launch_sums(a.part_d, rows * a.NB, 2LL * a.Dp, channels, add, s);
+    return launched();
+}
+
+} // extern "C"

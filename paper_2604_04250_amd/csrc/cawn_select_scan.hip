@@ -1,0 +1,184 @@
+// Selective state space scan by tiles of 16 tokens, forward.
+//
+// Four launches: B and C as the kernels read them; what each segment of a row makes of a zero state (its last states and the sum of delta: the
+// product of its factors is exp(A sum delta)); the chain over the segments; and all segments from their true states.  The second costs each state's
+// exponential and update twice, so that a few rows of many channels fill the chip; one segment does without it and the chain.
+// What bounds it: instruction issue.  A token's state costs a product, an exponential (two issue slots), a product and two sums, 24 cycles of a SIMD a
+// wave, and a token 150 more for softplus, the gate, conversions and memory.
+#include "cawn_select.hpp"
+
+namespace cawn {
+namespace select {
+
+// bc[b][tile][g][n][which][token of the tile]; zeros where there is no token or state
+template <typename T> __global__ __launch_bounds__(256) void select_prepare(const Args a)
+{
+    const int npt = a.NP * a.NB;
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int per = npt * 2 * TILE, i = (int)(id % per), tt = i % TILE, which = i / TILE % 2, n = i / (2 * TILE);
+    const long long rest = id / per, g = rest % a.G, bt = rest / a.G, b = bt / a.tiles;
+    if (b >= a.B) return;
+    const long long t = (bt - b * a.tiles) * TILE + tt;
+    float v = 0.f;
+    if (n < a.N && t < row_length(a, (int)b)) v = (float)((const T *)(which ? a.Cm : a.Bm))[b * a.bsb + t * a.bst + g * a.N + n];
+    a.bc[id] = v;
+}
+
+// NB waves share a channel's states
+template <typename T, int NP, int NB, bool SUMMARY> __global__ __launch_bounds__(NB > 1 ? 64 * NB : 256) void select_scan(const Args a)
+{
+    constexpr bool MULTI = NB > 1;
+    __shared__ float ys[2][MULTI && !SUMMARY ? NB : 1][TILE][64];       // the waves' shares of y
+    const Place p = place_of<MULTI>(a);
+    if (!MULTI && !p.there) return;
+    constexpr int NPT = NP * NB;
+    const int n = row_length(a, p.b);
+    const long long t0 = (long long)p.seg * a.seg_tiles * TILE, t1 = min((long long)n, t0 + (long long)a.seg_tiles * TILE);
+    if (SUMMARY && t0 >= t1) return;        // (the chain ends before it)
+    const long long sat = (((long long)p.b * a.segments + p.seg) * a.Dp + p.pad) * NPT + p.blk * NP;
+    const long long user = (long long)p.b * a.D + p.ch;
+    float A[NP], S[NP], total = 0.f;
+    load_rates<NP>(a, p, A);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) S[i] = 0.f;
+    if (!SUMMARY) {
+        if (a.segments > 1) {
+            if (t0 < t1 || (p.seg == 0 && n == 0)) load_states<NP>(a.seg_s + sat, S);
+        } else if (a.state_in) load_user<NP>(a.state_in, a, user, p.blk * NP, S);
+    }
+    const float bias = a.bias ? a.bias[p.ch] : 0.f, Dk = a.Dk && p.blk == 0 ? a.Dk[p.ch] : 0.f;
+    const T *xp = (const T *)a.x + p.b * a.xsb + p.ch, *dp = (const T *)a.dt + p.b * a.dsb + p.ch;
+    const T *zp = !SUMMARY && a.z ? (const T *)a.z + p.b * a.zsb + p.ch : nullptr;
+    T *yp = SUMMARY ? nullptr : (T *)a.y + p.b * a.ysb + p.ch;
+    int buf = 0;
+    for (long long t = t0; t < t1; t += TILE) {
+        const int left = (int)min(t1 - t, (long long)TILE);
+        const float *tile = a.bc + (((long long)p.b * a.tiles + t / TILE) * a.G + p.g) * NPT * 2 * TILE + p.blk * NP * 2 * TILE;
+        if (!SUMMARY && a.ck && p.there) store_states<NP>(a.ck + (((long long)p.b * a.tiles + t / TILE) * a.Dp + p.pad) * NPT + p.blk * NP, S);
+        float delta[TILE], u[TILE], y[SUMMARY ? 1 : TILE];
+        T zr[SUMMARY ? 1 : TILE];
+#pragma unroll
+        for (int i = 0; i < TILE; ++i) {
+            const long long at = t + min(i, left - 1);
+            delta[i] = (float)dp[at * a.dst] + bias;
+            u[i] = (float)xp[at * a.xst];
+            if constexpr (!SUMMARY) zr[i] = zp ? zp[at * a.zst] : (T)0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < TILE; ++i) {
+            if (a.softplus) delta[i] = softplus_f(delta[i]);
+            if constexpr (!SUMMARY) y[i] = Dk * u[i];
+            delta[i] = i < left ? delta[i] : 0.f;       // (behind the last token nothing changes)
+            u[i] = i < left ? delta[i] * u[i] : 0.f;
+            if (SUMMARY) total += delta[i];
+        }
+        // (the next state's B and C are asked for behind the first token of this one, whose wait would be for them too; without the fences the compiler
+        // asks for all at once and keeps them in lanes of vector registers)
+        f32x16 Bn = bc_tile(tile, 0, 0), Cn = Bn;
+        if constexpr (!SUMMARY) Cn = bc_tile(tile, 0, 1);
+#pragma unroll
+        for (int s = 0; s < NP; ++s) {
+            const f32x16 Bv = Bn, Cv = Cn;
+#pragma unroll
+            for (int i = 0; i < TILE; ++i) {
+                S[s] = fmaf(factor(delta[i], A[s]), S[s], u[i] * Bv[i]);
+                if constexpr (!SUMMARY) y[i] = fmaf(Cv[i], S[s], y[i]);
+                if (i == 0 && s + 1 < NP) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    Bn = bc_tile(tile, s + 1, 0);
+                    if constexpr (!SUMMARY) Cn = bc_tile(tile, s + 1, 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (!SUMMARY) {
+            stay<TILE>(y);
+            if (MULTI) {        // (two buffers: a wave may be a tile ahead of another)
+                buf ^= 1;
+#pragma unroll
+                for (int i = 0; i < TILE; ++i) ys[buf][p.blk][i][p.lane] = y[i];
+                __syncthreads();
+            }
+#pragma unroll
+            for (int i = 0; i < TILE; ++i) {
+                if (i >= left || (MULTI && i % NB != p.blk)) continue;
+                float v = y[i];
+                if (MULTI) {
+                    v = 0.f;
+#pragma unroll
+                    for (int k = 0; k < NB; ++k) v += ys[buf][MULTI ? k : 0][i][p.lane];
+                }
+                const float z = (float)zr[i];
+                if (zp) v *= z * sigmoid_f(z);
+                if (p.on) yp[(t + i) * a.yst] = (T)v;
+            }
+        }
+    }
+    if (SUMMARY) {
+        store_states<NP>(a.seg_b + sat, S);
+        if (p.blk == 0) a.seg_g[((long long)p.b * a.segments + p.seg) * a.Dp + p.pad] = total;
+        return;
+    }
+    if (p.on && p.blk == 0)
+        for (long long t = max(t0, (long long)n); t < min((long long)a.L, t0 + (long long)a.seg_tiles * TILE); ++t) yp[t * a.yst] = (T)0.f;
+    // the segment of the row's last token, or of a row without any the first
+    if (p.on && a.state_out && (n == 0 ? p.seg == 0 : t0 < t1 && t1 == n)) store_user<NP>(a.state_out, a, user, p.blk * NP, S);
+}
+
+// The chain over the segments.  Forward: their states at the begin; backward: what reaches their end, from the last that a row has to the first.
+template <bool REV> __global__ __launch_bounds__(256) void select_join(const Args a)
+{
+    const int NPT = a.NP * a.NB;
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x, per = (long long)a.Dp * NPT, b = id / per;
+    if (b >= a.B) return;
+    const long long i = id - b * per, pad = i / NPT;
+    const int s = (int)(i - pad * NPT), g = (int)(pad / 64 / a.cpg), in = (int)(pad - (long long)g * a.cpg * 64), ch = g * a.cg + in;
+    const bool on = in < a.cg && s < a.N;
+    const float *begin = REV ? a.dstate_out : a.state_in;
+    float S = on && begin ? begin[(b * a.D + ch) * a.N + s] : 0.f;
+    const float A = on ? rate(a.A[(long long)ch * a.N + s]) : 0.f;
+    const int seg_tokens = a.seg_tiles * TILE, live = (row_length(a, (int)b) + seg_tokens - 1) / seg_tokens;
+    const long long seg0 = b * a.segments;
+    if (live == 0) a.seg_s[seg0 * per + i] = S;
+    for (int k = 0; k < live; ++k) {
+        const long long seg = seg0 + (REV ? live - 1 - k : k);
+        a.seg_s[seg * per + i] = S;
+        if (k + 1 < live) S = fmaf(factor(a.seg_g[seg * a.Dp + pad], A), S, a.seg_b[seg * per + i]);
+    }
+}
+
+int launch_join(const Args &a, bool reverse, hipStream_t s)
+{
+    const dim3 grid((unsigned)ceil_div((long long)a.B * a.Dp * a.NP * a.NB, 256));
+    if (reverse) hipLaunchKernelGGL(select_join<true>, grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(select_join<false>, grid, dim3(256), 0, s, a);
+    return launched();
+}
+
+template <typename T, int NP, int NB> static void launch_np(const Args &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)((long long)a.B * a.segments * a.G * a.cbg)), block(64 * (NB > 1 ? NB : a.wide));
+    if (a.segments > 1) {
+        hipLaunchKernelGGL((select_scan<T, NP, NB, true>), grid, block, 0, s, a);
+        launch_join(a, false, s);
+    }
+    hipLaunchKernelGGL((select_scan<T, NP, NB, false>), grid, block, 0, s, a);
+}
+
+template <typename T> static int launch(const Args &a, hipStream_t s)
+{
+    if (a.tiles > 0) hipLaunchKernelGGL((select_prepare<T>), dim3((unsigned)ceil_div((long long)a.B * a.tiles * a.G * a.NP * a.NB * 2 * TILE, 256)), dim3(256), 0, s, a);
+    if (a.NB == 8) launch_np<T, 16, 8>(a, s);
+    else if (a.NB == 4) launch_np<T, 16, 4>(a, s);
+    else if (a.NB == 2) launch_np<T, 16, 2>(a, s);
+    else if (a.NP == 16) launch_np<T, 16, 1>(a, s);
+    else if (a.NP == 8) launch_np<T, 8, 1>(a, s);
+    else launch_np<T, 4, 1>(a, s);
+    return launched();
+}
+
+int launch_forward(const Args &a, bool bf16_, hipStream_t s) { return bf16_ ? launch<bf16>(a, s) : launch<float>(a, s); }
+
+} // namespace select
+} // namespace cawn

@@ -1,0 +1,44 @@
+// Sums over the rows of a matrix of partial sums, in a fixed order: what the workgroups of a backward pass leave of the parameters' gradients.
+#pragma once
+#include "cawn_ops.hpp"
+
+namespace cawn {
+namespace ops {
+
+constexpr int SUM_COLS = 32, SUM_RUNS = 32;
+
+// out(c) gives the place of column c's sum, or null.  A workgroup takes 32 columns; its 32 runs of threads take every 32nd row, and are
+// added up in their order.
+template <typename Out> __global__ __launch_bounds__(SUM_COLS *SUM_RUNS) void column_sums(const float *part, const long long rows, const long long cols, const Out out,
+                                                                                         const int accumulate)
+{
+    __shared__ float sh[SUM_RUNS][SUM_COLS + 1];
+    const int col = threadIdx.x % SUM_COLS, run = threadIdx.x / SUM_COLS;
+    const long long c = (long long)blockIdx.x * SUM_COLS + col;
+    float v = 0.f;
+    if (c < cols) {
+        const float *p = part + c;
+        long long r = run;
+        for (; r + 3 * SUM_RUNS < rows; r += 4 * SUM_RUNS) {
+            const float x0 = p[r * cols], x1 = p[(r + SUM_RUNS) * cols], x2 = p[(r + 2 * SUM_RUNS) * cols], x3 = p[(r + 3 * SUM_RUNS) * cols];
+            v += (x0 + x1) + (x2 + x3);
+        }
+        for (; r < rows; r += SUM_RUNS) v += p[r * cols];
+    }
+    sh[run][col] = v;
+    __syncthreads();
+    if (run == 0 && c < cols) {
+        float s = 0.f;
+        for (int q = 0; q < SUM_RUNS; ++q) s += sh[q][col];
+        float *at = out(c);
+        if (at) *at = accumulate ? *at + s : s;
+    }
+}
+
+template <typename Out> void launch_sums(const float *part, long long rows, long long cols, const Out &out, int accumulate, hipStream_t s)
+{
+    if (cols > 0) hipLaunchKernelGGL((column_sums<Out>), dim3((unsigned)ceil_div(cols, SUM_COLS)), dim3(SUM_COLS * SUM_RUNS), 0, s, part, rows, cols, out, accumulate);
+}
+
+} // namespace ops
+} // namespace cawn
