@@ -17,8 +17,6 @@ constexpr int TOKEN_MAX = 16;       // longest call that goes token by token
 constexpr int N_MAX = 128;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
 struct Args {
     int B, L, D, N, G, cg;          // cg: channels of a group
     int softplus;
@@ -54,15 +52,13 @@ __device__ inline int row_length(const Args &a, int b)
     return n < 0 ? 0 : n < a.L ? n : a.L;
 }
 
-// log(1 + e^v).  With u = 1 + e rounded, log(u) e / (u - 1) corrects the rounding of u (Goldberg 1991, theorem 4).  The hardware's exponential ends at
-// 2^-126, this at 2^-149: the smallest delta still meets a rate of minus infinity.
+// log(1 + e^v) = max(v, 0) + log(1 + e^-|v|).  u = 1 + e rounds e away; what it lost, e - (u - 1), is added to log(u) (its factor 1 / u is left out: it
+// is off from 1 by e, and what was lost is 2^-24 of u at most).  The exponential is the square of the half's: the hardware's ends at 2^-126, this at 2^-149,
+// so that the smallest delta still meets a rate of minus infinity.
 __device__ inline float softplus_f(float v)
 {
-    const float x = -fabsf(v) * LOG2E;
-    const bool low = x < -125.f;
-    const float e = __builtin_amdgcn_exp2f(low ? x + 64.f : x) * (low ? 0x1p-64f : 1.f), u = 1.f + e;
-    const float l = u == 1.f ? e : __builtin_amdgcn_logf(u) * LN2 * (e * __builtin_amdgcn_rcpf(u - 1.f));
-    return fmaxf(v, 0.f) + (v != v ? v : l);
+    const float half = __builtin_amdgcn_exp2f(fabsf(v) * (-0.5f * LOG2E)), e = half * half, u = 1.f + e;
+    return fmaxf(v, 0.f) + fmaf(__builtin_amdgcn_logf(u), LN2, e - (u - 1.f));
 }
 __device__ inline float sigmoid_f(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-z * LOG2E)); }
 
@@ -90,6 +86,9 @@ struct Place {
     int b, g, seg, col, blk, lane, cb;      // col: column of the group; blk: which of the channel's states; cb: workgroup of the group
     bool there, on;                         // the column exists; the lane has a channel
     int ch;                                 // channel (the group's last for lanes without one)
+    long long base;                         // of the group, the same for all lanes; ch = base + in
+    uint32_t in;
+    template <typename T> __device__ uint32_t bytes() const { return in * (uint32_t)sizeof(T); }
     long long pad;                          // place among Dp channels
 };
 
@@ -107,6 +106,7 @@ template <bool MULTI> __device__ inline Place place_of(const Args &a)
     p.there = p.col < a.cpg;
     const int in = min(p.col, a.cpg - 1) * 64 + p.lane;
     p.on = p.there && in < a.cg;
+    p.base = (long long)p.g * a.cg, p.in = min(in, a.cg - 1);
     p.ch = p.g * a.cg + min(in, a.cg - 1);
     p.pad = (long long)(p.g * a.cpg + min(p.col, a.cpg - 1)) * 64 + p.lane;
     return p;
@@ -155,9 +155,50 @@ template <int N> __device__ inline void stay(float (&v)[N])
     for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
 }
 
-// The 16 values of B (which = 0) or C (1) of a tile and a state, the same for all lanes: scalar loads.
-typedef const __attribute__((address_space(4))) f32x16 *ScalarTile;
-__device__ inline f32x16 bc_tile(const float *tile, int n, int which) { return *(ScalarTile)(uintptr_t)(tile + (n * 2 + which) * TILE); }
+// W values of B (which = 0) or C (1) of a tile and a state, the same for all lanes: scalar loads.
+template <int W> using Scalars = float __attribute__((ext_vector_type(W)));
+template <int W> __device__ inline Scalars<W> bc_run(const float *tile, int n, int which)
+{
+    typedef const __attribute__((address_space(4))) Scalars<W> *At;
+    return *(At)(uintptr_t)(tile + (n * 2 + which) * TILE);
+}
+
+// A stream's rows of W tokens from `row` on: the tokens' places are scalar, the lane's 32 bits of bytes, as buffer instructions take them.  (From pointers
+// the compiler adds the lane's place first and walks along the tokens with vector instructions.)  The resource ends nowhere: the callers' bounds count.
+__device__ inline __amdgpu_buffer_rsrc_t rows_at(const void *row) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(row), 0, -1, 0x00020000); }
+template <typename T> __device__ inline T load_at(__amdgpu_buffer_rsrc_t r, uint32_t lane, uint32_t token)
+{
+    if constexpr (sizeof(T) == 2) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(r, lane, token, 0));
+    else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(r, lane, token, 0));
+}
+template <typename T> __device__ inline void store_at(__amdgpu_buffer_rsrc_t r, uint32_t lane, uint32_t token, float v)
+{
+    const T x = (T)v;
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, x), r, lane, token, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x), r, lane, token, 0);
+}
+
+// W tokens of a stream, of which `left` are there (the last of them again for the others); step: of a token, in bytes
+template <typename T, int W> __device__ inline void load_run(const T *row, uint32_t step, int left, uint32_t lane, T (&v)[W])
+{
+    const auto r = rows_at(row);
+    uint32_t token = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        v[i] = load_at<T>(r, lane, token);
+        token += i + 1 < left ? step : 0;
+    }
+}
+
+// ... of an output, from f(i)
+template <typename T, int W, typename F> __device__ inline void store_run(T *row, uint32_t step, int left, uint32_t lane, F f)
+{
+    const auto r = rows_at(row);
+    uint32_t token = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i, token += step)
+        if (i < left) store_at<T>(r, lane, token, f(i));
+}
 
 } // namespace select
 } // namespace cawn

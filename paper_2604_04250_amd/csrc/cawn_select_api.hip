@@ -49,7 +49,9 @@ int check(const cawn_scan_desc *d, bool bwd, Args *a)
     a->wide = a->NB > 1 ? 1 : a->cpg < 4 ? a->cpg : 4;
     a->cbg = (int)ceil_div(a->cpg, a->wide);
     a->parts = a->cbg;
-    if ((long long)a->cpg * G > 0x7fffffffLL / 64) return CAWN_EUNSUPPORTED;
+    // places of a channel in its row and of a token among 16 are 32 bits of bytes
+    const long long wide = 1 << 25;
+    if (d->D > wide || a->xst > wide || a->dst > wide || a->zst > wide || a->yst > wide) return CAWN_EUNSUPPORTED;
     a->Dp = a->cpg * G * 64;
     a->tiles = (int)ceil_div(d->L, TILE);
     cut(a, bwd ? 2048 : 4096);

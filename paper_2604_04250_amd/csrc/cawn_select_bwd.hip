@@ -23,50 +23,71 @@ __device__ inline float dsilu(float z, float &silu)
 // What a segment hands on where nothing reaches its end, and its sum of delta.
 template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 * NB : 256) void select_back(const Args a)
 {
-    constexpr int NPT = NP * NB;
+    constexpr int NPT = NP * NB, AHEAD = 2;
     const Place p = place_of<(NB > 1)>(a);
     if (!p.there) return;
-    const int n = row_length(a, p.b);
-    const long long t0 = (long long)p.seg * a.seg_tiles * TILE, t1 = min((long long)n, t0 + (long long)a.seg_tiles * TILE);
-    if (t0 >= t1) return;
+    const int n = __builtin_amdgcn_readfirstlane(row_length(a, p.b));
+    const int t0 = p.seg * a.seg_tiles * TILE, t1 = min(n, t0 + a.seg_tiles * TILE);
+    if (t0 >= t1 || t0 == 0) return;        // (the chain ends behind the first)
+    const T *dp = (const T *)a.dt + p.b * a.dsb + p.base, *dyp = (const T *)a.dy + p.b * a.ysb + p.base, *zp = a.z ? (const T *)a.z + p.b * a.zsb + p.base : nullptr;
+    const uint32_t at = p.bytes<T>();
+    auto step = [](long long stride) { return (uint32_t)stride * (uint32_t)sizeof(T); };
+    T dr[TILE], yr[TILE], zr[TILE];
+    auto fetch = [&](int t) {
+        if (t < t0) return;
+        const int left = t1 - t;
+        load_run<T, TILE>(dp + t * a.dst, step(a.dst), left, at, dr);
+        load_run<T, TILE>(dyp + t * a.yst, step(a.yst), left, at, yr);
+        if (zp) load_run<T, TILE>(zp + t * a.zst, step(a.zst), left, at, zr);
+    };
+    const int last = (t1 - 1) / TILE * TILE;
+    fetch(last);
     float A[NP], h[NP], total = 0.f;
     load_rates<NP>(a, p, A);
 #pragma unroll
     for (int i = 0; i < NP; ++i) h[i] = 0.f;
     const float bias = a.bias ? a.bias[p.ch] : 0.f;
-    const T *dp = (const T *)a.dt + p.b * a.dsb + p.ch, *dyp = (const T *)a.dy + p.b * a.ysb + p.ch;
-    const T *zp = a.z ? (const T *)a.z + p.b * a.zsb + p.ch : nullptr;
-    for (long long t = (t1 - 1) / TILE * TILE; t >= t0; t -= TILE) {
-        const int left = (int)min(t1 - t, (long long)TILE);
+    for (int t = last; t >= t0; t -= TILE) {
+        const int left = t1 - t;
         const float *tile = a.bc + (((long long)p.b * a.tiles + t / TILE) * a.G + p.g) * NPT * 2 * TILE + p.blk * NP * 2 * TILE;
+        Scalars<TILE> Cq[NP];
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s) Cq[s] = bc_run<TILE>(tile, s, 1);
         float delta[TILE], g[TILE];
-        T zr[TILE];
 #pragma unroll
         for (int i = 0; i < TILE; ++i) {
-            const long long at = t + min(i, left - 1);
-            delta[i] = (float)dp[at * a.dst] + bias;
-            g[i] = (float)dyp[at * a.yst];
-            zr[i] = zp ? zp[at * a.zst] : (T)0.f;
+            delta[i] = (float)dr[i] + bias;
+            g[i] = (float)yr[i];
+        }
+        if (a.softplus) {
+#pragma unroll
+            for (int i = 0; i < TILE; ++i) delta[i] = softplus_f(delta[i]);
+        }
+        if (zp) {
+#pragma unroll
+            for (int i = 0; i < TILE; ++i) {
+                const float z = (float)zr[i];
+                g[i] *= z * sigmoid_f(z);
+            }
+        }
+        if (left < TILE) {
+#pragma unroll
+            for (int i = 0; i < TILE; ++i) {
+                delta[i] = i < left ? delta[i] : 0.f;
+                g[i] = i < left ? g[i] : 0.f;
+            }
         }
 #pragma unroll
-        for (int i = 0; i < TILE; ++i) {
-            if (a.softplus) delta[i] = softplus_f(delta[i]);
-            const float z = (float)zr[i];
-            if (zp) g[i] *= z * sigmoid_f(z);
-            delta[i] = i < left ? delta[i] : 0.f;
-            g[i] = i < left ? g[i] : 0.f;
-            total += delta[i];
-        }
-        f32x16 Cn = bc_tile(tile, 0, 1);
+        for (int i = 0; i < TILE; ++i) total += delta[i];
+        fetch(t - TILE);
 #pragma unroll
         for (int s = 0; s < NP; ++s) {
-            const f32x16 Cv = Cn;
 #pragma unroll
             for (int i = TILE - 1; i >= 0; --i) {
-                h[s] = factor(delta[i], A[s]) * fmaf(Cv[i], g[i], h[s]);
-                if (i == TILE - 1 && s + 1 < NP) {      // (as in the forward)
+                h[s] = factor(delta[i], A[s]) * fmaf(Cq[s][i], g[i], h[s]);
+                if (i == TILE - 1 && s + AHEAD < NP) {      // (as in the forward)
                     __builtin_amdgcn_sched_barrier(0);
-                    Cn = bc_tile(tile, s + 1, 1);
+                    Cq[s + AHEAD < NP ? s + AHEAD : 0] = bc_run<TILE>(tile, s + AHEAD, 1);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -124,9 +145,10 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
     __shared__ float stage[2][MULTI ? 1 : WAVES][TILE][2][NP];
     __shared__ float xch[MULTI ? NB : 1][TILE][64];
     const Place p = place_of<MULTI>(a);
-    const int n = row_length(a, p.b), w = MULTI ? p.blk : __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const long long t0 = (long long)p.seg * a.seg_tiles * TILE, t1 = min((long long)n, t0 + (long long)a.seg_tiles * TILE), end = min((long long)a.L, t0 + (long long)a.seg_tiles * TILE);
+    const int n = __builtin_amdgcn_readfirstlane(row_length(a, p.b)), w = MULTI ? p.blk : __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int t0 = p.seg * a.seg_tiles * TILE, t1 = min(n, t0 + a.seg_tiles * TILE), end = min(a.L, t0 + a.seg_tiles * TILE);
     const long long seg = (long long)p.b * a.segments + p.seg, user = (long long)p.b * a.D + p.ch;
+    const bool whole = (p.cb + 1) * (MULTI ? 1 : a.wide) * 64 <= a.cg;       // every lane of the workgroup has a channel
     float(*mine)[3][64] = carry[w];
     {
         float A[NP], h[NP];
@@ -140,90 +162,121 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
         for (int i = 0; i < NP; ++i) mine[i][0][p.lane] = h[i], mine[i][1][p.lane] = 0.f, mine[i][2][p.lane] = A[i];
     }
     const float bias = a.bias ? a.bias[p.ch] : 0.f, Dk = a.Dk ? a.Dk[p.ch] : 0.f;
-    const T *xp = (const T *)a.x + p.b * a.xsb + p.ch, *dp = (const T *)a.dt + p.b * a.dsb + p.ch, *dyp = (const T *)a.dy + p.b * a.ysb + p.ch;
-    const T *zp = a.z ? (const T *)a.z + p.b * a.zsb + p.ch : nullptr;
-    T *dxp = a.dx ? (T *)a.dx + p.b * a.xsb + p.ch : nullptr, *ddp = a.ddt ? (T *)a.ddt + p.b * a.dsb + p.ch : nullptr;
-    T *dzp = a.dz ? (T *)a.dz + p.b * a.zsb + p.ch : nullptr;
+    const T *xp = (const T *)a.x + p.b * a.xsb + p.base, *dp = (const T *)a.dt + p.b * a.dsb + p.base, *dyp = (const T *)a.dy + p.b * a.ysb + p.base;
+    const T *zp = a.z ? (const T *)a.z + p.b * a.zsb + p.base : nullptr;
+    T *dxp = a.dx ? (T *)a.dx + p.b * a.xsb + p.base : nullptr, *ddp = a.ddt ? (T *)a.ddt + p.b * a.dsb + p.base : nullptr;
+    T *dzp = a.dz ? (T *)a.dz + p.b * a.zsb + p.base : nullptr;
+    const uint32_t at = p.bytes<T>();
+    auto step = [](long long stride) { return (uint32_t)stride * (uint32_t)sizeof(T); };
+    T xr[TILE], xn[TILE], dr[TILE], yr[TILE], zr[TILE];
+    auto fetch = [&](int t) {
+        if (t < t0) return;
+        const int left = t1 - t;
+        load_run<T, TILE>(dp + t * a.dst, step(a.dst), left, at, dr);
+        load_run<T, TILE>(xp + t * a.xst, step(a.xst), left, at, xn);
+        load_run<T, TILE>(dyp + t * a.yst, step(a.yst), left, at, yr);
+        if (zp) load_run<T, TILE>(zp + t * a.zst, step(a.zst), left, at, zr);
+    };
+    const int last = t1 > t0 ? (t1 - 1) / TILE * TILE : t0 - 1;
+    fetch(last);
+    const float first = MULTI && p.blk > 0 ? 0.f : Dk;          // (one wave adds D x to y)
     float sumD = 0.f, sumb = 0.f;
     int buf = 0;
-    for (long long t = t1 > t0 ? (t1 - 1) / TILE * TILE : t0 - 1; t >= t0; t -= TILE) {
-        const int left = (int)min(t1 - t, (long long)TILE);
+    for (int t = last; t >= t0; t -= TILE) {
+        const int left = t1 - t;
         const long long bt = (long long)p.b * a.tiles + t / TILE;
         const float *tile = a.bc + (bt * a.G + p.g) * NPT * 2 * TILE + p.blk * NP * 2 * TILE;
         const float *ck = a.ck + (bt * a.Dp + p.pad) * NPT + p.blk * NP;
+        // a state's B, C, begin, h, dA and A, each asked for while the state before is worked on
+        Scalars<TILE> Bv[2], Cv[2];
+        float before[2], h[2], dA[2], A[2];
+        auto ask = [&](int j, int s) {
+            Bv[j] = bc_run<TILE>(tile, s, 0), Cv[j] = bc_run<TILE>(tile, s, 1);
+            before[j] = ck[s];
+            h[j] = mine[s][0][p.lane], dA[j] = mine[s][1][p.lane], A[j] = mine[s][2][p.lane];
+        };
+        ask(0, 0);
         float delta[TILE], slope[TILE], u[TILE], g[TILE], q[TILE], du[TILE], dd[TILE], y[TILE];
 #pragma unroll
         for (int i = 0; i < TILE; ++i) {
-            const long long at = t + min(i, left - 1);
-            delta[i] = (float)dp[at * a.dst] + bias;
-            u[i] = (float)xp[at * a.xst];
-            g[i] = (float)dyp[at * a.yst];
-            q[i] = zp ? (float)zp[at * a.zst] : 0.f;
+            xr[i] = xn[i];
+            const float x = (float)xr[i];
+            delta[i] = (float)dr[i] + bias;
+            g[i] = (float)yr[i];
+            slope[i] = 1.f, q[i] = 0.f, u[i] = x;
+            y[i] = first * x;
+            du[i] = dd[i] = 0.f;
         }
+        if (a.softplus) {
 #pragma unroll
-        for (int i = 0; i < TILE; ++i) {
-            slope[i] = 1.f;
-            if (a.softplus) {
+            for (int i = 0; i < TILE; ++i) {
                 slope[i] = sigmoid_f(delta[i]);
                 delta[i] = softplus_f(delta[i]);
             }
-            if (zp) {
+        }
+        if (zp) {
+#pragma unroll
+            for (int i = 0; i < TILE; ++i) {
                 float silu;
-                const float ds = dsilu(q[i], silu);
+                const float ds = dsilu((float)zr[i], silu);
                 q[i] = g[i] * ds;
                 g[i] *= silu;
             }
-            // (behind the last token, and where there is no channel, nothing is added anywhere)
-            delta[i] = i < left ? delta[i] : 0.f;
-            y[i] = Dk * u[i];
-            u[i] = i < left && p.on ? delta[i] * u[i] : 0.f;
-            g[i] = i < left && p.on ? g[i] : 0.f;
-            du[i] = dd[i] = 0.f;
         }
-        if (MULTI && p.blk > 0) {
 #pragma unroll
-            for (int i = 0; i < TILE; ++i) y[i] = 0.f;
+        for (int i = 0; i < TILE; ++i) u[i] *= delta[i];
+        if (left < TILE) {          // behind the last token nothing is added anywhere
+#pragma unroll
+            for (int i = 0; i < TILE; ++i) {
+                delta[i] = i < left ? delta[i] : 0.f;
+                u[i] = i < left ? u[i] : 0.f;
+                g[i] = i < left ? g[i] : 0.f;
+            }
         }
+        if (!whole) {               // ... nor where there is no channel
+#pragma unroll
+            for (int i = 0; i < TILE; ++i) {
+                u[i] = p.on ? u[i] : 0.f;
+                g[i] = p.on ? g[i] : 0.f;
+            }
+        }
+        stay<TILE>(slope);
+        stay<TILE>(q);
 #pragma unroll 1
         for (int s = 0; s < NP; s += 2) {
-            f32x16 Bv[2], Cv[2];
-            float S[2][TILE], e[2][MULTI ? 1 : TILE], before[2], h[2], dA[2], A[2], Af[2];     // (a channel's factors are made again where registers are short)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                Bv[j] = bc_tile(tile, s + j, 0), Cv[j] = bc_tile(tile, s + j, 1);
-                before[j] = ck[s + j];
-                h[j] = mine[s + j][0][p.lane], dA[j] = mine[s + j][1][p.lane], A[j] = mine[s + j][2][p.lane];
-                Af[j] = fmaxf(A[j], -3.4028235e38f);        // (where the rate is minus infinity p is 0, and so is its share)
-            }
-#pragma unroll
-            for (int i = 0; i < TILE; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float f = factor(delta[i], A[j]);
-                    if (!MULTI) e[j][MULTI ? 0 : i] = f;
-                    S[j][i] = fmaf(f, i ? S[j][i ? i - 1 : 0] : before[j], u[i] * Bv[j][i]);
-                    y[i] = fmaf(Cv[j][i], S[j][i], y[i]);
-                }
             LaneSums sums;
             float all = 0.f;
 #pragma unroll
-            for (int i = TILE - 1; i >= 0; --i)
+            for (int j = 0; j < 2; ++j) {
+                float S[TILE], e[TILE];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int k = ((TILE - 1 - i) * 2 + j) * 2;
+                for (int i = 0; i < TILE; ++i) {
+                    e[i] = factor(delta[i], A[j]);
+                    S[i] = fmaf(e[i], i ? S[i ? i - 1 : 0] : before[j], u[i] * Bv[j][i]);
+                    y[i] = fmaf(Cv[j][i], S[i], y[i]);
+                    if (i == 0) {       // (the wait for this state's is over)
+                        __builtin_amdgcn_sched_barrier(0);
+                        ask(1 - j, j ? min(s + 2, NP - 2) : s + 1);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                const float Af = fmaxf(A[j], -3.4028235e38f);       // (where the rate is minus infinity p is 0, and so is its share)
+#pragma unroll
+                for (int i = TILE - 1; i >= 0; --i) {
+                    const int k = (j * TILE + TILE - 1 - i) * 2;
                     const float dS = fmaf(Cv[j][i], g[i], h[j]);
                     du[i] = fmaf(Bv[j][i], dS, du[i]);
-                    h[j] = (MULTI ? factor(delta[i], A[j]) : e[j][MULTI ? 0 : i]) * dS;
-                    const float pr = h[j] * (i ? S[j][i ? i - 1 : 0] : before[j]);
-                    dd[i] = fmaf(Af[j], pr, dd[i]);
+                    h[j] = e[i] * dS;
+                    const float pr = h[j] * (i ? S[i ? i - 1 : 0] : before[j]);
+                    dd[i] = fmaf(Af, pr, dd[i]);
                     dA[j] = fmaf(delta[i], pr, dA[j]);
                     sums.push(k, u[i] * dS, p.lane);
-                    all = sums.push(k + 1, g[i] * S[j][i], p.lane);
+                    all = sums.push(k + 1, g[i] * S[i], p.lane);
                 }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) mine[s + j][0][p.lane] = h[j], mine[s + j][1][p.lane] = dA[j];
-            const int which = p.lane >> 5 & 1, j = p.lane >> 4 & 1;
-            const int i = TILE - 1 - ((p.lane >> 3 & 1) | (p.lane >> 1 & 2) | (p.lane << 1 & 4) | (p.lane << 3 & 8));
+                mine[s + j][0][p.lane] = h[j], mine[s + j][1][p.lane] = dA[j];
+            }
+            const int which = p.lane >> 5 & 1, j = p.lane & 1;
+            const int i = TILE - 1 - ((p.lane >> 4 & 1) | (p.lane >> 2 & 2) | (p.lane & 4) | (p.lane << 2 & 8));
             if (MULTI) {
                 if (a.part_bc) a.part_bc[((((bt * TILE + i) * a.G + p.g) * a.parts + p.cb) * 2 + which) * NPT + p.blk * NP + s + j] = all;
             } else stage[buf][MULTI ? 0 : w][i][which][s + j] = all;
@@ -231,6 +284,7 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
         stay<TILE>(du);
         stay<TILE>(dd);
         stay<TILE>(y);
+        fetch(t - TILE);
         if (!MULTI && a.part_bc) {
             __syncthreads();
             for (int k = threadIdx.x; k < TILE * 2 * NP; k += blockDim.x) {
@@ -259,26 +313,38 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
             exchange(dd);
             if (dzp) exchange(y);
         }
+        // (dd becomes the gradient of dt, du that of x, y that of z)
 #pragma unroll
         for (int i = 0; i < TILE; ++i) {
-            if (i >= left || (MULTI && i % NB != p.blk)) continue;
-            const long long at = t + i;
-            const float x = (float)xp[at * a.xst];
-            const float dv = fmaf(du[i], x, dd[i] * LN2) * slope[i];
-            sumD = fmaf(g[i], x, sumD);
-            if (p.on) {
-                sumb += dv;
-                if (dxp) dxp[at * a.xst] = (T)fmaf(du[i], delta[i], Dk * g[i]);
-                if (ddp) ddp[at * a.dst] = (T)dv;
-                if (dzp) dzp[at * a.zst] = (T)(q[i] * y[i]);
-            }
+            if (MULTI && i % NB != p.blk) continue;
+            const float x = (float)xr[i];
+            dd[i] = i < left ? fmaf(du[i], x, dd[i] * LN2) * slope[i] : 0.f;
+            du[i] = fmaf(du[i], delta[i], Dk * g[i]);
+            y[i] *= q[i];
+            sumD = fmaf(g[i], i < left ? x : 0.f, sumD);
+            sumb += dd[i];
+        }
+        if (p.on) {
+            auto out = [&](T *row, long long stride, const float(&v)[TILE]) {
+                if (!row) return;
+                row += t * stride;
+                if (!MULTI) store_run<T, TILE>(row, step(stride), left, at, [&](int i) { return v[i]; });
+                else {
+#pragma unroll
+                    for (int i = 0; i < TILE; ++i)
+                        if (i < left && i % NB == p.blk) store_at<T>(rows_at(row + i * stride), at, 0, v[i]);
+                }
+            };
+            out(dxp, a.xst, du);
+            out(ddp, a.dst, dd);
+            out(dzp, a.zst, y);
         }
     }
     if (p.on && p.blk == 0) {
-        for (long long t = max(t0, (long long)n); t < end; ++t) {
-            if (dxp) dxp[t * a.xst] = (T)0.f;
-            if (ddp) ddp[t * a.dst] = (T)0.f;
-            if (dzp) dzp[t * a.zst] = (T)0.f;
+        for (int t = max(t0, n); t < end; ++t) {
+            if (dxp) store_at<T>(rows_at(dxp + t * a.xst), at, 0, 0.f);
+            if (ddp) store_at<T>(rows_at(ddp + t * a.dst), at, 0, 0.f);
+            if (dzp) store_at<T>(rows_at(dzp + t * a.zst), at, 0, 0.f);
         }
     }
     if (!p.there) return;

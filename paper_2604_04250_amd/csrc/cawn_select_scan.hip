@@ -6,6 +6,10 @@
 // What bounds it: instruction issue.  A token's state costs a product, an exponential (two issue slots), a product and two sums, 24 cycles of a SIMD a
 // wave, and a token 150 more for softplus, the gate, conversions and memory.
 #include "cawn_select.hpp"
+#ifndef CAWN_RUN1
+#define CAWN_RUN1 16
+#define CAWN_RUN2 8
+#endif
 
 namespace cawn {
 namespace select {
@@ -24,19 +28,33 @@ template <typename T> __global__ __launch_bounds__(256) void select_prepare(cons
     a.bc[id] = v;
 }
 
-// NB waves share a channel's states
+// NB waves share a channel's states.  RUN tokens at a time, the next ones' streams on their way meanwhile.
 template <typename T, int NP, int NB, bool SUMMARY> __global__ __launch_bounds__(NB > 1 ? 64 * NB : 256) void select_scan(const Args a)
 {
     constexpr bool MULTI = NB > 1;
-    __shared__ float ys[2][MULTI && !SUMMARY ? NB : 1][TILE][64];       // the waves' shares of y
+    constexpr int RUN = SUMMARY ? CAWN_RUN1 : CAWN_RUN2, NPT = NP * NB, AHEAD = 2;
+    __shared__ float ys[2][MULTI && !SUMMARY ? NB : 1][RUN][64];        // the waves' shares of y
     const Place p = place_of<MULTI>(a);
     if (!MULTI && !p.there) return;
-    constexpr int NPT = NP * NB;
-    const int n = row_length(a, p.b);
-    const long long t0 = (long long)p.seg * a.seg_tiles * TILE, t1 = min((long long)n, t0 + (long long)a.seg_tiles * TILE);
-    if (SUMMARY && t0 >= t1) return;        // (the chain ends before it)
+    const int n = __builtin_amdgcn_readfirstlane(row_length(a, p.b));
+    const int t0 = p.seg * a.seg_tiles * TILE, t1 = min(n, t0 + a.seg_tiles * TILE), end = min(a.L, t0 + a.seg_tiles * TILE);
+    if (SUMMARY && (t0 >= t1 || t1 == n)) return;       // (the chain ends before it)
     const long long sat = (((long long)p.b * a.segments + p.seg) * a.Dp + p.pad) * NPT + p.blk * NP;
     const long long user = (long long)p.b * a.D + p.ch;
+    const T *xp = (const T *)a.x + p.b * a.xsb + p.base + t0 * a.xst, *dp = (const T *)a.dt + p.b * a.dsb + p.base + t0 * a.dst;
+    const T *zp = !SUMMARY && a.z ? (const T *)a.z + p.b * a.zsb + p.base + t0 * a.zst : nullptr;
+    const uint32_t at = p.bytes<T>();
+    auto step = [](long long stride) { return (uint32_t)stride * (uint32_t)sizeof(T); };
+    T xr[RUN], dr[RUN], zr[SUMMARY ? 1 : RUN];
+    auto fetch = [&](int t) {
+        const int left = t1 - t;
+        if (left > 0) {
+            load_run<T, RUN>(dp, step(a.dst), left, at, dr);
+            load_run<T, RUN>(xp, step(a.xst), left, at, xr);
+            dp += RUN * a.dst, xp += RUN * a.xst;
+        }
+    };
+    fetch(t0);
     float A[NP], S[NP], total = 0.f;
     load_rates<NP>(a, p, A);
 #pragma unroll
@@ -47,72 +65,97 @@ template <typename T, int NP, int NB, bool SUMMARY> __global__ __launch_bounds__
         } else if (a.state_in) load_user<NP>(a.state_in, a, user, p.blk * NP, S);
     }
     const float bias = a.bias ? a.bias[p.ch] : 0.f, Dk = a.Dk && p.blk == 0 ? a.Dk[p.ch] : 0.f;
-    const T *xp = (const T *)a.x + p.b * a.xsb + p.ch, *dp = (const T *)a.dt + p.b * a.dsb + p.ch;
-    const T *zp = !SUMMARY && a.z ? (const T *)a.z + p.b * a.zsb + p.ch : nullptr;
-    T *yp = SUMMARY ? nullptr : (T *)a.y + p.b * a.ysb + p.ch;
+    T *yp = SUMMARY ? nullptr : (T *)a.y + p.b * a.ysb + p.base + t0 * a.yst;
     int buf = 0;
-    for (long long t = t0; t < t1; t += TILE) {
-        const int left = (int)min(t1 - t, (long long)TILE);
-        const float *tile = a.bc + (((long long)p.b * a.tiles + t / TILE) * a.G + p.g) * NPT * 2 * TILE + p.blk * NP * 2 * TILE;
-        if (!SUMMARY && a.ck && p.there) store_states<NP>(a.ck + (((long long)p.b * a.tiles + t / TILE) * a.Dp + p.pad) * NPT + p.blk * NP, S);
-        float delta[TILE], u[TILE], y[SUMMARY ? 1 : TILE];
-        T zr[SUMMARY ? 1 : TILE];
+    for (int t = t0; t < t1; t += RUN) {
+        const int left = t1 - t;
+        const float *tile = a.bc + (((long long)p.b * a.tiles + t / TILE) * a.G + p.g) * NPT * 2 * TILE + p.blk * NP * 2 * TILE + t % TILE;
+        if (!SUMMARY && a.ck && p.there && t % TILE == 0) store_states<NP>(a.ck + (((long long)p.b * a.tiles + t / TILE) * a.Dp + p.pad) * NPT + p.blk * NP, S);
+        Scalars<RUN> Bq[NP], Cq[NP];
 #pragma unroll
-        for (int i = 0; i < TILE; ++i) {
-            const long long at = t + min(i, left - 1);
-            delta[i] = (float)dp[at * a.dst] + bias;
-            u[i] = (float)xp[at * a.xst];
-            if constexpr (!SUMMARY) zr[i] = zp ? zp[at * a.zst] : (T)0.f;
+        for (int s = 0; s < AHEAD; ++s) {
+            Bq[s] = bc_run<RUN>(tile, s, 0);
+            if (!SUMMARY) Cq[s] = bc_run<RUN>(tile, s, 1);
         }
+        float delta[RUN], u[RUN], y[SUMMARY ? 1 : RUN];
 #pragma unroll
-        for (int i = 0; i < TILE; ++i) {
-            if (a.softplus) delta[i] = softplus_f(delta[i]);
+        for (int i = 0; i < RUN; ++i) {
+            delta[i] = (float)dr[i] + bias, u[i] = (float)xr[i];
             if constexpr (!SUMMARY) y[i] = Dk * u[i];
-            delta[i] = i < left ? delta[i] : 0.f;       // (behind the last token nothing changes)
-            u[i] = i < left ? delta[i] * u[i] : 0.f;
-            if (SUMMARY) total += delta[i];
         }
-        // (the next state's B and C are asked for behind the first token of this one, whose wait would be for them too; without the fences the compiler
-        // asks for all at once and keeps them in lanes of vector registers)
-        f32x16 Bn = bc_tile(tile, 0, 0), Cn = Bn;
-        if constexpr (!SUMMARY) Cn = bc_tile(tile, 0, 1);
+        if (a.softplus) {
+#pragma unroll
+            for (int i = 0; i < RUN; ++i) delta[i] = softplus_f(delta[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) u[i] *= delta[i];
+        if (left < RUN) {           // behind the last token nothing changes
+#pragma unroll
+            for (int i = 0; i < RUN; ++i) {
+                delta[i] = i < left ? delta[i] : 0.f;
+                u[i] = i < left ? u[i] : 0.f;
+            }
+        }
+        if constexpr (SUMMARY) {
+#pragma unroll
+            for (int i = 0; i < RUN; ++i) total += delta[i];
+        } else {
+            if (zp) {
+                load_run<T, RUN>(zp, step(a.zst), left, at, zr);
+                zp += RUN * a.zst;
+            }
+        }
+        fetch(t + RUN);
+        // (B and C of the state after next are asked for behind the first token of this one, whose wait would be for them too; without the fences the
+        // compiler asks for all at once and keeps them in lanes of vector registers)
 #pragma unroll
         for (int s = 0; s < NP; ++s) {
-            const f32x16 Bv = Bn, Cv = Cn;
 #pragma unroll
-            for (int i = 0; i < TILE; ++i) {
-                S[s] = fmaf(factor(delta[i], A[s]), S[s], u[i] * Bv[i]);
-                if constexpr (!SUMMARY) y[i] = fmaf(Cv[i], S[s], y[i]);
-                if (i == 0 && s + 1 < NP) {
+            for (int i = 0; i < RUN; ++i) {
+                S[s] = fmaf(factor(delta[i], A[s]), S[s], u[i] * Bq[s][i]);
+                if constexpr (!SUMMARY) y[i] = fmaf(Cq[s][i], S[s], y[i]);
+                if (i == 0 && s + AHEAD < NP) {
                     __builtin_amdgcn_sched_barrier(0);
-                    Bn = bc_tile(tile, s + 1, 0);
-                    if constexpr (!SUMMARY) Cn = bc_tile(tile, s + 1, 1);
+                    Bq[s + AHEAD < NP ? s + AHEAD : 0] = bc_run<RUN>(tile, s + AHEAD, 0);
+                    if constexpr (!SUMMARY) Cq[s + AHEAD < NP ? s + AHEAD : 0] = bc_run<RUN>(tile, s + AHEAD, 1);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (!SUMMARY) {
-            stay<TILE>(y);
-            if (MULTI) {        // (two buffers: a wave may be a tile ahead of another)
+            stay<RUN>(y);
+            if (MULTI) {        // (two buffers: a wave may be a run ahead of another)
                 buf ^= 1;
 #pragma unroll
-                for (int i = 0; i < TILE; ++i) ys[buf][p.blk][i][p.lane] = y[i];
+                for (int i = 0; i < RUN; ++i) ys[buf][p.blk][i][p.lane] = y[i];
                 __syncthreads();
             }
+            if (MULTI) {
 #pragma unroll
-            for (int i = 0; i < TILE; ++i) {
-                if (i >= left || (MULTI && i % NB != p.blk)) continue;
-                float v = y[i];
-                if (MULTI) {
-                    v = 0.f;
+                for (int i = 0; i < RUN; ++i) {
+                    if (i % NB != p.blk) continue;
+                    y[i] = 0.f;
 #pragma unroll
-                    for (int k = 0; k < NB; ++k) v += ys[buf][MULTI ? k : 0][i][p.lane];
+                    for (int k = 0; k < NB; ++k) y[i] += ys[buf][MULTI ? k : 0][i][p.lane];
                 }
-                const float z = (float)zr[i];
-                if (zp) v *= z * sigmoid_f(z);
-                if (p.on) yp[(t + i) * a.yst] = (T)v;
             }
+            if (zp) {
+#pragma unroll
+                for (int i = 0; i < RUN; ++i) {
+                    const float z = (float)zr[i];
+                    y[i] *= z * sigmoid_f(z);
+                }
+            }
+            if (p.on) {
+                if (!MULTI) store_run<T, RUN>(yp, step(a.yst), left, at, [&](int i) { return y[i]; });
+                else {
+#pragma unroll
+                    for (int i = 0; i < RUN; ++i)
+                        if (i < left && i % NB == p.blk) store_at<T>(rows_at(yp + i * a.yst), at, 0, y[i]);
+                }
+            }
+            yp += RUN * a.yst;
         }
     }
     if (SUMMARY) {
@@ -121,7 +164,7 @@ template <typename T, int NP, int NB, bool SUMMARY> __global__ __launch_bounds__
         return;
     }
     if (p.on && p.blk == 0)
-        for (long long t = max(t0, (long long)n); t < min((long long)a.L, t0 + (long long)a.seg_tiles * TILE); ++t) yp[t * a.yst] = (T)0.f;
+        for (int t = max(t0, n); t < end; ++t) store_at<T>(rows_at((T *)a.y + p.b * a.ysb + p.base + t * a.yst), at, 0, 0.f);
     // the segment of the row's last token, or of a row without any the first
     if (p.on && a.state_out && (n == 0 ? p.seg == 0 : t0 < t1 && t1 == n)) store_user<NP>(a.state_out, a, user, p.blk * NP, S);
 }
@@ -139,12 +182,22 @@ template <bool REV> __global__ __launch_bounds__(256) void select_join(const Arg
     float S = on && begin ? begin[(b * a.D + ch) * a.N + s] : 0.f;
     const float A = on ? rate(a.A[(long long)ch * a.N + s]) : 0.f;
     const int seg_tokens = a.seg_tiles * TILE, live = (row_length(a, (int)b) + seg_tokens - 1) / seg_tokens;
-    const long long seg0 = b * a.segments;
-    if (live == 0) a.seg_s[seg0 * per + i] = S;
-    for (int k = 0; k < live; ++k) {
-        const long long seg = seg0 + (REV ? live - 1 - k : k);
-        a.seg_s[seg * per + i] = S;
-        if (k + 1 < live) S = fmaf(factor(a.seg_g[seg * a.Dp + pad], A), S, a.seg_b[seg * per + i]);
+    const long long seg0 = b * a.segments + (REV ? live - 1 : 0), to = REV ? -1 : 1;
+    if (live == 0) a.seg_s[b * a.segments * per + i] = S;
+    constexpr int LINKS = 8;            // asked for at once: none of their loads waits for another
+    for (int k = 0; k < live; k += LINKS) {
+        float gs[LINKS], bs[LINKS];
+#pragma unroll
+        for (int j = 0; j < LINKS; ++j) {
+            const long long seg = seg0 + to * min(k + j, max(live - 2, 0));
+            gs[j] = a.seg_g[seg * a.Dp + pad], bs[j] = a.seg_b[seg * per + i];
+        }
+#pragma unroll
+        for (int j = 0; j < LINKS; ++j) {
+            if (k + j >= live) break;
+            a.seg_s[(seg0 + to * (k + j)) * per + i] = S;
+            S = fmaf(factor(gs[j], A), S, bs[j]);       // (behind the last, of no use)
+        }
     }
 }
 
