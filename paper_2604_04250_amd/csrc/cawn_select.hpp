@@ -15,6 +15,7 @@ using namespace cawn::ops;
 constexpr int TILE = 16;            // tokens treated at once; the states before each tile are kept for a backward
 constexpr int TOKEN_MAX = 16;       // longest call that goes token by token
 constexpr int N_MAX = 128;
+constexpr int SEGMENTS_MAX = 256;   // of a row
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct Args {
@@ -128,17 +129,32 @@ template <int NP> __device__ inline void store_states(float *p, const float (&s)
     for (int i = 0; i < NP; i += 4) *reinterpret_cast<f32x4 *>(p + i) = f32x4{s[i], s[i + 1], s[i + 2], s[i + 3]};
 }
 
-// ... of the caller's [D][N], states n0 .. n0 + NP - 1 of channel ch, those that there are (0 for the others)
+// ... of the caller's [D][N], states n0 .. n0 + NP - 1 of channel ch, those that there are (0 for the others); four at a time where N and the address allow it
 template <int NP> __device__ inline void load_user(const float *p, const Args &a, long long ch, int n0, float (&s)[NP])
 {
+    if (a.N % 4 == 0 && ((uintptr_t)p & 15) == 0) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) s[i] = n0 + i < a.N ? p[ch * a.N + n0 + i] : 0.f;
+        for (int i = 0; i < NP; i += 4) {
+            const f32x4 v = n0 + i < a.N ? *reinterpret_cast<const f32x4 *>(p + ch * a.N + n0 + i) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[i + j] = v[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) s[i] = n0 + i < a.N ? p[ch * a.N + n0 + i] : 0.f;
+    }
 }
 template <int NP> __device__ inline void store_user(float *p, const Args &a, long long ch, int n0, const float (&s)[NP])
 {
+    if (a.N % 4 == 0 && ((uintptr_t)p & 15) == 0) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i)
-        if (n0 + i < a.N) p[ch * a.N + n0 + i] = s[i];
+        for (int i = 0; i < NP; i += 4)
+            if (n0 + i < a.N) *reinterpret_cast<f32x4 *>(p + ch * a.N + n0 + i) = f32x4{s[i], s[i + 1], s[i + 2], s[i + 3]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+            if (n0 + i < a.N) p[ch * a.N + n0 + i] = s[i];
+    }
 }
 
 template <int NP> __device__ inline void load_rates(const Args &a, const Place &p, float (&A)[NP])

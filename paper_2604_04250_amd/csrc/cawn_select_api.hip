@@ -1,5 +1,11 @@
 // Selective state space scan: argument checks, sizes and the choice of a form.
 #include "cawn_select.hpp"
+#ifndef CAWN_WF
+#define CAWN_WF 8192
+#endif
+#ifndef CAWN_WB
+#define CAWN_WB 6144
+#endif
 
 using namespace cawn;
 using namespace cawn::ops;
@@ -15,17 +21,16 @@ void cut(Args *a, long long waves)
     const long long want = columns > 0 ? waves / columns : 1;
     a->segments = 1, a->seg_tiles = a->tiles > 0 ? a->tiles : 1;
     if (want < 2 || a->tiles < 2) return;
-    a->seg_tiles = (int)ceil_div(a->tiles, want);
+    a->seg_tiles = (int)ceil_div(a->tiles, want < select::SEGMENTS_MAX ? want : select::SEGMENTS_MAX);
     a->segments = (int)ceil_div(a->tiles, a->seg_tiles);
 }
 
 // More workgroups than a grid has, in any of the launches, or more bytes than are counted.
 bool too_many(const Args &a)
 {
-    const long long most = 1LL << 38;       // threads
-    const double npt = a.NP * a.NB, rows = (double)a.B * a.G;
-    if ((double)a.B * a.tiles * a.Dp * npt > 1e17) return true;
-    return rows * a.tiles * npt * 2 * TILE > most || (double)a.B * a.Dp * npt > most || rows * a.segments * a.cbg > (double)0x7fffffff;
+    const double npt = a.NP * a.NB, rows = (double)a.B * a.G, most = 0x7fffffff;
+    return (double)a.B * a.tiles * a.Dp * npt > 1e17 || rows * a.tiles > most || (double)a.B * a.Dp * npt / 16 > most || rows * a.segments * a.cbg > most ||
+           rows * a.L * 2 * npt / 256 > most;
 }
 
 int check(const cawn_scan_desc *d, bool bwd, Args *a)
@@ -54,7 +59,7 @@ int check(const cawn_scan_desc *d, bool bwd, Args *a)
     if (d->D > wide || a->xst > wide || a->dst > wide || a->zst > wide || a->yst > wide) return CAWN_EUNSUPPORTED;
     a->Dp = a->cpg * G * 64;
     a->tiles = (int)ceil_div(d->L, TILE);
-    cut(a, bwd ? 2048 : 4096);
+    cut(a, bwd ? CAWN_WB : CAWN_WF);
     return too_many(*a) ? CAWN_EUNSUPPORTED : CAWN_OK;
 }
 

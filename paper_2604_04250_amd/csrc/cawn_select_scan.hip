@@ -14,18 +14,21 @@
 namespace cawn {
 namespace select {
 
-// bc[b][tile][g][n][which][token of the tile]; zeros where there is no token or state
+// bc[b][tile][g][n][which][token of the tile]; zeros where there is no token or state.  A workgroup takes a tile of a group, read along the states and
+// written along the tokens.
 template <typename T> __global__ __launch_bounds__(256) void select_prepare(const Args a)
 {
-    const int npt = a.NP * a.NB;
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
-    const int per = npt * 2 * TILE, i = (int)(id % per), tt = i % TILE, which = i / TILE % 2, n = i / (2 * TILE);
-    const long long rest = id / per, g = rest % a.G, bt = rest / a.G, b = bt / a.tiles;
-    if (b >= a.B) return;
-    const long long t = (bt - b * a.tiles) * TILE + tt;
-    float v = 0.f;
-    if (n < a.N && t < row_length(a, (int)b)) v = (float)((const T *)(which ? a.Cm : a.Bm))[b * a.bsb + t * a.bst + g * a.N + n];
-    a.bc[id] = v;
+    __shared__ float sh[2][TILE][N_MAX + 1];
+    const int npt = a.NP * a.NB, g = blockIdx.x % a.G;
+    const long long bt = blockIdx.x / a.G, b = bt / a.tiles, t = (bt - b * a.tiles) * TILE;
+    const int left = row_length(a, (int)b) - (int)t;
+    for (int i = threadIdx.x; i < 2 * TILE * npt; i += 256) {
+        const int n = i % npt, tt = i / npt % TILE, which = i / npt / TILE;
+        sh[which][tt][n] = n < a.N && tt < left ? (float)((const T *)(which ? a.Cm : a.Bm))[b * a.bsb + (t + tt) * a.bst + (long long)g * a.N + n] : 0.f;
+    }
+    __syncthreads();
+    float *out = a.bc + (long long)blockIdx.x * npt * 2 * TILE;
+    for (int i = threadIdx.x; i < 2 * TILE * npt; i += 256) out[i] = sh[i / TILE % 2][i % TILE][i / TILE / 2];
 }
 
 // NB waves share a channel's states.  RUN tokens at a time, the next ones' streams on their way meanwhile.
@@ -170,42 +173,69 @@ template <typename T, int NP, int NB, bool SUMMARY> __global__ __launch_bounds__
 }
 
 // The chain over the segments.  Forward: their states at the begin; backward: what reaches their end, from the last that a row has to the first.
-template <bool REV> __global__ __launch_bounds__(256) void select_join(const Args a)
+// The links are cut into RUNS runs of up to LINKS, which are joined first: no link's loads wait for another link.
+template <bool REV, int RUNS, int LINKS> __global__ __launch_bounds__(256) void select_join(const Args a)
 {
-    const int NPT = a.NP * a.NB;
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x, per = (long long)a.Dp * NPT, b = id / per;
-    if (b >= a.B) return;
-    const long long i = id - b * per, pad = i / NPT;
-    const int s = (int)(i - pad * NPT), g = (int)(pad / 64 / a.cpg), in = (int)(pad - (long long)g * a.cpg * 64), ch = g * a.cg + in;
+    constexpr int WIDE = 256 / RUNS;            // states side by side
+    __shared__ float2 sh[RUNS][WIDE];
+    const int NPT = a.NP * a.NB, e = threadIdx.x % WIDE, run = threadIdx.x / WIDE;
+    const long long per = (long long)a.Dp * NPT, groups = per / WIDE, b = blockIdx.x / groups, i = (blockIdx.x - b * groups) * WIDE + e, pad = i / NPT;
+    const int s = (int)(i - pad * NPT), g = (int)(pad / 64 / a.cpg), in = (int)(pad - (long long)g * a.cpg * 64);
     const bool on = in < a.cg && s < a.N;
+    const long long ch = (long long)g * a.cg + in;
+    const int seg_tokens = a.seg_tiles * TILE, live = (__builtin_amdgcn_readfirstlane(row_length(a, (int)b)) + seg_tokens - 1) / seg_tokens;
+    // link k leads from the k-th segment to the next
+    const int links = live > 0 ? live - 1 : 0, first = run * LINKS;
+    const long long seg0 = b * a.segments + (REV ? (live > 0 ? live - 1 : 0) : 0), to = REV ? -1 : 1;
+    float gs[LINKS], bs[LINKS];
+#pragma unroll
+    for (int j = 0; j < LINKS; ++j) {           // (behind the last, the last again: a load behind a branch would be waited for by itself)
+        const long long seg = seg0 + to * max(min(first + j, links - 1), 0);
+        gs[j] = a.seg_g[seg * a.Dp + pad], bs[j] = a.seg_b[seg * per + i];
+    }
+    const float A = on ? rate(a.A[ch * a.N + s]) : 0.f;
     const float *begin = REV ? a.dstate_out : a.state_in;
     float S = on && begin ? begin[(b * a.D + ch) * a.N + s] : 0.f;
-    const float A = on ? rate(a.A[(long long)ch * a.N + s]) : 0.f;
-    const int seg_tokens = a.seg_tiles * TILE, live = (row_length(a, (int)b) + seg_tokens - 1) / seg_tokens;
-    const long long seg0 = b * a.segments + (REV ? live - 1 : 0), to = REV ? -1 : 1;
-    if (live == 0) a.seg_s[b * a.segments * per + i] = S;
-    constexpr int LINKS = 8;            // asked for at once: none of their loads waits for another
-    for (int k = 0; k < live; k += LINKS) {
-        float gs[LINKS], bs[LINKS];
+    float product = 1.f, from_zero = 0.f;
 #pragma unroll
-        for (int j = 0; j < LINKS; ++j) {
-            const long long seg = seg0 + to * min(k + j, max(live - 2, 0));
-            gs[j] = a.seg_g[seg * a.Dp + pad], bs[j] = a.seg_b[seg * per + i];
-        }
-#pragma unroll
-        for (int j = 0; j < LINKS; ++j) {
-            if (k + j >= live) break;
-            a.seg_s[(seg0 + to * (k + j)) * per + i] = S;
-            S = fmaf(factor(gs[j], A), S, bs[j]);       // (behind the last, of no use)
-        }
+    for (int j = 0; j < LINKS; ++j) {
+        const bool link = first + j < links;
+        gs[j] = factor(link ? gs[j] : 0.f, A), bs[j] = link ? bs[j] : 0.f;          // (no link: 1 and 0)
+        from_zero = fmaf(gs[j], from_zero, bs[j]);
+        product *= gs[j];
     }
+    if (RUNS > 1) {
+        sh[run][e] = make_float2(product, from_zero);
+        __syncthreads();
+        for (int r = 0; r < run; ++r) S = fmaf(sh[r][e].x, S, sh[r][e].y);
+    }
+    if (run == 0) a.seg_s[seg0 * per + i] = S;
+#pragma unroll
+    for (int j = 0; j < LINKS; ++j) {           // a link writes the segment behind it
+        S = fmaf(gs[j], S, bs[j]);
+        if (first + j < links) a.seg_s[(seg0 + to * (first + j + 1)) * per + i] = S;
+    }
+}
+
+template <bool REV, int RUNS, int LINKS> static void go_join(const Args &a, hipStream_t s)
+{
+    hipLaunchKernelGGL((select_join<REV, RUNS, LINKS>), dim3((unsigned)((long long)a.B * a.Dp * a.NP * a.NB * RUNS / 256)), dim3(256), 0, s, a);
+}
+
+template <bool REV> static void join(const Args &a, hipStream_t s)
+{
+    const int links = a.segments - 1;
+    if (links <= 4) go_join<REV, 1, 4>(a, s);
+    else if (links <= 16) go_join<REV, 4, 4>(a, s);
+    else if (links <= 32) go_join<REV, 4, 8>(a, s);
+    else if (links <= 64) go_join<REV, 4, 16>(a, s);
+    else if (links <= 128) go_join<REV, 16, 8>(a, s);
+    else go_join<REV, 16, 16>(a, s);
 }
 
 int launch_join(const Args &a, bool reverse, hipStream_t s)
 {
-    const dim3 grid((unsigned)ceil_div((long long)a.B * a.Dp * a.NP * a.NB, 256));
-    if (reverse) hipLaunchKernelGGL(select_join<true>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(select_join<false>, grid, dim3(256), 0, s, a);
+    reverse ? join<true>(a, s) : join<false>(a, s);
     return launched();
 }
 
@@ -221,7 +251,7 @@ template <typename T, int NP, int NB> static void launch_np(const Args &a, hipSt
 
 template <typename T> static int launch(const Args &a, hipStream_t s)
 {
-    if (a.tiles > 0) hipLaunchKernelGGL((select_prepare<T>), dim3((unsigned)ceil_div((long long)a.B * a.tiles * a.G * a.NP * a.NB * 2 * TILE, 256)), dim3(256), 0, s, a);
+    if (a.tiles > 0) hipLaunchKernelGGL((select_prepare<T>), dim3((unsigned)((long long)a.B * a.tiles * a.G)), dim3(256), 0, s, a);
     if (a.NB == 8) launch_np<T, 16, 8>(a, s);
     else if (a.NB == 4) launch_np<T, 16, 4>(a, s);
     else if (a.NB == 2) launch_np<T, 16, 2>(a, s);
