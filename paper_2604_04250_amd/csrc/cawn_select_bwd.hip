@@ -32,13 +32,17 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
     const T *dp = (const T *)a.dt + p.b * a.dsb + p.base, *dyp = (const T *)a.dy + p.b * a.ysb + p.base, *zp = a.z ? (const T *)a.z + p.b * a.zsb + p.base : nullptr;
     const uint32_t at = p.bytes<T>();
     auto step = [](long long stride) { return (uint32_t)stride * (uint32_t)sizeof(T); };
-    T dr[TILE], yr[TILE], zr[TILE];
+    uint32_t dr[TILE], yr[TILE], zr[TILE];
     auto fetch = [&](int t) {
-        if (t < t0) return;
+        if (t < t0) {
+            no_run<TILE>(dr), no_run<TILE>(yr), no_run<TILE>(zr);
+            return;
+        }
         const int left = t1 - t;
         load_run<T, TILE>(dp + t * a.dst, step(a.dst), left, at, dr);
         load_run<T, TILE>(dyp + t * a.yst, step(a.yst), left, at, yr);
         if (zp) load_run<T, TILE>(zp + t * a.zst, step(a.zst), left, at, zr);
+        else no_run<TILE>(zr);
     };
     const int last = (t1 - 1) / TILE * TILE;
     fetch(last);
@@ -56,8 +60,8 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
         float delta[TILE], g[TILE];
 #pragma unroll
         for (int i = 0; i < TILE; ++i) {
-            delta[i] = (float)dr[i] + bias;
-            g[i] = (float)yr[i];
+            delta[i] = value<T>(dr[i]) + bias;
+            g[i] = value<T>(yr[i]);
         }
         if (a.softplus) {
 #pragma unroll
@@ -66,7 +70,7 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
         if (zp) {
 #pragma unroll
             for (int i = 0; i < TILE; ++i) {
-                const float z = (float)zr[i];
+                const float z = value<T>(zr[i]);
                 g[i] *= z * sigmoid_f(z);
             }
         }
@@ -170,12 +174,16 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
     auto step = [](long long stride) { return (uint32_t)stride * (uint32_t)sizeof(T); };
     T xr[TILE], xn[TILE], dr[TILE], yr[TILE], zr[TILE];
     auto fetch = [&](int t) {
-        if (t < t0) return;
+        if (t < t0) {
+            no_run<TILE>(dr), no_run<TILE>(xn), no_run<TILE>(yr), no_run<TILE>(zr);
+            return;
+        }
         const int left = t1 - t;
         load_run<T, TILE>(dp + t * a.dst, step(a.dst), left, at, dr);
         load_run<T, TILE>(xp + t * a.xst, step(a.xst), left, at, xn);
         load_run<T, TILE>(dyp + t * a.yst, step(a.yst), left, at, yr);
         if (zp) load_run<T, TILE>(zp + t * a.zst, step(a.zst), left, at, zr);
+        else no_run<TILE>(zr);
     };
     const int last = t1 > t0 ? (t1 - 1) / TILE * TILE : t0 - 1;
     fetch(last);
@@ -196,17 +204,10 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
             h[j] = mine[s][0][p.lane], dA[j] = mine[s][1][p.lane], A[j] = mine[s][2][p.lane];
         };
         ask(0, 0);
+        // (one stream after the other, so that what has been read makes room for what comes of it)
         float delta[TILE], slope[TILE], u[TILE], g[TILE], q[TILE], du[TILE], dd[TILE], y[TILE];
 #pragma unroll
-        for (int i = 0; i < TILE; ++i) {
-            xr[i] = xn[i];
-            const float x = (float)xr[i];
-            delta[i] = (float)dr[i] + bias;
-            g[i] = (float)yr[i];
-            slope[i] = 1.f, q[i] = 0.f, u[i] = x;
-            y[i] = first * x;
-            du[i] = dd[i] = 0.f;
-        }
+        for (int i = 0; i < TILE; ++i) delta[i] = (float)dr[i] + bias, slope[i] = 1.f;
         if (a.softplus) {
 #pragma unroll
             for (int i = 0; i < TILE; ++i) {
@@ -214,6 +215,9 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
                 delta[i] = softplus_f(delta[i]);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < TILE; ++i) g[i] = (float)yr[i], q[i] = 0.f;
         if (zp) {
 #pragma unroll
             for (int i = 0; i < TILE; ++i) {
@@ -223,8 +227,14 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
                 g[i] *= silu;
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < TILE; ++i) u[i] *= delta[i];
+        for (int i = 0; i < TILE; ++i) {
+            if (!MULTI) xr[i] = xn[i];
+            const float x = (float)xn[i];
+            u[i] = delta[i] * x;
+            y[i] = first * x;
+        }
         if (left < TILE) {          // behind the last token nothing is added anywhere
 #pragma unroll
             for (int i = 0; i < TILE; ++i) {
@@ -240,8 +250,13 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
                 g[i] = p.on ? g[i] : 0.f;
             }
         }
-        stay<TILE>(slope);
-        stay<TILE>(q);
+        if (!MULTI) {
+            stay<TILE>(slope);
+            stay<TILE>(q);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < TILE; ++i) du[i] = dd[i] = 0.f;
 #pragma unroll 1
         for (int s = 0; s < NP; s += 2) {
             LaneSums sums;
@@ -295,49 +310,62 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
             }
             buf ^= 1;
         }
-        if (MULTI) {        // the waves' shares of du, dd and y; wave i % NB goes on with token i
-            auto exchange = [&](float(&v)[TILE]) {
-#pragma unroll
-                for (int i = 0; i < TILE; ++i) xch[MULTI ? p.blk : 0][i][p.lane] = v[i];
-                __syncthreads();
-#pragma unroll
-                for (int i = 0; i < TILE; ++i) {
-                    if (i % NB != p.blk) continue;
-                    v[i] = 0.f;
-#pragma unroll
-                    for (int k = 0; k < NB; ++k) v[i] += xch[MULTI ? k : 0][i][p.lane];
-                }
-                __syncthreads();
-            };
-            exchange(du);
-            exchange(dd);
-            if (dzp) exchange(y);
-        }
         // (dd becomes the gradient of dt, du that of x, y that of z)
+        auto finish = [&](bool there, float x, float delta, float slope, float g, float q, float &du, float &dd, float &y) {
+            dd = there ? fmaf(du, x, dd * LN2) * slope : 0.f;
+            du = fmaf(du, delta, Dk * g);
+            y *= q;
+            sumD = fmaf(g, there ? x : 0.f, sumD);
+            sumb += dd;
+        };
+        if constexpr (!MULTI) {
 #pragma unroll
-        for (int i = 0; i < TILE; ++i) {
-            if (MULTI && i % NB != p.blk) continue;
-            const float x = (float)xr[i];
-            dd[i] = i < left ? fmaf(du[i], x, dd[i] * LN2) * slope[i] : 0.f;
-            du[i] = fmaf(du[i], delta[i], Dk * g[i]);
-            y[i] *= q[i];
-            sumD = fmaf(g[i], i < left ? x : 0.f, sumD);
-            sumb += dd[i];
-        }
-        if (p.on) {
-            auto out = [&](T *row, long long stride, const float(&v)[TILE]) {
-                if (!row) return;
-                row += t * stride;
-                if (!MULTI) store_run<T, TILE>(row, step(stride), left, at, [&](int i) { return v[i]; });
-                else {
+            for (int i = 0; i < TILE; ++i) finish(i < left, (float)xr[i], delta[i], slope[i], g[i], q[i], du[i], dd[i], y[i]);
+            if (p.on) {
+                if (dxp) store_run<T, TILE>(dxp + t * a.xst, step(a.xst), left, at, [&](int i) { return du[i]; });
+                if (ddp) store_run<T, TILE>(ddp + t * a.dst, step(a.dst), left, at, [&](int i) { return dd[i]; });
+                if (dzp) store_run<T, TILE>(dzp + t * a.zst, step(a.zst), left, at, [&](int i) { return y[i]; });
+            }
+        } else {
+            // the waves' shares of du, dd and y are added up; wave i % NB goes on with token i, whose streams it reads again
+            constexpr int OWN = TILE / NB;
+            float duo[OWN], ddo[OWN], yo[OWN];
+            auto exchange = [&](const float(&v)[TILE], float(&own)[OWN]) {
 #pragma unroll
-                    for (int i = 0; i < TILE; ++i)
-                        if (i < left && i % NB == p.blk) store_at<T>(rows_at(row + i * stride), at, 0, v[i]);
+                for (int i = 0; i < TILE; ++i) xch[p.blk][i][p.lane] = v[i];
+                __syncthreads();
+#pragma unroll
+                for (int k = 0; k < OWN; ++k) {
+                    own[k] = 0.f;
+#pragma unroll
+                    for (int m = 0; m < NB; ++m) own[k] += xch[m][k * NB + p.blk][p.lane];
                 }
+                __syncthreads();
             };
-            out(dxp, a.xst, du);
-            out(ddp, a.dst, dd);
-            out(dzp, a.zst, y);
+            exchange(du, duo);
+            exchange(dd, ddo);
+            exchange(y, yo);
+            const auto xs = rows_at(xp + t * a.xst), ds = rows_at(dp + t * a.dst), ys = rows_at(dyp + t * a.yst), zs = rows_at(zp ? zp + t * a.zst : nullptr);
+            float x[OWN], d[OWN], g1[OWN], z[OWN];
+#pragma unroll
+            for (int k = 0; k < OWN; ++k) {
+                const uint32_t i = min(k * NB + p.blk, left - 1);
+                x[k] = value<T>(load_at<T>(xs, at, i * step(a.xst))), d[k] = value<T>(load_at<T>(ds, at, i * step(a.dst)));
+                g1[k] = value<T>(load_at<T>(ys, at, i * step(a.yst))), z[k] = zp ? value<T>(load_at<T>(zs, at, i * step(a.zst))) : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < OWN; ++k) {
+                const int i = k * NB + p.blk;
+                const bool there = i < left && p.on;
+                const float v = d[k] + bias;
+                float silu = 1.f, q1 = 0.f;
+                if (zp) q1 = g1[k] * dsilu(z[k], silu);
+                finish(there, x[k], a.softplus ? softplus_f(v) : v, a.softplus ? sigmoid_f(v) : 1.f, there ? g1[k] * silu : 0.f, q1, duo[k], ddo[k], yo[k]);
+                if (!there) continue;
+                if (dxp) store_at<T>(rows_at(dxp + (t + i) * a.xst), at, 0, duo[k]);
+                if (ddp) store_at<T>(rows_at(ddp + (t + i) * a.dst), at, 0, ddo[k]);
+                if (dzp) store_at<T>(rows_at(dzp + (t + i) * a.zst), at, 0, yo[k]);
+            }
         }
     }
     if (p.on && p.blk == 0) {

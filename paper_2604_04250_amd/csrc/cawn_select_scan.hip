@@ -48,14 +48,14 @@ template <typename T, int NP, int NB, bool SUMMARY> __global__ __launch_bounds__
     const T *zp = !SUMMARY && a.z ? (const T *)a.z + p.b * a.zsb + p.base + t0 * a.zst : nullptr;
     const uint32_t at = p.bytes<T>();
     auto step = [](long long stride) { return (uint32_t)stride * (uint32_t)sizeof(T); };
-    T xr[RUN], dr[RUN], zr[SUMMARY ? 1 : RUN];
+    uint32_t xr[RUN], dr[RUN], zr[SUMMARY ? 1 : RUN];
     auto fetch = [&](int t) {
         const int left = t1 - t;
         if (left > 0) {
             load_run<T, RUN>(dp, step(a.dst), left, at, dr);
             load_run<T, RUN>(xp, step(a.xst), left, at, xr);
             dp += RUN * a.dst, xp += RUN * a.xst;
-        }
+        } else no_run<RUN>(dr), no_run<RUN>(xr);
     };
     fetch(t0);
     float A[NP], S[NP], total = 0.f;
@@ -83,7 +83,7 @@ template <typename T, int NP, int NB, bool SUMMARY> __global__ __launch_bounds__
         float delta[RUN], u[RUN], y[SUMMARY ? 1 : RUN];
 #pragma unroll
         for (int i = 0; i < RUN; ++i) {
-            delta[i] = (float)dr[i] + bias, u[i] = (float)xr[i];
+            delta[i] = value<T>(dr[i]) + bias, u[i] = value<T>(xr[i]);
             if constexpr (!SUMMARY) y[i] = Dk * u[i];
         }
         if (a.softplus) {
@@ -106,7 +106,7 @@ template <typename T, int NP, int NB, bool SUMMARY> __global__ __launch_bounds__
             if (zp) {
                 load_run<T, RUN>(zp, step(a.zst), left, at, zr);
                 zp += RUN * a.zst;
-            }
+            } else no_run<RUN>(zr);
         }
         fetch(t + RUN);
         // (B and C of the state after next are asked for behind the first token of this one, whose wait would be for them too; without the fences the
@@ -146,7 +146,7 @@ template <typename T, int NP, int NB, bool SUMMARY> __global__ __launch_bounds__
             if (zp) {
 #pragma unroll
                 for (int i = 0; i < RUN; ++i) {
-                    const float z = (float)zr[i];
+                    const float z = value<T>(zr[i]);
                     y[i] *= z * sigmoid_f(z);
                 }
             }
