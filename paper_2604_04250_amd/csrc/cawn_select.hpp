@@ -15,6 +15,7 @@ namespace select {
 using namespace cawn::ops;
 
 constexpr int TILE = 16;            // tokens treated at once; the states before each tile are kept for a backward
+constexpr int RUN = 8;              // tokens of which the passes without gradients keep what they have read
 constexpr int TOKEN_MAX = 16;       // longest call that goes token by token
 constexpr int N_MAX = 128;
 constexpr int SEGMENTS_MAX = 256;   // of a row
@@ -43,9 +44,9 @@ struct Args {
     // states [b][..][Dp][NPT]: before each tile (or null); of a segment from zero, its sum of delta [b][segment][Dp], and at its begin (backward:
     // what reaches its end)
     float *ck, *seg_b, *seg_g, *seg_s;
-    // backward: sums over the channels of a workgroup [b][tile][16][g][parts][2][NPT], over a segment's tokens [b][segment][Dp][NPT] and, of
-    // D's and the bias's gradients, [b][segment][wave of a channel][2][Dp]
-    float *part_bc, *part_a, *part_d;
+    // backward: sums over the channels of a workgroup [b][tile][16][g][parts][2][NPT], and over a segment's tokens of the parameters' gradients
+    // [b][segment], a row of Dp NPT for A, Dp for D, Dp for the bias
+    float *part_bc, *part_a;
     int parts;
 };
 

@@ -1,11 +1,5 @@
 // Selective state space scan: argument checks, sizes and the choice of a form.
 #include "cawn_select.hpp"
-#ifndef CAWN_WF
-#define CAWN_WF 8192
-#endif
-#ifndef CAWN_WB
-#define CAWN_WB 6144
-#endif
 
 using namespace cawn;
 using namespace cawn::ops;
@@ -14,14 +8,20 @@ using cawn::select::TILE;
 
 namespace {
 
-// How a row's tiles are cut into segments: until the chip has `waves` of them.
+// How a row's tiles are cut into segments.  Each but the last costs its tokens twice, whatever their number, and one link of the chain; more of them fill the
+// chip and even out its rounds.  `waves` in all, three or four rounds of what the chip holds; beyond 64 segments, where the chain costs more than the rounds gain,
+// half of that.
+// (us a pass for 4,096, 6,144, 8,192 and 16,384 waves, forward: 2 x 32,768 tokens of 4,096 channels 1,790, 1,720, 1,660, 1,637, training 8 x 8,192 of 768
+// channels 1,326, 1,290, 1,296, 1,292; backward, 2,048, 4,096, 6,144, 8,192 and 12,288: the latter 1,326, 1,306, 1,241, 1,287, 1,251.)
 void cut(Args *a, long long waves)
 {
     const long long columns = (long long)a->B * a->G * a->cbg * (a->NB > 1 ? a->NB : a->wide);
-    const long long want = columns > 0 ? waves / columns : 1;
+    long long want = columns > 0 ? waves / columns : 1;
+    if (want > 64) want = waves / 2 / columns > 64 ? waves / 2 / columns : 64;
+    if (want > select::SEGMENTS_MAX) want = select::SEGMENTS_MAX;
     a->segments = 1, a->seg_tiles = a->tiles > 0 ? a->tiles : 1;
     if (want < 2 || a->tiles < 2) return;
-    a->seg_tiles = (int)ceil_div(a->tiles, want < select::SEGMENTS_MAX ? want : select::SEGMENTS_MAX);
+    a->seg_tiles = (int)ceil_div(a->tiles, want);
     a->segments = (int)ceil_div(a->tiles, a->seg_tiles);
 }
 
@@ -59,13 +59,13 @@ int check(const cawn_scan_desc *d, bool bwd, Args *a)
     if (d->D > wide || a->xst > wide || a->dst > wide || a->zst > wide || a->yst > wide) return CAWN_EUNSUPPORTED;
     a->Dp = a->cpg * G * 64;
     a->tiles = (int)ceil_div(d->L, TILE);
-    cut(a, bwd ? CAWN_WB : CAWN_WF);
+    cut(a, bwd ? 6144 : 8192);
     return too_many(*a) ? CAWN_EUNSUPPORTED : CAWN_OK;
 }
 
 // Byte offsets.  Kept for the backward: B and C, states before each tile.  Scratch: forward B and C (unless kept), of segments their b, sum of delta and
 // begin; backward the same of its own segments, and the partial sums.
-struct Layout { size_t ck, ckpt; size_t b, g, s, fwd; size_t pbc, pa, pd, bwd; };
+struct Layout { size_t ck, ckpt; size_t b, g, s, fwd; size_t pbc, pa, bwd; };
 Layout layout_of(const Args &f, const Args &r)
 {
     const size_t npt = f.NP * f.NB, state = (size_t)f.Dp * npt * 4;
@@ -85,8 +85,7 @@ Layout layout_of(const Args &f, const Args &r)
     size_t b = 0, g, s;
     l.pbc = parts(rs, &b, &g, &s);
     l.pa = l.pbc + up((size_t)r.B * r.tiles * TILE * r.G * r.parts * 2 * npt * 4);
-    l.pd = l.pa + up((size_t)r.B * r.segments * state);
-    l.bwd = l.pd + (size_t)r.B * r.segments * r.NB * 2 * r.Dp * 4;
+    l.bwd = l.pa + (size_t)r.B * r.segments * r.Dp * (npt + 2) * 4;
     return l;
 }
 
@@ -96,25 +95,20 @@ void segments_of(Args *a, char *ws, size_t begin)
     a->seg_b = (float *)(ws + begin), a->seg_s = (float *)(ws + begin + n * state), a->seg_g = (float *)(ws + begin + 2 * n * state);
 }
 
-struct RateSums {       // column (channel in its padded place, state) -> A's
-    float *out;
-    int N, NPT, cpg, cg;
+struct ParamSums {      // column of a row of part_a -> its place in the gradients of A, D and the bias
+    float *dA, *dD, *db;
+    int N, NPT, Dp, cpg, cg;
     __device__ float *operator()(long long c) const
     {
-        const long long pad = c / NPT, g = pad / 64 / cpg, in = pad - g * cpg * 64;
-        const int n = (int)(c - pad * NPT);
-        return n < N && in < cg ? out + (g * cg + in) * N + n : nullptr;
-    }
-};
-
-struct ChannelSums {    // column (0: D, 1: bias; channel in its padded place)
-    float *dD, *db;
-    int Dp, cpg, cg;
-    __device__ float *operator()(long long c) const
-    {
-        float *out = c < Dp ? dD : db;
-        const long long pad = c < Dp ? c : c - Dp, g = pad / 64 / cpg, in = pad - g * cpg * 64;
-        return out && in < cg ? out + g * cg + in : nullptr;
+        const long long wide = (long long)Dp * NPT;
+        const long long pad = c < wide ? c / NPT : (c - wide) % Dp, g = pad / 64 / cpg, in = pad - g * cpg * 64;
+        if (in >= cg) return nullptr;
+        if (c < wide) {
+            const int n = (int)(c - pad * NPT);
+            return dA && n < N ? dA + (g * cg + in) * N + n : nullptr;
+        }
+        float *out = c - wide < Dp ? dD : db;
+        return out ? out + g * cg + in : nullptr;
     }
 };
 
@@ -179,13 +173,11 @@ int cawn_selective_scan_bwd(const cawn_scan_desc *d, const void *x, const void *
         !aligned_to(ckpt, 16) || !aligned_to(dstate_out, 4) || !aligned_to(dA, 4) || !aligned_to(dDskip, 4) || !aligned_to(ddt_bias, 4) || !aligned_to(dstate_in, 4))
         return CAWN_EINVAL;
     hipStream_t s = (hipStream_t)stream;
-    const select::Args &c = a;
-    const int NPT = c.NP * c.NB, add = d->accumulate_param_grads;
-    const RateSums rates{dA, c.N, NPT, c.cpg, c.cg};
-    const ChannelSums channels{dDskip, ddt_bias, c.Dp, c.cpg, c.cg};
+    const int NPT = a.NP * a.NB, add = d->accumulate_param_grads;
+    const bool params = dA || dDskip || ddt_bias;
+    const ParamSums sums{dA, dDskip, ddt_bias, a.N, NPT, a.Dp, a.cpg, a.cg};
     if (a.B == 0) {         // the sums over nothing
-        if (dA && !add) launch_sums(nullptr, 0, (long long)c.Dp * NPT, rates, 0, s);
-        if ((dDskip || ddt_bias) && !add) launch_sums(nullptr, 0, 2LL * c.Dp, channels, 0, s);
+        if (params && !add) launch_sums(nullptr, 0, (long long)a.Dp * (NPT + 2), sums, 0, s);
         return launched();
     }
     if (!A || (a.L > 0 && (!x || !dt || !Bm || !Cm || !ckpt || !dy))) return CAWN_EINVAL;
@@ -199,15 +191,12 @@ int cawn_selective_scan_bwd(const cawn_scan_desc *d, const void *x, const void *
     char *ws = (char *)workspace;
     segments_of(&a, ws, 0);
     a.part_bc = dBm || dCm ? (float *)(ws + l.pbc) : nullptr;
-    a.part_a = dA ? (float *)(ws + l.pa) : nullptr;
-    a.part_d = dDskip || ddt_bias ? (float *)(ws + l.pd) : nullptr;
+    a.part_a = params ? (float *)(ws + l.pa) : nullptr;
     if (int r = select::launch_backward(a, d->bf16, s)) return r;
     if (a.part_bc) {
         if (int r = select::launch_bc_sums(a, d->bf16, s)) return r;
     }
-    const long long rows = (long long)a.B * a.segments;
-    if (dA) launch_sums(a.part_a, rows, (long long)a.Dp * NPT, rates, add, s);
-    if (a.part_d) launch_sums(a.part_d, rows * a.NB, 2LL * a.Dp, channels, add, s);
+    if (params) launch_sums(a.part_a, (long long)a.B * a.segments, (long long)a.Dp * (NPT + 2), sums, add, s);
     return launched();
 }
 

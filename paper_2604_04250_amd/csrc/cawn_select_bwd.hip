@@ -32,66 +32,66 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
     const T *dp = (const T *)a.dt + p.b * a.dsb + p.base, *dyp = (const T *)a.dy + p.b * a.ysb + p.base, *zp = a.z ? (const T *)a.z + p.b * a.zsb + p.base : nullptr;
     const uint32_t at = p.bytes<T>();
     auto step = [](long long stride) { return (uint32_t)stride * (uint32_t)sizeof(T); };
-    uint32_t dr[TILE], yr[TILE], zr[TILE];
+    uint32_t dr[RUN], yr[RUN], zr[RUN];
     auto fetch = [&](int t) {
         if (t < t0) {
-            no_run<TILE>(dr), no_run<TILE>(yr), no_run<TILE>(zr);
+            no_run<RUN>(dr), no_run<RUN>(yr), no_run<RUN>(zr);
             return;
         }
         const int left = t1 - t;
-        load_run<T, TILE>(dp + t * a.dst, step(a.dst), left, at, dr);
-        load_run<T, TILE>(dyp + t * a.yst, step(a.yst), left, at, yr);
-        if (zp) load_run<T, TILE>(zp + t * a.zst, step(a.zst), left, at, zr);
-        else no_run<TILE>(zr);
+        load_run<T, RUN>(dp + t * a.dst, step(a.dst), left, at, dr);
+        load_run<T, RUN>(dyp + t * a.yst, step(a.yst), left, at, yr);
+        if (zp) load_run<T, RUN>(zp + t * a.zst, step(a.zst), left, at, zr);
+        else no_run<RUN>(zr);
     };
-    const int last = (t1 - 1) / TILE * TILE;
+    const int last = (t1 - 1) / RUN * RUN;
     fetch(last);
     float A[NP], h[NP], total = 0.f;
     load_rates<NP>(a, p, A);
 #pragma unroll
     for (int i = 0; i < NP; ++i) h[i] = 0.f;
     const float bias = a.bias ? a.bias[p.ch] : 0.f;
-    for (int t = last; t >= t0; t -= TILE) {
+    for (int t = last; t >= t0; t -= RUN) {
         const int left = t1 - t;
-        const float *tile = a.bc + (((long long)p.b * a.tiles + t / TILE) * a.G + p.g) * NPT * 2 * TILE + p.blk * NP * 2 * TILE;
-        Scalars<TILE> Cq[NP];
+        const float *tile = a.bc + (((long long)p.b * a.tiles + t / TILE) * a.G + p.g) * NPT * 2 * TILE + p.blk * NP * 2 * TILE + t % TILE;
+        Scalars<RUN> Cq[NP];
 #pragma unroll
-        for (int s = 0; s < AHEAD; ++s) Cq[s] = bc_run<TILE>(tile, s, 1);
-        float delta[TILE], g[TILE];
+        for (int s = 0; s < AHEAD; ++s) Cq[s] = bc_run<RUN>(tile, s, 1);
+        float delta[RUN], g[RUN];
 #pragma unroll
-        for (int i = 0; i < TILE; ++i) {
+        for (int i = 0; i < RUN; ++i) {
             delta[i] = value<T>(dr[i]) + bias;
             g[i] = value<T>(yr[i]);
         }
         if (a.softplus) {
 #pragma unroll
-            for (int i = 0; i < TILE; ++i) delta[i] = softplus_f(delta[i]);
+            for (int i = 0; i < RUN; ++i) delta[i] = softplus_f(delta[i]);
         }
         if (zp) {
 #pragma unroll
-            for (int i = 0; i < TILE; ++i) {
+            for (int i = 0; i < RUN; ++i) {
                 const float z = value<T>(zr[i]);
                 g[i] *= z * sigmoid_f(z);
             }
         }
-        if (left < TILE) {
+        if (left < RUN) {
 #pragma unroll
-            for (int i = 0; i < TILE; ++i) {
+            for (int i = 0; i < RUN; ++i) {
                 delta[i] = i < left ? delta[i] : 0.f;
                 g[i] = i < left ? g[i] : 0.f;
             }
         }
 #pragma unroll
-        for (int i = 0; i < TILE; ++i) total += delta[i];
-        fetch(t - TILE);
+        for (int i = 0; i < RUN; ++i) total += delta[i];
+        fetch(t - RUN);
 #pragma unroll
         for (int s = 0; s < NP; ++s) {
 #pragma unroll
-            for (int i = TILE - 1; i >= 0; --i) {
+            for (int i = RUN - 1; i >= 0; --i) {
                 h[s] = factor(delta[i], A[s]) * fmaf(Cq[s][i], g[i], h[s]);
-                if (i == TILE - 1 && s + AHEAD < NP) {      // (as in the forward)
+                if (i == RUN - 1 && s + AHEAD < NP) {      // (as in the forward)
                     __builtin_amdgcn_sched_barrier(0);
-                    Cq[s + AHEAD < NP ? s + AHEAD : 0] = bc_run<TILE>(tile, s + AHEAD, 1);
+                    Cq[s + AHEAD < NP ? s + AHEAD : 0] = bc_run<RUN>(tile, s + AHEAD, 1);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -379,35 +379,53 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
     float h[NP], dA[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) h[i] = mine[i][0][p.lane], dA[i] = mine[i][1][p.lane];
-    if (a.part_a) store_states<NP>(a.part_a + (seg * a.Dp + p.pad) * NPT + p.blk * NP, dA);
-    if (a.part_d) {
-        float *out = a.part_d + ((seg * NB + p.blk) * 2) * a.Dp + p.pad;
-        out[0] = sumD, out[a.Dp] = sumb;
+    if (a.part_a) {         // a row: [Dp][NPT] of A, [Dp] of D, [Dp] of the bias
+        float *out = a.part_a + seg * a.Dp * (NPT + 2);
+        store_states<NP>(out + p.pad * NPT + p.blk * NP, dA);
+        if (MULTI) {        // (the waves' tokens)
+            xch[MULTI ? p.blk : 0][0][p.lane] = sumD, xch[MULTI ? p.blk : 0][1][p.lane] = sumb;
+            __syncthreads();
+            sumD = sumb = 0.f;
+#pragma unroll
+            for (int m = 0; m < NB; ++m) sumD += xch[MULTI ? m : 0][0][p.lane], sumb += xch[MULTI ? m : 0][1][p.lane];
+        }
+        if (p.blk == 0) {
+            out += (long long)a.Dp * NPT + p.pad;
+            out[0] = sumD, out[a.Dp] = sumb;
+        }
     }
     if (p.on && a.dstate_in && p.seg == 0) store_user<NP>(a.dstate_in, a, user, p.blk * NP, h);
 }
 
-// dB and dC: the workgroups' sums, in their order.
+// dB and dC: the workgroups' sums, in their order; four states a thread.
 template <typename T> __global__ __launch_bounds__(256) void select_bc_sums(const Args a)
 {
-    const int NPT = a.NP * a.NB;
+    const int NPT = a.NP * a.NB, per = 2 * NPT;
     const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
-    const int per = 2 * NPT, at = (int)(id % per), which = at / NPT, n = at % NPT;
-    const long long rest = id / per, g = rest % a.G, bt = rest / a.G, b = bt / a.L, t = bt - b * a.L;
+    const int at = (int)(id % (per / 4)) * 4, which = at / NPT, n = at % NPT;
+    const long long rest = id / (per / 4), g = rest % a.G, bt = rest / a.G, b = bt / a.L, t = bt - b * a.L;
     if (b >= a.B || n >= a.N) return;
     T *out = (T *)(which ? a.dC : a.dB);
     if (!out) return;
-    float v = 0.f;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
     if (t < row_length(a, (int)b)) {
         const float *p = a.part_bc + (((b * a.tiles * TILE + t) * a.G + g) * a.parts) * per + at;
-        for (int k = 0; k < a.parts; ++k) v += p[(long long)k * per];
+        for (int k = 0; k < a.parts; ++k) v += *reinterpret_cast<const f32x4 *>(p + (long long)k * per);
     }
-    out[b * a.bsb + t * a.bst + g * a.N + n] = (T)v;
+    out += b * a.bsb + t * a.bst + g * a.N + n;
+    if (n + 4 <= a.N && ((uintptr_t)out & (4 * sizeof(T) - 1)) == 0) {
+        const float x[4] = {v[0], v[1], v[2], v[3]};
+        store_n<T, 4>(out, x);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (n + j < a.N) out[j] = (T)v[j];
+    }
 }
 
 int launch_bc_sums(const Args &a, bool bf16_, hipStream_t s)
 {
-    const dim3 grid((unsigned)ceil_div((long long)a.B * a.L * a.G * 2 * a.NP * a.NB, 256));
+    const dim3 grid((unsigned)ceil_div((long long)a.B * a.L * a.G * 2 * a.NP * a.NB / 4, 256));
     if (a.L == 0) return CAWN_OK;
     if (bf16_) hipLaunchKernelGGL(select_bc_sums<bf16>, grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL(select_bc_sums<float>, grid, dim3(256), 0, s, a);

@@ -6,10 +6,6 @@
 // What bounds it: instruction issue.  A token's state costs a product, an exponential (two issue slots), a product and two sums, 24 cycles of a SIMD a
 // wave, and a token 150 more for softplus, the gate, conversions and memory.
 #include "cawn_select.hpp"
-#ifndef CAWN_RUN1
-#define CAWN_RUN1 16
-#define CAWN_RUN2 8
-#endif
 
 namespace cawn {
 namespace select {
@@ -35,7 +31,7 @@ template <typename T> __global__ __launch_bounds__(256) void select_prepare(cons
 template <typename T, int NP, int NB, bool SUMMARY> __global__ __launch_bounds__(NB > 1 ? 64 * NB : 256) void select_scan(const Args a)
 {
     constexpr bool MULTI = NB > 1;
-    constexpr int RUN = SUMMARY ? CAWN_RUN1 : CAWN_RUN2, NPT = NP * NB, AHEAD = 2;
+    constexpr int NPT = NP * NB, AHEAD = 2;
     __shared__ float ys[2][MULTI && !SUMMARY ? NB : 1][RUN][64];        // the waves' shares of y
     const Place p = place_of<MULTI>(a);
     if (!MULTI && !p.there) return;
