@@ -94,6 +94,16 @@ template <int VEC> __device__ inline void write_q(uint8_t *q, const float (&y)[V
     else *reinterpret_cast<uint2 *>(q) = make_uint2(e4m3_4(v[0], v[1], v[2], v[3]), e4m3_4(v[4], v[5], v[6], v[7]));
 }
 
+// VEC weights; they begin on 16 bytes where several values are taken at once
+template <int VEC> __device__ inline void read_w(const RmsArgs &a, int c, float (&w)[VEC])
+{
+    if (a.w) read_n<float, VEC>(a.w + c, w);
+    else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) w[i] = 1.f;
+    }
+}
+
 // VEC values of h, as they are kept
 template <typename X, typename R, int VEC> __device__ inline void read_h(const RmsArgs &a, long long r, int c, float (&h)[VEC])
 {
@@ -129,8 +139,7 @@ template <typename X, typename R, int VEC, int NIT, bool WIDE, int THREADS> __gl
     for (int n = 0; n < NIT; ++n) {
         const int c = (n * step + lane) * VEC;
         in[n] = c < a.C;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) w[n][i] = in[n] && a.w ? a.w[c + i] : 1.f;
+        read_w<VEC>(a, in[n] ? c : 0, w[n]);
     }
     const long long stride = (long long)gridDim.x * a.rpw;
     const float inv = 1.f / (float)a.C;
@@ -283,8 +292,9 @@ template <typename X, typename R, int VEC, int NIT, bool WIDE, int THREADS> __gl
     for (int n = 0; n < NIT; ++n) {
         const int c = (n * step + lane) * VEC;
         in[n] = c < a.C;
+        read_w<VEC>(a, in[n] ? c : 0, w[n]);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) w[n][i] = in[n] && a.w ? a.w[c + i] : 1.f, sw[n][i] = 0.f;
+        for (int i = 0; i < VEC; ++i) sw[n][i] = 0.f;
     }
     const long long stride = (long long)gridDim.x * a.rpw;
     const float inv = 1.f / (float)a.C;
@@ -490,7 +500,8 @@ int cawn_rms_norm_add_fwd(const cawn_rms_desc *d, const void *x, const void *res
     if ((y == nullptr && q == nullptr) || (q == nullptr) != (scales == nullptr)) return CAWN_EINVAL;
     if (d->rows == 0) return CAWN_OK;
     if (!x) return CAWN_EINVAL;
-    if (!aligned_to(x, 16) || !aligned_to(y, 16) || !aligned_to(residual, 16) || !aligned_to(h, 16) || !aligned_to(q, 8)) plan_of(d, false, false, &p);
+    if (!aligned_to(x, 16) || !aligned_to(y, 16) || !aligned_to(residual, 16) || !aligned_to(h, 16) || !aligned_to(q, 8) || !aligned_to(weight, 16))
+        plan_of(d, false, false, &p);
     p.a.x = x, p.a.res = residual, p.a.w = weight, p.a.h = h, p.a.y = y, p.a.q = (uint8_t *)q, p.a.scales = scales, p.a.rstd = rstd;
     return run(d, p, false, (hipStream_t)stream);
 }
@@ -510,7 +521,8 @@ int cawn_rms_norm_add_bwd(const cawn_rms_desc *d, const void *h, const float *we
     }
     if (!h || !rstd || !dy) return CAWN_EINVAL;
     if (!dx && !dresidual && !dweight) return CAWN_OK;
-    if (!aligned_to(h, 16) || !aligned_to(dh, 16) || !aligned_to(dresidual, 16) || !aligned_to(dy, 16) || !aligned_to(dx, 16)) plan_of(d, false, true, &p);
+    if (!aligned_to(h, 16) || !aligned_to(dh, 16) || !aligned_to(dresidual, 16) || !aligned_to(dy, 16) || !aligned_to(dx, 16) || !aligned_to(weight, 16))
+        plan_of(d, false, true, &p);
     if (dweight && (!workspace || workspace_bytes < (size_t)p.blocks * p.a.C * 4 || !aligned_to(workspace, 256))) return CAWN_EWORKSPACE;
     p.a.x = h, p.a.w = weight, p.a.rstd_in = rstd, p.a.dy = dy, p.a.dh = dh, p.a.dx = dx, p.a.dres = dresidual, p.a.part = dweight ? (float *)workspace : nullptr;
     if (int r = run(d, p, true, s)) return r;
