@@ -428,7 +428,10 @@ int plan_of(const cawn_rms_desc *d, bool aligned, bool bwd, Plan *p)
         const int lanes = a.block / p->vec;
         if ((lanes & (lanes - 1)) == 0 && lanes <= 64 && lanes <= a.lpr) a.lpb = lanes;
     }
-    const long long all = ceil_div(a.rows, a.rpw), there = bwd ? 1024 : 4096;
+    // Workgroups: forward as many as rows are, up to 16,384; backward, where each leaves a row of sums for dweight, those that are there at once, three a CU.
+    // (32,768 rows of 4,096 channels, 8 bits, on 2,048, 4,096, 8,192, 32,768: 205, 193, 174, 174 us; forward and backward of 65,536 of 768 channels, bf16 with
+    // an fp32 residual, the latter on 384, 512, 768, 1,024, 2,048: 291, 273, 275, 290, 284.)
+    const long long all = ceil_div(a.rows, a.rpw), there = bwd ? 768 : 16384;
     p->blocks = all < there ? all : there;
     return CAWN_OK;
 }

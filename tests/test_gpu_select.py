@@ -195,6 +195,20 @@ def test_strong_forgetting_and_none(L):
         assert rel_err(s.state_out[:, c].cpu(), state[:, c]) <= 4 * tolerance(L, False), c
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("B,L,D,N,G", [(64, 1, 2100, 16, 1), (70, 2, 3000, 10, 3), (60, 1, 1500, 24, 1), (40, 1, 500, 128, 4)])
+def test_steps_of_many_rows(B, L, D, N, G, bf16):
+    """States in such number that a lane takes eight of them."""
+    i = scan_inputs(B, L, D, N, G, bf16, seed=N, ragged=True)
+    s = Scan(i, bf16, ckpt=False).forward()
+    y, state = R.scan_fwd(**reference_inputs(i))
+    assert rel_err(s.y.float().cpu(), y) <= tolerance(L, bf16)
+    assert rel_err(s.state_out.cpu(), state) <= tolerance(L, False)
+    held = s.state_in.clone()
+    t = Scan(i, bf16, ckpt=False).forward(state_in=held, state_out=held)
+    assert torch.equal(t.y, s.y) and torch.equal(held, s.state_out)
+
+
 @pytest.mark.parametrize("L", [12, 100])
 def test_gradients_with_a_rate_of_minus_infinity(L):
     """Its factor is 0, its own gradient 0 too, and the others' are those of a rate that is finite and forgets as completely."""
