@@ -540,7 +540,7 @@ int cawn_selective_scan_fwd(const cawn_scan_desc *d, const void *x, const void *
  * Backward.  x .. lengths as the forward had them, ckpt as it wrote it; dy, dstate_out or NULL (zeros).  dBm, dCm are summed over the
  * channels of a group, dA, dDskip, ddt_bias over rows and tokens.  Gradients of tokens beyond lengths[b] are 0.  Any of the gradients may be
  * NULL; dz without z, dDskip without Dskip, ddt_bias without dt_bias are not asked for with a pointer: CAWN_EINVAL.  dstate_in may be
- * dstate_out.  The same inputs give the same bits.
+ * dstate_out; other inputs must not alias outputs.  The same inputs give the same bits.
  */
 int cawn_selective_scan_bwd(const cawn_scan_desc *d, const void *x, const void *dt, const float *A, const void *Bm, const void *Cm,
                             const float *Dskip, const void *z, const float *dt_bias, const int32_t *lengths, const void *ckpt,
@@ -570,7 +570,7 @@ size_t cawn_causal_conv_workspace_bytes(const cawn_conv_desc *d);       /* of th
  *   w [C][k] fp32, bias [C] fp32 or NULL (0)
  *   lengths    as in cawn_selective_scan_fwd
  *   state_in   or NULL (zeros); state_out or NULL; they may be the same
- * x must not alias y.
+ * Inputs must not alias outputs, here and below, but for the states.
  */
 int cawn_causal_conv_fwd(const cawn_conv_desc *d, const void *x, const float *w, const float *bias, const int32_t *lengths,
                          const void *state_in, void *y, void *state_out, void *stream);
@@ -609,8 +609,8 @@ int cawn_rms_norm_add_fwd(const cawn_rms_desc *d, const void *x, const void *res
                           float *scales, float *rstd, void *stream);
 /*
  * h and rstd as the forward wrote them (without a residual and with equal types h is x); dy; dh, the gradient that reaches h from later, or NULL (0).
- * dx and dresidual hold the same gradient in their types; dx, dresidual, dweight: any may be NULL.  dy may be dx, dh may be dresidual.  The sums of
- * dweight run in a fixed order.
+ * dx and dresidual hold the same gradient in their types; dx, dresidual, dweight: any may be NULL.  dy may be dx, dh may be dresidual
+ * (with the same stride).  The sums of dweight run in a fixed order.
  */
 int cawn_rms_norm_add_bwd(const cawn_rms_desc *d, const void *h, const float *weight, const float *rstd, const void *dy, const void *dh,
                           void *dx, void *dresidual, float *dweight, void *workspace, size_t workspace_bytes, void *stream);

@@ -170,3 +170,43 @@ def test_gradients_against_differences():
         want = (value({**i, n: i[n] + v / 64}) - value({**i, n: i[n] - v / 64})) * 32
         got = float((host(g[n]) * v).sum())
         assert abs(got - want) <= 4e-3 * (float(np.sqrt((host(g[n]) ** 2).mean())) + abs(want)) + 1e-3, n
+
+
+def test_rows_far_apart():
+    """A batch whose rows lie more than 2^31 elements from each other."""
+    L, C, far = 70, 64, (1 << 31) + 64
+    i = _inputs(2, L, C, 4, True, seed=11)
+    base = Conv(i, 1, True).forward().backward()
+    c = Conv(i, 1, True)
+    new = lambda: torch.empty(far + L * C, device=DEV, dtype=torch.bfloat16).as_strided((2, L, C), (far, C, 1))  # noqa: E731
+    c.x, c.y, dx = new(), new(), new()
+    c.x.copy_(base.x)
+    c.d.x_stride_b = c.d.y_stride_b = far
+    c.forward()
+    assert torch.equal(c.y, base.y)
+    c.y.copy_(base.dy)
+    K.check(K.cawn_causal_conv_bwd(c.d, c.x, c.w, c.bias, None, c.state_in, c.y, c.dstate_out, dx, None, None, None, c.ws))
+    assert torch.equal(dx, base.g["x"])
+
+
+def test_captured_and_replayed():
+    i, j = (_inputs(3, 70, 40, 4, True, seed=k, ragged=True) for k in (12, 13))
+    j["lengths"] = i["lengths"]
+    want, c = Conv(j, 1, True).forward().backward(), Conv(i, 1, True).forward().backward()
+    new, g = Conv(j, 1, True), c.g
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.forward()
+        K.check(K.cawn_causal_conv_bwd(c.d, c.x, c.w, c.bias, c.lengths, c.state_in, c.dy, c.dstate_out, g["x"], g["w"], g["bias"], g["state_in"], c.ws))
+    for n in ("x", "dy", "w", "bias", "state_in", "dstate_out"):
+        getattr(c, n).copy_(getattr(new, n))
+    for _ in range(3):
+        for v in g.values():
+            v.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(c.y, want.y) and torch.equal(c.state_out, want.state_out)
+        assert all(torch.equal(g[n], want.g[n]) for n in g)
+        torch.ones(1000, device=DEV).sum()

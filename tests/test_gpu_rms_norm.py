@@ -177,3 +177,22 @@ def test_many_rows_of_few_channels_and_the_same_bits_again():
         assert torch.equal(a.g[n], b.g[n])
     d, dw = R.rms_bwd(a.held(), host(a.dy), host(a.w), host(a.dh))
     assert rel_err(host(a.g["x"]), d) <= TOL and rel_err(host(a.g["w"]), dw) <= 4 * TOLSUM        # (a column of 100,003 terms)
+
+
+def test_rows_far_apart():
+    """Rows more than 2^31 elements from each other."""
+    C, far = 768, (1 << 31) + 768
+    a = Rms(2, C, True, True, seed=8).forward().backward()
+    new = lambda: torch.empty(far + C, device=DEV, dtype=torch.bfloat16).as_strided((2, C), (far, 1))  # noqa: E731
+    x, h, y = new(), new(), new()
+    x.copy_(a.x)
+    d = K.make_rms_desc(2, C, bf16=1, residual_bf16=1, x_stride=far, residual_stride=far, y_stride=far)
+    h.copy_(a.res)
+    rstd = torch.empty(2, device=DEV)
+    K.check(K.cawn_rms_norm_add_fwd(d, x, h, a.w, h, y, None, None, rstd))
+    assert torch.equal(h, a.h) and torch.equal(y, a.y)
+    y.copy_(a.dy)
+    dw = torch.empty(C, device=DEV)
+    K.check(K.cawn_rms_norm_add_bwd(d, h, a.w, rstd, y, None, x, None, dw, a.ws))
+    b = Rms(2, C, True, True, seed=8).forward().backward(dh=False)
+    assert torch.equal(x, b.g["x"]) and torch.equal(dw, b.g["w"])

@@ -288,3 +288,36 @@ def test_graph_and_stream():
     assert torch.equal(s.y, want.y)
     for n in g:
         assert torch.equal(g[n], want.g[n]), n
+
+
+@pytest.mark.parametrize("ckpt", [False, True])
+def test_no_tokens_pass_the_state_and_its_gradient(ckpt):
+    i = scan_inputs(2, 0, 70, 16, 1, False, seed=17)
+    s = Scan(i, False, ckpt=ckpt).forward().backward()
+    assert torch.equal(s.state_out, s.state_in) and torch.equal(s.g["state_in"], s.dstate_out)
+    for n in ("A", "Dskip", "dt_bias"):
+        assert bool((s.g[n] == 0).all()), n
+
+
+def test_rows_far_apart():
+    """A batch whose rows lie more than 2^31 elements from each other."""
+    L, D, N, far = 40, 64, 16, (1 << 31) + 64
+    i = scan_inputs(2, L, D, N, 1, True, seed=18)
+    base = Scan(i, True).forward().backward()
+    s = Scan(i, True)
+    big = torch.empty(far + L * D, device="cuda", dtype=torch.bfloat16)
+    out = torch.empty(far + L * D, device="cuda", dtype=torch.bfloat16)
+    s.x = big.as_strided((2, L, D), (far, D, 1))
+    s.x.copy_(base.x)
+    s.y = out.as_strided((2, L, D), (far, D, 1))
+    s.dy = s.y                                           # (gradients have the stride of what they belong to: a call without y's comes behind)
+    s.d.x_stride_b = s.d.y_stride_b = far
+    s.forward()
+    torch.cuda.synchronize()
+    assert torch.equal(s.y, base.y) and torch.equal(s.state_out, base.state_out)
+    s.dy.copy_(base.dy)
+    from paper_2604_04250_amd import binding as K
+    dx = torch.empty(far + L * D, device="cuda", dtype=torch.bfloat16).as_strided((2, L, D), (far, D, 1))
+    K.check(K.cawn_selective_scan_bwd(s.d, s.x, s.dt, s.A, s.Bm, s.Cm, s.Dk, s.z, s.bias, None, s.ckpt, s.dy, s.dstate_out, dx, None, None, None, None, None, None, None, None,
+                                      s.ws))
+    assert torch.equal(dx, base.g["x"])
