@@ -5,8 +5,6 @@
 // A lane owns a channel, a wave 64 of them and up to 16 of their states: B and C, which the channels share, then come by scalar loads and are
 // operands of the vector instructions as they stand.  More than 16 states are shared out over the waves of a workgroup.
 #pragma once
-#include <type_traits>
-
 #include "cawn_sums.hpp"
 
 namespace cawn {
@@ -185,7 +183,7 @@ template <int W> __device__ inline Scalars<W> bc_run(const float *tile, int n, i
 // A stream's rows of W tokens from `row` on: the tokens' places are scalar, the lane's 32 bits of bytes, as buffer instructions take them.  (From pointers
 // the compiler adds the lane's place first and walks along the tokens with vector instructions.)  The resource ends nowhere: the callers' bounds count.
 __device__ inline __amdgpu_buffer_rsrc_t rows_at(const void *row) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(row), 0, -1, 0x00020000); }
-// A value as it comes, and what it is.  (Kept as 32 bits it has a register of its own; as a bf16, where registers are short, the compiler puts two in one.)
+// A value as it comes, in a register of its own (of values of 16 bits the compiler would put two in one, which costs instructions), and what it is.
 template <typename T> __device__ inline uint32_t load_at(__amdgpu_buffer_rsrc_t r, uint32_t lane, uint32_t token)
 {
     if constexpr (sizeof(T) == 2) return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, lane, token, 0);
@@ -200,25 +198,22 @@ template <typename T> __device__ inline void store_at(__amdgpu_buffer_rsrc_t r, 
 }
 
 // W tokens of a stream, of which `left` are there (the last of them again for the others); step: of a token, in bytes
-template <typename T, int W, typename R> __device__ inline void load_run(const T *row, uint32_t step, int left, uint32_t lane, R (&v)[W])
+template <typename T, int W> __device__ inline void load_run(const T *row, uint32_t step, int left, uint32_t lane, uint32_t (&v)[W])
 {
     const auto r = rows_at(row);
     uint32_t token = 0;
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-        const uint32_t x = load_at<T>(r, lane, token);
-        if constexpr (std::is_same<R, bf16>::value) v[i] = __builtin_bit_cast(bf16, (uint16_t)x);
-        else if constexpr (std::is_same<R, float>::value) v[i] = __uint_as_float(x);
-        else v[i] = x;
+        v[i] = load_at<T>(r, lane, token);
         token += i + 1 < left ? step : 0;
     }
 }
 
 // Nothing: values that a branch leaves alone would be kept from the round before.
-template <int W, typename R> __device__ inline void no_run(R (&v)[W])
+template <int W> __device__ inline void no_run(uint32_t (&v)[W])
 {
 #pragma unroll
-    for (int i = 0; i < W; ++i) v[i] = (R)0;
+    for (int i = 0; i < W; ++i) v[i] = 0;
 }
 
 // ... of an output, from f(i)

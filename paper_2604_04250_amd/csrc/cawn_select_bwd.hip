@@ -172,7 +172,7 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
     T *dzp = a.dz ? (T *)a.dz + p.b * a.zsb + p.base : nullptr;
     const uint32_t at = p.bytes<T>();
     auto step = [](long long stride) { return (uint32_t)stride * (uint32_t)sizeof(T); };
-    T xr[TILE], xn[TILE], dr[TILE], yr[TILE], zr[TILE];
+    uint32_t xr[TILE], xn[TILE], dr[TILE], yr[TILE], zr[TILE];
     auto fetch = [&](int t) {
         if (t < t0) {
             no_run<TILE>(dr), no_run<TILE>(xn), no_run<TILE>(yr), no_run<TILE>(zr);
@@ -207,7 +207,7 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
         // (one stream after the other, so that what has been read makes room for what comes of it)
         float delta[TILE], slope[TILE], u[TILE], g[TILE], q[TILE], du[TILE], dd[TILE], y[TILE];
 #pragma unroll
-        for (int i = 0; i < TILE; ++i) delta[i] = (float)dr[i] + bias, slope[i] = 1.f;
+        for (int i = 0; i < TILE; ++i) delta[i] = value<T>(dr[i]) + bias, slope[i] = 1.f;
         if (a.softplus) {
 #pragma unroll
             for (int i = 0; i < TILE; ++i) {
@@ -217,12 +217,12 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < TILE; ++i) g[i] = (float)yr[i], q[i] = 0.f;
+        for (int i = 0; i < TILE; ++i) g[i] = value<T>(yr[i]), q[i] = 0.f;
         if (zp) {
 #pragma unroll
             for (int i = 0; i < TILE; ++i) {
                 float silu;
-                const float ds = dsilu((float)zr[i], silu);
+                const float ds = dsilu(value<T>(zr[i]), silu);
                 q[i] = g[i] * ds;
                 g[i] *= silu;
             }
@@ -231,7 +231,7 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
 #pragma unroll
         for (int i = 0; i < TILE; ++i) {
             if (!MULTI) xr[i] = xn[i];
-            const float x = (float)xn[i];
+            const float x = value<T>(xn[i]);
             u[i] = delta[i] * x;
             y[i] = first * x;
         }
@@ -320,7 +320,7 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
         };
         if constexpr (!MULTI) {
 #pragma unroll
-            for (int i = 0; i < TILE; ++i) finish(i < left, (float)xr[i], delta[i], slope[i], g[i], q[i], du[i], dd[i], y[i]);
+            for (int i = 0; i < TILE; ++i) finish(i < left, value<T>(xr[i]), delta[i], slope[i], g[i], q[i], du[i], dd[i], y[i]);
             if (p.on) {
                 if (dxp) store_run<T, TILE>(dxp + t * a.xst, step(a.xst), left, at, [&](int i) { return du[i]; });
                 if (ddp) store_run<T, TILE>(ddp + t * a.dst, step(a.dst), left, at, [&](int i) { return dd[i]; });
