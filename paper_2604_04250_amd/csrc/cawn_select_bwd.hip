@@ -105,8 +105,30 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
 
 template <int CTRL> __device__ inline float from_lane(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false)); }
 
-// Two values a lane become one, each summed over pairs of lanes: the lanes without the level's bit (32, 16, 8, .. for level 0, 1, 2, ..) keep the first.
-__device__ inline float merge(int level, float first, float second, int lane)
+// Sums over lanes by a tree that halves the values as it halves the lanes: of two values one remains, summed over pairs of lanes, the first in the lanes
+// without a bit of the lane's number, the second in those with it.
+//
+// Four values, by bits 3 and 2: the lanes of a bit are banks of a row, which an addition may leave out, so that two instructions make one value of two (with
+// selections it takes three).  Whoever writes a register that is read across lanes has to be two instructions away: the s_nops; no lane is idle here.
+__device__ inline float four(float a0, float a1, float b0, float b1)
+{
+    float s, t, r;
+    asm("s_nop 1\n\t"
+        "v_add_f32_dpp %0, %3, %3 row_ror:8 row_mask:0xf bank_mask:0x3\n\t"
+        "v_add_f32_dpp %1, %5, %5 row_ror:8 row_mask:0xf bank_mask:0x3\n\t"
+        "v_add_f32_dpp %0, %4, %4 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+        "v_add_f32_dpp %1, %6, %6 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+        "s_nop 0\n\t"
+        "v_add_f32_dpp %2, %0, %0 row_half_mirror row_mask:0xf bank_mask:0x5\n\t"
+        "v_add_f32_dpp %2, %1, %1 row_half_mirror row_mask:0xf bank_mask:0xa\n\t"
+        "s_nop 1"
+        : "=&v"(s), "=&v"(t), "=&v"(r)
+        : "v"(a0), "v"(a1), "v"(b0), "v"(b1));
+    return r;
+}
+
+// Two values, by bit 5, 4, 1, 0 for level 0 to 3.
+__device__ inline float two_values(int level, float first, float second, int lane)
 {
     if (level == 0) {
         const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(first), __float_as_uint(second), false, false);
@@ -116,26 +138,24 @@ __device__ inline float merge(int level, float first, float second, int lane)
         const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(first), __float_as_uint(second), false, false);
         return __uint_as_float(r[0]) + __uint_as_float(r[1]);
     }
-    const bool bit = lane & (32 >> level);
+    const bool bit = lane & (level == 2 ? 2 : 1);
     const float keep = bit ? second : first, give = bit ? first : second;
-    if (level == 2) return keep + from_lane<0x128>(give);           // row_ror:8
-    if (level == 3) return keep + from_lane<0x141>(give);           // row_half_mirror: lane i from 7 - i
-    if (level == 4) return keep + from_lane<0x4e>(give);            // quad_perm 2,3,0,1
-    return keep + from_lane<0xb1>(give);                            // quad_perm 1,0,3,2
+    return keep + (level == 2 ? from_lane<0x4e>(give) : from_lane<0xb1>(give));         // quad_perm 2,3,0,1 and 1,0,3,2
 }
 
-// Sums of 64 values over the 64 lanes, given one by one: the i-th is then in the lane whose number is i's six bits turned round.
+// 64 values, four at a time: value i is then in the lane whose bits 3, 2, 5, 4, 1, 0 are i's bits 0 to 5.
 struct LaneSums {
-    float held[6];
-    __device__ inline float push(int i, float v, int lane)
+    float held[4];
+    __device__ inline float push(int group, float a0, float a1, float b0, float b1, int lane)
     {
+        float v = four(a0, a1, b0, b1);
 #pragma unroll
-        for (int level = 0; level < 6; ++level) {
-            if (!(i >> level & 1)) {
+        for (int level = 0; level < 4; ++level) {
+            if (!(group >> level & 1)) {
                 held[level] = v;
                 return v;
             }
-            v = merge(level, held[level], v, lane);
+            v = two_values(level, held[level], v, lane);
         }
         return v;
     }
@@ -276,22 +296,24 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
                     }
                 }
                 const float Af = fmaxf(A[j], -3.4028235e38f);       // (where the rate is minus infinity p is 0, and so is its share)
+                // (token pairs: their four products' sums are begun together)
+                float ub[2], gc[2];
 #pragma unroll
                 for (int i = TILE - 1; i >= 0; --i) {
-                    const int k = (j * TILE + TILE - 1 - i) * 2;
                     const float dS = fmaf(Cv[j][i], g[i], h[j]);
                     du[i] = fmaf(Bv[j][i], dS, du[i]);
                     h[j] = e[i] * dS;
                     const float pr = h[j] * (i ? S[i ? i - 1 : 0] : before[j]);
                     dd[i] = fmaf(Af, pr, dd[i]);
                     dA[j] = fmaf(delta[i], pr, dA[j]);
-                    sums.push(k, u[i] * dS, p.lane);
-                    all = sums.push(k + 1, g[i] * S[i], p.lane);
+                    ub[i & 1] = u[i] * dS, gc[i & 1] = g[i] * S[i];
+                    if ((i & 1) == 0) all = sums.push((j * TILE + TILE - 2 - i) / 2, ub[1], gc[1], ub[0], gc[0], p.lane);
                 }
                 mine[s + j][0][p.lane] = h[j], mine[s + j][1][p.lane] = dA[j];
             }
-            const int which = p.lane >> 5 & 1, j = p.lane & 1;
-            const int i = TILE - 1 - ((p.lane >> 4 & 1) | (p.lane >> 2 & 2) | (p.lane & 4) | (p.lane << 2 & 8));
+            // value 2 (16 j + 15 - i) + which
+            const int which = p.lane >> 3 & 1, j = p.lane & 1;
+            const int i = TILE - 1 - ((p.lane >> 2 & 1) | (p.lane >> 4 & 2) | (p.lane >> 2 & 4) | (p.lane << 2 & 8));
             if (MULTI) {
                 if (a.part_bc) a.part_bc[((((bt * TILE + i) * a.G + p.g) * a.parts + p.cb) * 2 + which) * NPT + p.blk * NP + s + j] = all;
             } else stage[buf][MULTI ? 0 : w][i][which][s + j] = all;
@@ -312,11 +334,13 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
         }
         // (dd becomes the gradient of dt, du that of x, y that of z)
         auto finish = [&](bool there, float x, float delta, float slope, float g, float q, float &du, float &dd, float &y) {
-            dd = there ? fmaf(du, x, dd * LN2) * slope : 0.f;
+            dd = fmaf(du, x, dd * LN2) * slope;
             du = fmaf(du, delta, Dk * g);
             y *= q;
-            sumD = fmaf(g, there ? x : 0.f, sumD);
-            sumb += dd;
+            if (there) {
+                sumD = fmaf(g, x, sumD);
+                sumb += dd;
+            }
         };
         if constexpr (!MULTI) {
 #pragma unroll
