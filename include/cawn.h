@@ -499,9 +499,10 @@ int cawn_dropout_add_bwd(const cawn_dropout_desc *d, const void *dy, const uint6
  *     y[t]  = (Cm[t][g] . S[t] + Dskip[c] x[t][c]) z[t][c] / (1 + e^-z[t][c])
  */
 typedef struct cawn_scan_desc {
-    int32_t B, L;         /* batch rows; tokens in THIS call (0 allowed: the state is passed through)               */
-    int32_t D, N;         /* channels, and states of each, 1..128 (beyond: CAWN_EUNSUPPORTED)                       */
-    int32_t G;            /* groups of channels that share Bm and Cm; divides D; 0 = 1                              */
+    int32_t B, L;         /* batch rows; tokens in THIS call (0 allowed: the state is passed through), up to 2^30   */
+    int32_t D, N;         /* channels, up to 2^25, and states of each, 1..128 (beyond any of these, or with a token stride of
+                             x, dt, z or y beyond 2^25: CAWN_EUNSUPPORTED)                                           */
+    int32_t G;            /* groups of channels that share Bm and Cm; divides D, up to 2^23; 0 = 1                  */
     int32_t bf16;         /* 0: x, dt, Bm, Cm, z, y and their gradients are fp32; 1: bfloat16.  A, Dskip, dt_bias, the state, the
                              checkpoint and their gradients are fp32 either way, as is all arithmetic                */
     int32_t dt_softplus;  /* 1: softplus (above); 0: delta = dt + dt_bias                                           */
@@ -553,8 +554,8 @@ int cawn_selective_scan_bwd(const cawn_scan_desc *d, const void *x, const void *
  * (cawn_syntax_conv is the layer's own, with its clamp and forward alone.)
  */
 typedef struct cawn_conv_desc {
-    int32_t B, L, C, k;                 /* rows, tokens of THIS call (0 allowed: the state is passed through), channels, taps 1..4 (beyond:
-                                           CAWN_EUNSUPPORTED)                                                                          */
+    int32_t B, L, C, k;                 /* rows, tokens of THIS call (0 allowed: the state is passed through), channels, both up to 2^30,
+                                           taps 1..4 (beyond: CAWN_EUNSUPPORTED)                                                       */
     int32_t act;                        /* 0 none, 1 SiLU                                                                              */
     int32_t bf16;                       /* 1: x, y, dy, dx are bfloat16, else fp32; taps, bias, state and their gradients are fp32     */
     int32_t accumulate_param_grads;     /* backward: 0 overwrite, 1 add into dw, dbias                                                 */

@@ -337,7 +337,7 @@ struct Plan {
 int plan_of(const cawn_conv_desc *d, bool aligned, bool bwd, Plan *p)
 {
     if (!d || d->B < 0 || d->L < 0 || d->C <= 0 || d->k <= 0 || d->act < 0 || d->act > 1 || (d->bf16 & ~1) || d->reserved) return CAWN_EINVAL;
-    if (d->k > K_MAX) return CAWN_EUNSUPPORTED;
+    if (d->k > K_MAX || d->L > 1 << 30 || d->C > 1 << 30) return CAWN_EUNSUPPORTED;        // (places of tokens and channels, and of a run behind them, in 32 bits)
     ConvArgs &a = p->a;
     a = ConvArgs{};
     a.B = d->B, a.L = d->L, a.C = d->C, a.act = d->act, p->k = d->k;

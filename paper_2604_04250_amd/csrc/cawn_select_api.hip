@@ -54,9 +54,9 @@ int check(const cawn_scan_desc *d, bool bwd, Args *a)
     a->wide = a->NB > 1 ? 1 : a->cpg < 4 ? a->cpg : 4;
     a->cbg = (int)ceil_div(a->cpg, a->wide);
     a->parts = a->cbg;
-    // places of a channel in its row and of a token among 16 are 32 bits of bytes
+    // places of a channel in its row and of a token among 16 are 32 bits of bytes; tokens of a row and places of channels are counted in 32 bits
     const long long wide = 1 << 25;
-    if (d->D > wide || a->xst > wide || a->dst > wide || a->zst > wide || a->yst > wide) return CAWN_EUNSUPPORTED;
+    if (d->D > wide || a->xst > wide || a->dst > wide || a->zst > wide || a->yst > wide || d->L > 1 << 30 || (long long)a->cpg * G > 1 << 24) return CAWN_EUNSUPPORTED;
     a->Dp = a->cpg * G * 64;
     a->tiles = (int)ceil_div(d->L, TILE);
     cut(a, bwd ? 6144 : 8192);

@@ -124,3 +124,22 @@ def test_the_bindings_wrappers_pass_as_many_arguments_as_their_entry_points_take
         assert f(d, *([None] * n), stream=0) == K.CAWN_EINVAL, name
         with pytest.raises(TypeError):
             f(K.make_dropout_desc(1, 1), *([None] * n), stream=0)
+
+
+def test_sizes_whose_places_32_bits_do_not_count_are_refused():
+    most = (1 << 31) - 1
+
+    def scan(d):
+        return d, "cawn_selective_scan_fwd", [*_args(14), BIG], K.cawn_selective_scan_workspace_bytes
+
+    def conv(d):
+        return d, "cawn_causal_conv_fwd", _args(7), K.cawn_causal_conv_workspace_bytes
+
+    for d, name, args, size in (scan(K.make_scan_desc(1, most, 4, 1)), scan(K.make_scan_desc(1, (1 << 30) + 1, 4, 1)),
+                             scan(K.make_scan_desc(1, 100, 1 << 25, 1, G=1 << 25)),        # 64 places a group
+                             scan(K.make_scan_desc(1, 100, 1 << 26, 1)), scan(K.make_scan_desc(1, 100, 4, 1, dt_stride_t=1 << 26)),
+                             conv(K.make_conv_desc(1, most, 1, 4)), conv(K.make_conv_desc(1, 1, most, 4))):
+        assert size(d) == 0
+        assert getattr(K.lib(), name)(C.byref(d), *args, None) == K.CAWN_EUNSUPPORTED
+    assert K.cawn_selective_scan_workspace_bytes(K.make_scan_desc(1, 1 << 30, 4, 1)) > 0
+    assert K.cawn_causal_conv_workspace_bytes(K.make_conv_desc(1, 1 << 30, 1, 4)) > 0
