@@ -6,6 +6,7 @@
 // A thread takes VEC adjacent channels (16 bytes) along a run of tokens; the k - 1 inputs before the run's first token are read again, and backward
 // the k - 1 tokens behind its last.  Bound by memory.
 // The row's state (the k - 1 inputs before its first token, in fp32) is read and replaced by the thread of the row's first run alone.
+#include "cawn_rows.hpp"
 #include "cawn_sums.hpp"
 
 using namespace cawn::ops;
@@ -58,11 +59,12 @@ template <int K, int VEC> __device__ inline void load_state(const ConvArgs &a, c
 #pragma unroll
     for (int j = 0; j < VEC; ++j) x[j] = p[j];
 }
-template <int K, int VEC> __device__ inline void store_state(const ConvArgs &a, float *p, long long b, int at, int c, const float (&x)[VEC])
+template <int K, int VEC> __device__ inline void store_state(const ConvArgs &a, float *p, long long b, int at, int c, int skip, const float (&x)[VEC])
 {
     p += (b * (K - 1) + at) * a.C + c;
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) p[j] = x[j];
+    for (int j = 0; j < VEC; ++j)
+        if (j >= skip) p[j] = x[j];
 }
 
 // Input `back` (1 .. K - 1) places before the row's first token
@@ -77,22 +79,23 @@ template <int K, int VEC> __device__ inline void before_row(const ConvArgs &a, i
 
 // U tokens' values from token t on, those below `end`; what is not there is the row's last again (a load behind a lane's branch would be waited for by
 // itself) and is left out where it is used
-template <typename T, int VEC> __device__ inline void fetch(const T *row, long long stride, int t, int end, Pack<T, VEC> (&v)[U])
+template <typename T, int VEC> __device__ inline void fetch(const T *row, long long stride, int t, int end, Loose<T, VEC> (&v)[U])
 {
 #pragma unroll
-    for (int i = 0; i < U; ++i) v[i] = *reinterpret_cast<const Pack<T, VEC> *>(row + min(t + i, end - 1) * stride);
+    for (int i = 0; i < U; ++i) v[i] = *reinterpret_cast<const Loose<T, VEC> *>(row + min(t + i, end - 1) * stride);
 }
 
-template <typename T, int VEC> __device__ inline void widen(const Pack<T, VEC> &v, float (&x)[VEC])
+template <typename T, int VEC> __device__ inline void widen(const Loose<T, VEC> &v, float (&x)[VEC])
 {
 #pragma unroll
     for (int j = 0; j < VEC; ++j) x[j] = (float)v.v[j];
 }
 
-template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void conv_forward(const ConvArgs a)
+template <typename T, int K, int VEC, bool TAIL> __global__ __launch_bounds__(256) void conv_forward(const ConvArgs a)
 {
     const long long id = (long long)blockIdx.x * 256 + threadIdx.x, rest = id / a.units;
-    const int c = (int)(id - rest * a.units) * VEC;
+    const Unit<VEC, TAIL> u((int)(id - rest * a.units), a.C);
+    const int c = u.c, skip = u.skip;
     const long long bl = rest / a.runs;
     if (bl >= a.B) return;
     const int b = (int)bl, t0 = (int)(rest - bl * a.runs) * a.run, end = min(a.L, t0 + a.run);
@@ -106,12 +109,12 @@ template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void con
         for (int i = 0; i < K - 1; ++i) before_row<K, VEC>(a, b, K - 1 - i, c, win[i]);
     }
     const int n = row_length(a, b), t1 = min(n, t0 + a.run);
-    Pack<T, VEC> next[U];
+    Loose<T, VEC> next[U];
     if (t0 < t1) {
         fetch<T, VEC>(x, a.xst, t0, t1, next);
         if (t0 > 0) {
 #pragma unroll
-            for (int i = 0; i < K - 1; ++i) load_n<T, VEC>(x + (t0 - (K - 1) + i) * a.xst, win[i]);
+            for (int i = 0; i < K - 1; ++i) read_n<T, VEC>(x + (t0 - (K - 1) + i) * a.xst, win[i]);
         }
     }
     if (t0 == 0 && K > 1 && a.state_out) {
@@ -120,11 +123,11 @@ template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void con
 #pragma unroll
         for (int i = 0; i < K - 1; ++i) {
             const int t = n - (K - 1) + i;
-            if (t >= 0) load_n<T, VEC>(x + t * a.xst, s[i]);
+            if (t >= 0) read_n<T, VEC>(x + t * a.xst, s[i]);
             else before_row<K, VEC>(a, b, -t, c, s[i]);
         }
 #pragma unroll
-        for (int i = 0; i < K - 1; ++i) store_state<K, VEC>(a, a.state_out, b, i, c, s[i]);
+        for (int i = 0; i < K - 1; ++i) store_state<K, VEC>(a, a.state_out, b, i, c, skip, s[i]);
     }
     for (int t = t0; t < t1; t += U) {
 #pragma unroll
@@ -141,7 +144,7 @@ template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void con
                 for (int i = 0; i < K; ++i) z[j] = fmaf(p.w[i][j], win[k + i][j], z[j]);
                 if (a.act) z[j] *= sigmoid_f(z[j]);
             }
-            store_n<T, VEC>(y + (t + k) * a.yst, z);
+            write_n<T, VEC>(y + (t + k) * a.yst, z, skip);
         }
 #pragma unroll
         for (int i = 0; i < K - 1; ++i)
@@ -150,7 +153,7 @@ template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void con
     }
     for (int t = max(t0, n); t < end; ++t) {
         const float z[VEC] = {};
-        store_n<T, VEC>(y + t * a.yst, z);
+        write_n<T, VEC>(y + t * a.yst, z, skip);
     }
 }
 
@@ -170,13 +173,13 @@ template <int K, int VEC> __device__ inline void slope(const ConvArgs &a, const 
     }
 }
 
-template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void conv_backward(const ConvArgs a)
+template <typename T, int K, int VEC, bool TAIL> __global__ __launch_bounds__(256) void conv_backward(const ConvArgs a)
 {
     __shared__ float sh[256 * VEC];
     const int unit = threadIdx.x % a.ub, row = threadIdx.x / a.ub;
     const long long rblk = blockIdx.x / a.ublocks;
-    const int u = (int)(blockIdx.x - rblk * a.ublocks) * a.ub + unit;
-    const int c = (u < a.units ? u : 0) * VEC;
+    const Unit<VEC, TAIL> u((int)(blockIdx.x - rblk * a.ublocks) * a.ub + unit, a.C);
+    const int c = u.c, skip = u.skip;
     const Taps<K, VEC> p(a, c);
     float dw[K][VEC], db[VEC];
 #pragma unroll
@@ -186,12 +189,12 @@ template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void con
         for (int i = 0; i < K; ++i) dw[i][j] = 0.f;
     }
     const long long all = a.runs * a.B;
-    for (long long rr = rblk * a.rb + row; u < a.units && row < a.rb && rr < all; rr += a.rblocks * a.rb) {
+    for (long long rr = rblk * a.rb + row; u.in && row < a.rb && rr < all; rr += a.rblocks * a.rb) {
         const int b = (int)(rr / a.runs), n = row_length(a, b);
         const int t0 = (int)(rr - b * a.runs) * a.run, t1 = min(n, t0 + a.run), end = min(a.L, t0 + a.run);
         const T *x = (const T *)a.x + b * a.xsb + c, *dyp = (const T *)a.dy + b * a.ysb + c;
         T *dx = a.dx ? (T *)a.dx + b * a.xsb + c : nullptr;
-        Pack<T, VEC> xn[U], dn[U];
+        Loose<T, VEC> xn[U], dn[U];
         if (t0 < t1) fetch<T, VEC>(x, a.xst, t0, n, xn), fetch<T, VEC>(dyp, a.yst, t0, n, dn);
         float win[K - 1 + U][VEC], dzs[K - 1 + U][VEC];         // the inputs that U tokens see; their dz and the K - 1 before them
 #pragma unroll
@@ -200,7 +203,7 @@ template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void con
 #pragma unroll
             for (int j = 0; j < VEC; ++j) dzs[i][j] = win[i][j] = 0.f;
             if (t0 >= t1) continue;
-            if (t >= 0) load_n<T, VEC>(x + t * a.xst, win[i]);
+            if (t >= 0) read_n<T, VEC>(x + t * a.xst, win[i]);
             else before_row<K, VEC>(a, b, -t, c, win[i]);
         }
         // up to K - 1 tokens behind the run: the gradients of its last inputs need their dz
@@ -242,8 +245,8 @@ template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void con
 #pragma unroll
                         for (int j = 0; j < VEC; ++j) d[j] += e[j];
                     }
-                    if (at >= 0) store_n<T, VEC>(dx + at * a.xst, d);
-                    else store_state<K, VEC>(a, a.dstate_in, b, at + K - 1, c, d);
+                    if (at >= 0) write_n<T, VEC>(dx + at * a.xst, d, skip);
+                    else store_state<K, VEC>(a, a.dstate_in, b, at + K - 1, c, skip, d);
                 }
             }
 #pragma unroll
@@ -254,7 +257,7 @@ template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void con
         if (dx) {
             for (int t = max(t0, n); t < end; ++t) {
                 const float z[VEC] = {};
-                store_n<T, VEC>(dx + t * a.xst, z);
+                write_n<T, VEC>(dx + t * a.xst, z, skip);
             }
         }
     }
@@ -266,12 +269,12 @@ template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void con
 #pragma unroll
         for (int j = 0; j < VEC; ++j) sh[threadIdx.x * VEC + j] = i < K ? dw[i < K ? i : 0][j] : db[j];
         __syncthreads();
-        if (row == 0 && u < a.units) {
+        if (row == 0 && u.in) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 float v = 0.f;
                 for (int q = 0; q < a.rb; ++q) v += sh[(q * a.ub + unit) * VEC + j];
-                a.part[(rblk * (K + 1) + i) * a.C + c + j] = v;
+                if (j >= skip) a.part[(rblk * (K + 1) + i) * a.C + c + j] = v;
             }
         }
     }
@@ -279,11 +282,12 @@ template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void con
 
 // The gradient of the state before the row alone, where it takes the place of that behind the row, which the other workgroups read: what its first
 // K - 1 tokens make of it, and what of it is still there behind the last.
-template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void conv_state_backward(const ConvArgs a)
+template <typename T, int K, int VEC, bool TAIL> __global__ __launch_bounds__(256) void conv_state_backward(const ConvArgs a)
 {
     const long long id = (long long)blockIdx.x * 256 + threadIdx.x, b = id / a.units;
     if (b >= a.B) return;
-    const int c = (int)(id - b * a.units) * VEC, n = row_length(a, (int)b);
+    const Unit<VEC, TAIL> u((int)(id - b * a.units), a.C);
+    const int c = u.c, n = row_length(a, (int)b);
     const Taps<K, VEC> p(a, c);
     float d[K][VEC], dz[K][VEC], win[K][VEC];
 #pragma unroll
@@ -298,8 +302,8 @@ template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void con
         for (int i = 0; i + 1 < K; ++i)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) win[i][j] = win[i + 1][j];
-        load_n<T, VEC>((const T *)a.x + b * a.xsb + t * a.xst + c, win[K - 1]);
-        load_n<T, VEC>((const T *)a.dy + b * a.ysb + t * a.yst + c, dy);
+        read_n<T, VEC>((const T *)a.x + b * a.xsb + t * a.xst + c, win[K - 1]);
+        read_n<T, VEC>((const T *)a.dy + b * a.ysb + t * a.yst + c, dy);
         slope<K, VEC>(a, p, win, dy, dz[t]);
     }
     // (the sum in the order of the other kernel, whose bits these are)
@@ -313,7 +317,7 @@ template <typename T, int K, int VEC> __global__ __launch_bounds__(256) void con
             if (a.dstate_out && s >= n) d[s][j] += a.dstate_out[(b * (K - 1) + (s - n)) * a.C + c + j];
         }
 #pragma unroll
-    for (int i = 0; i < K - 1; ++i) store_state<K, VEC>(a, a.dstate_in, b, i, c, d[i]);
+    for (int i = 0; i < K - 1; ++i) store_state<K, VEC>(a, a.dstate_in, b, i, c, u.skip, d[i]);
 }
 
 struct TapSums {        // column (i, c) of a part's [K + 1][C]
@@ -333,8 +337,7 @@ struct Plan {
     long long blocks;
 };
 
-// The geometry must not depend on pointers: the workspace is sized without them.  Rows that do not begin on 16 bytes are taken value by value.
-int plan_of(const cawn_conv_desc *d, bool aligned, bool bwd, Plan *p)
+int plan_of(const cawn_conv_desc *d, bool bwd, Plan *p)
 {
     if (!d || d->B < 0 || d->L < 0 || d->C <= 0 || d->k <= 0 || d->act < 0 || d->act > 1 || (d->bf16 & ~1) || d->reserved) return CAWN_EINVAL;
     if (d->k > K_MAX || d->L > 1 << 30 || d->C > 1 << 30) return CAWN_EUNSUPPORTED;        // (places of tokens and channels, and of a run behind them, in 32 bits)
@@ -344,9 +347,8 @@ int plan_of(const cawn_conv_desc *d, bool aligned, bool bwd, Plan *p)
     a.xst = d->x_stride_t ? d->x_stride_t : d->C, a.yst = d->y_stride_t ? d->y_stride_t : d->C;
     if (a.xst < a.C || a.yst < a.C) return CAWN_EINVAL;
     a.xsb = d->x_stride_b ? d->x_stride_b : a.xst * d->L, a.ysb = d->y_stride_b ? d->y_stride_b : a.yst * d->L;
-    const int most = 4;
-    p->vec = aligned && a.C % most == 0 && a.xst % most == 0 && a.xsb % most == 0 && a.yst % most == 0 && a.ysb % most == 0 ? most : 1;
-    a.units = a.C / p->vec;
+    p->vec = a.C >= 4 ? 4 : 1;
+    a.units = (int)ceil_div(a.C, p->vec);
     // Tokens of a run: a longer one reads fewer tokens twice, where as many threads are left as the chip holds.  (8 x 8,192 tokens of 768 channels in bf16,
     // forward and backward, us: runs of 32 and 64 109, 16 and 64 111, 32 and 32 118, 16 and 16 144.)
     a.run = bwd ? 64 : 32;
@@ -369,33 +371,38 @@ int plan_of(const cawn_conv_desc *d, bool aligned, bool bwd, Plan *p)
 
 size_t part_bytes(const Plan &p) { return (size_t)p.a.rblocks * (p.k + 1) * p.a.C * 4; }
 
-template <typename T, int K, int VEC> int launch(const Plan &p, bool bwd, hipStream_t s)
+template <typename T, int K, int VEC, bool TAIL> int launch(const Plan &p, bool bwd, hipStream_t s)
 {
-    if (!bwd) hipLaunchKernelGGL((conv_forward<T, K, VEC>), dim3((unsigned)p.blocks), dim3(256), 0, s, p.a);
+    if (!bwd) hipLaunchKernelGGL((conv_forward<T, K, VEC, TAIL>), dim3((unsigned)p.blocks), dim3(256), 0, s, p.a);
     else {
         ConvArgs a = p.a;
         const bool replaces = K > 1 && a.dstate_in && a.dstate_in == a.dstate_out;
         if (replaces) a.dstate_in = nullptr;
-        if (a.dx || a.part || a.dstate_in) hipLaunchKernelGGL((conv_backward<T, K, VEC>), dim3((unsigned)p.blocks), dim3(256), 0, s, a);
-        if (replaces) hipLaunchKernelGGL((conv_state_backward<T, K, VEC>), dim3((unsigned)ceil_div((long long)a.B * a.units, 256)), dim3(256), 0, s, p.a);
+        if (a.dx || a.part || a.dstate_in) hipLaunchKernelGGL((conv_backward<T, K, VEC, TAIL>), dim3((unsigned)p.blocks), dim3(256), 0, s, a);
+        if (replaces) hipLaunchKernelGGL((conv_state_backward<T, K, VEC, TAIL>), dim3((unsigned)ceil_div((long long)a.B * a.units, 256)), dim3(256), 0, s, p.a);
     }
     return launched();
 }
 
-template <typename T, int VEC> int launch_k(const Plan &p, bool bwd, hipStream_t s)
+template <typename T, int VEC, bool TAIL> int launch_k(const Plan &p, bool bwd, hipStream_t s)
 {
     switch (p.k) {
-    case 1: return launch<T, 1, VEC>(p, bwd, s);
-    case 2: return launch<T, 2, VEC>(p, bwd, s);
-    case 3: return launch<T, 3, VEC>(p, bwd, s);
-    default: return launch<T, 4, VEC>(p, bwd, s);
+    case 1: return launch<T, 1, VEC, TAIL>(p, bwd, s);
+    case 2: return launch<T, 2, VEC, TAIL>(p, bwd, s);
+    case 3: return launch<T, 3, VEC, TAIL>(p, bwd, s);
+    default: return launch<T, 4, VEC, TAIL>(p, bwd, s);
     }
+}
+
+template <typename T> int launch_vec(const Plan &p, bool bwd, hipStream_t s)
+{
+    if (p.vec == 1) return launch_k<T, 1, false>(p, bwd, s);        // fewer than four channels
+    return p.a.C % 4 ? launch_k<T, 4, true>(p, bwd, s) : launch_k<T, 4, false>(p, bwd, s);
 }
 
 int run(const cawn_conv_desc *d, const Plan &p, bool bwd, hipStream_t s)
 {
-    if (d->bf16) return p.vec > 1 ? launch_k<bf16, 4>(p, bwd, s) : launch_k<bf16, 1>(p, bwd, s);
-    return p.vec > 1 ? launch_k<float, 4>(p, bwd, s) : launch_k<float, 1>(p, bwd, s);
+    return d->bf16 ? launch_vec<bf16>(p, bwd, s) : launch_vec<float>(p, bwd, s);
 }
 
 } // namespace
@@ -405,33 +412,26 @@ extern "C" {
 size_t cawn_causal_conv_state_bytes(const cawn_conv_desc *d)
 {
     Plan p;
-    return plan_of(d, true, false, &p) != CAWN_OK ? 0 : (size_t)d->B * (d->k - 1) * d->C * 4;
+    return plan_of(d, false, &p) != CAWN_OK ? 0 : (size_t)d->B * (d->k - 1) * d->C * 4;
 }
 
 size_t cawn_causal_conv_workspace_bytes(const cawn_conv_desc *d)
 {
-    size_t most = 256;
-    for (int i = 0; i < 2; ++i) {
-        Plan p;
-        if (plan_of(d, i != 0, true, &p) != CAWN_OK) return 0;
-        most = most > part_bytes(p) ? most : part_bytes(p);
-    }
-    return most;
+    Plan p;
+    if (plan_of(d, true, &p) != CAWN_OK) return 0;
+    return part_bytes(p) > 256 ? part_bytes(p) : 256;
 }
 
 int cawn_causal_conv_fwd(const cawn_conv_desc *d, const void *x, const float *w, const float *bias, const int32_t *lengths, const void *state_in, void *y, void *state_out,
                          void *stream)
 {
     Plan p;
-    if (int r = plan_of(d, true, false, &p)) return r;
+    if (int r = plan_of(d, false, &p)) return r;
     const size_t e = d->bf16 ? 2 : 4;
     if (!aligned_to(x, e) || !aligned_to(y, e) || !aligned_to(w, 4) || !aligned_to(bias, 4) || !aligned_to(lengths, 4) || !aligned_to(state_in, 4) || !aligned_to(state_out, 4))
         return CAWN_EINVAL;
     if (d->B == 0) return CAWN_OK;
     if (!w || (d->L > 0 && (!x || !y))) return CAWN_EINVAL;
-    if (!aligned_to(x, 16) || !aligned_to(y, 16)) {
-        if (int r = plan_of(d, false, false, &p)) return r;
-    }
     p.a.x = x, p.a.w = w, p.a.bias = bias, p.a.lengths = lengths, p.a.state_in = (const float *)state_in, p.a.y = y, p.a.state_out = (float *)state_out;
     return run(d, p, false, (hipStream_t)stream);
 }
@@ -440,7 +440,7 @@ int cawn_causal_conv_bwd(const cawn_conv_desc *d, const void *x, const float *w,
                          const void *dstate_out, void *dx, float *dw, float *dbias, void *dstate_in, void *workspace, size_t workspace_bytes, void *stream)
 {
     Plan p;
-    if (int r = plan_of(d, true, true, &p)) return r;
+    if (int r = plan_of(d, true, &p)) return r;
     const size_t e = d->bf16 ? 2 : 4;
     if (!aligned_to(x, e) || !aligned_to(dy, e) || !aligned_to(dx, e) || !aligned_to(w, 4) || !aligned_to(bias, 4) || !aligned_to(lengths, 4) || !aligned_to(state_in, 4) ||
         !aligned_to(dstate_out, 4) || !aligned_to(dstate_in, 4) || !aligned_to(dw, 4) || !aligned_to(dbias, 4)) return CAWN_EINVAL;
@@ -452,9 +452,6 @@ int cawn_causal_conv_bwd(const cawn_conv_desc *d, const void *x, const float *w,
         return launched();
     }
     if (!w || (d->L > 0 && (!x || !dy))) return CAWN_EINVAL;
-    if (!aligned_to(x, 16) || !aligned_to(dy, 16) || !aligned_to(dx, 16)) {
-        if (int r = plan_of(d, false, true, &p)) return r;
-    }
     if (grads && (!workspace || workspace_bytes < part_bytes(p) || !aligned_to(workspace, 256))) return CAWN_EWORKSPACE;
     p.a.x = x, p.a.w = w, p.a.bias = bias, p.a.lengths = lengths, p.a.state_in = (const float *)state_in, p.a.dy = dy, p.a.dstate_out = (const float *)dstate_out;
     p.a.dx = dx, p.a.dstate_in = (float *)dstate_in, p.a.part = grads ? (float *)workspace : nullptr;

@@ -6,6 +6,7 @@
 // A row is in registers from its one read to its write: a run of 4 to 64 lanes holds it, or a workgroup of 256 to 1,024; the longest are read again.
 // Bound by memory.
 // The sum of squares is plain: all of its terms have one sign.
+#include "cawn_rows.hpp"
 #include "cawn_sums.hpp"
 
 using namespace cawn::ops;
@@ -26,29 +27,6 @@ struct RmsArgs {
 };
 
 constexpr float E4M3_MAX = 448.f;
-
-// N adjacent elements, 16 bytes an access at most
-template <typename T, int N> __device__ inline void read_n(const T *p, float (&x)[N])
-{
-    constexpr int W = N * sizeof(T) <= 16 ? N : 16 / sizeof(T);
-#pragma unroll
-    for (int i = 0; i < N; i += W) {
-        const Pack<T, W> a = *reinterpret_cast<const Pack<T, W> *>(p + i);
-#pragma unroll
-        for (int j = 0; j < W; ++j) x[i + j] = (float)a.v[j];
-    }
-}
-template <typename T, int N> __device__ inline void write_n(T *p, const float (&x)[N])
-{
-    constexpr int W = N * sizeof(T) <= 16 ? N : 16 / sizeof(T);
-#pragma unroll
-    for (int i = 0; i < N; i += W) {
-        Pack<T, W> a;
-#pragma unroll
-        for (int j = 0; j < W; ++j) a.v[j] = (T)x[i + j];
-        *reinterpret_cast<Pack<T, W> *>(p + i) = a;
-    }
-}
 
 __device__ inline float nan_max(float a, float b) { return a >= b || a != a ? a : b; }      // a NaN stays
 template <bool MAX> __device__ inline float two(float a, float b) { return MAX ? nan_max(a, b) : a + b; }
@@ -84,17 +62,24 @@ __device__ inline uint32_t e4m3_4(float a, float b, float c, float d)
 __device__ inline float scale_of(float m) { return m < E4M3_MAX * 1.17549435e-38f ? 0.f : m / E4M3_MAX; }
 
 // VEC values y of the type's 8 bits
-template <int VEC> __device__ inline void write_q(uint8_t *q, const float (&y)[VEC], float scale)
+template <int VEC> __device__ inline void write_q(uint8_t *q, const float (&y)[VEC], float scale, int skip)
 {
     float v[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) v[i] = scale == 0.f ? 0.f : y[i] / scale;
     if constexpr (VEC == 1) *q = (uint8_t)(e4m3_4(v[0], 0.f, 0.f, 0.f) & 0xff);
-    else if constexpr (VEC == 4) *reinterpret_cast<uint32_t *>(q) = e4m3_4(v[0], v[1], v[2], v[3]);
-    else *reinterpret_cast<uint2 *>(q) = make_uint2(e4m3_4(v[0], v[1], v[2], v[3]), e4m3_4(v[4], v[5], v[6], v[7]));
+    else {
+        Loose<uint32_t, VEC / 4> b;
+#pragma unroll
+        for (int i = 0; i < VEC; i += 4) b.v[i / 4] = e4m3_4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+        if (skip) {
+#pragma unroll
+            for (int i = 1; i < VEC; ++i)
+                if (i >= skip) q[i] = (uint8_t)(b.v[i / 4] >> i % 4 * 8);
+        } else *reinterpret_cast<Loose<uint8_t, VEC> *>(q) = __builtin_bit_cast(Loose<uint8_t, VEC>, b);
+    }
 }
 
-// VEC weights; they begin on 16 bytes where several values are taken at once
 template <int VEC> __device__ inline void read_w(const RmsArgs &a, int c, float (&w)[VEC])
 {
     if (a.w) read_n<float, VEC>(a.w + c, w);
@@ -127,19 +112,18 @@ template <int VEC> __device__ inline float largest(const float (&y)[VEC])
 }
 
 // X, R: types of x, y and of the residual stream.  WIDE: a row is the workgroup's.
-template <typename X, typename R, int VEC, int NIT, bool WIDE, int THREADS> __global__ __launch_bounds__(THREADS) void rms_forward(const RmsArgs a)
+template <typename X, typename R, int VEC, bool TAIL, int NIT, bool WIDE, int THREADS> __global__ __launch_bounds__(THREADS) void rms_forward(const RmsArgs a)
 {
     __shared__ float sh[WIDE ? THREADS / 64 : 1];
     __shared__ uint32_t most[THREADS * NIT * VEC / 16 + 256];     // maxima of the blocks, as the bits of values without a sign
     const int run = WIDE ? 0 : threadIdx.x / a.lpr, lane = WIDE ? threadIdx.x : threadIdx.x % a.lpr;
     const int step = WIDE ? THREADS : a.lpr;
     float w[NIT][VEC];
-    bool in[NIT];
+    Unit<VEC, TAIL> u[NIT];
 #pragma unroll
     for (int n = 0; n < NIT; ++n) {
-        const int c = (n * step + lane) * VEC;
-        in[n] = c < a.C;
-        read_w<VEC>(a, in[n] ? c : 0, w[n]);
+        u[n] = Unit<VEC, TAIL>(n * step + lane, a.C);
+        read_w<VEC>(a, u[n].c, w[n]);
     }
     const long long stride = (long long)gridDim.x * a.rpw;
     const float inv = 1.f / (float)a.C;
@@ -150,27 +134,27 @@ template <typename X, typename R, int VEC, int NIT, bool WIDE, int THREADS> __gl
         float h[NIT][VEC], s = 0.f;
 #pragma unroll
         for (int n = 0; n < NIT; ++n) {
-            read_h<X, R, VEC>(a, r, in[n] ? (n * step + lane) * VEC : 0, h[n]);
+            read_h<X, R, VEC>(a, r, u[n].c, h[n]);
+            u[n].own(h[n], u[n].in);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                h[n][i] = in[n] ? h[n][i] : 0.f;
-                s = fmaf(h[n][i], h[n][i], s);
-            }
+            for (int i = 0; i < VEC; ++i) s = fmaf(h[n][i], h[n][i], s);
         }
         const float rstd = 1.f / sqrtf(over_row<WIDE, false>(s, a.lpr, sh) * inv + a.eps);
         if (live && lane == 0 && a.rstd) a.rstd[r] = rstd;
 #pragma unroll
         for (int n = 0; n < NIT; ++n) {
-            const int c = (n * step + lane) * VEC;
-            if (live && in[n] && a.h) write_n<R, VEC>((R *)a.h + r * a.rs + c, h[n]);
+            if (live && u[n].in && a.h) write_n<R, VEC>((R *)a.h + r * a.rs + u[n].c, h[n], u[n].skip);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) h[n][i] = h[n][i] * rstd * w[n][i];
-            if (live && in[n] && a.y) write_n<X, VEC>((X *)a.y + r * a.ys + c, h[n]);
+            if (live && u[n].in && a.y) write_n<X, VEC>((X *)a.y + r * a.ys + u[n].c, h[n], u[n].skip);
         }
         if (!a.q) continue;
         float m[NIT];
 #pragma unroll
-        for (int n = 0; n < NIT; ++n) m[n] = in[n] ? largest<VEC>(h[n]) : 0.f;
+        for (int n = 0; n < NIT; ++n) {
+            u[n].own(h[n], u[n].in);       // (0 times an infinite weight or rstd is none)
+            m[n] = largest<VEC>(h[n]);
+        }
         if (a.block == 0) {
             float t = m[0];
 #pragma unroll
@@ -187,38 +171,37 @@ template <typename X, typename R, int VEC, int NIT, bool WIDE, int THREADS> __gl
             __syncthreads();
 #pragma unroll
             for (int n = 0; n < NIT; ++n) {
-                const int c = (n * step + lane) * VEC;      // (a block is a multiple of 16 channels: of VEC)
-                if (in[n] && live) atomicMax(&most[run * a.blocks + c / a.block], __float_as_uint(m[n]) & 0x7fffffffu);
+                // (a block is a multiple of 16 channels: of VEC)
+                if (u[n].in && live) atomicMax(&most[run * a.blocks + u[n].at / a.block], __float_as_uint(m[n]) & 0x7fffffffu);
             }
             __syncthreads();
 #pragma unroll
             for (int n = 0; n < NIT; ++n) {
-                const int c = (n * step + lane) * VEC;
-                if (in[n] && live) m[n] = __uint_as_float(most[run * a.blocks + c / a.block]);
+                if (u[n].in && live) m[n] = __uint_as_float(most[run * a.blocks + u[n].at / a.block]);
             }
         }
 #pragma unroll
         for (int n = 0; n < NIT; ++n) {
-            const int c = (n * step + lane) * VEC;
-            if (!live || !in[n]) continue;
+            if (!live || !u[n].in) continue;
             const float scale = scale_of(m[n]);
-            const int j = a.block ? c / a.block : 0;
-            if (c == j * a.block) a.scales[r * a.blocks + j] = scale;
-            write_q<VEC>(a.q + r * a.ys + c, h[n], scale);
+            const int j = a.block ? u[n].at / a.block : 0;
+            if (u[n].at == j * a.block) a.scales[r * a.blocks + j] = scale;
+            write_q<VEC>(a.q + r * a.ys + u[n].c, h[n], scale, u[n].skip);
         }
     }
 }
 
 // Rows that no workgroup's registers hold: read twice, three times where 8 bits are asked for.
-template <typename X, typename R, int VEC> __global__ __launch_bounds__(1024) void rms_forward_long(const RmsArgs a)
+template <typename X, typename R, int VEC, bool TAIL> __global__ __launch_bounds__(1024) void rms_forward_long(const RmsArgs a)
 {
     __shared__ float sh[16];
     __shared__ uint32_t most[2048];
     for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
         float s = 0.f;
-        for (int c = threadIdx.x * VEC; c < a.C; c += 1024 * VEC) {
+        for (Unit<VEC, TAIL> u(threadIdx.x, a.C); u.in; u = Unit<VEC, TAIL>(u.at / VEC + 1024, a.C)) {
             float h[VEC];
-            read_h<X, R, VEC>(a, r, c, h);
+            read_h<X, R, VEC>(a, r, u.c, h);
+            u.own(h, true);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) s = fmaf(h[i], h[i], s);
         }
@@ -227,35 +210,38 @@ template <typename X, typename R, int VEC> __global__ __launch_bounds__(1024) vo
         const int per = a.block ? a.block : a.C;
         float whole = 0.f;
         // (h or y may lie where x or the residual did: nothing is written before the last reading, and there by the thread that has read it)
-        auto norm = [&](int c, float(&h)[VEC]) {
+        auto norm = [&](const Unit<VEC, TAIL> &u, float(&h)[VEC]) {
+            float w[VEC];
+            read_w<VEC>(a, u.c, w);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) h[i] = h[i] * rstd * (a.w ? a.w[c + i] : 1.f);
+            for (int i = 0; i < VEC; ++i) h[i] = h[i] * rstd * w[i];
+            u.own(h, true);
         };
         if (a.q) {
             __syncthreads();
             for (int i = threadIdx.x; i < a.blocks; i += 1024) most[i] = 0;
             __syncthreads();
-            for (int c = threadIdx.x * VEC; c < a.C; c += 1024 * VEC) {
+            for (Unit<VEC, TAIL> u(threadIdx.x, a.C); u.in; u = Unit<VEC, TAIL>(u.at / VEC + 1024, a.C)) {
                 float h[VEC];
-                read_h<X, R, VEC>(a, r, c, h);
-                norm(c, h);
+                read_h<X, R, VEC>(a, r, u.c, h);
+                norm(u, h);
                 const float m = largest<VEC>(h);
-                if (a.block) atomicMax(&most[c / per], __float_as_uint(m) & 0x7fffffffu);
+                if (a.block) atomicMax(&most[u.at / per], __float_as_uint(m) & 0x7fffffffu);
                 else whole = nan_max(m, whole);
             }
             __syncthreads();
             if (!a.block) whole = over_row<true, true>(whole, 0, sh);
         }
-        for (int c = threadIdx.x * VEC; c < a.C; c += 1024 * VEC) {
+        for (Unit<VEC, TAIL> u(threadIdx.x, a.C); u.in; u = Unit<VEC, TAIL>(u.at / VEC + 1024, a.C)) {
             float h[VEC];
-            read_h<X, R, VEC>(a, r, c, h);
-            if (a.h) write_n<R, VEC>((R *)a.h + r * a.rs + c, h);
-            norm(c, h);
-            if (a.y) write_n<X, VEC>((X *)a.y + r * a.ys + c, h);
+            read_h<X, R, VEC>(a, r, u.c, h);
+            if (a.h) write_n<R, VEC>((R *)a.h + r * a.rs + u.c, h, u.skip);
+            norm(u, h);
+            if (a.y) write_n<X, VEC>((X *)a.y + r * a.ys + u.c, h, u.skip);
             if (a.q) {
-                const float scale = scale_of(a.block ? __uint_as_float(most[c / per]) : whole);
-                if (c % per == 0) a.scales[r * a.blocks + c / per] = scale;
-                write_q<VEC>(a.q + r * a.ys + c, h, scale);
+                const float scale = scale_of(a.block ? __uint_as_float(most[u.at / per]) : whole);
+                if (u.at % per == 0) a.scales[r * a.blocks + u.at / per] = scale;
+                write_q<VEC>(a.q + r * a.ys + u.c, h, scale, u.skip);
             }
         }
     }
@@ -271,28 +257,28 @@ template <typename X, typename R, int VEC> __device__ inline void read_back(cons
 }
 
 // dr of VEC values, into dx and dresidual
-template <typename X, typename R, int VEC> __device__ inline void write_back(const RmsArgs &a, long long r, int c, float rstd, float s, const float (&h)[VEC], const float (&t)[VEC])
+template <typename X, typename R, int VEC> __device__ inline void write_back(const RmsArgs &a, long long r, int c, float rstd, float s, const float (&h)[VEC], const float (&t)[VEC],
+                                                                                int skip)
 {
     float d[VEC];
     if (a.dh) read_n<R, VEC>((const R *)a.dh + r * a.rs + c, d);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) d[i] = fmaf(rstd, fmaf(-h[i], s, t[i]), a.dh ? d[i] : 0.f);
-    if (a.dx) write_n<X, VEC>((X *)a.dx + r * a.xs + c, d);
-    if (a.dres) write_n<R, VEC>((R *)a.dres + r * a.rs + c, d);
+    if (a.dx) write_n<X, VEC>((X *)a.dx + r * a.xs + c, d, skip);
+    if (a.dres) write_n<R, VEC>((R *)a.dres + r * a.rs + c, d, skip);
 }
 
-template <typename X, typename R, int VEC, int NIT, bool WIDE, int THREADS> __global__ __launch_bounds__(THREADS) void rms_backward(const RmsArgs a)
+template <typename X, typename R, int VEC, bool TAIL, int NIT, bool WIDE, int THREADS> __global__ __launch_bounds__(THREADS) void rms_backward(const RmsArgs a)
 {
     __shared__ float sh[WIDE ? THREADS / 64 : THREADS * NIT * VEC];
     const int run = WIDE ? 0 : threadIdx.x / a.lpr, lane = WIDE ? threadIdx.x : threadIdx.x % a.lpr;
     const int step = WIDE ? THREADS : a.lpr;
     float w[NIT][VEC], sw[NIT][VEC];
-    bool in[NIT];
+    Unit<VEC, TAIL> u[NIT];
 #pragma unroll
     for (int n = 0; n < NIT; ++n) {
-        const int c = (n * step + lane) * VEC;
-        in[n] = c < a.C;
-        read_w<VEC>(a, in[n] ? c : 0, w[n]);
+        u[n] = Unit<VEC, TAIL>(n * step + lane, a.C);
+        read_w<VEC>(a, u[n].c, w[n]);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) sw[n][i] = 0.f;
     }
@@ -305,11 +291,11 @@ template <typename X, typename R, int VEC, int NIT, bool WIDE, int THREADS> __gl
         float h[NIT][VEC], t[NIT][VEC], s = 0.f;
 #pragma unroll
         for (int n = 0; n < NIT; ++n) {
-            read_back<X, R, VEC>(a, r, in[n] ? (n * step + lane) * VEC : 0, rstd, h[n], t[n]);
+            read_back<X, R, VEC>(a, r, u[n].c, rstd, h[n], t[n]);
+            u[n].own(h[n], u[n].in && live);
+            u[n].own(t[n], u[n].in && live);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                h[n][i] = in[n] && live ? h[n][i] : 0.f;
-                t[n][i] = in[n] && live ? t[n][i] : 0.f;
                 sw[n][i] = fmaf(t[n][i], h[n][i], sw[n][i]);
                 t[n][i] *= w[n][i];
                 s = fmaf(t[n][i], h[n][i], s);
@@ -319,7 +305,7 @@ template <typename X, typename R, int VEC, int NIT, bool WIDE, int THREADS> __gl
         if (!live || (!a.dx && !a.dres)) continue;      // (the row's lanes all, and no barrier is left out: a workgroup's row is live)
 #pragma unroll
         for (int n = 0; n < NIT; ++n)
-            if (in[n]) write_back<X, R, VEC>(a, r, (n * step + lane) * VEC, rstd, s, h[n], t[n]);
+            if (u[n].in) write_back<X, R, VEC>(a, r, u[n].c, rstd, s, h[n], t[n], u[n].skip);
     }
     if (!a.part) return;
     float *out = a.part + (long long)blockIdx.x * a.C;
@@ -339,15 +325,12 @@ template <typename X, typename R, int VEC, int NIT, bool WIDE, int THREADS> __gl
     }
 #pragma unroll
     for (int n = 0; n < NIT; ++n) {
-        const int c = (n * step + lane) * VEC;
-        if (!in[n]) continue;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) out[c + i] = sw[n][i];
+        if (u[n].in) write_n<float, VEC>(out + u[n].c, sw[n], u[n].skip);
     }
 }
 
 // Rows that no workgroup's registers hold: read twice, the sums of dweight in the workspace.
-template <typename X, typename R, int VEC> __global__ __launch_bounds__(1024) void rms_backward_long(const RmsArgs a)
+template <typename X, typename R, int VEC, bool TAIL> __global__ __launch_bounds__(1024) void rms_backward_long(const RmsArgs a)
 {
     __shared__ float sh[16];
     float *part = a.part ? a.part + (long long)blockIdx.x * a.C : nullptr;
@@ -355,24 +338,27 @@ template <typename X, typename R, int VEC> __global__ __launch_bounds__(1024) vo
     for (long long r = blockIdx.x; r < a.rows; r += gridDim.x, first = false) {
         const float rstd = a.rstd_in[r];
         float s = 0.f;
-        for (int c = threadIdx.x * VEC; c < a.C; c += 1024 * VEC) {
-            float h[VEC], t[VEC];
-            read_back<X, R, VEC>(a, r, c, rstd, h, t);
+        for (Unit<VEC, TAIL> u(threadIdx.x, a.C); u.in; u = Unit<VEC, TAIL>(u.at / VEC + 1024, a.C)) {
+            float h[VEC], t[VEC], w[VEC], sum[VEC];
+            read_back<X, R, VEC>(a, r, u.c, rstd, h, t);
+            read_w<VEC>(a, u.c, w);
+            if (part && !first) read_n<float, VEC>(part + u.c, sum);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float g = t[i] * h[i];
-                if (part) part[c + i] = first ? g : part[c + i] + g;        // (the thread's own columns)
-                s = fmaf(g, a.w ? a.w[c + i] : 1.f, s);
-            }
+            for (int i = 0; i < VEC; ++i) h[i] *= t[i], t[i] = h[i] * w[i];
+            u.own(t, true);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) s += t[i], sum[i] = first ? h[i] : sum[i] + h[i];
+            if (part) write_n<float, VEC>(part + u.c, sum, u.skip);         // (the thread's own columns)
         }
         s = over_row<true, false>(s, 0, sh) / (float)a.C;
         if (!a.dx && !a.dres) continue;
-        for (int c = threadIdx.x * VEC; c < a.C; c += 1024 * VEC) {
-            float h[VEC], t[VEC];
-            read_back<X, R, VEC>(a, r, c, rstd, h, t);
+        for (Unit<VEC, TAIL> u(threadIdx.x, a.C); u.in; u = Unit<VEC, TAIL>(u.at / VEC + 1024, a.C)) {
+            float h[VEC], t[VEC], w[VEC];
+            read_back<X, R, VEC>(a, r, u.c, rstd, h, t);
+            read_w<VEC>(a, u.c, w);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) t[i] *= a.w ? a.w[c + i] : 1.f;
-            write_back<X, R, VEC>(a, r, c, rstd, s, h, t);
+            for (int i = 0; i < VEC; ++i) t[i] *= w[i];
+            write_back<X, R, VEC>(a, r, u.c, rstd, s, h, t, u.skip);
         }
     }
 }
@@ -390,8 +376,7 @@ struct Plan {
     long long blocks;
 };
 
-// The geometry must not depend on pointers: the workspace is sized without them.  Rows that do not begin on 16 bytes are taken value by value.
-int plan_of(const cawn_rms_desc *d, bool aligned, bool bwd, Plan *p)
+int plan_of(const cawn_rms_desc *d, bool bwd, Plan *p)
 {
     if (!d || d->rows < 0 || d->C <= 0 || (d->bf16 & ~1) || (d->residual_bf16 & ~1) || d->block < 0 || d->block % 16) return CAWN_EINVAL;
     if (d->C > 32768) return CAWN_EUNSUPPORTED;
@@ -402,8 +387,8 @@ int plan_of(const cawn_rms_desc *d, bool aligned, bool bwd, Plan *p)
     if (a.xs < a.C || a.rs < a.C || a.ys < a.C) return CAWN_EINVAL;
     a.block = d->block >= d->C ? 0 : d->block;
     a.blocks = a.block ? (int)ceil_div(a.C, a.block) : 1;
-    const int most = d->bf16 ? 8 : 4, each = d->bf16 || d->residual_bf16 ? 8 : 4;       // (strides of the narrower type)
-    p->vec = aligned && a.C % most == 0 && a.xs % each == 0 && a.rs % each == 0 && a.ys % each == 0 ? most : 1;
+    const int most = d->bf16 ? 8 : 4;
+    p->vec = a.C >= most ? most : 1;
     const int units = (int)ceil_div(a.C, p->vec);
     p->wide = units > 192;
     p->held = true;
@@ -415,13 +400,13 @@ int plan_of(const cawn_rms_desc *d, bool aligned, bool bwd, Plan *p)
                 if (lanes * nit >= units && lanes * nit < best) best = lanes * nit, a.lpr = lanes, p->nit = nit;
         p->threads = 256;
         a.rpw = 256 / a.lpr;
-    } else {        // 16 values a thread at most, 8 where they come one by one
-        const int top = p->vec == 8 ? 2 : p->vec == 4 ? 4 : 8;
+    } else {        // 16 values a thread at most
+        const int top = 16 / p->vec;
         p->threads = units <= 256 * top ? 256 : units <= 512 * top ? 512 : 1024;
         p->held = units <= 1024 * top;
         a.lpr = p->threads, a.rpw = 1;
         const int nit = (int)ceil_div(units, p->threads);
-        p->nit = nit <= 1 ? 1 : nit <= 2 ? 2 : nit <= 4 ? 4 : 8;
+        p->nit = nit <= 1 ? 1 : nit <= 2 ? 2 : 4;
     }
     a.lpb = 0;
     if (a.block) {
@@ -436,44 +421,47 @@ int plan_of(const cawn_rms_desc *d, bool aligned, bool bwd, Plan *p)
     return CAWN_OK;
 }
 
-template <typename X, typename R, int VEC, int NIT, bool WIDE, int THREADS> void go(const Plan &p, bool bwd, hipStream_t s)
+template <typename X, typename R, int VEC, bool TAIL, int NIT, bool WIDE, int THREADS> void go(const Plan &p, bool bwd, hipStream_t s)
 {
-    if (bwd) hipLaunchKernelGGL((rms_backward<X, R, VEC, NIT, WIDE, THREADS>), dim3((unsigned)p.blocks), dim3(THREADS), 0, s, p.a);
-    else hipLaunchKernelGGL((rms_forward<X, R, VEC, NIT, WIDE, THREADS>), dim3((unsigned)p.blocks), dim3(THREADS), 0, s, p.a);
+    if (bwd) hipLaunchKernelGGL((rms_backward<X, R, VEC, TAIL, NIT, WIDE, THREADS>), dim3((unsigned)p.blocks), dim3(THREADS), 0, s, p.a);
+    else hipLaunchKernelGGL((rms_forward<X, R, VEC, TAIL, NIT, WIDE, THREADS>), dim3((unsigned)p.blocks), dim3(THREADS), 0, s, p.a);
 }
 
-template <typename X, typename R, int VEC, int THREADS> void go_wide(const Plan &p, bool bwd, hipStream_t s)
+template <typename X, typename R, int VEC, bool TAIL, int THREADS> void go_wide(const Plan &p, bool bwd, hipStream_t s)
 {
-    constexpr int TOP = VEC == 8 ? 2 : VEC == 4 ? 4 : 8;
-    if (p.nit == 1) go<X, R, VEC, 1, true, THREADS>(p, bwd, s);
-    else if (p.nit == 2) go<X, R, VEC, 2, true, THREADS>(p, bwd, s);
-    else if (p.nit == 4) go<X, R, VEC, TOP < 4 ? TOP : 4, true, THREADS>(p, bwd, s);
-    else go<X, R, VEC, TOP, true, THREADS>(p, bwd, s);
+    if (p.nit == 1) go<X, R, VEC, TAIL, 1, true, THREADS>(p, bwd, s);
+    else if (p.nit == 2) go<X, R, VEC, TAIL, 2, true, THREADS>(p, bwd, s);
+    else go<X, R, VEC, TAIL, 16 / VEC, true, THREADS>(p, bwd, s);
 }
 
-template <typename X, typename R, int VEC> int launch(const Plan &p, bool bwd, hipStream_t s)
+template <typename X, typename R, int VEC, bool TAIL> int launch(const Plan &p, bool bwd, hipStream_t s)
 {
     if (!p.wide) {
-        if (p.nit == 1) go<X, R, VEC, 1, false, 256>(p, bwd, s);
-        else if (p.nit == 2) go<X, R, VEC, 2, false, 256>(p, bwd, s);
-        else go<X, R, VEC, 3, false, 256>(p, bwd, s);
+        if (p.nit == 1) go<X, R, VEC, TAIL, 1, false, 256>(p, bwd, s);
+        else if (p.nit == 2) go<X, R, VEC, TAIL, 2, false, 256>(p, bwd, s);
+        else go<X, R, VEC, TAIL, 3, false, 256>(p, bwd, s);
     } else if (!p.held) {
-        if (bwd) hipLaunchKernelGGL((rms_backward_long<X, R, VEC>), dim3((unsigned)p.blocks), dim3(1024), 0, s, p.a);
-        else hipLaunchKernelGGL((rms_forward_long<X, R, VEC>), dim3((unsigned)p.blocks), dim3(1024), 0, s, p.a);
-    } else if (p.threads == 256) go_wide<X, R, VEC, 256>(p, bwd, s);
-    else if (p.threads == 512) go_wide<X, R, VEC, 512>(p, bwd, s);
-    else go_wide<X, R, VEC, 1024>(p, bwd, s);
+        if (bwd) hipLaunchKernelGGL((rms_backward_long<X, R, VEC, TAIL>), dim3((unsigned)p.blocks), dim3(1024), 0, s, p.a);
+        else hipLaunchKernelGGL((rms_forward_long<X, R, VEC, TAIL>), dim3((unsigned)p.blocks), dim3(1024), 0, s, p.a);
+    } else if (p.threads == 256) go_wide<X, R, VEC, TAIL, 256>(p, bwd, s);
+    else if (p.threads == 512) go_wide<X, R, VEC, TAIL, 512>(p, bwd, s);
+    else go_wide<X, R, VEC, TAIL, 1024>(p, bwd, s);
     return launched();
+}
+
+template <typename X, typename R, int VEC> int launch_tail(const Plan &p, bool bwd, hipStream_t s)
+{
+    if (p.vec == 1) {           // fewer channels than VEC
+        go<X, R, 1, false, 1, false, 256>(p, bwd, s);
+        return launched();
+    }
+    return p.a.C % VEC ? launch<X, R, VEC, true>(p, bwd, s) : launch<X, R, VEC, false>(p, bwd, s);
 }
 
 int run(const cawn_rms_desc *d, const Plan &p, bool bwd, hipStream_t s)
 {
-    if (d->bf16) {
-        if (d->residual_bf16) return p.vec > 1 ? launch<bf16, bf16, 8>(p, bwd, s) : launch<bf16, bf16, 1>(p, bwd, s);
-        return p.vec > 1 ? launch<bf16, float, 8>(p, bwd, s) : launch<bf16, float, 1>(p, bwd, s);
-    }
-    if (d->residual_bf16) return p.vec > 1 ? launch<float, bf16, 4>(p, bwd, s) : launch<float, bf16, 1>(p, bwd, s);
-    return p.vec > 1 ? launch<float, float, 4>(p, bwd, s) : launch<float, float, 1>(p, bwd, s);
+    if (d->bf16) return d->residual_bf16 ? launch_tail<bf16, bf16, 8>(p, bwd, s) : launch_tail<bf16, float, 8>(p, bwd, s);
+    return d->residual_bf16 ? launch_tail<float, bf16, 4>(p, bwd, s) : launch_tail<float, float, 4>(p, bwd, s);
 }
 
 } // namespace
@@ -482,29 +470,23 @@ extern "C" {
 
 size_t cawn_rms_norm_add_workspace_bytes(const cawn_rms_desc *d)
 {
-    size_t most = 0;
-    for (int i = 0; i < 2; ++i) {
-        Plan p;
-        if (plan_of(d, i != 0, true, &p) != CAWN_OK) return 0;
-        const size_t bytes = (size_t)p.blocks * p.a.C * 4;
-        most = most > bytes ? most : bytes;
-    }
-    return most > 256 ? most : 256;
+    Plan p;
+    if (plan_of(d, true, &p) != CAWN_OK) return 0;
+    const size_t bytes = (size_t)p.blocks * p.a.C * 4;
+    return bytes > 256 ? bytes : 256;
 }
 
 int cawn_rms_norm_add_fwd(const cawn_rms_desc *d, const void *x, const void *residual, const float *weight, void *h, void *y, void *q, float *scales, float *rstd,
                           void *stream)
 {
     Plan p;
-    if (int r = plan_of(d, true, false, &p)) return r;
+    if (int r = plan_of(d, false, &p)) return r;
     const size_t e = d->bf16 ? 2 : 4, f = d->residual_bf16 ? 2 : 4;
     if (!aligned_to(x, e) || !aligned_to(y, e) || !aligned_to(residual, f) || !aligned_to(h, f) || !aligned_to(weight, 4) || !aligned_to(scales, 4) || !aligned_to(rstd, 4))
         return CAWN_EINVAL;
     if ((y == nullptr && q == nullptr) || (q == nullptr) != (scales == nullptr)) return CAWN_EINVAL;
     if (d->rows == 0) return CAWN_OK;
     if (!x) return CAWN_EINVAL;
-    if (!aligned_to(x, 16) || !aligned_to(y, 16) || !aligned_to(residual, 16) || !aligned_to(h, 16) || !aligned_to(q, 8) || !aligned_to(weight, 16))
-        plan_of(d, false, false, &p);
     p.a.x = x, p.a.res = residual, p.a.w = weight, p.a.h = h, p.a.y = y, p.a.q = (uint8_t *)q, p.a.scales = scales, p.a.rstd = rstd;
     return run(d, p, false, (hipStream_t)stream);
 }
@@ -513,7 +495,7 @@ int cawn_rms_norm_add_bwd(const cawn_rms_desc *d, const void *h, const float *we
                           float *dweight, void *workspace, size_t workspace_bytes, void *stream)
 {
     Plan p;
-    if (int r = plan_of(d, true, true, &p)) return r;
+    if (int r = plan_of(d, true, &p)) return r;
     const size_t e = d->bf16 ? 2 : 4, f = d->residual_bf16 ? 2 : 4;
     if (!aligned_to(h, f) || !aligned_to(dh, f) || !aligned_to(dresidual, f) || !aligned_to(dy, e) || !aligned_to(dx, e) || !aligned_to(weight, 4) || !aligned_to(rstd, 4) ||
         !aligned_to(dweight, 4)) return CAWN_EINVAL;
@@ -524,8 +506,6 @@ int cawn_rms_norm_add_bwd(const cawn_rms_desc *d, const void *h, const float *we
     }
     if (!h || !rstd || !dy) return CAWN_EINVAL;
     if (!dx && !dresidual && !dweight) return CAWN_OK;
-    if (!aligned_to(h, 16) || !aligned_to(dh, 16) || !aligned_to(dresidual, 16) || !aligned_to(dy, 16) || !aligned_to(dx, 16) || !aligned_to(weight, 16))
-        plan_of(d, false, true, &p);
     if (dweight && (!workspace || workspace_bytes < (size_t)p.blocks * p.a.C * 4 || !aligned_to(workspace, 256))) return CAWN_EWORKSPACE;
     p.a.x = h, p.a.w = weight, p.a.rstd_in = rstd, p.a.dy = dy, p.a.dh = dh, p.a.dx = dx, p.a.dres = dresidual, p.a.part = dweight ? (float *)workspace : nullptr;
     if (int r = run(d, p, true, s)) return r;

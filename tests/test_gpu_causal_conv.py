@@ -210,3 +210,31 @@ def test_captured_and_replayed():
         assert torch.equal(c.y, want.y) and torch.equal(c.state_out, want.state_out)
         assert all(torch.equal(g[n], want.g[n]) for n in g)
         torch.ones(1000, device=DEV).sum()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("k", [1, 2, 3, 4])
+def test_every_end_of_a_row(k, bf16):
+    """Widths one after the other: units of one to four channels at the end, rows of fewer than four."""
+    for C in [*range(1, 14), 129, 130, 131]:
+        i = _inputs(5, 37, C, k, bf16, seed=C, ragged=True)
+        c = Conv(i, 1, bf16, (0, 3), offset=1).forward().backward()
+        torch.cuda.synchronize()
+        _compare(c, i, 1, bf16)
+        assert untouched(c.y, 3)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("B,L,C", [(70, 1, 1027), (9, 40, 769), (33, 2, 258), (5, 0, 7)])
+def test_state_in_place_at_widths_that_end_inside_a_unit(B, L, C, bf16):
+    """The last channels of a row are read together with some that stand before them, whose state another thread replaces."""
+    i = _inputs(B, L, C, 4, bf16, seed=8)
+    i["lengths"] = np.asarray([(b * 7) % (L + 2) for b in range(B)], np.int32)
+    c, d = (Conv(i, 1, bf16) for _ in range(2))
+    c.forward().backward()
+    d.forward(state_in=d.state_in, state_out=d.state_in)
+    assert torch.equal(c.y, d.y) and torch.equal(c.state_out, d.state_in)
+    d.state_in.copy_(c.state_in)
+    d.backward(dstate="in place")
+    for n, g in c.g.items():
+        assert torch.equal(g, d.g[n]), n

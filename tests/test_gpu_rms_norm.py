@@ -196,3 +196,45 @@ def test_rows_far_apart():
     K.check(K.cawn_rms_norm_add_bwd(d, h, a.w, rstd, y, None, x, None, dw, a.ws))
     b = Rms(2, C, True, True, seed=8).forward().backward(dh=False)
     assert torch.equal(x, b.g["x"]) and torch.equal(dw, b.g["w"])
+
+
+@pytest.mark.parametrize("bf16,res_bf16", [(False, False), (True, False), (True, True), (False, True)])
+@pytest.mark.parametrize("C", [3, 7, 13, 97, 1001, 1541, 4093, 8190, 9001, 16385, 20001])
+def test_in_place_at_widths_that_end_inside_a_unit(C, bf16, res_bf16):
+    """The last channels of a row are read together with some that stand before them, which another thread replaces."""
+    s = Rms(37, C, bf16, res_bf16, seed=9).forward().backward()
+    t = Rms(37, C, bf16, res_bf16, seed=9)
+    K.check(K.cawn_rms_norm_add_fwd(t.d, t.x, t.res, t.w, t.res, t.x, None, None, t.rstd))
+    assert torch.equal(t.res, s.h) and torch.equal(t.x, s.y) and torch.equal(t.rstd, s.rstd)
+    dw = torch.empty(C, device=DEV)
+    K.check(K.cawn_rms_norm_add_bwd(t.d, t.res, t.w, t.rstd, t.dy, t.dh, t.dy, t.dh, dw, t.ws))
+    assert torch.equal(t.dy, s.g["x"]) and torch.equal(t.dh, s.g["res"]) and torch.equal(dw, s.g["w"])
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("block", [0, 16, 32])
+def test_every_end_of_a_row(block, bf16):
+    """Widths one after the other: units of all lengths at the end, blocks of one channel and of sixteen."""
+    for C in [*range(1, 50), *range(1530, 1546)]:
+        s = Rms(5, C, bf16, bf16, seed=C, block=block, extra=(0, 0, 3), offset=1).forward(q=True).backward()
+        torch.cuda.synchronize()
+        h = s.held()
+        assert np.array_equal(host(s.h), h)
+        assert rel_err(host(s.y), R.rms_fwd(h, host(s.w))[0]) <= (TOL16 if bf16 else TOL)
+        d, dw = R.rms_bwd(h, host(s.dy), host(s.w), host(s.dh))
+        assert rel_err(host(s.g["x"]), d) <= (TOL16 if bf16 else TOL) and rel_err(host(s.g["w"]), dw) <= TOLSUM
+        assert untouched(s.y, 3) and bool((s.q[1:].view(5, C + 3)[:, C:] == 0x55).all())
+        _check_q(s, h)
+
+
+@pytest.mark.parametrize("C", [21, 1001, 20001])
+def test_an_infinite_weight_stays_in_its_channel(C):
+    s = Rms(3, C, False, False, seed=11, block=16)
+    s.w[C - 6] = float("inf")       # read by the thread of the last channels too
+    s.forward(q=True)
+    t = Rms(3, C, False, False, seed=11, block=16).forward(q=True)
+    torch.cuda.synchronize()
+    there = torch.arange(C, device=DEV) != C - 6
+    assert bool(torch.isinf(s.y[:, C - 6]).all()) and torch.equal(s.y[:, there], t.y[:, there])
+    blocks = torch.arange(s.nb, device=DEV) != (C - 6) // 16
+    assert torch.equal(s.scales[:, blocks], t.scales[:, blocks]) and bool(torch.isinf(s.scales[:, (C - 6) // 16]).all())
