@@ -349,10 +349,14 @@ int plan_of(const cawn_conv_desc *d, bool bwd, Plan *p)
     a.xsb = d->x_stride_b ? d->x_stride_b : a.xst * d->L, a.ysb = d->y_stride_b ? d->y_stride_b : a.yst * d->L;
     p->vec = a.C >= 4 ? 4 : 1;
     a.units = (int)ceil_div(a.C, p->vec);
-    // Tokens of a run: a longer one reads fewer tokens twice, where as many threads are left as the chip holds.  (8 x 8,192 tokens of 768 channels in bf16,
-    // forward and backward, us: runs of 32 and 64 109, 16 and 64 111, 32 and 32 118, 16 and 16 144.)
+    // Tokens of a run: a longer one reads fewer tokens twice, where as many threads are left as the chip holds; the shortest, where each waits for its loads
+    // alone, for calls of few threads, whose partial sums are few too.  (Forward and backward, us: 8 x 8,192 tokens of 768 channels in bf16 with runs of 32 and
+    // 64 112, 16 and 16 144; 8 x 4,096 with 32 and 32 58, 32 and 64 70; 2 x 512 with 16, 8 and 4 backward 23.6, 19.6, 16.8; 16 x 2,000 of 200 in fp32 with
+    // 16 and 8 38, 46: the sums.)
     a.run = bwd ? 64 : 32;
-    while (a.run > (bwd ? 16 : 8) && ceil_div(a.L, a.run) * a.B * a.units < 1 << (bwd ? 16 : 17)) a.run /= 2;
+    auto threads = [&] { return ceil_div(a.L, a.run) * a.B * a.units; };
+    while (a.run > (bwd ? 16 : 8) && threads() < 1 << (bwd ? 17 : 18)) a.run /= 2;
+    while (a.run > 4 && bwd && threads() < 1 << 15) a.run /= 2;
     a.runs = a.L > 0 ? ceil_div(a.L, a.run) : 1;
     const long long all = a.runs * a.B;
     if (all > (1LL << 40) / a.units) return CAWN_EUNSUPPORTED;
