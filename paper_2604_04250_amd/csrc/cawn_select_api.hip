@@ -9,19 +9,27 @@ using cawn::select::TILE;
 namespace {
 
 // How a row's tiles are cut into segments.  Each but the last costs its tokens twice, whatever their number, and one link of the chain; more of them fill the
-// chip and even out its rounds.  `waves` in all, three or four rounds of what the chip holds; beyond 64 segments, where the chain costs more than the rounds gain,
-// half of that.
+// chip and even out its rounds.
+// One segment: where its waves fill the chip alone, or rows are so short that the passes over segments cost more than a wave's way along the row.  For each wave
+// on a SIMD (1,024 in all) a pass over segments takes 0.45 us a token, backward 1.05; a wave alone takes 0.38 for its way, two on a SIMD 0.57, backward 1.0 and
+// 1.6: they are even at 890 and 1,300 waves, 980 and 1,560.  What else segments cost, launches and the chain, is as long as 48 tokens, backward 24.  (us, cut and
+// in one: 64 x 256 tokens of 1,024 channels 145, 102, training 463, 368; 64 x 32 43, 21, training 106, 68; 16 x 64 29, 30, training 76, 103; 64 x 1,000 of 4,096
+// channels 1,577, 933; 16 x 1,024 of 2,048 channels 232, 379.)
+// Else 8,192 waves in all, backward 6,144, three or four rounds of what the chip holds; beyond 64 segments, where the chain costs more than the rounds gain,
+// half of that, and two tiles rather than one where that leaves 4,096 (4 x 512 tokens of 4,096 channels 88, 80).
 // (us a pass for 4,096, 6,144, 8,192 and 16,384 waves, forward: 2 x 32,768 tokens of 4,096 channels 1,790, 1,720, 1,660, 1,637, training 8 x 8,192 of 768
 // channels 1,326, 1,290, 1,296, 1,292; backward, 2,048, 4,096, 6,144, 8,192 and 12,288: the latter 1,326, 1,306, 1,241, 1,287, 1,251.)
-void cut(Args *a, long long waves)
+void cut(Args *a, bool bwd)
 {
-    const long long columns = (long long)a->B * a->G * a->cbg * (a->NB > 1 ? a->NB : a->wide);
+    const long long columns = (long long)a->B * a->G * a->cbg * (a->NB > 1 ? a->NB : a->wide), waves = bwd ? 6144 : 8192;
+    const long long even = columns <= 1024 ? (bwd ? 980 : 890) : bwd ? 1560 : 1300;
+    a->segments = 1, a->seg_tiles = a->tiles > 0 ? a->tiles : 1;
+    if (a->tiles < 2 || columns >= even || (long long)a->L * (even - columns) <= even * (bwd ? 24 : 48)) return;
     long long want = columns > 0 ? waves / columns : 1;
     if (want > 64) want = waves / 2 / columns > 64 ? waves / 2 / columns : 64;
     if (want > select::SEGMENTS_MAX) want = select::SEGMENTS_MAX;
-    a->segments = 1, a->seg_tiles = a->tiles > 0 ? a->tiles : 1;
-    if (want < 2 || a->tiles < 2) return;
     a->seg_tiles = (int)ceil_div(a->tiles, want);
+    if (a->seg_tiles == 1 && columns * (a->tiles / 2) >= 4096) a->seg_tiles = 2;
     a->segments = (int)ceil_div(a->tiles, a->seg_tiles);
 }
 
@@ -59,7 +67,7 @@ int check(const cawn_scan_desc *d, bool bwd, Args *a)
     if (d->D > wide || a->xst > wide || a->dst > wide || a->zst > wide || a->yst > wide || d->L > 1 << 30 || (long long)a->cpg * G > 1 << 24) return CAWN_EUNSUPPORTED;
     a->Dp = a->cpg * G * 64;
     a->tiles = (int)ceil_div(d->L, TILE);
-    cut(a, bwd ? 6144 : 8192);
+    cut(a, bwd);
     return too_many(*a) ? CAWN_EUNSUPPORTED : CAWN_OK;
 }
 
