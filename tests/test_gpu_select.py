@@ -321,3 +321,29 @@ def test_rows_far_apart():
     K.check(K.cawn_selective_scan_bwd(s.d, s.x, s.dt, s.A, s.Bm, s.Cm, s.Dk, s.z, s.bias, None, s.ckpt, s.dy, s.dstate_out, dx, None, None, None, None, None, None, None, None,
                                       s.ws))
     assert torch.equal(dx, base.g["x"])
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_rows_of_a_batch_that_fills_the_chip_are_the_rows_by_themselves(bf16):
+    """60 rows of 16 columns of channels go along their rows at once, a row by itself is cut into segments."""
+    B, L, D, N = 60, 75, 1024, 16
+    i = scan_inputs(B, L, D, N, 1, bf16, seed=77, ragged=True)
+    s = Scan(i, bf16).forward().backward()
+    torch.cuda.synchronize()
+    whole, sums = s.grads(), {}
+    tol, tol32 = 2 * tolerance(L, bf16), 2 * tolerance(L, False)        # (both are off)
+    for b in range(B):
+        row = {k: v if v is None or k in ("A", "Dk", "bias") else v[b:b + 1] for k, v in i.items()}
+        t = Scan(row, bf16).forward().backward()
+        torch.cuda.synchronize()
+        if i["lengths"][b]:
+            assert rel_err(s.y[b].float().cpu(), t.y[0].float().cpu()) <= tol and rel_err(s.state_out[b].cpu(), t.state_out[0].cpu()) <= tol32
+        else:
+            assert torch.equal(s.y[b], t.y[0]) and torch.equal(s.state_out[b], t.state_out[0])
+        for n, g in t.grads().items():
+            if n in ("dA", "dDskip", "ddt_bias"):
+                sums[n] = sums.get(n, 0) + g.astype(np.float64)
+            elif i["lengths"][b]:
+                assert rel_err(whole[n][b], g[0]) <= (tol32 if n == "dstate_in" else tol), (n, b)
+    for n, g in sums.items():
+        assert rel_err(whole[n], g) <= tol32, n
