@@ -5,6 +5,8 @@
 // A lane owns a channel, a wave 64 of them and up to 16 of their states: B and C, which the channels share, then come by scalar loads and are
 // operands of the vector instructions as they stand.  More than 16 states are shared out over the waves of a workgroup.
 #pragma once
+#include <type_traits>
+
 #include "cawn_sums.hpp"
 
 namespace cawn {
@@ -33,7 +35,7 @@ struct Args {
     const float *dstate_out;
     void *dx, *ddt, *dB, *dC, *dz;
     float *dstate_in;
-    // Geometry of the tiled form: states of a wave (4, 8 or 16) and waves that share a channel's (1, 2, 4, 8); columns of 64 channels in a group, of which a
+    // Geometry of the tiled form: states of a wave (4, 8, 12 or 16) and waves that share a channel's (1, 2, 4, 8); columns of 64 channels in a group, of which a
     // workgroup takes `wide`, and workgroups for a group; Dp = 64 x columns; tiles of a full row, segments of them
     int NP, NB, cpg, wide, cbg;
     int Dp, tiles, segments, seg_tiles;
@@ -81,6 +83,21 @@ int launch_forward(const Args &a, bool bf16, hipStream_t s);
 int launch_join(const Args &a, bool reverse, hipStream_t s);
 int launch_backward(const Args &a, bool bf16, hipStream_t s);       // behind it launch_bc
 int launch_bc_sums(const Args &a, bool bf16, hipStream_t s);
+
+// f(states of a wave, waves that share a channel's), as types
+template <typename F> void by_states(const Args &a, F f)
+{
+    auto waves = [&](auto nb) {
+        if (a.NP == 12) f(std::integral_constant<int, 12>(), nb);
+        else f(std::integral_constant<int, 16>(), nb);
+    };
+    if (a.NB == 8) waves(std::integral_constant<int, 8>());
+    else if (a.NB == 4) waves(std::integral_constant<int, 4>());
+    else if (a.NB == 2) waves(std::integral_constant<int, 2>());
+    else if (a.NP == 8) f(std::integral_constant<int, 8>(), std::integral_constant<int, 1>());
+    else if (a.NP == 4) f(std::integral_constant<int, 4>(), std::integral_constant<int, 1>());
+    else waves(std::integral_constant<int, 1>());
+}
 
 // ---------------------------------------------------------------------------------------------- the tiled kernels' common parts
 // Where a wave of the tiled form is.

@@ -56,8 +56,8 @@ int check(const cawn_scan_desc *d, bool bwd, Args *a)
     a->xsb = d->x_stride_b ? d->x_stride_b : a->xst * d->L, a->dsb = d->dt_stride_b ? d->dt_stride_b : a->dst * d->L;
     a->bsb = d->bc_stride_b ? d->bc_stride_b : a->bst * d->L, a->zsb = d->z_stride_b ? d->z_stride_b : a->zst * d->L;
     a->ysb = d->y_stride_b ? d->y_stride_b : a->yst * d->L;
-    a->NP = d->N <= 4 ? 4 : d->N <= 8 ? 8 : 16;
     a->NB = d->N <= 16 ? 1 : d->N <= 32 ? 2 : d->N <= 64 ? 4 : 8;
+    a->NP = (int)ceil_div(ceil_div(d->N, a->NB), 4) * 4;
     a->cpg = (int)ceil_div(a->cg, 64);
     a->wide = a->NB > 1 ? 1 : a->cpg < 4 ? a->cpg : 4;
     a->cbg = (int)ceil_div(a->cpg, a->wide);

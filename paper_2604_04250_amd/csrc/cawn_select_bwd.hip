@@ -470,12 +470,7 @@ template <typename T, int NP, int NB> static void launch_np(const Args &a, hipSt
 
 template <typename T> static int launch(const Args &a, hipStream_t s)
 {
-    if (a.NB == 8) launch_np<T, 16, 8>(a, s);
-    else if (a.NB == 4) launch_np<T, 16, 4>(a, s);
-    else if (a.NB == 2) launch_np<T, 16, 2>(a, s);
-    else if (a.NP == 16) launch_np<T, 16, 1>(a, s);
-    else if (a.NP == 8) launch_np<T, 8, 1>(a, s);
-    else launch_np<T, 4, 1>(a, s);
+    by_states(a, [&](auto np, auto nb) { launch_np<T, decltype(np)::value, decltype(nb)::value>(a, s); });
     return launched();
 }
 

@@ -347,3 +347,17 @@ def test_rows_of_a_batch_that_fills_the_chip_are_the_rows_by_themselves(bf16):
                 assert rel_err(whole[n][b], g[0]) <= (tol32 if n == "dstate_in" else tol), (n, b)
     for n, g in sums.items():
         assert rel_err(whole[n], g) <= tol32, n
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("N", [9, 11, 12, 17, 20, 24, 33, 40, 48, 65, 70, 96])
+def test_states_that_waves_share_in_twelves(N, bf16):
+    B, L, D, G = 2, 150, 74, 2
+    i = scan_inputs(B, L, D, N, G, bf16, seed=N, ragged=True)
+    s = Scan(i, bf16).forward().backward()
+    torch.cuda.synchronize()
+    y, state = R.scan_fwd(**reference_inputs(i))
+    assert rel_err(s.y.float().cpu(), y) <= tolerance(L, bf16) and rel_err(s.state_out.cpu(), state) <= tolerance(L, False)
+    ref, got = R.scan_bwd(dy=i["dy"], dstate_out=i["dstate_out"], **reference_inputs(i)), s.grads()
+    for n, r in ref.items():
+        assert rel_err(got[n], r) <= tolerance(L, bf16 and n in ("dx", "ddt", "dBm", "dCm", "dz")), n
