@@ -176,7 +176,7 @@ template <int K, int VEC> __device__ inline void slope(const ConvArgs &a, const 
 
 template <typename T, int K, int VEC, bool TAIL> __global__ __launch_bounds__(256) void conv_backward(const ConvArgs a)
 {
-    __shared__ float sh[256 * VEC];
+    __shared__ float sh[(K + 1) * VEC * 256];
     const int unit = threadIdx.x % a.ub, row = threadIdx.x / a.ub;
     const long long rblk = blockIdx.x / a.ublocks;
     const Unit<VEC, TAIL> u((int)(blockIdx.x - rblk * a.ublocks) * a.ub + unit, a.C);
@@ -263,22 +263,21 @@ template <typename T, int K, int VEC, bool TAIL> __global__ __launch_bounds__(25
         }
     }
     if (!a.part) return;
-    // the workgroup's runs, in their order: [K + 1][C] a workgroup
+    // [K + 1][C] a workgroup
+    float sums[(K + 1) * VEC];
 #pragma unroll
-    for (int i = 0; i <= K; ++i) {
-        __syncthreads();
+    for (int j = 0; j < VEC; ++j) {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) sh[threadIdx.x * VEC + j] = i < K ? dw[i < K ? i : 0][j] : db[j];
-        __syncthreads();
-        if (row == 0 && u.in) {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                float v = 0.f;
-                for (int q = 0; q < a.rb; ++q) v += sh[(q * a.ub + unit) * VEC + j];
-                if (j >= skip) a.part[(rblk * (K + 1) + i) * a.C + c + j] = v;
-            }
-        }
+        for (int i = 0; i < K; ++i) sums[i * VEC + j] = dw[i][j];
+        sums[K * VEC + j] = db[j];
     }
+    over_runs<256>(sums, a.rb, a.ub, sh);
+    if (row > 0 || !u.in) return;
+#pragma unroll
+    for (int i = 0; i <= K; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+            if (j >= skip) a.part[(rblk * (K + 1) + i) * a.C + c + j] = sums[i * VEC + j];
 }
 
 // The gradient of the state before the row alone, where it takes the place of that behind the row, which the other workgroups read: what its first

@@ -310,19 +310,14 @@ template <typename X, typename R, int VEC, bool TAIL, int NIT, bool WIDE, int TH
     }
     if (!a.part) return;
     float *out = a.part + (long long)blockIdx.x * a.C;
-    if (!WIDE) {        // the runs of a workgroup, in their order
-        __syncthreads();
+    if (!WIDE) {
+        float sums[NIT * VEC];
 #pragma unroll
-        for (int n = 0; n < NIT; ++n)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) sh[((run * NIT + n) * a.lpr + lane) * VEC + i] = sw[n][i];
-        __syncthreads();
+        for (int i = 0; i < NIT * VEC; ++i) sums[i] = sw[i / VEC][i % VEC];
+        over_runs<THREADS>(sums, a.rpw, a.lpr, sh);
         if (run) return;
 #pragma unroll
-        for (int n = 0; n < NIT; ++n)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                for (int q = 1; q < a.rpw; ++q) sw[n][i] += sh[((q * NIT + n) * a.lpr + lane) * VEC + i];
+        for (int i = 0; i < NIT * VEC; ++i) sw[i / VEC][i % VEC] = sums[i];
     }
 #pragma unroll
     for (int n = 0; n < NIT; ++n) {

@@ -5,6 +5,25 @@
 namespace cawn {
 namespace ops {
 
+// Sums of N values over the runs of a workgroup's threads, `each` threads a run: the first run has them then.  In halves: one after the other the 64 runs of
+// a narrow matrix took longer than its reading (2 rows of 77 channels, the norm's backward: 24 us, so 6).  sh: N x THREADS.
+template <int THREADS, int N> __device__ inline void over_runs(float (&v)[N], int runs, int each, float *sh)
+{
+    const int run = threadIdx.x / each;
+    for (int half; runs > 1; runs = half) {
+        half = (runs + 1) / 2;
+        if (run >= half && run < runs) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) sh[i * THREADS + threadIdx.x] = v[i];
+        }
+        __syncthreads();
+        if (run + half < runs) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] += sh[i * THREADS + threadIdx.x + half * each];
+        }
+    }
+}
+
 constexpr int SUM_COLS = 32, SUM_RUNS = 32;
 
 // out(c) gives the place of column c's sum, or null.  A workgroup takes 32 columns; its 32 runs of threads take every 32nd row, and are
