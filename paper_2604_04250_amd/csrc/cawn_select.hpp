@@ -78,11 +78,28 @@ __device__ float mul_zero(float a, float b) __asm("llvm.amdgcn.fmul.legacy");   
 // exp(delta A).  The product is 0 where delta is, also times minus infinity: there nothing is forgotten, and tokens that are none change nothing.
 __device__ inline float factor(float delta, float A) { return __builtin_amdgcn_exp2f(mul_zero(delta, A)); }
 
+struct ParamSums {      // column of a row of part_a -> its place in the gradients of A, D and the bias
+    float *dA, *dD, *db;
+    int N, NPT, Dp, cpg, cg;
+    __device__ float *operator()(long long c) const
+    {
+        const long long wide = (long long)Dp * NPT;
+        const long long pad = c < wide ? c / NPT : (c - wide) % Dp, g = pad / 64 / cpg, in = pad - g * cpg * 64;
+        if (in >= cg) return nullptr;
+        if (c < wide) {
+            const int n = (int)(c - pad * NPT);
+            return dA && n < N ? dA + (g * cg + in) * N + n : nullptr;
+        }
+        float *out = c - wide < Dp ? dD : db;
+        return out ? out + g * cg + in : nullptr;
+    }
+};
+
 int launch_token(const Args &a, bool bf16, hipStream_t s);
 int launch_forward(const Args &a, bool bf16, hipStream_t s);
 int launch_join(const Args &a, bool reverse, hipStream_t s);
 int launch_backward(const Args &a, bool bf16, hipStream_t s);       // behind it launch_bc
-int launch_bc_sums(const Args &a, bool bf16, hipStream_t s);
+int launch_bc_sums(const Args &a, bool bf16, const ParamSums &sums, int accumulate, hipStream_t s);
 
 // f(states of a wave, waves that share a channel's), as types
 template <typename F> void by_states(const Args &a, F f)

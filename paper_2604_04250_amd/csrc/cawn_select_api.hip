@@ -103,23 +103,6 @@ void segments_of(Args *a, char *ws, size_t begin)
     a->seg_b = (float *)(ws + begin), a->seg_s = (float *)(ws + begin + n * state), a->seg_g = (float *)(ws + begin + 2 * n * state);
 }
 
-struct ParamSums {      // column of a row of part_a -> its place in the gradients of A, D and the bias
-    float *dA, *dD, *db;
-    int N, NPT, Dp, cpg, cg;
-    __device__ float *operator()(long long c) const
-    {
-        const long long wide = (long long)Dp * NPT;
-        const long long pad = c < wide ? c / NPT : (c - wide) % Dp, g = pad / 64 / cpg, in = pad - g * cpg * 64;
-        if (in >= cg) return nullptr;
-        if (c < wide) {
-            const int n = (int)(c - pad * NPT);
-            return dA && n < N ? dA + (g * cg + in) * N + n : nullptr;
-        }
-        float *out = c - wide < Dp ? dD : db;
-        return out ? out + g * cg + in : nullptr;
-    }
-};
-
 bool misaligned(const cawn_scan_desc *d, const void *p) { return !aligned_to(p, d->bf16 ? 2 : 4); }
 
 } // namespace
@@ -183,7 +166,7 @@ int cawn_selective_scan_bwd(const cawn_scan_desc *d, const void *x, const void *
     hipStream_t s = (hipStream_t)stream;
     const int NPT = a.NP * a.NB, add = d->accumulate_param_grads;
     const bool params = dA || dDskip || ddt_bias;
-    const ParamSums sums{dA, dDskip, ddt_bias, a.N, NPT, a.Dp, a.cpg, a.cg};
+    const select::ParamSums sums{dA, dDskip, ddt_bias, a.N, NPT, a.Dp, a.cpg, a.cg};
     if (a.B == 0) {         // the sums over nothing
         if (params && !add) launch_sums(nullptr, 0, (long long)a.Dp * (NPT + 2), sums, 0, s);
         return launched();
@@ -201,11 +184,7 @@ int cawn_selective_scan_bwd(const cawn_scan_desc *d, const void *x, const void *
     a.part_bc = dBm || dCm ? (float *)(ws + l.pbc) : nullptr;
     a.part_a = params ? (float *)(ws + l.pa) : nullptr;
     if (int r = select::launch_backward(a, d->bf16, s)) return r;
-    if (a.part_bc) {
-        if (int r = select::launch_bc_sums(a, d->bf16, s)) return r;
-    }
-    if (params) launch_sums(a.part_a, (long long)a.B * a.segments, (long long)a.Dp * (NPT + 2), sums, add, s);
-    return launched();
+    return select::launch_bc_sums(a, d->bf16, sums, add, s);
 }
 
 } // extern "C"

@@ -423,11 +423,15 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
     if (p.on && a.dstate_in && p.seg == 0) store_user<NP>(a.dstate_in, a, user, p.blk * NP, h);
 }
 
-// dB and dC: the workgroups' sums, in their order; four states a thread.
-template <typename T> __global__ __launch_bounds__(256) void select_bc_sums(const Args a)
+// What the workgroups left, in their order: the first `bc` workgroups dB and dC, four states a thread, the others the parameters' gradients.
+template <typename T> __global__ __launch_bounds__(1024) void select_bc_sums(const Args a, const unsigned bc, const ParamSums sums, const int accumulate)
 {
     const int NPT = a.NP * a.NB, per = 2 * NPT;
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (blockIdx.x >= bc) {
+        sum_columns(blockIdx.x - bc, a.part_a, (long long)a.B * a.segments, (long long)a.Dp * (NPT + 2), sums, accumulate);
+        return;
+    }
+    const long long id = (long long)blockIdx.x * 1024 + threadIdx.x;
     const int at = (int)(id % (per / 4)) * 4, which = at / NPT, n = at % NPT;
     const long long rest = id / (per / 4), g = rest % a.G, bt = rest / a.G, b = bt / a.L, t = bt - b * a.L;
     if (b >= a.B || n >= a.N) return;
@@ -449,12 +453,14 @@ template <typename T> __global__ __launch_bounds__(256) void select_bc_sums(cons
     }
 }
 
-int launch_bc_sums(const Args &a, bool bf16_, hipStream_t s)
+int launch_bc_sums(const Args &a, bool bf16_, const ParamSums &sums, int accumulate, hipStream_t s)
 {
-    const dim3 grid((unsigned)ceil_div((long long)a.B * a.L * a.G * 2 * a.NP * a.NB / 4, 256));
-    if (a.L == 0) return CAWN_OK;
-    if (bf16_) hipLaunchKernelGGL(select_bc_sums<bf16>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(select_bc_sums<float>, grid, dim3(256), 0, s, a);
+    const int NPT = a.NP * a.NB;
+    const unsigned bc = a.part_bc ? (unsigned)ceil_div((long long)a.B * a.L * a.G * 2 * NPT / 4, 1024) : 0;
+    const unsigned pa = a.part_a ? (unsigned)ceil_div((long long)a.Dp * (NPT + 2), SUM_COLS) : 0;
+    if (bc + pa == 0) return CAWN_OK;
+    if (bf16_) hipLaunchKernelGGL(select_bc_sums<bf16>, dim3(bc + pa), dim3(1024), 0, s, a, bc, sums, accumulate);
+    else hipLaunchKernelGGL(select_bc_sums<float>, dim3(bc + pa), dim3(1024), 0, s, a, bc, sums, accumulate);
     return launched();
 }
 

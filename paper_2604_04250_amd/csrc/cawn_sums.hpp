@@ -6,7 +6,7 @@ namespace cawn {
 namespace ops {
 
 // Sums of N values over the runs of a workgroup's threads, `each` threads a run: the first run has them then.  In halves: one after the other the 64 runs of
-// a narrow matrix took longer than its reading (2 rows of 77 channels, the norm's backward: 24 us, so 6).  sh: N x THREADS.
+// a narrow matrix took longer than its reading (2 rows of 77 channels, the norm forward and backward: 31 us, so 12).  sh: N x THREADS.
 template <int THREADS, int N> __device__ inline void over_runs(float (&v)[N], int runs, int each, float *sh)
 {
     const int run = threadIdx.x / each;
@@ -28,12 +28,11 @@ constexpr int SUM_COLS = 32, SUM_RUNS = 32;
 
 // out(c) gives the place of column c's sum, or null.  A workgroup takes 32 columns; its 32 runs of threads take every 32nd row, and are
 // added up in their order.  (With 16 and 8 columns a workgroup the backward passes that end in it are up to 6 and 17 % slower.)
-template <typename Out> __global__ __launch_bounds__(SUM_COLS *SUM_RUNS) void column_sums(const float *part, const long long rows, const long long cols, const Out out,
-                                                                                         const int accumulate)
+template <typename Out> __device__ inline void sum_columns(const long long block, const float *part, const long long rows, const long long cols, const Out &out, const int accumulate)
 {
     __shared__ float sh[SUM_RUNS][SUM_COLS + 1];
     const int col = threadIdx.x % SUM_COLS, run = threadIdx.x / SUM_COLS;
-    const long long c = (long long)blockIdx.x * SUM_COLS + col;
+    const long long c = block * SUM_COLS + col;
     float v = 0.f;
     if (c < cols) {
         const float *p = part + c;
@@ -52,6 +51,12 @@ template <typename Out> __global__ __launch_bounds__(SUM_COLS *SUM_RUNS) void co
         float *at = out(c);
         if (at) *at = accumulate ? *at + s : s;
     }
+}
+
+template <typename Out> __global__ __launch_bounds__(SUM_COLS *SUM_RUNS) void column_sums(const float *part, const long long rows, const long long cols, const Out out,
+                                                                                         const int accumulate)
+{
+    sum_columns(blockIdx.x, part, rows, cols, out, accumulate);
 }
 
 template <typename Out> void launch_sums(const float *part, long long rows, long long cols, const Out &out, int accumulate, hipStream_t s)
