@@ -22,7 +22,7 @@ namespace {
 void cut(Args *a, bool bwd)
 {
     const long long columns = (long long)a->B * a->G * a->cbg * (a->NB > 1 ? a->NB : a->wide), waves = bwd ? 6144 : 8192;
-    const long long even = columns <= 1024 ? (bwd ? 980 : 890) : bwd ? 1560 : 1300;
+    const long long even = columns <= 1024 && a->NB < 8 ? (bwd ? 980 : 890) : bwd ? 1560 : 1300;       // (a workgroup of eight waves has two on a SIMD)
     a->segments = 1, a->seg_tiles = a->tiles > 0 ? a->tiles : 1;
     if (a->tiles < 2 || columns >= even || (long long)a->L * (even - columns) <= even * (bwd ? 24 : 48)) return;
     long long want = columns > 0 ? waves / columns : 1;

@@ -29,12 +29,16 @@ template <typename T> __global__ __launch_bounds__(256) void select_prepare(cons
     for (int i = threadIdx.x; i < 2 * TILE * npt; i += 256) out[i] = sh[i / TILE % 2][i % TILE][i / TILE / 2];
 }
 
-// NB waves share a channel's states.  RUN tokens at a time, the next ones' streams on their way meanwhile.
+// RUN tokens at a time, the next ones' streams on their way meanwhile.  NB waves share a channel's states: of a run's tokens each has every NB-th for its own,
+// makes their delta and u for all, and their y from all shares (67 tokens of 15 rows of 284 channels of 128 states 45 us, each wave all of them 56;
+// 4 x 2,048 of 1,024 of 24 110, 117).
 template <typename T, int NP, int NB, bool SUMMARY> __global__ __launch_bounds__(NB > 1 ? 64 * NB : 256) void select_scan(const Args a)
 {
     constexpr bool MULTI = NB > 1;
-    constexpr int NPT = NP * NB, AHEAD = 2;
+    constexpr bool SHARE = NB > 2 || (MULTI && !SUMMARY);              // (two waves without a barrier for y are better off without one for delta)
+    constexpr int NPT = NP * NB, AHEAD = 2, OWN = SHARE ? RUN / NB : RUN;
     __shared__ float ys[2][MULTI && !SUMMARY ? NB : 1][RUN][64];        // the waves' shares of y
+    __shared__ float2 shared[2][SHARE ? RUN : 1][64];                   // delta and u (two buffers: a wave may be a run ahead of another)
     const Place p = place_of<MULTI>(a);
     if (!MULTI && !p.there) return;
     const int n = __builtin_amdgcn_readfirstlane(row_length(a, p.b));
@@ -46,14 +50,22 @@ template <typename T, int NP, int NB, bool SUMMARY> __global__ __launch_bounds__
     const T *zp = !SUMMARY && a.z ? (const T *)a.z + p.b * a.zsb + p.base + t0 * a.zst : nullptr;
     const uint32_t at = p.bytes<T>();
     auto step = [](long long stride) { return (uint32_t)stride * (uint32_t)sizeof(T); };
-    uint32_t xr[RUN], dr[RUN], zr[SUMMARY ? 1 : RUN];
+    uint32_t xr[OWN], dr[OWN], zr[SUMMARY ? 1 : OWN];
+    auto load_own = [&](const T *row, long long stride, int left, uint32_t(&v)[OWN]) {
+        if constexpr (!SHARE) load_run<T, RUN>(row, step(stride), left, at, v);
+        else {
+            const auto r = rows_at(row);
+#pragma unroll
+            for (int k = 0; k < OWN; ++k) v[k] = load_at<T>(r, at, (uint32_t)min(k * NB + p.blk, left - 1) * step(stride));
+        }
+    };
     auto fetch = [&](int t) {
         const int left = t1 - t;
         if (left > 0) {
-            load_run<T, RUN>(dp, step(a.dst), left, at, dr);
-            load_run<T, RUN>(xp, step(a.xst), left, at, xr);
+            load_own(dp, a.dst, left, dr);
+            load_own(xp, a.xst, left, xr);
             dp += RUN * a.dst, xp += RUN * a.xst;
-        } else no_run<RUN>(dr), no_run<RUN>(xr);
+        } else no_run<OWN>(dr), no_run<OWN>(xr);
     };
     fetch(t0);
     float A[NP], S[NP], total = 0.f;
@@ -65,9 +77,42 @@ template <typename T, int NP, int NB, bool SUMMARY> __global__ __launch_bounds__
             if (t0 < t1 || (p.seg == 0 && n == 0)) load_states<NP>(a.seg_s + sat, S);
         } else if (a.state_in) load_user<NP>(a.state_in, a, user, p.blk * NP, S);
     }
-    const float bias = a.bias ? a.bias[p.ch] : 0.f, Dk = a.Dk && p.blk == 0 ? a.Dk[p.ch] : 0.f;
+    const float bias = a.bias ? a.bias[p.ch] : 0.f, Dk = a.Dk ? a.Dk[p.ch] : 0.f;
     T *yp = SUMMARY ? nullptr : (T *)a.y + p.b * a.ysb + p.base + t0 * a.yst;
     int buf = 0;
+    // the wave's own tokens: delta, u and x
+    float delta_own[OWN], u_own[OWN], x_own[OWN];
+    auto begin = [&](int left) {
+#pragma unroll
+        for (int k = 0; k < OWN; ++k) {
+            delta_own[k] = value<T>(dr[k]) + bias, u_own[k] = value<T>(xr[k]);
+            x_own[k] = u_own[k];
+        }
+        if (a.softplus) {
+#pragma unroll
+            for (int k = 0; k < OWN; ++k) delta_own[k] = softplus_f(delta_own[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < OWN; ++k) u_own[k] *= delta_own[k];
+        if (left < RUN) {           // behind the last token nothing changes
+#pragma unroll
+            for (int k = 0; k < OWN; ++k) {
+                const bool there = k * NB + p.blk < left;
+                delta_own[k] = there ? delta_own[k] : 0.f;
+                u_own[k] = there ? u_own[k] : 0.f;
+            }
+        }
+    };
+    auto hand_out = [&](int to) {
+#pragma unroll
+        for (int k = 0; k < OWN; ++k) shared[to][SHARE ? k * NB + p.blk : 0][p.lane] = make_float2(delta_own[k], u_own[k]);
+    };
+    if (SHARE && t0 < t1) {
+        begin(t1 - t0);
+        hand_out(0);
+        fetch(t0 + RUN);
+        __syncthreads();
+    }
     for (int t = t0; t < t1; t += RUN) {
         const int left = t1 - t;
         const float *tile = a.bc + (((long long)p.b * a.tiles + t / TILE) * a.G + p.g) * NPT * 2 * TILE + p.blk * NP * 2 * TILE + t % TILE;
@@ -78,35 +123,46 @@ template <typename T, int NP, int NB, bool SUMMARY> __global__ __launch_bounds__
             Bq[s] = bc_run<RUN>(tile, s, 0);
             if (!SUMMARY) Cq[s] = bc_run<RUN>(tile, s, 1);
         }
-        float delta[RUN], u[RUN], y[SUMMARY ? 1 : RUN];
-#pragma unroll
-        for (int i = 0; i < RUN; ++i) {
-            delta[i] = value<T>(dr[i]) + bias, u[i] = value<T>(xr[i]);
-            if constexpr (!SUMMARY) y[i] = Dk * u[i];
-        }
-        if (a.softplus) {
-#pragma unroll
-            for (int i = 0; i < RUN; ++i) delta[i] = softplus_f(delta[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < RUN; ++i) u[i] *= delta[i];
-        if (left < RUN) {           // behind the last token nothing changes
+        float delta[RUN], u[RUN], y[SUMMARY ? 1 : RUN], x[OWN];
+        if constexpr (!SHARE) {
 #pragma unroll
             for (int i = 0; i < RUN; ++i) {
-                delta[i] = i < left ? delta[i] : 0.f;
-                u[i] = i < left ? u[i] : 0.f;
+                delta[i] = value<T>(dr[i]) + bias, u[i] = value<T>(xr[i]);
+                if constexpr (!SUMMARY) y[i] = Dk * u[i];
             }
+            if (a.softplus) {
+#pragma unroll
+                for (int i = 0; i < RUN; ++i) delta[i] = softplus_f(delta[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < RUN; ++i) u[i] *= delta[i];
+            if (left < RUN) {
+#pragma unroll
+                for (int i = 0; i < RUN; ++i) {
+                    delta[i] = i < left ? delta[i] : 0.f;
+                    u[i] = i < left ? u[i] : 0.f;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < RUN; ++i) {
+                const float2 v = shared[buf][SHARE ? i : 0][p.lane];
+                delta[i] = v.x, u[i] = v.y;
+                if constexpr (!SUMMARY) y[i] = 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < OWN; ++k) x[k] = x_own[k];
         }
         if constexpr (SUMMARY) {
 #pragma unroll
             for (int i = 0; i < RUN; ++i) total += delta[i];
         } else {
             if (zp) {
-                load_run<T, RUN>(zp, step(a.zst), left, at, zr);
+                load_own(zp, a.zst, left, zr);
                 zp += RUN * a.zst;
-            } else no_run<RUN>(zr);
+            } else no_run<OWN>(zr);
         }
-        fetch(t + RUN);
+        if (!SHARE) fetch(t + RUN);
         // (B and C of the state after next are asked for behind the first token of this one, whose wait would be for them too; without the fences the
         // compiler asks for all at once and keeps them in lanes of vector registers)
 #pragma unroll
@@ -124,40 +180,46 @@ template <typename T, int NP, int NB, bool SUMMARY> __global__ __launch_bounds__
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        if constexpr (!SUMMARY) {
-            stay<RUN>(y);
-            if (MULTI) {        // (two buffers: a wave may be a run ahead of another)
-                buf ^= 1;
-#pragma unroll
-                for (int i = 0; i < RUN; ++i) ys[buf][p.blk][i][p.lane] = y[i];
-                __syncthreads();
+        if constexpr (!SUMMARY) stay<RUN>(y);
+        if (SHARE) {
+            if (t + RUN < t1) {
+                begin(left - RUN);
+                hand_out(buf ^ 1);
             }
-            if (MULTI) {
+            fetch(t + 2 * RUN);
+            if constexpr (!SUMMARY) {
 #pragma unroll
-                for (int i = 0; i < RUN; ++i) {
-                    if (i % NB != p.blk) continue;
-                    y[i] = 0.f;
+                for (int i = 0; i < RUN; ++i) ys[buf][MULTI ? p.blk : 0][i][p.lane] = y[i];
+            }
+            __syncthreads();
+        }
+        if constexpr (!SUMMARY) {
+            if constexpr (MULTI) {
 #pragma unroll
-                    for (int k = 0; k < NB; ++k) y[i] += ys[buf][MULTI ? k : 0][i][p.lane];
+                for (int k = 0; k < OWN; ++k) {
+                    y[k] = Dk * x[k];
+#pragma unroll
+                    for (int m = 0; m < NB; ++m) y[k] += ys[buf][MULTI ? m : 0][k * NB + p.blk][p.lane];
                 }
             }
             if (zp) {
 #pragma unroll
-                for (int i = 0; i < RUN; ++i) {
-                    const float z = value<T>(zr[i]);
-                    y[i] *= z * sigmoid_f(z);
+                for (int k = 0; k < OWN; ++k) {
+                    const float z = value<T>(zr[k]);
+                    y[k] *= z * sigmoid_f(z);
                 }
             }
             if (p.on) {
                 if (!MULTI) store_run<T, RUN>(yp, step(a.yst), left, at, [&](int i) { return y[i]; });
                 else {
 #pragma unroll
-                    for (int i = 0; i < RUN; ++i)
-                        if (i < left && i % NB == p.blk) store_at<T>(rows_at(yp + i * a.yst), at, 0, y[i]);
+                    for (int k = 0; k < OWN; ++k)
+                        if (k * NB + p.blk < left) store_at<T>(rows_at(yp + (k * NB + p.blk) * a.yst), at, 0, y[k]);
                 }
             }
             yp += RUN * a.yst;
         }
+        buf ^= 1;
     }
     if (SUMMARY) {
         store_states<NP>(a.seg_b + sat, S);
