@@ -35,6 +35,8 @@ template <typename T, int N> __device__ inline void store_n(T *p, const float (&
 inline bool aligned_to(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 inline int launched() { return hipGetLastError() == hipSuccess ? CAWN_OK : CAWN_ELAUNCH; }
 inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+// A launch counts its threads in 32 bits.
+inline bool launchable(double workgroups, int threads) { return workgroups * threads < 4294967296.; }
 
 } // namespace ops
 } // namespace cawn

@@ -428,7 +428,7 @@ template <typename T> __global__ __launch_bounds__(1024) void select_bc_sums(con
 {
     const int NPT = a.NP * a.NB, per = 2 * NPT;
     if (blockIdx.x >= bc) {
-        sum_columns(blockIdx.x - bc, a.part_a, (long long)a.B * a.segments, (long long)a.Dp * (NPT + 2), sums, accumulate);
+        sum_columns(blockIdx.x - bc, gridDim.x - bc, a.part_a, (long long)a.B * a.segments, (long long)a.Dp * (NPT + 2), sums, accumulate);
         return;
     }
     const long long id = (long long)blockIdx.x * 1024 + threadIdx.x;
@@ -457,7 +457,7 @@ int launch_bc_sums(const Args &a, bool bf16_, const ParamSums &sums, int accumul
 {
     const int NPT = a.NP * a.NB;
     const unsigned bc = a.part_bc ? (unsigned)ceil_div((long long)a.B * a.L * a.G * 2 * NPT / 4, 1024) : 0;
-    const unsigned pa = a.part_a ? (unsigned)ceil_div((long long)a.Dp * (NPT + 2), SUM_COLS) : 0;
+    const unsigned pa = a.part_a ? sum_blocks((long long)a.Dp * (NPT + 2)) : 0;
     if (bc + pa == 0) return CAWN_OK;
     if (bf16_) hipLaunchKernelGGL(select_bc_sums<bf16>, dim3(bc + pa), dim3(1024), 0, s, a, bc, sums, accumulate);
     else hipLaunchKernelGGL(select_bc_sums<float>, dim3(bc + pa), dim3(1024), 0, s, a, bc, sums, accumulate);
