@@ -501,7 +501,10 @@ int cawn_dropout_add_bwd(const cawn_dropout_desc *d, const void *dy, const uint6
 typedef struct cawn_scan_desc {
     int32_t B, L;         /* batch rows; tokens in THIS call (0 allowed: the state is passed through), up to 2^30   */
     int32_t D, N;         /* channels, up to 2^25, and states of each, 1..128 (beyond any of these, or with a token stride of
-                             x, dt, z or y beyond 2^25: CAWN_EUNSUPPORTED)                                           */
+                             x, dt, z or y beyond 2^25, or with 2^32 threads in a launch: CAWN_EUNSUPPORTED and 0 bytes.
+                             A thread is a channel of a row, channels counted in 64s or, where a group has more of them,
+                             in 128s, 192s or 256s; two, four or eight threads where N is above 16, 32 or 64; in calls of
+                             up to 16 tokens without a checkpoint it has four or eight states of one)                 */
     int32_t G;            /* groups of channels that share Bm and Cm; divides D, up to 2^23; 0 = 1                  */
     int32_t bf16;         /* 0: x, dt, Bm, Cm, z, y and their gradients are fp32; 1: bfloat16.  A, Dskip, dt_bias, the state, the
                              checkpoint and their gradients are fp32 either way, as is all arithmetic                */

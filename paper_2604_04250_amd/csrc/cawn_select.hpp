@@ -95,6 +95,16 @@ struct ParamSums {      // column of a row of part_a -> its place in the gradien
     }
 };
 
+// Token by token: eight states a lane, half the waves, where they are more than the chip holds at once (128 rows of 4,096 channels of 16 states: four 17.9 us,
+// eight 15.8, sixteen 20); lanes of a channel.
+inline int token_states(const Args &a) { return a.N > 4 && (long long)a.B * a.D * a.N >= 1 << 21 ? 8 : 4; }
+inline int token_lanes(const Args &a)
+{
+    int lanes = 1;
+    while (lanes * token_states(a) < a.N) lanes *= 2;
+    return lanes;
+}
+
 int launch_token(const Args &a, bool bf16, hipStream_t s);
 int launch_forward(const Args &a, bool bf16, hipStream_t s);
 int launch_join(const Args &a, bool reverse, hipStream_t s);

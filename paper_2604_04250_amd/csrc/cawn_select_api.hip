@@ -33,13 +33,14 @@ void cut(Args *a, bool bwd)
     a->segments = (int)ceil_div(a->tiles, a->seg_tiles);
 }
 
-// More workgroups than a grid has, in any of the launches, or more bytes than are counted.
-bool too_many(const Args &a)
-{
-    const double npt = a.NP * a.NB, rows = (double)a.B * a.G, most = 0x7fffffff;
-    return (double)a.B * a.tiles * a.Dp * npt > 1e17 || rows * a.tiles > most || (double)a.B * a.Dp * npt / 16 > most || rows * a.segments * a.cbg > most ||
-           rows * a.L * 2 * npt / 256 > most;
-}
+// More bytes than are counted.
+bool too_many(const Args &a) { return (double)a.B * (a.tiles + 1.) * a.Dp * (a.NP * a.NB) > 1e17; }
+
+// The passes of the tiled form, whose workgroups take a segment of columns each, and the launch of the other form.  (The chain has links only where the columns are
+// few, and the other launches go round.)
+bool tiles_fit(const Args &a) { return launchable((double)a.B * a.segments * a.G * a.cbg, 64 * (a.NB > 1 ? a.NB : a.wide)); }
+bool by_token(const Args &a) { return a.L <= select::TOKEN_MAX; }
+bool tokens_fit(const Args &a) { return launchable((double)ceil_div((long long)a.B * a.D * select::token_lanes(a), 256), 256); }
 
 int check(const cawn_scan_desc *d, bool bwd, Args *a)
 {
@@ -68,7 +69,7 @@ int check(const cawn_scan_desc *d, bool bwd, Args *a)
     a->Dp = a->cpg * G * 64;
     a->tiles = (int)ceil_div(d->L, TILE);
     cut(a, bwd);
-    return too_many(*a) ? CAWN_EUNSUPPORTED : CAWN_OK;
+    return too_many(*a) || !(tiles_fit(*a) || (!bwd && by_token(*a) && tokens_fit(*a))) ? CAWN_EUNSUPPORTED : CAWN_OK;
 }
 
 // Byte offsets.  Kept for the backward: B and C, states before each tile.  Scratch: forward B and C (unless kept), of segments their b, sum of delta and
@@ -118,13 +119,14 @@ size_t cawn_selective_scan_state_bytes(const cawn_scan_desc *d)
 size_t cawn_selective_scan_ckpt_bytes(const cawn_scan_desc *d)
 {
     Args a;
-    return check(d, false, &a) != CAWN_OK ? 0 : layout_of(a, a).ckpt;
+    return check(d, false, &a) != CAWN_OK || !tiles_fit(a) ? 0 : layout_of(a, a).ckpt;
 }
 
 size_t cawn_selective_scan_workspace_bytes(const cawn_scan_desc *d)
 {
     Args a, r;
-    if (check(d, false, &a) != CAWN_OK || check(d, true, &r) != CAWN_OK) return 0;
+    if (check(d, false, &a) != CAWN_OK) return 0;
+    if (check(d, true, &r) != CAWN_OK) return by_token(a) && tokens_fit(a) ? 256 : 0;         // (what uses none)
     const Layout l = layout_of(a, r);
     const size_t bytes = l.fwd > l.bwd ? l.fwd : l.bwd;
     return bytes > 256 ? bytes : 256;
@@ -136,6 +138,8 @@ int cawn_selective_scan_fwd(const cawn_scan_desc *d, const void *x, const void *
 {
     Args a;
     if (int r = check(d, false, &a)) return r;
+    const bool tokens = by_token(a) && !ckpt;
+    if (!(tokens ? tokens_fit(a) : tiles_fit(a))) return CAWN_EUNSUPPORTED;
     if (a.B == 0) return CAWN_OK;
     if (!A || (a.L > 0 && (!x || !dt || !Bm || !Cm || !y))) return CAWN_EINVAL;
     if (misaligned(d, x) || misaligned(d, dt) || misaligned(d, Bm) || misaligned(d, Cm) || misaligned(d, z) || misaligned(d, y) || !aligned_to(A, 4) || !aligned_to(Dskip, 4) ||
@@ -143,7 +147,7 @@ int cawn_selective_scan_fwd(const cawn_scan_desc *d, const void *x, const void *
     a.x = x, a.dt = dt, a.A = A, a.Bm = Bm, a.Cm = Cm, a.Dk = Dskip, a.z = z, a.bias = dt_bias, a.lengths = lengths, a.state_in = (const float *)state_in;
     a.y = y, a.state_out = (float *)state_out;
     hipStream_t s = (hipStream_t)stream;
-    if (a.L <= select::TOKEN_MAX && !ckpt) return select::launch_token(a, d->bf16, s);
+    if (tokens) return select::launch_token(a, d->bf16, s);
     const Layout l = layout_of(a, a);
     if (!workspace || workspace_bytes < l.fwd || !aligned_to(workspace, 256)) return CAWN_EWORKSPACE;
     a.bc = (float *)(ckpt ? ckpt : workspace);

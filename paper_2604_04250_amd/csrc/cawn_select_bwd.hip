@@ -423,7 +423,10 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
     if (p.on && a.dstate_in && p.seg == 0) store_user<NP>(a.dstate_in, a, user, p.blk * NP, h);
 }
 
-// What the workgroups left, in their order: the first `bc` workgroups dB and dC, four states a thread, the others the parameters' gradients.
+// What the workgroups left, in their order: the first `bc` workgroups dB and dC, four states a thread, the others the parameters' gradients.  Beyond BC_BLOCKS
+// the former go round.
+constexpr long long BC_BLOCKS = 1 << 12;
+
 template <typename T> __global__ __launch_bounds__(1024) void select_bc_sums(const Args a, const unsigned bc, const ParamSums sums, const int accumulate)
 {
     const int NPT = a.NP * a.NB, per = 2 * NPT;
@@ -431,32 +434,34 @@ template <typename T> __global__ __launch_bounds__(1024) void select_bc_sums(con
         sum_columns(blockIdx.x - bc, gridDim.x - bc, a.part_a, (long long)a.B * a.segments, (long long)a.Dp * (NPT + 2), sums, accumulate);
         return;
     }
-    const long long id = (long long)blockIdx.x * 1024 + threadIdx.x;
-    const int at = (int)(id % (per / 4)) * 4, which = at / NPT, n = at % NPT;
-    const long long rest = id / (per / 4), g = rest % a.G, bt = rest / a.G, b = bt / a.L, t = bt - b * a.L;
-    if (b >= a.B || n >= a.N) return;
-    T *out = (T *)(which ? a.dC : a.dB);
-    if (!out) return;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (t < row_length(a, (int)b)) {
-        const float *p = a.part_bc + (((b * a.tiles * TILE + t) * a.G + g) * a.parts) * per + at;
-        for (int k = 0; k < a.parts; ++k) v += *reinterpret_cast<const f32x4 *>(p + (long long)k * per);
-    }
-    out += b * a.bsb + t * a.bst + g * a.N + n;
-    if (n + 4 <= a.N && ((uintptr_t)out & (4 * sizeof(T) - 1)) == 0) {
-        const float x[4] = {v[0], v[1], v[2], v[3]};
-        store_n<T, 4>(out, x);
-    } else {
+    const long long all = (long long)a.B * a.L * a.G * (per / 4);
+    for (long long id = (long long)blockIdx.x * 1024 + threadIdx.x; id < all; id += (long long)bc * 1024) {
+        const int at = (int)(id % (per / 4)) * 4, which = at / NPT, n = at % NPT;
+        const long long rest = id / (per / 4), g = rest % a.G, bt = rest / a.G, b = bt / a.L, t = bt - b * a.L;
+        T *out = (T *)(which ? a.dC : a.dB);
+        if (n >= a.N || !out) continue;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        if (t < row_length(a, (int)b)) {
+            const float *p = a.part_bc + (((b * a.tiles * TILE + t) * a.G + g) * a.parts) * per + at;
+            for (int k = 0; k < a.parts; ++k) v += *reinterpret_cast<const f32x4 *>(p + (long long)k * per);
+        }
+        out += b * a.bsb + t * a.bst + g * a.N + n;
+        if (n + 4 <= a.N && ((uintptr_t)out & (4 * sizeof(T) - 1)) == 0) {
+            const float x[4] = {v[0], v[1], v[2], v[3]};
+            store_n<T, 4>(out, x);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (n + j < a.N) out[j] = (T)v[j];
+            for (int j = 0; j < 4; ++j)
+                if (n + j < a.N) out[j] = (T)v[j];
+        }
     }
 }
 
 int launch_bc_sums(const Args &a, bool bf16_, const ParamSums &sums, int accumulate, hipStream_t s)
 {
     const int NPT = a.NP * a.NB;
-    const unsigned bc = a.part_bc ? (unsigned)ceil_div((long long)a.B * a.L * a.G * 2 * NPT / 4, 1024) : 0;
+    const long long want = ceil_div((long long)a.B * a.L * a.G * 2 * NPT / 4, 1024);
+    const unsigned bc = a.part_bc ? (unsigned)(want < BC_BLOCKS ? want : BC_BLOCKS) : 0;
     const unsigned pa = a.part_a ? sum_blocks((long long)a.Dp * (NPT + 2)) : 0;
     if (bc + pa == 0) return CAWN_OK;
     if (bf16_) hipLaunchKernelGGL(select_bc_sums<bf16>, dim3(bc + pa), dim3(1024), 0, s, a, bc, sums, accumulate);

@@ -13,20 +13,25 @@ namespace cawn {
 namespace select {
 
 // bc[b][tile][g][n][which][token of the tile]; zeros where there is no token or state.  A workgroup takes a tile of a group, read along the states and
-// written along the tokens.
+// written along the tokens; beyond PREPARE_BLOCKS of them the workgroups go round.
+constexpr long long PREPARE_BLOCKS = 1 << 16;
+
 template <typename T> __global__ __launch_bounds__(256) void select_prepare(const Args a)
 {
     __shared__ float sh[2][TILE][N_MAX + 1];
-    const int npt = a.NP * a.NB, g = blockIdx.x % a.G;
-    const long long bt = blockIdx.x / a.G, b = bt / a.tiles, t = (bt - b * a.tiles) * TILE;
-    const int left = row_length(a, (int)b) - (int)t;
-    for (int i = threadIdx.x; i < 2 * TILE * npt; i += 256) {
-        const int n = i % npt, tt = i / npt % TILE, which = i / npt / TILE;
-        sh[which][tt][n] = n < a.N && tt < left ? (float)((const T *)(which ? a.Cm : a.Bm))[b * a.bsb + (t + tt) * a.bst + (long long)g * a.N + n] : 0.f;
+    const int npt = a.NP * a.NB;
+    for (long long at = blockIdx.x, all = (long long)a.B * a.tiles * a.G; at < all; at += gridDim.x) {
+        if (at != blockIdx.x) __syncthreads();      // (the tile before has been written)
+        const long long bt = at / a.G, b = bt / a.tiles, t = (bt - b * a.tiles) * TILE;
+        const int g = (int)(at - bt * a.G), left = row_length(a, (int)b) - (int)t;
+        for (int i = threadIdx.x; i < 2 * TILE * npt; i += 256) {
+            const int n = i % npt, tt = i / npt % TILE, which = i / npt / TILE;
+            sh[which][tt][n] = n < a.N && tt < left ? (float)((const T *)(which ? a.Cm : a.Bm))[b * a.bsb + (t + tt) * a.bst + (long long)g * a.N + n] : 0.f;
+        }
+        __syncthreads();
+        float *out = a.bc + at * npt * 2 * TILE;
+        for (int i = threadIdx.x; i < 2 * TILE * npt; i += 256) out[i] = sh[i / TILE % 2][i % TILE][i / TILE / 2];
     }
-    __syncthreads();
-    float *out = a.bc + (long long)blockIdx.x * npt * 2 * TILE;
-    for (int i = threadIdx.x; i < 2 * TILE * npt; i += 256) out[i] = sh[i / TILE % 2][i % TILE][i / TILE / 2];
 }
 
 // RUN tokens at a time, the next ones' streams on their way meanwhile.  NB waves share a channel's states: of a run's tokens each has every NB-th for its own,
@@ -312,7 +317,11 @@ template <typename T, int NP, int NB> static void launch_np(const Args &a, hipSt
 
 template <typename T> static int launch(const Args &a, hipStream_t s)
 {
-    if (a.tiles > 0) hipLaunchKernelGGL((select_prepare<T>), dim3((unsigned)((long long)a.B * a.tiles * a.G)), dim3(256), 0, s, a);
+    const long long all = (long long)a.B * a.tiles * a.G;
+    if (all > 0) {
+        hipLaunchKernelGGL((select_prepare<T>), dim3((unsigned)(all < PREPARE_BLOCKS ? all : PREPARE_BLOCKS)), dim3(256), 0, s, a);
+        if (int r = launched()) return r;           // (without B and C the scan would write over y and the state what is none)
+    }
     by_states(a, [&](auto np, auto nb) { launch_np<T, decltype(np)::value, decltype(nb)::value>(a, s); });
     return launched();
 }

@@ -91,16 +91,10 @@ template <typename T, int LPC, int W, bool VEC> __global__ __launch_bounds__(256
 
 template <typename T> static int launch(const Args &a, hipStream_t s)
 {
-    // Eight states a lane, half the waves, where they are more than the chip holds at once.  (128 rows of 4,096 channels of 16 states: four 17.9 us, eight 15.8,
-    // sixteen 20.)
-    const int w = a.N > 4 && (long long)a.B * a.D * a.N >= 1 << 21 ? 8 : 4;
-    int lpc = 1;
-    while (lpc * w < a.N) lpc *= 2;
+    const int w = token_states(a), lpc = token_lanes(a);
     const bool vec4 = a.N % 4 == 0 && aligned_to(a.state_in, 16) && aligned_to(a.state_out, 16) && aligned_to(a.A, 16) && a.bst % 4 == 0 && a.bsb % 4 == 0 &&
                       aligned_to(a.Bm, 4 * sizeof(T)) && aligned_to(a.Cm, 4 * sizeof(T));
-    const long long blocks = ceil_div((long long)a.B * a.D * lpc, 256);
-    if (blocks > 0x7fffffffLL) return CAWN_EUNSUPPORTED;
-    const dim3 grid((unsigned)blocks);
+    const dim3 grid((unsigned)ceil_div((long long)a.B * a.D * lpc, 256));
 #define CAWN_TOKENS(LPC, W)                                                                                        \
     case LPC:                                                                                                   \
         if (vec4) hipLaunchKernelGGL((select_tokens<T, LPC, W, true>), grid, dim3(256), 0, s, a);                \

@@ -2,7 +2,8 @@
 import pytest
 import torch
 
-from layer_util import DEV, scratch
+import layer_ref as R
+from layer_util import DEV, EPS, ROUND16, Scan, reference_inputs, rel_err, scan_inputs, scratch
 from paper_2604_04250_amd import binding as K
 
 pytestmark = pytest.mark.gpu
@@ -22,3 +23,21 @@ def test_parameter_sums_over_more_columns_than_a_launch_counts_threads_for():
         assert torch.equal(dw[:, i], dy[0, 0] * (state[0, i] if i < k - 1 else x[0, 0])), i
     K.check(K.cawn_causal_conv_bwd(K.make_conv_desc(0, 1, C, k), x, w, None, None, state, dy, None, None, dw, db, None, None))        # sums over nothing
     assert not bool(dw.any()) and not bool(db.any())
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("B,L,D,N,G,ragged", [
+    (3, 720, 500, 8, 500, True),            # 67,500 tiles of B and C, 4,219 workgroups of their gradients: both go round
+    (1, 18, 1 << 18, 2, 4, False),          # 1,572,864 columns of parameter sums
+])
+def test_scan_whose_launches_go_round(B, L, D, N, G, ragged, bf16):
+    i = scan_inputs(B, L, D, N, G, bf16, seed=D, ragged=ragged)
+    s = Scan(i, bf16).forward().backward()
+    torch.cuda.synchronize()
+    # as in the scan's own tests: 256 tokens of memory at most, four roundings a token
+    tol = 4 * EPS * (16 + 4 * min(L, 256))
+    y, state = R.scan_fwd(**reference_inputs(i))
+    assert rel_err(s.y.float().cpu(), y) <= tol + (ROUND16 if bf16 else 0) and rel_err(s.state_out.cpu(), state) <= tol
+    ref, got = R.scan_bwd(dy=i["dy"], dstate_out=i["dstate_out"], **reference_inputs(i)), s.grads()
+    for n, r in ref.items():
+        assert rel_err(got[n], r) <= tol + (ROUND16 if bf16 and n in ("dx", "ddt", "dBm", "dCm", "dz") else 0), n
