@@ -558,7 +558,8 @@ int cawn_selective_scan_bwd(const cawn_scan_desc *d, const void *x, const void *
  */
 typedef struct cawn_conv_desc {
     int32_t B, L, C, k;                 /* rows, tokens of THIS call (0 allowed: the state is passed through), channels, both up to 2^30,
-                                           taps 1..4 (beyond: CAWN_EUNSUPPORTED)                                                       */
+                                           taps 1..4 (beyond, or where the forward's launch would have 2^32 threads, of four channels
+                                           and 8 to 32 tokens of a row: CAWN_EUNSUPPORTED)                                             */
     int32_t act;                        /* 0 none, 1 SiLU                                                                              */
     int32_t bf16;                       /* 1: x, y, dy, dx are bfloat16, else fp32; taps, bias, state and their gradients are fp32     */
     int32_t accumulate_param_grads;     /* backward: 0 overwrite, 1 add into dw, dbias                                                 */

@@ -281,43 +281,46 @@ template <typename T, int K, int VEC, bool TAIL> __global__ __launch_bounds__(25
 }
 
 // The gradient of the state before the row alone, where it takes the place of that behind the row, which the other workgroups read: what its first
-// K - 1 tokens make of it, and what of it is still there behind the last.
+// K - 1 tokens make of it, and what of it is still there behind the last.  Beyond STATE_BLOCKS workgroups they go round.
+constexpr long long STATE_BLOCKS = 1 << 16;
+
 template <typename T, int K, int VEC, bool TAIL> __global__ __launch_bounds__(256) void conv_state_backward(const ConvArgs a)
 {
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x, b = id / a.units;
-    if (b >= a.B) return;
-    const Unit<VEC, TAIL> u((int)(id - b * a.units), a.C);
-    const int c = u.c, n = row_length(a, (int)b);
-    const Taps<K, VEC> p(a, c);
-    float d[K][VEC], dz[K][VEC], win[K][VEC];
+    for (long long id = (long long)blockIdx.x * 256 + threadIdx.x, all = (long long)a.B * a.units; id < all; id += (long long)gridDim.x * 256) {
+        const long long b = id / a.units;
+        const Unit<VEC, TAIL> u((int)(id - b * a.units), a.C);
+        const int c = u.c, n = row_length(a, (int)b);
+        const Taps<K, VEC> p(a, c);
+        float d[K][VEC], dz[K][VEC], win[K][VEC];
 #pragma unroll
-    for (int i = 1; i < K; ++i) before_row<K, VEC>(a, (int)b, K - i, c, win[i]);
+        for (int i = 1; i < K; ++i) before_row<K, VEC>(a, (int)b, K - i, c, win[i]);
 #pragma unroll
-    for (int t = 0; t < K - 1; ++t) {
-        float dy[VEC];
+        for (int t = 0; t < K - 1; ++t) {
+            float dy[VEC];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) dz[t][j] = 0.f;
-        if (t >= n) continue;
+            for (int j = 0; j < VEC; ++j) dz[t][j] = 0.f;
+            if (t >= n) continue;
 #pragma unroll
-        for (int i = 0; i + 1 < K; ++i)
+            for (int i = 0; i + 1 < K; ++i)
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) win[i][j] = win[i + 1][j];
-        read_n<T, VEC>((const T *)a.x + b * a.xsb + t * a.xst + c, win[K - 1]);
-        read_n<T, VEC>((const T *)a.dy + b * a.ysb + t * a.yst + c, dy);
-        slope<K, VEC>(a, p, win, dy, dz[t]);
-    }
-    // (the sum in the order of the other kernel, whose bits these are)
-#pragma unroll
-    for (int s = 0; s < K - 1; ++s)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            d[s][j] = 0.f;
-#pragma unroll
-            for (int t = 0; t <= s; ++t) d[s][j] = fmaf(p.w[s - t][j], dz[t][j], d[s][j]);
-            if (a.dstate_out && s >= n) d[s][j] += a.dstate_out[(b * (K - 1) + (s - n)) * a.C + c + j];
+                for (int j = 0; j < VEC; ++j) win[i][j] = win[i + 1][j];
+            read_n<T, VEC>((const T *)a.x + b * a.xsb + t * a.xst + c, win[K - 1]);
+            read_n<T, VEC>((const T *)a.dy + b * a.ysb + t * a.yst + c, dy);
+            slope<K, VEC>(a, p, win, dy, dz[t]);
         }
+        // (the sum in the order of the other kernel, whose bits these are)
 #pragma unroll
-    for (int i = 0; i < K - 1; ++i) store_state<K, VEC>(a, a.dstate_in, b, i, c, u.skip, d[i]);
+        for (int s = 0; s < K - 1; ++s)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                d[s][j] = 0.f;
+#pragma unroll
+                for (int t = 0; t <= s; ++t) d[s][j] = fmaf(p.w[s - t][j], dz[t][j], d[s][j]);
+                if (a.dstate_out && s >= n) d[s][j] += a.dstate_out[(b * (K - 1) + (s - n)) * a.C + c + j];
+            }
+#pragma unroll
+        for (int i = 0; i < K - 1; ++i) store_state<K, VEC>(a, a.dstate_in, b, i, c, u.skip, d[i]);
+    }
 }
 
 struct TapSums {        // column (i, c) of a part's [K + 1][C]
@@ -370,7 +373,7 @@ int plan_of(const cawn_conv_desc *d, bool bwd, Plan *p)
         if (a.rblocks < 1) a.rblocks = 1;
         p->blocks = a.rblocks * a.ublocks;
     }
-    return p->blocks > 0x7fffffffLL ? CAWN_EUNSUPPORTED : CAWN_OK;
+    return launchable((double)p->blocks, 256) ? CAWN_OK : CAWN_EUNSUPPORTED;
 }
 
 size_t part_bytes(const Plan &p) { return (size_t)p.a.rblocks * (p.k + 1) * p.a.C * 4; }
@@ -383,7 +386,8 @@ template <typename T, int K, int VEC, bool TAIL> int launch(const Plan &p, bool 
         const bool replaces = K > 1 && a.dstate_in && a.dstate_in == a.dstate_out;
         if (replaces) a.dstate_in = nullptr;
         if (a.dx || a.part || a.dstate_in) hipLaunchKernelGGL((conv_backward<T, K, VEC, TAIL>), dim3((unsigned)p.blocks), dim3(256), 0, s, a);
-        if (replaces) hipLaunchKernelGGL((conv_state_backward<T, K, VEC, TAIL>), dim3((unsigned)ceil_div((long long)a.B * a.units, 256)), dim3(256), 0, s, p.a);
+        const long long all = ceil_div((long long)a.B * a.units, 256), blocks = all < STATE_BLOCKS ? all : STATE_BLOCKS;
+        if (replaces) hipLaunchKernelGGL((conv_state_backward<T, K, VEC, TAIL>), dim3((unsigned)blocks), dim3(256), 0, s, p.a);
     }
     return launched();
 }

@@ -41,3 +41,18 @@ def test_scan_whose_launches_go_round(B, L, D, N, G, ragged, bf16):
     ref, got = R.scan_bwd(dy=i["dy"], dstate_out=i["dstate_out"], **reference_inputs(i)), s.grads()
     for n, r in ref.items():
         assert rel_err(got[n], r) <= tol + (ROUND16 if bf16 and n in ("dx", "ddt", "dBm", "dCm", "dz") else 0), n
+
+
+def test_state_gradients_in_place_of_more_rows_than_a_launch_takes_at_once():
+    """18 million threads on 16.8 million; one token of two taps: the state's gradient is that token's share of the older tap, or, of a row without it, what was there."""
+    B, C = 6000003, 3
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    x, dy, state, dstate = (torch.randn((B, 1, C), generator=gen, device=DEV) for _ in range(4))
+    w = torch.randn((C, 2), generator=gen, device=DEV)
+    lengths = (torch.arange(B, device=DEV) % 3 > 0).int()
+    there = lengths.bool()[:, None, None]
+    want, wx = torch.where(there, w[:, 0] * dy, dstate), torch.where(there, w[:, 1] * dy + dstate, 0)
+    d, dx = K.make_conv_desc(B, 1, C, 2), torch.empty_like(x)
+    K.check(K.cawn_causal_conv_bwd(d, x, w, None, lengths, state, dy, dstate, dx, None, None, dstate, None))
+    assert torch.equal(dstate, want)
+    assert float((dx - wx).abs().max()) <= 2 * 2.0 ** -24 * float(wx.abs().max())        # (a product and a sum, rounded once or twice)

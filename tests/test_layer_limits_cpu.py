@@ -53,3 +53,15 @@ def test_tokens_and_groups_that_the_launches_go_round_for():
     for d in (K.make_scan_desc(1, 1 << 30, 4, 1), K.make_scan_desc(64, 1 << 20, 64, 1, G=64)):
         assert K.cawn_selective_scan_ckpt_bytes(d) > 0 and K.cawn_selective_scan_workspace_bytes(d) > 0
         assert _scan(d, "tiles") == K.CAWN_EINVAL and _scan(d, "back") == K.CAWN_EWORKSPACE
+
+
+@pytest.mark.parametrize("L,channels,k,threads", [(1, 64, 4, 16), (8, 13, 2, 4), (33, 3, 1, 6), (65, 1024, 4, 768)])
+def test_rows_of_the_convolution(L, channels, k, threads):
+    """Threads of a row: runs of 32 tokens, four channels each or, of fewer than four, one."""
+    most = ((1 << 32) - 256) // threads
+    held, beyond = (K.make_conv_desc(B, L, channels, k) for B in (most, most + 256 // threads + 1))
+    fwd = lambda d: K.lib().cawn_causal_conv_fwd(C.byref(d), *([FAKE] * 5), C.c_void_p(0x1001), FAKE, None)  # noqa: E731
+    assert K.cawn_causal_conv_state_bytes(held) == most * (k - 1) * channels * 4
+    assert fwd(held) == K.CAWN_EINVAL           # (a misaligned y)
+    assert K.cawn_causal_conv_state_bytes(beyond) == 0
+    assert fwd(beyond) == K.CAWN_EUNSUPPORTED
