@@ -72,6 +72,7 @@ class ShortConv(torch.autograd.Function):
         _types(torch.float32, w=w, bias=bias, state=state)
         _types(torch.int32, lengths=lengths)
         x, w, bias, state = (t.contiguous() for t in (x, w, bias, state))
+        lengths = None if lengths is None else lengths.contiguous()
         d = K.make_conv_desc(*x.shape, w.shape[1], act=1, bf16=int(x.dtype == torch.bfloat16))
         y, out = torch.empty_like(x), torch.empty_like(state)
         K.check(K.cawn_causal_conv_fwd(d, x, w, bias, lengths, state, y, out))
@@ -98,6 +99,7 @@ class SelectiveScan(torch.autograd.Function):
         _types(torch.float32, A=A, skip=skip, dt_bias=dt_bias, state=state)
         _types(torch.int32, lengths=lengths)
         x, dt, A, Bm, Cm, skip, z, dt_bias, state = (t.contiguous() for t in (x, dt, A, Bm, Cm, skip, z, dt_bias, state))
+        lengths = None if lengths is None else lengths.contiguous()
         d = K.make_scan_desc(*x.shape, A.shape[1], G=Bm.shape[2], dt_softplus=1, bf16=int(x.dtype == torch.bfloat16))
         ckpt = _scratch(K.cawn_selective_scan_ckpt_bytes(d), x.device) if any(ctx.needs_input_grad) else None
         y, out = torch.empty_like(x), torch.empty_like(state)
