@@ -50,18 +50,18 @@ class DeltaRule(torch.autograd.Function):
         workspace = _scratch(K.cawn_delta_workspace_bytes(d), v.device)
         o, state_out = torch.empty_like(v), torch.empty((B, H, Kw, V), device=v.device)
         K.check(K.cawn_delta_rule_fwd(d, q, k, v, decay, beta, lengths, state, o, state_out, ckpt, workspace))
-        ctx.d, ctx.ckpt, ctx.lengths, ctx.workspace = d, ckpt, lengths, workspace
-        ctx.save_for_backward(q, k, v, decay, beta)
+        ctx.d, ctx.ckpt, ctx.workspace = d, ckpt, workspace
+        ctx.save_for_backward(q, k, v, decay, beta, lengths)
         return o, state_out
 
     @staticmethod
     @once_differentiable
     def backward(ctx, do, dstate_out):
-        q, k, v, decay, beta = ctx.saved_tensors
+        q, k, v, decay, beta, lengths = ctx.saved_tensors
         do, dstate_out = do.contiguous(), dstate_out.contiguous()
         dq, dk, dv, ddecay, dbeta = (torch.empty_like(t) for t in (q, k, v, decay, beta))
         dstate = torch.empty_like(dstate_out) if ctx.needs_input_grad[5] else None
-        K.check(K.cawn_delta_rule_bwd(ctx.d, q, k, v, decay, beta, ctx.lengths, ctx.ckpt, do, dstate_out, dq, dk, dv, ddecay,
+        K.check(K.cawn_delta_rule_bwd(ctx.d, q, k, v, decay, beta, lengths, ctx.ckpt, do, dstate_out, dq, dk, dv, ddecay,
                                       dbeta, dstate, ctx.workspace))
         return dq, dk, dv, ddecay, dbeta, dstate, None
 

@@ -76,16 +76,16 @@ class ShortConv(torch.autograd.Function):
         d = K.make_conv_desc(*x.shape, w.shape[1], act=1, bf16=int(x.dtype == torch.bfloat16))
         y, out = torch.empty_like(x), torch.empty_like(state)
         K.check(K.cawn_causal_conv_fwd(d, x, w, bias, lengths, state, y, out))
-        ctx.d, ctx.lengths = d, lengths
-        ctx.save_for_backward(x, w, bias, state)
+        ctx.d = d
+        ctx.save_for_backward(x, w, bias, state, lengths)
         return y, out
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy, dout):
-        x, w, bias, state = ctx.saved_tensors
+        x, w, bias, state, lengths = ctx.saved_tensors
         dx, dw, db, dstate = (torch.empty_like(t) for t in (x, w, bias, state))
-        K.check(K.cawn_causal_conv_bwd(ctx.d, x, w, bias, ctx.lengths, state, dy.contiguous(), dout.contiguous(), dx, dw, db, dstate,
+        K.check(K.cawn_causal_conv_bwd(ctx.d, x, w, bias, lengths, state, dy.contiguous(), dout.contiguous(), dx, dw, db, dstate,
                                        _scratch(K.cawn_causal_conv_workspace_bytes(ctx.d), x.device)))
         return dx, dw, db, dstate, None
 
@@ -105,18 +105,18 @@ class SelectiveScan(torch.autograd.Function):
         y, out = torch.empty_like(x), torch.empty_like(state)
         K.check(K.cawn_selective_scan_fwd(d, x, dt, A, Bm, Cm, skip, z, dt_bias, lengths, state, y, out, ckpt,
                                           _scratch(K.cawn_selective_scan_workspace_bytes(d), x.device)))
-        ctx.d, ctx.ckpt, ctx.lengths = d, ckpt, lengths
-        ctx.save_for_backward(x, dt, A, Bm, Cm, skip, z, dt_bias)
+        ctx.d, ctx.ckpt = d, ckpt
+        ctx.save_for_backward(x, dt, A, Bm, Cm, skip, z, dt_bias, lengths)
         return y, out
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy, dout):
-        saved = ctx.saved_tensors
+        *saved, lengths = ctx.saved_tensors
         x, dt, A, Bm, Cm, skip, z, dt_bias = saved
         dx, ddt, dA, dB, dC, dskip, dz, dbias = (torch.empty_like(t) for t in saved)
         dstate = torch.empty_like(dout, memory_format=torch.contiguous_format)
-        K.check(K.cawn_selective_scan_bwd(ctx.d, x, dt, A, Bm, Cm, skip, z, dt_bias, ctx.lengths, ctx.ckpt, dy.contiguous(), dout.contiguous(), dx, ddt, dA,
+        K.check(K.cawn_selective_scan_bwd(ctx.d, x, dt, A, Bm, Cm, skip, z, dt_bias, lengths, ctx.ckpt, dy.contiguous(), dout.contiguous(), dx, ddt, dA,
                                           dB, dC, dskip, dz, dbias, dstate, _scratch(K.cawn_selective_scan_workspace_bytes(ctx.d), x.device)))
         return dx, ddt, dA, dB, dC, dskip, dz, dbias, dstate, None
 

@@ -66,3 +66,13 @@ def test_lengths_with_a_stride_are_handed_on_as_dense_ones(calls, f, args, fwd, 
     for (name, a), at in zip(calls, (fwd, bwd)):
         got = a[1 + at]
         assert got.is_contiguous() and got.tolist() == [5, 0, 2], name
+
+
+@pytest.mark.parametrize("f,args,fwd,bwd", OPS)
+def test_lengths_overwritten_before_the_backward_are_an_error(calls, f, args, fwd, bwd):
+    lengths = torch.tensor([5, 0, 2], dtype=torch.int32)
+    out, _ = f.apply(*args(True), lengths)
+    lengths.fill_(1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()
+    assert len(calls) == 1
