@@ -32,6 +32,13 @@ def _types(wanted, **tensors):
             raise TypeError(f"{name} is {t.dtype}, not {wanted}")
 
 
+def _shapes(**wanted):
+    """... and how much of it there is: name = (tensor, shape)."""
+    for name, (t, shape) in wanted.items():
+        if t is not None and tuple(t.shape) != shape:
+            raise ValueError(f"{name} is {list(t.shape)}, not {list(shape)}")
+
+
 class DeltaRule(torch.autograd.Function):
     """q, k [B,L,Hk,K], v [B,L,H,V], decay, beta [B,L,H] fp32, state [B,H,K,V] fp32 -> o [B,L,H,V], state behind the last token."""
 
@@ -42,6 +49,8 @@ class DeltaRule(torch.autograd.Function):
         _types(torch.bfloat16 if v.dtype == torch.bfloat16 else torch.float32, q=q, k=k, v=v)
         _types(torch.float32, decay=decay, beta=beta, state=state)
         _types(torch.int32, lengths=lengths)
+        _shapes(q=(q, (B, L, Hk, Kw)), k=(k, (B, L, Hk, Kw)), decay=(decay, (B, L, H)), beta=(beta, (B, L, H)), state=(state, (B, H, Kw, V)),
+                lengths=(lengths, (B,)))
         d = K.make_delta_desc(B, L, H, Kw, V, Hk=Hk, scale=Kw ** -0.5, qk_norm=1, bf16=int(v.dtype == torch.bfloat16))
         q, k, v, decay, beta, state = (t.contiguous() for t in (q, k, v, decay, beta, state))
         lengths = None if lengths is None else lengths.contiguous()
@@ -72,6 +81,7 @@ class HeadNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, groups):
         _types(torch.bfloat16 if x.dtype == torch.bfloat16 else torch.float32, x=x)
+        _shapes(weight=(weight, (x.shape[-1],)), bias=(bias, (x.shape[-1],)))
         ctx.types = weight.dtype, bias.dtype
         x, weight, bias = x.contiguous(), weight.float().contiguous(), bias.float().contiguous()
         d = K.make_norm_desc(x.shape[0], 1, x.shape[1], groups, act=1, bf16=int(x.dtype == torch.bfloat16))
@@ -98,6 +108,7 @@ class DropoutAdd(torch.autograd.Function):
     def forward(ctx, x, residual, rng, p):
         _types(torch.bfloat16 if x.dtype == torch.bfloat16 else torch.float32, x=x, residual=residual)
         _types(torch.int64, rng=rng)
+        _shapes(residual=(residual, tuple(x.shape)), rng=(rng, (2,)))
         d = K.make_dropout_desc(*x.shape, p=p, bf16=int(x.dtype == torch.bfloat16))
         x, residual = x.contiguous(), residual.contiguous()
         y = torch.empty_like(x)

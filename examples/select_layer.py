@@ -33,6 +33,13 @@ def _types(wanted, **tensors):
             raise TypeError(f"{name} is {t.dtype}, not {wanted}")
 
 
+def _shapes(**wanted):
+    """... and how much of it there is: name = (tensor, shape)."""
+    for name, (t, shape) in wanted.items():
+        if t is not None and tuple(t.shape) != shape:
+            raise ValueError(f"{name} is {list(t.shape)}, not {list(shape)}")
+
+
 def _activation(t):
     return torch.bfloat16 if t.dtype == torch.bfloat16 else torch.float32
 
@@ -45,6 +52,7 @@ class AddNorm(torch.autograd.Function):
         _types(_activation(x), x=x)
         _types(_activation(residual), residual=residual)
         _types(torch.float32, weight=weight)
+        _shapes(residual=(residual, tuple(x.shape)), weight=(weight, (x.shape[-1],)))
         x, residual, weight = x.contiguous(), residual.contiguous(), weight.contiguous()
         d = K.make_rms_desc(*x.shape, eps=eps, bf16=int(x.dtype == torch.bfloat16), residual_bf16=int(residual.dtype == torch.bfloat16))
         h, y, rstd = torch.empty_like(residual), torch.empty_like(x), torch.empty(x.shape[0], device=x.device)
@@ -71,9 +79,11 @@ class ShortConv(torch.autograd.Function):
         _types(_activation(x), x=x)
         _types(torch.float32, w=w, bias=bias, state=state)
         _types(torch.int32, lengths=lengths)
+        (B, _, C), k = x.shape, w.shape[1]
+        _shapes(w=(w, (C, k)), bias=(bias, (C,)), state=(state, (B, k - 1, C)), lengths=(lengths, (B,)))
         x, w, bias, state = (t.contiguous() for t in (x, w, bias, state))
         lengths = None if lengths is None else lengths.contiguous()
-        d = K.make_conv_desc(*x.shape, w.shape[1], act=1, bf16=int(x.dtype == torch.bfloat16))
+        d = K.make_conv_desc(*x.shape, k, act=1, bf16=int(x.dtype == torch.bfloat16))
         y, out = torch.empty_like(x), torch.empty_like(state)
         K.check(K.cawn_causal_conv_fwd(d, x, w, bias, lengths, state, y, out))
         ctx.d = d
@@ -98,9 +108,12 @@ class SelectiveScan(torch.autograd.Function):
         _types(_activation(x), x=x, dt=dt, Bm=Bm, Cm=Cm, z=z)
         _types(torch.float32, A=A, skip=skip, dt_bias=dt_bias, state=state)
         _types(torch.int32, lengths=lengths)
+        (B, L, D), N, G = x.shape, A.shape[1], Bm.shape[2]
+        _shapes(dt=(dt, (B, L, D)), z=(z, (B, L, D)), A=(A, (D, N)), Bm=(Bm, (B, L, G, N)), Cm=(Cm, (B, L, G, N)), skip=(skip, (D,)),
+                dt_bias=(dt_bias, (D,)), state=(state, (B, D, N)), lengths=(lengths, (B,)))
         x, dt, A, Bm, Cm, skip, z, dt_bias, state = (t.contiguous() for t in (x, dt, A, Bm, Cm, skip, z, dt_bias, state))
         lengths = None if lengths is None else lengths.contiguous()
-        d = K.make_scan_desc(*x.shape, A.shape[1], G=Bm.shape[2], dt_softplus=1, bf16=int(x.dtype == torch.bfloat16))
+        d = K.make_scan_desc(B, L, D, N, G=G, dt_softplus=1, bf16=int(x.dtype == torch.bfloat16))
         ckpt = _scratch(K.cawn_selective_scan_ckpt_bytes(d), x.device) if any(ctx.needs_input_grad) else None
         y, out = torch.empty_like(x), torch.empty_like(state)
         K.check(K.cawn_selective_scan_fwd(d, x, dt, A, Bm, Cm, skip, z, dt_bias, lengths, state, y, out, ckpt,

@@ -76,3 +76,24 @@ def test_lengths_overwritten_before_the_backward_are_an_error(calls, f, args, fw
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         out.sum().backward()
     assert len(calls) == 1
+
+
+LENGTHS = torch.tensor([5, 0, 2], dtype=torch.int32)
+X, W = torch.randn(6, 8), torch.randn(8)
+# functions, what they take as it should be, how many of it are tensors, and what nothing else has to agree with: a tensor's axis
+TAKES = [(S.ShortConv, [*_conv_args(), LENGTHS], 5, (0, 1)), (S.SelectiveScan, [*_scan_args(), LENGTHS], 10, None), (S.AddNorm, [X, X, W, 1e-5], 3, None),
+         (D.DeltaRule, [*_delta_args(), LENGTHS], 7, None), (D.HeadNorm, [X, W, W, 2], 3, (0, 0)), (D.DropoutAdd, [X, X, torch.zeros(2, dtype=torch.int64), 0.1], 3, None)]
+
+
+@pytest.mark.parametrize("f,args,n,free", TAKES)
+def test_sizes_that_do_not_agree_are_refused(calls, f, args, n, free):
+    """Every tensor in turn one entry shorter along every axis: an entry point would read beyond its end, or the others would be read beyond theirs."""
+    f.apply(*args)
+    assert len(calls) == 1
+    for i in range(n):
+        for axis in range(args[i].dim()):
+            if (i, axis) == free:
+                continue
+            with pytest.raises(ValueError):
+                f.apply(*args[:i], args[i].narrow(axis, 0, args[i].shape[axis] - 1), *args[i + 1:])
+    assert len(calls) == 1
