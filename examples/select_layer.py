@@ -101,10 +101,13 @@ class ShortConv(torch.autograd.Function):
 
 
 class SelectiveScan(torch.autograd.Function):
-    """x, dt, z [B,L,D], A [D,N], Bm, Cm [B,L,G,N], skip, dt_bias [D], state [B,D,N] fp32 -> y [B,L,D], the state behind the last token."""
+    """x, dt, z [B,L,D], A [D,N], Bm, Cm [B,L,G,N], skip, dt_bias [D], state [B,D,N] fp32 -> y [B,L,D], the state behind the last token.
+
+    grad: the caller's torch.is_grad_enabled(), which is off inside; a parameter needs its gradient whether or not.  Without a backward to come there is
+    no checkpoint, and calls of a few tokens go token by token."""
 
     @staticmethod
-    def forward(ctx, x, dt, A, Bm, Cm, skip, z, dt_bias, state, lengths):
+    def forward(ctx, x, dt, A, Bm, Cm, skip, z, dt_bias, state, lengths, grad=True):
         _types(_activation(x), x=x, dt=dt, Bm=Bm, Cm=Cm, z=z)
         _types(torch.float32, A=A, skip=skip, dt_bias=dt_bias, state=state)
         _types(torch.int32, lengths=lengths)
@@ -114,7 +117,7 @@ class SelectiveScan(torch.autograd.Function):
         x, dt, A, Bm, Cm, skip, z, dt_bias, state = (t.contiguous() for t in (x, dt, A, Bm, Cm, skip, z, dt_bias, state))
         lengths = None if lengths is None else lengths.contiguous()
         d = K.make_scan_desc(B, L, D, N, G=G, dt_softplus=1, bf16=int(x.dtype == torch.bfloat16))
-        ckpt = _scratch(K.cawn_selective_scan_ckpt_bytes(d), x.device) if any(ctx.needs_input_grad) else None
+        ckpt = _scratch(K.cawn_selective_scan_ckpt_bytes(d), x.device) if grad and any(ctx.needs_input_grad) else None
         y, out = torch.empty_like(x), torch.empty_like(state)
         K.check(K.cawn_selective_scan_fwd(d, x, dt, A, Bm, Cm, skip, z, dt_bias, lengths, state, y, out, ckpt,
                                           _scratch(K.cawn_selective_scan_workspace_bytes(d), x.device)))
@@ -131,7 +134,7 @@ class SelectiveScan(torch.autograd.Function):
         dstate = torch.empty_like(dout, memory_format=torch.contiguous_format)
         K.check(K.cawn_selective_scan_bwd(ctx.d, x, dt, A, Bm, Cm, skip, z, dt_bias, lengths, ctx.ckpt, dy.contiguous(), dout.contiguous(), dx, ddt, dA,
                                           dB, dC, dskip, dz, dbias, dstate, _scratch(K.cawn_selective_scan_workspace_bytes(ctx.d), x.device)))
-        return dx, ddt, dA, dB, dC, dskip, dz, dbias, dstate, None
+        return dx, ddt, dA, dB, dC, dskip, dz, dbias, dstate, None, None
 
 
 class SelectLayer(torch.nn.Module):
@@ -163,7 +166,8 @@ class SelectLayer(torch.nn.Module):
         u, conv = ShortConv.apply(u, self.conv_w, self.conv_b, conv, lengths)
         dt, Bm, Cm = self.select(u).split([self.rank, self.groups * self.states, self.groups * self.states], -1)
         Bm, Cm = (t.reshape(B, L, self.groups, self.states) for t in (Bm, Cm))
-        u, ssm = SelectiveScan.apply(u, self.steps(dt), -torch.exp(self.log_rate), Bm, Cm, self.skip, z, self.dt_bias, ssm, lengths)
+        u, ssm = SelectiveScan.apply(u, self.steps(dt), -torch.exp(self.log_rate), Bm, Cm, self.skip, z, self.dt_bias, ssm, lengths,
+                                     torch.is_grad_enabled())
         return self.out(u), h.view(B, L, width), (conv, ssm)
 
 

@@ -97,3 +97,21 @@ def test_sizes_that_do_not_agree_are_refused(calls, f, args, n, free):
             with pytest.raises(ValueError):
                 f.apply(*args[:i], args[i].narrow(axis, 0, args[i].shape[axis] - 1), *args[i + 1:])
     assert len(calls) == 1
+
+
+@pytest.mark.parametrize("mode", [torch.no_grad, torch.inference_mode])
+@pytest.mark.parametrize("L", [1, 40])
+def test_without_gradients_no_checkpoint_is_made(calls, mode, L):
+    """The scan of a call without one goes token by token where the tokens are few, and writes no states for a backward where they are many."""
+    layer = S.SelectLayer(12, 8, 4)
+    x = torch.randn(2, L, 12)
+    ckpt = lambda: [a[13] for name, a in calls if name == "cawn_selective_scan_fwd"]  # noqa: E731
+    with mode():
+        layer(x, torch.zeros_like(x))
+    assert ckpt() == [None]
+    layer(x, torch.zeros_like(x))
+    assert ckpt()[1] is not None
+    for p in layer.parameters():
+        p.requires_grad_(False)
+    layer(x, torch.zeros_like(x))
+    assert ckpt()[2] is None
