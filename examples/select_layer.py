@@ -118,9 +118,9 @@ class SelectiveScan(torch.autograd.Function):
         lengths = None if lengths is None else lengths.contiguous()
         d = K.make_scan_desc(B, L, D, N, G=G, dt_softplus=1, bf16=int(x.dtype == torch.bfloat16))
         ckpt = _scratch(K.cawn_selective_scan_ckpt_bytes(d), x.device) if grad and any(ctx.needs_input_grad) else None
+        size = K.cawn_selective_scan_serve_workspace_bytes if ckpt is None else K.cawn_selective_scan_workspace_bytes
         y, out = torch.empty_like(x), torch.empty_like(state)
-        K.check(K.cawn_selective_scan_fwd(d, x, dt, A, Bm, Cm, skip, z, dt_bias, lengths, state, y, out, ckpt,
-                                          _scratch(K.cawn_selective_scan_workspace_bytes(d), x.device)))
+        K.check(K.cawn_selective_scan_fwd(d, x, dt, A, Bm, Cm, skip, z, dt_bias, lengths, state, y, out, ckpt, _scratch(size(d), x.device)))
         ctx.d, ctx.ckpt = d, ckpt
         ctx.save_for_backward(x, dt, A, Bm, Cm, skip, z, dt_bias, lengths)
         return y, out

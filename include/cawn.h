@@ -517,12 +517,14 @@ typedef struct cawn_scan_desc {
     int64_t y_stride_b, y_stride_t;     /*   of y, dy [B][L][D].  Values of one token lie side by side               */
 } cawn_scan_desc;
 
-/* The state [B][D][N] fp32 (its gradient alike).  0 for an invalid descriptor, as the two below. */
+/* The state [B][D][N] fp32 (its gradient alike).  0 for an invalid descriptor, as the three below. */
 size_t cawn_selective_scan_state_bytes(const cawn_scan_desc *d);
 /* What the forward leaves for the backward: the states before every run of 16 tokens, Bm and Cm in fp32. */
 size_t cawn_selective_scan_ckpt_bytes(const cawn_scan_desc *d);
 /* Scratch of either direction, 256-byte aligned. */
 size_t cawn_selective_scan_workspace_bytes(const cawn_scan_desc *d);
+/* ... of a forward without ckpt alone, which has none of the backward's partial sums: what a program that only serves has to keep. */
+size_t cawn_selective_scan_serve_workspace_bytes(const cawn_scan_desc *d);
 
 /*
  * Forward: prefill, training, and single tokens (L = 1: one pass over the state).
@@ -532,7 +534,8 @@ size_t cawn_selective_scan_workspace_bytes(const cawn_scan_desc *d);
  *       and the state is that behind the last token.  0: an unused slot, whose state is passed through
  *   state_in   or NULL (zeros); state_out or NULL; they may be the same
  *   ckpt       cawn_selective_scan_ckpt_bytes(), 16-byte aligned, or NULL when no backward will follow
- *   workspace  >= cawn_selective_scan_workspace_bytes(d); calls of up to 16 tokens without ckpt use none
+ *   workspace  >= cawn_selective_scan_workspace_bytes(d), without ckpt cawn_selective_scan_serve_workspace_bytes(d); calls of up to 16 tokens without
+ *       ckpt use none
  * Inputs must not alias outputs (but for the state).  A value that is not finite reaches the tokens behind it, as the formula has it; one that
  * the formula makes infinite may be NaN.
  */

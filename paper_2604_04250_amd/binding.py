@@ -28,7 +28,7 @@ EXPORTS = ["cawn_state_bytes", "cawn_workspace_bytes", "cawn_ckpt_bytes", "cawn_
            "cawn_delta_rule_bwd", "cawn_group_norm_workspace_bytes", "cawn_group_norm_fwd", "cawn_group_norm_bwd",
            "cawn_dropout_add_fwd", "cawn_dropout_add_bwd",
            "cawn_selective_scan_state_bytes", "cawn_selective_scan_ckpt_bytes", "cawn_selective_scan_workspace_bytes",
-           "cawn_selective_scan_fwd", "cawn_selective_scan_bwd", "cawn_causal_conv_state_bytes", "cawn_causal_conv_workspace_bytes",
+           "cawn_selective_scan_serve_workspace_bytes", "cawn_selective_scan_fwd", "cawn_selective_scan_bwd", "cawn_causal_conv_state_bytes", "cawn_causal_conv_workspace_bytes",
            "cawn_causal_conv_fwd", "cawn_causal_conv_bwd", "cawn_rms_norm_add_workspace_bytes", "cawn_rms_norm_add_fwd",
            "cawn_rms_norm_add_bwd"]
 
@@ -177,7 +177,8 @@ def lib() -> C.CDLL:
         for n, ty in (("cawn_delta_state_bytes", cawn_delta_desc), ("cawn_delta_ckpt_bytes", cawn_delta_desc),
                       ("cawn_delta_workspace_bytes", cawn_delta_desc), ("cawn_group_norm_workspace_bytes", cawn_norm_desc),
                       ("cawn_selective_scan_state_bytes", cawn_scan_desc), ("cawn_selective_scan_ckpt_bytes", cawn_scan_desc),
-                      ("cawn_selective_scan_workspace_bytes", cawn_scan_desc), ("cawn_causal_conv_state_bytes", cawn_conv_desc),
+                      ("cawn_selective_scan_workspace_bytes", cawn_scan_desc), ("cawn_selective_scan_serve_workspace_bytes", cawn_scan_desc),
+                      ("cawn_causal_conv_state_bytes", cawn_conv_desc),
                       ("cawn_causal_conv_workspace_bytes", cawn_conv_desc), ("cawn_rms_norm_add_workspace_bytes", cawn_rms_desc)):
             getattr(L, n).restype = C.c_size_t
             getattr(L, n).argtypes = [C.POINTER(ty)]
@@ -444,6 +445,11 @@ def cawn_selective_scan_ckpt_bytes(d: cawn_scan_desc) -> int:
 
 def cawn_selective_scan_workspace_bytes(d: cawn_scan_desc) -> int:
     return int(lib().cawn_selective_scan_workspace_bytes(C.byref(d)))
+
+
+def cawn_selective_scan_serve_workspace_bytes(d: cawn_scan_desc) -> int:
+    """Of a forward without a checkpoint."""
+    return int(lib().cawn_selective_scan_serve_workspace_bytes(C.byref(d)))
 
 
 def cawn_selective_scan_fwd(d, x, dt, A, Bm, Cm, Dskip, z, dt_bias, lengths, state_in, y, state_out, ckpt, workspace, stream=None) -> int:

@@ -132,6 +132,14 @@ size_t cawn_selective_scan_workspace_bytes(const cawn_scan_desc *d)
     return bytes > 256 ? bytes : 256;
 }
 
+size_t cawn_selective_scan_serve_workspace_bytes(const cawn_scan_desc *d)
+{
+    Args a;
+    if (check(d, false, &a) != CAWN_OK || (!by_token(a) && !tiles_fit(a))) return 0;
+    const size_t bytes = by_token(a) ? 0 : layout_of(a, a).fwd;
+    return bytes > 256 ? bytes : 256;
+}
+
 int cawn_selective_scan_fwd(const cawn_scan_desc *d, const void *x, const void *dt, const float *A, const void *Bm, const void *Cm, const float *Dskip, const void *z,
                             const float *dt_bias, const int32_t *lengths, const void *state_in, void *y, void *state_out, void *ckpt, void *workspace,
                             size_t workspace_bytes, void *stream)

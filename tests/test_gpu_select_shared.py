@@ -93,3 +93,19 @@ def test_parameter_gradients_of_long_rows_in_one_segment():
     torch.autograd.backward([y, S], [torch.from_numpy(np.asarray(i[n], np.float64)).cuda() for n in ("dy", "dstate_out")])
     names = dict(dx="x", ddt="dt", dA="A", dBm="Bm", dCm="Cm", dDskip="Dk", dz="z", ddt_bias="bias", dstate_in="state_in")
     _compare_norms(s, L, y.detach().cpu(), S.detach().cpu(), {g: v[n].grad.cpu() for g, n in names.items()}, False)
+
+
+@pytest.mark.parametrize("B,L,D,N,G", [(2, 1500, 70, 16, 1), (3, 100, 130, 64, 2), (64, 40, 1024, 8, 1), (2, 16, 70, 16, 1), (2, 1, 70, 128, 1)])
+def test_a_forward_in_the_scratch_of_serving(B, L, D, N, G):
+    """The same bits as in the larger one, and nothing written behind it."""
+    from paper_2604_04250_amd import binding as K
+    i = scan_inputs(B, L, D, N, G, True, seed=L, ragged=True)
+    a, b = (Scan(i, True, ckpt=False) for _ in range(2))
+    n = K.cawn_selective_scan_serve_workspace_bytes(b.d)
+    guarded = torch.full((n + 4096,), 0xa5, dtype=torch.uint8, device="cuda")
+    b.ws = guarded[:n]
+    a.forward()
+    b.forward()
+    torch.cuda.synchronize()
+    assert torch.equal(a.y, b.y) and torch.equal(a.state_out, b.state_out)
+    assert bool((guarded[n:] == 0xa5).all())
