@@ -33,11 +33,11 @@ void cut(Args *a, bool bwd)
     a->segments = (int)ceil_div(a->tiles, a->seg_tiles);
 }
 
-// More bytes than are counted.
-bool too_many(const Args &a) { return (double)a.B * (a.tiles + 1.) * a.Dp * (a.NP * a.NB) > 1e17; }
+// More bytes than are counted, or more tiles of B and C.
+bool too_many(const Args &a) { return (double)a.B * (a.tiles + 1.) * a.Dp * (a.NP * a.NB) > 1e17 || (double)a.B * a.tiles * a.G > 0x7fffffff; }
 
 // The passes of the tiled form, whose workgroups take a segment of columns each, and the launch of the other form.  (The chain has links only where the columns are
-// few, and the other launches go round.)
+// few, and the other launches go round or are several.)
 bool tiles_fit(const Args &a) { return launchable((double)a.B * a.segments * a.G * a.cbg, 64 * (a.NB > 1 ? a.NB : a.wide)); }
 bool by_token(const Args &a) { return a.L <= select::TOKEN_MAX; }
 bool tokens_fit(const Args &a) { return launchable((double)ceil_div((long long)a.B * a.D * select::token_lanes(a), 256), 256); }

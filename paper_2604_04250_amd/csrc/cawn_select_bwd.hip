@@ -423,49 +423,53 @@ template <typename T, int NP, int NB> __global__ __launch_bounds__(NB > 1 ? 64 *
     if (p.on && a.dstate_in && p.seg == 0) store_user<NP>(a.dstate_in, a, user, p.blk * NP, h);
 }
 
-// What the workgroups left, in their order: the first `bc` workgroups dB and dC, four states a thread, the others the parameters' gradients.  Beyond BC_BLOCKS
-// the former go round.
+// What the workgroups left, in their order: the first `bc` workgroups dB and dC, four states a thread, from workgroup `from` of these sums on; the others the
+// parameters' gradients.  (A launch counts its threads in 32 bits.  Workgroups that go round take 65 registers for 46 and are one a CU: 6.6 us for 5.0 in a call of
+// few rows, 16.2 for 14.8 at 8 x 8,192 tokens; what is beyond BC_BLOCKS is a launch more.)
 constexpr long long BC_BLOCKS = 1 << 12;
 
-template <typename T> __global__ __launch_bounds__(1024) void select_bc_sums(const Args a, const unsigned bc, const ParamSums sums, const int accumulate)
+template <typename T> __global__ __launch_bounds__(1024) void select_bc_sums(const Args a, const long long from, const unsigned bc, const ParamSums sums, const int accumulate)
 {
     const int NPT = a.NP * a.NB, per = 2 * NPT;
     if (blockIdx.x >= bc) {
-        sum_columns(blockIdx.x - bc, gridDim.x - bc, a.part_a, (long long)a.B * a.segments, (long long)a.Dp * (NPT + 2), sums, accumulate);
+        sum_columns(blockIdx.x - bc, a.part_a, (long long)a.B * a.segments, (long long)a.Dp * (NPT + 2), sums, accumulate);
         return;
     }
-    const long long all = (long long)a.B * a.L * a.G * (per / 4);
-    for (long long id = (long long)blockIdx.x * 1024 + threadIdx.x; id < all; id += (long long)bc * 1024) {
-        const int at = (int)(id % (per / 4)) * 4, which = at / NPT, n = at % NPT;
-        const long long rest = id / (per / 4), g = rest % a.G, bt = rest / a.G, b = bt / a.L, t = bt - b * a.L;
-        T *out = (T *)(which ? a.dC : a.dB);
-        if (n >= a.N || !out) continue;
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        if (t < row_length(a, (int)b)) {
-            const float *p = a.part_bc + (((b * a.tiles * TILE + t) * a.G + g) * a.parts) * per + at;
-            for (int k = 0; k < a.parts; ++k) v += *reinterpret_cast<const f32x4 *>(p + (long long)k * per);
-        }
-        out += b * a.bsb + t * a.bst + g * a.N + n;
-        if (n + 4 <= a.N && ((uintptr_t)out & (4 * sizeof(T) - 1)) == 0) {
-            const float x[4] = {v[0], v[1], v[2], v[3]};
-            store_n<T, 4>(out, x);
-        } else {
+    const long long id = (from + blockIdx.x) * 1024 + threadIdx.x;
+    const int at = (int)(id % (per / 4)) * 4, which = at / NPT, n = at % NPT;
+    const long long rest = id / (per / 4), g = rest % a.G, bt = rest / a.G, b = bt / a.L, t = bt - b * a.L;
+    if (b >= a.B || n >= a.N) return;
+    T *out = (T *)(which ? a.dC : a.dB);
+    if (!out) return;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (t < row_length(a, (int)b)) {
+        const float *p = a.part_bc + (((b * a.tiles * TILE + t) * a.G + g) * a.parts) * per + at;
+        for (int k = 0; k < a.parts; ++k) v += *reinterpret_cast<const f32x4 *>(p + (long long)k * per);
+    }
+    out += b * a.bsb + t * a.bst + g * a.N + n;
+    if (n + 4 <= a.N && ((uintptr_t)out & (4 * sizeof(T) - 1)) == 0) {
+        const float x[4] = {v[0], v[1], v[2], v[3]};
+        store_n<T, 4>(out, x);
+    } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (n + j < a.N) out[j] = (T)v[j];
-        }
+        for (int j = 0; j < 4; ++j)
+            if (n + j < a.N) out[j] = (T)v[j];
     }
 }
 
 int launch_bc_sums(const Args &a, bool bf16_, const ParamSums &sums, int accumulate, hipStream_t s)
 {
     const int NPT = a.NP * a.NB;
-    const long long want = ceil_div((long long)a.B * a.L * a.G * 2 * NPT / 4, 1024);
-    const unsigned bc = a.part_bc ? (unsigned)(want < BC_BLOCKS ? want : BC_BLOCKS) : 0;
-    const unsigned pa = a.part_a ? sum_blocks((long long)a.Dp * (NPT + 2)) : 0;
-    if (bc + pa == 0) return CAWN_OK;
-    if (bf16_) hipLaunchKernelGGL(select_bc_sums<bf16>, dim3(bc + pa), dim3(1024), 0, s, a, bc, sums, accumulate);
-    else hipLaunchKernelGGL(select_bc_sums<float>, dim3(bc + pa), dim3(1024), 0, s, a, bc, sums, accumulate);
+    const long long cols = (long long)a.Dp * (NPT + 2), columns = ceil_div(cols, SUM_COLS);
+    const bool apart = a.part_a && columns > SUM_BLOCKS;            // (a launch of their own goes round)
+    if (apart) launch_sums(a.part_a, (long long)a.B * a.segments, cols, sums, accumulate, s);
+    unsigned pa = a.part_a && !apart ? (unsigned)columns : 0;
+    const long long all = a.part_bc ? ceil_div((long long)a.B * a.L * a.G * 2 * NPT / 4, 1024) : 0;
+    for (long long from = 0; from < all || pa > 0; from += BC_BLOCKS, pa = 0) {
+        const unsigned bc = (unsigned)(all - from < BC_BLOCKS ? all - from : BC_BLOCKS);
+        if (bf16_) hipLaunchKernelGGL(select_bc_sums<bf16>, dim3(bc + pa), dim3(1024), 0, s, a, from, bc, sums, accumulate);
+        else hipLaunchKernelGGL(select_bc_sums<float>, dim3(bc + pa), dim3(1024), 0, s, a, from, bc, sums, accumulate);
+    }
     return launched();
 }
 

@@ -20,16 +20,17 @@ template <typename T> __global__ __launch_bounds__(256) void select_prepare(cons
 {
     __shared__ float sh[2][TILE][N_MAX + 1];
     const int npt = a.NP * a.NB;
-    for (long long at = blockIdx.x, all = (long long)a.B * a.tiles * a.G; at < all; at += gridDim.x) {
+    for (unsigned at = blockIdx.x, all = (unsigned)a.B * a.tiles * a.G; at < all; at += gridDim.x) {
         if (at != blockIdx.x) __syncthreads();      // (the tile before has been written)
-        const long long bt = at / a.G, b = bt / a.tiles, t = (bt - b * a.tiles) * TILE;
-        const int g = (int)(at - bt * a.G), left = row_length(a, (int)b) - (int)t;
+        const unsigned bt = at / (unsigned)a.G, row = bt / (unsigned)a.tiles;
+        const long long b = row, t = (long long)(bt - row * a.tiles) * TILE;
+        const int g = (int)(at - bt * a.G), left = row_length(a, (int)row) - (int)t;
         for (int i = threadIdx.x; i < 2 * TILE * npt; i += 256) {
             const int n = i % npt, tt = i / npt % TILE, which = i / npt / TILE;
             sh[which][tt][n] = n < a.N && tt < left ? (float)((const T *)(which ? a.Cm : a.Bm))[b * a.bsb + (t + tt) * a.bst + (long long)g * a.N + n] : 0.f;
         }
         __syncthreads();
-        float *out = a.bc + at * npt * 2 * TILE;
+        float *out = a.bc + (long long)at * npt * 2 * TILE;
         for (int i = threadIdx.x; i < 2 * TILE * npt; i += 256) out[i] = sh[i / TILE % 2][i % TILE][i / TILE / 2];
     }
 }

@@ -25,50 +25,48 @@ template <int THREADS, int N> __device__ inline void over_runs(float (&v)[N], in
 }
 
 constexpr int SUM_COLS = 32, SUM_RUNS = 32;
-constexpr long long SUM_BLOCKS = 1 << 14;       // workgroups at most (a launch counts its threads in 32 bits): what is beyond goes to the first again
+constexpr long long SUM_BLOCKS = 1 << 14;       // workgroups at most (a launch counts its threads in 32 bits), which go round
 
-inline unsigned sum_blocks(long long cols) { return (unsigned)(ceil_div(cols, SUM_COLS) < SUM_BLOCKS ? ceil_div(cols, SUM_COLS) : SUM_BLOCKS); }
-
-// Workgroup `block` of `blocks`; out(c) gives the place of column c's sum, or null.  A workgroup takes 32 columns; its 32 runs of threads take every 32nd row, and are
+// out(c) gives the place of column c's sum, or null.  A workgroup takes 32 columns; its 32 runs of threads take every 32nd row, and are
 // added up in their order.  (With 16 and 8 columns a workgroup the backward passes that end in it are up to 6 and 17 % slower.)
-template <typename Out> __device__ inline void sum_columns(const long long block, const long long blocks, const float *part, const long long rows, const long long cols,
-                                                           const Out &out, const int accumulate)
+template <typename Out> __device__ inline void sum_columns(const long long block, const float *part, const long long rows, const long long cols, const Out &out, const int accumulate)
 {
     __shared__ float sh[SUM_RUNS][SUM_COLS + 1];
     const int col = threadIdx.x % SUM_COLS, run = threadIdx.x / SUM_COLS;
-    for (long long first = block * SUM_COLS; first < cols; first += blocks * SUM_COLS) {
-        const long long c = first + col;
-        float v = 0.f;
-        if (c < cols) {
-            const float *p = part + c;
-            long long r = run;
-            for (; r + 3 * SUM_RUNS < rows; r += 4 * SUM_RUNS) {
-                const float x0 = p[r * cols], x1 = p[(r + SUM_RUNS) * cols], x2 = p[(r + 2 * SUM_RUNS) * cols], x3 = p[(r + 3 * SUM_RUNS) * cols];
-                v += (x0 + x1) + (x2 + x3);
-            }
-            for (; r < rows; r += SUM_RUNS) v += p[r * cols];
+    const long long c = block * SUM_COLS + col;
+    float v = 0.f;
+    if (c < cols) {
+        const float *p = part + c;
+        long long r = run;
+        for (; r + 3 * SUM_RUNS < rows; r += 4 * SUM_RUNS) {
+            const float x0 = p[r * cols], x1 = p[(r + SUM_RUNS) * cols], x2 = p[(r + 2 * SUM_RUNS) * cols], x3 = p[(r + 3 * SUM_RUNS) * cols];
+            v += (x0 + x1) + (x2 + x3);
         }
-        if (first != block * SUM_COLS) __syncthreads();         // (the columns before have been added up)
-        sh[run][col] = v;
-        __syncthreads();
-        if (run == 0 && c < cols) {
-            float s = 0.f;
-            for (int q = 0; q < SUM_RUNS; ++q) s += sh[q][col];
-            float *at = out(c);
-            if (at) *at = accumulate ? *at + s : s;
-        }
+        for (; r < rows; r += SUM_RUNS) v += p[r * cols];
+    }
+    sh[run][col] = v;
+    __syncthreads();
+    if (run == 0 && c < cols) {
+        float s = 0.f;
+        for (int q = 0; q < SUM_RUNS; ++q) s += sh[q][col];
+        float *at = out(c);
+        if (at) *at = accumulate ? *at + s : s;
     }
 }
 
 template <typename Out> __global__ __launch_bounds__(SUM_COLS *SUM_RUNS) void column_sums(const float *part, const long long rows, const long long cols, const Out out,
                                                                                          const int accumulate)
 {
-    sum_columns(blockIdx.x, gridDim.x, part, rows, cols, out, accumulate);
+    for (long long block = blockIdx.x; block * SUM_COLS < cols; block += gridDim.x) {
+        if (block != blockIdx.x) __syncthreads();           // (the columns before have been added up)
+        sum_columns(block, part, rows, cols, out, accumulate);
+    }
 }
 
 template <typename Out> void launch_sums(const float *part, long long rows, long long cols, const Out &out, int accumulate, hipStream_t s)
 {
-    if (cols > 0) hipLaunchKernelGGL((column_sums<Out>), dim3(sum_blocks(cols)), dim3(SUM_COLS * SUM_RUNS), 0, s, part, rows, cols, out, accumulate);
+    const long long blocks = ceil_div(cols, SUM_COLS) < SUM_BLOCKS ? ceil_div(cols, SUM_COLS) : SUM_BLOCKS;
+    if (cols > 0) hipLaunchKernelGGL((column_sums<Out>), dim3((unsigned)blocks), dim3(SUM_COLS * SUM_RUNS), 0, s, part, rows, cols, out, accumulate);
 }
 
 } // namespace ops
