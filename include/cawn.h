@@ -537,7 +537,8 @@ size_t cawn_selective_scan_serve_workspace_bytes(const cawn_scan_desc *d);
  *   workspace  >= cawn_selective_scan_workspace_bytes(d), without ckpt cawn_selective_scan_serve_workspace_bytes(d); calls of up to 16 tokens without
  *       ckpt use none
  * Inputs must not alias outputs (but for the state).  A value that is not finite reaches the tokens behind it, as the formula has it; one that
- * the formula makes infinite may be NaN.
+ * the formula makes infinite may be NaN.  Where delta A is above 0 (states grow) e to its sum over the row's tokens has to be finite in fp32:
+ * rows are cut, and a part's factors are taken as one.
  */
 int cawn_selective_scan_fwd(const cawn_scan_desc *d, const void *x, const void *dt, const float *A, const void *Bm, const void *Cm,
                             const float *Dskip, const void *z, const float *dt_bias, const int32_t *lengths, const void *state_in,
@@ -595,6 +596,7 @@ int cawn_causal_conv_bwd(const cawn_conv_desc *d, const void *x, const float *w,
  * and, on request, y in 8 bits for a product in 8 bits:
  *     scales[r][j] = max |y| / 448 over the j-th `block` channels of the row;  q = y / scale rounded to OCP e4m3 (y is not rounded before)
  * A block of zeros (or of values below 448 x 2^-126) has the scale 0 and zeros; one that holds a NaN has a NaN for its scale.
+ * The sum of a row's squares is fp32: beyond its range (values of some 1e17 and more) rstd is 0, and squares below 2^-149 count as 0.
  */
 typedef struct cawn_rms_desc {
     int64_t rows;                       /* 0 allowed (nothing is read or written but dweight, which is 0 then)                          */

@@ -4,7 +4,7 @@
 // Backward: dz = dy act'(z) with z made again, dx[t] = sum_i w[k-1-i] dz[t+i], dw[i] = sum_t dz[t] x[t-(k-1)+i], db = sum_t dz[t].
 //
 // A thread takes four adjacent channels along a run of tokens; the k - 1 inputs before the run's first token are read again, and backward the k - 1 tokens behind
-// its last.  Bound by memory: 8 x 8,192 tokens of 768 channels in bf16 forward 39 us (5.2 TB/s), backward 73 (4.1: also what it computes, z and two products a
+// its last.  Bound by memory: 8 x 8,192 tokens of 768 channels in bf16 forward 38 us (5.2 TB/s), backward 70 (4.3: also what it computes, z and two products a
 // tap, two thirds of the issue slots), the sums of dw 5.  A step of 128 rows of 4,096 channels 5.6.  (Two channels a thread, both directions: 119 us, eight 151.)
 // The row's state (the k - 1 inputs before its first token, in fp32) is read and replaced by the thread of the row's first run alone.
 #include "cawn_rows.hpp"

@@ -5,7 +5,8 @@
 //
 // A row is in registers from its one read to its write: a run of 4 to 64 lanes holds it, or a workgroup of 256 to 1,024; the longest, beyond 16,384 channels, are
 // read again.  Bound by memory: 65,536 rows of 768 channels in bf16 with an fp32 residual forward 115 us (5.2 TB/s), backward 155 (5.2); 32,768 rows of 4,096 with
-// 8 bits and a scale for 128 channels 172 (5.5).  A few rows are a launch: 4 of 768 4.6.
+// 8 bits and a scale for 128 channels 172 (5.5).  Wide rows of an odd width begin between the 16 bytes of an access: 4,096 rows of 12,001 channels in bf16 forward 114,
+// backward 160 (3.4, 3.1), of 12,000 84 and 111.  A few rows are a launch: 4 of 768 4.6.
 // The sum of squares is plain: all of its terms have one sign.
 #include "cawn_rows.hpp"
 #include "cawn_sums.hpp"

@@ -8,8 +8,8 @@
 // with what reaches their end.  A tile's states are made again from those kept before it, two states of a channel at a time for its 16 tokens, which then
 // stay in registers for the way back.  The sums over channels go through a tree of lanes that halves the values as it halves the lanes (64 values in 129
 // instructions, one by one they would take 384); a workgroup adds up its waves, and what the workgroups leave is added in their order.
-// Bound by instruction issue: 8 x 8,192 tokens of 768 channels of 16 states in bf16 163 us for what segments hand on, 562 for the gradients (341 instructions a
-// token of a wave, vector units busy for 89 % of the time), the chain 12, the sums 15.
+// Bound by instruction issue: 8 x 8,192 tokens of 768 channels of 16 states in bf16 163 us for what segments hand on, 567 for the gradients (341 instructions a
+// token of a wave, vector units busy for 88 % of the time), the chain 13, the sums 14.
 #include "cawn_select.hpp"
 
 namespace cawn {

@@ -5,7 +5,7 @@
 // exponential and update twice, so that a few rows of many channels fill the chip; one segment does without it and the chain.
 // What bounds it: instruction issue.  A token's state costs a product, an exponential (two issue slots), a product and two sums (without y one), 24 (20) cycles
 // of a SIMD a wave, and a token 27 (15) instructions more for softplus, the gate, conversions and memory.  2 x 32,768 tokens of 4,096 channels of 16 states in
-// bf16: 705 us without y, 909 with it, vector units busy for 97 and 98 % of both; the chain 19, B and C 9.
+// bf16: 703 us without y, 904 with it, vector units busy for 99 % of both; the chain 18, B and C 9.
 // Runs of eight tokens: with 16 the registers of two more waves a SIMD are gone (the same call 1,673 us for 1,579).
 #include "cawn_select.hpp"
 
